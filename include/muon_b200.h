@@ -384,6 +384,121 @@ int muon_orthogonalize_static(const void* in, void* out, int32_t rows, int32_t c
                               int32_t ns_steps, const float* coeffs, float eps, uint32_t flags,
                               int32_t* status, void* stream);
 
+/* ------------------------------------------------------------------ the layer around the matrices
+ * What a training program needs next to the matrices that the step updates, to turn tokens into the gradients it
+ * consumes: layer norm, rotary positions and attention, each forward and backward.  These calls use a context only for
+ * its device, its status word and its launch count; they neither use nor need the workspace of muon_set_workspace, and
+ * the scratch some of them take is an argument (256-byte aligned, caller-owned, contents undefined before and after).
+ * Every result is bit-identical from run to run: no float atomics.  Statistics, sums and accumulators are fp32. */
+
+/* Layer norm over the last dimension of `rows` rows of `cols` elements (1 <= cols <= 16384), in `dtype`; weight, bias and
+ * their gradients have `param_dtype`.
+ *   center = 1:  y = (x - mean) rstd * weight + bias,  rstd = 1 / sqrt(mean((x - mean)^2) + eps)
+ *   center = 0:  y = x rstd * weight + bias,           rstd = 1 / sqrt(mean(x^2) + eps)            (RMS norm)      */
+typedef struct {
+  int32_t dtype, param_dtype;
+  int32_t center;
+  int32_t cols;
+  int64_t rows;
+  float   eps;
+  int32_t reserved;              /* must be 0 */
+} muon_norm_desc_t;
+
+/* x, y: row r starts ldx / ldy elements after row r-1 (>= cols); y may be x itself (with ldy == ldx).  weight, bias: [cols] or
+ * NULL (1 and 0).  mean [rows] (center = 1 only; NULL otherwise) and rstd [rows] are fp32 and are what the backward pass reads. */
+int muon_layer_norm_forward(muon_ctx_t* ctx, const muon_norm_desc_t* desc, const void* x, int64_t ldx, const void* weight,
+                            const void* bias, void* y, int64_t ldy, float* mean, float* rstd, void* stream);
+
+/* Bytes of scratch of muon_layer_norm_backward (partial sums of dweight and dbias).  Host arithmetic only. */
+int muon_layer_norm_workspace_bytes(const muon_norm_desc_t* desc, size_t* bytes);
+
+/* With g = dy * weight and xh = (x - mean) rstd:
+ *   dx = rstd (g - mean(g) - xh mean(g xh))  (mean(g) only with center = 1),  dweight = sum_rows dy xh,  dbias = sum_rows dy
+ * dx may be dy itself or x itself (with equal strides).  dweight, dbias: [cols] in param_dtype, or NULL when not wanted. */
+int muon_layer_norm_backward(muon_ctx_t* ctx, const muon_norm_desc_t* desc, const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                             const void* weight, const float* mean, const float* rstd, void* dx, int64_t lddx, void* dweight,
+                             void* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* A [batch, tokens, heads, head_dim] tensor of any strides (in elements) whose last dimension is contiguous: a view into a
+ * fused projection's output, or a tensor stored head by head.  The tensors a call reads are not written. */
+typedef struct {
+  void*   data;
+  int64_t batch_stride, token_stride, head_stride;
+} muon_heads_t;
+
+/* Rotary positions: pair i of the first rotary_dim elements of every head is turned by the angle position * inv_freq[i]
+ * (by its negative when inverse = 1, which is the backward pass) and multiplied by amplitude; the rest of the head is copied.
+ *   interleaved = 0: pair i is elements (i, i + rotary_dim/2);  1: elements (2i, 2i+1)
+ * Angles are reduced in double, so a position of any size keeps the precision of fp32. */
+typedef struct {
+  int32_t dtype, interleaved, inverse;
+  int32_t head_dim, rotary_dim;  /* rotary_dim even, 2 <= rotary_dim <= min(head_dim, 512) */
+  int32_t batch, tokens;
+  float   amplitude;             /* 1, or the factor some scalings of long contexts put on the queries and keys */
+  const double*  inv_freq;       /* host, [rotary_dim / 2], radians per position */
+  const int32_t* positions;      /* device, [batch][tokens], or NULL: position_offset + token index */
+  int64_t position_offset;       /* added to every position */
+} muon_rotary_desc_t;
+
+typedef struct {
+  muon_heads_t in, out;          /* out may be in itself (same strides): rotated in place */
+  int32_t heads, reserved;       /* reserved must be 0 */
+} muon_rotary_item_t;
+
+/* Rotates up to 4 tensors that share positions (queries and keys) in one launch. */
+int muon_rotary(muon_ctx_t* ctx, const muon_rotary_desc_t* desc, const muon_rotary_item_t* items, int32_t count, void* stream);
+
+/* Host-only: inv_freq[i] = base^(-2i / rotary_dim) for i < rotary_dim/2, stretched for long contexts:
+ *   MUON_ROTARY_LINEAR     f / factor
+ *   MUON_ROTARY_BY_PARTS   with t = original_length f / 2 pi turns within the context trained on and k = clamp((t - low) /
+ *                          (high - low), 0, 1):  k f + (1 - k) f / factor   (fast pairs keep their frequency, slow ones are stretched)
+ * factor, original_length, low < high are read by the scalings that name them. */
+#define MUON_ROTARY_PLAIN    0
+#define MUON_ROTARY_LINEAR   1
+#define MUON_ROTARY_BY_PARTS 2
+int muon_rotary_frequencies(double base, int32_t rotary_dim, int32_t scaling, double factor, double original_length, double low,
+                            double high, double* inv_freq);
+
+/* Attention of q_heads query heads over kv_heads key heads (query head h reads key head h / (q_heads / kv_heads)):
+ *   S = scale q k^T where the mask lets query i see key j,  lse = log sum_j exp(S),  o = sum_j exp(S - lse) v_j
+ * Sequences come in one of two forms.
+ *   batched: row b of the batch is one sequence of q_tokens queries and k_tokens keys, of which only the first q_lens[b] and
+ *            k_lens[b] count when those are given (device, [batch]; values outside [0, tokens] are clamped)
+ *   packed:  batch = 1 and q_offsets, k_offsets (device, [num_seqs + 1], non-decreasing, from 0) cut the q_tokens and k_tokens
+ *            tokens into sequences; tokens after the last offset belong to none
+ * With nq queries and nk keys of a sequence, query i sees key j < nk when i < nq and, with causal = 1, j <= i + nk - nq, and, with
+ * window > 0 (causal only), also j > i + nk - nq - window.  A query that sees nothing has o = 0 and lse = -inf, takes and gives no
+ * gradient; so have tokens that do not count.  What such tokens hold (NaN, infinities) reaches no result of another token. */
+typedef struct {
+  int32_t dtype;                 /* MUON_DTYPE_BF16: tensor cores when every pointer is 16-byte aligned, head_dim is a multiple of 8 up  */
+                                 /* to 128 and every stride is a multiple of 8; otherwise, and for MUON_DTYPE_FP32, CUDA cores         */
+  int32_t batch, q_tokens, k_tokens;
+  int32_t q_heads, kv_heads, head_dim;   /* q_heads a multiple of kv_heads; head_dim <= 256 */
+  int32_t causal, window;
+  float   scale;                 /* > 0 */
+  int32_t num_seqs;              /* packed form: sequences; else 0 */
+  int32_t reserved;              /* must be 0 */
+  const int32_t* q_lens;
+  const int32_t* k_lens;
+  const int32_t* q_offsets;
+  const int32_t* k_offsets;
+} muon_attention_desc_t;
+
+/* lse: fp32 [batch][q_heads][q_tokens], contiguous. */
+int muon_attention_forward(muon_ctx_t* ctx, const muon_attention_desc_t* desc, const muon_heads_t* q, const muon_heads_t* k,
+                           const muon_heads_t* v, const muon_heads_t* o, float* lse, void* stream);
+
+/* Bytes of scratch of muon_attention_backward.  Host arithmetic only. */
+int muon_attention_workspace_bytes(const muon_attention_desc_t* desc, size_t* bytes);
+
+/* With P = exp(S - lse) formed anew from q, k and lse:  delta = sum_d do o,  dv = P^T do,  dS = P (do v^T - delta),
+ *   dq = scale dS k,  dk = scale dS^T q;  dk and dv are sums over the query heads that share a key head.
+ * o and lse are what the forward pass gave.  dq, dk, dv may not alias an input. */
+int muon_attention_backward(muon_ctx_t* ctx, const muon_attention_desc_t* desc, const muon_heads_t* dout, const muon_heads_t* q,
+                            const muon_heads_t* k, const muon_heads_t* v, const muon_heads_t* o, const float* lse,
+                            const muon_heads_t* dq, const muon_heads_t* dk, const muon_heads_t* dv, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
 /* Device-side status word: the tensor-core pipeline bounds every wait on a barrier; a wait
  * that gives up records a non-zero code here and the kernel exits cleanly.  Reads the word
  * after synchronising `stream`; 0 = no bounded wait ever expired on this context. */

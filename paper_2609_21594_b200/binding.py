@@ -29,6 +29,7 @@ NS_BF16, NS_FP32 = 0, 1
 ENGINE_TENSOR, ENGINE_CUDA_CORE, ENGINE_TENSOR_1CTA = 0, 1, 2
 ORTHO_NO_NORMALIZE = 1
 PHASE_MOMENTUM, PHASE_NS, PHASE_UPDATE, PHASE_GATHER, PHASE_SCATTER = range(5)
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BY_PARTS = 0, 1, 2
 PHASE_NAMES = ("momentum", "ns", "update", "gather", "scatter")
 
 
@@ -55,6 +56,32 @@ class Options(C.Structure):
     _fields_ = [("grad_dtype", C.c_int32), ("ns_precision", C.c_int32), ("nesterov", C.c_int32),
                 ("coeffs_per_step", C.c_int32), ("eps", C.c_float), ("engine", C.c_int32),
                 ("chunk_elems", C.c_int64), ("coeffs_per_matrix", C.c_int32), ("launch_per_product", C.c_int32)]
+
+
+class NormDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("param_dtype", C.c_int32), ("center", C.c_int32), ("cols", C.c_int32), ("rows", C.c_int64),
+                ("eps", C.c_float), ("reserved", C.c_int32)]
+
+
+class Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class RotaryDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("interleaved", C.c_int32), ("inverse", C.c_int32), ("head_dim", C.c_int32),
+                ("rotary_dim", C.c_int32), ("batch", C.c_int32), ("tokens", C.c_int32), ("amplitude", C.c_float),
+                ("inv_freq", C.c_void_p), ("positions", C.c_void_p), ("position_offset", C.c_int64)]
+
+
+class RotaryItem(C.Structure):
+    _fields_ = [("inp", Heads), ("out", Heads), ("heads", C.c_int32), ("reserved", C.c_int32)]
+
+
+class AttentionDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("batch", C.c_int32), ("q_tokens", C.c_int32), ("k_tokens", C.c_int32), ("q_heads", C.c_int32),
+                ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("causal", C.c_int32), ("window", C.c_int32), ("scale", C.c_float),
+                ("num_seqs", C.c_int32), ("reserved", C.c_int32), ("q_lens", C.c_void_p), ("k_lens", C.c_void_p),
+                ("q_offsets", C.c_void_p), ("k_offsets", C.c_void_p)]
 
 
 _vp = C.c_void_p
@@ -97,6 +124,16 @@ _sig = {
                                   C.c_int32, _vp]),
     "muon_orthogonalize_static": (C.c_int, [_vp, _vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_float),
                                             C.c_float, C.c_uint32, _vp, _vp]),
+    "muon_layer_norm_forward": (C.c_int, [_vp, C.POINTER(NormDesc), _vp, C.c_int64, _vp, _vp, _vp, C.c_int64, _vp, _vp, _vp]),
+    "muon_layer_norm_workspace_bytes": (C.c_int, [C.POINTER(NormDesc), C.POINTER(C.c_size_t)]),
+    "muon_layer_norm_backward": (C.c_int, [_vp, C.POINTER(NormDesc), _vp, C.c_int64, _vp, C.c_int64, _vp, _vp, _vp, _vp, C.c_int64, _vp,
+                                           _vp, _vp, C.c_size_t, _vp]),
+    "muon_rotary": (C.c_int, [_vp, C.POINTER(RotaryDesc), C.POINTER(RotaryItem), C.c_int32, _vp]),
+    "muon_rotary_frequencies": (C.c_int, [C.c_double, C.c_int32, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double, _vp]),
+    "muon_attention_forward": (C.c_int, [_vp, C.POINTER(AttentionDesc)] + [C.POINTER(Heads)] * 4 + [_vp, _vp]),
+    "muon_attention_workspace_bytes": (C.c_int, [C.POINTER(AttentionDesc), C.POINTER(C.c_size_t)]),
+    "muon_attention_backward": (C.c_int, [_vp, C.POINTER(AttentionDesc)] + [C.POINTER(Heads)] * 5 + [_vp] + [C.POINTER(Heads)] * 3
+                                + [_vp, C.c_size_t, _vp]),
     "muon_last_device_status": (C.c_int, [_vp, _vp, C.POINTER(C.c_int32)]),
     "muon_clear_device_status": (C.c_int, [_vp, _vp]),
     "muon_synchronize_and_check": (C.c_int, [_vp, _vp]),
@@ -242,6 +279,28 @@ def muon_orthogonalize_static(inp, out, rows, cols, ns_precision, ns_steps, coef
     _check(lib.muon_orthogonalize_static(inp.data_ptr(), out.data_ptr(), rows, cols, ns_precision, ns_steps, co, eps, flags,
                                          None if status is None else status.data_ptr(), _stream(stream)),
            "muon_orthogonalize_static")
+
+
+# ---- layer operators: host-only queries
+def muon_layer_norm_workspace_bytes(desc: NormDesc) -> int:
+    out = C.c_size_t(0)
+    _check(lib.muon_layer_norm_workspace_bytes(C.byref(desc), C.byref(out)), "muon_layer_norm_workspace_bytes")
+    return int(out.value)
+
+
+def muon_attention_workspace_bytes(desc: AttentionDesc) -> int:
+    out = C.c_size_t(0)
+    _check(lib.muon_attention_workspace_bytes(C.byref(desc), C.byref(out)), "muon_attention_workspace_bytes")
+    return int(out.value)
+
+
+def muon_rotary_frequencies(base: float, rotary_dim: int, scaling: int = ROTARY_PLAIN, factor: float = 1.0, original_length: float = 0.0,
+                            low: float = 1.0, high: float = 4.0) -> np.ndarray:
+    """Radians per position of every pair, fp64 [rotary_dim / 2]."""
+    out = np.empty(max(1, rotary_dim // 2), dtype=np.float64)
+    _check(lib.muon_rotary_frequencies(base, rotary_dim, scaling, factor, original_length, low, high, out.ctypes.data),
+           "muon_rotary_frequencies")
+    return out
 
 
 # ---- logical-matrix views: pure address arithmetic on tensors that share one physical layout
@@ -423,6 +482,30 @@ class Context:
                                    c.data_ptr(), m, n, k, ldp, ldq, ldc, stride_p, stride_q, stride_c, batch, nn,
                                    alpha, beta, None if gamma is None else gamma.data_ptr(), gamma_mode,
                                    _stream(stream)), "muon_ns_product")
+
+    # -- layer operators: device addresses (ints, None for NULL) and descriptors; `functional` makes them from tensors
+    def muon_layer_norm_forward(self, desc: NormDesc, x, ldx, weight, bias, y, ldy, mean, rstd, stream=None) -> None:
+        _check(lib.muon_layer_norm_forward(self.handle, C.byref(desc), x, ldx, weight, bias, y, ldy, mean, rstd, _stream(stream)),
+               "muon_layer_norm_forward")
+
+    def muon_layer_norm_backward(self, desc: NormDesc, dy, lddy, x, ldx, weight, mean, rstd, dx, lddx, dweight, dbias, workspace,
+                                 workspace_bytes, stream=None) -> None:
+        _check(lib.muon_layer_norm_backward(self.handle, C.byref(desc), dy, lddy, x, ldx, weight, mean, rstd, dx, lddx, dweight, dbias,
+                                            workspace, workspace_bytes, _stream(stream)), "muon_layer_norm_backward")
+
+    def muon_rotary(self, desc: RotaryDesc, items, count, stream=None) -> None:
+        """items: a ctypes array of RotaryItem."""
+        _check(lib.muon_rotary(self.handle, C.byref(desc), items, count, _stream(stream)), "muon_rotary")
+
+    def muon_attention_forward(self, desc: AttentionDesc, q: Heads, k: Heads, v: Heads, o: Heads, lse, stream=None) -> None:
+        _check(lib.muon_attention_forward(self.handle, C.byref(desc), C.byref(q), C.byref(k), C.byref(v), C.byref(o), lse, _stream(stream)),
+               "muon_attention_forward")
+
+    def muon_attention_backward(self, desc: AttentionDesc, dout: Heads, q: Heads, k: Heads, v: Heads, o: Heads, lse, dq: Heads, dk: Heads,
+                                dv: Heads, workspace, workspace_bytes, stream=None) -> None:
+        _check(lib.muon_attention_backward(self.handle, C.byref(desc), C.byref(dout), C.byref(q), C.byref(k), C.byref(v), C.byref(o), lse,
+                                           C.byref(dq), C.byref(dk), C.byref(dv), workspace, workspace_bytes, _stream(stream)),
+               "muon_attention_backward")
 
     def muon_last_device_status(self, stream=None) -> int:
         v = C.c_int32(0)
