@@ -1,0 +1,337 @@
+// Attention forward on the tensor cores (bf16): one pass over the keys with a running maximum and sum.
+//
+// A block owns two tiles of 128 queries of one head and walks the blocks of 128 keys that they see.  320 threads:
+//   warps 0-3, 4-7  softmax of tile 0 and of tile 1: a thread owns one row (one TMEM lane), so maxima and sums need no exchange
+//   warp 8          TMA producer: the two q tiles once, then k and v tiles, two stages of each
+//   warp 9          MMA issuer:  S_t = q_t k^T (128 x 128 x head_dim),  O_t += P_t v with P_t read from tensor memory
+// Tensor memory: S_0, S_1 (128 columns each), O_0, O_1.  P_t takes the place of S_t, rounded once to bf16.  While one tile's softmax runs,
+// the issuer works for the other.  A tcgen05.commit covers everything issued before it, so "S_t of block j is ready" also says that the
+// product that read P_t of block j - 1 is done and O_t may be touched.
+//
+// The running maximum is raised only when a row's scores exceed it by more than 2^8 in the exponential: until then P is at most 256 and
+// the sum is exact enough in fp32 (P's rounding is relative), and O, which sits in tensor memory, is not read and rewritten.
+#include <cuda_bf16.h>
+
+#include "attention_tc.cuh"
+
+namespace muon {
+namespace {
+
+using namespace attn;
+
+constexpr int THREADS = 320, STAGES = 2, TMEM_COLS = 512;
+constexpr float kRaise = 8.f;                    // log2 of the largest P
+
+template <int BOXES> struct Smem {
+  static constexpr uint32_t kTile = BOXES * BOX_BYTES;
+  static constexpr uint32_t q = 0, k = 2 * kTile, v = k + STAGES * kTile, bars = v + STAGES * kTile;
+  static constexpr uint32_t bytes = bars + 256 + 1024;   // barriers, slack for the 1024-byte alignment of swizzled tiles
+};
+
+template <int BOXES>
+__global__ void __launch_bounds__(THREADS, 1)
+attention_forward_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnArgs a) {
+  using L = Smem<BOXES>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (base - raw);
+  const uint32_t bars = base + L::bars;
+  auto q_full = [&](int t) { return bars + uint32_t(t) * 8u; };
+  auto s_full = [&](int t) { return bars + uint32_t(2 + t) * 8u; };
+  auto p_ready = [&](int t) { return bars + uint32_t(4 + t) * 8u; };
+  auto o_full = [&](int t) { return bars + uint32_t(6 + t) * 8u; };
+  auto k_full = [&](int s) { return bars + uint32_t(8 + s) * 8u; };
+  auto k_empty = [&](int s) { return bars + uint32_t(8 + STAGES + s) * 8u; };
+  auto v_full = [&](int s) { return bars + uint32_t(8 + 2 * STAGES + s) * 8u; };
+  auto v_empty = [&](int s) { return bars + uint32_t(8 + 3 * STAGES + s) * 8u; };
+  const uint32_t done_bar = bars + uint32_t(8 + 4 * STAGES) * 8u;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + L::bars + 192);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + L::bars + 200);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // Heads vary fastest, so that blocks that share keys run together; within a batched call the last queries, which see most keys, go first.
+  const int head = int(blockIdx.x % unsigned(a.hq)), kvh = head / (a.hq / a.hkv);
+  int si, blk;
+  if (!attn_find_block(a, int(blockIdx.x / unsigned(a.hq)), 2 * BLK, false, &si, &blk)) return;
+  if (!a.nseq) {
+    const int rest = int(blockIdx.x / unsigned(a.hq)), per = (a.nq + 2 * BLK - 1) / (2 * BLK);
+    si = rest % a.batch;
+    blk = per - 1 - rest / a.batch;
+  }
+  const AttnSeq s = attn_seq(a, si);
+  const int r0 = blk * 2 * BLK;
+  const BlockRange rg[2] = {key_blocks(a, s, r0), key_blocks(a, s, r0 + BLK)};
+  int u0 = rg[0].n0, u1 = rg[0].n1;
+  if (rg[1].n1 > rg[1].n0) {
+    u0 = u1 > u0 ? min(u0, rg[1].n0) : rg[1].n0;
+    u1 = max(u1, rg[1].n1);
+  }
+
+  if (threadIdx.x == 0) {
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(q_full(t), 1);
+      mbar_init(s_full(t), 1);
+      mbar_init(p_ready(t), 4);
+      mbar_init(o_full(t), 1);
+    }
+    for (int i = 0; i < STAGES; ++i) {
+      mbar_init(k_full(i), 1);
+      mbar_init(k_empty(i), 1);
+      mbar_init(v_full(i), 1);
+      mbar_init(v_empty(i), 1);
+    }
+    mbar_init(done_bar, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async_smem();
+  }
+  if (warp == 9) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(TMEM_COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const uint32_t t_s[2] = {tmem, tmem + 128}, t_o[2] = {tmem + 256, tmem + 256 + BOXES * 64};
+  const float c2 = a.scale * kLog2e;
+
+  if (warp == 8) {
+    // ------------------------------------------------------------------ TMA producer
+    if (lane == 0 && u1 > u0) {
+      bool ok = true;
+      for (int t = 0; t < 2; ++t) {
+        if (rg[t].n1 <= rg[t].n0) continue;
+        mbar_expect_tx(q_full(t), L::kTile);
+        load_tile<BOXES>(base + L::q + t * L::kTile, &maps.q, q_full(t), head, s.q0 + r0 + t * BLK, s.tb);
+      }
+      int j = u0;
+      for (; j < u1 && ok; ++j) {
+        const int i = j - u0, st = i % STAGES;
+        const uint32_t ph = uint32_t(i / STAGES) & 1u;
+        if (!(ok = mbar_wait(k_empty(st), ph ^ 1u, abort_flag))) break;
+        mbar_expect_tx(k_full(st), L::kTile);
+        load_tile<BOXES>(base + L::k + st * L::kTile, &maps.k, k_full(st), kvh, s.k0 + j * BLK, s.tb);
+        ok = mbar_wait(v_empty(st), ph ^ 1u, abort_flag);
+        mbar_expect_tx(v_full(st), L::kTile);              // armed even when giving up, so that the drain below is one rule
+        load_tile<BOXES>(base + L::v + st * L::kTile, &maps.v, v_full(st), kvh, s.k0 + j * BLK, s.tb);
+      }
+      if (!ok) {
+        *abort_flag = 1;
+        atomicExch(a.status, 21);
+      }
+      // Everything asked for must have landed before this block's shared memory is released.
+      for (int t = 0; t < 2; ++t)
+        if (rg[t].n1 > rg[t].n0) mbar_wait(q_full(t), 0, abort_flag, false, WAIT_CYCLES / 8);
+      for (int i = max(0, j - u0 - STAGES); i < j - u0; ++i) {
+        const uint32_t ph = uint32_t(i / STAGES) & 1u;
+        if (!mbar_wait(k_full(i % STAGES), ph, abort_flag, false, WAIT_CYCLES / 8) ||
+            !mbar_wait(v_full(i % STAGES), ph, abort_flag, false, WAIT_CYCLES / 8))
+          atomicExch(a.status, 22);
+      }
+    }
+  } else if (warp == 9) {
+    // ------------------------------------------------------------------ MMA issuer (the whole warp waits, lane 0 issues)
+    if (u1 > u0) {
+      const int ksteps = (a.dim + 15) / 16;
+      const uint32_t idesc_o = make_idesc(true, BLK, ksteps * 16);
+      bool ok = true;
+      auto in = [&](int t, int j) { return j >= rg[t].n0 && j < rg[t].n1; };
+      auto await = [&](uint32_t bar, uint32_t ph) {
+        ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, ph, abort_flag));
+        tc_fence_after();
+      };
+      auto scores = [&](int t, int j) {
+        if (j == rg[t].n0) await(q_full(t), 0);
+        if (!ok) return;
+        if (lane == 0) {
+          mma_rows_rows(t_s[t], base + L::q + t * L::kTile, base + L::k + uint32_t((j - u0) % STAGES) * L::kTile, ksteps);
+          tc_commit(s_full(t));
+        }
+        __syncwarp();
+      };
+      auto await_k = [&](int j) { await(k_full((j - u0) % STAGES), uint32_t((j - u0) / STAGES) & 1u); };
+      auto free_k = [&](int j) {
+        if (lane == 0) tc_commit(k_empty((j - u0) % STAGES));
+        __syncwarp();
+      };
+      await_k(u0);
+      for (int t = 0; t < 2 && ok; ++t)
+        if (in(t, u0)) scores(t, u0);
+      if (ok) free_k(u0);
+      for (int j = u0; j < u1 && ok; ++j) {
+        const int st = (j - u0) % STAGES;
+        const uint32_t v = base + L::v + uint32_t(st) * L::kTile;
+        await(v_full(st), uint32_t((j - u0) / STAGES) & 1u);
+        if (!ok) break;
+        if ((j + 1) * BLK > s.kn) clear_rows<BOXES>(v, s.kn - j * BLK, lane);
+        if (j + 1 < u1) await_k(j + 1);
+        for (int t = 0; t < 2 && ok; ++t) {
+          if (in(t, j)) {
+            await(p_ready(t), uint32_t(j - rg[t].n0) & 1u);
+            if (!ok) break;
+            if (lane == 0) {
+              mma_probs_rows(t_o[t], t_s[t], t_s[t] + 32, v, idesc_o, j > rg[t].n0);
+              if (j + 1 == rg[t].n1) tc_commit(o_full(t));
+            }
+            __syncwarp();
+          }
+          if (in(t, j + 1)) scores(t, j + 1);
+        }
+        if (!ok) break;
+        if (lane == 0) tc_commit(v_empty(st));
+        __syncwarp();
+        if (j + 1 < u1) free_k(j + 1);
+      }
+      // Nothing may be in flight when tensor memory is freed.
+      if (lane == 0) {
+        if (!ok) {
+          *abort_flag = 1;
+          atomicExch(a.status, 23);
+        }
+        tc_commit(done_bar);
+        if (!mbar_wait(done_bar, 0, abort_flag, false, WAIT_CYCLES / 8)) atomicExch(a.status, 24);
+      }
+      __syncwarp();
+    }
+  } else {
+    // ------------------------------------------------------------------ softmax and results
+    const int t = warp >> 2, quad = warp & 3;
+    const int row = r0 + t * BLK + quad * 32 + lane;
+    const uint32_t lanes = uint32_t(quad * 32) << 16;
+    const uint32_t ts = t_s[t] + lanes, to = t_o[t] + lanes;
+    const int lo = attn_key_lo(a, s, row), hi = attn_key_hi(a, s, row);
+    float m = -INFINITY, l = 0.f;
+    bool ok = true;
+    for (int j = rg[t].n0; j < rg[t].n1; ++j) {
+      ok = __all_sync(0xffffffffu, mbar_wait(s_full(t), uint32_t(j - rg[t].n0) & 1u, abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+      float x[128];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tc_ld32(ts + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[i * 32]));
+      tc_wait_ld();
+      const int c0 = j * BLK;
+      if (block_masked(a, s, r0 + t * BLK, c0)) {
+#pragma unroll
+        for (int i = 0; i < 128; ++i)
+          if (c0 + i < lo || c0 + i >= hi) x[i] = -INFINITY;
+      }
+      float top[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+      for (int i = 4; i < 128; ++i) top[i & 3] = fmaxf(top[i & 3], x[i]);
+      const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+      const bool raise = mx > m && (m == -INFINITY || (mx - m) * c2 > kRaise);
+      if (__any_sync(0xffffffffu, raise)) {
+        const float shrink = raise ? exp2_approx((m - mx) * c2) : 1.f;
+        if (raise) m = mx;
+        l *= shrink;
+        if (j > rg[t].n0) {
+#pragma unroll
+          for (int i = 0; i < BOXES * 2; ++i) {
+            uint32_t o[32];
+            tc_ld32(to + i * 32, o);
+            tc_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
+            tc_st32(to + i * 32, o);
+          }
+        }
+      }
+      const float mc = m == -INFINITY ? 0.f : m * c2;
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t p[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const float p0 = exp2_approx(fmaf(x[h * 64 + 2 * i], c2, -mc)), p1 = exp2_approx(fmaf(x[h * 64 + 2 * i + 1], c2, -mc));
+          sum[(2 * i) & 3] += p0;
+          sum[(2 * i + 1) & 3] += p1;
+          p[i] = pack_bf16(p0, p1);
+        }
+        tc_st32(ts + h * 32, p);
+      }
+      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      tc_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(p_ready(t));
+    }
+    const bool any = rg[t].n1 > rg[t].n0;
+    if (ok && any) {
+      ok = __all_sync(0xffffffffu, mbar_wait(o_full(t), 0, abort_flag));
+      tc_fence_after();
+    }
+    if (!ok) {
+      if (lane == 0) {
+        *abort_flag = 1;
+        atomicExch(a.status, 25);
+      }
+    } else {
+      const bool dead = l == 0.f || hi <= lo;              // a row that sees nothing
+      const float inv = dead ? 0.f : 1.f / l;
+      const bool store = row < s.qext;
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.o.data) + int64_t(s.tb) * a.o.sb + int64_t(s.q0 + row) * a.o.st + int64_t(head) * a.o.sh;
+#pragma unroll
+      for (int i = 0; i < BOXES * 2; ++i) {
+        uint32_t o[32];
+        if (any) {
+          tc_ld32(to + i * 32, o);
+          tc_wait_ld();
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int d = i * 32 + e * 8;
+          uint4 w = make_uint4(0, 0, 0, 0);
+          if (!dead) {
+            w.x = pack_bf16(__uint_as_float(o[e * 8]) * inv, __uint_as_float(o[e * 8 + 1]) * inv);
+            w.y = pack_bf16(__uint_as_float(o[e * 8 + 2]) * inv, __uint_as_float(o[e * 8 + 3]) * inv);
+            w.z = pack_bf16(__uint_as_float(o[e * 8 + 4]) * inv, __uint_as_float(o[e * 8 + 5]) * inv);
+            w.w = pack_bf16(__uint_as_float(o[e * 8 + 6]) * inv, __uint_as_float(o[e * 8 + 7]) * inv);
+          }
+          if (store && d < a.dim) *reinterpret_cast<uint4*>(out + d) = w;
+        }
+      }
+      if (store) a.lse[(int64_t(s.tb) * a.hq + head) * a.nq + s.q0 + row] = dead ? -INFINITY : fmaf(m, a.scale, logf(l));
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 9) {
+    __syncwarp();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
+  }
+}
+
+template <int BOXES>
+int run(const AttnMaps& maps, const AttnArgs& a, cudaStream_t st) {
+  const int64_t blocks = attn_max_blocks(a, 2 * BLK, false) * a.hq;
+  if (blocks > 0x7fffffff) return MUON_ERR_UNSUPPORTED;
+  auto kernel = attention_forward_tc_kernel<BOXES>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<BOXES>::bytes) != cudaSuccess) return MUON_ERR_CUDA;
+  kernel<<<unsigned(blocks), THREADS, Smem<BOXES>::bytes, st>>>(maps, a);
+  return cudaGetLastError() == cudaSuccess ? 1 : MUON_ERR_CUDA;
+}
+
+}  // namespace
+
+bool attention_forward_tc_takes(const AttnArgs& a) {
+  return a.dim % 8 == 0 && a.dim <= 128 && a.nk > 0 && map_takes(a.q, a.batch, a.nq, a.hq) && map_takes(a.k, a.batch, a.nk, a.hkv) &&
+         map_takes(a.v, a.batch, a.nk, a.hkv) && map_takes(a.o, a.batch, a.nq, a.hq);
+}
+
+int launch_attention_forward_tc(muon_ctx* ctx, const AttnArgs& a, cudaStream_t st) {
+  if (!ctx->tmap_encode) return MUON_ERR_CUDA;
+  AttnMaps m;
+  if (!encode_tile_map(ctx->tmap_encode, &m.q, a.q, a.dim, a.batch, a.nq, a.hq) ||
+      !encode_tile_map(ctx->tmap_encode, &m.k, a.k, a.dim, a.batch, a.nk, a.hkv) ||
+      !encode_tile_map(ctx->tmap_encode, &m.v, a.v, a.dim, a.batch, a.nk, a.hkv))
+    return MUON_ERR_CUDA;
+  m.dout = m.q;
+  ctx->tmap_encodes += 3;
+  return a.dim <= 64 ? run<1>(m, a, st) : run<2>(m, a, st);
+}
+
+}  // namespace muon

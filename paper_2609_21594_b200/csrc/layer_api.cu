@@ -250,7 +250,9 @@ int muon_attention_forward(muon_ctx_t* ctx, const muon_attention_desc_t* desc, c
   a.v = attn_tensor(v);
   a.o = attn_tensor(o);
   a.lse = lse;
-  return launched(ctx, launch_attention_forward_simt(a, desc->dtype, static_cast<cudaStream_t>(stream)));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (desc->dtype == MUON_DTYPE_BF16 && attention_forward_tc_takes(a)) return launched(ctx, launch_attention_forward_tc(ctx, a, st));
+  return launched(ctx, launch_attention_forward_simt(a, desc->dtype, st));
 }
 
 int muon_attention_workspace_bytes(const muon_attention_desc_t* desc, size_t* bytes) {
