@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmuon_b200.so")
 SOURCES = ["api.cu", "plan.cu", "layout_kernels.cu", "elementwise_kernels.cu", "ns_simt.cu", "ns_tcgen05.cu", "ns_tcgen05_pair.cu", "ns_tables.cu",
-           "layer_api.cu", "layer_norm.cu", "rotary.cu", "attention_simt.cu", "attention_fwd.cu"]
+           "layer_api.cu", "layer_norm.cu", "rotary.cu", "attention_simt.cu", "attention_fwd.cu", "attention_bwd.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"] + os.environ.get("MUON_NVCC_EXTRA", "").split()
 

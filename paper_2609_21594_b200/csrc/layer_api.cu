@@ -312,6 +312,7 @@ int muon_attention_backward(muon_ctx_t* ctx, const muon_attention_desc_t* desc, 
   const int rows = launch_attention_rows(a, desc->dtype, st);
   if (rows < 0) return rows;
   ctx->launches += rows;
+  if (desc->dtype == MUON_DTYPE_BF16 && attention_backward_tc_takes(a)) return launched(ctx, launch_attention_backward_tc(ctx, a, st));
   return launched(ctx, launch_attention_backward_simt(a, desc->dtype, st));
 }
 

@@ -177,6 +177,8 @@ int launch_attention_backward_simt(const AttnArgs& a, int dtype, cudaStream_t st
 // The tensor-core kernels take bf16 heads of a multiple of 8 up to 128 elements whose tensors TMA can address.
 bool attention_forward_tc_takes(const AttnArgs& a);
 int launch_attention_forward_tc(muon_ctx* ctx, const AttnArgs& a, cudaStream_t st);
+bool attention_backward_tc_takes(const AttnArgs& a);
+int launch_attention_backward_tc(muon_ctx* ctx, const AttnArgs& a, cudaStream_t st);
 int launch_attention_rows(const AttnArgs& a, int dtype, cudaStream_t st);           // fills AttnArgs::rows
 
 }  // namespace muon
