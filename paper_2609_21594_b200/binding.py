@@ -124,16 +124,15 @@ _sig = {
                                   C.c_int32, _vp]),
     "muon_orthogonalize_static": (C.c_int, [_vp, _vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_float),
                                             C.c_float, C.c_uint32, _vp, _vp]),
-    "muon_layer_norm_forward": (C.c_int, [_vp, C.POINTER(NormDesc), _vp, C.c_int64, _vp, _vp, _vp, C.c_int64, _vp, _vp, _vp]),
-    "muon_layer_norm_workspace_bytes": (C.c_int, [C.POINTER(NormDesc), C.POINTER(C.c_size_t)]),
-    "muon_layer_norm_backward": (C.c_int, [_vp, C.POINTER(NormDesc), _vp, C.c_int64, _vp, C.c_int64, _vp, _vp, _vp, _vp, C.c_int64, _vp,
-                                           _vp, _vp, C.c_size_t, _vp]),
-    "muon_rotary": (C.c_int, [_vp, C.POINTER(RotaryDesc), C.POINTER(RotaryItem), C.c_int32, _vp]),
+    # descriptors and tensors of the layer operators travel as addresses: of a structure (byref) or of packed memory (an int)
+    "muon_layer_norm_forward": (C.c_int, [_vp, _vp, _vp, C.c_int64, _vp, _vp, _vp, C.c_int64, _vp, _vp, _vp]),
+    "muon_layer_norm_workspace_bytes": (C.c_int, [_vp, C.POINTER(C.c_size_t)]),
+    "muon_layer_norm_backward": (C.c_int, [_vp, _vp, _vp, C.c_int64, _vp, C.c_int64, _vp, _vp, _vp, _vp, C.c_int64, _vp, _vp, _vp, C.c_size_t, _vp]),
+    "muon_rotary": (C.c_int, [_vp, _vp, _vp, C.c_int32, _vp]),
     "muon_rotary_frequencies": (C.c_int, [C.c_double, C.c_int32, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double, _vp]),
-    "muon_attention_forward": (C.c_int, [_vp, C.POINTER(AttentionDesc)] + [C.POINTER(Heads)] * 4 + [_vp, _vp]),
-    "muon_attention_workspace_bytes": (C.c_int, [C.POINTER(AttentionDesc), C.POINTER(C.c_size_t)]),
-    "muon_attention_backward": (C.c_int, [_vp, C.POINTER(AttentionDesc)] + [C.POINTER(Heads)] * 5 + [_vp] + [C.POINTER(Heads)] * 3
-                                + [_vp, C.c_size_t, _vp]),
+    "muon_attention_forward": (C.c_int, [_vp] * 8),
+    "muon_attention_workspace_bytes": (C.c_int, [_vp, C.POINTER(C.c_size_t)]),
+    "muon_attention_backward": (C.c_int, [_vp] * 12 + [C.c_size_t, _vp]),
     "muon_last_device_status": (C.c_int, [_vp, _vp, C.POINTER(C.c_int32)]),
     "muon_clear_device_status": (C.c_int, [_vp, _vp]),
     "muon_synchronize_and_check": (C.c_int, [_vp, _vp]),
@@ -281,17 +280,26 @@ def muon_orthogonalize_static(inp, out, rows, cols, ns_precision, ns_steps, coef
            "muon_orthogonalize_static")
 
 
-# ---- layer operators: host-only queries
-def muon_layer_norm_workspace_bytes(desc: NormDesc) -> int:
-    out = C.c_size_t(0)
-    _check(lib.muon_layer_norm_workspace_bytes(C.byref(desc), C.byref(out)), "muon_layer_norm_workspace_bytes")
-    return int(out.value)
+# ---- layer operators
+_norm_forward, _norm_backward, _rotary = lib.muon_layer_norm_forward, lib.muon_layer_norm_backward, lib.muon_rotary
+_attention_forward, _attention_backward = lib.muon_attention_forward, lib.muon_attention_backward
 
 
-def muon_attention_workspace_bytes(desc: AttentionDesc) -> int:
+def _at(x):
+    """What a pointer argument takes for a structure, an array or an address."""
+    return x if type(x) is int else C.byref(x)
+
+
+def muon_layer_norm_workspace_bytes(desc) -> int:
     out = C.c_size_t(0)
-    _check(lib.muon_attention_workspace_bytes(C.byref(desc), C.byref(out)), "muon_attention_workspace_bytes")
-    return int(out.value)
+    _check(lib.muon_layer_norm_workspace_bytes(_at(desc), C.byref(out)), "muon_layer_norm_workspace_bytes")
+    return out.value
+
+
+def muon_attention_workspace_bytes(desc) -> int:
+    out = C.c_size_t(0)
+    _check(lib.muon_attention_workspace_bytes(_at(desc), C.byref(out)), "muon_attention_workspace_bytes")
+    return out.value
 
 
 def muon_rotary_frequencies(base: float, rotary_dim: int, scaling: int = ROTARY_PLAIN, factor: float = 1.0, original_length: float = 0.0,
@@ -483,29 +491,36 @@ class Context:
                                    alpha, beta, None if gamma is None else gamma.data_ptr(), gamma_mode,
                                    _stream(stream)), "muon_ns_product")
 
-    # -- layer operators: device addresses (ints, None for NULL) and descriptors; `functional` makes them from tensors
-    def muon_layer_norm_forward(self, desc: NormDesc, x, ldx, weight, bias, y, ldy, mean, rstd, stream=None) -> None:
-        _check(lib.muon_layer_norm_forward(self.handle, C.byref(desc), x, ldx, weight, bias, y, ldy, mean, rstd, _stream(stream)),
-               "muon_layer_norm_forward")
+    # -- layer operators.  Device pointers are ints (None for NULL); a descriptor or tensor is its ctypes structure or the int address of
+    # memory laid out like it, which `functional` packs without building objects (a call's host time is most of a small one's).
+    def muon_layer_norm_forward(self, desc, x, ldx, weight, bias, y, ldy, mean, rstd, stream=None) -> None:
+        rc = _norm_forward(self.handle, _at(desc), x, ldx, weight, bias, y, ldy, mean, rstd, _stream(stream))
+        if rc:
+            raise MuonError(rc, "muon_layer_norm_forward")
 
-    def muon_layer_norm_backward(self, desc: NormDesc, dy, lddy, x, ldx, weight, mean, rstd, dx, lddx, dweight, dbias, workspace,
-                                 workspace_bytes, stream=None) -> None:
-        _check(lib.muon_layer_norm_backward(self.handle, C.byref(desc), dy, lddy, x, ldx, weight, mean, rstd, dx, lddx, dweight, dbias,
-                                            workspace, workspace_bytes, _stream(stream)), "muon_layer_norm_backward")
+    def muon_layer_norm_backward(self, desc, dy, lddy, x, ldx, weight, mean, rstd, dx, lddx, dweight, dbias, workspace, workspace_bytes,
+                                 stream=None) -> None:
+        rc = _norm_backward(self.handle, _at(desc), dy, lddy, x, ldx, weight, mean, rstd, dx, lddx, dweight, dbias, workspace, workspace_bytes,
+                            _stream(stream))
+        if rc:
+            raise MuonError(rc, "muon_layer_norm_backward")
 
-    def muon_rotary(self, desc: RotaryDesc, items, count, stream=None) -> None:
-        """items: a ctypes array of RotaryItem."""
-        _check(lib.muon_rotary(self.handle, C.byref(desc), items, count, _stream(stream)), "muon_rotary")
+    def muon_rotary(self, desc, items, count, stream=None) -> None:
+        """items: a ctypes array of RotaryItem, or the address of as many."""
+        rc = _rotary(self.handle, _at(desc), _at(items), count, _stream(stream))
+        if rc:
+            raise MuonError(rc, "muon_rotary")
 
-    def muon_attention_forward(self, desc: AttentionDesc, q: Heads, k: Heads, v: Heads, o: Heads, lse, stream=None) -> None:
-        _check(lib.muon_attention_forward(self.handle, C.byref(desc), C.byref(q), C.byref(k), C.byref(v), C.byref(o), lse, _stream(stream)),
-               "muon_attention_forward")
+    def muon_attention_forward(self, desc, q, k, v, o, lse, stream=None) -> None:
+        rc = _attention_forward(self.handle, _at(desc), _at(q), _at(k), _at(v), _at(o), lse, _stream(stream))
+        if rc:
+            raise MuonError(rc, "muon_attention_forward")
 
-    def muon_attention_backward(self, desc: AttentionDesc, dout: Heads, q: Heads, k: Heads, v: Heads, o: Heads, lse, dq: Heads, dk: Heads,
-                                dv: Heads, workspace, workspace_bytes, stream=None) -> None:
-        _check(lib.muon_attention_backward(self.handle, C.byref(desc), C.byref(dout), C.byref(q), C.byref(k), C.byref(v), C.byref(o), lse,
-                                           C.byref(dq), C.byref(dk), C.byref(dv), workspace, workspace_bytes, _stream(stream)),
-               "muon_attention_backward")
+    def muon_attention_backward(self, desc, dout, q, k, v, o, lse, dq, dk, dv, workspace, workspace_bytes, stream=None) -> None:
+        rc = _attention_backward(self.handle, _at(desc), _at(dout), _at(q), _at(k), _at(v), _at(o), lse, _at(dq), _at(dk), _at(dv), workspace,
+                                 workspace_bytes, _stream(stream))
+        if rc:
+            raise MuonError(rc, "muon_attention_backward")
 
     def muon_last_device_status(self, stream=None) -> int:
         v = C.c_int32(0)

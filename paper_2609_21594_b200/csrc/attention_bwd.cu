@@ -529,9 +529,8 @@ int run(const AttnMaps& m, const AttnArgs& a, cudaStream_t st) {
   const int64_t kb = attn_max_blocks(a, BLK, true) * a.hkv, qb = attn_max_blocks(a, BLK, false) * a.hq;
   if (kb > 0x7fffffff || qb > 0x7fffffff) return MUON_ERR_UNSUPPORTED;
   constexpr uint32_t bytes = Smem<BOXES>::bytes;
-  if (cudaFuncSetAttribute(attention_dkv_tc_kernel<BOXES>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess ||
-      cudaFuncSetAttribute(attention_dq_tc_kernel<BOXES>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess)
-    return MUON_ERR_CUDA;
+  static SharedMemoryLimit limit;
+  if (!limit.raise(a.device, bytes, attention_dkv_tc_kernel<BOXES>, attention_dq_tc_kernel<BOXES>)) return MUON_ERR_CUDA;
   attention_dkv_tc_kernel<BOXES><<<unsigned(kb), THREADS, bytes, st>>>(m, a);
   attention_dq_tc_kernel<BOXES><<<unsigned(qb), THREADS, bytes, st>>>(m, a);
   return cudaGetLastError() == cudaSuccess ? 2 : MUON_ERR_CUDA;

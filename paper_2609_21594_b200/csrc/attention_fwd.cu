@@ -310,7 +310,8 @@ int run(const AttnMaps& maps, const AttnArgs& a, cudaStream_t st) {
   const int64_t blocks = attn_max_blocks(a, 2 * BLK, false) * a.hq;
   if (blocks > 0x7fffffff) return MUON_ERR_UNSUPPORTED;
   auto kernel = attention_forward_tc_kernel<BOXES>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<BOXES>::bytes) != cudaSuccess) return MUON_ERR_CUDA;
+  static SharedMemoryLimit limit;
+  if (!limit.raise(a.device, Smem<BOXES>::bytes, kernel)) return MUON_ERR_CUDA;
   kernel<<<unsigned(blocks), THREADS, Smem<BOXES>::bytes, st>>>(maps, a);
   return cudaGetLastError() == cudaSuccess ? 1 : MUON_ERR_CUDA;
 }

@@ -88,6 +88,7 @@ AttnArgs attention_args(const muon_ctx* ctx, const muon_attention_desc_t* d) {
   a.q_off = d->q_offsets;
   a.k_off = d->k_offsets;
   a.status = ctx ? ctx->d_status : nullptr;
+  a.device = ctx ? ctx->device : -1;
   return a;
 }
 

@@ -1,9 +1,27 @@
 // Shared declarations of the layer operators (layer norm, rotary positions, attention).  Internal to the library.
 #pragma once
 
+#include <atomic>
+
 #include "internal.h"
 
 namespace muon {
+
+// Raises the dynamic shared memory that kernels may use, once per device (the call costs about as much as a launch).  One object serves one
+// set of kernels and one size; host threads may race to it, setting the same value twice.
+class SharedMemoryLimit {
+  std::atomic<uint64_t> done_{0};             // a bit per device; devices past 63 set it every time
+
+ public:
+  template <typename... K>
+  bool raise(int device, uint32_t bytes, K... kernels) {
+    const uint64_t bit = device < 64 ? uint64_t(1) << device : 0;
+    if (done_.load(std::memory_order_relaxed) & bit) return true;
+    const bool ok = ((cudaFuncSetAttribute(kernels, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes)) == cudaSuccess) && ...);
+    if (ok) done_.fetch_or(bit, std::memory_order_relaxed);
+    return ok;
+  }
+};
 
 // ------------------------------------------------------------------ layer norm
 constexpr int kNormMaxCols = 16384;
@@ -64,6 +82,7 @@ struct AttnArgs {
   const int32_t* q_off;
   const int32_t* k_off;
   int32_t* status;
+  int32_t device;
 };
 
 // One sequence as the kernels see it.  Rows [q0, q0 + qext) of batch row `tb` are its queries; the first qn count, the others

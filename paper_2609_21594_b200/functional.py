@@ -8,6 +8,7 @@ of its own per device (autograd calls backward passes from another thread).
 from __future__ import annotations
 
 import ctypes as C
+import struct
 import threading
 from typing import Optional, Sequence, Tuple
 
@@ -18,20 +19,40 @@ from . import binding as mb
 from .binding import muon_rotary_frequencies as rotary_frequencies  # noqa: F401  (part of this module's interface)
 
 _DTYPES = {torch.bfloat16: mb.DTYPE_BF16, torch.float32: mb.DTYPE_FP32}
+_current_device = torch.cuda.current_device
+_raw_stream = torch._C._cuda_getCurrentRawStream         # the current stream's handle, without building a Stream object
+# memory images of muon_norm_desc_t, muon_rotary_desc_t, muon_attention_desc_t and of runs of muon_heads_t / muon_rotary_item_t
+_NORM, _ROTARY, _ATTENTION = struct.Struct("4iqfi"), struct.Struct("7ifQQq"), struct.Struct("9if2i4Q")
+_HEADS = {n: struct.Struct(f"{'Q3q' * n}") for n in (4, 8)}
+_ITEM = struct.Struct("Q3qQ3q2i")
+_DESC_BYTES, _HEADS_BYTES = 128, 32
 _local = threading.local()
+
+
+class _Lane:
+    """What one host thread uses on one device: a context, and memory that descriptors are packed into for the length of a call."""
+
+    def __init__(self, index: int):
+        with torch.cuda.device(index):
+            self.ctx = mb.Context()
+        self.memory = C.create_string_buffer(_DESC_BYTES + 10 * _HEADS_BYTES)
+        self.desc = C.addressof(self.memory)
+        self.heads = [self.desc + _DESC_BYTES + i * _HEADS_BYTES for i in range(10)]
+
+
+def _lane(index: int) -> _Lane:
+    try:
+        return _local.lanes[index]
+    except (AttributeError, KeyError):
+        if not hasattr(_local, "lanes"):
+            _local.lanes = {}
+        lane = _local.lanes[index] = _Lane(index)
+        return lane
 
 
 def context(device: Optional[torch.device] = None) -> mb.Context:
     """This thread's context of a device (default: the current one): the one the functions of this module use there."""
-    index = torch.cuda.current_device() if device is None or device.index is None else device.index
-    per = getattr(_local, "contexts", None)
-    if per is None:
-        per = _local.contexts = {}
-    ctx = per.get(index)
-    if ctx is None:
-        with torch.cuda.device(index):
-            ctx = per[index] = mb.Context()
-    return ctx
+    return _lane(_current_device() if device is None or device.index is None else device.index).ctx
 
 
 def _dtype(t: torch.Tensor, what: str) -> int:
@@ -41,31 +62,23 @@ def _dtype(t: torch.Tensor, what: str) -> int:
     return d
 
 
-def _on(t: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
-    if not t.is_cuda:
+def _on(t: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
+    """The index of the device that all the tensors are on."""
+    index = t.get_device()
+    if index < 0:
         raise ValueError("the layer operators take CUDA tensors (there is no CPU fallback)")
     for o in others:
-        if o is not None and o.device != t.device:
+        if o is not None and o.get_device() != index:
             raise ValueError(f"tensors on {o.device} and {t.device} in one call")
-
-
-class _Guard:
-    """Makes the tensors' device current for the call when it is not."""
-
-    def __init__(self, t: torch.Tensor):
-        self._guard = None if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
-
-    def __enter__(self):
-        if self._guard is not None:
-            self._guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self._guard is not None:
-            self._guard.__exit__(*exc)
+    return index
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
+
+
+def _address(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else t.data_ptr()
 
 
 # ------------------------------------------------------------------------------------------------ layer norm
@@ -73,7 +86,7 @@ def _rows(t: torch.Tensor, what: str) -> torch.Tensor:
     """[..., cols] as [rows, cols] with contiguous rows: a view where the strides allow one, else a copy."""
     if t.dim() < 1 or t.shape[-1] < 1:
         raise ValueError(f"{what} needs a last dimension of at least one element")
-    r = t.reshape(-1, t.shape[-1])
+    r = t if t.dim() == 2 else t.reshape(-1, t.shape[-1])
     return r if (r.shape[1] == 1 or r.stride(1) == 1) and (r.shape[0] <= 1 or r.stride(0) >= r.shape[1]) else r.contiguous()
 
 
@@ -89,27 +102,28 @@ def _param(p: Optional[torch.Tensor], cols: int, what: str) -> Optional[torch.Te
     return p.contiguous()
 
 
-def _norm_desc(x: torch.Tensor, r: torch.Tensor, weight, bias, eps: float, center: bool) -> mb.NormDesc:
-    if weight is not None and bias is not None and weight.dtype != bias.dtype:
-        raise ValueError("weight and bias must have one dtype")
-    p = weight if weight is not None else bias
-    return mb.NormDesc(_dtype(x, "x"), mb.DTYPE_FP32 if p is None else _dtype(p, "weight and bias"), 1 if center else 0, r.shape[1], r.shape[0],
-                       eps, 0)
-
-
 def layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
                        center: bool = True) -> Tuple[torch.Tensor, Optional[torch.Tensor], torch.Tensor]:
     """(y, mean, rstd) over the last dimension; center=False is RMS norm and gives mean = None.  mean, rstd: fp32, x.shape[:-1]."""
-    _on(x, weight, bias)
+    index = _on(x, weight, bias)
+    if index != _current_device():
+        with torch.cuda.device(index):
+            return layer_norm_forward(x, weight, bias, eps, center)
     r = _rows(x, "x")
-    weight, bias = _param(weight, r.shape[1], "weight"), _param(bias, r.shape[1], "bias")
-    desc = _norm_desc(x, r, weight, bias, eps, center)
-    with _Guard(x):
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if center else None
-        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-        context(x.device).muon_layer_norm_forward(desc, r.data_ptr(), _ld(r), _ptr(weight), _ptr(bias), y.data_ptr(), r.shape[1], _ptr(mean),
-                                                  rstd.data_ptr())
+    rows, cols = r.shape
+    weight, bias = _param(weight, cols, "weight"), _param(bias, cols, "bias")
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise ValueError("weight and bias must have one dtype")
+    p = weight if weight is not None else bias
+    lane = _lane(index)
+    _NORM.pack_into(lane.memory, 0, _dtype(x, "x"), mb.DTYPE_FP32 if p is None else _dtype(p, "weight and bias"), 1 if center else 0, cols, rows,
+                    eps, 0)
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    stat = x.shape[:-1]
+    mean = x.new_empty(stat, dtype=torch.float32) if center else None
+    rstd = x.new_empty(stat, dtype=torch.float32)
+    lane.ctx.muon_layer_norm_forward(lane.desc, r.data_ptr(), _ld(r), _ptr(weight), _ptr(bias), y.data_ptr(), cols, _ptr(mean), rstd.data_ptr(),
+                                     _raw_stream(index))
     return y, mean, rstd
 
 
@@ -118,7 +132,10 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
                         ) -> Tuple[torch.Tensor, Optional[torch.Tensor], Optional[torch.Tensor]]:
     """(dx, dweight, dbias); dweight is None without a weight, dbias unless `bias`.  The gradients have the weight's dtype (without a
     weight: bias_dtype, fp32 by default)."""
-    _on(x, dy, weight, mean, rstd)
+    index = _on(x, dy, weight, mean, rstd)
+    if index != _current_device():
+        with torch.cuda.device(index):
+            return layer_norm_backward(dy, x, weight, mean, rstd, bias, bias_dtype)
     if dy.shape != x.shape or dy.dtype != x.dtype:
         raise ValueError("dy must have the shape and dtype of x")
     if rstd.shape != x.shape[:-1] or (mean is not None and mean.shape != rstd.shape):
@@ -126,21 +143,21 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
     if rstd.dtype != torch.float32 or (mean is not None and mean.dtype != torch.float32):
         raise ValueError("mean and rstd must be fp32")
     r, g = _rows(x, "x"), _rows(dy, "dy")
-    weight = _param(weight, r.shape[1], "weight")
+    rows, cols = r.shape
+    weight = _param(weight, cols, "weight")
     mean, rstd = None if mean is None else mean.contiguous(), rstd.contiguous()
-    desc = _norm_desc(x, r, weight, None, 0.0, mean is not None)
     pt = weight.dtype if weight is not None else (bias_dtype or torch.float32)
     if pt not in _DTYPES:
         raise ValueError(f"gradients must be bf16 or fp32, not {pt}")
-    desc.param_dtype = _DTYPES[pt]
-    with _Guard(x):
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        dw = torch.empty(r.shape[1], dtype=pt, device=x.device) if weight is not None else None
-        db = torch.empty(r.shape[1], dtype=pt, device=x.device) if bias else None
-        n = mb.muon_layer_norm_workspace_bytes(desc) if dw is not None or db is not None else 0
-        ws = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
-        context(x.device).muon_layer_norm_backward(desc, g.data_ptr(), _ld(g), r.data_ptr(), _ld(r), _ptr(weight), _ptr(mean), rstd.data_ptr(),
-                                                   dx.data_ptr(), r.shape[1], _ptr(dw), _ptr(db), _ptr(ws), n)
+    lane = _lane(index)
+    _NORM.pack_into(lane.memory, 0, _dtype(x, "x"), _DTYPES[pt], 0 if mean is None else 1, cols, rows, 0.0, 0)
+    dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+    dw = torch.empty_like(weight) if weight is not None else None
+    db = None if not bias else torch.empty_like(weight) if weight is not None else x.new_empty(cols, dtype=pt)
+    n = mb.muon_layer_norm_workspace_bytes(lane.desc) if dw is not None or db is not None else 0
+    ws = x.new_empty(n, dtype=torch.uint8) if n else None
+    lane.ctx.muon_layer_norm_backward(lane.desc, g.data_ptr(), _ld(g), r.data_ptr(), _ld(r), _ptr(weight), _ptr(mean), rstd.data_ptr(),
+                                      dx.data_ptr(), cols, _ptr(dw), _ptr(db), _ptr(ws), n, _raw_stream(index))
     return dx, dw, db
 
 
@@ -171,18 +188,19 @@ def _heads4(t: torch.Tensor, what: str) -> torch.Tensor:
     """As [batch, tokens, heads, dim] with a contiguous last dimension (a copy only where it is not)."""
     if t.dim() == 3:
         t = t[None]
-    if t.dim() != 4:
+    elif t.dim() != 4:
         raise ValueError(f"{what} must be [batch, tokens, heads, dim] or [tokens, heads, dim]")
     return t if t.stride(3) == 1 or t.shape[3] == 1 else t.contiguous()
 
 
 def _heads(t: torch.Tensor) -> mb.Heads:
+    """The descriptor of a 4-D tensor as an object, for calls of the binding."""
     s = t.stride()
     return mb.Heads(t.data_ptr(), s[0], s[1], s[2])
 
 
 def _like(t: torch.Tensor) -> torch.Tensor:
-    return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 # ------------------------------------------------------------------------------------------------ rotary positions
@@ -195,18 +213,21 @@ def rotary_forward(tensors: Sequence[torch.Tensor], inv_freq, layout: str = "hal
     turned, the rest is copied.  layout: "half" (i with i + n/2) or "interleaved" (2i with 2i + 1).  positions: int32 [batch, tokens] on
     the device, else offset + 0, 1, 2...; offset is added to given positions too.  inverse turns back, which is the backward pass.
     out: tensors to write, which may be the inputs themselves."""
-    tensors = list(tensors)
     if not 1 <= len(tensors) <= 4:
         raise ValueError("one to four tensors")
-    if layout not in ("half", "interleaved"):
+    if layout != "half" and layout != "interleaved":
         raise ValueError("layout is 'half' or 'interleaved'")
     first = tensors[0]
-    _on(first, positions, *tensors[1:])
+    index = _on(first, positions, *tensors[1:])
+    if index != _current_device():
+        with torch.cuda.device(index):
+            return rotary_forward(tensors, inv_freq, layout, amplitude, positions, offset, inverse, out)
     freq = np.ascontiguousarray(inv_freq, dtype=np.float64)
     xs = [_heads4(t, "a tensor") for t in tensors]
     b, n, _, d = xs[0].shape
     for t in xs[1:]:
-        if t.shape[:2] != (b, n) or t.shape[3] != d or t.dtype != first.dtype:
+        s = t.shape
+        if s[0] != b or s[1] != n or s[3] != d or t.dtype != first.dtype:
             raise ValueError("the tensors must agree in batch, tokens, head size and dtype")
     if freq.ndim != 1 or not 1 <= freq.size <= d // 2:
         raise ValueError(f"inv_freq must hold one to {d // 2} frequencies for heads of {d}")
@@ -214,21 +235,23 @@ def rotary_forward(tensors: Sequence[torch.Tensor], inv_freq, layout: str = "hal
         if positions.dtype != torch.int32 or positions.numel() != b * n:
             raise ValueError("positions must be int32, one for each token")
         positions = positions.contiguous()
-    with _Guard(first):
-        if out is None:
-            res = [_like(t) for t in tensors]
-        else:
-            res = list(out)
-            if len(res) != len(tensors) or any(o.shape != t.shape or o.dtype != t.dtype or o.device != t.device for o, t in zip(res, tensors)):
-                raise ValueError("out must match the tensors")
-            if any(o.stride(-1) != 1 and o.shape[-1] > 1 for o in res):
-                raise ValueError("out must have a contiguous last dimension")
-        items = (mb.RotaryItem * len(xs))()
-        for i, (x, o) in enumerate(zip(xs, res)):
-            items[i].inp, items[i].out, items[i].heads = _heads(x), _heads(o if o.dim() == 4 else o[None]), x.shape[2]
-        desc = mb.RotaryDesc(_dtype(first, "the tensors"), 1 if layout == "interleaved" else 0, 1 if inverse else 0, d, 2 * freq.size, b, n,
-                             amplitude, freq.ctypes.data, _ptr(positions), offset)
-        context(first.device).muon_rotary(desc, items, len(xs))
+    if out is None:
+        res = [_like(t) for t in tensors]
+    else:
+        res = list(out)
+        if len(res) != len(tensors) or any(o.shape != t.shape or o.dtype != t.dtype or o.device != t.device for o, t in zip(res, tensors)):
+            raise ValueError("out must match the tensors")
+        if any(o.stride(-1) != 1 and o.shape[-1] > 1 for o in res):
+            raise ValueError("out must have a contiguous last dimension")
+    lane = _lane(index)
+    _ROTARY.pack_into(lane.memory, 0, _dtype(first, "the tensors"), 1 if layout == "interleaved" else 0, 1 if inverse else 0, d, 2 * freq.size, b, n,
+                      amplitude, freq.ctypes.data, _address(positions), offset)
+    at = _DESC_BYTES
+    for x, o in zip(xs, res):
+        s, t = x.stride(), o.stride()
+        _ITEM.pack_into(lane.memory, at, x.data_ptr(), s[0], s[1], s[2], o.data_ptr(), t[0] if len(t) == 4 else 0, t[-3], t[-2], x.shape[2], 0)
+        at += _ITEM.size
+    lane.ctx.muon_rotary(lane.desc, lane.desc + _DESC_BYTES, len(xs), _raw_stream(index))
     return tuple(res)
 
 
@@ -252,27 +275,25 @@ def rotary(tensors: Sequence[torch.Tensor], inv_freq, layout: str = "half", ampl
 
 
 # ------------------------------------------------------------------------------------------------ attention
-def _int32(t: Optional[torch.Tensor], n: Optional[int], what: str) -> Optional[torch.Tensor]:
-    if t is None:
-        return None
-    if t.dtype != torch.int32 or t.dim() != 1 or (n is not None and t.numel() != n):
-        raise ValueError(f"{what} must be a 1-D int32 tensor" + ("" if n is None else f" of {n}"))
+def _int32(t: torch.Tensor, n: int, what: str) -> torch.Tensor:
+    if t.dtype != torch.int32 or t.dim() != 1 or t.numel() != n:
+        raise ValueError(f"{what} must be a 1-D int32 tensor of {n}")
     return t.contiguous()
 
 
-def _attention_call(q, k, v, causal, window, scale, q_lens, k_lens, q_offsets, k_offsets):
-    """(descriptor, 4-D q, k, v, tensors the descriptor points into)"""
-    _on(q, k, v, q_lens, k_lens, q_offsets, k_offsets)
+def _attention_call(lane: _Lane, q, k, v, causal, window, scale, q_lens, k_lens, q_offsets, k_offsets):
+    """Packs the descriptor; gives q, k, v as 4-D tensors, and the tensors that the descriptor points into, to be kept for the call."""
     packed = q_offsets is not None or k_offsets is not None
-    if q.dim() != (3 if packed else 4) or k.dim() != q.dim() or v.dim() != q.dim():
+    dims = 3 if packed else 4
+    if q.dim() != dims or k.dim() != dims or v.dim() != dims:
         raise ValueError("q, k, v are [batch, tokens, heads, dim], or [tokens, heads, dim] with offsets")
-    if not (q.dtype == k.dtype == v.dtype):
+    if q.dtype != k.dtype or q.dtype != v.dtype:
         raise ValueError("q, k and v must have one dtype")
-    if k.shape != v.shape or k.shape[-1] != q.shape[-1] or (not packed and k.shape[0] != q.shape[0]):
-        raise ValueError(f"shapes do not fit: q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}")
     q4, k4, v4 = _heads4(q, "q"), _heads4(k, "k"), _heads4(v, "v")
     b, nq, hq, d = q4.shape
-    nk, hkv = k4.shape[1:3]
+    kb, nk, hkv, kd = ks = k4.shape
+    if v4.shape != ks or kd != d or kb != b:
+        raise ValueError(f"shapes do not fit: q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}")
     if hkv < 1 or hq < 1 or hq % hkv:
         raise ValueError(f"{hq} query heads cannot share {hkv} key heads evenly")
     nseq = 0
@@ -283,10 +304,13 @@ def _attention_call(q, k, v, causal, window, scale, q_lens, k_lens, q_offsets, k
         if nseq < 1:
             raise ValueError("offsets need at least two entries")
         q_offsets, k_offsets = _int32(q_offsets, nseq + 1, "q_offsets"), _int32(k_offsets, nseq + 1, "k_offsets")
-    q_lens, k_lens = _int32(q_lens, b, "q_lens"), _int32(k_lens, b, "k_lens")
-    desc = mb.AttentionDesc(_dtype(q, "q, k and v"), b, nq, nk, hq, hkv, d, 1 if causal else 0, window, d ** -0.5 if scale is None else scale,
-                            nseq, 0, _ptr(q_lens), _ptr(k_lens), _ptr(q_offsets), _ptr(k_offsets))
-    return desc, q4, k4, v4, (q_lens, k_lens, q_offsets, k_offsets)
+    if q_lens is not None:
+        q_lens = _int32(q_lens, b, "q_lens")
+    if k_lens is not None:
+        k_lens = _int32(k_lens, b, "k_lens")
+    _ATTENTION.pack_into(lane.memory, 0, _dtype(q, "q, k and v"), b, nq, nk, hq, hkv, d, 1 if causal else 0, window,
+                         d ** -0.5 if scale is None else scale, nseq, 0, _address(q_lens), _address(k_lens), _address(q_offsets), _address(k_offsets))
+    return q4, k4, v4, (hq, nq) if nseq else (b, hq, nq), (q_lens, k_lens, q_offsets, k_offsets)
 
 
 def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = True, window: int = 0, scale: Optional[float] = None,
@@ -296,13 +320,18 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal:
     contiguous last dimension.  q_lens, k_lens (int32 [batch]): how many tokens of each row count.  With q_offsets and k_offsets (int32
     [sequences + 1]) the tensors are [tokens, heads, dim] and hold packed sequences.  causal aligns the last query with the last key;
     window > 0 limits it to that many keys.  scale: dim ** -0.5 by default.  lse: fp32 [batch, heads, tokens] ([heads, tokens] packed)."""
-    desc, q4, k4, v4, keep = _attention_call(q, k, v, causal, window, scale, q_lens, k_lens, q_offsets, k_offsets)
-    with _Guard(q):
-        o = _like(q)
-        lse = torch.empty((desc.q_heads, desc.q_tokens) if desc.num_seqs else (desc.batch, desc.q_heads, desc.q_tokens), dtype=torch.float32,
-                          device=q.device)
-        context(q.device).muon_attention_forward(desc, _heads(q4), _heads(k4), _heads(v4), _heads(o if o.dim() == 4 else o[None]), lse.data_ptr())
-    return o, lse
+    index = _on(q, k, v, q_lens, k_lens, q_offsets, k_offsets)
+    if index != _current_device():
+        with torch.cuda.device(index):
+            return attention_forward(q, k, v, causal, window, scale, q_lens, k_lens, q_offsets, k_offsets)
+    lane = _lane(index)
+    q4, k4, v4, stat, keep = _attention_call(lane, q, k, v, causal, window, scale, q_lens, k_lens, q_offsets, k_offsets)
+    o, lse = _like(q4), q.new_empty(stat, dtype=torch.float32)
+    a, b, c, d, h = q4.stride(), k4.stride(), v4.stride(), o.stride(), lane.heads
+    _HEADS[4].pack_into(lane.memory, _DESC_BYTES, q4.data_ptr(), a[0], a[1], a[2], k4.data_ptr(), b[0], b[1], b[2], v4.data_ptr(), c[0], c[1], c[2],
+                        o.data_ptr(), d[0], d[1], d[2])
+    lane.ctx.muon_attention_forward(lane.desc, h[0], h[1], h[2], h[3], lse.data_ptr(), _raw_stream(index))
+    return o if len(stat) == 3 else o[0], lse
 
 
 def attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
@@ -311,22 +340,28 @@ def attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: to
                        q_offsets: Optional[torch.Tensor] = None, k_offsets: Optional[torch.Tensor] = None
                        ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """(dq, dk, dv) from what `attention_forward` took and gave."""
-    desc, q4, k4, v4, keep = _attention_call(q, k, v, causal, window, scale, q_lens, k_lens, q_offsets, k_offsets)
-    _on(q, do, o, lse)
+    index = _on(q, k, v, do, o, lse, q_lens, k_lens, q_offsets, k_offsets)
+    if index != _current_device():
+        with torch.cuda.device(index):
+            return attention_backward(do, q, k, v, o, lse, causal, window, scale, q_lens, k_lens, q_offsets, k_offsets)
+    lane = _lane(index)
+    q4, k4, v4, stat, keep = _attention_call(lane, q, k, v, causal, window, scale, q_lens, k_lens, q_offsets, k_offsets)
     if do.shape != q.shape or o.shape != q.shape or do.dtype != q.dtype or o.dtype != q.dtype:
         raise ValueError("do and o must have the shape and dtype of q")
-    want = (desc.q_heads, desc.q_tokens) if desc.num_seqs else (desc.batch, desc.q_heads, desc.q_tokens)
-    if lse.shape != want or lse.dtype != torch.float32:
-        raise ValueError(f"lse must be fp32 of shape {want}")
+    if lse.shape != stat or lse.dtype != torch.float32:
+        raise ValueError(f"lse must be fp32 of shape {tuple(stat)}")
     do4, o4, lse = _heads4(do, "do"), _heads4(o, "o"), lse.contiguous()
-    with _Guard(q):
-        dq, dk, dv = _like(q), _like(k), _like(v)
-        n = mb.muon_attention_workspace_bytes(desc)
-        ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
-        up = (lambda t: t[None]) if desc.num_seqs else (lambda t: t)
-        context(q.device).muon_attention_backward(desc, _heads(do4), _heads(q4), _heads(k4), _heads(v4), _heads(o4), lse.data_ptr(),
-                                                  _heads(up(dq)), _heads(up(dk)), _heads(up(dv)), _ptr(ws), n)
-    return dq, dk, dv
+    dq, dk, dv = _like(q4), _like(k4), _like(v4)
+    n = mb.muon_attention_workspace_bytes(lane.desc)
+    ws = q.new_empty(n, dtype=torch.uint8) if n else None
+    values = []
+    for t in (do4, q4, k4, v4, o4, dq, dk, dv):
+        s = t.stride()
+        values += (t.data_ptr(), s[0], s[1], s[2])
+    _HEADS[8].pack_into(lane.memory, _DESC_BYTES, *values)
+    h = lane.heads
+    lane.ctx.muon_attention_backward(lane.desc, h[0], h[1], h[2], h[3], h[4], lse.data_ptr(), h[5], h[6], h[7], _ptr(ws), n, _raw_stream(index))
+    return (dq, dk, dv) if len(stat) == 3 else (dq[0], dk[0], dv[0])
 
 
 class _Attention(torch.autograd.Function):
