@@ -23,7 +23,10 @@ int device_of(const muon_ctx* ctx, int* sms) {
 }
 
 int launched(muon_ctx* ctx, int n) {
-  if (n < 0) return n;
+  if (n < 0) {
+    (void)cudaGetLastError();      // a refused launch is this call's error, not the next one's
+    return n;
+  }
   ctx->launches += n;
   return MUON_OK;
 }
@@ -114,6 +117,7 @@ int muon_layer_norm_forward(muon_ctx_t* ctx, const muon_norm_desc_t* desc, const
   int sms = 0;
   if ((rc = device_of(ctx, &sms)) != MUON_OK) return rc;
   NormArgs a = norm_args(desc);
+  a.device = ctx->device;
   a.x = x;
   a.ldx = ldx;
   a.weight = weight;
@@ -157,6 +161,7 @@ int muon_layer_norm_backward(muon_ctx_t* ctx, const muon_norm_desc_t* desc, cons
   int sms = 0;
   if ((rc = device_of(ctx, &sms)) != MUON_OK) return rc;
   NormArgs a = norm_args(desc);
+  a.device = ctx->device;
   a.x = x;
   a.ldx = ldx;
   a.dy = dy;
@@ -311,7 +316,7 @@ int muon_attention_backward(muon_ctx_t* ctx, const muon_attention_desc_t* desc, 
   a.rows = static_cast<float*>(workspace);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int rows = launch_attention_rows(a, desc->dtype, st);
-  if (rows < 0) return rows;
+  if (rows < 0) return launched(ctx, rows);
   ctx->launches += rows;
   if (desc->dtype == MUON_DTYPE_BF16 && attention_backward_tc_takes(a)) return launched(ctx, launch_attention_backward_tc(ctx, a, st));
   return launched(ctx, launch_attention_backward_simt(a, desc->dtype, st));
