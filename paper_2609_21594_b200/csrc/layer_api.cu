@@ -118,6 +118,7 @@ int muon_layer_norm_forward(muon_ctx_t* ctx, const muon_norm_desc_t* desc, const
   if ((rc = device_of(ctx, &sms)) != MUON_OK) return rc;
   NormArgs a = norm_args(desc);
   a.device = ctx->device;
+  a.status = ctx->d_status;
   a.x = x;
   a.ldx = ldx;
   a.weight = weight;
@@ -162,6 +163,7 @@ int muon_layer_norm_backward(muon_ctx_t* ctx, const muon_norm_desc_t* desc, cons
   if ((rc = device_of(ctx, &sms)) != MUON_OK) return rc;
   NormArgs a = norm_args(desc);
   a.device = ctx->device;
+  a.status = ctx->d_status;
   a.x = x;
   a.ldx = ldx;
   a.dy = dy;

@@ -15,6 +15,7 @@
 #include <cuda_bf16.h>
 
 #include "layer_ops.h"
+#include "tc_common.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -27,157 +28,6 @@ __device__ __forceinline__ float up(float v) { return v; }
 __device__ __forceinline__ float up(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ void down(float* p, float v) { *p = v; }
 __device__ __forceinline__ void down(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
-
-__device__ __forceinline__ float param_at(const void* p, int dtype, float missing, int c) {
-  if (!p) return missing;
-  return dtype == MUON_DTYPE_BF16 ? up(static_cast<const __nv_bfloat16*>(p)[c]) : static_cast<const float*>(p)[c];
-}
-
-__device__ __forceinline__ void copy_piece(uint32_t dst, const void* src, bool in) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int LEFT> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
-
-// Columns of thread t of a row: piece i of N elements starts at (i * TPR + t) * N.  In pieces of 16 bytes the thread asks for a row ahead
-// of time (fetch) and takes it from its places of the ring; element by element (rows without the alignment) it reads the row directly.
-template <typename T, int N, int TPR, int EPT, int THREADS>
-struct Rows {
-  static constexpr bool kRing = N * sizeof(T) == 16;
-  static constexpr int kPieces = EPT / N;
-  static constexpr int kStageBytes = kRing ? THREADS * kPieces * 16 : 0;
-  __device__ static __forceinline__ void fetch(uint32_t stage, const T* row, int t, int cols) {
-    if constexpr (kRing) {
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        const int c = (i * TPR + t) * N;
-        copy_piece(stage + uint32_t(i * THREADS + threadIdx.x) * 16u, c < cols ? row + c : row, c < cols);
-      }
-    }
-  }
-  __device__ static __forceinline__ void raw(Pack<T, N> (&p)[kPieces], uint32_t stage, const T* row, int t, int cols) {
-    if constexpr (kRing) {
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        uint32_t* u = reinterpret_cast<uint32_t*>(&p[i]);
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
-                     : "r"(stage + uint32_t(i * THREADS + threadIdx.x) * 16u));
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < EPT; ++i) {
-        const int c = i * TPR + t;
-        if (c < cols) p[i].v[0] = row[c];
-        else down(&p[i].v[0], 0.f);
-      }
-    }
-  }
-  __device__ static __forceinline__ void take(float (&v)[EPT], uint32_t stage, const T* row, int t, int cols) {
-    Pack<T, N> p[kPieces];
-    raw(p, stage, row, t, cols);
-#pragma unroll
-    for (int i = 0; i < EPT; ++i) v[i] = up(p[i / N].v[i % N]);
-  }
-};
-
-// ------------------------------------------------------------------ forward
-constexpr int FWD_THREADS = 512, FWD_STAGES = 2;
-
-// Sum over the TPR threads of a row, the same in all of them.  The warps of a row meet at a named barrier of their own; `buf` has two
-// halves that alternate, so one meeting per sum is enough.
-template <int TPR>
-__device__ __forceinline__ float group_sum(float v, float* buf, int& half) {
-#pragma unroll
-  for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-  if (TPR == 32) return v;
-  constexpr int W = TPR / 32;
-  const int g = threadIdx.x / TPR;
-  float* b = buf + (half * (FWD_THREADS / TPR) + g) * W;
-  half ^= 1;
-  if ((threadIdx.x & 31) == 0) b[(threadIdx.x % TPR) / 32] = v;
-  asm volatile("bar.sync %0, %1;" ::"r"(g + 1), "n"(TPR) : "memory");
-  float s = 0.f;
-#pragma unroll
-  for (int i = 0; i < W; ++i) s += b[i];
-  return s;
-}
-
-template <typename T, int N, int TPR, int EPT, int BLOCKS, bool SHARED_PARAMS>
-__global__ void __launch_bounds__(FWD_THREADS, BLOCKS) norm_forward_kernel(const NormArgs a) {
-  using RW = Rows<T, N, TPR, EPT, FWD_THREADS>;
-  extern __shared__ __align__(16) float param[];      // weight, then bias (unless they stay in global memory); then the ring
-  __shared__ float buf[2 * FWD_THREADS / 32];
-  constexpr int G = FWD_THREADS / TPR;
-  const int t = threadIdx.x % TPR, pitch = SHARED_PARAMS ? (a.cols + 3) & ~3 : 0;
-  const uint32_t ring = uint32_t(__cvta_generic_to_shared(param + 2 * pitch));
-  const T* x = static_cast<const T*>(a.x);
-  T* y = static_cast<T*>(a.out);
-  const int64_t step = int64_t(gridDim.x) * G;
-  int64_t r = int64_t(blockIdx.x) * G + threadIdx.x / TPR;
-  if (r < a.rows) RW::fetch(ring, x + r * a.ldx, t, a.cols);
-  copy_commit();
-  for (int c = threadIdx.x; SHARED_PARAMS && c < a.cols; c += FWD_THREADS) {
-    param[c] = param_at(a.weight, a.param_dtype, 1.f, c);
-    param[pitch + c] = param_at(a.bias, a.param_dtype, 0.f, c);
-  }
-  __syncthreads();
-  const float inv = 1.f / float(a.cols);
-  int half = 0;
-  uint32_t stage = 0;
-  for (; r < a.rows; r += step, stage ^= 1) {
-    if (r + step < a.rows) RW::fetch(ring + (stage ^ 1) * RW::kStageBytes, x + (r + step) * a.ldx, t, a.cols);
-    copy_commit();
-    copy_wait<1>();
-    float v[EPT], mean = 0.f;
-    RW::take(v, ring + stage * RW::kStageBytes, x + r * a.ldx, t, a.cols);
-    if (a.center) {
-      float s[2] = {0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < EPT; ++i) s[i & 1] += v[i];
-      mean = group_sum<TPR>(s[0] + s[1], buf, half) * inv;
-#pragma unroll
-      for (int i = 0; i < EPT; ++i) v[i] -= mean;
-    }
-    float q[2] = {0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < EPT / N; ++i)
-      if ((i * TPR + t) * N < a.cols) {
-#pragma unroll
-        for (int e = 0; e < N; ++e) q[(i * N + e) & 1] = fmaf(v[i * N + e], v[i * N + e], q[(i * N + e) & 1]);
-      }
-    const float rstd = 1.f / sqrtf(group_sum<TPR>(q[0] + q[1], buf, half) * inv + a.eps);
-#pragma unroll
-    for (int i = 0; i < EPT / N; ++i) {
-      const int c = (i * TPR + t) * N;
-      if (c >= a.cols) continue;
-      Pack<T, N> o;
-      if constexpr (!SHARED_PARAMS) {
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-          down(&o.v[e], fmaf(v[i * N + e] * rstd, param_at(a.weight, a.param_dtype, 1.f, c + e), param_at(a.bias, a.param_dtype, 0.f, c + e)));
-      } else if constexpr (N >= 4) {
-#pragma unroll
-        for (int e = 0; e < N; e += 4) {
-          const float4 w = *reinterpret_cast<const float4*>(param + c + e), b = *reinterpret_cast<const float4*>(param + pitch + c + e);
-          down(&o.v[e], fmaf(v[i * N + e] * rstd, w.x, b.x));
-          down(&o.v[e + 1], fmaf(v[i * N + e + 1] * rstd, w.y, b.y));
-          down(&o.v[e + 2], fmaf(v[i * N + e + 2] * rstd, w.z, b.z));
-          down(&o.v[e + 3], fmaf(v[i * N + e + 3] * rstd, w.w, b.w));
-        }
-      } else {
-        down(&o.v[0], fmaf(v[i] * rstd, param[c], param[pitch + c]));
-      }
-      *reinterpret_cast<Pack<T, N>*>(y + r * a.ldo + c) = o;
-    }
-    if (t == 0) {
-      if (a.mean) a.mean[r] = mean;
-      a.rstd[r] = rstd;
-    }
-  }
-}
-
-// ------------------------------------------------------------------ backward
-constexpr int BWD_EPT = 16, BWD_STAGES = 3;
 
 // Two fp32 values in one instruction: half the issue slots of the arithmetic, which would otherwise bound the kernel.
 __device__ __forceinline__ uint64_t two(float a, float b) {
@@ -205,6 +55,214 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
+
+__device__ __forceinline__ uint64_t twice(float a) { return two(a, a); }
+
+// Values 2 i and 2 i + 1 of a thread's pieces.  Two bf16 share a word: the upper one is its fp32 value with the lower bits cleared.
+template <typename T, int N>
+__device__ __forceinline__ uint64_t pair_up(const Pack<T, N>* p, int i) {
+  if constexpr (sizeof(T) == 2 && N > 1) {
+    const uint32_t w = reinterpret_cast<const uint32_t*>(&p[2 * i / N])[2 * i % N / 2];
+    return two(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  } else {
+    return two(up(p[2 * i / N].v[2 * i % N]), up(p[(2 * i + 1) / N].v[(2 * i + 1) % N]));
+  }
+}
+template <typename T, int N>
+__device__ __forceinline__ void pair_down(Pack<T, N>* p, int i, uint64_t v) {
+  const float2 f = both(v);
+  if constexpr (sizeof(T) == 2 && N > 1) {
+    *reinterpret_cast<__nv_bfloat162*>(&p[2 * i / N].v[2 * i % N]) = __floats2bfloat162_rn(f.x, f.y);
+  } else {
+    down(&p[2 * i / N].v[2 * i % N], f.x);
+    down(&p[(2 * i + 1) / N].v[(2 * i + 1) % N], f.y);
+  }
+}
+
+__device__ __forceinline__ float param_at(const void* p, int dtype, float missing, int c) {
+  if (!p) return missing;
+  return dtype == MUON_DTYPE_BF16 ? up(static_cast<const __nv_bfloat16*>(p)[c]) : static_cast<const float*>(p)[c];
+}
+
+// Columns of thread t of a row: piece i of N elements starts at (i * TPR + t) * N.  Rows in 16-byte pieces come through a ring in shared
+// memory: one thread of the row's group asks for whole rows ahead of time with bulk copies that arrive on an mbarrier.  Other rows
+// (without the alignment) are read directly, element by element.
+template <typename T, int N, int TPR, int EPT>
+struct Rows {
+  static constexpr bool kRing = N * sizeof(T) == 16;
+  static constexpr int kPieces = EPT / N;
+  static constexpr int kRowBytes = kRing ? TPR * kPieces * 16 : 0;      // room for a row of the widest kind
+  __device__ static __forceinline__ void raw(Pack<T, N> (&p)[kPieces], uint32_t place, const T* row, int t, int cols) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int c = (i * TPR + t) * N;
+      if constexpr (kRing) {
+        uint32_t* u = reinterpret_cast<uint32_t*>(&p[i]);
+        u[0] = u[1] = u[2] = u[3] = 0;
+        if (c < cols)
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
+                       : "r"(place + uint32_t(i * TPR + t) * 16u));
+      } else {
+        if (c < cols) p[i].v[0] = row[c];
+        else down(&p[i].v[0], 0.f);
+      }
+    }
+  }
+};
+
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+// Bounded like every wait of the library; a copy that never arrives is recorded and the row computed from what is there.
+__device__ __forceinline__ void await_copy(uint32_t bar, uint32_t phase, int32_t* status) {
+  if (tc::mbar_try(bar, phase)) return;
+  const long long t0 = clock64();
+  while (!tc::mbar_try(bar, phase))
+    if (clock64() - t0 > tc::WAIT_CYCLES) {
+      atomicExch(status, 41);
+      return;
+    }
+}
+
+// ------------------------------------------------------------------ forward
+constexpr int FWD_THREADS = 512, FWD_STAGES = 2;
+
+// Sum over the TPR threads of a row, the same in all of them.  The warps of a row meet at a named barrier of their own; `buf` has two
+// halves that alternate, so one meeting per sum is enough.
+template <int TPR>
+__device__ __forceinline__ float group_sum(float v, float* buf, int& half) {
+#pragma unroll
+  for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+  if (TPR == 32) return v;
+  constexpr int W = TPR / 32;
+  const int g = threadIdx.x / TPR;
+  float* b = buf + (half * (FWD_THREADS / TPR) + g) * W;
+  half ^= 1;
+  if ((threadIdx.x & 31) == 0) b[(threadIdx.x % TPR) / 32] = v;
+  asm volatile("bar.sync %0, %1;" ::"r"(g + 1), "n"(TPR) : "memory");
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < W; ++i) s += b[i];
+  return s;
+}
+
+template <typename T, int N, int TPR, int EPT, int BLOCKS, bool SHARED_PARAMS>
+__global__ void __launch_bounds__(FWD_THREADS, BLOCKS) norm_forward_kernel(const NormArgs a) {
+  using RW = Rows<T, N, TPR, EPT>;
+  extern __shared__ __align__(16) float param[];      // weight, then bias (unless they stay in global memory); then the ring
+  __shared__ float buf[2 * FWD_THREADS / 32];
+  constexpr int G = FWD_THREADS / TPR;
+  __shared__ __align__(8) uint64_t bars[G * FWD_STAGES];
+  const int t = threadIdx.x % TPR, pitch = SHARED_PARAMS ? (a.cols + 3) & ~3 : 0;
+  const int group = threadIdx.x / TPR;
+  const uint32_t ring = uint32_t(__cvta_generic_to_shared(param + 2 * pitch)) + uint32_t(group * FWD_STAGES * RW::kRowBytes);
+  const uint32_t bar = uint32_t(__cvta_generic_to_shared(bars + group * FWD_STAGES));
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < G * FWD_STAGES; ++i) tc::mbar_init(uint32_t(__cvta_generic_to_shared(bars + i)), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  for (int c = threadIdx.x; SHARED_PARAMS && c < a.cols; c += FWD_THREADS) {
+    param[c] = param_at(a.weight, a.param_dtype, 1.f, c);
+    param[pitch + c] = param_at(a.bias, a.param_dtype, 0.f, c);
+  }
+  __syncthreads();
+  const T* x = static_cast<const T*>(a.x);
+  T* y = static_cast<T*>(a.out);
+  const int64_t step = int64_t(gridDim.x) * G;
+  const int64_t r0 = int64_t(blockIdx.x) * G + group;
+  auto fetch = [&](uint32_t stage, int64_t r) {
+    if constexpr (RW::kRing)
+      if (t == 0 && r < a.rows) {
+        const uint32_t bytes = uint32_t(a.cols) * uint32_t(sizeof(T));
+        tc::mbar_expect_tx(bar + stage * 8u, bytes);
+        bulk_copy(ring + stage * uint32_t(RW::kRowBytes), x + r * a.ldx, bytes, bar + stage * 8u);
+      }
+  };
+#pragma unroll
+  for (int k = 0; k < FWD_STAGES; ++k) fetch(k, r0 + k * step);
+  const float inv = 1.f / float(a.cols);
+  int half = 0;
+  uint32_t stage = 0, phase = 0;
+  for (int64_t r = r0; r < a.rows; r += step) {
+    if constexpr (RW::kRing) await_copy(bar + stage * 8u, phase, a.status);
+    Pack<T, N> p[EPT / N];
+    RW::raw(p, ring + stage * uint32_t(RW::kRowBytes), x + r * a.ldx, t, a.cols);
+    uint64_t v[EPT / 2];
+    float mean = 0.f;
+#pragma unroll
+    for (int i = 0; i < EPT / 2; ++i) v[i] = pair_up<T, N>(p, i);
+    if (a.center) {
+      uint64_t s[2] = {0, 0};
+#pragma unroll
+      for (int i = 0; i < EPT / 2; ++i) s[i & 1] = add2(s[i & 1], v[i]);
+      const float2 f = both(add2(s[0], s[1]));
+      mean = group_sum<TPR>(f.x + f.y, buf, half) * inv;
+#pragma unroll
+      for (int i = 0; i < EPT / 2; ++i) v[i] = add2(v[i], twice(-mean));
+    }
+    // columns past the end are zeros that the mean has been taken from: they must not count
+    if constexpr (N > 1) {
+#pragma unroll
+      for (int i = 0; i < EPT / N; ++i)
+        if ((i * TPR + t) * N >= a.cols) {
+#pragma unroll
+          for (int e = 0; e < N / 2; ++e) v[i * N / 2 + e] = 0;
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < EPT / 2; ++i) {
+        const float2 f = both(v[i]);
+        v[i] = two(2 * i * TPR + t < a.cols ? f.x : 0.f, (2 * i + 1) * TPR + t < a.cols ? f.y : 0.f);
+      }
+    }
+    uint64_t q[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < EPT / 2; ++i) q[i & 1] = fma2(v[i], v[i], q[i & 1]);
+    const float2 qq = both(add2(q[0], q[1]));
+    const float rstd = 1.f / sqrtf(group_sum<TPR>(qq.x + qq.y, buf, half) * inv + a.eps);
+    if constexpr (TPR == 32) __syncwarp();
+    fetch(stage, r + FWD_STAGES * step);              // everybody has read the row: the sum above was a meeting
+    if (++stage == FWD_STAGES) {
+      stage = 0;
+      phase ^= 1;
+    }
+    auto scaled = [&](int i, float w0, float w1, float b0, float b1) {
+      pair_down<T, N>(p, i, fma2(mul2(v[i], twice(rstd)), two(w0, w1), two(b0, b1)));
+    };
+    T* out = y + r * a.ldo;
+    if constexpr (!SHARED_PARAMS || N == 1) {
+#pragma unroll
+      for (int i = 0; i < EPT / 2; ++i) {
+        const int c = (2 * i / N * TPR + t) * N + 2 * i % N, d = ((2 * i + 1) / N * TPR + t) * N + (2 * i + 1) % N;
+        auto weight = [&](int k) { return k >= a.cols ? 0.f : SHARED_PARAMS ? param[k] : param_at(a.weight, a.param_dtype, 1.f, k); };
+        auto bias = [&](int k) { return k >= a.cols ? 0.f : SHARED_PARAMS ? param[pitch + k] : param_at(a.bias, a.param_dtype, 0.f, k); };
+        scaled(i, weight(c), weight(d), bias(c), bias(d));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < EPT / 4; ++i) {
+        const int c = min((4 * i / N * TPR + t) * N + 4 * i % N, pitch - 4);
+        const float4 w = *reinterpret_cast<const float4*>(param + c), b = *reinterpret_cast<const float4*>(param + pitch + c);
+        scaled(2 * i, w.x, w.y, b.x, b.y);
+        scaled(2 * i + 1, w.z, w.w, b.z, b.w);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < EPT / N; ++i) {
+      const int c = (i * TPR + t) * N;
+      if (c < a.cols) *reinterpret_cast<Pack<T, N>*>(out + c) = p[i];
+    }
+    if (t == 0) {
+      if (a.mean) a.mean[r] = mean;
+      a.rstd[r] = rstd;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ backward
+constexpr int BWD_EPT = 16, BWD_STAGES = 3;
 
 // K = 2 or 4 sums over the threads of a row group (a warp, a block, or the two blocks of a cluster), the same in every thread.  Lanes trade
 // values as they halve the distance, so K sums over a warp take K + 3 shuffles at most, and afterwards lane 32 / K * k holds sum k.  Two halves of
@@ -261,7 +319,7 @@ template <typename T, int N> constexpr int kRowsAtATime = sizeof(T) == 2 && N > 
 template <typename T, int N, int TPR, int CLUSTER, int BLOCKS>
 __global__ void __launch_bounds__(Geometry<TPR>::kThreads, BLOCKS) norm_backward_kernel(const NormArgs a) {
   constexpr int G = Geometry<TPR>::kGroups, THREADS = Geometry<TPR>::kThreads, EPT = BWD_EPT, R = kRowsAtATime<T, N>, H = EPT / 2;
-  using RW = Rows<T, N, TPR, EPT, THREADS>;
+  using RW = Rows<T, N, TPR, EPT>;
   extern __shared__ __align__(16) float dynamic[];    // the ring; one warp per row: at the end [8][2][32 * EPT] sums
   __shared__ float buf[2 * 2 * R * (TPR / 32) * CLUSTER];
   const int t = threadIdx.x % TPR;
@@ -271,20 +329,30 @@ __global__ void __launch_bounds__(Geometry<TPR>::kThreads, BLOCKS) norm_backward
   const T* x = static_cast<const T*>(a.x) + c0;
   const T* dy = static_cast<const T*>(a.dy) + c0;
   T* dx = static_cast<T*>(a.out) + c0;
-  const uint32_t ring = uint32_t(__cvta_generic_to_shared(dynamic));
-  auto place = [&](uint32_t stage, int k, int which) { return ring + ((stage * R + k) * 2 + which) * uint32_t(RW::kStageBytes); };
-  const int64_t step = int64_t(gridDim.x / CLUSTER) * G * R, r0 = (int64_t(blockIdx.x / CLUSTER) * G + threadIdx.x / TPR) * R;
+  __shared__ __align__(8) uint64_t bars[G * BWD_STAGES];
+  const int group = threadIdx.x / TPR;
+  const uint32_t ring = uint32_t(__cvta_generic_to_shared(dynamic)) + uint32_t(group * BWD_STAGES * R * 2 * RW::kRowBytes);
+  const uint32_t bar = uint32_t(__cvta_generic_to_shared(bars + group * BWD_STAGES));
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < G * BWD_STAGES; ++i) tc::mbar_init(uint32_t(__cvta_generic_to_shared(bars + i)), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  auto place = [&](uint32_t stage, int k, int which) { return ring + ((stage * R + k) * 2 + which) * uint32_t(RW::kRowBytes); };
+  const int64_t step = int64_t(gridDim.x / CLUSTER) * G * R, r0 = (int64_t(blockIdx.x / CLUSTER) * G + group) * R;
   auto fetch = [&](uint32_t stage, int64_t r) {
-#pragma unroll
-    for (int k = 0; k < R; ++k) {                      // a row past the end is one of zeros
-      const int has = r + k < a.rows ? cols : 0;
-      RW::fetch(place(stage, k, 0), has ? x + (r + k) * a.ldx : x, t, has);
-      RW::fetch(place(stage, k, 1), has ? dy + (r + k) * a.lddy : dy, t, has);
-    }
-    copy_commit();
+    if constexpr (RW::kRing)
+      if (t == 0 && r < a.rows && cols > 0) {
+        const uint32_t bytes = uint32_t(cols) * uint32_t(sizeof(T)), rows = R == 2 && r + 1 < a.rows ? 2 : 1;
+        tc::mbar_expect_tx(bar + stage * 8u, 2 * rows * bytes);
+        for (uint32_t k = 0; k < rows; ++k) {
+          bulk_copy(place(stage, k, 0), x + (r + k) * a.ldx, bytes, bar + stage * 8u);
+          bulk_copy(place(stage, k, 1), dy + (r + k) * a.lddy, bytes, bar + stage * 8u);
+        }
+      }
   };
 #pragma unroll
-  for (int k = 0; k < BWD_STAGES - 1; ++k) fetch(k, r0 + k * step);
+  for (int k = 0; k < BWD_STAGES; ++k) fetch(k, r0 + k * step);
   uint64_t w[H], dw[H], db[H];
 #pragma unroll
   for (int i = 0; i < H; ++i) {
@@ -298,44 +366,38 @@ __global__ void __launch_bounds__(Geometry<TPR>::kThreads, BLOCKS) norm_backward
     dw[i] = db[i] = 0;
   }
   const float inv = 1.f / float(a.cols);
-  float next_mean[R], next_rstd[R];
-  auto statistics = [&](int64_t r) {                  // a row past the end has rstd = 0: it adds nothing
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-      next_mean[k] = a.mean && r + k < a.rows ? a.mean[r + k] : 0.f;
-      next_rstd[k] = r + k < a.rows ? a.rstd[r + k] : 0.f;
-    }
+  // Lane 2 k + 1 of every warp holds rstd of row k, lane 2 k its mean, two steps ahead; a row past the end has rstd = 0 and adds nothing.
+  auto statistic = [&](int64_t r) {
+    const int lane = threadIdx.x & 31;
+    const float* from = lane & 1 ? a.rstd : a.mean;
+    return lane < 2 * R && from && r + lane / 2 < a.rows ? from[r + lane / 2] : 0.f;
   };
-  statistics(r0);
+  float stat = statistic(r0), stat_next = statistic(r0 + step);
   int half = 0;
-  uint32_t stage = 0;
+  uint32_t stage = 0, phase = 0;
   for (int64_t r = r0; r < a.rows; r += step) {
-    fetch((stage + BWD_STAGES - 1) % BWD_STAGES, r + (BWD_STAGES - 1) * step);
     float mean[R], rstd[R];
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      mean[k] = next_mean[k];
-      rstd[k] = next_rstd[k];
+      mean[k] = __shfl_sync(0xffffffffu, stat, 2 * k);
+      rstd[k] = __shfl_sync(0xffffffffu, stat, 2 * k + 1);
     }
-    statistics(r + step);
-    copy_wait<BWD_STAGES - 1>();
+    stat = stat_next;
+    stat_next = statistic(r + 2 * step);
+    if constexpr (RW::kRing)
+      if (cols > 0) await_copy(bar + stage * 8u, phase, a.status);
     float s[2 * R];
-    Pack<T, N> px[R][EPT / N], py[R][EPT / N];
-    // (x - mean, dy) of values 2 i and 2 i + 1; columns past the end have dy = 0 and weight 0
-    auto pair = [&](int k, int i, uint64_t& xc, uint64_t& d) {
-      xc = add2(two(up(px[k][2 * i / N].v[2 * i % N]), up(px[k][(2 * i + 1) / N].v[(2 * i + 1) % N])), two(-mean[k], -mean[k]));
-      d = two(up(py[k][2 * i / N].v[2 * i % N]), up(py[k][(2 * i + 1) / N].v[(2 * i + 1) % N]));
-    };
+    Pack<T, N> px[R][EPT / N], py[R][EPT / N];        // columns past the end have dy = 0 and weight 0
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      RW::raw(px[k], place(stage, k, 0), x + (r + k) * a.ldx, t, cols);
-      RW::raw(py[k], place(stage, k, 1), dy + (r + k) * a.lddy, t, cols);
+      const int has = r + k < a.rows ? cols : 0;      // a row past the end is one of zeros
+      RW::raw(px[k], place(stage, k, 0), x + (r + k) * a.ldx, t, has);
+      RW::raw(py[k], place(stage, k, 1), dy + (r + k) * a.lddy, t, has);
       uint64_t s0 = 0, s1 = 0;
 #pragma unroll
       for (int i = 0; i < H; ++i) {
-        uint64_t xc, d;
-        pair(k, i, xc, d);
-        dw[i] = fma2(mul2(xc, two(rstd[k], rstd[k])), d, dw[i]);
+        const uint64_t xc = add2(pair_up<T, N>(px[k], i), twice(-mean[k])), d = pair_up<T, N>(py[k], i);
+        dw[i] = fma2(mul2(xc, twice(rstd[k])), d, dw[i]);
         db[i] = add2(db[i], d);
         const uint64_t g = mul2(d, w[i]);
         s0 = add2(s0, g);
@@ -345,29 +407,25 @@ __global__ void __launch_bounds__(Geometry<TPR>::kThreads, BLOCKS) norm_backward
       s[2 * k] = f0.x + f0.y;
       s[2 * k + 1] = (f1.x + f1.y) * rstd[k];
     }
-    stage = (stage + 1) % BWD_STAGES;
     row_sums<2 * R, TPR, CLUSTER>(s, buf, half);
+    fetch(stage, r + BWD_STAGES * step);              // everybody has read the rows: the sums above were a meeting
+    if (++stage == BWD_STAGES) {
+      stage = 0;
+      phase ^= 1;
+    }
 #pragma unroll
     for (int k = 0; k < R; ++k) {                     // dx = rstd g - rstd mean(g) - (x - mean) rstd^2 mean(g xh)
       const float m1 = a.mean ? -rstd[k] * (s[2 * k] * inv) : 0.f, m2 = -rstd[k] * rstd[k] * (s[2 * k + 1] * inv);
       const int end = r + k < a.rows ? cols : 0;
-      float v[EPT];
 #pragma unroll
       for (int i = 0; i < H; ++i) {
-        uint64_t xc, d;
-        pair(k, i, xc, d);
-        const float2 o = both(fma2(mul2(d, w[i]), two(rstd[k], rstd[k]), fma2(xc, two(m2, m2), two(m1, m1))));
-        v[2 * i] = o.x;
-        v[2 * i + 1] = o.y;
+        const uint64_t xc = add2(pair_up<T, N>(px[k], i), twice(-mean[k])), g = mul2(pair_up<T, N>(py[k], i), w[i]);
+        pair_down<T, N>(px[k], i, fma2(g, twice(rstd[k]), fma2(xc, twice(m2), twice(m1))));
       }
 #pragma unroll
       for (int i = 0; i < EPT / N; ++i) {
         const int c = (i * TPR + t) * N;
-        if (c >= end) continue;
-        Pack<T, N> o;
-#pragma unroll
-        for (int e = 0; e < N; ++e) down(&o.v[e], v[i * N + e]);
-        *reinterpret_cast<Pack<T, N>*>(dx + (r + k) * a.ldo + c) = o;
+        if (c < end) *reinterpret_cast<Pack<T, N>*>(dx + (r + k) * a.ldo + c) = px[k][i];
       }
     }
   }
@@ -377,7 +435,6 @@ __global__ void __launch_bounds__(Geometry<TPR>::kThreads, BLOCKS) norm_backward
   float* out = a.parts + int64_t(blockIdx.x / CLUSTER) * 2 * a.cols + c0;
   if constexpr (TPR == 32) {                          // add the block's warps in order
     const int wp = threadIdx.x / 32;
-    copy_wait<0>();
     __syncthreads();                                  // the ring's memory is free
 #pragma unroll
     for (int i = 0; i < EPT; ++i) {
@@ -441,7 +498,7 @@ int forward(const NormArgs& a, int sms, cudaStream_t st) {
   // fp32 rows of more than 8192 columns: 128 KiB of ring, and as much again of weight and bias would not fit
   constexpr bool SHARED_PARAMS = !(N == 4 && EPT == 32);
   constexpr int BLOCKS = !SHARED_PARAMS ? 1 : EPT > 8 ? 2 : 3;
-  const int bytes = (SHARED_PARAMS ? 2 * ((a.cols + 3) & ~3) * int(sizeof(float)) : 0) + FWD_STAGES * Rows<T, N, TPR, EPT, FWD_THREADS>::kStageBytes;
+  const int bytes = (SHARED_PARAMS ? 2 * ((a.cols + 3) & ~3) * int(sizeof(float)) : 0) + FWD_STAGES * (FWD_THREADS / TPR) * Rows<T, N, TPR, EPT>::kRowBytes;
   // weight and bias of wide rows leave room for one block per SM only
   const int blocks = blocks_for(a.rows, FWD_THREADS / TPR, sms * (bytes * BLOCKS <= 216 * 1024 ? BLOCKS : bytes * 2 <= 216 * 1024 ? 2 : 1));
   auto kernel = norm_forward_kernel<T, N, TPR, EPT, BLOCKS, SHARED_PARAMS>;
@@ -454,7 +511,7 @@ int forward(const NormArgs& a, int sms, cudaStream_t st) {
 template <typename T, int N, int TPR, int BLOCKS, int CLUSTER = 1>
 int backward(const NormArgs& a, int sms, cudaStream_t st) {
   using G = Geometry<TPR>;
-  constexpr int R = kRowsAtATime<T, N>, ring = BWD_STAGES * R * 2 * Rows<T, N, TPR, BWD_EPT, G::kThreads>::kStageBytes, ends = TPR == 32 ? 8 * 2 * 32 * BWD_EPT * 4 : 0;
+  constexpr int R = kRowsAtATime<T, N>, ring = BWD_STAGES * R * 2 * G::kGroups * Rows<T, N, TPR, BWD_EPT>::kRowBytes, ends = TPR == 32 ? 8 * 2 * 32 * BWD_EPT * 4 : 0;
   constexpr int bytes = ring > ends ? ring : ends;
   const int most = sms * BLOCKS / CLUSTER < kNormMaxParts ? sms * BLOCKS / CLUSTER : kNormMaxParts;
   const int blocks = blocks_for(a.rows, G::kGroups * R, most);

@@ -42,6 +42,7 @@ struct NormArgs {
   int64_t rows;
   int32_t cols, dtype, param_dtype, center;
   float eps;
+  int32_t* status;
   int32_t device;
 };
 int launch_norm_forward(const NormArgs& a, int sms, cudaStream_t st);
