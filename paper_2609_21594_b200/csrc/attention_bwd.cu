@@ -10,8 +10,9 @@
 // block's share of dq (or of dk and dv) with float atomics, whose order changes from run to run, or keep fp32 partial sums as large as
 // the number of blocks; here every sum has one owner and a fixed order.
 //
-// 320 threads: eight warps compute (two per lane quadrant, half of the 128 columns each), one loads, one issues.  The issuer alternates:
-// while the warps turn S into P it multiplies with the dS before, while they turn dP into dS it forms the next S.
+// 352 threads: eight warps compute (two per lane quadrant, half of the 128 columns each), one loads, one issues, one clears the rows of a
+// streamed tile that lie past the sequence's end.  The issuer alternates: while the warps turn S into P it multiplies with the dS before,
+// while they turn dP into dS it forms the next S.
 #include <cuda_bf16.h>
 
 #include "attention_tc.cuh"
@@ -21,7 +22,7 @@ namespace {
 
 using namespace attn;
 
-constexpr int THREADS = 320, STAGES = 2, TMEM_COLS = 512;
+constexpr int THREADS = 352, STAGES = 2, TMEM_COLS = 512, LOADER = 8, ISSUER = 9, SWEEPER = 10;
 constexpr uint32_t ROWS_BYTES = 2 * kAttnRowBlock * sizeof(float);     // lse and delta of 128 queries
 
 template <int BOXES> struct Smem {
@@ -42,6 +43,8 @@ struct Bars {
   __device__ __forceinline__ uint32_t all_done() const { return base + 48u; }
   __device__ __forceinline__ uint32_t full(int which, int st) const { return base + 56u + uint32_t(which * STAGES + st) * 8u; }
   __device__ __forceinline__ uint32_t empty(int which, int st) const { return base + 56u + uint32_t((2 + which) * STAGES + st) * 8u; }
+  // where a tile with rows past the end arrives; the sweeper passes it on to `full`
+  __device__ __forceinline__ uint32_t raw(int which, int st) const { return base + 128u + uint32_t(which * STAGES + st) * 8u; }
 };
 
 template <int BOXES>
@@ -59,12 +62,13 @@ __device__ __forceinline__ void set_up(const Bars& b, int warp, uint32_t* tmem_s
       for (int i = 0; i < STAGES; ++i) {
         mbar_init(b.full(w, i), 1);
         mbar_init(b.empty(w, i), 1);
+        mbar_init(b.raw(w, i), 1);
       }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
   }
-  if (warp == 9) {
+  if (warp == ISSUER) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(TMEM_COLS) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -77,31 +81,34 @@ __device__ __forceinline__ void tear_down(int warp, uint32_t tmem) {
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 9) {
+  if (warp == ISSUER) {
     __syncwarp();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
   }
 }
 
 // Waits until everything issued is done, so that tensor memory may be freed (and, without an error, tells the computing warps).
-__device__ __forceinline__ void finish_issue(const Bars& b, bool ok, volatile int* abort_flag, int32_t* status, int lane) {
-  if (lane == 0) {
-    if (!ok) {
-      *abort_flag = 1;
-      atomicExch(status, 33);
-    }
-    tc_commit(b.all_done());
-    if (!mbar_wait(b.all_done(), 0, abort_flag, false, WAIT_CYCLES / 8)) atomicExch(status, 34);
+__device__ __forceinline__ void finish_issue(const Bars& b, bool ok, volatile int* abort_flag, int32_t* status) {
+  if (!ok) {
+    *abort_flag = 1;
+    atomicExch(status, 33);
   }
-  __syncwarp();
+  tc_commit(b.all_done());
+  if (!mbar_wait(b.all_done(), 0, abort_flag, false, WAIT_CYCLES / 8)) atomicExch(status, 34);
 }
 
-// Waits for what was asked for last of both streams, so that shared memory may be released.
-__device__ __forceinline__ void drain(const Bars& b, int issued0, int issued1, volatile int* abort_flag, int32_t* status) {
+// Waits for what was asked for last of both streams, so that shared memory may be released.  After an error the sweeper may have left
+// tiles on their raw barriers: those get time to land.
+__device__ __forceinline__ void drain(const Bars& b, int issued, bool ok, volatile int* abort_flag, int32_t* status) {
   for (int w = 0; w < 2; ++w) {
-    const int issued = w ? issued1 : issued0;
+    mbar_wait(b.own(w), 0, abort_flag, false, WAIT_CYCLES / 8);
     for (int i = max(0, issued - STAGES); i < issued; ++i)
       if (!mbar_wait(b.full(w, i % STAGES), uint32_t(i / STAGES) & 1u, abort_flag, false, WAIT_CYCLES / 8)) atomicExch(status, 32);
+  }
+  if (!ok) {
+    *abort_flag = 1;
+    atomicExch(status, 31);
+    for (int i = 0; i < 64; ++i) __nanosleep(1000);
   }
 }
 
@@ -130,10 +137,20 @@ __device__ __forceinline__ void store_half(const AttnTensor& t, int tb, int toke
   }
 }
 
-__device__ __forceinline__ float4 lds4(uint32_t addr) {
-  float4 v;
-  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+struct Pairs { uint64_t a, b; };
+__device__ __forceinline__ Pairs lds_pairs(uint32_t addr) {
+  Pairs v;
+  asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(v.a), "=l"(v.b) : "r"(addr));
   return v;
+}
+
+// dS = P (dP + (-delta)), rounded.  Where a mask made P zero dP may be a NaN: selected, not multiplied.
+template <bool MASK>
+__device__ __forceinline__ uint32_t ds_pair(uint64_t p, uint64_t dp, uint64_t minus_delta) {
+  const uint64_t v = mul2(p, add2(dp, minus_delta));
+  if constexpr (!MASK) return pack_bf16(v);
+  const float2 f = both(v), q = both(p);
+  return pack_bf16(q.x == 0.f ? 0.f : f.x, q.y == 0.f ? 0.f : f.y);
 }
 
 // ------------------------------------------------------------------ dk, dv
@@ -171,7 +188,7 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
   const uint32_t tmem = *tmem_slot, t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 256 + BOXES * 64;
   auto phase = [](int n) { return uint32_t(n / STAGES) & 1u; };
 
-  if (warp == 8) {
+  if (warp == LOADER) {
     // ------------------------------------------------------------------ loads: stream 0 is q with its row statistics, stream 1 is do
     if (lane == 0 && total > 0) {
       const int64_t row_blocks = attn_row_blocks(a);
@@ -184,87 +201,80 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
       for (; n < total && ok; ++n) {
         const int h = kvh * group + n / per, i = i0 + n % per, st = n % STAGES;
         if (!(ok = mbar_wait(b.empty(0, st), phase(n) ^ 1u, abort_flag))) break;
-        mbar_expect_tx(b.full(0, st), L::kTile + ROWS_BYTES);
-        load_tile<BOXES>(base + L::s0 + uint32_t(st) * L::kTile, &maps.q, b.full(0, st), h, s.q0 + i * BLK, s.tb);
+        const bool ragged = (i + 1) * BLK > s.qn;
+        const uint32_t bar0 = ragged ? b.raw(0, st) : b.full(0, st), bar1 = ragged ? b.raw(1, st) : b.full(1, st);
+        mbar_expect_tx(bar0, L::kTile + ROWS_BYTES);
+        load_tile<BOXES>(base + L::s0 + uint32_t(st) * L::kTile, &maps.q, bar0, h, s.q0 + i * BLK, s.tb);
         bulk_load(base + L::rows + uint32_t(st) * ROWS_BYTES,
-                  a.rows + ((int64_t(s.tb) * a.hq + h) * row_blocks + (a.nseq ? s.q0 / kAttnRowBlock + si : 0) + i) * (2 * kAttnRowBlock), ROWS_BYTES,
-                  b.full(0, st));
+                  a.rows + ((int64_t(s.tb) * a.hq + h) * row_blocks + (a.nseq ? s.q0 / kAttnRowBlock + si : 0) + i) * (2 * kAttnRowBlock), ROWS_BYTES, bar0);
         ok = mbar_wait(b.empty(1, st), phase(n) ^ 1u, abort_flag);
-        mbar_expect_tx(b.full(1, st), L::kTile);           // armed even when giving up, so that the drain is one rule
-        load_tile<BOXES>(base + L::s1 + uint32_t(st) * L::kTile, &maps.dout, b.full(1, st), h, s.q0 + i * BLK, s.tb);
+        mbar_expect_tx(bar1, L::kTile);                    // armed even when giving up, so that the drain is one rule
+        load_tile<BOXES>(base + L::s1 + uint32_t(st) * L::kTile, &maps.dout, bar1, h, s.q0 + i * BLK, s.tb);
       }
-      if (!ok) {
-        *abort_flag = 1;
-        atomicExch(a.status, 31);
-      }
-      for (int w = 0; w < 2; ++w) mbar_wait(b.own(w), 0, abort_flag, false, WAIT_CYCLES / 8);
-      drain(b, n, n, abort_flag, a.status);
+      drain(b, n, ok, abort_flag, a.status);
     }
-  } else if (warp == 9) {
+  } else if (warp == SWEEPER) {
+    // ------------------------------------------------------------------ rows past the end: the last block of every head
+    if (total > 0 && i1 * BLK > s.qn) {
+      int uses[STAGES] = {};
+      for (int h = 0; h < group; ++h) {
+        const int st = (h * per + per - 1) % STAGES;
+        const uint32_t ph = uint32_t(st ? uses[1]++ : uses[0]++) & 1u;
+        bool ok = true;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          ok = ok && __all_sync(0xffffffffu, mbar_wait(b.raw(w, st), ph, abort_flag));
+          if (ok) clear_rows<BOXES>(base + (w ? L::s1 : L::s0) + uint32_t(st) * L::kTile, s.qn - (i1 - 1) * BLK, lane, b.full(w, st));
+        }
+        if (!ok) {
+          if (lane == 0) *abort_flag = 1;
+          break;
+        }
+      }
+    }
+  } else if (warp == ISSUER) {
     // ------------------------------------------------------------------ MMA issuer
-    if (total > 0) {
+    if (lane == 0 && total > 0) {
       const int ksteps = (a.dim + 15) / 16;
       const uint32_t idesc = make_idesc(true, BLK, ksteps * 16);
       bool ok = true;
       auto await = [&](uint32_t bar, uint32_t ph) {
-        ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, ph, abort_flag));
+        ok = ok && mbar_wait(bar, ph, abort_flag);
         tc_fence_after();
       };
       auto q_at = [&](int n) { return base + L::s0 + uint32_t(n % STAGES) * L::kTile; };
       auto do_at = [&](int n) { return base + L::s1 + uint32_t(n % STAGES) * L::kTile; };
-      auto arrived = [&](int which, int n) {               // a tile of queries; its rows past the sequence's end are cleared
-        await(b.full(which, n % STAGES), phase(n));
-        const int first = s.qn - (i0 + n % per) * BLK;
-        if (ok && first < BLK) clear_rows<BOXES>(which ? do_at(n) : q_at(n), first, lane);
-      };
       auto scores = [&](int n) {
-        if (lane == 0) {
-          mma_rows_rows(t_s, base + L::own0, q_at(n), ksteps);
-          tc_commit(b.s_full());
-        }
-        __syncwarp();
+        await(b.full(0, n % STAGES), phase(n));
+        if (!ok) return;
+        mma_rows_rows<BOXES>(t_s, base + L::own0, q_at(n), ksteps);
+        tc_commit(b.s_full());
       };
       auto dprobs = [&](int n) {
-        if (lane == 0) {
-          mma_rows_rows(t_dp, base + L::own1, do_at(n), ksteps);
-          tc_commit(b.dp_full());
-        }
-        __syncwarp();
+        await(b.full(1, n % STAGES), phase(n));
+        if (!ok) return;
+        mma_rows_rows<BOXES>(t_dp, base + L::own1, do_at(n), ksteps);
+        tc_commit(b.dp_full());
       };
       await(b.own(0), 0);
-      arrived(0, 0);
-      if (ok) scores(0);
+      scores(0);
       await(b.own(1), 0);
-      arrived(1, 0);
-      if (ok) dprobs(0);
+      dprobs(0);
       for (int n = 0; n < total && ok; ++n) {
         await(b.p_ready(), uint32_t(n) & 1u);
         if (!ok) break;
-        if (lane == 0) {
-          mma_probs_rows(t_dv, t_s, t_s + 64, do_at(n), idesc, n > 0);       // dv += P^T do
-          tc_commit(b.empty(1, n % STAGES));                                 // dP^T of this block was issued earlier
-        }
-        __syncwarp();
-        if (n + 1 < total) {
-          arrived(0, n + 1);
-          if (!ok) break;
-          scores(n + 1);                                                     // takes the place of P^T, which dv has read by then
-        }
+        mma_probs_rows(t_dv, t_s, t_s + 64, do_at(n), idesc, n > 0);         // dv += P^T do
+        tc_commit(b.empty(1, n % STAGES));                                   // dP^T of this block was issued earlier
+        if (n + 1 < total) scores(n + 1);                                    // takes the place of P^T, which dv has read by then
         await(b.ds_ready(), uint32_t(n) & 1u);
         if (!ok) break;
-        if (lane == 0) {
-          mma_probs_rows(t_dk, t_dp, t_dp + 64, q_at(n), idesc, n > 0);      // dk += dS^T q
-          tc_commit(b.empty(0, n % STAGES));
-        }
-        __syncwarp();
-        if (n + 1 < total) {
-          arrived(1, n + 1);
-          if (!ok) break;
-          dprobs(n + 1);
-        }
+        mma_probs_rows(t_dk, t_dp, t_dp + 64, q_at(n), idesc, n > 0);        // dk += dS^T q
+        tc_commit(b.empty(0, n % STAGES));
+        if (n + 1 < total) dprobs(n + 1);
       }
-      finish_issue(b, ok, abort_flag, a.status, lane);
+      finish_issue(b, ok, abort_flag, a.status);
     }
+    __syncwarp();
   } else {
     // ------------------------------------------------------------------ P^T and dS^T: lane = key, this warp's 64 of the 128 queries
     const int quad = warp & 3, half = warp >> 2;
@@ -283,58 +293,60 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
       if (!ok) break;
       tc_fence_after();
       const uint32_t rows = base + L::rows + uint32_t(n % STAGES) * ROWS_BYTES + uint32_t(half) * 256u;
-      float p[64];
+      const int first = qlo - r0 - half * 64, last = qhi - r0 - half * 64;
+      auto step = [&](auto with_mask) {
+        constexpr bool MASK = decltype(with_mask)::value;
+        uint64_t p[32];
+        {
+          uint32_t x[64], w[32];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) tc_ld32(ts + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&p[i * 32]));
-      tc_wait_ld();
-      const bool masked = block_masked(a, s, r0, c0) || r0 + BLK > s.qn || c0 + BLK > s.kn;
-      const int q0 = r0 + half * 64;
+          for (int i = 0; i < 2; ++i) tc_ld32(ts + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[i * 32]));
+          tc_wait_ld();
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float4 l2 = lds4(rows + uint32_t(i) * 16u);
-        p[4 * i] = exp2_approx(fmaf(p[4 * i], c2, -l2.x));
-        p[4 * i + 1] = exp2_approx(fmaf(p[4 * i + 1], c2, -l2.y));
-        p[4 * i + 2] = exp2_approx(fmaf(p[4 * i + 2], c2, -l2.z));
-        p[4 * i + 3] = exp2_approx(fmaf(p[4 * i + 3], c2, -l2.w));
-      }
-      if (masked) {
+          for (int i = 0; i < 16; ++i) {
+            const Pairs l2 = lds_pairs(rows + uint32_t(i) * 16u);
+            p[2 * i] = exp2_approx(fma2(words(x[4 * i], x[4 * i + 1]), twice(c2), l2.a));
+            p[2 * i + 1] = exp2_approx(fma2(words(x[4 * i + 2], x[4 * i + 3]), twice(c2), l2.b));
+            if constexpr (MASK) {
 #pragma unroll
-        for (int i = 0; i < 64; ++i)
-          if (q0 + i < qlo || q0 + i >= qhi) p[i] = 0.f;
-      }
-      {
-        uint32_t w[32];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) w[i] = pack_bf16(p[2 * i], p[2 * i + 1]);
-        tc_st32(ts, w);                                    // into this warp's own columns: the other half may still be read
-      }
-      tc_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(b.p_ready());
+              for (int e = 0; e < 2; ++e) {
+                const float2 f = both(p[2 * i + e]);
+                const int q = 4 * i + 2 * e;
+                p[2 * i + e] = two(q < first || q >= last ? 0.f : f.x, q + 1 < first || q + 1 >= last ? 0.f : f.y);
+              }
+            }
+            w[2 * i] = pack_bf16(p[2 * i]);
+            w[2 * i + 1] = pack_bf16(p[2 * i + 1]);
+          }
+          tc_st32(ts, w);                                  // into this warp's own columns: the other half may still be read
+        }
+        tc_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b.p_ready());
 
-      ok = __all_sync(0xffffffffu, mbar_wait(b.dp_full(), uint32_t(n) & 1u, abort_flag));
+        ok = __all_sync(0xffffffffu, mbar_wait(b.dp_full(), uint32_t(n) & 1u, abort_flag));
+        if (!ok) return;
+        tc_fence_after();
+        uint32_t x[64], w[32];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) tc_ld32(tp + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[i * 32]));
+        tc_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const Pairs d = lds_pairs(rows + kAttnRowBlock * 4u + uint32_t(i) * 16u);
+          w[2 * i] = ds_pair<MASK>(p[2 * i], words(x[4 * i], x[4 * i + 1]), d.a);
+          w[2 * i + 1] = ds_pair<MASK>(p[2 * i + 1], words(x[4 * i + 2], x[4 * i + 3]), d.b);
+        }
+        tc_st32(tp, w);
+        tc_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b.ds_ready());
+      };
+      if (block_masked(a, s, r0, c0) || r0 + BLK > s.qn || c0 + BLK > s.kn) step(Yes());
+      else step(No());
       if (!ok) break;
-      tc_fence_after();
-      float dp[64];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) tc_ld32(tp + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&dp[i * 32]));
-      tc_wait_ld();
-      uint32_t w[32];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float4 d = lds4(rows + kAttnRowBlock * 4u + uint32_t(i) * 16u);
-        // selected, not multiplied: dP of a masked pair may be a NaN
-        const float x0 = p[4 * i] * (dp[4 * i] - d.x), x1 = p[4 * i + 1] * (dp[4 * i + 1] - d.y);
-        const float x2 = p[4 * i + 2] * (dp[4 * i + 2] - d.z), x3 = p[4 * i + 3] * (dp[4 * i + 3] - d.w);
-        w[2 * i] = pack_bf16(p[4 * i] == 0.f ? 0.f : x0, p[4 * i + 1] == 0.f ? 0.f : x1);
-        w[2 * i + 1] = pack_bf16(p[4 * i + 2] == 0.f ? 0.f : x2, p[4 * i + 3] == 0.f ? 0.f : x3);
-      }
-      tc_st32(tp, w);
-      tc_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(b.ds_ready());
     }
     if (ok && total > 0) {
       ok = __all_sync(0xffffffffu, mbar_wait(b.all_done(), 0, abort_flag));
@@ -386,7 +398,7 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
   auto t_s = [&](int n) { return tmem + uint32_t(n & 1) * 128u; };
   auto phase = [](int n) { return uint32_t(n / STAGES) & 1u; };
 
-  if (warp == 8) {
+  if (warp == LOADER) {
     // ------------------------------------------------------------------ loads: stream 0 is k, stream 1 is v
     if (lane == 0 && total > 0) {
       for (int w = 0; w < 2; ++w) {
@@ -398,67 +410,63 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
       for (; n < total && ok; ++n) {
         const int st = n % STAGES, token = s.k0 + (rg.n0 + n) * BLK;
         if (!(ok = mbar_wait(b.empty(0, st), phase(n) ^ 1u, abort_flag))) break;
-        mbar_expect_tx(b.full(0, st), L::kTile);
-        load_tile<BOXES>(base + L::s0 + uint32_t(st) * L::kTile, &maps.k, b.full(0, st), kvh, token, s.tb);
+        const uint32_t bar0 = (rg.n0 + n + 1) * BLK > s.kn ? b.raw(0, st) : b.full(0, st);
+        mbar_expect_tx(bar0, L::kTile);
+        load_tile<BOXES>(base + L::s0 + uint32_t(st) * L::kTile, &maps.k, bar0, kvh, token, s.tb);
         ok = mbar_wait(b.empty(1, st), phase(n) ^ 1u, abort_flag);
         mbar_expect_tx(b.full(1, st), L::kTile);
         load_tile<BOXES>(base + L::s1 + uint32_t(st) * L::kTile, &maps.v, b.full(1, st), kvh, token, s.tb);
       }
-      if (!ok) {
-        *abort_flag = 1;
-        atomicExch(a.status, 31);
-      }
-      for (int w = 0; w < 2; ++w) mbar_wait(b.own(w), 0, abort_flag, false, WAIT_CYCLES / 8);
-      drain(b, n, n, abort_flag, a.status);
+      drain(b, n, ok, abort_flag, a.status);
     }
-  } else if (warp == 9) {
+  } else if (warp == SWEEPER) {
+    // ------------------------------------------------------------------ rows of the last k tile past the end: their dS is zero, and so must be dS k
+    if (total > 0 && rg.n1 * BLK > s.kn) {
+      const int st = (total - 1) % STAGES;
+      if (__all_sync(0xffffffffu, mbar_wait(b.raw(0, st), 0, abort_flag)))
+        clear_rows<BOXES>(base + L::s0 + uint32_t(st) * L::kTile, s.kn - (rg.n1 - 1) * BLK, lane, b.full(0, st));
+      else if (lane == 0) *abort_flag = 1;
+    }
+  } else if (warp == ISSUER) {
     // ------------------------------------------------------------------ MMA issuer
-    if (total > 0) {
+    if (lane == 0 && total > 0) {
       const int ksteps = (a.dim + 15) / 16;
       const uint32_t idesc = make_idesc(true, BLK, ksteps * 16);
       bool ok = true;
       auto await = [&](uint32_t bar, uint32_t ph) {
-        ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, ph, abort_flag));
+        ok = ok && mbar_wait(bar, ph, abort_flag);
         tc_fence_after();
       };
       auto k_at = [&](int n) { return base + L::s0 + uint32_t(n % STAGES) * L::kTile; };
       auto v_at = [&](int n) { return base + L::s1 + uint32_t(n % STAGES) * L::kTile; };
       auto scores = [&](int n) {
         await(b.full(0, n % STAGES), phase(n));
-        const int first = s.kn - (rg.n0 + n) * BLK;
-        if (ok && first < BLK) clear_rows<BOXES>(k_at(n), first, lane);      // dS of these keys is zero, and so must be dS k
-        if (ok && lane == 0) {
-          mma_rows_rows(t_s(n), base + L::own0, k_at(n), ksteps);
-          tc_commit(b.s_full(n & 1));
-        }
-        __syncwarp();
+        if (!ok) return;
+        mma_rows_rows<BOXES>(t_s(n), base + L::own0, k_at(n), ksteps);
+        tc_commit(b.s_full(n & 1));
       };
       auto dprobs = [&](int n) {
         await(b.full(1, n % STAGES), phase(n));
-        if (ok && lane == 0) {
-          mma_rows_rows(t_dp, base + L::own1, v_at(n), ksteps);
-          tc_commit(b.dp_full());
-          tc_commit(b.empty(1, n % STAGES));
-        }
-        __syncwarp();
+        if (!ok) return;
+        mma_rows_rows<BOXES>(t_dp, base + L::own1, v_at(n), ksteps);
+        tc_commit(b.dp_full());
+        tc_commit(b.empty(1, n % STAGES));
       };
       await(b.own(0), 0);
-      if (ok) scores(0);
+      scores(0);
       await(b.own(1), 0);
-      if (ok) dprobs(0);
+      dprobs(0);
       for (int n = 0; n < total && ok; ++n) {
         if (n + 1 < total) scores(n + 1);                  // its place was read before dS of block n - 1 was ready
         await(b.ds_ready(), uint32_t(n) & 1u);
         if (!ok) break;
-        if (lane == 0) {
-          mma_probs_rows(t_dq, t_dp, t_dp + 64, k_at(n), idesc, n > 0);      // dq += dS k
-          tc_commit(b.empty(0, n % STAGES));
-        }
-        __syncwarp();
+        mma_probs_rows(t_dq, t_dp, t_dp + 64, k_at(n), idesc, n > 0);        // dq += dS k
+        tc_commit(b.empty(0, n % STAGES));
         if (n + 1 < total) dprobs(n + 1);
       }
-      finish_issue(b, ok, abort_flag, a.status, lane);
+      finish_issue(b, ok, abort_flag, a.status);
     }
+    __syncwarp();
   } else {
     // ------------------------------------------------------------------ dS: lane = query, this warp's 64 of the 128 keys
     const int quad = warp & 3, half = warp >> 2;
@@ -476,35 +484,42 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
       ok = __all_sync(0xffffffffu, mbar_wait(b.s_full(n & 1), uint32_t(n >> 1) & 1u, abort_flag));
       if (!ok) break;
       tc_fence_after();
-      float p[64];
+      const int first = lo - c0 - half * 64, last = hi - c0 - half * 64;
+      auto step = [&](auto with_mask) {
+        constexpr bool MASK = decltype(with_mask)::value;
+        uint64_t p[32];
+        {
+          uint32_t x[64];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) tc_ld32(t_s(n) + lanes + uint32_t(half) * 64u + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&p[i * 32]));
-      tc_wait_ld();
+          for (int i = 0; i < 2; ++i) tc_ld32(t_s(n) + lanes + uint32_t(half) * 64u + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[i * 32]));
+          tc_wait_ld();
 #pragma unroll
-      for (int i = 0; i < 64; ++i) p[i] = exp2_approx(fmaf(p[i], c2, -l2));
-      if (block_masked(a, s, r0, c0) || r0 + BLK > s.qn) {
+          for (int i = 0; i < 32; ++i) {
+            p[i] = exp2_approx(fma2(words(x[2 * i], x[2 * i + 1]), twice(c2), twice(l2)));
+            if constexpr (MASK) {
+              const float2 f = both(p[i]);
+              p[i] = two(2 * i < first || 2 * i >= last ? 0.f : f.x, 2 * i + 1 < first || 2 * i + 1 >= last ? 0.f : f.y);
+            }
+          }
+        }
+        ok = __all_sync(0xffffffffu, mbar_wait(b.dp_full(), uint32_t(n) & 1u, abort_flag));
+        if (!ok) return;
+        tc_fence_after();
+        uint32_t x[64], w[32];
 #pragma unroll
-        for (int i = 0; i < 64; ++i)
-          if (c0 + half * 64 + i < lo || c0 + half * 64 + i >= hi) p[i] = 0.f;
-      }
-      ok = __all_sync(0xffffffffu, mbar_wait(b.dp_full(), uint32_t(n) & 1u, abort_flag));
+        for (int i = 0; i < 2; ++i) tc_ld32(tp + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[i * 32]));
+        tc_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) w[i] = ds_pair<MASK>(p[i], words(x[2 * i], x[2 * i + 1]), twice(delta));
+        tc_st32(tp, w);
+        tc_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b.ds_ready());
+      };
+      if (block_masked(a, s, r0, c0) || r0 + BLK > s.qn) step(Yes());
+      else step(No());
       if (!ok) break;
-      tc_fence_after();
-      float dp[64];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) tc_ld32(tp + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&dp[i * 32]));
-      tc_wait_ld();
-      uint32_t w[32];
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        const float x0 = p[2 * i] * (dp[2 * i] - delta), x1 = p[2 * i + 1] * (dp[2 * i + 1] - delta);
-        w[i] = pack_bf16(p[2 * i] == 0.f ? 0.f : x0, p[2 * i + 1] == 0.f ? 0.f : x1);
-      }
-      tc_st32(tp, w);
-      tc_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(b.ds_ready());
     }
     if (ok && total > 0) {
       ok = __all_sync(0xffffffffu, mbar_wait(b.all_done(), 0, abort_flag));

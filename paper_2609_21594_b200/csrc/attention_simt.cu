@@ -112,7 +112,8 @@ __global__ void __launch_bounds__(THREADS) attention_forward_simt_kernel(const A
   if (c == 0) a.lse[(int64_t(s.tb) * a.hq + head) * a.nq + s.q0 + row] = l == 0.f ? -INFINITY : m + logf(l);
 }
 
-// delta = sum_d do o, and lse in units of log 2, into the padded row blocks.  One warp per row.
+// -lse in units of log 2 and -delta, delta = sum_d do o, into the padded row blocks: P = exp2(scale' S + (-lse)) and dS = P (dP + (-delta)) are
+// then a multiply-add and an add.  One warp per row.
 template <typename T>
 __global__ void __launch_bounds__(256) attention_rows_kernel(const AttnArgs a) {
   int si, blk;
@@ -123,14 +124,14 @@ __global__ void __launch_bounds__(256) attention_rows_kernel(const AttnArgs a) {
   float* out = a.rows + ((int64_t(s.tb) * a.hq + head) * per + (a.nseq ? s.q0 / kAttnRowBlock + si : 0) + blk) * (2 * kAttnRowBlock);
   for (int r = warp; r < kAttnRowBlock; r += 8) {
     const int row = blk * kAttnRowBlock + r;
-    float l2 = INFINITY, delta = 0.f;
+    float l2 = -INFINITY, delta = 0.f;
     if (row < s.qn) {
       const float lse = a.lse[(int64_t(s.tb) * a.hq + head) * a.nq + s.q0 + row];
       if (lse != -INFINITY) {
-        l2 = lse * kLog2e;
+        l2 = -lse * kLog2e;
         const T* x = row_of<T>(a.dout, s.tb, s.q0 + row, head);
         const T* y = row_of<T>(a.o, s.tb, s.q0 + row, head);
-        for (int d = lane; d < a.dim; d += 32) delta = fmaf(to_f(x[d]), to_f(y[d]), delta);
+        for (int d = lane; d < a.dim; d += 32) delta = fmaf(-to_f(x[d]), to_f(y[d]), delta);
 #pragma unroll
         for (int d = 16; d; d >>= 1) delta += __shfl_xor_sync(0xffffffffu, delta, d);
       }
@@ -177,7 +178,7 @@ __global__ void __launch_bounds__(THREADS) attention_dq_simt_kernel(const AttnAr
       const int k = c + j * LANES, key = c0 + k;
       float ds = 0.f;
       if (key >= lo && key < hi)
-        ds = exp2f(fmaf(dot(sq + r * pitch, sk + k * pitch, a.dim), c2, -l2)) * (dot(sdo + r * pitch, sv + k * pitch, a.dim) - delta);
+        ds = exp2f(fmaf(dot(sq + r * pitch, sk + k * pitch, a.dim), c2, l2)) * (dot(sdo + r * pitch, sv + k * pitch, a.dim) + delta);
       sp[r * (COLS + 1) + k] = ds;
     }
     __syncwarp();
@@ -232,8 +233,8 @@ __global__ void __launch_bounds__(THREADS) attention_dkv_simt_kernel(const AttnA
         float p = 0.f, ds = 0.f;
         if (i < s.qn && key >= attn_key_lo(a, s, i) && key < attn_key_hi(a, s, i)) {
           const float* at = info + i / kAttnRowBlock * (2 * kAttnRowBlock) + i % kAttnRowBlock;
-          p = exp2f(fmaf(dot(sk + r * pitch, sq + q * pitch, a.dim), c2, -at[0]));
-          ds = p * (dot(sv + r * pitch, sdo + q * pitch, a.dim) - at[kAttnRowBlock]);
+          p = exp2f(fmaf(dot(sk + r * pitch, sq + q * pitch, a.dim), c2, at[0]));
+          ds = p * (dot(sv + r * pitch, sdo + q * pitch, a.dim) + at[kAttnRowBlock]);
         }
         sp[r * (COLS + 1) + q] = p;
         sds[r * (COLS + 1) + q] = ds;

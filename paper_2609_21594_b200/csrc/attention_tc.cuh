@@ -5,6 +5,7 @@
 // times rows: q k^T) and as an MN-major one (the tokens are summed over: P v).
 #pragma once
 
+#include "f32x2.cuh"
 #include "layer_ops.h"
 #include "tc_common.cuh"
 
@@ -67,39 +68,81 @@ __device__ __forceinline__ float exp2_approx(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+__device__ __forceinline__ uint64_t words(uint32_t a, uint32_t b) { return two(__uint_as_float(a), __uint_as_float(b)); }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&p);
 }
+__device__ __forceinline__ uint32_t pack_bf16(uint64_t v) {
+  const float2 f = both(v);
+  return pack_bf16(f.x, f.y);
+}
+__device__ __forceinline__ uint64_t exp2_approx(uint64_t v) {
+  const float2 f = both(v);
+  return two(exp2_approx(f.x), exp2_approx(f.y));
+}
+// 2^x on the multiply-add pipe, for the share of the exponentials that the exponential unit (16 per clock and SM, as many as the tensor
+// cores need clocks for the products around them) leaves over.  x = n + r with n the nearest integer, which adding 1.5 * 2^23 puts in
+// the low bits; 2^r on [-1/2, 1/2] by the polynomial of degree 4 whose largest relative error is least (2.7e-6 in fp32; fitted by
+// reweighted least squares); n goes to the exponent.  x is at most 127; below -126 the result is 2^-126.
+__device__ __forceinline__ uint64_t exp2_poly(uint64_t v) {
+  const float2 in = both(v);
+  const uint64_t x = two(fmaxf(in.x, -126.f), fmaxf(in.y, -126.f));
+  const uint64_t t = add2(x, twice(12582912.f));
+  const uint64_t r = add2(x, mul2(add2(t, twice(-12582912.f)), twice(-1.f)));
+  uint64_t p = fma2(twice(0.009570102207362652f), r, twice(0.05591786280274391f));
+  p = fma2(p, r, twice(0.240247443318367f));
+  p = fma2(p, r, twice(0.6931217908859253f));
+  p = fma2(p, r, twice(0.9999992847442627f));
+  const float2 n = both(t), y = both(p);
+  return two(__int_as_float(__float_as_int(y.x) + (__float_as_int(n.x) << 23)), __int_as_float(__float_as_int(y.y) + (__float_as_int(n.y) << 23)));
+}
 
+// Descriptors are formed once per tile: a step adds to the address field, which no address in shared memory carries out of.  A step of the
+// issuing thread has to take less than the 64 clocks of its instruction; formed anew each time, they took 107.
+//
 // S[128 x 128] = X Y^T over the head: both tiles K-major.  `ksteps` steps of 16 elements cover head_dim.
+template <int BOXES>
 __device__ __forceinline__ void mma_rows_rows(uint32_t d_tmem, uint32_t x, uint32_t y, int ksteps) {
   constexpr uint32_t idesc = make_idesc(false, BLK, BLK);
-  for (int k = 0; k < ksteps; ++k) {
-    const uint32_t off = uint32_t(k >> 2) * BOX_BYTES + uint32_t(k & 3) * 32u;
-    tc_mma(d_tmem, make_desc(x + off, 16, 1024), make_desc(y + off, 16, 1024), idesc, k > 0);
+  const uint64_t dx = make_desc(x, 16, 1024), dy = make_desc(y, 16, 1024);
+#pragma unroll
+  for (int k = 0; k < BOXES * 4; ++k) {
+    constexpr uint32_t box = BOX_BYTES >> 4;
+    const uint32_t off = uint32_t(k >> 2) * box + uint32_t(k & 3) * 2u;
+    if (k < ksteps) tc_mma(d_tmem, dx + off, dy + off, idesc, k > 0);
   }
 }
-// D[128 x n] (+)= P[128 x 128] Y[128 tokens x n]: P from tensor memory, 64 columns of bf16 pairs from `p_lo` on for the first 64 tokens
-// and from `p_hi` on for the others; Y MN-major.  `idesc` holds n (a multiple of 16 that covers head_dim).
+// Steps [k0, k1) of D[128 x n] (+)= P[128 x 128] Y[128 tokens x n]: P from tensor memory, 64 columns of bf16 pairs from `p_lo` on for the first
+// 64 tokens and from `p_hi` on for the others; Y MN-major.  `idesc` holds n (a multiple of 16 that covers head_dim).
+template <int K0 = 0, int K1 = 8>
 __device__ __forceinline__ void mma_probs_rows(uint32_t d_tmem, uint32_t p_lo, uint32_t p_hi, uint32_t y, uint32_t idesc, bool accumulate) {
+  const uint64_t dy = make_desc(y, BOX_BYTES, 1024);
 #pragma unroll
-  for (int k = 0; k < 8; ++k)
-    tc_mma_ts(d_tmem, (k < 4 ? p_lo : p_hi) + uint32_t(k & 3) * 8u, make_desc(y + uint32_t(k) * 2048u, BOX_BYTES, 1024), idesc,
-              accumulate || k > 0);
+  for (int k = K0; k < K1; ++k)
+    tc_mma_ts(d_tmem, (k < 4 ? p_lo : p_hi) + uint32_t(k & 3) * 8u, dy + uint32_t(k) * 128u, idesc, accumulate || k > 0);
 }
 
-// Clears the rows of a tile from `first` on (whole warp).  Rows past a sequence's end hold another sequence's tokens or padding; they meet
+// Clears the rows of a tile from `first` on (a whole warp) and arrives on `bar`.  Rows past a sequence's end hold another sequence's tokens or padding; they meet
 // probabilities that are zero, but zero times a NaN or an infinity is not zero.
 template <int BOXES>
-__device__ __forceinline__ void clear_rows(uint32_t tile, int first, int lane) {
+__device__ __forceinline__ void clear_rows(uint32_t tile, int first, int lane, uint32_t bar) {
 #pragma unroll
   for (int b = 0; b < BOXES; ++b)
     for (int i = first * 8 + lane; i < BLK * 8; i += 32)
       asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + uint32_t(b) * BOX_BYTES + uint32_t(i) * 16u), "r"(0) : "memory");
   fence_async_smem();
   __syncwarp();
+  if (lane == 0) mbar_arrive(bar);
 }
+
+struct Yes { static constexpr bool value = true; };
+struct No { static constexpr bool value = false; };
 
 // Blocks [n0, n1) of 128 keys that some query of rows [r0, r0 + 128) sees.
 struct BlockRange {

@@ -14,6 +14,7 @@
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
+#include "f32x2.cuh"
 #include "layer_ops.h"
 #include "tc_common.cuh"
 
@@ -28,35 +29,6 @@ __device__ __forceinline__ float up(float v) { return v; }
 __device__ __forceinline__ float up(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ void down(float* p, float v) { *p = v; }
 __device__ __forceinline__ void down(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
-
-// Two fp32 values in one instruction: half the issue slots of the arithmetic, which would otherwise bound the kernel.
-__device__ __forceinline__ uint64_t two(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float2 both(uint64_t v) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-  return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-
-__device__ __forceinline__ uint64_t twice(float a) { return two(a, a); }
 
 // Values 2 i and 2 i + 1 of a thread's pieces.  Two bf16 share a word: the upper one is its fp32 value with the lower bits cleared.
 template <typename T, int N>
@@ -318,7 +290,7 @@ template <typename T, int N> constexpr int kRowsAtATime = sizeof(T) == 2 && N > 
 
 template <typename T, int N, int TPR, int CLUSTER, int BLOCKS>
 __global__ void __launch_bounds__(Geometry<TPR>::kThreads, BLOCKS) norm_backward_kernel(const NormArgs a) {
-  constexpr int G = Geometry<TPR>::kGroups, THREADS = Geometry<TPR>::kThreads, EPT = BWD_EPT, R = kRowsAtATime<T, N>, H = EPT / 2;
+  constexpr int G = Geometry<TPR>::kGroups, EPT = BWD_EPT, R = kRowsAtATime<T, N>, H = EPT / 2;
   using RW = Rows<T, N, TPR, EPT>;
   extern __shared__ __align__(16) float dynamic[];    // the ring; one warp per row: at the end [8][2][32 * EPT] sums
   __shared__ float buf[2 * 2 * R * (TPR / 32) * CLUSTER];
@@ -511,7 +483,8 @@ int forward(const NormArgs& a, int sms, cudaStream_t st) {
 template <typename T, int N, int TPR, int BLOCKS, int CLUSTER = 1>
 int backward(const NormArgs& a, int sms, cudaStream_t st) {
   using G = Geometry<TPR>;
-  constexpr int R = kRowsAtATime<T, N>, ring = BWD_STAGES * R * 2 * G::kGroups * Rows<T, N, TPR, BWD_EPT>::kRowBytes, ends = TPR == 32 ? 8 * 2 * 32 * BWD_EPT * 4 : 0;
+  constexpr int R = kRowsAtATime<T, N>;
+  constexpr int ring = BWD_STAGES * R * 2 * G::kGroups * Rows<T, N, TPR, BWD_EPT>::kRowBytes, ends = TPR == 32 ? 8 * 2 * 32 * BWD_EPT * 4 : 0;
   constexpr int bytes = ring > ends ? ring : ends;
   const int most = sms * BLOCKS / CLUSTER < kNormMaxParts ? sms * BLOCKS / CLUSTER : kNormMaxParts;
   const int blocks = blocks_for(a.rows, G::kGroups * R, most);

@@ -185,8 +185,8 @@ inline int64_t attn_max_blocks(const AttnArgs& a, int rows, bool keys) {
   return a.nseq ? n / rows + a.nseq + 1 : int64_t(a.batch) * ((n + rows - 1) / rows);
 }
 
-// Backward scratch: for every head and every block of 128 queries of a sequence, 128 values of lse (in units of log 2; +inf for a row
-// that sees nothing) and then 128 of delta, so that a block's 1 KiB is one aligned copy.  Packed sequence s starts at block
+// Backward scratch: for every head and every block of 128 queries of a sequence, 128 values of -lse (in units of log 2; -inf for a row
+// that sees nothing) and then 128 of -delta, so that a block's 1 KiB is one aligned copy.  Packed sequence s starts at block
 // q0 / 128 + s, which leaves room for the blocks before it: floor(q0 / 128) + floor(n / 128) + 1 >= floor(q0 / 128) + ceil(n / 128).
 constexpr int kAttnRowBlock = 128;
 __host__ __device__ inline int64_t attn_row_blocks(const AttnArgs& a) {      // per head (batched: per batch row and head)
