@@ -164,7 +164,7 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
   const Bars b{base + L::bars};
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + L::bars + 192);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + L::bars + 200);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform_warp(), lane = threadIdx.x & 31;
   const int kvh = int(blockIdx.x % unsigned(a.hkv)), group = a.hq / a.hkv;
   int si, blk;
   if (!attn_find_block(a, int(blockIdx.x / unsigned(a.hkv)), BLK, true, &si, &blk)) return;
@@ -234,45 +234,47 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
     }
   } else if (warp == ISSUER) {
     // ------------------------------------------------------------------ MMA issuer
-    if (lane == 0 && total > 0) {
+    if (total > 0) {
       const int ksteps = (a.dim + 15) / 16;
       const uint32_t idesc = make_idesc(true, BLK, ksteps * 16);
       bool ok = true;
-      auto await = [&](uint32_t bar, uint32_t ph) {
-        ok = ok && mbar_wait(bar, ph, abort_flag);
-        tc_fence_after();
-      };
+      auto await = [&](uint32_t bar, uint32_t ph) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, ph, abort_flag)); };
       auto q_at = [&](int n) { return base + L::s0 + uint32_t(n % STAGES) * L::kTile; };
       auto do_at = [&](int n) { return base + L::s1 + uint32_t(n % STAGES) * L::kTile; };
       auto scores = [&](int n) {
-        await(b.full(0, n % STAGES), phase(n));
-        if (!ok) return;
         mma_rows_rows<BOXES>(t_s, base + L::own0, q_at(n), ksteps);
         tc_commit(b.s_full());
       };
       auto dprobs = [&](int n) {
-        await(b.full(1, n % STAGES), phase(n));
-        if (!ok) return;
         mma_rows_rows<BOXES>(t_dp, base + L::own1, do_at(n), ksteps);
         tc_commit(b.dp_full());
       };
       await(b.own(0), 0);
-      scores(0);
+      await(b.full(0, 0), 0);
+      if (ok && elect_one()) scores(0);
       await(b.own(1), 0);
-      dprobs(0);
+      await(b.full(1, 0), 0);
+      if (ok && elect_one()) dprobs(0);
       for (int n = 0; n < total && ok; ++n) {
+        const bool next = n + 1 < total;
+        if (next) await(b.full(0, (n + 1) % STAGES), phase(n + 1));
         await(b.p_ready(), uint32_t(n) & 1u);
-        if (!ok) break;
-        mma_probs_rows(t_dv, t_s, t_s + 64, do_at(n), idesc, n > 0);         // dv += P^T do
-        tc_commit(b.empty(1, n % STAGES));                                   // dP^T of this block was issued earlier
-        if (n + 1 < total) scores(n + 1);                                    // takes the place of P^T, which dv has read by then
+        tc_fence_after();                                  // tensor memory written by other threads; tiles need no such fence
+        if (ok && elect_one()) {
+          mma_probs_rows(t_dv, t_s, t_s + 64, do_at(n), idesc, n > 0);       // dv += P^T do
+          if (next) scores(n + 1);                         // takes the place of P^T, which dv has read by then
+          tc_commit(b.empty(1, n % STAGES));               // dP^T of this block was issued earlier
+        }
+        if (next) await(b.full(1, (n + 1) % STAGES), phase(n + 1));
         await(b.ds_ready(), uint32_t(n) & 1u);
-        if (!ok) break;
-        mma_probs_rows(t_dk, t_dp, t_dp + 64, q_at(n), idesc, n > 0);        // dk += dS^T q
-        tc_commit(b.empty(0, n % STAGES));
-        if (n + 1 < total) dprobs(n + 1);
+        tc_fence_after();
+        if (ok && elect_one()) {
+          mma_probs_rows(t_dk, t_dp, t_dp + 64, q_at(n), idesc, n > 0);      // dk += dS^T q
+          if (next) dprobs(n + 1);
+          tc_commit(b.empty(0, n % STAGES));
+        }
       }
-      finish_issue(b, ok, abort_flag, a.status);
+      if (elect_one()) finish_issue(b, ok, abort_flag, a.status);
     }
     __syncwarp();
   } else {
@@ -378,7 +380,7 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
   const Bars b{base + L::bars};
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + L::bars + 192);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + L::bars + 200);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform_warp(), lane = threadIdx.x & 31;
   const int head = int(blockIdx.x % unsigned(a.hq)), kvh = head / (a.hq / a.hkv);
   int si, blk;
   if (!attn_find_block(a, int(blockIdx.x / unsigned(a.hq)), BLK, false, &si, &blk)) return;
@@ -429,42 +431,44 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
     }
   } else if (warp == ISSUER) {
     // ------------------------------------------------------------------ MMA issuer
-    if (lane == 0 && total > 0) {
+    if (total > 0) {
       const int ksteps = (a.dim + 15) / 16;
       const uint32_t idesc = make_idesc(true, BLK, ksteps * 16);
       bool ok = true;
-      auto await = [&](uint32_t bar, uint32_t ph) {
-        ok = ok && mbar_wait(bar, ph, abort_flag);
-        tc_fence_after();
-      };
+      auto await = [&](uint32_t bar, uint32_t ph) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, ph, abort_flag)); };
       auto k_at = [&](int n) { return base + L::s0 + uint32_t(n % STAGES) * L::kTile; };
       auto v_at = [&](int n) { return base + L::s1 + uint32_t(n % STAGES) * L::kTile; };
       auto scores = [&](int n) {
-        await(b.full(0, n % STAGES), phase(n));
-        if (!ok) return;
         mma_rows_rows<BOXES>(t_s(n), base + L::own0, k_at(n), ksteps);
         tc_commit(b.s_full(n & 1));
       };
       auto dprobs = [&](int n) {
-        await(b.full(1, n % STAGES), phase(n));
-        if (!ok) return;
         mma_rows_rows<BOXES>(t_dp, base + L::own1, v_at(n), ksteps);
         tc_commit(b.dp_full());
         tc_commit(b.empty(1, n % STAGES));
       };
       await(b.own(0), 0);
-      scores(0);
+      await(b.full(0, 0), 0);
+      if (ok && elect_one()) scores(0);
       await(b.own(1), 0);
-      dprobs(0);
+      await(b.full(1, 0), 0);
+      if (ok && elect_one()) dprobs(0);
       for (int n = 0; n < total && ok; ++n) {
-        if (n + 1 < total) scores(n + 1);                  // its place was read before dS of block n - 1 was ready
+        const bool next = n + 1 < total;
+        if (next) {
+          await(b.full(0, (n + 1) % STAGES), phase(n + 1));
+          if (ok && elect_one()) scores(n + 1);            // its place was read before dS of block n - 1 was ready
+          await(b.full(1, (n + 1) % STAGES), phase(n + 1));
+        }
         await(b.ds_ready(), uint32_t(n) & 1u);
-        if (!ok) break;
-        mma_probs_rows(t_dq, t_dp, t_dp + 64, k_at(n), idesc, n > 0);        // dq += dS k
-        tc_commit(b.empty(0, n % STAGES));
-        if (n + 1 < total) dprobs(n + 1);
+        tc_fence_after();                                  // tensor memory written by other threads; tiles need no such fence
+        if (ok && elect_one()) {
+          mma_probs_rows(t_dq, t_dp, t_dp + 64, k_at(n), idesc, n > 0);      // dq += dS k
+          if (next) dprobs(n + 1);
+          tc_commit(b.empty(0, n % STAGES));
+        }
       }
-      finish_issue(b, ok, abort_flag, a.status);
+      if (elect_one()) finish_issue(b, ok, abort_flag, a.status);
     }
     __syncwarp();
   } else {

@@ -1,12 +1,12 @@
 // Attention forward on the tensor cores (bf16): one pass over the keys with a running maximum and sum.
 //
-// A block owns two tiles of 128 queries of one head and walks the blocks of 128 keys that they see.  608 threads:
-//   warps 0-7, 8-15  softmax of tile 0 and of tile 1: a row (one TMEM lane) belongs to two threads, 64 of the 128 keys each, which exchange
-//                    their maxima through shared memory.  One thread per row needs twice the registers for a chain twice as long, and two
-//                    warps per scheduler do not hide it (measured: 35 % of the exponential unit's rate, against 779 TFLOP/s)
-//   warp 16          TMA producer: the two q tiles once, then k and v tiles, two stages of each
-//   warp 17          MMA issuer:  S_t = q_t k^T (128 x 128 x head_dim),  O_t += P_t v with P_t read from tensor memory
-//   warp 18          clears the rows of the last v tile that lie past the sequence's end
+// A block owns two tiles of 128 queries of one head and walks the blocks of 128 keys that they see.  384 threads:
+//   warps 0-3, 4-7  softmax of tile 0 and of tile 1: a thread owns one row (one TMEM lane) and keeps its 128 scores in registers, so maxima
+//                   and sums need no exchange.  These two warpgroups take 216 registers per thread and leave 72 to the third: one spilled
+//                   register costs dearly where shared memory leaves no first-level cache
+//   warp 8          TMA producer: the two q tiles once, then k and v tiles, two stages of each
+//   warp 9          MMA issuer:  S_t = q_t k^T (128 x 128 x head_dim),  O_t += P_t v with P_t read from tensor memory
+//   warp 10         clears the rows of the last v tile that lie past the sequence's end
 // Tensor memory: S_0, S_1 (128 columns each), O_0, O_1.  P_t takes the place of S_t, rounded once to bf16.  While one tile's softmax runs,
 // the issuer works for the other.  A tcgen05.commit covers everything issued before it, so "S_t of block j is ready" also says that the
 // product that read P_t of block j - 1 is done and O_t may be touched.
@@ -22,15 +22,14 @@ namespace {
 
 using namespace attn;
 
-constexpr int THREADS = 608, STAGES = 2, TMEM_COLS = 512, LOADER = 16, ISSUER = 17, SWEEPER = 18;
+constexpr int THREADS = 384, STAGES = 2, TMEM_COLS = 512, LOADER = 8, ISSUER = 9, SWEEPER = 10;
+constexpr int SOFTMAX_REGS = 216, OTHER_REGS = 72;   // 2 x 216 + 72 = 3 x 168, what a block of 384 is launched with
 constexpr float kRaise = 8.f;                    // log2 of the largest P
-constexpr int kPolyOf = 4;                       // one pair of exponentials in so many is computed on the multiply-add pipe
 
 template <int BOXES> struct Smem {
   static constexpr uint32_t kTile = BOXES * BOX_BYTES;
   static constexpr uint32_t q = 0, k = 2 * kTile, v = k + STAGES * kTile, bars = v + STAGES * kTile;
-  static constexpr uint32_t swap = bars + 256;           // [2 tiles][2 halves][128 rows]
-  static constexpr uint32_t bytes = swap + 4 * BLK * 4 + 1024;   // barriers, slack for the 1024-byte alignment of swizzled tiles
+  static constexpr uint32_t bytes = bars + 256 + 1024;   // barriers, slack for the 1024-byte alignment of swizzled tiles
 };
 
 template <int BOXES>
@@ -43,17 +42,18 @@ attention_forward_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_
   const uint32_t bars = base + L::bars;
   auto q_full = [&](int t) { return bars + uint32_t(t) * 8u; };
   auto s_full = [&](int t) { return bars + uint32_t(2 + t) * 8u; };
-  auto p_ready = [&](int t) { return bars + uint32_t(4 + t) * 8u; };
-  auto o_full = [&](int t) { return bars + uint32_t(6 + t) * 8u; };
-  auto k_full = [&](int s) { return bars + uint32_t(8 + s) * 8u; };
-  auto k_empty = [&](int s) { return bars + uint32_t(8 + STAGES + s) * 8u; };
-  auto v_full = [&](int s) { return bars + uint32_t(8 + 2 * STAGES + s) * 8u; };
-  auto v_empty = [&](int s) { return bars + uint32_t(8 + 3 * STAGES + s) * 8u; };
-  const uint32_t done_bar = bars + uint32_t(8 + 4 * STAGES) * 8u, raw_bar = done_bar + 8u;
+  auto o_full = [&](int t) { return bars + uint32_t(4 + t) * 8u; };
+  auto p_ready = [&](int t, int h) { return bars + uint32_t(6 + 2 * t + h) * 8u; };      // P of the first 64 keys, of the others
+  auto k_full = [&](int s) { return bars + uint32_t(10 + s) * 8u; };
+  auto k_empty = [&](int s) { return bars + uint32_t(10 + STAGES + s) * 8u; };
+  auto v_full = [&](int s) { return bars + uint32_t(10 + 2 * STAGES + s) * 8u; };
+  auto v_empty = [&](int s) { return bars + uint32_t(10 + 3 * STAGES + s) * 8u; };
+  const uint32_t done_bar = bars + uint32_t(10 + 4 * STAGES) * 8u, raw_bar = done_bar + 8u;
+  static_assert((12 + 4 * STAGES) * 8 <= 192, "barriers");
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + L::bars + 192);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + L::bars + 200);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform_warp(), lane = threadIdx.x & 31;
   // Heads vary fastest, so that blocks that share keys run together; within a batched call the last queries, which see most keys, go first.
   const int head = int(blockIdx.x % unsigned(a.hq)), kvh = head / (a.hq / a.hkv);
   int si, blk;
@@ -76,7 +76,8 @@ attention_forward_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_
     for (int t = 0; t < 2; ++t) {
       mbar_init(q_full(t), 1);
       mbar_init(s_full(t), 1);
-      mbar_init(p_ready(t), 8);
+      mbar_init(p_ready(t, 0), 4);
+      mbar_init(p_ready(t, 1), 4);
       mbar_init(o_full(t), 1);
     }
     for (int i = 0; i < STAGES; ++i) {
@@ -102,199 +103,192 @@ attention_forward_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_
   const uint32_t t_s[2] = {tmem, tmem + 128}, t_o[2] = {tmem + 256, tmem + 256 + BOXES * 64};
   const float c2 = a.scale * kLog2e;
 
-  if (warp == LOADER) {
-    // ------------------------------------------------------------------ TMA producer
-    if (lane == 0 && u1 > u0) {
-      bool ok = true;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if (rg[t].n1 <= rg[t].n0) continue;
-        mbar_expect_tx(q_full(t), L::kTile);
-        load_tile<BOXES>(base + L::q + t * L::kTile, &maps.q, q_full(t), head, s.q0 + r0 + t * BLK, s.tb);
-      }
-      int j = u0;
-      for (; j < u1 && ok; ++j) {
-        const int i = j - u0, st = i % STAGES;
-        const uint32_t ph = uint32_t(i / STAGES) & 1u;
-        if (!(ok = mbar_wait(k_empty(st), ph ^ 1u, abort_flag))) break;
-        mbar_expect_tx(k_full(st), L::kTile);
-        load_tile<BOXES>(base + L::k + st * L::kTile, &maps.k, k_full(st), kvh, s.k0 + j * BLK, s.tb);
-        ok = mbar_wait(v_empty(st), ph ^ 1u, abort_flag);
-        // armed even when giving up, so that the drain below is one rule; a tile with rows past the end goes through the sweeper
-        const uint32_t bar = j + 1 == u1 && u1 * BLK > s.kn ? raw_bar : v_full(st);
-        mbar_expect_tx(bar, L::kTile);
-        load_tile<BOXES>(base + L::v + st * L::kTile, &maps.v, bar, kvh, s.k0 + j * BLK, s.tb);
-      }
-      if (!ok) {
-        *abort_flag = 1;
-        atomicExch(a.status, 21);
-      }
-      // Everything asked for must have landed before this block's shared memory is released.
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        if (rg[t].n1 > rg[t].n0) mbar_wait(q_full(t), 0, abort_flag, false, WAIT_CYCLES / 8);
-      if (u1 * BLK > s.kn) mbar_wait(raw_bar, 0, abort_flag, false, WAIT_CYCLES / 8);
-      for (int i = max(0, j - u0 - STAGES); i < j - u0; ++i) {
-        const uint32_t ph = uint32_t(i / STAGES) & 1u;
-        if (!mbar_wait(k_full(i % STAGES), ph, abort_flag, false, WAIT_CYCLES / 8) ||
-            !mbar_wait(v_full(i % STAGES), ph, abort_flag, false, WAIT_CYCLES / 8))
-          atomicExch(a.status, 22);
-      }
-    }
-  } else if (warp == ISSUER) {
-    // ------------------------------------------------------------------ MMA issuer
-    if (lane == 0 && u1 > u0) {
-      const int ksteps = (a.dim + 15) / 16;
-      const uint32_t idesc_o = make_idesc(true, BLK, ksteps * 16);
-      bool ok = true;
-      auto in = [&](int t, int j) { return j >= rg[t].n0 && j < rg[t].n1; };
-      auto await = [&](uint32_t bar, uint32_t ph) {
-        ok = ok && mbar_wait(bar, ph, abort_flag);
-        tc_fence_after();
-      };
-      auto scores = [&](int t, int j) {
-        if (j == rg[t].n0) await(q_full(t), 0);
-        if (!ok) return;
-        mma_rows_rows<BOXES>(t_s[t], base + L::q + t * L::kTile, base + L::k + uint32_t((j - u0) % STAGES) * L::kTile, ksteps);
-        tc_commit(s_full(t));
-      };
-      auto await_k = [&](int j) { await(k_full((j - u0) % STAGES), uint32_t((j - u0) / STAGES) & 1u); };
-      await_k(u0);
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        if (ok && in(t, u0)) scores(t, u0);
-      if (ok) tc_commit(k_empty(0));
-      for (int j = u0; j < u1 && ok; ++j) {
-        const int st = (j - u0) % STAGES;
-        const uint32_t v = base + L::v + uint32_t(st) * L::kTile;
-        await(v_full(st), uint32_t((j - u0) / STAGES) & 1u);
-        if (j + 1 < u1) await_k(j + 1);
+  if (warp >= LOADER) {
+    fewer_registers<OTHER_REGS>();
+    if (warp == LOADER) {
+      // ------------------------------------------------------------------ TMA producer
+      if (lane == 0 && u1 > u0) {
+        bool ok = true;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          if (ok && in(t, j)) {
-            await(p_ready(t), uint32_t(j - rg[t].n0) & 1u);
-            if (ok) {
-              mma_probs_rows(t_o[t], t_s[t], t_s[t] + 64, v, idesc_o, j > rg[t].n0);
-              if (j + 1 == rg[t].n1) tc_commit(o_full(t));
+          if (rg[t].n1 <= rg[t].n0) continue;
+          mbar_expect_tx(q_full(t), L::kTile);
+          load_tile<BOXES>(base + L::q + t * L::kTile, &maps.q, q_full(t), head, s.q0 + r0 + t * BLK, s.tb);
+        }
+        int j = u0;
+        for (; j < u1 && ok; ++j) {
+          const int i = j - u0, st = i % STAGES;
+          const uint32_t ph = uint32_t(i / STAGES) & 1u;
+          if (!(ok = mbar_wait(k_empty(st), ph ^ 1u, abort_flag))) break;
+          mbar_expect_tx(k_full(st), L::kTile);
+          load_tile<BOXES>(base + L::k + st * L::kTile, &maps.k, k_full(st), kvh, s.k0 + j * BLK, s.tb);
+          ok = mbar_wait(v_empty(st), ph ^ 1u, abort_flag);
+          // armed even when giving up, so that the drain below is one rule; a tile with rows past the end goes through the sweeper
+          const uint32_t bar = j + 1 == u1 && u1 * BLK > s.kn ? raw_bar : v_full(st);
+          mbar_expect_tx(bar, L::kTile);
+          load_tile<BOXES>(base + L::v + st * L::kTile, &maps.v, bar, kvh, s.k0 + j * BLK, s.tb);
+        }
+        if (!ok) {
+          *abort_flag = 1;
+          atomicExch(a.status, 21);
+        }
+        // Everything asked for must have landed before this block's shared memory is released.
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          if (rg[t].n1 > rg[t].n0) mbar_wait(q_full(t), 0, abort_flag, false, WAIT_CYCLES / 8);
+        if (u1 * BLK > s.kn) mbar_wait(raw_bar, 0, abort_flag, false, WAIT_CYCLES / 8);
+        for (int i = max(0, j - u0 - STAGES); i < j - u0; ++i) {
+          const uint32_t ph = uint32_t(i / STAGES) & 1u;
+          if (!mbar_wait(k_full(i % STAGES), ph, abort_flag, false, WAIT_CYCLES / 8) ||
+              !mbar_wait(v_full(i % STAGES), ph, abort_flag, false, WAIT_CYCLES / 8))
+            atomicExch(a.status, 22);
+        }
+      }
+    } else if (warp == ISSUER) {
+      // ------------------------------------------------------------------ MMA issuer
+      if (u1 > u0) {
+        const int ksteps = (a.dim + 15) / 16;
+        const uint32_t idesc_o = make_idesc(true, BLK, ksteps * 16);
+        bool ok = true;
+        auto in = [&](int t, int j) { return j >= rg[t].n0 && j < rg[t].n1; };
+        auto await = [&](uint32_t bar, uint32_t ph) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, ph, abort_flag)); };
+        auto await_k = [&](int j) { await(k_full((j - u0) % STAGES), uint32_t((j - u0) / STAGES) & 1u); };
+        auto issue_scores = [&](int t, int j) {
+          mma_rows_rows<BOXES>(t_s[t], base + L::q + t * L::kTile, base + L::k + uint32_t((j - u0) % STAGES) * L::kTile, ksteps);
+          tc_commit(s_full(t));
+        };
+        await_k(u0);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          if (in(t, u0)) {
+            await(q_full(t), 0);
+            if (ok && elect_one()) issue_scores(t, u0);
+          }
+        if (ok && elect_one()) tc_commit(k_empty(0));
+        for (int j = u0; j < u1 && ok; ++j) {
+          const int st = (j - u0) % STAGES;
+          const uint32_t v = base + L::v + uint32_t(st) * L::kTile;
+          await(v_full(st), uint32_t((j - u0) / STAGES) & 1u);
+          if (j + 1 < u1) await_k(j + 1);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const bool pv = in(t, j), next = in(t, j + 1);
+            if (pv) {
+              await(p_ready(t, 0), uint32_t(j - rg[t].n0) & 1u);
+              tc_fence_after();                            // tensor memory written by other threads; tiles need no such fence
+              if (ok && elect_one()) mma_probs_rows<0, 4>(t_o[t], t_s[t], t_s[t] + 32, v, idesc_o, j > rg[t].n0);
+              await(p_ready(t, 1), uint32_t(j - rg[t].n0) & 1u);
+              tc_fence_after();
+            }
+            if (next && j + 1 == rg[t].n0) await(q_full(t), 0);
+            if (ok && elect_one()) {
+              if (pv) mma_probs_rows<4, 8>(t_o[t], t_s[t], t_s[t] + 32, v, idesc_o, true);
+              if (pv && !next) tc_commit(o_full(t));
+              if (next) issue_scores(t, j + 1);
+              if (t == 1) {
+                tc_commit(v_empty(st));
+                if (j + 1 < u1) tc_commit(k_empty((j + 1 - u0) % STAGES));
+              }
             }
           }
-          if (ok && in(t, j + 1)) scores(t, j + 1);
         }
-        if (!ok) break;
-        tc_commit(v_empty(st));
-        if (j + 1 < u1) tc_commit(k_empty((j + 1 - u0) % STAGES));
+        // Nothing may be in flight when tensor memory is freed.
+        if (elect_one()) {
+          if (!ok) {
+            *abort_flag = 1;
+            atomicExch(a.status, 23);
+          }
+          tc_commit(done_bar);
+          if (!mbar_wait(done_bar, 0, abort_flag, false, WAIT_CYCLES / 8)) atomicExch(a.status, 24);
+        }
       }
-      // Nothing may be in flight when tensor memory is freed.
-      if (!ok) {
-        *abort_flag = 1;
-        atomicExch(a.status, 23);
+      __syncwarp();
+    } else if (warp == SWEEPER) {
+      // ------------------------------------------------------------------ rows past the end
+      if (u1 > u0 && u1 * BLK > s.kn) {
+        const int st = (u1 - 1 - u0) % STAGES;
+        if (__all_sync(0xffffffffu, mbar_wait(raw_bar, 0, abort_flag)))
+          clear_rows<BOXES>(base + L::v + uint32_t(st) * L::kTile, s.kn - (u1 - 1) * BLK, lane, v_full(st));
+        else if (lane == 0) *abort_flag = 1;
       }
-      tc_commit(done_bar);
-      if (!mbar_wait(done_bar, 0, abort_flag, false, WAIT_CYCLES / 8)) atomicExch(a.status, 24);
-    }
-    __syncwarp();
-  } else if (warp == SWEEPER) {
-    // ------------------------------------------------------------------ rows past the end
-    if (u1 > u0 && u1 * BLK > s.kn) {
-      const int st = (u1 - 1 - u0) % STAGES;
-      if (__all_sync(0xffffffffu, mbar_wait(raw_bar, 0, abort_flag)))
-        clear_rows<BOXES>(base + L::v + uint32_t(st) * L::kTile, s.kn - (u1 - 1) * BLK, lane, v_full(st));
-      else if (lane == 0) *abort_flag = 1;
     }
   } else {
     // ------------------------------------------------------------------ softmax and results
-    const int t = warp >> 3, half = (warp >> 2) & 1, quad = warp & 3;
-    const int lrow = quad * 32 + lane, row = r0 + t * BLK + lrow;
+    more_registers<SOFTMAX_REGS>();
+    const int t = warp >> 2, quad = warp & 3;
+    const int row = r0 + t * BLK + quad * 32 + lane;
     const uint32_t lanes = uint32_t(quad * 32) << 16;
     const BlockRange keys = t ? rg[1] : rg[0];
-    const uint32_t ts = (t ? t_s[1] : t_s[0]) + lanes + uint32_t(half) * 64u, to = (t ? t_o[1] : t_o[0]) + lanes + uint32_t(half) * (BOXES * 32);
-    // what the two threads of a row tell each other: a place each, and a barrier of their two warps
-    const uint32_t mine = base + L::swap + uint32_t((t * 2 + half) * BLK + lrow) * 4u, other = base + L::swap + uint32_t((t * 2 + (half ^ 1)) * BLK + lrow) * 4u;
-    auto swap = [&](float v) {
-      asm volatile("st.shared.f32 [%0], %1;" ::"r"(mine), "f"(v) : "memory");
-      asm volatile("bar.sync %0, 64;" ::"r"(1 + t * 4 + quad) : "memory");
-      float w;
-      asm volatile("ld.shared.f32 %0, [%1];" : "=f"(w) : "r"(other) : "memory");
-      return w;
-    };
+    const uint32_t ts = (t ? t_s[1] : t_s[0]) + lanes, to = (t ? t_o[1] : t_o[0]) + lanes;
     const int lo = attn_key_lo(a, s, row), hi = attn_key_hi(a, s, row);
     float m = -INFINITY;
-    uint64_t l = 0;                                        // sums of this thread's even and odd keys
+    uint64_t l = 0;                                        // sums of the even and of the odd keys
     bool ok = true;
     for (int j = keys.n0; j < keys.n1; ++j) {
       ok = __all_sync(0xffffffffu, mbar_wait(s_full(t), uint32_t(j - keys.n0) & 1u, abort_flag));
       if (!ok) break;
       tc_fence_after();
       const int c0 = j * BLK;
-      const int first = lo - c0 - half * 64, last = hi - c0 - half * 64;
-      // The scores are read twice, 32 at a time, rather than kept: 64 of them and their exponentials would not fit 96 registers.
       auto step = [&](auto with_mask) {
         constexpr bool MASK = decltype(with_mask)::value;
-        auto scores = [&](int i, uint32_t (&x)[32]) {
-          tc_ld32(ts + i * 32, x);
-          tc_wait_ld();
-          if constexpr (MASK) {
+        uint32_t x[128];
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (i * 32 + e < first || i * 32 + e >= last) x[e] = 0xff800000u;    // -inf
-          }
-        };
-        float mx = -INFINITY;
+        for (int i = 0; i < 4; ++i) tc_ld32(ts + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[i * 32]));
+        tc_wait_ld();
+        if constexpr (MASK) {
+          const int first = lo - c0, last = hi - c0;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          uint32_t x[32];
-          scores(i, x);
-          float top[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t* y = x + e * 8;
-            auto f = [&](int k) { return __uint_as_float(y[k]); };
-            top[e] = max3(max3(f(0), f(1), f(2)), max3(f(3), f(4), f(5)), fmaxf(f(6), f(7)));
-          }
-          mx = fmaxf(mx, fmaxf(max3(top[0], top[1], top[2]), top[3]));
+          for (int i = 0; i < 128; ++i)
+            if (i < first || i >= last) x[i] = 0xff800000u;                // -inf
         }
-        mx = fmaxf(mx, swap(mx));
+        auto f = [&](int i) { return __uint_as_float(x[i]); };
+        float top[4] = {f(0), f(1), f(2), f(3)};
+#pragma unroll
+        for (int i = 4; i < 124; i += 8)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top[e] = max3(top[e], f(i + 2 * e), f(i + 2 * e + 1));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top[e] = fmaxf(top[e], f(124 + e));
+        const float mx = fmaxf(max3(top[0], top[1], top[2]), top[3]);
         const bool raise = mx > m && (m == -INFINITY || (mx - m) * c2 > kRaise);
         if (__any_sync(0xffffffffu, raise)) {
           const float shrink = raise ? exp2_approx((m - mx) * c2) : 1.f;
           if (raise) m = mx;
           l = mul2(l, twice(shrink));
           if (j > keys.n0) {
-#pragma unroll
-            for (int i = 0; i < BOXES; ++i) {              // this warp's half of the head
-              uint32_t o[32];
-              tc_ld32(to + i * 32, o);
+#pragma unroll 1
+            for (int i = 0; i < BOXES * 8; ++i) {          // rare: few registers matter more than speed
+              uint32_t o[8];
+              tc_ld8(to + i * 8, o);
               tc_wait_ld();
 #pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
-              tc_st32(to + i * 32, o);
+              for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
+              tc_st8(to + i * 8, o);
             }
           }
         }
         const uint64_t scale = twice(c2), shift = twice(m == -INFINITY ? 0.f : -m * c2);
         uint64_t sum[2] = {0, 0};
-        uint32_t p[32];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          uint32_t x[32];
-          scores(i, x);
+        for (int h = 0; h < 2; ++h) {
+          uint32_t p[32];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const uint64_t z = fma2(words(x[2 * e], x[2 * e + 1]), scale, shift);
-            const uint64_t v = !MASK && e % kPolyOf == kPolyOf - 1 ? exp2_poly(z) : exp2_approx(z);   // a masked key's has to be 0
-            sum[e & 1] = add2(sum[e & 1], v);
-            p[i * 16 + e] = pack_bf16(v);
+          for (int i = 0; i < 32; ++i) {
+            const uint64_t z = fma2(words(x[h * 64 + 2 * i], x[h * 64 + 2 * i + 1]), scale, shift);
+            const uint64_t v = exp2_approx(z);
+            sum[i & 1] = add2(sum[i & 1], v);
+            p[i] = pack_bf16(v);
           }
+          tc_st32(ts + h * 32, p);
+          tc_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(p_ready(t, h));
         }
-        tc_st32(ts, p);                                    // into this warp's own columns: the other half may still be read
         l = add2(l, add2(sum[0], sum[1]));
       };
       if (block_masked(a, s, r0 + t * BLK, c0)) step(Yes());
       else step(No());
-      tc_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(p_ready(t));
     }
     const bool any = keys.n1 > keys.n0;
     if (ok && any) {
@@ -307,13 +301,13 @@ attention_forward_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_
         atomicExch(a.status, 25);
       }
     } else {
-      const float part = both(l).x + both(l).y, total = part + swap(part);
+      const float total = both(l).x + both(l).y;
       const bool dead = total == 0.f || hi <= lo;          // a row that sees nothing
       const float inv = dead ? 0.f : 1.f / total;
       const bool store = row < s.qext;
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.o.data) + int64_t(s.tb) * a.o.sb + int64_t(s.q0 + row) * a.o.st + int64_t(head) * a.o.sh;
 #pragma unroll
-      for (int i = 0; i < BOXES; ++i) {
+      for (int i = 0; i < BOXES * 2; ++i) {
         uint32_t o[32];
         if (any) {
           tc_ld32(to + i * 32, o);
@@ -321,7 +315,7 @@ attention_forward_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int d = half * (BOXES * 32) + i * 32 + e * 8;
+          const int d = i * 32 + e * 8;
           uint4 w = make_uint4(0, 0, 0, 0);
           if (!dead) {
             w.x = pack_bf16(__uint_as_float(o[e * 8]) * inv, __uint_as_float(o[e * 8 + 1]) * inv);
@@ -332,7 +326,7 @@ attention_forward_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_
           if (store && d < a.dim) *reinterpret_cast<uint4*>(out + d) = w;
         }
       }
-      if (store && half == 0) a.lse[(int64_t(s.tb) * a.hq + head) * a.nq + s.q0 + row] = dead ? -INFINITY : fmaf(m, a.scale, logf(total));
+      if (store) a.lse[(int64_t(s.tb) * a.hq + head) * a.nq + s.q0 + row] = dead ? -INFINITY : fmaf(m, a.scale, logf(total));
     }
   }
   tc_fence_before();

@@ -73,6 +73,22 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
   return y;
 }
+// Registers per thread of a warpgroup.  The sum over a block's warpgroups must not exceed what the block was launched with.
+template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+__device__ __forceinline__ void tc_ld8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void tc_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+
 __device__ __forceinline__ uint64_t words(uint32_t a, uint32_t b) { return two(__uint_as_float(a), __uint_as_float(b)); }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
@@ -86,25 +102,21 @@ __device__ __forceinline__ uint64_t exp2_approx(uint64_t v) {
   const float2 f = both(v);
   return two(exp2_approx(f.x), exp2_approx(f.y));
 }
-// 2^x on the multiply-add pipe, for the share of the exponentials that the exponential unit (16 per clock and SM, as many as the tensor
-// cores need clocks for the products around them) leaves over.  x = n + r with n the nearest integer, which adding 1.5 * 2^23 puts in
-// the low bits; 2^r on [-1/2, 1/2] by the polynomial of degree 4 whose largest relative error is least (2.7e-6 in fp32; fitted by
-// reweighted least squares); n goes to the exponent.  x is at most 127; below -126 the result is 2^-126.
-__device__ __forceinline__ uint64_t exp2_poly(uint64_t v) {
-  const float2 in = both(v);
-  const uint64_t x = two(fmaxf(in.x, -126.f), fmaxf(in.y, -126.f));
-  const uint64_t t = add2(x, twice(12582912.f));
-  const uint64_t r = add2(x, mul2(add2(t, twice(-12582912.f)), twice(-1.f)));
-  uint64_t p = fma2(twice(0.009570102207362652f), r, twice(0.05591786280274391f));
-  p = fma2(p, r, twice(0.240247443318367f));
-  p = fma2(p, r, twice(0.6931217908859253f));
-  p = fma2(p, r, twice(0.9999992847442627f));
-  const float2 n = both(t), y = both(p);
-  return two(__int_as_float(__float_as_int(y.x) + (__float_as_int(n.x) << 23)), __int_as_float(__float_as_int(y.y) + (__float_as_int(n.y) << 23)));
+// The issuing warp runs converged, its warp index taken from lane 0 and every wait followed by a vote, and one elected lane issues: then
+// descriptors and addresses are values of the whole warp and stay in uniform registers.  A step has to take less than the 64 clocks that
+// its instruction keeps the tensor cores busy; issued from a branch on the lane it took 85, with descriptors formed anew each time 107.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(one));
+  return one != 0;
 }
+__device__ __forceinline__ int uniform_warp() { return __shfl_sync(0xffffffffu, int(threadIdx.x >> 5), 0); }
 
-// Descriptors are formed once per tile: a step adds to the address field, which no address in shared memory carries out of.  A step of the
-// issuing thread has to take less than the 64 clocks of its instruction; formed anew each time, they took 107.
+// Descriptors are formed once per tile: a step adds to the address field, which no address in shared memory carries out of.
 //
 // S[128 x 128] = X Y^T over the head: both tiles K-major.  `ksteps` steps of 16 elements cover head_dim.
 template <int BOXES>
