@@ -4,8 +4,9 @@
 //   warps 0-3, 4-7  softmax of tile 0 and of tile 1: a thread owns one row (one TMEM lane) and keeps its 128 scores in registers, so maxima
 //                   and sums need no exchange.  These two warpgroups take 216 registers per thread and leave 72 to the third: one spilled
 //                   register costs dearly where shared memory leaves no first-level cache
-//   warp 8          TMA producer: the two q tiles once, then k and v tiles, two stages of each
-//   warp 9          MMA issuer:  S_t = q_t k^T (128 x 128 x head_dim),  O_t += P_t v with P_t read from tensor memory
+//   warp 8          TMA producer: the two q tiles once, then rounds of a v tile and the k tile after it
+//   warp 9          MMA issuer:  O_t += P_t v with P_t read from tensor memory, then S_t = q_t k^T of the next keys (128 x 128 x head_dim), for
+//                   the tiles in turn.  (An issuer per tile would let the tiles' products mix, and each softmax wait for both.)
 //   warp 10         clears the rows of the last v tile that lie past the sequence's end
 // Tensor memory: S_0, S_1 (128 columns each), O_0, O_1.  P_t takes the place of S_t, rounded once to bf16.  While one tile's softmax runs,
 // the issuer works for the other.  A tcgen05.commit covers everything issued before it, so "S_t of block j is ready" also says that the
@@ -22,13 +23,14 @@ namespace {
 
 using namespace attn;
 
-constexpr int THREADS = 384, STAGES = 2, TMEM_COLS = 512, LOADER = 8, ISSUER = 9, SWEEPER = 10;
+constexpr int THREADS = 384, TMEM_COLS = 512, LOADER = 8, ISSUER = 9, SWEEPER = 10;
 constexpr int SOFTMAX_REGS = 216, OTHER_REGS = 72;   // 2 x 216 + 72 = 3 x 168, what a block of 384 is launched with
 constexpr float kRaise = 8.f;                    // log2 of the largest P
 
 template <int BOXES> struct Smem {
   static constexpr uint32_t kTile = BOXES * BOX_BYTES;
-  static constexpr uint32_t q = 0, k = 2 * kTile, v = k + STAGES * kTile, bars = v + STAGES * kTile;
+  static constexpr int kStages = BOXES == 1 ? 4 : 2;
+  static constexpr uint32_t q = 0, k = 2 * kTile, v = k + kStages * kTile, bars = v + kStages * kTile;
   static constexpr uint32_t bytes = bars + 256 + 1024;   // barriers, slack for the 1024-byte alignment of swizzled tiles
 };
 
@@ -44,12 +46,11 @@ attention_forward_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_
   auto s_full = [&](int t) { return bars + uint32_t(2 + t) * 8u; };
   auto o_full = [&](int t) { return bars + uint32_t(4 + t) * 8u; };
   auto p_ready = [&](int t, int h) { return bars + uint32_t(6 + 2 * t + h) * 8u; };      // P of the first 64 keys, of the others
-  auto k_full = [&](int s) { return bars + uint32_t(10 + s) * 8u; };
-  auto k_empty = [&](int s) { return bars + uint32_t(10 + STAGES + s) * 8u; };
-  auto v_full = [&](int s) { return bars + uint32_t(10 + 2 * STAGES + s) * 8u; };
-  auto v_empty = [&](int s) { return bars + uint32_t(10 + 3 * STAGES + s) * 8u; };
-  const uint32_t done_bar = bars + uint32_t(10 + 4 * STAGES) * 8u, raw_bar = done_bar + 8u;
-  static_assert((12 + 4 * STAGES) * 8 <= 192, "barriers");
+  constexpr int STAGES = L::kStages;
+  auto full = [&](int s) { return bars + uint32_t(10 + s) * 8u; };
+  auto empty = [&](int s) { return bars + uint32_t(10 + STAGES + s) * 8u; };
+  const uint32_t done_bar = bars + uint32_t(10 + 2 * STAGES) * 8u, raw_bar = done_bar + 8u;
+  static_assert((12 + 2 * STAGES) * 8 <= 192, "barriers");
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + L::bars + 192);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + L::bars + 200);
 
@@ -81,10 +82,8 @@ attention_forward_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_
       mbar_init(o_full(t), 1);
     }
     for (int i = 0; i < STAGES; ++i) {
-      mbar_init(k_full(i), 1);
-      mbar_init(k_empty(i), 1);
-      mbar_init(v_full(i), 1);
-      mbar_init(v_empty(i), 1);
+      mbar_init(full(i), 1);
+      mbar_init(empty(i), 1);
     }
     mbar_init(done_bar, 1);
     mbar_init(raw_bar, 1);
@@ -115,18 +114,16 @@ attention_forward_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_
           mbar_expect_tx(q_full(t), L::kTile);
           load_tile<BOXES>(base + L::q + t * L::kTile, &maps.q, q_full(t), head, s.q0 + r0 + t * BLK, s.tb);
         }
-        int j = u0;
-        for (; j < u1 && ok; ++j) {
-          const int i = j - u0, st = i % STAGES;
-          const uint32_t ph = uint32_t(i / STAGES) & 1u;
-          if (!(ok = mbar_wait(k_empty(st), ph ^ 1u, abort_flag))) break;
-          mbar_expect_tx(k_full(st), L::kTile);
-          load_tile<BOXES>(base + L::k + st * L::kTile, &maps.k, k_full(st), kvh, s.k0 + j * BLK, s.tb);
-          ok = mbar_wait(v_empty(st), ph ^ 1u, abort_flag);
-          // armed even when giving up, so that the drain below is one rule; a tile with rows past the end goes through the sweeper
-          const uint32_t bar = j + 1 == u1 && u1 * BLK > s.kn ? raw_bar : v_full(st);
-          mbar_expect_tx(bar, L::kTile);
-          load_tile<BOXES>(base + L::v + st * L::kTile, &maps.v, bar, kvh, s.k0 + j * BLK, s.tb);
+        // Round p brings v of block u0 + p - 1 and k of block u0 + p; the first has no v, the last no k.
+        int p = 0;
+        for (; p <= u1 - u0; ++p) {
+          const int st = p % STAGES, j = u0 + p;
+          if (!(ok = mbar_wait(empty(st), (uint32_t(p / STAGES) & 1u) ^ 1u, abort_flag))) break;
+          // a v tile with rows past the end goes through the sweeper
+          const uint32_t bar = j == u1 && u1 * BLK > s.kn ? raw_bar : full(st);
+          mbar_expect_tx(bar, (p > 0) + (j < u1) == 2 ? 2 * L::kTile : L::kTile);
+          if (p > 0) load_tile<BOXES>(base + L::v + st * L::kTile, &maps.v, bar, kvh, s.k0 + (j - 1) * BLK, s.tb);
+          if (j < u1) load_tile<BOXES>(base + L::k + st * L::kTile, &maps.k, bar, kvh, s.k0 + j * BLK, s.tb);
         }
         if (!ok) {
           *abort_flag = 1;
@@ -137,12 +134,8 @@ attention_forward_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_
         for (int t = 0; t < 2; ++t)
           if (rg[t].n1 > rg[t].n0) mbar_wait(q_full(t), 0, abort_flag, false, WAIT_CYCLES / 8);
         if (u1 * BLK > s.kn) mbar_wait(raw_bar, 0, abort_flag, false, WAIT_CYCLES / 8);
-        for (int i = max(0, j - u0 - STAGES); i < j - u0; ++i) {
-          const uint32_t ph = uint32_t(i / STAGES) & 1u;
-          if (!mbar_wait(k_full(i % STAGES), ph, abort_flag, false, WAIT_CYCLES / 8) ||
-              !mbar_wait(v_full(i % STAGES), ph, abort_flag, false, WAIT_CYCLES / 8))
-            atomicExch(a.status, 22);
-        }
+        for (int i = max(0, p - STAGES); i < p; ++i)
+          if (!mbar_wait(full(i % STAGES), uint32_t(i / STAGES) & 1u, abort_flag, false, WAIT_CYCLES / 8)) atomicExch(a.status, 22);
       }
     } else if (warp == ISSUER) {
       // ------------------------------------------------------------------ MMA issuer
@@ -150,45 +143,31 @@ attention_forward_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_
         const int ksteps = (a.dim + 15) / 16;
         const uint32_t idesc_o = make_idesc(true, BLK, ksteps * 16);
         bool ok = true;
-        auto in = [&](int t, int j) { return j >= rg[t].n0 && j < rg[t].n1; };
         auto await = [&](uint32_t bar, uint32_t ph) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, ph, abort_flag)); };
-        auto await_k = [&](int j) { await(k_full((j - u0) % STAGES), uint32_t((j - u0) / STAGES) & 1u); };
-        auto issue_scores = [&](int t, int j) {
-          mma_rows_rows<BOXES>(t_s[t], base + L::q + t * L::kTile, base + L::k + uint32_t((j - u0) % STAGES) * L::kTile, ksteps);
-          tc_commit(s_full(t));
-        };
-        await_k(u0);
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-          if (in(t, u0)) {
-            await(q_full(t), 0);
-            if (ok && elect_one()) issue_scores(t, u0);
-          }
-        if (ok && elect_one()) tc_commit(k_empty(0));
-        for (int j = u0; j < u1 && ok; ++j) {
-          const int st = (j - u0) % STAGES;
-          const uint32_t v = base + L::v + uint32_t(st) * L::kTile;
-          await(v_full(st), uint32_t((j - u0) / STAGES) & 1u);
-          if (j + 1 < u1) await_k(j + 1);
+        for (int p = 0; p <= u1 - u0 && ok; ++p) {
+          const int st = p % STAGES, j = u0 + p - 1;
+          const uint32_t v = base + L::v + uint32_t(st) * L::kTile, k = base + L::k + uint32_t(st) * L::kTile;
+          await(full(st), uint32_t(p / STAGES) & 1u);
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
-            const bool pv = in(t, j), next = in(t, j + 1);
+            const bool pv = j >= rg[t].n0 && j < rg[t].n1, next = j + 1 >= rg[t].n0 && j + 1 < rg[t].n1;
             if (pv) {
               await(p_ready(t, 0), uint32_t(j - rg[t].n0) & 1u);
               tc_fence_after();                            // tensor memory written by other threads; tiles need no such fence
               if (ok && elect_one()) mma_probs_rows<0, 4>(t_o[t], t_s[t], t_s[t] + 32, v, idesc_o, j > rg[t].n0);
               await(p_ready(t, 1), uint32_t(j - rg[t].n0) & 1u);
               tc_fence_after();
+            } else if (next) {
+              await(q_full(t), 0);
             }
-            if (next && j + 1 == rg[t].n0) await(q_full(t), 0);
             if (ok && elect_one()) {
               if (pv) mma_probs_rows<4, 8>(t_o[t], t_s[t], t_s[t] + 32, v, idesc_o, true);
               if (pv && !next) tc_commit(o_full(t));
-              if (next) issue_scores(t, j + 1);
-              if (t == 1) {
-                tc_commit(v_empty(st));
-                if (j + 1 < u1) tc_commit(k_empty((j + 1 - u0) % STAGES));
+              if (next) {
+                mma_rows_rows<BOXES>(t_s[t], base + L::q + uint32_t(t) * L::kTile, k, ksteps);    // over P_t, which the product before has read
+                tc_commit(s_full(t));
               }
+              if (t == 1) tc_commit(empty(st));
             }
           }
         }
@@ -206,9 +185,9 @@ attention_forward_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_
     } else if (warp == SWEEPER) {
       // ------------------------------------------------------------------ rows past the end
       if (u1 > u0 && u1 * BLK > s.kn) {
-        const int st = (u1 - 1 - u0) % STAGES;
+        const int st = (u1 - u0) % STAGES;
         if (__all_sync(0xffffffffu, mbar_wait(raw_bar, 0, abort_flag)))
-          clear_rows<BOXES>(base + L::v + uint32_t(st) * L::kTile, s.kn - (u1 - 1) * BLK, lane, v_full(st));
+          clear_rows<BOXES>(base + L::v + uint32_t(st) * L::kTile, s.kn - (u1 - 1) * BLK, lane, full(st));
         else if (lane == 0) *abort_flag = 1;
       }
     }
@@ -269,22 +248,25 @@ attention_forward_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_
         }
         const uint64_t scale = twice(c2), shift = twice(m == -INFINITY ? 0.f : -m * c2);
         uint64_t sum[2] = {0, 0};
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t p[32];
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const uint64_t z = fma2(words(x[h * 64 + 2 * i], x[h * 64 + 2 * i + 1]), scale, shift);
-            const uint64_t v = exp2_approx(z);
-            sum[i & 1] = add2(sum[i & 1], v);
-            p[i] = pack_bf16(v);
-          }
-          tc_st32(ts + h * 32, p);
+        auto hand_over = [&](int h) {
           tc_wait_st();
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(p_ready(t, h));
+        };
+        uint32_t p[32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const uint64_t v = exp2_approx(fma2(words(x[c * 32 + 2 * i], x[c * 32 + 2 * i + 1]), scale, shift));
+            sum[i & 1] = add2(sum[i & 1], v);
+            p[(c & 1) * 16 + i] = pack_bf16(v);
+          }
+          if (c == 2) hand_over(0);                        // the first half has long been stored: nothing waits
+          if (c & 1) tc_st32(ts + (c >> 1) * 32, p);
         }
+        hand_over(1);
         l = add2(l, add2(sum[0], sum[1]));
       };
       if (block_masked(a, s, r0 + t * BLK, c0)) step(Yes());
