@@ -22,48 +22,49 @@ namespace {
 
 using namespace attn;
 
-constexpr int THREADS = 352, STAGES = 2, TMEM_COLS = 512, LOADER = 8, ISSUER = 9, SWEEPER = 10;
+constexpr int THREADS = 352, TMEM_COLS = 512, LOADER = 8, ISSUER = 9, SWEEPER = 10;
 constexpr uint32_t ROWS_BYTES = 2 * kAttnRowBlock * sizeof(float);     // lse and delta of 128 queries
+
+// Both streams bring one tile per round.  Stream 0 (q; k in the dq kernel) feeds the first product of a round and the last, so when the next
+// round begins its tile has only just been read for the last time: three places.  Stream 1 (do with the row statistics; v) has two.
+constexpr int PLACES0 = 3, PLACES1 = 2;
 
 template <int BOXES> struct Smem {
   static constexpr uint32_t kTile = BOXES * BOX_BYTES;
-  // two tiles that stay, two stages of the two that stream, row statistics
-  static constexpr uint32_t own0 = 0, own1 = kTile, s0 = 2 * kTile, s1 = s0 + STAGES * kTile, rows = s1 + STAGES * kTile;
-  static constexpr uint32_t bars = rows + STAGES * ROWS_BYTES;
-  static constexpr uint32_t bytes = bars + 256 + 1024;
+  static constexpr uint32_t own0 = 0, own1 = kTile, s0 = 2 * kTile, s1 = s0 + PLACES0 * kTile, rows = s1 + PLACES1 * kTile;
+  static constexpr uint32_t bars = rows + PLACES1 * ROWS_BYTES;
+  static constexpr uint32_t bytes = bars + 256;
+  static_assert(bytes <= 227 * 1024, "shared memory of a block");   // no room to align the base, which its declaration aligns (and the kernels check)
 };
 
 struct Bars {
   uint32_t base;
-  __device__ __forceinline__ uint32_t own(int i) const { return base + uint32_t(i) * 8u; }
-  __device__ __forceinline__ uint32_t s_full(int place = 0) const { return base + (place ? 120u : 16u); }
-  __device__ __forceinline__ uint32_t dp_full() const { return base + 24u; }
-  __device__ __forceinline__ uint32_t p_ready() const { return base + 32u; }
-  __device__ __forceinline__ uint32_t ds_ready() const { return base + 40u; }
-  __device__ __forceinline__ uint32_t all_done() const { return base + 48u; }
-  __device__ __forceinline__ uint32_t full(int which, int st) const { return base + 56u + uint32_t(which * STAGES + st) * 8u; }
-  __device__ __forceinline__ uint32_t empty(int which, int st) const { return base + 56u + uint32_t((2 + which) * STAGES + st) * 8u; }
+  __device__ __forceinline__ uint32_t at(int i) const { return base + uint32_t(i) * 8u; }
+  __device__ __forceinline__ uint32_t own(int i) const { return at(i); }
+  __device__ __forceinline__ uint32_t s_full(int place = 0) const { return at(2 + place); }
+  __device__ __forceinline__ uint32_t dp_full() const { return at(4); }
+  __device__ __forceinline__ uint32_t p_ready(int part = 0) const { return at(5 + part); }
+  __device__ __forceinline__ uint32_t ds_ready() const { return at(7); }
+  __device__ __forceinline__ uint32_t all_done() const { return at(8); }
+  // Round n has been read: its places may be loaded again.  Two barriers in turn: round n + 2 cannot end before the loader, past round n,
+  // has brought what it needs, so neither completes twice unseen.
+  __device__ __forceinline__ uint32_t round_done(int n) const { return at(9 + (n & 1)); }
+  __device__ __forceinline__ uint32_t full0(int n) const { return at(11 + n % PLACES0); }
+  __device__ __forceinline__ uint32_t full1(int n) const { return at(11 + PLACES0 + n % PLACES1); }
   // where a tile with rows past the end arrives; the sweeper passes it on to `full`
-  __device__ __forceinline__ uint32_t raw(int which, int st) const { return base + 128u + uint32_t(which * STAGES + st) * 8u; }
+  __device__ __forceinline__ uint32_t raw0(int n) const { return at(11 + PLACES0 + PLACES1 + n % PLACES0); }
+  __device__ __forceinline__ uint32_t raw1(int n) const { return at(11 + 2 * PLACES0 + PLACES1 + n % PLACES1); }
+  static constexpr int count = 11 + 2 * (PLACES0 + PLACES1);
 };
+static_assert(Bars::count * 8 <= 192, "barriers");
+__device__ __forceinline__ uint32_t phase0(int n) { return uint32_t(n / PLACES0) & 1u; }
+__device__ __forceinline__ uint32_t phase1(int n) { return uint32_t(n / PLACES1) & 1u; }
+__device__ __forceinline__ uint32_t phase_done(int n) { return uint32_t(n >> 1) & 1u; }
 
 template <int BOXES>
 __device__ __forceinline__ void set_up(const Bars& b, int warp, uint32_t* tmem_slot, volatile int* abort_flag) {
   if (threadIdx.x == 0) {
-    mbar_init(b.own(0), 1);
-    mbar_init(b.own(1), 1);
-    mbar_init(b.s_full(0), 1);
-    mbar_init(b.s_full(1), 1);
-    mbar_init(b.dp_full(), 1);
-    mbar_init(b.p_ready(), 8);
-    mbar_init(b.ds_ready(), 8);
-    mbar_init(b.all_done(), 1);
-    for (int w = 0; w < 2; ++w)
-      for (int i = 0; i < STAGES; ++i) {
-        mbar_init(b.full(w, i), 1);
-        mbar_init(b.empty(w, i), 1);
-        mbar_init(b.raw(w, i), 1);
-      }
+    for (int i = 0; i < Bars::count; ++i) mbar_init(b.at(i), i >= 5 && i <= 7 ? 8 : 1);     // P and dS come from eight warps
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
@@ -87,6 +88,37 @@ __device__ __forceinline__ void tear_down(int warp, uint32_t tmem) {
   }
 }
 
+// The loading thread: load0(n) and load1(n) ask for round n's tiles as soon as their places are free.
+template <typename L0, typename L1>
+__device__ __forceinline__ void load_rounds(const Bars& b, int total, volatile int* abort_flag, int32_t* status, L0 load0, L1 load1) {
+  bool ok = true;
+  int n0 = 0, n1 = 0;
+  while (ok && n0 < total) {
+    if (n0 >= PLACES0) ok = mbar_wait(b.round_done(n0 - PLACES0), phase_done(n0 - PLACES0), abort_flag);
+    if (!ok) break;
+    for (; n1 < total && n1 <= n0 - PLACES0 + PLACES1; ++n1) load1(n1);
+    load0(n0++);
+    if (n0 <= PLACES1)
+      for (; n1 < n0; ++n1) load1(n1);
+  }
+  for (; ok && n1 < total; ++n1) {
+    if (n1 >= PLACES1) ok = mbar_wait(b.round_done(n1 - PLACES1), phase_done(n1 - PLACES1), abort_flag);
+    if (ok) load1(n1);
+  }
+  // Everything asked for must have landed before this block's shared memory is released.  After an error the sweeper may have left tiles
+  // on their raw barriers: those get time to land.
+  for (int w = 0; w < 2; ++w) mbar_wait(b.own(w), 0, abort_flag, false, WAIT_CYCLES / 8);
+  for (int i = max(0, n0 - PLACES0); i < n0; ++i)
+    if (!mbar_wait(b.full0(i), phase0(i), abort_flag, false, WAIT_CYCLES / 8)) atomicExch(status, 32);
+  for (int i = max(0, n1 - PLACES1); i < n1; ++i)
+    if (!mbar_wait(b.full1(i), phase1(i), abort_flag, false, WAIT_CYCLES / 8)) atomicExch(status, 32);
+  if (!ok) {
+    *abort_flag = 1;
+    atomicExch(status, 31);
+    for (int i = 0; i < 64; ++i) __nanosleep(1000);
+  }
+}
+
 // Waits until everything issued is done, so that tensor memory may be freed (and, without an error, tells the computing warps).
 __device__ __forceinline__ void finish_issue(const Bars& b, bool ok, volatile int* abort_flag, int32_t* status) {
   if (!ok) {
@@ -95,21 +127,6 @@ __device__ __forceinline__ void finish_issue(const Bars& b, bool ok, volatile in
   }
   tc_commit(b.all_done());
   if (!mbar_wait(b.all_done(), 0, abort_flag, false, WAIT_CYCLES / 8)) atomicExch(status, 34);
-}
-
-// Waits for what was asked for last of both streams, so that shared memory may be released.  After an error the sweeper may have left
-// tiles on their raw barriers: those get time to land.
-__device__ __forceinline__ void drain(const Bars& b, int issued, bool ok, volatile int* abort_flag, int32_t* status) {
-  for (int w = 0; w < 2; ++w) {
-    mbar_wait(b.own(w), 0, abort_flag, false, WAIT_CYCLES / 8);
-    for (int i = max(0, issued - STAGES); i < issued; ++i)
-      if (!mbar_wait(b.full(w, i % STAGES), uint32_t(i / STAGES) & 1u, abort_flag, false, WAIT_CYCLES / 8)) atomicExch(status, 32);
-  }
-  if (!ok) {
-    *abort_flag = 1;
-    atomicExch(status, 31);
-    for (int i = 0; i < 64; ++i) __nanosleep(1000);
-  }
 }
 
 // 64 columns of a row times `scale`, rounded, to global memory; the accumulator is ignored where `zero`.
@@ -158,9 +175,13 @@ template <int BOXES>
 __global__ void __launch_bounds__(THREADS, 1)
 attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnArgs a) {
   using L = Smem<BOXES>;
-  extern __shared__ uint8_t smem_raw[];
-  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  uint8_t* gen = smem_raw + (base - raw);
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  const uint32_t base = smem_u32(smem_raw);
+  uint8_t* gen = smem_raw;
+  if (base & 1023u) {                            // swizzled tiles would lie wrong
+    if (threadIdx.x == 0) atomicExch(a.status, 30);
+    return;
+  }
   const Bars b{base + L::bars};
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + L::bars + 192);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + L::bars + 200);
@@ -186,51 +207,59 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
   const int per = i1 - i0, total = per * group;
   set_up<BOXES>(b, warp, tmem_slot, abort_flag);
   const uint32_t tmem = *tmem_slot, t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 256 + BOXES * 64;
-  auto phase = [](int n) { return uint32_t(n / STAGES) & 1u; };
+  auto q_at = [&](int n) { return base + L::s0 + uint32_t(n % PLACES0) * L::kTile; };
+  auto do_at = [&](int n) { return base + L::s1 + uint32_t(n % PLACES1) * L::kTile; };
+  auto rows_at = [&](int n) { return base + L::rows + uint32_t(n % PLACES1) * ROWS_BYTES; };
 
   if (warp == LOADER) {
-    // ------------------------------------------------------------------ loads: stream 0 is q with its row statistics, stream 1 is do
+    // ------------------------------------------------------------------ loads
     if (lane == 0 && total > 0) {
       const int64_t row_blocks = attn_row_blocks(a);
       for (int w = 0; w < 2; ++w) {
         mbar_expect_tx(b.own(w), L::kTile);
         load_tile<BOXES>(base + (w ? L::own1 : L::own0), w ? &maps.v : &maps.k, b.own(w), kvh, s.k0 + c0, s.tb);
       }
-      bool ok = true;
-      int n = 0;
-      for (; n < total && ok; ++n) {
-        const int h = kvh * group + n / per, i = i0 + n % per, st = n % STAGES;
-        if (!(ok = mbar_wait(b.empty(0, st), phase(n) ^ 1u, abort_flag))) break;
-        const bool ragged = (i + 1) * BLK > s.qn;
-        const uint32_t bar0 = ragged ? b.raw(0, st) : b.full(0, st), bar1 = ragged ? b.raw(1, st) : b.full(1, st);
-        mbar_expect_tx(bar0, L::kTile + ROWS_BYTES);
-        load_tile<BOXES>(base + L::s0 + uint32_t(st) * L::kTile, &maps.q, bar0, h, s.q0 + i * BLK, s.tb);
-        bulk_load(base + L::rows + uint32_t(st) * ROWS_BYTES,
-                  a.rows + ((int64_t(s.tb) * a.hq + h) * row_blocks + (a.nseq ? s.q0 / kAttnRowBlock + si : 0) + i) * (2 * kAttnRowBlock), ROWS_BYTES, bar0);
-        ok = mbar_wait(b.empty(1, st), phase(n) ^ 1u, abort_flag);
-        mbar_expect_tx(bar1, L::kTile);                    // armed even when giving up, so that the drain is one rule
-        load_tile<BOXES>(base + L::s1 + uint32_t(st) * L::kTile, &maps.dout, bar1, h, s.q0 + i * BLK, s.tb);
-      }
-      drain(b, n, ok, abort_flag, a.status);
+      auto load_q = [&](int n) {
+        const int h = kvh * group + n / per, i = i0 + n % per;
+        const uint32_t bar = (i + 1) * BLK > s.qn ? b.raw0(n) : b.full0(n);
+        mbar_expect_tx(bar, L::kTile);
+        load_tile<BOXES>(q_at(n), &maps.q, bar, h, s.q0 + i * BLK, s.tb);
+      };
+      auto load_do = [&](int n) {
+        const int h = kvh * group + n / per, i = i0 + n % per;
+        const uint32_t bar = (i + 1) * BLK > s.qn ? b.raw1(n) : b.full1(n);
+        mbar_expect_tx(bar, L::kTile + ROWS_BYTES);
+        bulk_load(rows_at(n), a.rows + ((int64_t(s.tb) * a.hq + h) * row_blocks + (a.nseq ? s.q0 / kAttnRowBlock + si : 0) + i) * (2 * kAttnRowBlock),
+                  ROWS_BYTES, bar);
+        load_tile<BOXES>(do_at(n), &maps.dout, bar, h, s.q0 + i * BLK, s.tb);
+      };
+      load_rounds(b, total, abort_flag, a.status, load_q, load_do);
     }
   } else if (warp == SWEEPER) {
     // ------------------------------------------------------------------ rows past the end: the last block of every head
     if (total > 0 && i1 * BLK > s.qn) {
-      int uses[STAGES] = {};
-      for (int h = 0; h < group; ++h) {
-        const int st = (h * per + per - 1) % STAGES;
-        const uint32_t ph = uint32_t(st ? uses[1]++ : uses[0]++) & 1u;
-        bool ok = true;
+      int uses0[PLACES0] = {}, uses1[PLACES1] = {};
+      auto next_use = [](int (&uses)[PLACES0], int (&uses1)[PLACES1], int w, int n) {
+        int u = 0;
+#pragma unroll
+        for (int i = 0; i < PLACES0; ++i)
+          if (w == 0 && i == n % PLACES0) u = uses[i]++;
+#pragma unroll
+        for (int i = 0; i < PLACES1; ++i)
+          if (w == 1 && i == n % PLACES1) u = uses1[i]++;
+        return uint32_t(u) & 1u;
+      };
+      bool ok = true;
+      for (int h = 0; h < group && ok; ++h) {
+        const int n = h * per + per - 1;
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
-          ok = ok && __all_sync(0xffffffffu, mbar_wait(b.raw(w, st), ph, abort_flag));
-          if (ok) clear_rows<BOXES>(base + (w ? L::s1 : L::s0) + uint32_t(st) * L::kTile, s.qn - (i1 - 1) * BLK, lane, b.full(w, st));
-        }
-        if (!ok) {
-          if (lane == 0) *abort_flag = 1;
-          break;
+          const uint32_t ph = next_use(uses0, uses1, w, n);
+          ok = ok && __all_sync(0xffffffffu, mbar_wait(w ? b.raw1(n) : b.raw0(n), ph, abort_flag));
+          if (ok) clear_rows<BOXES>(w ? do_at(n) : q_at(n), s.qn - (i1 - 1) * BLK, lane, w ? b.full1(n) : b.full0(n));
         }
       }
+      if (!ok && lane == 0) *abort_flag = 1;
     }
   } else if (warp == ISSUER) {
     // ------------------------------------------------------------------ MMA issuer
@@ -239,8 +268,6 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
       const uint32_t idesc = make_idesc(true, BLK, ksteps * 16);
       bool ok = true;
       auto await = [&](uint32_t bar, uint32_t ph) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, ph, abort_flag)); };
-      auto q_at = [&](int n) { return base + L::s0 + uint32_t(n % STAGES) * L::kTile; };
-      auto do_at = [&](int n) { return base + L::s1 + uint32_t(n % STAGES) * L::kTile; };
       auto scores = [&](int n) {
         mma_rows_rows<BOXES>(t_s, base + L::own0, q_at(n), ksteps);
         tc_commit(b.s_full());
@@ -250,28 +277,35 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
         tc_commit(b.dp_full());
       };
       await(b.own(0), 0);
-      await(b.full(0, 0), 0);
+      await(b.full0(0), 0);
       if (ok && elect_one()) scores(0);
       await(b.own(1), 0);
-      await(b.full(1, 0), 0);
+      await(b.full1(0), 0);
       if (ok && elect_one()) dprobs(0);
       for (int n = 0; n < total && ok; ++n) {
         const bool next = n + 1 < total;
-        if (next) await(b.full(0, (n + 1) % STAGES), phase(n + 1));
-        await(b.p_ready(), uint32_t(n) & 1u);
+        if (next) await(b.full0(n + 1), phase0(n + 1));
+        // P comes in two parts, each half of what either warp of a quadrant has: steps 0, 1, 4, 5 and then 2, 3, 6, 7
+        await(b.p_ready(0), uint32_t(n) & 1u);
         tc_fence_after();                                  // tensor memory written by other threads; tiles need no such fence
-        if (ok && elect_one()) {
-          mma_probs_rows(t_dv, t_s, t_s + 64, do_at(n), idesc, n > 0);       // dv += P^T do
-          if (next) scores(n + 1);                         // takes the place of P^T, which dv has read by then
-          tc_commit(b.empty(1, n % STAGES));               // dP^T of this block was issued earlier
+        if (ok && elect_one()) {                           // dv += P^T do
+          mma_probs_rows<0, 2>(t_dv, t_s, t_s + 64, do_at(n), idesc, n > 0);
+          mma_probs_rows<4, 6>(t_dv, t_s, t_s + 64, do_at(n), idesc, true);
         }
-        if (next) await(b.full(1, (n + 1) % STAGES), phase(n + 1));
+        await(b.p_ready(1), uint32_t(n) & 1u);
+        tc_fence_after();
+        if (ok && elect_one()) {
+          mma_probs_rows<2, 4>(t_dv, t_s, t_s + 64, do_at(n), idesc, true);
+          mma_probs_rows<6, 8>(t_dv, t_s, t_s + 64, do_at(n), idesc, true);
+          if (next) scores(n + 1);                         // takes the place of P^T, which dv has read by then
+        }
+        if (next) await(b.full1(n + 1), phase1(n + 1));
         await(b.ds_ready(), uint32_t(n) & 1u);
         tc_fence_after();
         if (ok && elect_one()) {
           mma_probs_rows(t_dk, t_dp, t_dp + 64, q_at(n), idesc, n > 0);      // dk += dS^T q
           if (next) dprobs(n + 1);
-          tc_commit(b.empty(0, n % STAGES));
+          tc_commit(b.round_done(n));
         }
       }
       if (elect_one()) finish_issue(b, ok, abort_flag, a.status);
@@ -290,42 +324,49 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
     bool ok = true;
     for (int n = 0; n < total; ++n) {
       const int r0 = (i0 + n % per) * BLK;
-      ok = __all_sync(0xffffffffu, mbar_wait(b.full(0, n % STAGES), phase(n), abort_flag)) &&     // the row statistics
+      ok = __all_sync(0xffffffffu, mbar_wait(b.full1(n), phase1(n), abort_flag)) &&               // the row statistics
            __all_sync(0xffffffffu, mbar_wait(b.s_full(), uint32_t(n) & 1u, abort_flag));
       if (!ok) break;
       tc_fence_after();
-      const uint32_t rows = base + L::rows + uint32_t(n % STAGES) * ROWS_BYTES + uint32_t(half) * 256u;
+      const uint32_t rows = rows_at(n) + uint32_t(half) * 256u;
       const int first = qlo - r0 - half * 64, last = qhi - r0 - half * 64;
       auto step = [&](auto with_mask) {
         constexpr bool MASK = decltype(with_mask)::value;
         uint64_t p[32];
+        auto hand_over = [&](uint32_t bar) {
+          tc_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar);
+        };
         {
-          uint32_t x[64], w[32];
+          uint32_t x[64];
 #pragma unroll
           for (int i = 0; i < 2; ++i) tc_ld32(ts + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[i * 32]));
           tc_wait_ld();
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const Pairs l2 = lds_pairs(rows + uint32_t(i) * 16u);
-            p[2 * i] = exp2_approx(fma2(words(x[4 * i], x[4 * i + 1]), twice(c2), l2.a));
-            p[2 * i + 1] = exp2_approx(fma2(words(x[4 * i + 2], x[4 * i + 3]), twice(c2), l2.b));
-            if constexpr (MASK) {
+          for (int c = 0; c < 2; ++c) {                    // 32 of this warp's queries at a time, into its own columns: the other half may still be read
+            uint32_t w[16];
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const float2 f = both(p[2 * i + e]);
-                const int q = 4 * i + 2 * e;
-                p[2 * i + e] = two(q < first || q >= last ? 0.f : f.x, q + 1 < first || q + 1 >= last ? 0.f : f.y);
+            for (int i = c * 8; i < c * 8 + 8; ++i) {
+              const Pairs l2 = lds_pairs(rows + uint32_t(i) * 16u);
+              p[2 * i] = exp2_approx(fma2(words(x[4 * i], x[4 * i + 1]), twice(c2), l2.a));
+              p[2 * i + 1] = exp2_approx(fma2(words(x[4 * i + 2], x[4 * i + 3]), twice(c2), l2.b));
+              if constexpr (MASK) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  const float2 f = both(p[2 * i + e]);
+                  const int q = 4 * i + 2 * e;
+                  p[2 * i + e] = two(q < first || q >= last ? 0.f : f.x, q + 1 < first || q + 1 >= last ? 0.f : f.y);
+                }
               }
+              w[2 * i - c * 16] = pack_bf16(p[2 * i]);
+              w[2 * i + 1 - c * 16] = pack_bf16(p[2 * i + 1]);
             }
-            w[2 * i] = pack_bf16(p[2 * i]);
-            w[2 * i + 1] = pack_bf16(p[2 * i + 1]);
+            tc_st16(ts + c * 16, w);
+            hand_over(b.p_ready(c));
           }
-          tc_st32(ts, w);                                  // into this warp's own columns: the other half may still be read
         }
-        tc_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(b.p_ready());
 
         ok = __all_sync(0xffffffffu, mbar_wait(b.dp_full(), uint32_t(n) & 1u, abort_flag));
         if (!ok) return;
@@ -341,10 +382,7 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
           w[2 * i + 1] = ds_pair<MASK>(p[2 * i + 1], words(x[4 * i + 2], x[4 * i + 3]), d.b);
         }
         tc_st32(tp, w);
-        tc_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(b.ds_ready());
+        hand_over(b.ds_ready());
       };
       if (block_masked(a, s, r0, c0) || r0 + BLK > s.qn || c0 + BLK > s.kn) step(Yes());
       else step(No());
@@ -374,9 +412,13 @@ template <int BOXES>
 __global__ void __launch_bounds__(THREADS, 1)
 attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnArgs a) {
   using L = Smem<BOXES>;
-  extern __shared__ uint8_t smem_raw[];
-  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  uint8_t* gen = smem_raw + (base - raw);
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  const uint32_t base = smem_u32(smem_raw);
+  uint8_t* gen = smem_raw;
+  if (base & 1023u) {                            // swizzled tiles would lie wrong
+    if (threadIdx.x == 0) atomicExch(a.status, 30);
+    return;
+  }
   const Bars b{base + L::bars};
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + L::bars + 192);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + L::bars + 200);
@@ -398,35 +440,32 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
   // Two places for S, each with its barrier: the next S is formed while this one is read, and a barrier that both shared could complete
   // twice before a slow warp looks at it.
   auto t_s = [&](int n) { return tmem + uint32_t(n & 1) * 128u; };
-  auto phase = [](int n) { return uint32_t(n / STAGES) & 1u; };
+  auto k_at = [&](int n) { return base + L::s0 + uint32_t(n % PLACES0) * L::kTile; };
+  auto v_at = [&](int n) { return base + L::s1 + uint32_t(n % PLACES1) * L::kTile; };
 
   if (warp == LOADER) {
-    // ------------------------------------------------------------------ loads: stream 0 is k, stream 1 is v
+    // ------------------------------------------------------------------ loads
     if (lane == 0 && total > 0) {
       for (int w = 0; w < 2; ++w) {
         mbar_expect_tx(b.own(w), L::kTile);
         load_tile<BOXES>(base + (w ? L::own1 : L::own0), w ? &maps.dout : &maps.q, b.own(w), head, s.q0 + r0, s.tb);
       }
-      bool ok = true;
-      int n = 0;
-      for (; n < total && ok; ++n) {
-        const int st = n % STAGES, token = s.k0 + (rg.n0 + n) * BLK;
-        if (!(ok = mbar_wait(b.empty(0, st), phase(n) ^ 1u, abort_flag))) break;
-        const uint32_t bar0 = (rg.n0 + n + 1) * BLK > s.kn ? b.raw(0, st) : b.full(0, st);
-        mbar_expect_tx(bar0, L::kTile);
-        load_tile<BOXES>(base + L::s0 + uint32_t(st) * L::kTile, &maps.k, bar0, kvh, token, s.tb);
-        ok = mbar_wait(b.empty(1, st), phase(n) ^ 1u, abort_flag);
-        mbar_expect_tx(b.full(1, st), L::kTile);
-        load_tile<BOXES>(base + L::s1 + uint32_t(st) * L::kTile, &maps.v, b.full(1, st), kvh, token, s.tb);
-      }
-      drain(b, n, ok, abort_flag, a.status);
+      auto load_k = [&](int n) {
+        const uint32_t bar = (rg.n0 + n + 1) * BLK > s.kn ? b.raw0(n) : b.full0(n);
+        mbar_expect_tx(bar, L::kTile);
+        load_tile<BOXES>(k_at(n), &maps.k, bar, kvh, s.k0 + (rg.n0 + n) * BLK, s.tb);
+      };
+      auto load_v = [&](int n) {
+        mbar_expect_tx(b.full1(n), L::kTile);
+        load_tile<BOXES>(v_at(n), &maps.v, b.full1(n), kvh, s.k0 + (rg.n0 + n) * BLK, s.tb);
+      };
+      load_rounds(b, total, abort_flag, a.status, load_k, load_v);
     }
   } else if (warp == SWEEPER) {
     // ------------------------------------------------------------------ rows of the last k tile past the end: their dS is zero, and so must be dS k
     if (total > 0 && rg.n1 * BLK > s.kn) {
-      const int st = (total - 1) % STAGES;
-      if (__all_sync(0xffffffffu, mbar_wait(b.raw(0, st), 0, abort_flag)))
-        clear_rows<BOXES>(base + L::s0 + uint32_t(st) * L::kTile, s.kn - (rg.n1 - 1) * BLK, lane, b.full(0, st));
+      if (__all_sync(0xffffffffu, mbar_wait(b.raw0(total - 1), 0, abort_flag)))
+        clear_rows<BOXES>(k_at(total - 1), s.kn - (rg.n1 - 1) * BLK, lane, b.full0(total - 1));
       else if (lane == 0) *abort_flag = 1;
     }
   } else if (warp == ISSUER) {
@@ -436,8 +475,6 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
       const uint32_t idesc = make_idesc(true, BLK, ksteps * 16);
       bool ok = true;
       auto await = [&](uint32_t bar, uint32_t ph) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, ph, abort_flag)); };
-      auto k_at = [&](int n) { return base + L::s0 + uint32_t(n % STAGES) * L::kTile; };
-      auto v_at = [&](int n) { return base + L::s1 + uint32_t(n % STAGES) * L::kTile; };
       auto scores = [&](int n) {
         mma_rows_rows<BOXES>(t_s(n), base + L::own0, k_at(n), ksteps);
         tc_commit(b.s_full(n & 1));
@@ -445,27 +482,26 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
       auto dprobs = [&](int n) {
         mma_rows_rows<BOXES>(t_dp, base + L::own1, v_at(n), ksteps);
         tc_commit(b.dp_full());
-        tc_commit(b.empty(1, n % STAGES));
       };
       await(b.own(0), 0);
-      await(b.full(0, 0), 0);
+      await(b.full0(0), 0);
       if (ok && elect_one()) scores(0);
       await(b.own(1), 0);
-      await(b.full(1, 0), 0);
+      await(b.full1(0), 0);
       if (ok && elect_one()) dprobs(0);
       for (int n = 0; n < total && ok; ++n) {
         const bool next = n + 1 < total;
         if (next) {
-          await(b.full(0, (n + 1) % STAGES), phase(n + 1));
+          await(b.full0(n + 1), phase0(n + 1));
           if (ok && elect_one()) scores(n + 1);            // its place was read before dS of block n - 1 was ready
-          await(b.full(1, (n + 1) % STAGES), phase(n + 1));
+          await(b.full1(n + 1), phase1(n + 1));
         }
         await(b.ds_ready(), uint32_t(n) & 1u);
         tc_fence_after();                                  // tensor memory written by other threads; tiles need no such fence
         if (ok && elect_one()) {
           mma_probs_rows(t_dq, t_dp, t_dp + 64, k_at(n), idesc, n > 0);      // dq += dS k
           if (next) dprobs(n + 1);
-          tc_commit(b.empty(0, n % STAGES));
+          tc_commit(b.round_done(n));
         }
       }
       if (elect_one()) finish_issue(b, ok, abort_flag, a.status);

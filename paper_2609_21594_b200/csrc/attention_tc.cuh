@@ -89,6 +89,15 @@ __device__ __forceinline__ void tc_st8(uint32_t taddr, const uint32_t (&r)[8]) {
                : "memory");
 }
 
+__device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
 __device__ __forceinline__ uint64_t words(uint32_t a, uint32_t b) { return two(__uint_as_float(a), __uint_as_float(b)); }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
@@ -137,7 +146,7 @@ __device__ __forceinline__ void mma_probs_rows(uint32_t d_tmem, uint32_t p_lo, u
   const uint64_t dy = make_desc(y, BOX_BYTES, 1024);
 #pragma unroll
   for (int k = K0; k < K1; ++k)
-    tc_mma_ts(d_tmem, (k < 4 ? p_lo : p_hi) + uint32_t(k & 3) * 8u, dy + uint32_t(k) * 128u, idesc, accumulate || k > 0);
+    tc_mma_ts(d_tmem, (k < 4 ? p_lo : p_hi) + uint32_t(k & 3) * 8u, dy + uint32_t(k) * 128u, idesc, accumulate || k > K0);
 }
 
 // Clears the rows of a tile from `first` on (a whole warp) and arrives on `bar`.  Rows past a sequence's end hold another sequence's tokens or padding; they meet
