@@ -23,16 +23,17 @@ namespace {
 using namespace attn;
 
 constexpr int THREADS = 352, TMEM_COLS = 512, LOADER = 8, ISSUER = 9, SWEEPER = 10;
-constexpr uint32_t ROWS_BYTES = 2 * kAttnRowBlock * sizeof(float);     // lse and delta of 128 queries
+constexpr uint32_t ROW_BYTES = kAttnRowBlock * sizeof(float);          // one value for each of 128 queries
 
-// Both streams bring one tile per round.  Stream 0 (q; k in the dq kernel) feeds the first product of a round and the last, so when the next
-// round begins its tile has only just been read for the last time: three places.  Stream 1 (do with the row statistics; v) has two.
+// Both streams bring one tile per round, and a tile takes 1200 to 1700 clocks from the request to its arrival, most of a round.  Stream 0 (q; k
+// in the dq kernel) feeds the first product of a round and the last: three places.  Stream 1 (do; v) is read for the last time early in
+// its round: two.  Of the row statistics, lse is read with stream 1's tile and delta until the end of the round.
 constexpr int PLACES0 = 3, PLACES1 = 2;
 
 template <int BOXES> struct Smem {
   static constexpr uint32_t kTile = BOXES * BOX_BYTES;
-  static constexpr uint32_t own0 = 0, own1 = kTile, s0 = 2 * kTile, s1 = s0 + PLACES0 * kTile, rows = s1 + PLACES1 * kTile;
-  static constexpr uint32_t bars = rows + PLACES1 * ROWS_BYTES;
+  static constexpr uint32_t own0 = 0, own1 = kTile, s0 = 2 * kTile, s1 = s0 + PLACES0 * kTile, lse = s1 + PLACES1 * kTile;
+  static constexpr uint32_t delta = lse + PLACES1 * ROW_BYTES, bars = delta + PLACES0 * ROW_BYTES;
   static constexpr uint32_t bytes = bars + 256;
   static_assert(bytes <= 227 * 1024, "shared memory of a block");   // no room to align the base, which its declaration aligns (and the kernels check)
 };
@@ -46,20 +47,21 @@ struct Bars {
   __device__ __forceinline__ uint32_t p_ready(int part = 0) const { return at(5 + part); }
   __device__ __forceinline__ uint32_t ds_ready() const { return at(7); }
   __device__ __forceinline__ uint32_t all_done() const { return at(8); }
-  // Round n has been read: its places may be loaded again.  Two barriers in turn: round n + 2 cannot end before the loader, past round n,
-  // has brought what it needs, so neither completes twice unseen.
-  __device__ __forceinline__ uint32_t round_done(int n) const { return at(9 + (n & 1)); }
+  // Round n's tile of the stream has been read: its place may be loaded again.  Two barriers in turn: round n + 2 cannot get there before
+  // the loader, past round n, has brought what it needs, so neither completes twice unseen.
+  __device__ __forceinline__ uint32_t free0(int n) const { return at(9 + (n & 1)); }
+  __device__ __forceinline__ uint32_t free1(int n) const { return at(11 + 2 * (PLACES0 + PLACES1) + (n & 1)); }
   __device__ __forceinline__ uint32_t full0(int n) const { return at(11 + n % PLACES0); }
   __device__ __forceinline__ uint32_t full1(int n) const { return at(11 + PLACES0 + n % PLACES1); }
   // where a tile with rows past the end arrives; the sweeper passes it on to `full`
   __device__ __forceinline__ uint32_t raw0(int n) const { return at(11 + PLACES0 + PLACES1 + n % PLACES0); }
   __device__ __forceinline__ uint32_t raw1(int n) const { return at(11 + 2 * PLACES0 + PLACES1 + n % PLACES1); }
-  static constexpr int count = 11 + 2 * (PLACES0 + PLACES1);
+  static constexpr int count = 13 + 2 * (PLACES0 + PLACES1);
 };
 static_assert(Bars::count * 8 <= 192, "barriers");
 __device__ __forceinline__ uint32_t phase0(int n) { return uint32_t(n / PLACES0) & 1u; }
 __device__ __forceinline__ uint32_t phase1(int n) { return uint32_t(n / PLACES1) & 1u; }
-__device__ __forceinline__ uint32_t phase_done(int n) { return uint32_t(n >> 1) & 1u; }
+__device__ __forceinline__ uint32_t phase_free(int n) { return uint32_t(n >> 1) & 1u; }
 
 template <int BOXES>
 __device__ __forceinline__ void set_up(const Bars& b, int warp, uint32_t* tmem_slot, volatile int* abort_flag) {
@@ -88,22 +90,22 @@ __device__ __forceinline__ void tear_down(int warp, uint32_t tmem) {
   }
 }
 
-// The loading thread: load0(n) and load1(n) ask for round n's tiles as soon as their places are free.
+// The loading thread: load0(n) and load1(n) ask for round n's tiles as soon as their places are free, in the order in which that happens.
 template <typename L0, typename L1>
 __device__ __forceinline__ void load_rounds(const Bars& b, int total, volatile int* abort_flag, int32_t* status, L0 load0, L1 load1) {
   bool ok = true;
   int n0 = 0, n1 = 0;
-  while (ok && n0 < total) {
-    if (n0 >= PLACES0) ok = mbar_wait(b.round_done(n0 - PLACES0), phase_done(n0 - PLACES0), abort_flag);
-    if (!ok) break;
-    for (; n1 < total && n1 <= n0 - PLACES0 + PLACES1; ++n1) load1(n1);
-    load0(n0++);
-    if (n0 <= PLACES1)
-      for (; n1 < n0; ++n1) load1(n1);
+  for (; n0 < total && n0 < PLACES0; ++n0) {
+    load0(n0);
+    if (n1 < total && n1 < PLACES1) load1(n1++);
   }
-  for (; ok && n1 < total; ++n1) {
-    if (n1 >= PLACES1) ok = mbar_wait(b.round_done(n1 - PLACES1), phase_done(n1 - PLACES1), abort_flag);
-    if (ok) load1(n1);
+  for (int n = 0; ok && n1 < total; ++n) {
+    ok = mbar_wait(b.free1(n), phase_free(n), abort_flag);
+    if (ok) load1(n1++);
+    if (ok && n0 < total) {
+      ok = mbar_wait(b.free0(n), phase_free(n), abort_flag);
+      if (ok) load0(n0++);
+    }
   }
   // Everything asked for must have landed before this block's shared memory is released.  After an error the sweeper may have left tiles
   // on their raw barriers: those get time to land.
@@ -209,7 +211,8 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
   const uint32_t tmem = *tmem_slot, t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 256 + BOXES * 64;
   auto q_at = [&](int n) { return base + L::s0 + uint32_t(n % PLACES0) * L::kTile; };
   auto do_at = [&](int n) { return base + L::s1 + uint32_t(n % PLACES1) * L::kTile; };
-  auto rows_at = [&](int n) { return base + L::rows + uint32_t(n % PLACES1) * ROWS_BYTES; };
+  auto lse_at = [&](int n) { return base + L::lse + uint32_t(n % PLACES1) * ROW_BYTES; };
+  auto delta_at = [&](int n) { return base + L::delta + uint32_t(n % PLACES0) * ROW_BYTES; };
 
   if (warp == LOADER) {
     // ------------------------------------------------------------------ loads
@@ -228,9 +231,10 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
       auto load_do = [&](int n) {
         const int h = kvh * group + n / per, i = i0 + n % per;
         const uint32_t bar = (i + 1) * BLK > s.qn ? b.raw1(n) : b.full1(n);
-        mbar_expect_tx(bar, L::kTile + ROWS_BYTES);
-        bulk_load(rows_at(n), a.rows + ((int64_t(s.tb) * a.hq + h) * row_blocks + (a.nseq ? s.q0 / kAttnRowBlock + si : 0) + i) * (2 * kAttnRowBlock),
-                  ROWS_BYTES, bar);
+        const float* rows = a.rows + ((int64_t(s.tb) * a.hq + h) * row_blocks + (a.nseq ? s.q0 / kAttnRowBlock + si : 0) + i) * (2 * kAttnRowBlock);
+        mbar_expect_tx(bar, L::kTile + 2 * ROW_BYTES);
+        bulk_load(lse_at(n), rows, ROW_BYTES, bar);
+        bulk_load(delta_at(n), rows + kAttnRowBlock, ROW_BYTES, bar);
         load_tile<BOXES>(do_at(n), &maps.dout, bar, h, s.q0 + i * BLK, s.tb);
       };
       load_rounds(b, total, abort_flag, a.status, load_q, load_do);
@@ -297,6 +301,7 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
         if (ok && elect_one()) {
           mma_probs_rows<2, 4>(t_dv, t_s, t_s + 64, do_at(n), idesc, true);
           mma_probs_rows<6, 8>(t_dv, t_s, t_s + 64, do_at(n), idesc, true);
+          tc_commit(b.free1(n));                           // dP^T of this block was issued earlier
           if (next) scores(n + 1);                         // takes the place of P^T, which dv has read by then
         }
         if (next) await(b.full1(n + 1), phase1(n + 1));
@@ -304,8 +309,8 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
         tc_fence_after();
         if (ok && elect_one()) {
           mma_probs_rows(t_dk, t_dp, t_dp + 64, q_at(n), idesc, n > 0);      // dk += dS^T q
+          tc_commit(b.free0(n));
           if (next) dprobs(n + 1);
-          tc_commit(b.round_done(n));
         }
       }
       if (elect_one()) finish_issue(b, ok, abort_flag, a.status);
@@ -328,7 +333,7 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
            __all_sync(0xffffffffu, mbar_wait(b.s_full(), uint32_t(n) & 1u, abort_flag));
       if (!ok) break;
       tc_fence_after();
-      const uint32_t rows = rows_at(n) + uint32_t(half) * 256u;
+      const uint32_t lse = lse_at(n) + uint32_t(half) * 256u, delta = delta_at(n) + uint32_t(half) * 256u;
       const int first = qlo - r0 - half * 64, last = qhi - r0 - half * 64;
       auto step = [&](auto with_mask) {
         constexpr bool MASK = decltype(with_mask)::value;
@@ -349,7 +354,7 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
             uint32_t w[16];
 #pragma unroll
             for (int i = c * 8; i < c * 8 + 8; ++i) {
-              const Pairs l2 = lds_pairs(rows + uint32_t(i) * 16u);
+              const Pairs l2 = lds_pairs(lse + uint32_t(i) * 16u);
               p[2 * i] = exp2_approx(fma2(words(x[4 * i], x[4 * i + 1]), twice(c2), l2.a));
               p[2 * i + 1] = exp2_approx(fma2(words(x[4 * i + 2], x[4 * i + 3]), twice(c2), l2.b));
               if constexpr (MASK) {
@@ -377,7 +382,7 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
         tc_wait_ld();
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const Pairs d = lds_pairs(rows + kAttnRowBlock * 4u + uint32_t(i) * 16u);
+          const Pairs d = lds_pairs(delta + uint32_t(i) * 16u);
           w[2 * i] = ds_pair<MASK>(p[2 * i], words(x[4 * i], x[4 * i + 1]), d.a);
           w[2 * i + 1] = ds_pair<MASK>(p[2 * i + 1], words(x[4 * i + 2], x[4 * i + 3]), d.b);
         }
@@ -482,6 +487,7 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
       auto dprobs = [&](int n) {
         mma_rows_rows<BOXES>(t_dp, base + L::own1, v_at(n), ksteps);
         tc_commit(b.dp_full());
+        tc_commit(b.free1(n));
       };
       await(b.own(0), 0);
       await(b.full0(0), 0);
@@ -500,8 +506,8 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
         tc_fence_after();                                  // tensor memory written by other threads; tiles need no such fence
         if (ok && elect_one()) {
           mma_probs_rows(t_dq, t_dp, t_dp + 64, k_at(n), idesc, n > 0);      // dq += dS k
+          tc_commit(b.free0(n));
           if (next) dprobs(n + 1);
-          tc_commit(b.round_done(n));
         }
       }
       if (elect_one()) finish_issue(b, ok, abort_flag, a.status);
