@@ -282,38 +282,38 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
       };
       await(b.own(0), 0);
       await(b.full0(0), 0);
-      if (ok && elect_one()) scores(0);
+      elected(ok, [&] { scores(0); });
       await(b.own(1), 0);
       await(b.full1(0), 0);
-      if (ok && elect_one()) dprobs(0);
+      elected(ok, [&] { dprobs(0); });
       for (int n = 0; n < total && ok; ++n) {
         const bool next = n + 1 < total;
         if (next) await(b.full0(n + 1), phase0(n + 1));
         // P comes in two parts, each half of what either warp of a quadrant has: steps 0, 1, 4, 5 and then 2, 3, 6, 7
         await(b.p_ready(0), uint32_t(n) & 1u);
         tc_fence_after();                                  // tensor memory written by other threads; tiles need no such fence
-        if (ok && elect_one()) {                           // dv += P^T do
+        elected(ok, [&] {                           // dv += P^T do
           mma_probs_rows<0, 2>(t_dv, t_s, t_s + 64, do_at(n), idesc, n > 0);
           mma_probs_rows<4, 6>(t_dv, t_s, t_s + 64, do_at(n), idesc, true);
-        }
+        });
         await(b.p_ready(1), uint32_t(n) & 1u);
         tc_fence_after();
-        if (ok && elect_one()) {
+        elected(ok, [&] {
           mma_probs_rows<2, 4>(t_dv, t_s, t_s + 64, do_at(n), idesc, true);
           mma_probs_rows<6, 8>(t_dv, t_s, t_s + 64, do_at(n), idesc, true);
           tc_commit(b.free1(n));                           // dP^T of this block was issued earlier
           if (next) scores(n + 1);                         // takes the place of P^T, which dv has read by then
-        }
+        });
         if (next) await(b.full1(n + 1), phase1(n + 1));
         await(b.ds_ready(), uint32_t(n) & 1u);
         tc_fence_after();
-        if (ok && elect_one()) {
+        elected(ok, [&] {
           mma_probs_rows(t_dk, t_dp, t_dp + 64, q_at(n), idesc, n > 0);      // dk += dS^T q
           tc_commit(b.free0(n));
           if (next) dprobs(n + 1);
-        }
+        });
       }
-      if (elect_one()) finish_issue(b, ok, abort_flag, a.status);
+      elected(true, [&] { finish_issue(b, ok, abort_flag, a.status); });
     }
     __syncwarp();
   } else {
@@ -491,26 +491,26 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
       };
       await(b.own(0), 0);
       await(b.full0(0), 0);
-      if (ok && elect_one()) scores(0);
+      elected(ok, [&] { scores(0); });
       await(b.own(1), 0);
       await(b.full1(0), 0);
-      if (ok && elect_one()) dprobs(0);
+      elected(ok, [&] { dprobs(0); });
       for (int n = 0; n < total && ok; ++n) {
         const bool next = n + 1 < total;
         if (next) {
           await(b.full0(n + 1), phase0(n + 1));
-          if (ok && elect_one()) scores(n + 1);            // its place was read before dS of block n - 1 was ready
+          elected(ok, [&] { scores(n + 1); });            // its place was read before dS of block n - 1 was ready
           await(b.full1(n + 1), phase1(n + 1));
         }
         await(b.ds_ready(), uint32_t(n) & 1u);
         tc_fence_after();                                  // tensor memory written by other threads; tiles need no such fence
-        if (ok && elect_one()) {
+        elected(ok, [&] {
           mma_probs_rows(t_dq, t_dp, t_dp + 64, k_at(n), idesc, n > 0);      // dq += dS k
           tc_commit(b.free0(n));
           if (next) dprobs(n + 1);
-        }
+        });
       }
-      if (elect_one()) finish_issue(b, ok, abort_flag, a.status);
+      elected(true, [&] { finish_issue(b, ok, abort_flag, a.status); });
     }
     __syncwarp();
   } else {

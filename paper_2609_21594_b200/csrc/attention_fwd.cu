@@ -154,13 +154,13 @@ attention_forward_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_
             if (pv) {
               await(p_ready(t, 0), uint32_t(j - rg[t].n0) & 1u);
               tc_fence_after();                            // tensor memory written by other threads; tiles need no such fence
-              if (ok && elect_one()) mma_probs_rows<0, 4>(t_o[t], t_s[t], t_s[t] + 32, v, idesc_o, j > rg[t].n0);
+              elected(ok, [&] { mma_probs_rows<0, 4>(t_o[t], t_s[t], t_s[t] + 32, v, idesc_o, j > rg[t].n0); });
               await(p_ready(t, 1), uint32_t(j - rg[t].n0) & 1u);
               tc_fence_after();
             } else if (next) {
               await(q_full(t), 0);
             }
-            if (ok && elect_one()) {
+            elected(ok, [&] {
               if (pv) mma_probs_rows<4, 8>(t_o[t], t_s[t], t_s[t] + 32, v, idesc_o, true);
               if (pv && !next) tc_commit(o_full(t));
               if (next) {
@@ -168,7 +168,7 @@ attention_forward_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_
                 tc_commit(s_full(t));
               }
               if (t == 1) tc_commit(empty(st));
-            }
+            });
           }
         }
         // Nothing may be in flight when tensor memory is freed.

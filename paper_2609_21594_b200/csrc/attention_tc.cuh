@@ -123,6 +123,12 @@ __device__ __forceinline__ bool elect_one() {
       : "=r"(one));
   return one != 0;
 }
+// Runs f on the elected lane.  Without the meeting behind it the other lanes go on to the next wait and share the issue slots with it.
+template <typename F>
+__device__ __forceinline__ void elected(bool go, F f) {
+  if (go && elect_one()) f();
+  __syncwarp();
+}
 __device__ __forceinline__ int uniform_warp() { return __shfl_sync(0xffffffffu, int(threadIdx.x >> 5), 0); }
 
 // Descriptors are formed once per tile: a step adds to the address field, which no address in shared memory carries out of.
