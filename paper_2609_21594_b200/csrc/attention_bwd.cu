@@ -156,6 +156,9 @@ __device__ __forceinline__ void store_half(const AttnTensor& t, int tb, int toke
   }
 }
 
+constexpr int kPolyOf = 2;                       // one pair of exponentials in 2 * kPolyOf on the multiply-add pipe; `poly` is known at compile time
+__device__ __forceinline__ uint64_t exp2_share(bool poly, uint64_t v) { return poly ? exp2_poly(v) : exp2_approx(v); }
+
 struct Pairs { uint64_t a, b; };
 __device__ __forceinline__ Pairs lds_pairs(uint32_t addr) {
   Pairs v;
@@ -356,7 +359,7 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
             for (int i = c * 8; i < c * 8 + 8; ++i) {
               const Pairs l2 = lds_pairs(lse + uint32_t(i) * 16u);
               p[2 * i] = exp2_approx(fma2(words(x[4 * i], x[4 * i + 1]), twice(c2), l2.a));
-              p[2 * i + 1] = exp2_approx(fma2(words(x[4 * i + 2], x[4 * i + 3]), twice(c2), l2.b));
+              p[2 * i + 1] = exp2_share(!MASK && i % kPolyOf == 0, fma2(words(x[4 * i + 2], x[4 * i + 3]), twice(c2), l2.b));
               if constexpr (MASK) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
@@ -541,7 +544,7 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
           tc_wait_ld();
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
-            p[i] = exp2_approx(fma2(words(x[2 * i], x[2 * i + 1]), twice(c2), twice(l2)));
+            p[i] = exp2_share(!MASK && i % (2 * kPolyOf) == 1, fma2(words(x[2 * i], x[2 * i + 1]), twice(c2), twice(l2)));
             if constexpr (MASK) {
               const float2 f = both(p[i]);
               p[i] = two(2 * i < first || 2 * i >= last ? 0.f : f.x, 2 * i + 1 < first || 2 * i + 1 >= last ? 0.f : f.y);
