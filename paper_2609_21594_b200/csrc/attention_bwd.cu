@@ -6,7 +6,10 @@
 //            per block of queries enters shared memory.
 //   dq:      a block owns 128 queries and walks the blocks of keys they see: S = q k^T, dP = do v^T, dq += dS k.
 //
-// Seven products of 128 x 128 x head_dim per pair of blocks instead of the five that a single kernel needs: a single kernel would add every
+// Both start with their longest blocks, and those of dq, which need nothing of dk and dv, fill the SMs that the last blocks of dk and dv leave
+// (launched programmatically; as two kinds of blocks of one kernel each would run 5 % slower).
+//
+// Seven products of 128 x 128 x head_dim per pair of tiles instead of the five that a single kernel needs: that would add every
 // block's share of dq (or of dk and dv) with float atomics, whose order changes from run to run, or keep fp32 partial sums as large as
 // the number of blocks; here every sum has one owner and a fixed order.
 //
@@ -219,6 +222,12 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
 
   if (warp == LOADER) {
     // ------------------------------------------------------------------ loads
+    // Only this thread reads the row statistics here.  Once every block has waited for them (so they are there for the dq kernel too), the
+    // dq kernel may begin.  (The same two calls by all threads cost 10 % of the kernel's time.)
+    if (lane == 0) {
+      cudaGridDependencySynchronize();
+      cudaTriggerProgrammaticLaunchCompletion();
+    }
     if (lane == 0 && total > 0) {
       const int64_t row_blocks = attn_row_blocks(a);
       for (int w = 0; w < 2; ++w) {
@@ -416,6 +425,11 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
 }
 
 // ------------------------------------------------------------------ dq
+// Whoever waits for the dq kernel waits for both: its last block stays until the kernel before it, which it may have overtaken, has ended.
+__device__ __forceinline__ void stay() {
+  if (blockIdx.x == gridDim.x - 1) cudaGridDependencySynchronize();
+}
+
 template <int BOXES>
 __global__ void __launch_bounds__(THREADS, 1)
 attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnArgs a) {
@@ -424,7 +438,10 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
   const uint32_t base = smem_u32(smem_raw);
   uint8_t* gen = smem_raw;
   if (base & 1023u) {                            // swizzled tiles would lie wrong
-    if (threadIdx.x == 0) atomicExch(a.status, 30);
+    if (threadIdx.x == 0) {
+      atomicExch(a.status, 30);
+      stay();
+    }
     return;
   }
   const Bars b{base + L::bars};
@@ -433,7 +450,10 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
   const int warp = uniform_warp(), lane = threadIdx.x & 31;
   const int head = int(blockIdx.x % unsigned(a.hq)), kvh = head / (a.hq / a.hkv);
   int si, blk;
-  if (!attn_find_block(a, int(blockIdx.x / unsigned(a.hq)), BLK, false, &si, &blk)) return;
+  if (!attn_find_block(a, int(blockIdx.x / unsigned(a.hq)), BLK, false, &si, &blk)) {
+    if (threadIdx.x == 0) stay();
+    return;
+  }
   if (!a.nseq) {
     const int rest = int(blockIdx.x / unsigned(a.hq)), per = (a.nq + BLK - 1) / BLK;
     si = rest % a.batch;
@@ -469,6 +489,7 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
       };
       load_rounds(b, total, abort_flag, a.status, load_k, load_v);
     }
+    if (lane == 0) stay();
   } else if (warp == SWEEPER) {
     // ------------------------------------------------------------------ rows of the last k tile past the end: their dS is zero, and so must be dS k
     if (total > 0 && rg.n1 * BLK > s.kn) {
@@ -595,9 +616,19 @@ int run(const AttnMaps& m, const AttnArgs& a, cudaStream_t st) {
   constexpr uint32_t bytes = Smem<BOXES>::bytes;
   static SharedMemoryLimit limit;
   if (!limit.raise(a.device, bytes, attention_dkv_tc_kernel<BOXES>, attention_dq_tc_kernel<BOXES>)) return MUON_ERR_CUDA;
-  attention_dkv_tc_kernel<BOXES><<<unsigned(kb), THREADS, bytes, st>>>(m, a);
-  attention_dq_tc_kernel<BOXES><<<unsigned(qb), THREADS, bytes, st>>>(m, a);
-  return cudaGetLastError() == cudaSuccess ? 2 : MUON_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = bytes;
+  cfg.stream = st;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  cfg.gridDim = dim3(unsigned(kb));
+  if (cudaLaunchKernelEx(&cfg, attention_dkv_tc_kernel<BOXES>, m, a) != cudaSuccess) return MUON_ERR_CUDA;
+  cfg.gridDim = dim3(unsigned(qb));
+  return cudaLaunchKernelEx(&cfg, attention_dq_tc_kernel<BOXES>, m, a) == cudaSuccess ? 2 : MUON_ERR_CUDA;
 }
 
 }  // namespace

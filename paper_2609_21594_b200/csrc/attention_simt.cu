@@ -113,32 +113,57 @@ __global__ void __launch_bounds__(THREADS) attention_forward_simt_kernel(const A
 }
 
 // -lse in units of log 2 and -delta, delta = sum_d do o, into the padded row blocks: P = exp2(scale' S + (-lse)) and dS = P (dP + (-delta)) are
-// then a multiply-add and an add.  One warp per row.
-template <typename T>
-__global__ void __launch_bounds__(256) attention_rows_kernel(const AttnArgs a) {
+// then a multiply-add and an add.  Memory bound: do and o are read once.  LANES threads share a row, one 16-byte piece each (N elements); a block
+// of 256 takes the 128 rows in PASSES, the loads of four of them in flight together.  Heads vary fastest over the blocks: a token's heads lie
+// together in memory, and a block alone touches 256 bytes of every 8 KiB.  Rows that 16-byte pieces do not fit take one warp each (N = 1).
+template <typename T, int N, int LANES>
+__global__ void __launch_bounds__(256, 4) attention_rows_kernel(const AttnArgs a) {
+  constexpr int AT_ONCE = 256 / LANES, PASSES = kAttnRowBlock / AT_ONCE;
+  cudaTriggerProgrammaticLaunchCompletion();            // the kernel after this one may set itself up; it waits for this one's end
   int si, blk;
-  if (!attn_find_block(a, blockIdx.x, kAttnRowBlock, false, &si, &blk)) return;
+  if (!attn_find_block(a, int(blockIdx.x / unsigned(a.hq)), kAttnRowBlock, false, &si, &blk)) return;
   const AttnSeq s = attn_seq(a, si);
-  const int head = blockIdx.y, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int64_t per = attn_row_blocks(a);
-  float* out = a.rows + ((int64_t(s.tb) * a.hq + head) * per + (a.nseq ? s.q0 / kAttnRowBlock + si : 0) + blk) * (2 * kAttnRowBlock);
-  for (int r = warp; r < kAttnRowBlock; r += 8) {
-    const int row = blk * kAttnRowBlock + r;
-    float l2 = -INFINITY, delta = 0.f;
-    if (row < s.qn) {
-      const float lse = a.lse[(int64_t(s.tb) * a.hq + head) * a.nq + s.q0 + row];
-      if (lse != -INFINITY) {
-        l2 = -lse * kLog2e;
-        const T* x = row_of<T>(a.dout, s.tb, s.q0 + row, head);
-        const T* y = row_of<T>(a.o, s.tb, s.q0 + row, head);
-        for (int d = lane; d < a.dim; d += 32) delta = fmaf(-to_f(x[d]), to_f(y[d]), delta);
+  const int head = int(blockIdx.x % unsigned(a.hq)), lane = threadIdx.x % LANES;
+  float* out = a.rows + ((int64_t(s.tb) * a.hq + head) * attn_row_blocks(a) + (a.nseq ? s.q0 / kAttnRowBlock + si : 0) + blk) * (2 * kAttnRowBlock);
+  struct alignas(sizeof(T) * N) Piece { T v[N]; };
+  constexpr int UNROLL = N > 1 ? 4 : 1;
+#pragma unroll 1
+  for (int p0 = 0; p0 < PASSES; p0 += UNROLL) {
+    float delta[UNROLL], l2[UNROLL];
+    Piece x[UNROLL], y[UNROLL];
 #pragma unroll
-        for (int d = 16; d; d >>= 1) delta += __shfl_xor_sync(0xffffffffu, delta, d);
+    for (int p = 0; p < UNROLL; ++p) {
+      const int row = blk * kAttnRowBlock + (p0 + p) * AT_ONCE + threadIdx.x / LANES;
+      delta[p] = 0.f;
+      l2[p] = -INFINITY;
+      if (row < s.qn) l2[p] = -a.lse[(int64_t(s.tb) * a.hq + head) * a.nq + s.q0 + row] * kLog2e;
+      if (l2[p] == INFINITY) l2[p] = -INFINITY;           // lse = -inf: the row sees nothing
+      if constexpr (N > 1) {
+        if (row < s.qn && lane * N < a.dim) {
+          x[p] = *reinterpret_cast<const Piece*>(row_of<T>(a.dout, s.tb, s.q0 + row, head) + lane * N);
+          y[p] = *reinterpret_cast<const Piece*>(row_of<T>(a.o, s.tb, s.q0 + row, head) + lane * N);
+        } else {
+#pragma unroll
+          for (int e = 0; e < N; ++e) x[p].v[e] = y[p].v[e] = from_f<T>(0.f);
+        }
+      } else if (row < s.qn) {
+        for (int d = lane; d < a.dim; d += LANES)
+          delta[p] = fmaf(-to_f(row_of<T>(a.dout, s.tb, s.q0 + row, head)[d]), to_f(row_of<T>(a.o, s.tb, s.q0 + row, head)[d]), delta[p]);
       }
     }
-    if (lane == 0) {
-      out[r] = l2;
-      out[kAttnRowBlock + r] = delta;
+#pragma unroll
+    for (int p = 0; p < UNROLL; ++p) {
+      const int r = (p0 + p) * AT_ONCE + threadIdx.x / LANES;
+      if constexpr (N > 1) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) delta[p] = fmaf(-to_f(x[p].v[e]), to_f(y[p].v[e]), delta[p]);
+      }
+#pragma unroll
+      for (int d = LANES / 2; d; d >>= 1) delta[p] += __shfl_xor_sync(0xffffffffu, delta[p], d);
+      if (lane == 0) {
+        out[r] = l2[p];
+        out[kAttnRowBlock + r] = l2[p] == -INFINITY ? 0.f : delta[p];     // whatever a row that counts for nothing holds
+      }
     }
   }
 }
@@ -298,12 +323,17 @@ int backward(const AttnArgs& a, cudaStream_t st) {
 }  // namespace
 
 int launch_attention_rows(const AttnArgs& a, int dtype, cudaStream_t st) {
-  const int64_t blocks = attn_max_blocks(a, kAttnRowBlock, false);
+  const int64_t blocks = attn_max_blocks(a, kAttnRowBlock, false) * a.hq;
   if (blocks == 0) return 0;
-  if (blocks > 0x7fffffff || a.hq > 65535) return MUON_ERR_UNSUPPORTED;
-  const dim3 grid{unsigned(blocks), unsigned(a.hq)};
-  if (dtype == MUON_DTYPE_BF16) attention_rows_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(a);
-  else attention_rows_kernel<float><<<grid, 256, 0, st>>>(a);
+  if (blocks > 0x7fffffff) return MUON_ERR_UNSUPPORTED;
+  const unsigned grid = unsigned(blocks);
+  auto pieces = [&](const AttnTensor& t, int64_t e) {
+    return reinterpret_cast<uintptr_t>(t.data) % 16 == 0 && t.sb * e % 16 == 0 && t.st * e % 16 == 0 && t.sh * e % 16 == 0;
+  };
+  if (dtype == MUON_DTYPE_FP32) attention_rows_kernel<float, 1, 32><<<grid, 256, 0, st>>>(a);
+  else if (a.dim % 8 || a.dim > 128 || !pieces(a.dout, 2) || !pieces(a.o, 2)) attention_rows_kernel<__nv_bfloat16, 1, 32><<<grid, 256, 0, st>>>(a);
+  else if (a.dim <= 64) attention_rows_kernel<__nv_bfloat16, 8, 8><<<grid, 256, 0, st>>>(a);
+  else attention_rows_kernel<__nv_bfloat16, 8, 16><<<grid, 256, 0, st>>>(a);
   return cudaGetLastError() == cudaSuccess ? 1 : MUON_ERR_CUDA;
 }
 
