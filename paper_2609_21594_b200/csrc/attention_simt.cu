@@ -117,55 +117,64 @@ __global__ void __launch_bounds__(THREADS) attention_forward_simt_kernel(const A
 // of 256 takes the 128 rows in PASSES, the loads of four of them in flight together.  Heads vary fastest over the blocks: a token's heads lie
 // together in memory, and a block alone touches 256 bytes of every 8 KiB.  Rows that 16-byte pieces do not fit take one warp each (N = 1).
 template <typename T, int N, int LANES>
-__global__ void __launch_bounds__(256, 4) attention_rows_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(256, 4) attention_rows_kernel(const __grid_constant__ AttnArgs a) {
   constexpr int AT_ONCE = 256 / LANES, PASSES = kAttnRowBlock / AT_ONCE;
+  __shared__ float sums[kAttnRowBlock];
   cudaTriggerProgrammaticLaunchCompletion();            // the kernel after this one may set itself up; it waits for this one's end
   int si, blk;
   if (!attn_find_block(a, int(blockIdx.x / unsigned(a.hq)), kAttnRowBlock, false, &si, &blk)) return;
   const AttnSeq s = attn_seq(a, si);
-  const int head = int(blockIdx.x % unsigned(a.hq)), lane = threadIdx.x % LANES;
-  float* out = a.rows + ((int64_t(s.tb) * a.hq + head) * attn_row_blocks(a) + (a.nseq ? s.q0 / kAttnRowBlock + si : 0) + blk) * (2 * kAttnRowBlock);
-  struct alignas(sizeof(T) * N) Piece { T v[N]; };
-  constexpr int UNROLL = N > 1 ? 4 : 1;
+  const int head = int(blockIdx.x % unsigned(a.hq)), lane = threadIdx.x % LANES, first = threadIdx.x / LANES;
+  const int rows = s.qn - blk * kAttnRowBlock;          // that count
+  const T* px = row_of<T>(a.dout, s.tb, s.q0 + blk * kAttnRowBlock + first, head) + lane * N;
+  const T* py = row_of<T>(a.o, s.tb, s.q0 + blk * kAttnRowBlock + first, head) + lane * N;
+  float lse = -INFINITY;
+  if (int(threadIdx.x) < min(rows, kAttnRowBlock)) lse = a.lse[(int64_t(s.tb) * a.hq + head) * a.nq + s.q0 + blk * kAttnRowBlock + threadIdx.x];
+  if constexpr (N > 1) {
+    struct alignas(sizeof(T) * N) Piece { T v[N]; };
+    const bool in = lane * N < a.dim;
+    const int64_t sx = AT_ONCE * a.dout.st, sy = AT_ONCE * a.o.st;
 #pragma unroll 1
-  for (int p0 = 0; p0 < PASSES; p0 += UNROLL) {
-    float delta[UNROLL], l2[UNROLL];
-    Piece x[UNROLL], y[UNROLL];
+    for (int p0 = 0; p0 < PASSES; p0 += 4) {
+      Piece x[4], y[4];
 #pragma unroll
-    for (int p = 0; p < UNROLL; ++p) {
-      const int row = blk * kAttnRowBlock + (p0 + p) * AT_ONCE + threadIdx.x / LANES;
-      delta[p] = 0.f;
-      l2[p] = -INFINITY;
-      if (row < s.qn) l2[p] = -a.lse[(int64_t(s.tb) * a.hq + head) * a.nq + s.q0 + row] * kLog2e;
-      if (l2[p] == INFINITY) l2[p] = -INFINITY;           // lse = -inf: the row sees nothing
-      if constexpr (N > 1) {
-        if (row < s.qn && lane * N < a.dim) {
-          x[p] = *reinterpret_cast<const Piece*>(row_of<T>(a.dout, s.tb, s.q0 + row, head) + lane * N);
-          y[p] = *reinterpret_cast<const Piece*>(row_of<T>(a.o, s.tb, s.q0 + row, head) + lane * N);
+      for (int p = 0; p < 4; ++p) {
+        if (in && first + (p0 + p) * AT_ONCE < rows) {
+          x[p] = *reinterpret_cast<const Piece*>(px + p * sx);
+          y[p] = *reinterpret_cast<const Piece*>(py + p * sy);
         } else {
 #pragma unroll
           for (int e = 0; e < N; ++e) x[p].v[e] = y[p].v[e] = from_f<T>(0.f);
         }
-      } else if (row < s.qn) {
-        for (int d = lane; d < a.dim; d += LANES)
-          delta[p] = fmaf(-to_f(row_of<T>(a.dout, s.tb, s.q0 + row, head)[d]), to_f(row_of<T>(a.o, s.tb, s.q0 + row, head)[d]), delta[p]);
+      }
+      px += 4 * sx;
+      py += 4 * sy;
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        float d = 0.f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) d = fmaf(-to_f(x[p].v[e]), to_f(y[p].v[e]), d);
+#pragma unroll
+        for (int k = LANES / 2; k; k >>= 1) d += __shfl_xor_sync(0xffffffffu, d, k);
+        if (lane == 0) sums[first + (p0 + p) * AT_ONCE] = d;
       }
     }
+  } else {
+    for (int p = 0; p < PASSES; ++p) {
+      float d = 0.f;
+      if (first + p * AT_ONCE < rows)
+        for (int i = 0; i + lane < a.dim; i += LANES) d = fmaf(-to_f(px[p * AT_ONCE * a.dout.st + i]), to_f(py[p * AT_ONCE * a.o.st + i]), d);
 #pragma unroll
-    for (int p = 0; p < UNROLL; ++p) {
-      const int r = (p0 + p) * AT_ONCE + threadIdx.x / LANES;
-      if constexpr (N > 1) {
-#pragma unroll
-        for (int e = 0; e < N; ++e) delta[p] = fmaf(-to_f(x[p].v[e]), to_f(y[p].v[e]), delta[p]);
-      }
-#pragma unroll
-      for (int d = LANES / 2; d; d >>= 1) delta[p] += __shfl_xor_sync(0xffffffffu, delta[p], d);
-      if (lane == 0) {
-        out[r] = l2[p];
-        out[kAttnRowBlock + r] = l2[p] == -INFINITY ? 0.f : delta[p];     // whatever a row that counts for nothing holds
-      }
+      for (int k = LANES / 2; k; k >>= 1) d += __shfl_xor_sync(0xffffffffu, d, k);
+      if (lane == 0) sums[first + p * AT_ONCE] = d;
     }
   }
+  __syncthreads();
+  if (threadIdx.x >= kAttnRowBlock) return;
+  float* out = a.rows + ((int64_t(s.tb) * a.hq + head) * attn_row_blocks(a) + (a.nseq ? s.q0 / kAttnRowBlock + si : 0) + blk) * (2 * kAttnRowBlock);
+  const bool seen = lse != -INFINITY;
+  out[threadIdx.x] = seen ? -lse * kLog2e : -INFINITY;
+  out[kAttnRowBlock + threadIdx.x] = seen ? sums[threadIdx.x] : 0.f;          // whatever a row that counts for nothing holds
 }
 
 template <typename T, int NACC>
