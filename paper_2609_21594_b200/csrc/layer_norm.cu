@@ -136,8 +136,10 @@ __global__ void __launch_bounds__(FWD_THREADS, BLOCKS) norm_forward_kernel(const
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   for (int c = threadIdx.x; SHARED_PARAMS && c < a.cols; c += FWD_THREADS) {
-    param[c] = param_at(a.weight, a.param_dtype, 1.f, c);
-    param[pitch + c] = param_at(a.bias, a.param_dtype, 0.f, c);
+    // groups of four columns, the first groups of all pieces before the second ones: neighbouring threads read neighbouring 16 bytes
+    const int at = N > 4 ? (c % N / 4 * (a.cols / N) + c / N) * 4 + c % 4 : c;
+    param[at] = param_at(a.weight, a.param_dtype, 1.f, c);
+    param[pitch + at] = param_at(a.bias, a.param_dtype, 0.f, c);
   }
   __syncthreads();
   const T* x = static_cast<const T*>(a.x);
@@ -215,7 +217,7 @@ __global__ void __launch_bounds__(FWD_THREADS, BLOCKS) norm_forward_kernel(const
     } else {
 #pragma unroll
       for (int i = 0; i < EPT / 4; ++i) {
-        const int c = min((4 * i / N * TPR + t) * N + 4 * i % N, pitch - 4);
+        const int piece = min(4 * i / N * TPR + t, a.cols / N - 1), c = (4 * i % N) * (a.cols / N) + piece * 4;
         const float4 w = *reinterpret_cast<const float4*>(param + c), b = *reinterpret_cast<const float4*>(param + pitch + c);
         scaled(2 * i, w.x, w.y, b.x, b.y);
         scaled(2 * i + 1, w.z, w.w, b.z, b.w);
