@@ -99,7 +99,9 @@ __device__ __forceinline__ void await_copy(uint32_t bar, uint32_t phase, int32_t
 }
 
 // ------------------------------------------------------------------ forward
-constexpr int FWD_THREADS = 512, FWD_STAGES = 2;
+constexpr int FWD_THREADS = 512;
+// Rows asked for ahead, per row group.  fp32 rows of more than 8192 columns are 64 KiB, beside 128 KiB of weight and bias: one.
+template <int N, int EPT> constexpr int kFwdStages = N == 4 && EPT == 32 ? 1 : 2;
 
 // Sum over the TPR threads of a row, the same in all of them.  The warps of a row meet at a named barrier of their own; `buf` has two
 // halves that alternate, so one meeting per sum is enough.
@@ -120,22 +122,22 @@ __device__ __forceinline__ float group_sum(float v, float* buf, int& half) {
   return s;
 }
 
-template <typename T, int N, int TPR, int EPT, int BLOCKS, bool SHARED_PARAMS>
+template <typename T, int N, int TPR, int EPT, int BLOCKS>
 __global__ void __launch_bounds__(FWD_THREADS, BLOCKS) norm_forward_kernel(const NormArgs a) {
   using RW = Rows<T, N, TPR, EPT>;
-  extern __shared__ __align__(16) float param[];      // weight, then bias (unless they stay in global memory); then the ring
+  extern __shared__ __align__(16) float param[];      // weight, then bias; then the ring
   __shared__ float buf[2 * FWD_THREADS / 32];
-  constexpr int G = FWD_THREADS / TPR;
-  __shared__ __align__(8) uint64_t bars[G * FWD_STAGES];
-  const int t = threadIdx.x % TPR, pitch = SHARED_PARAMS ? (a.cols + 3) & ~3 : 0;
+  constexpr int G = FWD_THREADS / TPR, STAGES = kFwdStages<N, EPT>;
+  __shared__ __align__(8) uint64_t bars[G * STAGES];
+  const int t = threadIdx.x % TPR, pitch = (a.cols + 3) & ~3;
   const int group = threadIdx.x / TPR;
-  const uint32_t ring = uint32_t(__cvta_generic_to_shared(param + 2 * pitch)) + uint32_t(group * FWD_STAGES * RW::kRowBytes);
-  const uint32_t bar = uint32_t(__cvta_generic_to_shared(bars + group * FWD_STAGES));
+  const uint32_t ring = uint32_t(__cvta_generic_to_shared(param + 2 * pitch)) + uint32_t(group * STAGES * RW::kRowBytes);
+  const uint32_t bar = uint32_t(__cvta_generic_to_shared(bars + group * STAGES));
   if (threadIdx.x == 0) {
-    for (int i = 0; i < G * FWD_STAGES; ++i) tc::mbar_init(uint32_t(__cvta_generic_to_shared(bars + i)), 1);
+    for (int i = 0; i < G * STAGES; ++i) tc::mbar_init(uint32_t(__cvta_generic_to_shared(bars + i)), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  for (int c = threadIdx.x; SHARED_PARAMS && c < a.cols; c += FWD_THREADS) {
+  for (int c = threadIdx.x; c < a.cols; c += FWD_THREADS) {
     // groups of four columns, the first groups of all pieces before the second ones: neighbouring threads read neighbouring 16 bytes
     const int at = N > 4 ? (c % N / 4 * (a.cols / N) + c / N) * 4 + c % 4 : c;
     param[at] = param_at(a.weight, a.param_dtype, 1.f, c);
@@ -155,7 +157,7 @@ __global__ void __launch_bounds__(FWD_THREADS, BLOCKS) norm_forward_kernel(const
       }
   };
 #pragma unroll
-  for (int k = 0; k < FWD_STAGES; ++k) fetch(k, r0 + k * step);
+  for (int k = 0; k < STAGES; ++k) fetch(k, r0 + k * step);
   const float inv = 1.f / float(a.cols);
   int half = 0;
   uint32_t stage = 0, phase = 0;
@@ -197,8 +199,8 @@ __global__ void __launch_bounds__(FWD_THREADS, BLOCKS) norm_forward_kernel(const
     const float2 qq = both(add2(q[0], q[1]));
     const float rstd = 1.f / sqrtf(group_sum<TPR>(qq.x + qq.y, buf, half) * inv + a.eps);
     if constexpr (TPR == 32) __syncwarp();
-    fetch(stage, r + FWD_STAGES * step);              // everybody has read the row: the sum above was a meeting
-    if (++stage == FWD_STAGES) {
+    fetch(stage, r + STAGES * step);              // everybody has read the row: the sum above was a meeting
+    if (++stage == STAGES) {
       stage = 0;
       phase ^= 1;
     }
@@ -206,13 +208,12 @@ __global__ void __launch_bounds__(FWD_THREADS, BLOCKS) norm_forward_kernel(const
       pair_down<T, N>(p, i, fma2(mul2(v[i], twice(rstd)), two(w0, w1), two(b0, b1)));
     };
     T* out = y + r * a.ldo;
-    if constexpr (!SHARED_PARAMS || N == 1) {
+    if constexpr (N == 1) {
 #pragma unroll
       for (int i = 0; i < EPT / 2; ++i) {
         const int c = (2 * i / N * TPR + t) * N + 2 * i % N, d = ((2 * i + 1) / N * TPR + t) * N + (2 * i + 1) % N;
-        auto weight = [&](int k) { return k >= a.cols ? 0.f : SHARED_PARAMS ? param[k] : param_at(a.weight, a.param_dtype, 1.f, k); };
-        auto bias = [&](int k) { return k >= a.cols ? 0.f : SHARED_PARAMS ? param[pitch + k] : param_at(a.bias, a.param_dtype, 0.f, k); };
-        scaled(i, weight(c), weight(d), bias(c), bias(d));
+        const bool ci = c < a.cols, di = d < a.cols;
+        scaled(i, ci ? param[c] : 0.f, di ? param[d] : 0.f, ci ? param[pitch + c] : 0.f, di ? param[pitch + d] : 0.f);
       }
     } else {
 #pragma unroll
@@ -469,13 +470,11 @@ int blocks_for(int64_t rows, int rows_per_block, int most) {
 
 template <typename T, int N, int TPR, int EPT>
 int forward(const NormArgs& a, int sms, cudaStream_t st) {
-  // fp32 rows of more than 8192 columns: 128 KiB of ring, and as much again of weight and bias would not fit
-  constexpr bool SHARED_PARAMS = !(N == 4 && EPT == 32);
-  constexpr int BLOCKS = !SHARED_PARAMS ? 1 : EPT > 8 ? 2 : 3;
-  const int bytes = (SHARED_PARAMS ? 2 * ((a.cols + 3) & ~3) * int(sizeof(float)) : 0) + FWD_STAGES * (FWD_THREADS / TPR) * Rows<T, N, TPR, EPT>::kRowBytes;
+  constexpr int BLOCKS = kFwdStages<N, EPT> == 1 ? 1 : EPT > 8 ? 2 : 3;
+  const int bytes = 2 * ((a.cols + 3) & ~3) * int(sizeof(float)) + kFwdStages<N, EPT> * (FWD_THREADS / TPR) * Rows<T, N, TPR, EPT>::kRowBytes;
   // weight and bias of wide rows leave room for one block per SM only
   const int blocks = blocks_for(a.rows, FWD_THREADS / TPR, sms * (bytes * BLOCKS <= 216 * 1024 ? BLOCKS : bytes * 2 <= 216 * 1024 ? 2 : 1));
-  auto kernel = norm_forward_kernel<T, N, TPR, EPT, BLOCKS, SHARED_PARAMS>;
+  auto kernel = norm_forward_kernel<T, N, TPR, EPT, BLOCKS>;
   static SharedMemoryLimit limit;
   if (bytes > 40 * 1024 && !limit.raise(a.device, 220 * 1024, kernel)) return MUON_ERR_CUDA;
   kernel<<<blocks, FWD_THREADS, bytes, st>>>(a);
@@ -530,7 +529,8 @@ int forward_by_cols(const NormArgs& a, int sms, cudaStream_t st) {
   if (a.cols <= 64 * most) return forward<T, N, 64, most>(a, sms, st);
   if (a.cols <= 128 * most) return forward<T, N, 128, most>(a, sms, st);
   if (a.cols <= 256 * most) return forward<T, N, 256, most>(a, sms, st);
-  return forward<T, N, 512, most == 16 ? 32 : most>(a, sms, st);
+  if (a.cols <= 512 * most) return forward<T, N, 512, most>(a, sms, st);
+  return forward<T, N, 512, 32>(a, sms, st);
 }
 
 template <typename T, int N>
