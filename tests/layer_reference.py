@@ -100,3 +100,9 @@ def attention(q, k, v, causal=True, window=0, scale=None, do=None, o=None, lse=N
                 r["dq" + name][qb, qs, h] = t @ a(ki) * scale
                 r["dk" + name][kb, ks, g] += t.T @ a(torch.where(live[:, None], qi, 0.0)) * scale
     return r
+
+
+def norm_of(x, w, b, eps):
+    """Differentiable layer norm in the precision of x."""
+    c = x - x.mean(-1, keepdim=True)
+    return c / torch.sqrt((c * c).mean(-1, keepdim=True) + eps) * w + b
