@@ -175,7 +175,7 @@ int muon_layer_norm_backward(muon_ctx_t* ctx, const muon_norm_desc_t* desc, cons
   a.ldo = lddx;
   a.dweight = dweight;
   a.dbias = dbias;
-  a.parts = sums ? static_cast<float*>(workspace) : nullptr;
+  a.parts = sums && need > 0 ? static_cast<float*>(workspace) : nullptr;
   return launched(ctx, launch_norm_backward(a, sms, static_cast<cudaStream_t>(stream)));
 }
 

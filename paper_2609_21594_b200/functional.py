@@ -25,7 +25,9 @@ _raw_stream = torch._C._cuda_getCurrentRawStream         # the current stream's 
 _NORM, _ROTARY, _ATTENTION = struct.Struct("4iqfi"), struct.Struct("7ifQQq"), struct.Struct("9if2i4Q")
 _HEADS = {n: struct.Struct(f"{'Q3q' * n}") for n in (4, 8)}
 _ITEM = struct.Struct("Q3qQ3q2i")
-_DESC_BYTES, _HEADS_BYTES = 128, 32
+_DESC_BYTES, _HEADS_BYTES, _MAX_PAIRS = 128, 32, 256
+_norm_forward, _norm_backward, _rotary_call = mb.lib.muon_layer_norm_forward, mb.lib.muon_layer_norm_backward, mb.lib.muon_rotary
+_attention_forward, _attention_backward = mb.lib.muon_attention_forward, mb.lib.muon_attention_backward
 _local = threading.local()
 
 
@@ -35,9 +37,12 @@ class _Lane:
     def __init__(self, index: int):
         with torch.cuda.device(index):
             self.ctx = mb.Context()
+        self.handle = self.ctx.handle
         self.memory = C.create_string_buffer(_DESC_BYTES + 10 * _HEADS_BYTES)
         self.desc = C.addressof(self.memory)
         self.heads = [self.desc + _DESC_BYTES + i * _HEADS_BYTES for i in range(10)]
+        self.freq = np.empty(_MAX_PAIRS, dtype=np.float64)
+        self.freq_at = self.freq.ctypes.data
 
 
 def _lane(index: int) -> _Lane:
@@ -73,8 +78,8 @@ def _on(t: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
     return index
 
 
-def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
-    return None if t is None else t.data_ptr()
+def _refused(code: int, where: str) -> None:
+    raise mb.MuonError(code, where)
 
 
 def _address(t: Optional[torch.Tensor]) -> int:
@@ -122,8 +127,10 @@ def layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, b
     stat = x.shape[:-1]
     mean = x.new_empty(stat, dtype=torch.float32) if center else None
     rstd = x.new_empty(stat, dtype=torch.float32)
-    lane.ctx.muon_layer_norm_forward(lane.desc, r.data_ptr(), _ld(r), _ptr(weight), _ptr(bias), y.data_ptr(), cols, _ptr(mean), rstd.data_ptr(),
-                                     _raw_stream(index))
+    rc = _norm_forward(lane.handle, lane.desc, r.data_ptr(), _ld(r), _address(weight), _address(bias), y.data_ptr(), cols, _address(mean),
+                       rstd.data_ptr(), _raw_stream(index))
+    if rc:
+        _refused(rc, "muon_layer_norm_forward")
     return y, mean, rstd
 
 
@@ -156,8 +163,10 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
     db = None if not bias else torch.empty_like(weight) if weight is not None else x.new_empty(cols, dtype=pt)
     n = mb.muon_layer_norm_workspace_bytes(lane.desc) if dw is not None or db is not None else 0
     ws = x.new_empty(n, dtype=torch.uint8) if n else None
-    lane.ctx.muon_layer_norm_backward(lane.desc, g.data_ptr(), _ld(g), r.data_ptr(), _ld(r), _ptr(weight), _ptr(mean), rstd.data_ptr(),
-                                      dx.data_ptr(), cols, _ptr(dw), _ptr(db), _ptr(ws), n, _raw_stream(index))
+    rc = _norm_backward(lane.handle, lane.desc, g.data_ptr(), _ld(g), r.data_ptr(), _ld(r), _address(weight), _address(mean), rstd.data_ptr(),
+                        dx.data_ptr(), cols, _address(dw), _address(db), _address(ws), n, _raw_stream(index))
+    if rc:
+        _refused(rc, "muon_layer_norm_backward")
     return dx, dw, db
 
 
@@ -213,7 +222,8 @@ def rotary_forward(tensors: Sequence[torch.Tensor], inv_freq, layout: str = "hal
     turned, the rest is copied.  layout: "half" (i with i + n/2) or "interleaved" (2i with 2i + 1).  positions: int32 [batch, tokens] on
     the device, else offset + 0, 1, 2...; offset is added to given positions too.  inverse turns back, which is the backward pass.
     out: tensors to write, which may be the inputs themselves."""
-    if not 1 <= len(tensors) <= 4:
+    count = len(tensors)
+    if not 1 <= count <= 4:
         raise ValueError("one to four tensors")
     if layout != "half" and layout != "interleaved":
         raise ValueError("layout is 'half' or 'interleaved'")
@@ -222,36 +232,45 @@ def rotary_forward(tensors: Sequence[torch.Tensor], inv_freq, layout: str = "hal
     if index != _current_device():
         with torch.cuda.device(index):
             return rotary_forward(tensors, inv_freq, layout, amplitude, positions, offset, inverse, out)
-    freq = np.ascontiguousarray(inv_freq, dtype=np.float64)
-    xs = [_heads4(t, "a tensor") for t in tensors]
-    b, n, _, d = xs[0].shape
-    for t in xs[1:]:
-        s = t.shape
-        if s[0] != b or s[1] != n or s[3] != d or t.dtype != first.dtype:
+    lane = _lane(index)
+    dtype = first.dtype
+    b, n, d = None, None, None
+    at = _DESC_BYTES
+    keep, res = [], []
+    if out is not None and (len(out) != count or any(o.shape != t.shape or o.dtype != t.dtype or o.device != t.device for o, t in zip(out, tensors))):
+        raise ValueError("out must match the tensors")
+    for i, t in enumerate(tensors):
+        x = _heads4(t, "a tensor")
+        xb, xn, xh, xd = x.shape
+        if b is None:
+            b, n, d = xb, xn, xd
+        elif xb != b or xn != n or xd != d or t.dtype != dtype:
             raise ValueError("the tensors must agree in batch, tokens, head size and dtype")
-    if freq.ndim != 1 or not 1 <= freq.size <= d // 2:
-        raise ValueError(f"inv_freq must hold one to {d // 2} frequencies for heads of {d}")
+        if out is None:
+            o = torch.empty_like(t, memory_format=torch.contiguous_format)
+        else:
+            o = out[i]
+            if o.stride(-1) != 1 and xd > 1:
+                raise ValueError("out must have a contiguous last dimension")
+        s, u = x.stride(), o.stride()
+        _ITEM.pack_into(lane.memory, at, x.data_ptr(), s[0], s[1], s[2], o.data_ptr(), u[0] if len(u) == 4 else 0, u[-3], u[-2], xh, 0)
+        at += _ITEM.size
+        keep.append(x)
+        res.append(o)
+    freq = np.asarray(inv_freq, dtype=np.float64)
+    pairs = freq.size
+    if freq.ndim != 1 or not 1 <= pairs <= d // 2 or pairs > _MAX_PAIRS:
+        raise ValueError(f"inv_freq must hold one to {min(d // 2, _MAX_PAIRS)} frequencies for heads of {d}")
+    lane.freq[:pairs] = freq
     if positions is not None:
         if positions.dtype != torch.int32 or positions.numel() != b * n:
             raise ValueError("positions must be int32, one for each token")
         positions = positions.contiguous()
-    if out is None:
-        res = [_like(t) for t in tensors]
-    else:
-        res = list(out)
-        if len(res) != len(tensors) or any(o.shape != t.shape or o.dtype != t.dtype or o.device != t.device for o, t in zip(res, tensors)):
-            raise ValueError("out must match the tensors")
-        if any(o.stride(-1) != 1 and o.shape[-1] > 1 for o in res):
-            raise ValueError("out must have a contiguous last dimension")
-    lane = _lane(index)
-    _ROTARY.pack_into(lane.memory, 0, _dtype(first, "the tensors"), 1 if layout == "interleaved" else 0, 1 if inverse else 0, d, 2 * freq.size, b, n,
-                      amplitude, freq.ctypes.data, _address(positions), offset)
-    at = _DESC_BYTES
-    for x, o in zip(xs, res):
-        s, t = x.stride(), o.stride()
-        _ITEM.pack_into(lane.memory, at, x.data_ptr(), s[0], s[1], s[2], o.data_ptr(), t[0] if len(t) == 4 else 0, t[-3], t[-2], x.shape[2], 0)
-        at += _ITEM.size
-    lane.ctx.muon_rotary(lane.desc, lane.desc + _DESC_BYTES, len(xs), _raw_stream(index))
+    _ROTARY.pack_into(lane.memory, 0, _dtype(first, "the tensors"), 1 if layout == "interleaved" else 0, 1 if inverse else 0, d, 2 * pairs, b, n,
+                      amplitude, lane.freq_at, _address(positions), offset)
+    rc = _rotary_call(lane.handle, lane.desc, lane.desc + _DESC_BYTES, count, _raw_stream(index))
+    if rc:
+        _refused(rc, "muon_rotary")
     return tuple(res)
 
 
@@ -330,7 +349,9 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal:
     a, b, c, d, h = q4.stride(), k4.stride(), v4.stride(), o.stride(), lane.heads
     _HEADS[4].pack_into(lane.memory, _DESC_BYTES, q4.data_ptr(), a[0], a[1], a[2], k4.data_ptr(), b[0], b[1], b[2], v4.data_ptr(), c[0], c[1], c[2],
                         o.data_ptr(), d[0], d[1], d[2])
-    lane.ctx.muon_attention_forward(lane.desc, h[0], h[1], h[2], h[3], lse.data_ptr(), _raw_stream(index))
+    rc = _attention_forward(lane.handle, lane.desc, h[0], h[1], h[2], h[3], lse.data_ptr(), _raw_stream(index))
+    if rc:
+        _refused(rc, "muon_attention_forward")
     return o if len(stat) == 3 else o[0], lse
 
 
@@ -360,7 +381,10 @@ def attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: to
         values += (t.data_ptr(), s[0], s[1], s[2])
     _HEADS[8].pack_into(lane.memory, _DESC_BYTES, *values)
     h = lane.heads
-    lane.ctx.muon_attention_backward(lane.desc, h[0], h[1], h[2], h[3], h[4], lse.data_ptr(), h[5], h[6], h[7], _ptr(ws), n, _raw_stream(index))
+    rc = _attention_backward(lane.handle, lane.desc, h[0], h[1], h[2], h[3], h[4], lse.data_ptr(), h[5], h[6], h[7], _address(ws), n,
+                             _raw_stream(index))
+    if rc:
+        _refused(rc, "muon_attention_backward")
     return (dq, dk, dv) if len(stat) == 3 else (dq[0], dk[0], dv[0])
 
 

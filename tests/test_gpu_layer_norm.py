@@ -83,7 +83,7 @@ def test_every_width(cols, dtype, param, center):
     check_backward(dy, x, w, mean, rstd)
 
 
-@pytest.mark.parametrize("rows", [1, 2, 7, 8, 9, 147, 149, 600, 5000])
+@pytest.mark.parametrize("rows", [1, 2, 7, 8, 9, 64, 127, 128, 129, 147, 149, 600, 5000])
 @pytest.mark.parametrize("cols", [48, 256, 640, 4096, 9000])
 def test_row_counts(rows, cols):
     x, w, b, dy = make(rows, cols, torch.bfloat16, torch.float32)
@@ -251,6 +251,7 @@ def test_refusals():
             call()
         assert e.value.code == mb.ERR_INVALID_ARG
     with pytest.raises(mb.MuonError) as e:
-        c.muon_layer_norm_backward(desc, p, 64, p, 64, None, mean.data_ptr(), rstd.data_ptr(), y.data_ptr(), 64, w.data_ptr(), None, None, 0)
+        many = mb.NormDesc(mb.DTYPE_FP32, mb.DTYPE_FP32, 1, 64, 1000, 1e-5, 0)      # enough rows to need scratch
+        c.muon_layer_norm_backward(many, p, 64, p, 64, None, mean.data_ptr(), rstd.data_ptr(), y.data_ptr(), 64, w.data_ptr(), None, None, 0)
     assert e.value.code == mb.ERR_WORKSPACE_TOO_SMALL
     assert c.muon_launch_count() == before
