@@ -1,13 +1,16 @@
-"""Builds libmuon_b200.so in-tree with nvcc for sm_100a (no JIT cache, no pip install)."""
+"""Builds, in-tree (no JIT cache, no pip install), libmuon_b200.so with nvcc for sm_100a and _front.so, the torch front end of the layer operators."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmuon_b200.so")
+FRONT = os.path.join(HERE, "_front.so")
 SOURCES = ["api.cu", "plan.cu", "layout_kernels.cu", "elementwise_kernels.cu", "ns_simt.cu", "ns_tcgen05.cu", "ns_tcgen05_pair.cu", "ns_tables.cu",
            "layer_api.cu", "layer_norm.cu", "rotary.cu", "attention_simt.cu", "attention_fwd.cu", "attention_bwd.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -22,15 +25,26 @@ def _nvcc() -> str:
 
 
 def needs_build() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(FRONT):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(FRONT))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(HERE, "..", "include", "muon_b200.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _front_command() -> list:
+    """The host compiler's command for csrc/front.cpp, linked with torch and with the library next to it."""
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    cuda = os.path.dirname(os.path.dirname(_nvcc())) or "/usr/local/cuda"
+    include = [os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"],
+               os.path.join(cuda, "include")]
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-DTORCH_EXTENSION_NAME=_front", *[f"-I{d}" for d in include],
+            os.path.join(CSRC, "front.cpp"), "-o", FRONT, "-L" + os.path.join(torch, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch", "-ltorch_python",
+            "-L" + HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN"]
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compiles every .cu under csrc/ into one shared library next to this file; returns its path."""
+    """Compiles every .cu under csrc/ into one shared library next to this file, and the front end beside it; returns the library's path."""
     if not force and not needs_build():
         return LIB
     objs = []
@@ -53,6 +67,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if failed:
         raise RuntimeError("nvcc failed")
     subprocess.check_call([_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", LIB, *objs, "-lcudart_static", "-ldl", "-lpthread", "-lrt"])
+    subprocess.check_call(_front_command())
     return LIB
 
 
