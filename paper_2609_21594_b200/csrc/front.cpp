@@ -2,7 +2,7 @@
 // no arithmetic.  It stands in C++ because a small call's time is the host's: the same checks in Python cost 14 to 18 us per call, of which
 // the device needed 5.
 //
-// Every host thread has a context of its own per device (autograd calls backward passes from another thread); it ends with the thread.
+// Every host thread has a context of its own per device (autograd calls backward passes from another thread).
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <pybind11/numpy.h>
@@ -10,9 +10,11 @@
 
 #include <algorithm>
 #include <cmath>
+#include <mutex>
 #include <optional>
 #include <string>
 #include <tuple>
+#include <utility>
 #include <vector>
 
 #include "../../include/muon_b200.h"
@@ -23,11 +25,33 @@ using MaybeTensor = std::optional<Tensor>;
 
 namespace {
 
+// A thread that ends leaves its contexts to the next one.  Nothing here is ever destroyed: threads (autograd's among them) end while the
+// process exits too, when CUDA may be gone already and a call into it would crash.
 struct Contexts {
+  struct Pool {
+    std::mutex lock;
+    std::vector<std::pair<int, muon_ctx_t*>> free;
+  };
+  static Pool& pool() {
+    static Pool* p = new Pool;
+    return *p;
+  }
   std::vector<muon_ctx_t*> of;
+  muon_ctx_t* take(int index) {
+    std::lock_guard<std::mutex> hold(pool().lock);
+    for (auto& f : pool().free)
+      if (f.first == index) {
+        muon_ctx_t* c = f.second;
+        f = pool().free.back();
+        pool().free.pop_back();
+        return c;
+      }
+    return nullptr;
+  }
   ~Contexts() {
-    for (muon_ctx_t* c : of)
-      if (c) muon_destroy(c);
+    std::lock_guard<std::mutex> hold(pool().lock);
+    for (size_t i = 0; i < of.size(); ++i)
+      if (of[i]) pool().free.push_back({int(i), of[i]});
   }
 };
 
@@ -44,6 +68,7 @@ muon_ctx_t* context(int index) {
   thread_local Contexts mine;
   if (index >= int(mine.of.size())) mine.of.resize(size_t(index) + 1, nullptr);
   muon_ctx_t*& c = mine.of[size_t(index)];
+  if (!c) c = mine.take(index);
   if (!c) {
     muon_options_t opt;
     muon_default_options(&opt);

@@ -26,7 +26,7 @@ _front.set_refused(_refused)
 
 
 class _ThreadContext(mb.Context):
-    """A context that belongs to its thread and ends with it."""
+    """A context that belongs to its thread: closing this object leaves it."""
 
     def __init__(self, address: int):
         self.opt, self.handle, self._ws = mb.muon_default_options(), C.c_void_p(address), None

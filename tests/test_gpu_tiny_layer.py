@@ -3,6 +3,8 @@ layer written out in 64 bits."""
 import importlib.util
 import math
 import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -10,6 +12,7 @@ import torch
 import layer_reference as ref
 
 pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 def example():
@@ -56,3 +59,29 @@ def test_gradients_against_the_layer_in_64_bits():
     for n, w in model.named_parameters():
         off = float((w.grad.double() - p[n].grad).norm() / p[n].grad.norm())
         assert off <= 2.0 ** -4, (n, off)
+
+
+_EXIT = """
+import threading, torch
+from paper_2609_21594_b200 import functional as F
+x = torch.randn(1, 32, 4, 64, device="cuda", dtype=torch.bfloat16, requires_grad=True)
+F.attention(x, x, x).sum().backward()
+seen = []
+def other():
+    F.layer_norm_forward(torch.ones(4, 8, device="cuda"))
+    seen.append(F.context().handle.value)
+for _ in range(3):
+    t = threading.Thread(target=other)
+    t.start()
+    t.join()
+torch.cuda.synchronize()
+assert seen[0] != F.context().handle.value and len(set(seen)) == 1
+assert F.context().muon_last_device_status() == 0
+"""
+
+
+def test_threads_end_and_the_process_exits():
+    """A thread's context passes to the next one, and threads that end while the process exits (autograd's) do not call into the device."""
+    for _ in range(3):
+        r = subprocess.run([sys.executable, "-c", _EXIT], cwd=ROOT, capture_output=True, text=True, timeout=300)
+        assert r.returncode == 0, r.stderr[-2000:]
