@@ -169,17 +169,30 @@ __device__ __forceinline__ Pairs lds_pairs(uint32_t addr) {
   return v;
 }
 
-// dS = P (dP + (-delta)), rounded.  Where a mask made P zero dP may be a NaN: selected, not multiplied.
+// dS = P (dP + (-delta)).  Where a mask made P zero dP may be a NaN: selected, not multiplied.
 template <bool MASK>
-__device__ __forceinline__ uint32_t ds_pair(uint64_t p, uint64_t dp, uint64_t minus_delta) {
+__device__ __forceinline__ uint64_t ds_pair(uint64_t p, uint64_t dp, uint64_t minus_delta) {
   const uint64_t v = mul2(p, add2(dp, minus_delta));
-  if constexpr (!MASK) return pack_bf16(v);
+  if constexpr (!MASK) return v;
   const float2 f = both(v), q = both(p);
-  return pack_bf16(q.x == 0.f ? 0.f : f.x, q.y == 0.f ? 0.f : f.y);
+  return two(q.x == 0.f ? 0.f : f.x, q.y == 0.f ? 0.f : f.y);
 }
 
+// What rounding a pair to bf16 (`hi`) left out, rounded in its turn.
+__device__ __forceinline__ uint32_t pack_rest(uint64_t v, uint32_t hi) {
+  const float2 f = both(v);
+  return pack_bf16(f.x - __uint_as_float(hi << 16), f.y - __uint_as_float(hi & 0xffff0000u));
+}
+
+// P and dS are rounded to bf16 for the products that sum over them: errors of 2^-9 that are independent, so that a sum over n terms has
+// about the relative error of one, as much again as the rounding of the result: sqrt 2 of it together.  With few keys that is wide: at 2 to 40
+// keys up to 1.8 times the rounding of the result, from 128 on 1.46 at the most.  Up to kSplitKeys keys (four times as many packed ones, which
+// several sequences share) both are therefore kept as two bf16 terms, the second in the columns of the scores that the first leaves free, and
+// each of these products is issued twice.  At 32/8 heads of 128 that takes 20.5 us instead of 18.5 for 128 tokens, and 28.7 instead of 24.6 for 256.
+constexpr int kSplitKeys = 128;
+
 // ------------------------------------------------------------------ dk, dv
-template <int BOXES>
+template <int BOXES, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, 1)
 attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnArgs a) {
   using L = Smem<BOXES>;
@@ -307,12 +320,20 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
         elected(ok, [&] {                           // dv += P^T do
           mma_probs_rows<0, 2>(t_dv, t_s, t_s + 64, do_at(n), idesc, n > 0);
           mma_probs_rows<4, 6>(t_dv, t_s, t_s + 64, do_at(n), idesc, true);
+          if constexpr (SPLIT) {
+            mma_probs_rows<0, 2>(t_dv, t_s + 32, t_s + 96, do_at(n), idesc, true);
+            mma_probs_rows<4, 6>(t_dv, t_s + 32, t_s + 96, do_at(n), idesc, true);
+          }
         });
         await(b.p_ready(1), uint32_t(n) & 1u);
         tc_fence_after();
         elected(ok, [&] {
           mma_probs_rows<2, 4>(t_dv, t_s, t_s + 64, do_at(n), idesc, true);
           mma_probs_rows<6, 8>(t_dv, t_s, t_s + 64, do_at(n), idesc, true);
+          if constexpr (SPLIT) {
+            mma_probs_rows<2, 4>(t_dv, t_s + 32, t_s + 96, do_at(n), idesc, true);
+            mma_probs_rows<6, 8>(t_dv, t_s + 32, t_s + 96, do_at(n), idesc, true);
+          }
           tc_commit(b.free1(n));                           // dP^T of this block was issued earlier
           if (next) scores(n + 1);                         // takes the place of P^T, which dv has read by then
         });
@@ -321,6 +342,7 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
         tc_fence_after();
         elected(ok, [&] {
           mma_probs_rows(t_dk, t_dp, t_dp + 64, q_at(n), idesc, n > 0);      // dk += dS^T q
+          if constexpr (SPLIT) mma_probs_rows(t_dk, t_dp + 32, t_dp + 96, q_at(n), idesc, true);
           tc_commit(b.free0(n));
           if (next) dprobs(n + 1);
         });
@@ -368,7 +390,7 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
             for (int i = c * 8; i < c * 8 + 8; ++i) {
               const Pairs l2 = lds_pairs(lse + uint32_t(i) * 16u);
               p[2 * i] = exp2_approx(fma2(words(x[4 * i], x[4 * i + 1]), twice(c2), l2.a));
-              p[2 * i + 1] = exp2_share(!MASK && i % kPolyOf == 0, fma2(words(x[4 * i + 2], x[4 * i + 3]), twice(c2), l2.b));
+              p[2 * i + 1] = exp2_share(!MASK && !SPLIT && i % kPolyOf == 0, fma2(words(x[4 * i + 2], x[4 * i + 3]), twice(c2), l2.b));
               if constexpr (MASK) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
@@ -381,6 +403,11 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
               w[2 * i + 1 - c * 16] = pack_bf16(p[2 * i + 1]);
             }
             tc_st16(ts + c * 16, w);
+            if constexpr (SPLIT) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) w[i] = pack_rest(p[c * 16 + i], w[i]);
+              tc_st16(ts + 32 + c * 16, w);
+            }
             hand_over(b.p_ready(c));
           }
         }
@@ -395,10 +422,17 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const Pairs d = lds_pairs(delta + uint32_t(i) * 16u);
-          w[2 * i] = ds_pair<MASK>(p[2 * i], words(x[4 * i], x[4 * i + 1]), d.a);
-          w[2 * i + 1] = ds_pair<MASK>(p[2 * i + 1], words(x[4 * i + 2], x[4 * i + 3]), d.b);
+          p[2 * i] = ds_pair<MASK>(p[2 * i], words(x[4 * i], x[4 * i + 1]), d.a);
+          p[2 * i + 1] = ds_pair<MASK>(p[2 * i + 1], words(x[4 * i + 2], x[4 * i + 3]), d.b);
+          w[2 * i] = pack_bf16(p[2 * i]);
+          w[2 * i + 1] = pack_bf16(p[2 * i + 1]);
         }
         tc_st32(tp, w);
+        if constexpr (SPLIT) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) w[i] = pack_rest(p[i], w[i]);
+          tc_st32(tp + 32, w);
+        }
         hand_over(b.ds_ready());
       };
       if (block_masked(a, s, r0, c0) || r0 + BLK > s.qn || c0 + BLK > s.kn) step(Yes());
@@ -430,7 +464,7 @@ __device__ __forceinline__ void stay() {
   if (blockIdx.x == gridDim.x - 1) cudaGridDependencySynchronize();
 }
 
-template <int BOXES>
+template <int BOXES, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, 1)
 attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnArgs a) {
   using L = Smem<BOXES>;
@@ -530,6 +564,7 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
         tc_fence_after();                                  // tensor memory written by other threads; tiles need no such fence
         elected(ok, [&] {
           mma_probs_rows(t_dq, t_dp, t_dp + 64, k_at(n), idesc, n > 0);      // dq += dS k
+          if constexpr (SPLIT) mma_probs_rows(t_dq, t_dp + 32, t_dp + 96, k_at(n), idesc, true);
           tc_commit(b.free0(n));
           if (next) dprobs(n + 1);
         });
@@ -565,7 +600,7 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
           tc_wait_ld();
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
-            p[i] = exp2_share(!MASK && i % (2 * kPolyOf) == 1, fma2(words(x[2 * i], x[2 * i + 1]), twice(c2), twice(l2)));
+            p[i] = exp2_share(!MASK && !SPLIT && i % (2 * kPolyOf) == 1, fma2(words(x[2 * i], x[2 * i + 1]), twice(c2), twice(l2)));
             if constexpr (MASK) {
               const float2 f = both(p[i]);
               p[i] = two(2 * i < first || 2 * i >= last ? 0.f : f.x, 2 * i + 1 < first || 2 * i + 1 >= last ? 0.f : f.y);
@@ -580,8 +615,16 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
         for (int i = 0; i < 2; ++i) tc_ld32(tp + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[i * 32]));
         tc_wait_ld();
 #pragma unroll
-        for (int i = 0; i < 32; ++i) w[i] = ds_pair<MASK>(p[i], words(x[2 * i], x[2 * i + 1]), twice(delta));
+        for (int i = 0; i < 32; ++i) {
+          p[i] = ds_pair<MASK>(p[i], words(x[2 * i], x[2 * i + 1]), twice(delta));
+          w[i] = pack_bf16(p[i]);
+        }
         tc_st32(tp, w);
+        if constexpr (SPLIT) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) w[i] = pack_rest(p[i], w[i]);
+          tc_st32(tp + 32, w);
+        }
         tc_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -609,13 +652,13 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
   tear_down(warp, tmem);
 }
 
-template <int BOXES>
+template <int BOXES, bool SPLIT>
 int run(const AttnMaps& m, const AttnArgs& a, cudaStream_t st) {
   const int64_t kb = attn_max_blocks(a, BLK, true) * a.hkv, qb = attn_max_blocks(a, BLK, false) * a.hq;
   if (kb > 0x7fffffff || qb > 0x7fffffff) return MUON_ERR_UNSUPPORTED;
   constexpr uint32_t bytes = Smem<BOXES>::bytes;
   static SharedMemoryLimit limit;
-  if (!limit.raise(a.device, bytes, attention_dkv_tc_kernel<BOXES>, attention_dq_tc_kernel<BOXES>)) return MUON_ERR_CUDA;
+  if (!limit.raise(a.device, bytes, attention_dkv_tc_kernel<BOXES, SPLIT>, attention_dq_tc_kernel<BOXES, SPLIT>)) return MUON_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(THREADS);
   cfg.dynamicSmemBytes = bytes;
@@ -626,9 +669,9 @@ int run(const AttnMaps& m, const AttnArgs& a, cudaStream_t st) {
   cfg.attrs = &at;
   cfg.numAttrs = 1;
   cfg.gridDim = dim3(unsigned(kb));
-  if (cudaLaunchKernelEx(&cfg, attention_dkv_tc_kernel<BOXES>, m, a) != cudaSuccess) return MUON_ERR_CUDA;
+  if (cudaLaunchKernelEx(&cfg, attention_dkv_tc_kernel<BOXES, SPLIT>, m, a) != cudaSuccess) return MUON_ERR_CUDA;
   cfg.gridDim = dim3(unsigned(qb));
-  return cudaLaunchKernelEx(&cfg, attention_dq_tc_kernel<BOXES>, m, a) == cudaSuccess ? 2 : MUON_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, attention_dq_tc_kernel<BOXES, SPLIT>, m, a) == cudaSuccess ? 2 : MUON_ERR_CUDA;
 }
 
 }  // namespace
@@ -648,7 +691,8 @@ int launch_attention_backward_tc(muon_ctx* ctx, const AttnArgs& a, cudaStream_t 
       !encode_tile_map(ctx->tmap_encode, &m.dout, a.dout, a.dim, a.batch, a.nq, a.hq))
     return MUON_ERR_CUDA;
   ctx->tmap_encodes += 4;
-  return a.dim <= 64 ? run<1>(m, a, st) : run<2>(m, a, st);
+  if (a.nk <= (a.nseq ? 4 : 1) * kSplitKeys) return a.dim <= 64 ? run<1, true>(m, a, st) : run<2, true>(m, a, st);
+  return a.dim <= 64 ? run<1, false>(m, a, st) : run<2, false>(m, a, st);
 }
 
 }  // namespace muon

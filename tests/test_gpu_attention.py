@@ -304,6 +304,31 @@ def test_autograd_takes_broadcast_gradients():
         assert torch.equal(t.grad, g)
 
 
+@pytest.mark.parametrize("d", [64, 80, 128])
+@pytest.mark.parametrize("cuts", [[2], [3], [20], [128], [0, 2, 4, 20, 21, 149, 470, 512]])
+def test_few_keys_keep_the_gradients_precision(cuts, d):
+    """Up to 128 keys (512 packed ones) P and dS are two bf16 terms, 2^-16 together: with fp32's 2^-14 for the sums, 2^-13 of the absolute sums
+    instead of 2^-8; only the rounding of the result is that of bf16."""
+    from paper_2609_21594_b200 import functional as F
+
+    n = cuts[-1]
+    q, k, v, do = make(1, n, n, 4, 2, d, BF, seed=n + d)
+    lens = {}
+    if len(cuts) > 1:
+        q, k, v, do = (t[0] for t in (q, k, v, do))
+        at = torch.tensor(cuts, dtype=torch.int32, device="cuda")
+        lens = dict(q_offsets=at, k_offsets=at)
+    up = (lambda t: t[None]) if lens else (lambda t: t)
+    o, lse = F.attention_forward(q, k, v, **lens)
+    got = F.attention_backward(do, q, k, v, o, lse, **lens)
+    r = ref.attention(up(q), up(k), up(v), do=up(do), o=up(o), lse=up(lse), **lens)
+    for name, g in zip(("dq", "dk", "dv"), got):
+        tol = 2.0 ** -13 * r[name + "_abs"] + 2.0 ** -8 * 1.01 * r[name].abs() + 1e-30
+        if name != "dv":
+            tol = tol + 2.0 ** -16 * r[name + "_pre"]
+        close(up(g), r[name], tol, name)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_empty_calls(dtype):
     from paper_2609_21594_b200 import functional as F
