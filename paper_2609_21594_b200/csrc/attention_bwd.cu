@@ -16,6 +16,12 @@
 // 352 threads: eight warps compute (two per lane quadrant, half of the 128 columns each), one loads, one issues, one clears the rows of a
 // streamed tile that lie past the sequence's end.  The issuer alternates: while the warps turn S into P it multiplies with the dS before,
 // while they turn dP into dS it forms the next S.
+//
+// Measured, causal, 32/8 heads of 128: 4096 tokens 431 us, 798 TFLOP/s of the five products that the gradient needs (1117 of the seven issued,
+// 67 % of the library's matrix product alone), 8192 tokens 1.6 ms; 4 x 2048 tokens of heads of 64 363 us.  A round takes 2700 clocks in the dk, dv
+// kernel (its products alone 2048) and 1985 in the dq kernel (1536): the rest is the handing over of P and dS, each a few hundred clocks during
+// which the tensor pipe has only the other product left.  Short and packed sequences (a few rounds per block) pay 1.3 us to start a block and 2
+// to 4 us for its results: 9 documents in 6000 tokens, heads of 64: 205 us.
 #include <cuda_bf16.h>
 
 #include "attention_tc.cuh"
@@ -159,7 +165,8 @@ __device__ __forceinline__ void store_half(const AttnTensor& t, int tb, int toke
   }
 }
 
-constexpr int kPolyOf = 2;                       // one pair of exponentials in 2 * kPolyOf on the multiply-add pipe; `poly` is known at compile time
+// One pair of exponentials in 2 * kPolyOf on the multiply-add pipe: 1 to 2.5 % faster than none.  `poly` is known at compile time.
+constexpr int kPolyOf = 2;
 __device__ __forceinline__ uint64_t exp2_share(bool poly, uint64_t v) { return poly ? exp2_poly(v) : exp2_approx(v); }
 
 struct Pairs { uint64_t a, b; };

