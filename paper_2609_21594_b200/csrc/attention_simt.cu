@@ -6,10 +6,15 @@
 // queries (dq), the other blocks of keys (dk, dv), so every result is summed by one thread in a fixed order, at the price of forming
 // S and do v^T twice.
 //
-// 16 rows per block of 128 threads: thread (r, c) of 16 x 8 holds scores c, c + 8, ... of row r and elements c, c + 8, ... of its
-// accumulators; the 32 streamed rows lie in shared memory at an odd pitch.  Bound by shared-memory reads (two per multiply-add pair) and, for few
-// rows, by the latency of one block's walk: causal, fp32 arithmetic, 4 x 512 tokens of 32/8 heads of 128: forward 1.68 ms (10 TFLOP/s), backward
-// 6.4 ms; one row of 128 tokens of 4 heads of 64: 51 and 135 us.
+// A block owns 64 rows and streams 64 (32 in the backward pass of heads of more than 128) of the other side through shared memory.  256 threads
+// as 16 x 16: thread (ty, tx) forms the scores of rows 4 ty .. 4 ty + 3 with the streamed rows tx, tx + 16, ..., four elements of the head at a
+// time from either side (16 bytes per access, 64 multiply-adds for eight of them), and owns columns 4 tx .. 4 tx + 3 of every 64 of the
+// results of its rows.  Probabilities pass between the two through shared memory, transposed; those of a row stay within its half warp.
+// Tiles lie at a pitch of 4 past a multiple of 64, so that neither kind of access meets a bank twice.  Bound by the multiply-adds and their
+// operands from shared memory.
+// Measured, causal, fp32, 4096 tokens of 8 heads of 128: forward 990 us (34.7 TFLOP/s of the pairs that count), backward 4.2 ms (20.4 of five
+// products, 28.6 of the seven issued); 4 x 512 tokens of 32/8 heads of 128: 291 us and 1.3 ms; 128 tokens of 4 heads of 64: 21 and 64 us, one
+// block's walk.  Few key heads leave SMs without a block of keys: 2048 tokens of 8/2 heads of 256 670 us and 6.3 ms.
 #include <cuda_bf16.h>
 
 #include "layer_ops.h"
@@ -17,7 +22,7 @@
 namespace muon {
 namespace {
 
-constexpr int ROWS = 16, COLS = 32, THREADS = 128, LANES = 8, PER = COLS / LANES;
+constexpr int ROWS = 64, THREADS = 256, PP = ROWS + 4;   // PP: pitch of transposed probabilities
 constexpr float kLog2e = 1.4426950408889634f;
 
 template <typename T> __device__ __forceinline__ float to_f(T v);
@@ -32,86 +37,205 @@ __device__ __forceinline__ T* row_of(const AttnTensor& t, int b, int token, int 
   return static_cast<T*>(t.data) + int64_t(b) * t.sb + int64_t(token) * t.st + int64_t(head) * t.sh;
 }
 
-// Rows [r0, r0 + n) of a head into shared memory; rows from `valid` on are zero, whatever memory holds there.
-template <typename T>
+__device__ __forceinline__ void madd(float4& acc, float x, const float4& y) {
+  acc.x = fmaf(x, y.x, acc.x);
+  acc.y = fmaf(x, y.y, acc.y);
+  acc.z = fmaf(x, y.z, acc.z);
+  acc.w = fmaf(x, y.w, acc.w);
+}
+__device__ __forceinline__ float dot(const float4& x, const float4& y, float s) {
+  return fmaf(x.w, y.w, fmaf(x.z, y.z, fmaf(x.y, y.y, fmaf(x.x, y.x, s))));
+}
+__device__ __forceinline__ float at(const float4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
+// Heads of up to 64 DT elements, tiles of `n` rows.
+template <int DT> struct Tile {
+  static constexpr int kPitch = 64 * DT + 4;
+  __host__ __device__ static constexpr int floats(int n) { return n * kPitch; }
+};
+
+template <typename T> struct alignas(4 * sizeof(T)) Four { T v[4]; };
+
+// Rows [r0, r0 + n) of a head into shared memory; rows from `valid` on and elements past the head are zero, whatever memory holds there.
+template <typename T, int DT>
 __device__ __forceinline__ void load_rows(float* dst, const AttnTensor& t, int tb, int first, int head, int r0, int n, int valid, int dim) {
-  for (int i = threadIdx.x; i < n * dim; i += THREADS) {
-    const int r = i / dim, d = i - r * dim;
-    dst[r * (dim + 1) + d] = r0 + r < valid ? to_f(row_of<T>(t, tb, first + r0 + r, head)[d]) : 0.f;
+  const T* src = row_of<T>(t, tb, first + r0, head);
+  const bool whole = dim % 4 == 0 && reinterpret_cast<uintptr_t>(src) % sizeof(Four<T>) == 0 && t.st % 4 == 0;
+#pragma unroll 8
+  for (int i = threadIdx.x; i < n * 16 * DT; i += THREADS) {
+    const int r = i / (16 * DT), d = i % (16 * DT) * 4;
+    float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (r0 + r < valid && d < dim) {
+      const T* p = src + int64_t(r) * t.st + d;
+      if (whole) {
+        const Four<T> v = *reinterpret_cast<const Four<T>*>(p);
+        w = make_float4(to_f(v.v[0]), to_f(v.v[1]), to_f(v.v[2]), to_f(v.v[3]));
+      } else {
+        w.x = to_f(p[0]);
+        if (d + 1 < dim) w.y = to_f(p[1]);
+        if (d + 2 < dim) w.z = to_f(p[2]);
+        if (d + 3 < dim) w.w = to_f(p[3]);
+      }
+    }
+    *reinterpret_cast<float4*>(dst + r * Tile<DT>::kPitch + d) = w;
   }
 }
 
-__device__ __forceinline__ float dot(const float* x, const float* y, int dim) {
-  float s = 0.f;
-#pragma unroll 8
-  for (int d = 0; d < dim; ++d) s = fmaf(x[d], y[d], s);
-  return s;
+// s[i][j] = <x_(4 ty + i), y_(tx + 16 j)>
+template <int DT, int J>
+__device__ __forceinline__ void products(float (&s)[4][J], const float* x, const float* y, int dim) {
+  constexpr int P = Tile<DT>::kPitch;
+  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < J; ++j) s[i][j] = 0.f;
+#pragma unroll 2
+  for (int d = 0; d < dim; d += 4) {
+    float4 u[4], v[J];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = *reinterpret_cast<const float4*>(x + (4 * ty + i) * P + d);
+#pragma unroll
+    for (int j = 0; j < J; ++j) v[j] = *reinterpret_cast<const float4*>(y + (tx + 16 * j) * P + d);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < J; ++j) s[i][j] = dot(u[i], v[j], s[i][j]);
+  }
 }
 
-template <typename T, int NACC>
-__global__ void __launch_bounds__(THREADS) attention_forward_simt_kernel(const AttnArgs a) {
-  extern __shared__ float sm[];
-  const int pitch = a.dim + 1;
+// The transposed probabilities of this thread: element (row, streamed row) at p[streamed row * PP + row].
+template <int J>
+__device__ __forceinline__ void put(float* p, const float (&s)[4][J]) {
+  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+#pragma unroll
+  for (int j = 0; j < J; ++j) *reinterpret_cast<float4*>(p + (tx + 16 * j) * PP + 4 * ty) = make_float4(s[0][j], s[1][j], s[2][j], s[3][j]);
+}
+
+// acc += P Y over `n` streamed rows
+template <int DT>
+__device__ __forceinline__ void accumulate(float4 (&acc)[4][DT], const float* p, const float* y, int n) {
+  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+#pragma unroll 4
+  for (int k = 0; k < n; ++k) {
+    const float4 w = *reinterpret_cast<const float4*>(p + k * PP + 4 * ty);
+#pragma unroll
+    for (int c = 0; c < DT; ++c) {
+      const float4 v = *reinterpret_cast<const float4*>(y + k * Tile<DT>::kPitch + 4 * tx + 64 * c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) madd(acc[i][c], at(w, i), v);
+    }
+  }
+}
+
+template <int DT> __device__ __forceinline__ void clear(float4 (&acc)[4][DT]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int c = 0; c < DT; ++c) acc[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+}
+
+template <typename T, int DT>
+__device__ __forceinline__ void store_row(T* out, const float4 (&acc)[DT], float scale, int dim) {
+#pragma unroll
+  for (int c = 0; c < DT; ++c)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int d = 4 * int(threadIdx.x % 16) + 64 * c + e;
+      if (d < dim) out[d] = from_f<T>(at(acc[c], e) * scale);
+    }
+}
+
+__device__ __forceinline__ const float* row_info(const AttnArgs& a, const AttnSeq& s, int si, int head, int row) {
+  return a.rows + ((int64_t(s.tb) * a.hq + head) * attn_row_blocks(a) + (a.nseq ? s.q0 / kAttnRowBlock + si : 0) + row / kAttnRowBlock) * (2 * kAttnRowBlock) +
+         row % kAttnRowBlock;
+}
+
+// This block's head, sequence and 64 rows; false past the end.  Heads vary fastest; within a batched call the blocks with most to do go first (the
+// last queries, the first keys).
+__device__ __forceinline__ bool find_work(const AttnArgs& a, bool keys, int* head, int* si, int* blk) {
+  const int heads = keys ? a.hkv : a.hq, t = int(blockIdx.x / unsigned(heads));
+  *head = int(blockIdx.x % unsigned(heads));
+  if (!attn_find_block(a, t, ROWS, keys, si, blk)) return false;
+  if (!a.nseq) {
+    *si = t % a.batch;
+    *blk = keys ? t / a.batch : (a.nq + ROWS - 1) / ROWS - 1 - t / a.batch;
+  }
+  return true;
+}
+
+template <typename T, int DT>
+__global__ void __launch_bounds__(THREADS, DT <= 2 ? 2 : 1) attention_forward_simt_kernel(const __grid_constant__ AttnArgs a) {
+  extern __shared__ __align__(16) float sm[];
   float* sq = sm;
-  float* sk = sq + ROWS * pitch;
-  float* sv = sk + COLS * pitch;
-  float* sp = sv + COLS * pitch;                     // [ROWS][COLS + 1]
-  int si, blk;
-  if (!attn_find_block(a, blockIdx.x, ROWS, false, &si, &blk)) return;
+  float* sk = sq + Tile<DT>::floats(ROWS);
+  float* sv = sk + Tile<DT>::floats(ROWS);
+  float* sp = sk;                                    // the keys are not needed any more when there are probabilities
+  int head, si, blk;
+  if (!find_work(a, false, &head, &si, &blk)) return;
   const AttnSeq s = attn_seq(a, si);
-  const int head = blockIdx.y, kvh = head / (a.hq / a.hkv);
-  const int r0 = blk * ROWS, r = threadIdx.x / LANES, c = threadIdx.x % LANES, row = r0 + r;
-  load_rows<T>(sq, a.q, s.tb, s.q0, head, r0, ROWS, s.qn, a.dim);
-  const int lo = attn_key_lo(a, s, row), hi = attn_key_hi(a, s, row);
+  const int kvh = head / (a.hq / a.hkv), tx = threadIdx.x % 16;
+  const int r0 = blk * ROWS, row = r0 + int(threadIdx.x) / 16 * 4;
+  load_rows<T, DT>(sq, a.q, s.tb, s.q0, head, r0, ROWS, s.qn, a.dim);
+  int lo[4], hi[4];
+  float m[4], l[4];
+  float4 acc[4][DT];
+  clear(acc);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    lo[i] = attn_key_lo(a, s, row + i);
+    hi[i] = attn_key_hi(a, s, row + i);
+    m[i] = -INFINITY;
+    l[i] = 0.f;
+  }
   const int last = min(r0 + ROWS, s.qn) - 1;
   const int klo = attn_key_lo(a, s, r0), khi = last >= r0 ? attn_key_hi(a, s, last) : 0;
-  float m = -INFINITY, l = 0.f, acc[NACC];
-#pragma unroll
-  for (int i = 0; i < NACC; ++i) acc[i] = 0.f;
-  for (int c0 = klo / COLS * COLS; c0 < khi; c0 += COLS) {
+  for (int c0 = klo / ROWS * ROWS; c0 < khi; c0 += ROWS) {
     __syncthreads();
-    load_rows<T>(sk, a.k, s.tb, s.k0, kvh, c0, COLS, s.kn, a.dim);
-    load_rows<T>(sv, a.v, s.tb, s.k0, kvh, c0, COLS, s.kn, a.dim);
+    load_rows<T, DT>(sk, a.k, s.tb, s.k0, kvh, c0, ROWS, s.kn, a.dim);
+    load_rows<T, DT>(sv, a.v, s.tb, s.k0, kvh, c0, ROWS, s.kn, a.dim);
     __syncthreads();
-    float sc[PER], top = -INFINITY;
+    float p[4][4];
+    products<DT, 4>(p, sq, sk, a.dim);
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const int key = c0 + c + j * LANES;
-      sc[j] = key >= lo && key < hi ? dot(sq + r * pitch, sk + (c + j * LANES) * pitch, a.dim) * a.scale : -INFINITY;
-      top = fmaxf(top, sc[j]);
+    for (int i = 0; i < 4; ++i) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int key = c0 + tx + 16 * j;
+        p[i][j] = key >= lo[i] && key < hi[i] ? p[i][j] * a.scale : -INFINITY;
+        top = fmaxf(top, p[i][j]);
+      }
+#pragma unroll
+      for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+      const float mn = fmaxf(m[i], top), base = mn == -INFINITY ? 0.f : mn;
+      const float shrink = m[i] == -INFINITY ? 0.f : exp2f((m[i] - base) * kLog2e);
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum += p[i][j] = exp2f((p[i][j] - base) * kLog2e);
+#pragma unroll
+      for (int d = 1; d < 16; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      l[i] = l[i] * shrink + sum;
+      m[i] = mn;
+#pragma unroll
+      for (int c = 0; c < DT; ++c) {
+        acc[i][c].x *= shrink;
+        acc[i][c].y *= shrink;
+        acc[i][c].z *= shrink;
+        acc[i][c].w *= shrink;
+      }
     }
-#pragma unroll
-    for (int d = 1; d < LANES; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    const float mn = fmaxf(m, top), base = mn == -INFINITY ? 0.f : mn;
-    const float shrink = m == -INFINITY ? 0.f : exp2f((m - base) * kLog2e);
-    float sum = 0.f;
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const float p = exp2f((sc[j] - base) * kLog2e);
-      sp[r * (COLS + 1) + c + j * LANES] = p;
-      sum += p;
-    }
-#pragma unroll
-    for (int d = 1; d < LANES; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    l = l * shrink + sum;
-    m = mn;
-    __syncwarp();                                    // the eight threads of a row are in one warp
-#pragma unroll
-    for (int i = 0; i < NACC; ++i) acc[i] *= shrink;
-    for (int k = 0; k < COLS; ++k) {
-      const float p = sp[r * (COLS + 1) + k];
-#pragma unroll
-      for (int i = 0; i < NACC; ++i)
-        if (c + i * LANES < a.dim) acc[i] = fmaf(p, sv[k * pitch + c + i * LANES], acc[i]);
-    }
+    __syncthreads();                                 // everybody has read the keys
+    put(sp, p);
     __syncwarp();
+    accumulate(acc, sp, sv, min(ROWS, khi - c0));
   }
-  if (row >= s.qext) return;
-  T* out = row_of<T>(a.o, s.tb, s.q0 + row, head);
 #pragma unroll
-  for (int i = 0; i < NACC; ++i)
-    if (c + i * LANES < a.dim) out[c + i * LANES] = from_f<T>(l == 0.f ? 0.f : acc[i] / l);
-  if (c == 0) a.lse[(int64_t(s.tb) * a.hq + head) * a.nq + s.q0 + row] = l == 0.f ? -INFINITY : m + logf(l);
+  for (int i = 0; i < 4; ++i) {
+    if (row + i >= s.qext) break;
+    store_row<T, DT>(row_of<T>(a.o, s.tb, s.q0 + row + i, head), acc[i], l[i] == 0.f ? 0.f : 1.f / l[i], a.dim);
+    if (tx == 0) a.lse[(int64_t(s.tb) * a.hq + head) * a.nq + s.q0 + row + i] = l[i] == 0.f ? -INFINITY : m[i] + logf(l[i]);
+  }
 }
 
 // -lse in units of log 2 and -delta, delta = sum_d do o, into the padded row blocks: P = exp2(scale' S + (-lse)) and dS = P (dP + (-delta)) are
@@ -180,156 +304,160 @@ __global__ void __launch_bounds__(256, 4) attention_rows_kernel(const __grid_con
   out[kAttnRowBlock + threadIdx.x] = seen ? sums[threadIdx.x] : 0.f;          // whatever a row that counts for nothing holds
 }
 
-template <typename T, int NACC>
-__global__ void __launch_bounds__(THREADS) attention_dq_simt_kernel(const AttnArgs a) {
-  extern __shared__ float sm[];
-  const int pitch = a.dim + 1;
+template <int DT> constexpr int kStreamed = DT == 4 ? 32 : 64;   // rows streamed at a time in the backward pass
+
+template <typename T, int DT>
+__global__ void __launch_bounds__(THREADS, DT == 1 ? 2 : 1) attention_dq_simt_kernel(const __grid_constant__ AttnArgs a) {
+  constexpr int COLS = kStreamed<DT>, J = COLS / 16;
+  extern __shared__ __align__(16) float sm[];
   float* sq = sm;
-  float* sdo = sq + ROWS * pitch;
-  float* sk = sdo + ROWS * pitch;
-  float* sv = sk + COLS * pitch;
-  float* sp = sv + COLS * pitch;
-  int si, blk;
-  if (!attn_find_block(a, blockIdx.x, ROWS, false, &si, &blk)) return;
+  float* sdo = sq + Tile<DT>::floats(ROWS);
+  float* sk = sdo + Tile<DT>::floats(ROWS);
+  float* sv = sk + Tile<DT>::floats(COLS);
+  float* sds = sv;                                   // the values are not needed any more when there is dS
+  int head, si, blk;
+  if (!find_work(a, false, &head, &si, &blk)) return;
   const AttnSeq s = attn_seq(a, si);
-  const int head = blockIdx.y, kvh = head / (a.hq / a.hkv);
-  const int r0 = blk * ROWS, r = threadIdx.x / LANES, c = threadIdx.x % LANES, row = r0 + r;
-  load_rows<T>(sq, a.q, s.tb, s.q0, head, r0, ROWS, s.qn, a.dim);
-  load_rows<T>(sdo, a.dout, s.tb, s.q0, head, r0, ROWS, s.qn, a.dim);
-  const float* info = a.rows + ((int64_t(s.tb) * a.hq + head) * attn_row_blocks(a) + (a.nseq ? s.q0 / kAttnRowBlock + si : 0) + row / kAttnRowBlock) *
-                                   (2 * kAttnRowBlock) + row % kAttnRowBlock;
-  const float l2 = info[0], delta = info[kAttnRowBlock], c2 = a.scale * kLog2e;
-  const int lo = attn_key_lo(a, s, row), hi = attn_key_hi(a, s, row);
+  const int kvh = head / (a.hq / a.hkv), tx = threadIdx.x % 16;
+  const int r0 = blk * ROWS, row = r0 + int(threadIdx.x) / 16 * 4;
+  load_rows<T, DT>(sq, a.q, s.tb, s.q0, head, r0, ROWS, s.qn, a.dim);
+  load_rows<T, DT>(sdo, a.dout, s.tb, s.q0, head, r0, ROWS, s.qn, a.dim);
+  const float* info = row_info(a, s, si, head, row);  // four rows of one block of 128: row is a multiple of four
+  const float c2 = a.scale * kLog2e;
+  int lo[4], hi[4];
+  float l2[4], delta[4];
+  float4 acc[4][DT];
+  clear(acc);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    lo[i] = attn_key_lo(a, s, row + i);
+    hi[i] = attn_key_hi(a, s, row + i);
+    l2[i] = info[i];
+    delta[i] = info[kAttnRowBlock + i];
+  }
   const int last = min(r0 + ROWS, s.qn) - 1;
   const int klo = attn_key_lo(a, s, r0), khi = last >= r0 ? attn_key_hi(a, s, last) : 0;
-  float acc[NACC];
-#pragma unroll
-  for (int i = 0; i < NACC; ++i) acc[i] = 0.f;
   for (int c0 = klo / COLS * COLS; c0 < khi; c0 += COLS) {
     __syncthreads();
-    load_rows<T>(sk, a.k, s.tb, s.k0, kvh, c0, COLS, s.kn, a.dim);
-    load_rows<T>(sv, a.v, s.tb, s.k0, kvh, c0, COLS, s.kn, a.dim);
+    load_rows<T, DT>(sk, a.k, s.tb, s.k0, kvh, c0, COLS, s.kn, a.dim);
+    load_rows<T, DT>(sv, a.v, s.tb, s.k0, kvh, c0, COLS, s.kn, a.dim);
     __syncthreads();
+    float p[4][J], dp[4][J];
+    products<DT, J>(p, sq, sk, a.dim);
+    products<DT, J>(dp, sdo, sv, a.dim);
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const int k = c + j * LANES, key = c0 + k;
-      float ds = 0.f;
-      if (key >= lo && key < hi)
-        ds = exp2f(fmaf(dot(sq + r * pitch, sk + k * pitch, a.dim), c2, l2)) * (dot(sdo + r * pitch, sv + k * pitch, a.dim) + delta);
-      sp[r * (COLS + 1) + k] = ds;
-    }
-    __syncwarp();
-    for (int k = 0; k < COLS; ++k) {
-      const float ds = sp[r * (COLS + 1) + k];
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int i = 0; i < NACC; ++i)
-        if (c + i * LANES < a.dim) acc[i] = fmaf(ds, sk[k * pitch + c + i * LANES], acc[i]);
-    }
+      for (int j = 0; j < J; ++j) {
+        const int key = c0 + tx + 16 * j;
+        p[i][j] = key >= lo[i] && key < hi[i] ? exp2f(fmaf(p[i][j], c2, l2[i])) * (dp[i][j] + delta[i]) : 0.f;
+      }
+    __syncthreads();                                 // everybody has read the values
+    put(sds, p);
     __syncwarp();
+    accumulate(acc, sds, sk, min(COLS, khi - c0));
   }
-  if (row >= s.qext) return;
-  T* out = row_of<T>(a.dq, s.tb, s.q0 + row, head);
 #pragma unroll
-  for (int i = 0; i < NACC; ++i)
-    if (c + i * LANES < a.dim) out[c + i * LANES] = from_f<T>(acc[i] * a.scale);
+  for (int i = 0; i < 4; ++i)
+    if (row + i < s.qext) store_row<T, DT>(row_of<T>(a.dq, s.tb, s.q0 + row + i, head), acc[i], a.scale, a.dim);
 }
 
-template <typename T, int NACC>
-__global__ void __launch_bounds__(THREADS) attention_dkv_simt_kernel(const AttnArgs a) {
-  extern __shared__ float sm[];
-  const int pitch = a.dim + 1;
+template <typename T, int DT>
+__global__ void __launch_bounds__(THREADS, DT == 1 ? 2 : 1) attention_dkv_simt_kernel(const __grid_constant__ AttnArgs a) {
+  constexpr int COLS = kStreamed<DT>, J = COLS / 16;
+  extern __shared__ __align__(16) float sm[];
   float* sk = sm;
-  float* sv = sk + ROWS * pitch;
-  float* sq = sv + ROWS * pitch;
-  float* sdo = sq + COLS * pitch;
-  float* sp = sdo + COLS * pitch;
-  float* sds = sp + ROWS * (COLS + 1);
-  int si, blk;
-  if (!attn_find_block(a, blockIdx.x, ROWS, true, &si, &blk)) return;
+  float* sv = sk + Tile<DT>::floats(ROWS);
+  float* sq = sv + Tile<DT>::floats(ROWS);
+  float* sdo = sq + Tile<DT>::floats(COLS);
+  float* sp = sdo + Tile<DT>::floats(COLS);
+  float* sds = sp + COLS * PP;
+  int kvh, si, blk;
+  if (!find_work(a, true, &kvh, &si, &blk)) return;
   const AttnSeq s = attn_seq(a, si);
-  const int kvh = blockIdx.y, group = a.hq / a.hkv;
-  const int r0 = blk * ROWS, r = threadIdx.x / LANES, c = threadIdx.x % LANES, key = r0 + r;
-  load_rows<T>(sk, a.k, s.tb, s.k0, kvh, r0, ROWS, s.kn, a.dim);
-  load_rows<T>(sv, a.v, s.tb, s.k0, kvh, r0, ROWS, s.kn, a.dim);
+  const int group = a.hq / a.hkv, tx = threadIdx.x % 16;
+  const int r0 = blk * ROWS, key = r0 + int(threadIdx.x) / 16 * 4;
+  load_rows<T, DT>(sk, a.k, s.tb, s.k0, kvh, r0, ROWS, s.kn, a.dim);
+  load_rows<T, DT>(sv, a.v, s.tb, s.k0, kvh, r0, ROWS, s.kn, a.dim);
   const float c2 = a.scale * kLog2e;
   const int c1 = min(r0 + ROWS, s.kn);
   const int qlo = r0 < s.kn ? attn_query_lo(a, s, r0) : 0, qhi = r0 < s.kn ? attn_query_hi(a, s, c1) : 0;
-  float dk[NACC], dv[NACC];
-#pragma unroll
-  for (int i = 0; i < NACC; ++i) dk[i] = dv[i] = 0.f;
-  for (int h = kvh * group; h < (kvh + 1) * group; ++h) {
-    const float* info = a.rows + ((int64_t(s.tb) * a.hq + h) * attn_row_blocks(a) + (a.nseq ? s.q0 / kAttnRowBlock + si : 0)) * (2 * kAttnRowBlock);
+  float4 dk[4][DT], dv[4][DT];
+  clear(dk);
+  clear(dv);
+  for (int h = kvh * group; h < (kvh + 1) * group; ++h)
     for (int i0 = qlo / COLS * COLS; i0 < qhi; i0 += COLS) {
       __syncthreads();
-      load_rows<T>(sq, a.q, s.tb, s.q0, h, i0, COLS, s.qn, a.dim);
-      load_rows<T>(sdo, a.dout, s.tb, s.q0, h, i0, COLS, s.qn, a.dim);
+      load_rows<T, DT>(sq, a.q, s.tb, s.q0, h, i0, COLS, s.qn, a.dim);
+      load_rows<T, DT>(sdo, a.dout, s.tb, s.q0, h, i0, COLS, s.qn, a.dim);
       __syncthreads();
+      float p[4][J], ds[4][J];
+      products<DT, J>(p, sk, sq, a.dim);
+      products<DT, J>(ds, sv, sdo, a.dim);
 #pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        const int q = c + j * LANES, i = i0 + q;
-        float p = 0.f, ds = 0.f;
-        if (i < s.qn && key >= attn_key_lo(a, s, i) && key < attn_key_hi(a, s, i)) {
-          const float* at = info + i / kAttnRowBlock * (2 * kAttnRowBlock) + i % kAttnRowBlock;
-          p = exp2f(fmaf(dot(sk + r * pitch, sq + q * pitch, a.dim), c2, at[0]));
-          ds = p * (dot(sv + r * pitch, sdo + q * pitch, a.dim) + at[kAttnRowBlock]);
+      for (int j = 0; j < J; ++j) {
+        const int i = i0 + tx + 16 * j;
+        const bool in = i < s.qn;
+        const float* info = row_info(a, s, si, h, in ? i : 0);
+        const int lo = in ? attn_key_lo(a, s, i) : 0, hi = in ? attn_key_hi(a, s, i) : 0;
+        const float l2 = info[0], delta = info[kAttnRowBlock];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool seen = key + e >= lo && key + e < hi;
+          p[e][j] = seen ? exp2f(fmaf(p[e][j], c2, l2)) : 0.f;
+          ds[e][j] = seen ? p[e][j] * (ds[e][j] + delta) : 0.f;
         }
-        sp[r * (COLS + 1) + q] = p;
-        sds[r * (COLS + 1) + q] = ds;
       }
+      put(sp, p);                                    // read by this half warp alone, before the next meeting
+      put(sds, ds);
       __syncwarp();
-      for (int q = 0; q < COLS; ++q) {
-        const float p = sp[r * (COLS + 1) + q], ds = sds[r * (COLS + 1) + q];
-#pragma unroll
-        for (int i = 0; i < NACC; ++i)
-          if (c + i * LANES < a.dim) {
-            dv[i] = fmaf(p, sdo[q * pitch + c + i * LANES], dv[i]);
-            dk[i] = fmaf(ds, sq[q * pitch + c + i * LANES], dk[i]);
-          }
-      }
-      __syncwarp();
+      const int n = min(COLS, qhi - i0);
+      accumulate(dv, sp, sdo, n);
+      accumulate(dk, sds, sq, n);
     }
-  }
-  if (key >= s.kext) return;
-  T* ok = row_of<T>(a.dk, s.tb, s.k0 + key, kvh);
-  T* ov = row_of<T>(a.dv, s.tb, s.k0 + key, kvh);
 #pragma unroll
-  for (int i = 0; i < NACC; ++i)
-    if (c + i * LANES < a.dim) {
-      ok[c + i * LANES] = from_f<T>(dk[i] * a.scale);
-      ov[c + i * LANES] = from_f<T>(dv[i]);
+  for (int i = 0; i < 4; ++i)
+    if (key + i < s.kext) {
+      store_row<T, DT>(row_of<T>(a.dk, s.tb, s.k0 + key + i, kvh), dk[i], a.scale, a.dim);
+      store_row<T, DT>(row_of<T>(a.dv, s.tb, s.k0 + key + i, kvh), dv[i], 1.f, a.dim);
     }
 }
 
 template <typename K>
-int run(K kernel, const AttnArgs& a, bool keys, int row_tiles, int score_tiles, cudaStream_t st) {
-  const int64_t blocks = attn_max_blocks(a, ROWS, keys);
+int run(K kernel, const AttnArgs& a, bool keys, int floats, SharedMemoryLimit& limit, cudaStream_t st) {
+  const int64_t blocks = attn_max_blocks(a, ROWS, keys) * (keys ? a.hkv : a.hq);
   if (blocks == 0) return 0;
-  const int heads = keys ? a.hkv : a.hq;
-  if (blocks > 0x7fffffff || heads > 65535) return MUON_ERR_UNSUPPORTED;
-  const int bytes = int(sizeof(float)) * ((row_tiles * ROWS + 2 * COLS) * (a.dim + 1) + score_tiles * ROWS * (COLS + 1));
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return MUON_ERR_CUDA;
-  kernel<<<dim3(unsigned(blocks), unsigned(heads)), THREADS, bytes, st>>>(a);
+  if (blocks > 0x7fffffff) return MUON_ERR_UNSUPPORTED;
+  const int bytes = int(sizeof(float)) * floats;
+  if (!limit.raise(a.device, bytes, kernel)) return MUON_ERR_CUDA;
+  kernel<<<unsigned(blocks), THREADS, bytes, st>>>(a);
   return cudaGetLastError() == cudaSuccess ? 1 : MUON_ERR_CUDA;
 }
 
-// Registers are sized for the head: 8, 16 or 32 accumulators for up to 64, 128 or 256 elements.
-template <typename T>
+template <typename T, int DT>
 int forward(const AttnArgs& a, cudaStream_t st) {
-  if (a.dim <= 64) return run(attention_forward_simt_kernel<T, 8>, a, false, 1, 1, st);
-  if (a.dim <= 128) return run(attention_forward_simt_kernel<T, 16>, a, false, 1, 1, st);
-  return run(attention_forward_simt_kernel<T, 32>, a, false, 1, 1, st);
+  static SharedMemoryLimit limit;
+  return run(attention_forward_simt_kernel<T, DT>, a, false, 3 * Tile<DT>::floats(ROWS), limit, st);
 }
 
-template <typename T>
+template <typename T, int DT>
 int backward(const AttnArgs& a, cudaStream_t st) {
-  const int dq = a.dim <= 64    ? run(attention_dq_simt_kernel<T, 8>, a, false, 2, 1, st)
-                 : a.dim <= 128 ? run(attention_dq_simt_kernel<T, 16>, a, false, 2, 1, st)
-                                : run(attention_dq_simt_kernel<T, 32>, a, false, 2, 1, st);
+  constexpr int C = kStreamed<DT>, tiles = 2 * Tile<DT>::floats(ROWS) + 2 * Tile<DT>::floats(C);
+  static SharedMemoryLimit limit_dq, limit_dkv;
+  const int dq = run(attention_dq_simt_kernel<T, DT>, a, false, tiles, limit_dq, st);
   if (dq < 0) return dq;
-  const int dkv = a.dim <= 64    ? run(attention_dkv_simt_kernel<T, 8>, a, true, 2, 2, st)
-                  : a.dim <= 128 ? run(attention_dkv_simt_kernel<T, 16>, a, true, 2, 2, st)
-                                 : run(attention_dkv_simt_kernel<T, 32>, a, true, 2, 2, st);
+  const int dkv = run(attention_dkv_simt_kernel<T, DT>, a, true, tiles + 2 * C * PP, limit_dkv, st);
   return dkv < 0 ? dkv : dq + dkv;
+}
+
+// Registers and shared memory are sized for heads of up to 64, 128 or 256 elements.
+template <typename T>
+int forward_by_dim(const AttnArgs& a, cudaStream_t st) {
+  return a.dim <= 64 ? forward<T, 1>(a, st) : a.dim <= 128 ? forward<T, 2>(a, st) : forward<T, 4>(a, st);
+}
+template <typename T>
+int backward_by_dim(const AttnArgs& a, cudaStream_t st) {
+  return a.dim <= 64 ? backward<T, 1>(a, st) : a.dim <= 128 ? backward<T, 2>(a, st) : backward<T, 4>(a, st);
 }
 
 }  // namespace
@@ -350,11 +478,11 @@ int launch_attention_rows(const AttnArgs& a, int dtype, cudaStream_t st) {
 }
 
 int launch_attention_forward_simt(const AttnArgs& a, int dtype, cudaStream_t st) {
-  return dtype == MUON_DTYPE_BF16 ? forward<__nv_bfloat16>(a, st) : forward<float>(a, st);
+  return dtype == MUON_DTYPE_BF16 ? forward_by_dim<__nv_bfloat16>(a, st) : forward_by_dim<float>(a, st);
 }
 
 int launch_attention_backward_simt(const AttnArgs& a, int dtype, cudaStream_t st) {
-  return dtype == MUON_DTYPE_BF16 ? backward<__nv_bfloat16>(a, st) : backward<float>(a, st);
+  return dtype == MUON_DTYPE_BF16 ? backward_by_dim<__nv_bfloat16>(a, st) : backward_by_dim<float>(a, st);
 }
 
 }  // namespace muon
