@@ -321,7 +321,9 @@ __global__ void __launch_bounds__(Geometry<TPR>::kThreads, BLOCKS) norm_backward
     for (int i = 0; i < G * BWD_STAGES; ++i) tc::mbar_init(uint32_t(__cvta_generic_to_shared(bars + i)), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  __syncthreads();
+  // The sums of a row are stored into the other block's shared memory, which may be touched only once that block runs: the cluster meets here.
+  if constexpr (CLUSTER > 1) cg::this_cluster().sync();
+  else __syncthreads();
   auto place = [&](uint32_t stage, int k, int which) { return ring + ((stage * R + k) * 2 + which) * uint32_t(RW::kRowBytes); };
   const int64_t step = int64_t(gridDim.x / CLUSTER) * G * R, r0 = (int64_t(blockIdx.x / CLUSTER) * G + group) * R;
   auto fetch = [&](uint32_t stage, int64_t r) {
