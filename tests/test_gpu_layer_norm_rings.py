@@ -25,3 +25,12 @@ def test_rows_cut_between_two_blocks_keep_their_sums(dtype, rows, cols):
         got = F.layer_norm_backward(dy, x, w, mean, rstd)
         assert all(torch.equal(a, b) for a, b in zip(got, want))
     torch.cuda.current_stream().wait_stream(side)
+
+
+@pytest.mark.parametrize("center", [True, False])
+@pytest.mark.parametrize("rows,cols", [(5000, 40), (5000, 256), (3000, 512), (2500, 1024), (1300, 4096), (1000, 8192), (700, 12288), (700, 16384), (900, 1001)])
+def test_many_fp32_rows_per_group(rows, cols, center):
+    """fp32 rows by pieces: two places ahead forward (one above 8192 columns), three backward, each used several times."""
+    x, w, b, dy = make(rows, cols, torch.float32, torch.float32)
+    mean, rstd = check_forward(x, w, b, 1e-5, center)
+    check_backward(dy, x, w, mean, rstd)
