@@ -468,7 +468,10 @@ int muon_rotary_frequencies(double base, int32_t rotary_dim, int32_t scaling, do
  *            tokens into sequences; tokens after the last offset belong to none
  * With nq queries and nk keys of a sequence, query i sees key j < nk when i < nq and, with causal = 1, j <= i + nk - nq, and, with
  * window > 0 (causal only), also j > i + nk - nq - window.  A query that sees nothing has o = 0 and lse = -inf, takes and gives no
- * gradient; so have tokens that do not count.  What such tokens hold (NaN, infinities) reaches no result of another token. */
+ * gradient; so have tokens that do not count, and a key that no query sees takes no gradient.  What queries that see nothing and tokens that
+ * do not count hold (NaN, infinities) reaches no result of another token.  A key that counts and is masked from a query only by causal or
+ * window meets it, within its block of 128 keys, as a product with a probability of zero: there a NaN or an infinity in v still
+ * reaches that query's o, and one in q or do of a query the dk and dv of keys of its block that it does not see. */
 typedef struct {
   int32_t dtype;                 /* MUON_DTYPE_BF16: tensor cores when every pointer is 16-byte aligned, head_dim is a multiple of 8 up  */
                                  /* to 128 and every stride is a multiple of 8; otherwise, and for MUON_DTYPE_FP32, CUDA cores         */

@@ -140,9 +140,10 @@ __device__ __forceinline__ void finish_issue(const Bars& b, bool ok, volatile in
   if (!mbar_wait(b.all_done(), 0, abort_flag, false, WAIT_CYCLES / 8)) atomicExch(status, 34);
 }
 
-// 64 columns of a row times `scale`, rounded, to global memory; the accumulator is ignored where `zero`.
+// 64 columns of a row times `scale`, rounded, to global memory; the accumulator is not read where `zero` (the whole warp) and does not count where
+// `dead` (this row: it saw nothing, and has met zeros times whatever the others hold).
 __device__ __forceinline__ void store_half(const AttnTensor& t, int tb, int token, int head, int d0, int dim, uint32_t taddr, int cols, float scale,
-                                           bool zero, bool store) {
+                                           bool zero, bool dead, bool store) {
   __nv_bfloat16* out = static_cast<__nv_bfloat16*>(t.data) + int64_t(tb) * t.sb + int64_t(token) * t.st + int64_t(head) * t.sh;
   for (int i = 0; i < cols / 32; ++i) {
     uint32_t o[32];
@@ -154,7 +155,7 @@ __device__ __forceinline__ void store_half(const AttnTensor& t, int tb, int toke
     for (int e = 0; e < 4; ++e) {
       const int d = d0 + i * 32 + e * 8;
       uint4 w = make_uint4(0, 0, 0, 0);
-      if (!zero) {
+      if (!zero && !dead) {
         w.x = pack_bf16(__uint_as_float(o[e * 8]) * scale, __uint_as_float(o[e * 8 + 1]) * scale);
         w.y = pack_bf16(__uint_as_float(o[e * 8 + 2]) * scale, __uint_as_float(o[e * 8 + 3]) * scale);
         w.z = pack_bf16(__uint_as_float(o[e * 8 + 4]) * scale, __uint_as_float(o[e * 8 + 5]) * scale);
@@ -233,6 +234,9 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
     }
   }
   const int per = i1 - i0, total = per * group;
+  // Blocks of queries with rows to clear: the last where it passes the sequence's end, the first where queries see nothing.
+  const int blind = attn_blind(a, s);
+  auto ragged = [&](int i) { return i * BLK < blind || (i + 1) * BLK > s.qn; };
   set_up<BOXES>(b, warp, tmem_slot, abort_flag);
   const uint32_t tmem = *tmem_slot, t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 256 + BOXES * 64;
   auto q_at = [&](int n) { return base + L::s0 + uint32_t(n % PLACES0) * L::kTile; };
@@ -256,13 +260,13 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
       }
       auto load_q = [&](int n) {
         const int h = kvh * group + n / per, i = i0 + n % per;
-        const uint32_t bar = (i + 1) * BLK > s.qn ? b.raw0(n) : b.full0(n);
+        const uint32_t bar = ragged(i) ? b.raw0(n) : b.full0(n);
         mbar_expect_tx(bar, L::kTile);
         load_tile<BOXES>(q_at(n), &maps.q, bar, h, s.q0 + i * BLK, s.tb);
       };
       auto load_do = [&](int n) {
         const int h = kvh * group + n / per, i = i0 + n % per;
-        const uint32_t bar = (i + 1) * BLK > s.qn ? b.raw1(n) : b.full1(n);
+        const uint32_t bar = ragged(i) ? b.raw1(n) : b.full1(n);
         const float* rows = a.rows + ((int64_t(s.tb) * a.hq + h) * row_blocks + (a.nseq ? s.q0 / kAttnRowBlock + si : 0) + i) * (2 * kAttnRowBlock);
         mbar_expect_tx(bar, L::kTile + 2 * ROW_BYTES);
         bulk_load(lse_at(n), rows, ROW_BYTES, bar);
@@ -272,8 +276,9 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
       load_rounds(b, total, abort_flag, a.status, load_q, load_do);
     }
   } else if (warp == SWEEPER) {
-    // ------------------------------------------------------------------ rows past the end: the last block of every head
-    if (total > 0 && i1 * BLK > s.qn) {
+    // ------------------------------------------------------------------ rows that do not count: in the first and the last block of every head
+    const bool head_rows = per > 1 && ragged(i0), tail_rows = per > 0 && ragged(i1 - 1);
+    if (head_rows || tail_rows) {
       int uses0[PLACES0] = {}, uses1[PLACES1] = {};
       auto next_use = [](int (&uses)[PLACES0], int (&uses1)[PLACES1], int w, int n) {
         int u = 0;
@@ -286,13 +291,14 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
         return uint32_t(u) & 1u;
       };
       bool ok = true;
-      for (int h = 0; h < group && ok; ++h) {
-        const int n = h * per + per - 1;
+      for (int t = 0; t < 2 * group && ok; ++t) {
+        if (!(t & 1 ? tail_rows : head_rows)) continue;
+        const int i = t & 1 ? i1 - 1 : i0, n = (t >> 1) * per + (i - i0);
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
           const uint32_t ph = next_use(uses0, uses1, w, n);
           ok = ok && __all_sync(0xffffffffu, mbar_wait(w ? b.raw1(n) : b.raw0(n), ph, abort_flag));
-          if (ok) clear_rows<BOXES>(w ? do_at(n) : q_at(n), s.qn - (i1 - 1) * BLK, lane, w ? b.full1(n) : b.full0(n));
+          if (ok) clear_rows<BOXES>(w ? do_at(n) : q_at(n), blind - i * BLK, s.qn - i * BLK, lane, w ? b.full1(n) : b.full0(n));
         }
       }
       if (!ok && lane == 0) *abort_flag = 1;
@@ -456,10 +462,10 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
         atomicExch(a.status, 35);
       }
     } else {
-      const bool zero = total == 0, store = key < s.kext;
+      const bool zero = total == 0, store = key < s.kext, unseen = qhi <= max(qlo, 0);
       constexpr int cols = BOXES * 32;                     // the two warps of a quadrant share the head
-      store_half(a.dv, s.tb, s.k0 + key, kvh, half * cols, a.dim, t_dv + lanes + uint32_t(half * cols), cols, 1.f, zero, store);
-      store_half(a.dk, s.tb, s.k0 + key, kvh, half * cols, a.dim, t_dk + lanes + uint32_t(half * cols), cols, a.scale, zero, store);
+      store_half(a.dv, s.tb, s.k0 + key, kvh, half * cols, a.dim, t_dv + lanes + uint32_t(half * cols), cols, 1.f, zero, unseen, store);
+      store_half(a.dk, s.tb, s.k0 + key, kvh, half * cols, a.dim, t_dk + lanes + uint32_t(half * cols), cols, a.scale, zero, unseen, store);
     }
   }
   tear_down(warp, tmem);
@@ -535,7 +541,7 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
     // ------------------------------------------------------------------ rows of the last k tile past the end: their dS is zero, and so must be dS k
     if (total > 0 && rg.n1 * BLK > s.kn) {
       if (__all_sync(0xffffffffu, mbar_wait(b.raw0(total - 1), 0, abort_flag)))
-        clear_rows<BOXES>(k_at(total - 1), s.kn - (rg.n1 - 1) * BLK, lane, b.full0(total - 1));
+        clear_rows<BOXES>(k_at(total - 1), 0, s.kn - (rg.n1 - 1) * BLK, lane, b.full0(total - 1));
       else if (lane == 0) *abort_flag = 1;
     }
   } else if (warp == ISSUER) {
@@ -652,7 +658,7 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
       }
     } else {
       constexpr int cols = BOXES * 32;
-      store_half(a.dq, s.tb, s.q0 + row, head, half * cols, a.dim, t_dq + lanes + uint32_t(half * cols), cols, a.scale, total == 0,
+      store_half(a.dq, s.tb, s.q0 + row, head, half * cols, a.dim, t_dq + lanes + uint32_t(half * cols), cols, a.scale, total == 0, hi <= lo,
                  row < s.qext);
     }
   }

@@ -193,7 +193,7 @@ attention_forward_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_
       if (u1 > u0 && u1 * BLK > s.kn) {
         const int st = (u1 - u0) % STAGES;
         if (__all_sync(0xffffffffu, mbar_wait(raw_bar, 0, abort_flag)))
-          clear_rows<BOXES>(base + L::v + uint32_t(st) * L::kTile, s.kn - (u1 - 1) * BLK, lane, full(st));
+          clear_rows<BOXES>(base + L::v + uint32_t(st) * L::kTile, 0, s.kn - (u1 - 1) * BLK, lane, full(st));
         else if (lane == 0) *abort_flag = 1;
       }
     }

@@ -56,16 +56,18 @@ template <int DT> struct Tile {
 
 template <typename T> struct alignas(4 * sizeof(T)) Four { T v[4]; };
 
-// Rows [r0, r0 + n) of a head into shared memory; rows from `valid` on and elements past the head are zero, whatever memory holds there.
+// Rows [r0, r0 + n) of a head into shared memory; rows before `from`, rows from `valid` on and elements past the head are zero, whatever memory
+// holds there.
 template <typename T, int DT>
-__device__ __forceinline__ void load_rows(float* dst, const AttnTensor& t, int tb, int first, int head, int r0, int n, int valid, int dim) {
+__device__ __forceinline__ void load_rows(float* dst, const AttnTensor& t, int tb, int first, int head, int r0, int n, int valid, int dim,
+                                          int from = 0) {
   const T* src = row_of<T>(t, tb, first + r0, head);
   const bool whole = dim % 4 == 0 && reinterpret_cast<uintptr_t>(src) % sizeof(Four<T>) == 0 && t.st % 4 == 0;
 #pragma unroll 8
   for (int i = threadIdx.x; i < n * 16 * DT; i += THREADS) {
     const int r = i / (16 * DT), d = i % (16 * DT) * 4;
     float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (r0 + r < valid && d < dim) {
+    if (r0 + r >= from && r0 + r < valid && d < dim) {
       const T* p = src + int64_t(r) * t.st + d;
       if (whole) {
         const Four<T> v = *reinterpret_cast<const Four<T>*>(p);
@@ -135,14 +137,15 @@ template <int DT> __device__ __forceinline__ void clear(float4 (&acc)[4][DT]) {
     for (int c = 0; c < DT; ++c) acc[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
 }
 
+// A row times `scale`; a `dead` one saw nothing and has met zeros times whatever the others hold.
 template <typename T, int DT>
-__device__ __forceinline__ void store_row(T* out, const float4 (&acc)[DT], float scale, int dim) {
+__device__ __forceinline__ void store_row(T* out, const float4 (&acc)[DT], float scale, bool dead, int dim) {
 #pragma unroll
   for (int c = 0; c < DT; ++c)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int d = 4 * int(threadIdx.x % 16) + 64 * c + e;
-      if (d < dim) out[d] = from_f<T>(at(acc[c], e) * scale);
+      if (d < dim) out[d] = from_f<T>(dead ? 0.f : at(acc[c], e) * scale);
     }
 }
 
@@ -233,7 +236,7 @@ __global__ void __launch_bounds__(THREADS, DT <= 2 ? 2 : 1) attention_forward_si
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if (row + i >= s.qext) break;
-    store_row<T, DT>(row_of<T>(a.o, s.tb, s.q0 + row + i, head), acc[i], l[i] == 0.f ? 0.f : 1.f / l[i], a.dim);
+    store_row<T, DT>(row_of<T>(a.o, s.tb, s.q0 + row + i, head), acc[i], 1.f / l[i], l[i] == 0.f, a.dim);
     if (tx == 0) a.lse[(int64_t(s.tb) * a.hq + head) * a.nq + s.q0 + row + i] = l[i] == 0.f ? -INFINITY : m[i] + logf(l[i]);
   }
 }
@@ -359,7 +362,7 @@ __global__ void __launch_bounds__(THREADS, DT == 1 ? 2 : 1) attention_dq_simt_ke
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (row + i < s.qext) store_row<T, DT>(row_of<T>(a.dq, s.tb, s.q0 + row + i, head), acc[i], a.scale, a.dim);
+    if (row + i < s.qext) store_row<T, DT>(row_of<T>(a.dq, s.tb, s.q0 + row + i, head), acc[i], a.scale, hi[i] <= lo[i], a.dim);
 }
 
 template <typename T, int DT>
@@ -380,7 +383,7 @@ __global__ void __launch_bounds__(THREADS, DT == 1 ? 2 : 1) attention_dkv_simt_k
   load_rows<T, DT>(sk, a.k, s.tb, s.k0, kvh, r0, ROWS, s.kn, a.dim);
   load_rows<T, DT>(sv, a.v, s.tb, s.k0, kvh, r0, ROWS, s.kn, a.dim);
   const float c2 = a.scale * kLog2e;
-  const int c1 = min(r0 + ROWS, s.kn);
+  const int c1 = min(r0 + ROWS, s.kn), blind = attn_blind(a, s);
   const int qlo = r0 < s.kn ? attn_query_lo(a, s, r0) : 0, qhi = r0 < s.kn ? attn_query_hi(a, s, c1) : 0;
   float4 dk[4][DT], dv[4][DT];
   clear(dk);
@@ -388,8 +391,8 @@ __global__ void __launch_bounds__(THREADS, DT == 1 ? 2 : 1) attention_dkv_simt_k
   for (int h = kvh * group; h < (kvh + 1) * group; ++h)
     for (int i0 = qlo / COLS * COLS; i0 < qhi; i0 += COLS) {
       __syncthreads();
-      load_rows<T, DT>(sq, a.q, s.tb, s.q0, h, i0, COLS, s.qn, a.dim);
-      load_rows<T, DT>(sdo, a.dout, s.tb, s.q0, h, i0, COLS, s.qn, a.dim);
+      load_rows<T, DT>(sq, a.q, s.tb, s.q0, h, i0, COLS, s.qn, a.dim, blind);
+      load_rows<T, DT>(sdo, a.dout, s.tb, s.q0, h, i0, COLS, s.qn, a.dim, blind);
       __syncthreads();
       float p[4][J], ds[4][J];
       products<DT, J>(p, sk, sq, a.dim);
@@ -418,8 +421,9 @@ __global__ void __launch_bounds__(THREADS, DT == 1 ? 2 : 1) attention_dkv_simt_k
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (key + i < s.kext) {
-      store_row<T, DT>(row_of<T>(a.dk, s.tb, s.k0 + key + i, kvh), dk[i], a.scale, a.dim);
-      store_row<T, DT>(row_of<T>(a.dv, s.tb, s.k0 + key + i, kvh), dv[i], 1.f, a.dim);
+      const bool unseen = key + i >= s.kn || attn_query_hi(a, s, key + i + 1) <= attn_query_lo(a, s, key + i);
+      store_row<T, DT>(row_of<T>(a.dk, s.tb, s.k0 + key + i, kvh), dk[i], a.scale, unseen, a.dim);
+      store_row<T, DT>(row_of<T>(a.dv, s.tb, s.k0 + key + i, kvh), dv[i], 1.f, unseen, a.dim);
     }
 }
 

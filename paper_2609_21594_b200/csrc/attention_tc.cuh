@@ -172,14 +172,19 @@ __device__ __forceinline__ void mma_probs_rows(uint32_t d_tmem, uint32_t p_lo, u
     tc_mma_ts(d_tmem, (k < 4 ? p_lo : p_hi) + uint32_t(k & 3) * 8u, dy + uint32_t(k) * 128u, idesc, accumulate || k > K0);
 }
 
-// Clears the rows of a tile from `first` on (a whole warp) and arrives on `bar`.  Rows past a sequence's end hold another sequence's tokens or padding; they meet
-// probabilities that are zero, but zero times a NaN or an infinity is not zero.
+// Clears the rows of a tile before `from` and those from `to` on (a whole warp) and arrives on `bar`.  Rows past a sequence's end hold another sequence's
+// tokens or padding, and the first queries may see no key; such rows meet probabilities that are zero, but zero times a NaN or an infinity is
+// not zero.
 template <int BOXES>
-__device__ __forceinline__ void clear_rows(uint32_t tile, int first, int lane, uint32_t bar) {
+__device__ __forceinline__ void clear_rows(uint32_t tile, int from, int to, int lane, uint32_t bar) {
+  auto clear = [&](int first, int last) {
 #pragma unroll
-  for (int b = 0; b < BOXES; ++b)
-    for (int i = first * 8 + lane; i < BLK * 8; i += 32)
-      asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + uint32_t(b) * BOX_BYTES + uint32_t(i) * 16u), "r"(0) : "memory");
+    for (int b = 0; b < BOXES; ++b)
+      for (int i = first * 8 + lane; i < last * 8; i += 32)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + uint32_t(b) * BOX_BYTES + uint32_t(i) * 16u), "r"(0) : "memory");
+  };
+  clear(0, from);
+  clear(max(to, 0), BLK);
   fence_async_smem();
   __syncwarp();
   if (lane == 0) mbar_arrive(bar);

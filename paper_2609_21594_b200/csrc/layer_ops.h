@@ -143,6 +143,13 @@ __device__ __forceinline__ int attn_query_hi(const AttnArgs& a, const AttnSeq& s
   return h < 0 ? 0 : h < s.qn ? int(h) : s.qn;
 }
 
+// The first queries of a sequence, which see nothing because it has fewer keys than queries (or none).  They count, so their rows lie inside the
+// tiles that others are read from; whatever they hold has to be cleared there, for a probability of zero times a NaN is a NaN.
+__device__ __forceinline__ int attn_blind(const AttnArgs& a, const AttnSeq& s) {
+  if (s.kn == 0) return s.qn;
+  return a.causal && s.qn > s.kn ? s.qn - s.kn : 0;
+}
+
 // Finds block `t` of the list "ceil(ext / rows) blocks of each sequence" (ext: its queries, or its keys); the whole warp calls it.
 // Returns false past the end of the list.  Batched: the sequences have equal extents and no search is needed.
 __device__ __forceinline__ bool attn_find_block(const AttnArgs& a, int t, int rows, bool keys, int* seq, int* block) {
