@@ -114,18 +114,24 @@ __device__ __forceinline__ uint64_t exp2_approx(uint64_t v) {
 // 2^x on the multiply-add pipe, for a share of the exponentials where two warps of a scheduler form them at the same time and the
 // exponential unit (one warp's instruction in 8 clocks) is what both wait for.  x = n + r with n the nearest integer, which adding
 // 1.5 * 2^23 puts in the low bits; 2^r on [-1/2, 1/2] by the polynomial of degree 4 whose largest relative error is least (2.7e-6 in
-// fp32; fitted by reweighted least squares); n goes to the exponent.  x is at most 127; below -126 the result is 2^-126.
+// fp32; fitted by reweighted least squares); 2^n is made from its exponent and multiplied on.  x is at most 127; below -126 the result is
+// 2^-126.  A NaN stays one: the clamp hands it on, and the product keeps it (n added to the exponent's bits would make it a number).
+__device__ __forceinline__ float clamp_below(float x) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(x), "f"(-126.f));
+  return y;
+}
 __device__ __forceinline__ uint64_t exp2_poly(uint64_t v) {
   const float2 in = both(v);
-  const uint64_t x = two(fmaxf(in.x, -126.f), fmaxf(in.y, -126.f));
+  const uint64_t x = two(clamp_below(in.x), clamp_below(in.y));
   const uint64_t t = add2(x, twice(12582912.f));
   const uint64_t r = fma2(add2(t, twice(-12582912.f)), twice(-1.f), x);
   uint64_t p = fma2(twice(0.009570102207362652f), r, twice(0.05591786280274391f));
   p = fma2(p, r, twice(0.240247443318367f));
   p = fma2(p, r, twice(0.6931217908859253f));
   p = fma2(p, r, twice(0.9999992847442627f));
-  const float2 n = both(t), y = both(p);
-  return two(__int_as_float(__float_as_int(y.x) + (__float_as_int(n.x) << 23)), __int_as_float(__float_as_int(y.y) + (__float_as_int(n.y) << 23)));
+  const float2 n = both(t);
+  return mul2(p, two(__int_as_float(0x3f800000 + (__float_as_int(n.x) << 23)), __int_as_float(0x3f800000 + (__float_as_int(n.y) << 23))));
 }
 
 // The issuing warp runs converged, its warp index taken from lane 0 and every wait followed by a vote, and one elected lane issues: then
