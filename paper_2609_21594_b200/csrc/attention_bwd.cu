@@ -192,15 +192,28 @@ __device__ __forceinline__ uint32_t pack_rest(uint64_t v, uint32_t hi) {
   return pack_bf16(f.x - __uint_as_float(hi << 16), f.y - __uint_as_float(hi & 0xffff0000u));
 }
 
-// P and dS are rounded to bf16 for the products that sum over them: errors of 2^-9 that are independent, so that a sum over n terms has
+// P and dS are rounded to bf16 for the products that sum over them: errors of up to 2^-9 that are independent, so that a sum over n terms has
 // about the relative error of one, as much again as the rounding of the result: sqrt 2 of it together.  With few keys that is wide: at 2 to 40
-// keys up to 1.8 times the rounding of the result, from 128 on 1.46 at the most.  Up to kSplitKeys keys (four times as many packed ones, which
-// several sequences share) both are therefore kept as two bf16 terms, the second in the columns of the scores that the first leaves free, and
-// each of these products is issued twice.  At 32/8 heads of 128 that takes 20.5 us instead of 18.5 for 128 tokens, and 28.7 instead of 24.6 for 256.
-constexpr int kSplitKeys = 128;
+// keys up to 1.8 times the rounding of the result, from 128 on 1.46 at the most.  A sequence of up to kSplitKeys keys (packed: kSplitPackedKeys)
+// therefore keeps both as two bf16 terms, the second in the columns of the scores that the first leaves free, and each of these products is
+// issued twice.  The sequence's own keys decide, not the call's, so that a document's gradients do not depend on what it is packed or padded
+// with.  They do not depend on the mask either: the first queries of a long causal sequence and those of a short window see few keys and
+// get one term.  Price, at 32/8 heads: 128 tokens of heads of 128 20.5 us instead of 18.5, 256 28.7 instead of 24.6; packed heads of 64, 9 documents in
+// 6000 tokens 214 us instead of 205 (four of them have 512 keys at most; 207 to 209 with 128 for the limit), 32 documents in 6000 tokens 203 instead of
+// 178 (189).  512 for packed ones: rows of short documents are what packing is for.
+constexpr int kSplitKeys = 128, kSplitPackedKeys = 512;
+__device__ __forceinline__ bool few_keys(const AttnArgs& a, const AttnSeq& s) { return s.kn <= (a.nseq ? kSplitPackedKeys : kSplitKeys); }
+
+// Runs a role's rounds with one term or with two: loops of their own, for one that decides in every round keeps the registers of both.
+template <bool MIXED, typename F>
+__device__ __forceinline__ void in_terms(bool split, F rounds) {
+  if constexpr (MIXED)
+    if (split) return rounds(Yes());
+  rounds(No());
+}
 
 // ------------------------------------------------------------------ dk, dv
-template <int BOXES, bool SPLIT>
+template <int BOXES, bool MIXED>
 __global__ void __launch_bounds__(THREADS, 1)
 attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnArgs a) {
   using L = Smem<BOXES>;
@@ -224,6 +237,7 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
     blk = rest / a.batch;
   }
   const AttnSeq s = attn_seq(a, si);
+  const bool split = MIXED && few_keys(a, s);
   const int c0 = blk * BLK;
   int i0 = 0, i1 = 0;                            // blocks of queries
   if (c0 < s.kn) {
@@ -324,42 +338,46 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
       await(b.own(1), 0);
       await(b.full1(0), 0);
       elected(ok, [&] { dprobs(0); });
-      for (int n = 0; n < total && ok; ++n) {
-        const bool next = n + 1 < total;
-        if (next) await(b.full0(n + 1), phase0(n + 1));
-        // P comes in two parts, each half of what either warp of a quadrant has: steps 0, 1, 4, 5 and then 2, 3, 6, 7
-        await(b.p_ready(0), uint32_t(n) & 1u);
-        tc_fence_after();                                  // tensor memory written by other threads; tiles need no such fence
-        elected(ok, [&] {                           // dv += P^T do
-          mma_probs_rows<0, 2>(t_dv, t_s, t_s + 64, do_at(n), idesc, n > 0);
-          mma_probs_rows<4, 6>(t_dv, t_s, t_s + 64, do_at(n), idesc, true);
-          if constexpr (SPLIT) {
-            mma_probs_rows<0, 2>(t_dv, t_s + 32, t_s + 96, do_at(n), idesc, true);
-            mma_probs_rows<4, 6>(t_dv, t_s + 32, t_s + 96, do_at(n), idesc, true);
-          }
-        });
-        await(b.p_ready(1), uint32_t(n) & 1u);
-        tc_fence_after();
-        elected(ok, [&] {
-          mma_probs_rows<2, 4>(t_dv, t_s, t_s + 64, do_at(n), idesc, true);
-          mma_probs_rows<6, 8>(t_dv, t_s, t_s + 64, do_at(n), idesc, true);
-          if constexpr (SPLIT) {
-            mma_probs_rows<2, 4>(t_dv, t_s + 32, t_s + 96, do_at(n), idesc, true);
-            mma_probs_rows<6, 8>(t_dv, t_s + 32, t_s + 96, do_at(n), idesc, true);
-          }
-          tc_commit(b.free1(n));                           // dP^T of this block was issued earlier
-          if (next) scores(n + 1);                         // takes the place of P^T, which dv has read by then
-        });
-        if (next) await(b.full1(n + 1), phase1(n + 1));
-        await(b.ds_ready(), uint32_t(n) & 1u);
-        tc_fence_after();
-        elected(ok, [&] {
-          mma_probs_rows(t_dk, t_dp, t_dp + 64, q_at(n), idesc, n > 0);      // dk += dS^T q
-          if constexpr (SPLIT) mma_probs_rows(t_dk, t_dp + 32, t_dp + 96, q_at(n), idesc, true);
-          tc_commit(b.free0(n));
-          if (next) dprobs(n + 1);
-        });
-      }
+      auto rounds = [&](auto two_terms) {
+        constexpr bool SPLIT = decltype(two_terms)::value;
+        for (int n = 0; n < total && ok; ++n) {
+          const bool next = n + 1 < total;
+          if (next) await(b.full0(n + 1), phase0(n + 1));
+          // P comes in two parts, each half of what either warp of a quadrant has: steps 0, 1, 4, 5 and then 2, 3, 6, 7
+          await(b.p_ready(0), uint32_t(n) & 1u);
+          tc_fence_after();                                  // tensor memory written by other threads; tiles need no such fence
+          elected(ok, [&] {                           // dv += P^T do
+            mma_probs_rows<0, 2>(t_dv, t_s, t_s + 64, do_at(n), idesc, n > 0);
+            mma_probs_rows<4, 6>(t_dv, t_s, t_s + 64, do_at(n), idesc, true);
+            if constexpr (SPLIT) {
+              mma_probs_rows<0, 2>(t_dv, t_s + 32, t_s + 96, do_at(n), idesc, true);
+              mma_probs_rows<4, 6>(t_dv, t_s + 32, t_s + 96, do_at(n), idesc, true);
+            }
+          });
+          await(b.p_ready(1), uint32_t(n) & 1u);
+          tc_fence_after();
+          elected(ok, [&] {
+            mma_probs_rows<2, 4>(t_dv, t_s, t_s + 64, do_at(n), idesc, true);
+            mma_probs_rows<6, 8>(t_dv, t_s, t_s + 64, do_at(n), idesc, true);
+            if constexpr (SPLIT) {
+              mma_probs_rows<2, 4>(t_dv, t_s + 32, t_s + 96, do_at(n), idesc, true);
+              mma_probs_rows<6, 8>(t_dv, t_s + 32, t_s + 96, do_at(n), idesc, true);
+            }
+            tc_commit(b.free1(n));                           // dP^T of this block was issued earlier
+            if (next) scores(n + 1);                         // takes the place of P^T, which dv has read by then
+          });
+          if (next) await(b.full1(n + 1), phase1(n + 1));
+          await(b.ds_ready(), uint32_t(n) & 1u);
+          tc_fence_after();
+          elected(ok, [&] {
+            mma_probs_rows(t_dk, t_dp, t_dp + 64, q_at(n), idesc, n > 0);      // dk += dS^T q
+            if constexpr (SPLIT) mma_probs_rows(t_dk, t_dp + 32, t_dp + 96, q_at(n), idesc, true);
+            tc_commit(b.free0(n));
+            if (next) dprobs(n + 1);
+          });
+        }
+      };
+      in_terms<MIXED>(split, rounds);
       elected(true, [&] { finish_issue(b, ok, abort_flag, a.status); });
     }
     __syncwarp();
@@ -374,84 +392,88 @@ attention_dkv_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_cons
     const int qlo = key < s.kn ? (a.causal ? key - off : 0) : 0x7fffffff;
     const int qhi = key < s.kn ? attn_query_hi(a, s, key + 1) : 0;
     bool ok = true;
-    for (int n = 0; n < total; ++n) {
-      const int r0 = (i0 + n % per) * BLK;
-      ok = __all_sync(0xffffffffu, mbar_wait(b.full1(n), phase1(n), abort_flag)) &&               // the row statistics
-           __all_sync(0xffffffffu, mbar_wait(b.s_full(), uint32_t(n) & 1u, abort_flag));
-      if (!ok) break;
-      tc_fence_after();
-      const uint32_t lse = lse_at(n) + uint32_t(half) * 256u, delta = delta_at(n) + uint32_t(half) * 256u;
-      const int first = qlo - r0 - half * 64, last = qhi - r0 - half * 64;
-      auto step = [&](auto with_mask) {
-        constexpr bool MASK = decltype(with_mask)::value;
-        uint64_t p[32];
-        auto hand_over = [&](uint32_t bar) {
-          tc_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar);
-        };
-        {
-          uint32_t x[64];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) tc_ld32(ts + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[i * 32]));
-          tc_wait_ld();
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {                    // 32 of this warp's queries at a time, into its own columns: the other half may still be read
-            uint32_t w[16];
-#pragma unroll
-            for (int i = c * 8; i < c * 8 + 8; ++i) {
-              const Pairs l2 = lds_pairs(lse + uint32_t(i) * 16u);
-              p[2 * i] = exp2_approx(fma2(words(x[4 * i], x[4 * i + 1]), twice(c2), l2.a));
-              p[2 * i + 1] = exp2_share(!MASK && !SPLIT && i % kPolyOf == 0, fma2(words(x[4 * i + 2], x[4 * i + 3]), twice(c2), l2.b));
-              if constexpr (MASK) {
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                  const float2 f = both(p[2 * i + e]);
-                  const int q = 4 * i + 2 * e;
-                  p[2 * i + e] = two(q < first || q >= last ? 0.f : f.x, q + 1 < first || q + 1 >= last ? 0.f : f.y);
-                }
-              }
-              w[2 * i - c * 16] = pack_bf16(p[2 * i]);
-              w[2 * i + 1 - c * 16] = pack_bf16(p[2 * i + 1]);
-            }
-            tc_st16(ts + c * 16, w);
-            if constexpr (SPLIT) {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) w[i] = pack_rest(p[c * 16 + i], w[i]);
-              tc_st16(ts + 32 + c * 16, w);
-            }
-            hand_over(b.p_ready(c));
-          }
-        }
-
-        ok = __all_sync(0xffffffffu, mbar_wait(b.dp_full(), uint32_t(n) & 1u, abort_flag));
-        if (!ok) return;
+    auto rounds = [&](auto two_terms) {
+      constexpr bool SPLIT = decltype(two_terms)::value;
+      for (int n = 0; n < total; ++n) {
+        const int r0 = (i0 + n % per) * BLK;
+        ok = __all_sync(0xffffffffu, mbar_wait(b.full1(n), phase1(n), abort_flag)) &&               // the row statistics
+             __all_sync(0xffffffffu, mbar_wait(b.s_full(), uint32_t(n) & 1u, abort_flag));
+        if (!ok) break;
         tc_fence_after();
-        uint32_t x[64], w[32];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) tc_ld32(tp + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[i * 32]));
-        tc_wait_ld();
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const Pairs d = lds_pairs(delta + uint32_t(i) * 16u);
-          p[2 * i] = ds_pair<MASK>(p[2 * i], words(x[4 * i], x[4 * i + 1]), d.a);
-          p[2 * i + 1] = ds_pair<MASK>(p[2 * i + 1], words(x[4 * i + 2], x[4 * i + 3]), d.b);
-          w[2 * i] = pack_bf16(p[2 * i]);
-          w[2 * i + 1] = pack_bf16(p[2 * i + 1]);
-        }
-        tc_st32(tp, w);
-        if constexpr (SPLIT) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) w[i] = pack_rest(p[i], w[i]);
-          tc_st32(tp + 32, w);
-        }
-        hand_over(b.ds_ready());
-      };
-      if (block_masked(a, s, r0, c0) || r0 + BLK > s.qn || c0 + BLK > s.kn) step(Yes());
-      else step(No());
-      if (!ok) break;
-    }
+        const uint32_t lse = lse_at(n) + uint32_t(half) * 256u, delta = delta_at(n) + uint32_t(half) * 256u;
+        const int first = qlo - r0 - half * 64, last = qhi - r0 - half * 64;
+        auto step = [&](auto with_mask) {
+          constexpr bool MASK = decltype(with_mask)::value;
+          uint64_t p[32];
+          auto hand_over = [&](uint32_t bar) {
+            tc_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
+          };
+          {
+            uint32_t x[64];
+  #pragma unroll
+            for (int i = 0; i < 2; ++i) tc_ld32(ts + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[i * 32]));
+            tc_wait_ld();
+  #pragma unroll
+            for (int c = 0; c < 2; ++c) {                    // 32 of this warp's queries at a time, into its own columns: the other half may still be read
+              uint32_t w[16];
+  #pragma unroll
+              for (int i = c * 8; i < c * 8 + 8; ++i) {
+                const Pairs l2 = lds_pairs(lse + uint32_t(i) * 16u);
+                p[2 * i] = exp2_approx(fma2(words(x[4 * i], x[4 * i + 1]), twice(c2), l2.a));
+                p[2 * i + 1] = exp2_share(!MASK && !SPLIT && i % kPolyOf == 0, fma2(words(x[4 * i + 2], x[4 * i + 3]), twice(c2), l2.b));
+                if constexpr (MASK) {
+  #pragma unroll
+                  for (int e = 0; e < 2; ++e) {
+                    const float2 f = both(p[2 * i + e]);
+                    const int q = 4 * i + 2 * e;
+                    p[2 * i + e] = two(q < first || q >= last ? 0.f : f.x, q + 1 < first || q + 1 >= last ? 0.f : f.y);
+                  }
+                }
+                w[2 * i - c * 16] = pack_bf16(p[2 * i]);
+                w[2 * i + 1 - c * 16] = pack_bf16(p[2 * i + 1]);
+              }
+              tc_st16(ts + c * 16, w);
+              if constexpr (SPLIT) {
+  #pragma unroll
+                for (int i = 0; i < 16; ++i) w[i] = pack_rest(p[c * 16 + i], w[i]);
+                tc_st16(ts + 32 + c * 16, w);
+              }
+              hand_over(b.p_ready(c));
+            }
+          }
+
+          ok = __all_sync(0xffffffffu, mbar_wait(b.dp_full(), uint32_t(n) & 1u, abort_flag));
+          if (!ok) return;
+          tc_fence_after();
+          uint32_t x[64], w[32];
+  #pragma unroll
+          for (int i = 0; i < 2; ++i) tc_ld32(tp + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[i * 32]));
+          tc_wait_ld();
+  #pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const Pairs d = lds_pairs(delta + uint32_t(i) * 16u);
+            p[2 * i] = ds_pair<MASK>(p[2 * i], words(x[4 * i], x[4 * i + 1]), d.a);
+            p[2 * i + 1] = ds_pair<MASK>(p[2 * i + 1], words(x[4 * i + 2], x[4 * i + 3]), d.b);
+            w[2 * i] = pack_bf16(p[2 * i]);
+            w[2 * i + 1] = pack_bf16(p[2 * i + 1]);
+          }
+          tc_st32(tp, w);
+          if constexpr (SPLIT) {
+  #pragma unroll
+            for (int i = 0; i < 32; ++i) w[i] = pack_rest(p[i], w[i]);
+            tc_st32(tp + 32, w);
+          }
+          hand_over(b.ds_ready());
+        };
+        if (block_masked(a, s, r0, c0) || r0 + BLK > s.qn || c0 + BLK > s.kn) step(Yes());
+        else step(No());
+        if (!ok) break;
+      }
+    };
+    in_terms<MIXED>(split, rounds);
     if (ok && total > 0) {
       ok = __all_sync(0xffffffffu, mbar_wait(b.all_done(), 0, abort_flag));
       tc_fence_after();
@@ -477,7 +499,7 @@ __device__ __forceinline__ void stay() {
   if (blockIdx.x == gridDim.x - 1) cudaGridDependencySynchronize();
 }
 
-template <int BOXES, bool SPLIT>
+template <int BOXES, bool MIXED>
 __global__ void __launch_bounds__(THREADS, 1)
 attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnArgs a) {
   using L = Smem<BOXES>;
@@ -507,6 +529,7 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
     blk = per - 1 - rest / a.batch;
   }
   const AttnSeq s = attn_seq(a, si);
+  const bool split = MIXED && few_keys(a, s);
   const int r0 = blk * BLK;
   const BlockRange rg = key_blocks(a, s, r0);
   const int total = rg.n1 - rg.n0;
@@ -566,22 +589,26 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
       await(b.own(1), 0);
       await(b.full1(0), 0);
       elected(ok, [&] { dprobs(0); });
-      for (int n = 0; n < total && ok; ++n) {
-        const bool next = n + 1 < total;
-        if (next) {
-          await(b.full0(n + 1), phase0(n + 1));
-          elected(ok, [&] { scores(n + 1); });            // its place was read before dS of block n - 1 was ready
-          await(b.full1(n + 1), phase1(n + 1));
+      auto rounds = [&](auto two_terms) {
+        constexpr bool SPLIT = decltype(two_terms)::value;
+        for (int n = 0; n < total && ok; ++n) {
+          const bool next = n + 1 < total;
+          if (next) {
+            await(b.full0(n + 1), phase0(n + 1));
+            elected(ok, [&] { scores(n + 1); });            // its place was read before dS of block n - 1 was ready
+            await(b.full1(n + 1), phase1(n + 1));
+          }
+          await(b.ds_ready(), uint32_t(n) & 1u);
+          tc_fence_after();                                  // tensor memory written by other threads; tiles need no such fence
+          elected(ok, [&] {
+            mma_probs_rows(t_dq, t_dp, t_dp + 64, k_at(n), idesc, n > 0);      // dq += dS k
+            if constexpr (SPLIT) mma_probs_rows(t_dq, t_dp + 32, t_dp + 96, k_at(n), idesc, true);
+            tc_commit(b.free0(n));
+            if (next) dprobs(n + 1);
+          });
         }
-        await(b.ds_ready(), uint32_t(n) & 1u);
-        tc_fence_after();                                  // tensor memory written by other threads; tiles need no such fence
-        elected(ok, [&] {
-          mma_probs_rows(t_dq, t_dp, t_dp + 64, k_at(n), idesc, n > 0);      // dq += dS k
-          if constexpr (SPLIT) mma_probs_rows(t_dq, t_dp + 32, t_dp + 96, k_at(n), idesc, true);
-          tc_commit(b.free0(n));
-          if (next) dprobs(n + 1);
-        });
-      }
+      };
+      in_terms<MIXED>(split, rounds);
       elected(true, [&] { finish_issue(b, ok, abort_flag, a.status); });
     }
     __syncwarp();
@@ -597,56 +624,60 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
                         quad * 32 + lane;
     const float l2 = info[0], delta = info[kAttnRowBlock];
     bool ok = true;
-    for (int n = 0; n < total; ++n) {
-      const int c0 = (rg.n0 + n) * BLK;
-      ok = __all_sync(0xffffffffu, mbar_wait(b.s_full(n & 1), uint32_t(n >> 1) & 1u, abort_flag));
-      if (!ok) break;
-      tc_fence_after();
-      const int first = lo - c0 - half * 64, last = hi - c0 - half * 64;
-      auto step = [&](auto with_mask) {
-        constexpr bool MASK = decltype(with_mask)::value;
-        uint64_t p[32];
-        {
-          uint32_t x[64];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) tc_ld32(t_s(n) + lanes + uint32_t(half) * 64u + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[i * 32]));
-          tc_wait_ld();
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            p[i] = exp2_share(!MASK && !SPLIT && i % (2 * kPolyOf) == 1, fma2(words(x[2 * i], x[2 * i + 1]), twice(c2), twice(l2)));
-            if constexpr (MASK) {
-              const float2 f = both(p[i]);
-              p[i] = two(2 * i < first || 2 * i >= last ? 0.f : f.x, 2 * i + 1 < first || 2 * i + 1 >= last ? 0.f : f.y);
+    auto rounds = [&](auto two_terms) {
+      constexpr bool SPLIT = decltype(two_terms)::value;
+      for (int n = 0; n < total; ++n) {
+        const int c0 = (rg.n0 + n) * BLK;
+        ok = __all_sync(0xffffffffu, mbar_wait(b.s_full(n & 1), uint32_t(n >> 1) & 1u, abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        const int first = lo - c0 - half * 64, last = hi - c0 - half * 64;
+        auto step = [&](auto with_mask) {
+          constexpr bool MASK = decltype(with_mask)::value;
+          uint64_t p[32];
+          {
+            uint32_t x[64];
+  #pragma unroll
+            for (int i = 0; i < 2; ++i) tc_ld32(t_s(n) + lanes + uint32_t(half) * 64u + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[i * 32]));
+            tc_wait_ld();
+  #pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              p[i] = exp2_share(!MASK && !SPLIT && i % (2 * kPolyOf) == 1, fma2(words(x[2 * i], x[2 * i + 1]), twice(c2), twice(l2)));
+              if constexpr (MASK) {
+                const float2 f = both(p[i]);
+                p[i] = two(2 * i < first || 2 * i >= last ? 0.f : f.x, 2 * i + 1 < first || 2 * i + 1 >= last ? 0.f : f.y);
+              }
             }
           }
-        }
-        ok = __all_sync(0xffffffffu, mbar_wait(b.dp_full(), uint32_t(n) & 1u, abort_flag));
-        if (!ok) return;
-        tc_fence_after();
-        uint32_t x[64], w[32];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) tc_ld32(tp + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[i * 32]));
-        tc_wait_ld();
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          p[i] = ds_pair<MASK>(p[i], words(x[2 * i], x[2 * i + 1]), twice(delta));
-          w[i] = pack_bf16(p[i]);
-        }
-        tc_st32(tp, w);
-        if constexpr (SPLIT) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) w[i] = pack_rest(p[i], w[i]);
-          tc_st32(tp + 32, w);
-        }
-        tc_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(b.ds_ready());
-      };
-      if (block_masked(a, s, r0, c0) || r0 + BLK > s.qn) step(Yes());
-      else step(No());
-      if (!ok) break;
-    }
+          ok = __all_sync(0xffffffffu, mbar_wait(b.dp_full(), uint32_t(n) & 1u, abort_flag));
+          if (!ok) return;
+          tc_fence_after();
+          uint32_t x[64], w[32];
+  #pragma unroll
+          for (int i = 0; i < 2; ++i) tc_ld32(tp + i * 32, *reinterpret_cast<uint32_t(*)[32]>(&x[i * 32]));
+          tc_wait_ld();
+  #pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            p[i] = ds_pair<MASK>(p[i], words(x[2 * i], x[2 * i + 1]), twice(delta));
+            w[i] = pack_bf16(p[i]);
+          }
+          tc_st32(tp, w);
+          if constexpr (SPLIT) {
+  #pragma unroll
+            for (int i = 0; i < 32; ++i) w[i] = pack_rest(p[i], w[i]);
+            tc_st32(tp + 32, w);
+          }
+          tc_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(b.ds_ready());
+        };
+        if (block_masked(a, s, r0, c0) || r0 + BLK > s.qn) step(Yes());
+        else step(No());
+        if (!ok) break;
+      }
+    };
+    in_terms<MIXED>(split, rounds);
     if (ok && total > 0) {
       ok = __all_sync(0xffffffffu, mbar_wait(b.all_done(), 0, abort_flag));
       tc_fence_after();
@@ -665,13 +696,13 @@ attention_dq_tc_kernel(const __grid_constant__ AttnMaps maps, const __grid_const
   tear_down(warp, tmem);
 }
 
-template <int BOXES, bool SPLIT>
+template <int BOXES, bool MIXED>
 int run(const AttnMaps& m, const AttnArgs& a, cudaStream_t st) {
   const int64_t kb = attn_max_blocks(a, BLK, true) * a.hkv, qb = attn_max_blocks(a, BLK, false) * a.hq;
   if (kb > 0x7fffffff || qb > 0x7fffffff) return MUON_ERR_UNSUPPORTED;
   constexpr uint32_t bytes = Smem<BOXES>::bytes;
   static SharedMemoryLimit limit;
-  if (!limit.raise(a.device, bytes, attention_dkv_tc_kernel<BOXES, SPLIT>, attention_dq_tc_kernel<BOXES, SPLIT>)) return MUON_ERR_CUDA;
+  if (!limit.raise(a.device, bytes, attention_dkv_tc_kernel<BOXES, MIXED>, attention_dq_tc_kernel<BOXES, MIXED>)) return MUON_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(THREADS);
   cfg.dynamicSmemBytes = bytes;
@@ -682,9 +713,9 @@ int run(const AttnMaps& m, const AttnArgs& a, cudaStream_t st) {
   cfg.attrs = &at;
   cfg.numAttrs = 1;
   cfg.gridDim = dim3(unsigned(kb));
-  if (cudaLaunchKernelEx(&cfg, attention_dkv_tc_kernel<BOXES, SPLIT>, m, a) != cudaSuccess) return MUON_ERR_CUDA;
+  if (cudaLaunchKernelEx(&cfg, attention_dkv_tc_kernel<BOXES, MIXED>, m, a) != cudaSuccess) return MUON_ERR_CUDA;
   cfg.gridDim = dim3(unsigned(qb));
-  return cudaLaunchKernelEx(&cfg, attention_dq_tc_kernel<BOXES, SPLIT>, m, a) == cudaSuccess ? 2 : MUON_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, attention_dq_tc_kernel<BOXES, MIXED>, m, a) == cudaSuccess ? 2 : MUON_ERR_CUDA;
 }
 
 }  // namespace
@@ -704,7 +735,7 @@ int launch_attention_backward_tc(muon_ctx* ctx, const AttnArgs& a, cudaStream_t 
       !encode_tile_map(ctx->tmap_encode, &m.dout, a.dout, a.dim, a.batch, a.nq, a.hq))
     return MUON_ERR_CUDA;
   ctx->tmap_encodes += 4;
-  if (a.nk <= (a.nseq ? 4 : 1) * kSplitKeys) return a.dim <= 64 ? run<1, true>(m, a, st) : run<2, true>(m, a, st);
+  if (a.nseq || a.k_lens || a.nk <= kSplitKeys) return a.dim <= 64 ? run<1, true>(m, a, st) : run<2, true>(m, a, st);
   return a.dim <= 64 ? run<1, false>(m, a, st) : run<2, false>(m, a, st);
 }
 
