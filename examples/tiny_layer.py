@@ -87,6 +87,7 @@ def train(steps: int, seed: int = 0, report: int = 0):
         losses.append(loss.detach())
         if report and (step + 1) % report == 0:
             print(f"step {step + 1:4d}  loss {float(losses[-1]):.3f}", flush=True)
+    F.synchronize_and_check()                            # no bounded wait has expired, in the backward passes' thread either
     return torch.stack(losses).tolist()
 
 

@@ -510,6 +510,12 @@ int muon_last_device_status(muon_ctx_t* ctx, void* stream, int32_t* status);
 /* Resets the status word to 0 (stream-ordered). */
 int muon_clear_device_status(muon_ctx_t* ctx, void* stream);
 
+/* The device address of the status word that this context's calls record into, and the word of other calls to come: contexts of
+ * one device that share a word answer for one another in the calls above and below, so a thread can check work that another thread
+ * launched with a context of its own.  `word`: an int32 on the context's device that outlives its calls, or NULL: its own word again. */
+int muon_device_status_word(const muon_ctx_t* ctx, int32_t** word);
+int muon_share_device_status(muon_ctx_t* ctx, int32_t* word);
+
 /* Opt-in synchronous check: synchronises `stream`, then returns MUON_OK when no bounded wait has expired on this
  * context and MUON_ERR_DEVICE_TIMEOUT when one has (the results of the affected call are then incomplete).
  * The step entry points themselves never synchronise and therefore never return that code: a caller that wants

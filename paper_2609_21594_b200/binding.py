@@ -135,6 +135,8 @@ _sig = {
     "muon_attention_backward": (C.c_int, [_vp] * 12 + [C.c_size_t, _vp]),
     "muon_last_device_status": (C.c_int, [_vp, _vp, C.POINTER(C.c_int32)]),
     "muon_clear_device_status": (C.c_int, [_vp, _vp]),
+    "muon_device_status_word": (C.c_int, [_vp, C.POINTER(_vp)]),
+    "muon_share_device_status": (C.c_int, [_vp, _vp]),
     "muon_synchronize_and_check": (C.c_int, [_vp, _vp]),
     "muon_tensor_map_encodes": (C.c_int64, [_vp]),
     "muon_self_test_bounded_wait": (C.c_int, [_vp, _vp]),
@@ -529,6 +531,16 @@ class Context:
 
     def muon_clear_device_status(self, stream=None) -> None:
         _check(lib.muon_clear_device_status(self.handle, _stream(stream)), "muon_clear_device_status")
+
+    def muon_device_status_word(self) -> int:
+        """Device address of the word that this context's calls record an expired wait in."""
+        v = _vp()
+        _check(lib.muon_device_status_word(self.handle, C.byref(v)), "muon_device_status_word")
+        return v.value
+
+    def muon_share_device_status(self, word: Optional[int]) -> None:
+        """Records into the word of another context of the device from now on (None: its own again)."""
+        _check(lib.muon_share_device_status(self.handle, word), "muon_share_device_status")
 
     def muon_synchronize_and_check(self, stream=None) -> int:
         """Returns OK or ERR_DEVICE_TIMEOUT (does not raise for the latter: it is the answer, not a failure of the call)."""

@@ -218,7 +218,7 @@ int run_set_products(muon_ctx* ctx, const SetRun& sr, const ChunkRun& r, cudaStr
         L.status = ctx->d_status;
         L.persist = sr.tables->persist;
         L.ns_steps = r.ns_steps;
-        L.barrier = reinterpret_cast<uint32_t*>(ctx->d_status + 16);
+        L.barrier = reinterpret_cast<uint32_t*>(ctx->d_own + 16);
         L.barrier_base = ctx->barrier_count;
         for (int k = 0; k < r.ns_steps; ++k)
           for (int j = 0; j < 3; ++j) L.coef[k][j] = r.coeffs[(ctx->opt.coeffs_per_step ? 3 * k : 0) + j];
@@ -565,10 +565,11 @@ int muon_create(muon_ctx_t** out, const muon_options_t* opt) {
   if (!ctx) return MUON_ERR_CUDA;
   ctx->opt = o;
   ctx->device = dev;
-  if (cudaMalloc(&ctx->d_status, 256) != cudaSuccess || cudaMemset(ctx->d_status, 0, 256) != cudaSuccess) {
+  if (cudaMalloc(&ctx->d_own, 256) != cudaSuccess || cudaMemset(ctx->d_own, 0, 256) != cudaSuccess) {
     delete ctx;
     return MUON_ERR_CUDA;
   }
+  ctx->d_status = ctx->d_own;
   cudaDriverEntryPointQueryResult qres;
   void* fn = nullptr;
   if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) == cudaSuccess &&
@@ -595,7 +596,7 @@ void muon_destroy(muon_ctx_t* ctx) {
   for (cudaEvent_t e : ctx->sync_events) cudaEventDestroy(e);
   if (ctx->h2d_stream) cudaStreamDestroy(ctx->h2d_stream);
   if (ctx->d2h_stream) cudaStreamDestroy(ctx->d2h_stream);
-  if (ctx->d_status) cudaFree(ctx->d_status);
+  if (ctx->d_own) cudaFree(ctx->d_own);
   delete ctx;
 }
 
@@ -1092,6 +1093,18 @@ int muon_clear_device_status(muon_ctx_t* ctx, void* stream) {
   if (!ctx) return MUON_ERR_INVALID_ARG;
   return cudaMemsetAsync(ctx->d_status, 0, sizeof(int32_t), static_cast<cudaStream_t>(stream)) == cudaSuccess ? MUON_OK
                                                                                                                : MUON_ERR_CUDA;
+}
+
+int muon_device_status_word(const muon_ctx_t* ctx, int32_t** word) {
+  if (!ctx || !word) return MUON_ERR_INVALID_ARG;
+  *word = ctx->d_status;
+  return MUON_OK;
+}
+
+int muon_share_device_status(muon_ctx_t* ctx, int32_t* word) {
+  if (!ctx || (reinterpret_cast<uintptr_t>(word) & 3u)) return MUON_ERR_INVALID_ARG;
+  ctx->d_status = word ? word : ctx->d_own;
+  return MUON_OK;
 }
 
 int muon_synchronize_and_check(muon_ctx_t* ctx, void* stream) {

@@ -2,7 +2,7 @@
 // no arithmetic.  It stands in C++ because a small call's time is the host's: the same checks in Python cost 14 to 18 us per call, of which
 // the device needed 5.
 //
-// Every host thread has a context of its own per device (autograd calls backward passes from another thread).
+// Every host thread has a context of its own per device (autograd calls backward passes from another thread); they share one status word.
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <pybind11/numpy.h>
@@ -31,6 +31,7 @@ struct Contexts {
   struct Pool {
     std::mutex lock;
     std::vector<std::pair<int, muon_ctx_t*>> free;
+    std::vector<int32_t*> word;                // per device: the status word that all its contexts share
   };
   static Pool& pool() {
     static Pool* p = new Pool;
@@ -47,6 +48,13 @@ struct Contexts {
         return c;
       }
     return nullptr;
+  }
+  // A bounded wait that expires is seen from every thread: autograd's backward passes run in threads that nobody can ask.
+  static int share(int index, muon_ctx_t* c) {
+    std::lock_guard<std::mutex> hold(pool().lock);
+    std::vector<int32_t*>& word = pool().word;
+    if (index >= int(word.size())) word.resize(size_t(index) + 1, nullptr);
+    return word[size_t(index)] ? muon_share_device_status(c, word[size_t(index)]) : muon_device_status_word(c, &word[size_t(index)]);
   }
   ~Contexts() {
     std::lock_guard<std::mutex> hold(pool().lock);
@@ -73,6 +81,7 @@ muon_ctx_t* context(int index) {
     muon_options_t opt;
     muon_default_options(&opt);
     check(muon_create(&c, &opt), "muon_create");
+    check(Contexts::share(index, c), "muon_share_device_status");
   }
   return c;
 }

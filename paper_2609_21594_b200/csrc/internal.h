@@ -133,7 +133,8 @@ struct muon_ctx {
   int device = 0;
   void* ws = nullptr;
   size_t ws_bytes = 0;
-  int32_t* d_status = nullptr;                     // device status word of the bounded waits
+  int32_t* d_status = nullptr;                     // device status word of the bounded waits: its own, or one that several contexts share
+  int32_t* d_own = nullptr;                        // 256 bytes: the context's own status word, and the grid barrier's counter at [16]
   muon::StagingSlot slots[4];
   int next_slot = 0;
   std::unordered_map<std::string, muon::Plan> plans;
@@ -144,7 +145,7 @@ struct muon_ctx {
   int64_t phase_launches[MUON_NUM_PHASES] = {0, 0, 0, 0, 0};
   int64_t launches = 0;
   int64_t tmap_encodes = 0;                        // tensor maps encoded so far (plan binding and the per-launch engines)
-  uint32_t barrier_count = 0;                      // arrivals the grid-barrier counter (d_status[16]) has seen so far
+  uint32_t barrier_count = 0;                      // arrivals the grid-barrier counter (d_own[16]) has seen so far
   int persist_pairs = -1;                          // CTA pairs a whole-iteration launch may use (-1: not asked yet, 0: off)
   void* tmap_encode = nullptr;                     // cuTensorMapEncodeTiled, resolved at run time
   cudaStream_t h2d_stream = nullptr, d2h_stream = nullptr;   // copy streams of the host-buffer path (created on first use)

@@ -3,7 +3,8 @@
 What a training program needs around the matrices that `optim.Muon` updates.  The `*_forward` / `*_backward` pairs are defined in
 `csrc/front.cpp` (argument checks and marshalling, built as `_front`) and their arithmetic runs in the CUDA library, on the current
 stream of the tensors' device.  `layer_norm`, `rotary` and `attention` are differentiable; the pairs are the same calls for programs that
-keep their own tape.  Each host thread has a context of its own per device (autograd calls backward passes from another thread).
+keep their own tape.  Each host thread has a context of its own per device (autograd calls backward passes from another thread); all
+of a device's record an expired wait in one word, which `synchronize_and_check` reads.
 """
 from __future__ import annotations
 
@@ -38,6 +39,18 @@ class _ThreadContext(mb.Context):
 def context(device: Optional[torch.device] = None) -> mb.Context:
     """This thread's context of a device (default: the current one): the one the functions of this module use there."""
     return _ThreadContext(_front.context(torch.cuda.current_device() if device is None or device.index is None else device.index))
+
+
+def synchronize_and_check(device: Optional[torch.device] = None) -> None:
+    """Synchronises the device (default: the current one) and raises MuonError (ERR_DEVICE_TIMEOUT) when a bounded wait of a call of this module
+    has expired there, from whatever thread: that call's results are incomplete.  The word stays set until
+    `context(device).muon_clear_device_status()`."""
+    index = torch.cuda.current_device() if device is None or device.index is None else device.index
+    torch.cuda.synchronize(index)
+    with torch.cuda.device(index):
+        code = context(torch.device("cuda", index)).muon_synchronize_and_check()
+    if code != mb.OK:
+        raise mb.MuonError(code, "muon_synchronize_and_check")
 
 
 def _heads(t: torch.Tensor) -> mb.Heads:
