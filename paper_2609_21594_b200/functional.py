@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes as C
 from typing import Optional, Sequence, Tuple
 
+import numpy as np
 import torch
 
 from . import binding as mb  # first: it loads the library that _front is linked with
@@ -84,19 +85,22 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
 class _Rotary(torch.autograd.Function):
     @staticmethod
     def forward(ctx, inv_freq, layout, amplitude, positions, offset, *tensors):
-        ctx.args = (inv_freq, layout, amplitude, positions, offset)
+        inv_freq = np.array(inv_freq, dtype=np.float64)      # a copy: the caller may change its own before the backward pass
+        ctx.save_for_backward(positions)                     # watched: autograd refuses a backward pass after they were written
+        ctx.args = (inv_freq, layout, amplitude, offset)
         return rotary_forward(tensors, inv_freq, layout, amplitude, positions, offset)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, *grads):
-        inv_freq, layout, amplitude, positions, offset = ctx.args
+        inv_freq, layout, amplitude, offset = ctx.args
+        positions, = ctx.saved_tensors
         return (None,) * 5 + rotary_forward(grads, inv_freq, layout, amplitude, positions, offset, inverse=True)
 
 
 def rotary(tensors: Sequence[torch.Tensor], inv_freq, layout: str = "half", amplitude: float = 1.0,
            positions: Optional[torch.Tensor] = None, offset: int = 0) -> Tuple[torch.Tensor, ...]:
-    """Differentiable `rotary_forward`."""
+    """Differentiable `rotary_forward`.  The backward pass turns by the same angles: positions written in between are an error, inv_freq is copied."""
     return _Rotary.apply(inv_freq, layout, amplitude, positions, offset, *tensors)
 
 
