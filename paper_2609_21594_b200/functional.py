@@ -85,7 +85,7 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
 class _Rotary(torch.autograd.Function):
     @staticmethod
     def forward(ctx, inv_freq, layout, amplitude, positions, offset, *tensors):
-        inv_freq = np.array(inv_freq, dtype=np.float64)      # a copy: the caller may change its own before the backward pass
+        inv_freq = np.asarray(inv_freq, dtype=np.float64).copy()      # the caller may change its own before the backward pass
         ctx.save_for_backward(positions)                     # watched: autograd refuses a backward pass after they were written
         ctx.args = (inv_freq, layout, amplitude, offset)
         return rotary_forward(tensors, inv_freq, layout, amplitude, positions, offset)
