@@ -241,6 +241,7 @@ std::vector<Tensor> rotary(const std::vector<Tensor>& tensors, const Frequencies
       const Tensor& o = (*out)[i];
       if (!o.sizes().equals(t.sizes()) || o.scalar_type() != t.scalar_type() || o.device() != t.device()) bad("out must match the tensors");
       if (o.stride(-1) != 1 && o.size(-1) > 1) bad("out must have a contiguous last dimension");
+      if (o.requires_grad() && at::GradMode::is_enabled()) bad("out requires grad, and what is written there is not recorded: use rotary, or no_grad");
       result.push_back(o);
     } else {
       result.push_back(new_like(t));
@@ -269,6 +270,9 @@ std::vector<Tensor> rotary(const std::vector<Tensor>& tensors, const Frequencies
   d.positions = static_cast<const int32_t*>(address(positions));
   d.position_offset = offset;
   check(muon_rotary(context(index), &d, items, int32_t(tensors.size()), stream_of(index)), "muon_rotary");
+  if (out)                                             // what another operation saved of them is not there any more: autograd must know
+    for (const Tensor& o : result)
+      if (!o.is_inference()) o.unsafeGetTensorImpl()->bump_version();
   return result;
 }
 
@@ -410,7 +414,7 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
       "inv_freq: host, fp64 radians per position of each pair (see `rotary_frequencies`); twice its length is the part of the head that is\n"
       "turned, the rest is copied.  layout: \"half\" (i with i + n/2) or \"interleaved\" (2i with 2i + 1).  positions: int32 [batch, tokens] on\n"
       "the device, else offset + 0, 1, 2...; offset is added to given positions too.  inverse turns back, which is the backward pass.\n"
-      "out: tensors to write, which may be the inputs themselves.");
+      "out: tensors to write, which may be the inputs themselves; written in place for autograd too, so none may require grad while it records.");
   m.def("attention_forward", &attention_forward, release(), py::arg("q"), py::arg("k"), py::arg("v"), py::arg("causal") = true, py::arg("window") = 0,
         py::arg("scale") = none, py::arg("q_lens") = none, py::arg("k_lens") = none, py::arg("q_offsets") = none, py::arg("k_offsets") = none,
         "(o, lse).  q: [batch, tokens, heads, dim]; k, v: [batch, tokens, kv heads, dim], heads a multiple of kv heads; any strides with a\n"
