@@ -420,11 +420,19 @@ int muon_layer_norm_backward(muon_ctx_t* ctx, const muon_norm_desc_t* desc, cons
                              void* dbias, void* workspace, size_t workspace_bytes, void* stream);
 
 /* A [batch, tokens, heads, head_dim] tensor of any strides (in elements) whose last dimension is contiguous: a view into a
- * fused projection's output, or a tensor stored head by head.  The tensors a call reads are not written. */
+ * fused projection's output, or a tensor stored head by head.  The tensors a call reads are not written.  A result must not share an element with
+ * an input or another result (MUON_ERR_INVALID_ARG, before any launch), except exactly where a call says that it works in place; tensors
+ * may interleave. */
 typedef struct {
   void*   data;
   int64_t batch_stride, token_stride, head_stride;
 } muon_heads_t;
+
+/* Host arithmetic only (needs no device): *overlap = 1 when tensors a and b, of shapes {batch, tokens, heads, head_dim}, share a byte, and with
+ * b = NULL when two elements of a share a place.  What the calls below refuse results by; exact for layouts whose strides nest, and
+ * for others unless it would take a million steps (then 1). */
+int muon_heads_overlap(const muon_heads_t* a, const int32_t* a_shape, const muon_heads_t* b, const int32_t* b_shape, int32_t elem_size,
+                       int32_t* overlap);
 
 /* Rotary positions: pair i of the first rotary_dim elements of every head is turned by the angle position * inv_freq[i]
  * (by its negative when inverse = 1, which is the backward pass) and multiplied by amplitude; the rest of the head is copied.

@@ -128,6 +128,7 @@ _sig = {
     "muon_layer_norm_forward": (C.c_int, [_vp, _vp, _vp, C.c_int64, _vp, _vp, _vp, C.c_int64, _vp, _vp, _vp]),
     "muon_layer_norm_workspace_bytes": (C.c_int, [_vp, C.POINTER(C.c_size_t)]),
     "muon_layer_norm_backward": (C.c_int, [_vp, _vp, _vp, C.c_int64, _vp, C.c_int64, _vp, _vp, _vp, _vp, C.c_int64, _vp, _vp, _vp, C.c_size_t, _vp]),
+    "muon_heads_overlap": (C.c_int, [_vp, _vp, _vp, _vp, C.c_int32, C.POINTER(C.c_int32)]),
     "muon_rotary": (C.c_int, [_vp, _vp, _vp, C.c_int32, _vp]),
     "muon_rotary_frequencies": (C.c_int, [C.c_double, C.c_int32, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double, _vp]),
     "muon_attention_forward": (C.c_int, [_vp] * 8),
@@ -302,6 +303,14 @@ def muon_attention_workspace_bytes(desc) -> int:
     out = C.c_size_t(0)
     _check(lib.muon_attention_workspace_bytes(_at(desc), C.byref(out)), "muon_attention_workspace_bytes")
     return out.value
+
+
+def muon_heads_overlap(a: Heads, a_shape: Sequence[int], b: Optional[Heads], b_shape: Sequence[int], elem_size: int) -> bool:
+    """Do two strided [batch, tokens, heads, dim] tensors share a byte?  With b = None: do two elements of a share a place?"""
+    out, shape = C.c_int32(0), C.c_int32 * 4
+    _check(lib.muon_heads_overlap(C.byref(a), shape(*a_shape), None if b is None else C.byref(b), None if b is None else shape(*b_shape), elem_size,
+                                  C.byref(out)), "muon_heads_overlap")
+    return bool(out.value)
 
 
 def muon_rotary_frequencies(base: float, rotary_dim: int, scaling: int = ROTARY_PLAIN, factor: float = 1.0, original_length: float = 0.0,

@@ -1,6 +1,8 @@
 // extern "C" entry points of the layer operators: argument validation and the choice of kernels.
 #include <cmath>
+#include <initializer_list>
 
+#include "boxes.h"
 #include "layer_ops.h"
 
 using namespace muon;
@@ -53,9 +55,31 @@ bool good_heads(const muon_heads_t* t, size_t elem) {
   return t && t->data && aligned_to(t->data, elem) && t->batch_stride >= 0 && t->token_stride >= 0 && t->head_stride >= 0;
 }
 
-// Two elements of a result must not share a place: a dimension longer than one has a stride.
+// A result has a stride in every dimension longer than one; box_meets_itself looks at whether its elements share a place.
 bool good_output(const muon_heads_t* t, size_t elem, int64_t batch, int64_t tokens, int64_t heads) {
   return good_heads(t, elem) && (batch <= 1 || t->batch_stride > 0) && (tokens <= 1 || t->token_stride > 0) && (heads <= 1 || t->head_stride > 0);
+}
+
+Box box_of(const muon_heads_t* t, size_t elem, int64_t batch, int64_t tokens, int64_t heads, int64_t dim) {
+  const int64_t e = int64_t(elem);
+  return {reinterpret_cast<uintptr_t>(t->data), {batch, tokens, heads, dim * e}, {t->batch_stride * e, t->token_stride * e, t->head_stride * e}};
+}
+Box rows_of(const void* p, int64_t rows, int64_t cols, int64_t ld, size_t elem) {
+  const int64_t e = int64_t(elem);
+  return {reinterpret_cast<uintptr_t>(p), {1, 1, rows, cols * e}, {0, 0, ld * e}};
+}
+
+// Whether a result lies over an input or over another result.  The first result may be one of `in_place` exactly.
+bool results_clash(std::initializer_list<Box> results, std::initializer_list<Box> inputs, std::initializer_list<Box> in_place = {}) {
+  for (const Box* r = results.begin(); r != results.end(); ++r) {
+    for (const Box& in : inputs)
+      if (boxes_meet(*r, in)) return true;
+    for (const Box& in : in_place)
+      if (!(r == results.begin() && same_box(*r, in)) && boxes_meet(*r, in)) return true;
+    for (const Box* other = results.begin(); other != r; ++other)
+      if (boxes_meet(*r, *other)) return true;
+  }
+  return false;
 }
 
 int check_attention(const muon_attention_desc_t* d) {
@@ -114,6 +138,10 @@ int muon_layer_norm_forward(muon_ctx_t* ctx, const muon_norm_desc_t* desc, const
   if (!aligned_to(x, e) || !aligned_to(y, e) || !aligned_to(weight, pe) || !aligned_to(bias, pe) || !aligned_to(mean, 4) || !aligned_to(rstd, 4))
     return MUON_ERR_INVALID_ARG;
   if (y == x && ldy != ldx) return MUON_ERR_INVALID_ARG;
+  const int64_t rows = desc->rows, cols = desc->cols, params = cols * int64_t(pe);
+  if (results_clash({rows_of(y, rows, cols, ldy, e), run_of(mean, rows * 4), run_of(rstd, rows * 4)}, {run_of(weight, params), run_of(bias, params)},
+                    {rows_of(x, rows, cols, ldx, e)}))
+    return MUON_ERR_INVALID_ARG;
   int sms = 0;
   if ((rc = device_of(ctx, &sms)) != MUON_OK) return rc;
   NormArgs a = norm_args(desc);
@@ -159,6 +187,11 @@ int muon_layer_norm_backward(muon_ctx_t* ctx, const muon_norm_desc_t* desc, cons
     if (!workspace || workspace_bytes < need) return MUON_ERR_WORKSPACE_TOO_SMALL;
     if (!aligned_to(workspace, 256)) return MUON_ERR_INVALID_ARG;
   }
+  const int64_t rows = desc->rows, cols = desc->cols, params = cols * int64_t(pe);
+  if (results_clash({rows_of(dx, rows, cols, lddx, e), run_of(dweight, params), run_of(dbias, params), run_of(sums ? workspace : nullptr, int64_t(need))},
+                    {run_of(weight, params), run_of(mean, rows * 4), run_of(rstd, rows * 4)},
+                    {rows_of(dy, rows, cols, lddy, e), rows_of(x, rows, cols, ldx, e)}))
+    return MUON_ERR_INVALID_ARG;
   int sms = 0;
   if ((rc = device_of(ctx, &sms)) != MUON_OK) return rc;
   NormArgs a = norm_args(desc);
@@ -177,6 +210,15 @@ int muon_layer_norm_backward(muon_ctx_t* ctx, const muon_norm_desc_t* desc, cons
   a.dbias = dbias;
   a.parts = sums && need > 0 ? static_cast<float*>(workspace) : nullptr;
   return launched(ctx, launch_norm_backward(a, sms, static_cast<cudaStream_t>(stream)));
+}
+
+int muon_heads_overlap(const muon_heads_t* a, const int32_t* a_shape, const muon_heads_t* b, const int32_t* b_shape, int32_t elem_size, int32_t* overlap) {
+  if (!a || !a_shape || (b && !b_shape) || elem_size < 1 || !overlap) return MUON_ERR_INVALID_ARG;
+  for (const muon_heads_t* t : {a, b})
+    if (t && (t->batch_stride < 0 || t->token_stride < 0 || t->head_stride < 0)) return MUON_ERR_INVALID_ARG;
+  const Box box = box_of(a, size_t(elem_size), a_shape[0], a_shape[1], a_shape[2], a_shape[3]);
+  *overlap = b ? boxes_meet(box, box_of(b, size_t(elem_size), b_shape[0], b_shape[1], b_shape[2], b_shape[3])) : box_meets_itself(box);
+  return MUON_OK;
 }
 
 int muon_rotary(muon_ctx_t* ctx, const muon_rotary_desc_t* desc, const muon_rotary_item_t* items, int32_t count, void* stream) {
@@ -202,6 +244,16 @@ int muon_rotary(muon_ctx_t* ctx, const muon_rotary_desc_t* desc, const muon_rota
   }
   if (int64_t(a.head_begin[count]) * desc->head_dim > (int64_t(1) << 24)) return MUON_ERR_UNSUPPORTED;   // items of a block fit 32 bits
   if (int64_t(desc->batch) * desc->tokens == 0 || a.head_begin[count] == 0) return MUON_OK;
+  auto box = [&](const muon_heads_t& t, int k) { return box_of(&t, e, desc->batch, desc->tokens, items[k].heads, desc->head_dim); };
+  for (int k = 0; k < count; ++k) {                  // a tensor may be turned in place, but not over another one
+    const Box out = box(items[k].out, k);
+    if (box_meets_itself(out)) return MUON_ERR_INVALID_ARG;
+    for (int j = 0; j < count; ++j) {
+      const Box in = box(items[j].in, j);
+      if (!(j == k && same_box(out, in)) && boxes_meet(out, in)) return MUON_ERR_INVALID_ARG;
+      if (j < k && boxes_meet(out, box(items[j].out, j))) return MUON_ERR_INVALID_ARG;
+    }
+  }
   a.count = count;
   a.dtype = desc->dtype;
   a.interleaved = desc->interleaved;
@@ -250,6 +302,9 @@ int muon_attention_forward(muon_ctx_t* ctx, const muon_attention_desc_t* desc, c
   if (!good_heads(q, e) || !good_output(o, e, desc->batch, desc->q_tokens, desc->q_heads) || !lse || !aligned_to(lse, 4)) return MUON_ERR_INVALID_ARG;
   if (!k || !v || (nk > 0 && (!good_heads(k, e) || !good_heads(v, e)))) return MUON_ERR_INVALID_ARG;
   if (o->data == q->data || o->data == k->data || o->data == v->data) return MUON_ERR_INVALID_ARG;
+  const Box bq = box_of(q, e, desc->batch, desc->q_tokens, desc->q_heads, desc->head_dim), bo = box_of(o, e, desc->batch, desc->q_tokens, desc->q_heads, desc->head_dim);
+  const Box bk = box_of(k, e, desc->batch, desc->k_tokens, desc->kv_heads, desc->head_dim), bv = box_of(v, e, desc->batch, desc->k_tokens, desc->kv_heads, desc->head_dim);
+  if (box_meets_itself(bo) || results_clash({bo, run_of(lse, nq * desc->q_heads * 4)}, {bq, bk, bv})) return MUON_ERR_INVALID_ARG;
   int sms = 0;
   if ((rc = device_of(ctx, &sms)) != MUON_OK) return rc;
   AttnArgs a = attention_args(ctx, desc);
@@ -304,6 +359,12 @@ int muon_attention_backward(muon_ctx_t* ctx, const muon_attention_desc_t* desc, 
     if (!workspace || workspace_bytes < need) return MUON_ERR_WORKSPACE_TOO_SMALL;
     if (!aligned_to(workspace, 256)) return MUON_ERR_INVALID_ARG;
   }
+  auto queries = [&](const muon_heads_t* t) { return box_of(t, e, desc->batch, desc->q_tokens, desc->q_heads, desc->head_dim); };
+  auto keys = [&](const muon_heads_t* t) { return box_of(t, e, desc->batch, desc->k_tokens, desc->kv_heads, desc->head_dim); };
+  if (box_meets_itself(queries(dq)) || box_meets_itself(keys(dk)) || box_meets_itself(keys(dv)) ||
+      results_clash({queries(dq), keys(dk), keys(dv), run_of(workspace, int64_t(need))},
+                    {queries(dout), queries(q), keys(k), keys(v), queries(o), run_of(lse, nq * desc->q_heads * 4)}))
+    return MUON_ERR_INVALID_ARG;
   int sms = 0;
   if ((rc = device_of(ctx, &sms)) != MUON_OK) return rc;
   a.q = attn_tensor(q);
