@@ -15,7 +15,12 @@ import numpy as np
 import torch
 
 from . import binding as mb  # first: it loads the library that _front is linked with
-from . import _front
+
+try:
+    from . import _front
+except ImportError as e:
+    raise ImportError("the torch front end of the layer operators (_front.so) is missing or does not fit this torch: build it with "
+                      "`python -m paper_2609_21594_b200.build`, which needs a C++ compiler and the headers of Python and torch") from e
 from ._front import attention_backward, attention_forward, layer_norm_backward, layer_norm_forward, rotary_forward  # noqa: F401
 from .binding import muon_rotary_frequencies as rotary_frequencies  # noqa: F401  (part of this module's interface)
 
