@@ -5,6 +5,7 @@ What a training program needs around the matrices that `optim.Muon` updates.  Th
 stream of the tensors' device.  `layer_norm`, `rotary` and `attention` are differentiable; the pairs are the same calls for programs that
 keep their own tape.  Each host thread has a context of its own per device (autograd calls backward passes from another thread); all
 of a device's record an expired wait in one word, which `synchronize_and_check` reads.
+A thread's first call on a device makes its context, which allocates: calls are captured into a graph after one ordinary call.
 """
 from __future__ import annotations
 
