@@ -12,14 +12,14 @@ struct Box {
   uintptr_t base;
   int64_t n[4];
   int64_t s[3];
-  bool empty() const { return !base || n[0] <= 0 || n[1] <= 0 || n[2] <= 0 || n[3] <= 0; }
-  __int128 span() const {              // bytes from the first to one past the last
-    __int128 r = n[3];
-    for (int k = 0; k < 3; ++k) r += __int128(s[k]) * (n[k] - 1);
-    return r;
+  __int128 end;                        // one past the last byte; the base where there is none, so that an empty box meets nothing
+  Box(const void* p, int64_t n0, int64_t n1, int64_t n2, int64_t bytes, int64_t s0, int64_t s1, int64_t s2)
+      : base(reinterpret_cast<uintptr_t>(p)), n{n0, n1, n2, bytes}, s{s0, s1, s2}, end(base) {
+    if (p && n0 > 0 && n1 > 0 && n2 > 0 && bytes > 0) end += bytes + __int128(s0) * (n0 - 1) + __int128(s1) * (n1 - 1) + __int128(s2) * (n2 - 1);
   }
+  bool empty() const { return end == __int128(base); }
 };
-inline Box run_of(const void* p, int64_t bytes) { return {reinterpret_cast<uintptr_t>(p), {1, 1, 1, bytes}, {0, 0, 0}}; }
+inline Box run_of(const void* p, int64_t bytes) { return Box(p, 1, 1, 1, bytes, 0, 0, 0); }
 
 // Whether sum stride_k d_k = delta has a solution with lo_k <= d_k <= hi_k.  Largest stride first: what the smaller ones can still reach leaves one or
 // two values to try where the strides nest, as those of tensors do.
@@ -75,9 +75,8 @@ inline bool same_box(const Box& a, const Box& b) {
 }
 
 inline bool boxes_meet(const Box& a, const Box& b) {
-  if (a.empty() || b.empty()) return false;
+  if (a.end <= __int128(b.base) || b.end <= __int128(a.base) || a.empty() || b.empty()) return false;
   const __int128 delta = __int128(b.base) - __int128(a.base);
-  if (delta >= a.span() || -delta >= b.span()) return false;
   StrideSum sum;                       // place in a minus place in b
   for (int k = 0; k < 4; ++k) {
     sum.add(k < 3 ? a.s[k] : 1, 0, a.n[k] - 1);

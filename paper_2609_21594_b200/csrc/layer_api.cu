@@ -62,11 +62,11 @@ bool good_output(const muon_heads_t* t, size_t elem, int64_t batch, int64_t toke
 
 Box box_of(const muon_heads_t* t, size_t elem, int64_t batch, int64_t tokens, int64_t heads, int64_t dim) {
   const int64_t e = int64_t(elem);
-  return {reinterpret_cast<uintptr_t>(t->data), {batch, tokens, heads, dim * e}, {t->batch_stride * e, t->token_stride * e, t->head_stride * e}};
+  return Box(t->data, batch, tokens, heads, dim * e, t->batch_stride * e, t->token_stride * e, t->head_stride * e);
 }
 Box rows_of(const void* p, int64_t rows, int64_t cols, int64_t ld, size_t elem) {
   const int64_t e = int64_t(elem);
-  return {reinterpret_cast<uintptr_t>(p), {1, 1, rows, cols * e}, {0, 0, ld * e}};
+  return Box(p, 1, 1, rows, cols * e, 0, 0, ld * e);
 }
 
 // Whether a result lies over an input or over another result.  The first result may be one of `in_place` exactly.
