@@ -389,7 +389,9 @@ int muon_orthogonalize_static(const void* in, void* out, int32_t rows, int32_t c
  * consumes: layer norm, rotary positions and attention, each forward and backward.  These calls use a context only for
  * its device, its status word and its launch count; they neither use nor need the workspace of muon_set_workspace, and
  * the scratch some of them take is an argument (256-byte aligned, caller-owned, contents undefined before and after).
- * Every result is bit-identical from run to run: no float atomics.  Statistics, sums and accumulators are fp32. */
+ * Every result is bit-identical from run to run: no float atomics.  Statistics, sums and accumulators are fp32; results are rounded once to
+ * their type.  Attention in bf16 on the tensor cores rounds P, and in the backward pass dS, to bf16 for the products that sum over them; the
+ * backward pass keeps both as two bf16 terms where a sequence has up to 128 keys (packed: 512). */
 
 /* Layer norm over the last dimension of `rows` rows of `cols` elements (1 <= cols <= 16384), in `dtype`; weight, bias and
  * their gradients have `param_dtype`.

@@ -502,8 +502,8 @@ class Context:
                                    alpha, beta, None if gamma is None else gamma.data_ptr(), gamma_mode,
                                    _stream(stream)), "muon_ns_product")
 
-    # -- layer operators.  Device pointers are ints (None for NULL); a descriptor or tensor is its ctypes structure or the int address of
-    # memory laid out like it, which `functional` packs without building objects (a call's host time is most of a small one's).
+    # -- layer operators, for programs that call the C ABI themselves (`functional` goes through csrc/front.cpp).  Device pointers are ints (None for
+    # NULL); a descriptor or tensor is its ctypes structure or the int address of memory laid out like it.
     def muon_layer_norm_forward(self, desc, x, ldx, weight, bias, y, ldy, mean, rstd, stream=None) -> None:
         rc = _norm_forward(self.handle, _at(desc), x, ldx, weight, bias, y, ldy, mean, rstd, _stream(stream))
         if rc:

@@ -11,17 +11,18 @@
 //
 // Seven products of 128 x 128 x head_dim per pair of tiles instead of the five that a single kernel needs: that would add every
 // block's share of dq (or of dk and dv) with float atomics, whose order changes from run to run, or keep fp32 partial sums as large as
-// the number of blocks; here every sum has one owner and a fixed order.
+// the number of blocks, or let the blocks that share a sum wait for one another in a fixed order; here every sum has one owner.
 //
 // 352 threads: eight warps compute (two per lane quadrant, half of the 128 columns each), one loads, one issues, one clears the rows of a
 // streamed tile that lie past the sequence's end.  The issuer alternates: while the warps turn S into P it multiplies with the dS before,
 // while they turn dP into dS it forms the next S.
 //
-// Measured, causal, 32/8 heads of 128: 4096 tokens 431 us, 798 TFLOP/s of the five products that the gradient needs (1117 of the seven issued,
-// 67 % of the library's matrix product alone), 8192 tokens 1.6 ms; 4 x 2048 tokens of heads of 64 363 us.  A round takes 2700 clocks in the dk, dv
+// Measured, causal, 32/8 heads of 128: 4096 tokens 421 to 457 us over several runs, 750 to 816 TFLOP/s of the five products that the gradient needs
+// (1050 to 1142 of the seven issued, 63 to 68 % of the library's matrix product alone), 8192 tokens 1.6 ms; 4 x 2048 tokens of heads of 64 349 to
+// 363 us.  A round takes 2700 clocks in the dk, dv
 // kernel (its products alone 2048) and 1985 in the dq kernel (1536): the rest is the handing over of P and dS, each a few hundred clocks during
 // which the tensor pipe has only the other product left.  Short and packed sequences (a few rounds per block) pay 1.3 us to start a block and 2
-// to 4 us for its results: 9 documents in 6000 tokens, heads of 64: 205 us.
+// to 4 us for its results: 9 documents in 6000 tokens, heads of 64: 214 us.
 #include <cuda_bf16.h>
 
 #include "attention_tc.cuh"
@@ -56,8 +57,9 @@ struct Bars {
   __device__ __forceinline__ uint32_t p_ready(int part = 0) const { return at(5 + part); }
   __device__ __forceinline__ uint32_t ds_ready() const { return at(7); }
   __device__ __forceinline__ uint32_t all_done() const { return at(8); }
-  // Round n's tile of the stream has been read: its place may be loaded again.  Two barriers in turn: round n + 2 cannot get there before
-  // the loader, past round n, has brought what it needs, so neither completes twice unseen.
+  // Round n's tile of the stream has been read: its place may be loaded again.  Two barriers in turn, and neither completes twice unseen: stream 1's
+  // is committed in round n + 2 behind tile n + 2, which the loader brings after it has seen round n's; stream 0's behind tile n + 3, which
+  // round n + 2 awaits first and the loader brings after it has seen round n's (the last rounds await no tile, and there the loader none of theirs).
   __device__ __forceinline__ uint32_t free0(int n) const { return at(9 + (n & 1)); }
   __device__ __forceinline__ uint32_t free1(int n) const { return at(11 + 2 * (PLACES0 + PLACES1) + (n & 1)); }
   __device__ __forceinline__ uint32_t full0(int n) const { return at(11 + n % PLACES0); }
@@ -166,7 +168,8 @@ __device__ __forceinline__ void store_half(const AttnTensor& t, int tb, int toke
   }
 }
 
-// One pair of exponentials in 2 * kPolyOf on the multiply-add pipe: 1 to 2.5 % faster than none.  `poly` is known at compile time.
+// One pair of exponentials in 2 * kPolyOf on the multiply-add pipe: 1 to 2.5 % faster than none.  `poly` is known at compile time.  Only tiles without
+// a mask and sequences with one term take it: its 2.7e-6 is a seven-hundredth of the rounding of P that follows there.
 constexpr int kPolyOf = 2;
 __device__ __forceinline__ uint64_t exp2_share(bool poly, uint64_t v) { return poly ? exp2_poly(v) : exp2_approx(v); }
 

@@ -8,15 +8,17 @@
 //   warp 9          MMA issuer:  O_t += P_t v with P_t read from tensor memory, then S_t = q_t k^T of the next keys (128 x 128 x head_dim), for
 //                   the tiles in turn.  (An issuer per tile lets the tiles' products mix, and each softmax waits for both: 519 against 507 us, below.)
 //   warp 10         clears the rows of the last v tile that lie past the sequence's end
-// Tensor memory: S_0, S_1 (128 columns each), O_0, O_1.  P_t takes the place of S_t, rounded once to bf16.  While one tile's softmax runs,
+// Tensor memory: S_0, S_1 (128 columns each), O_0, O_1.  P_t takes the place of S_t, rounded once to bf16, the type of the product's
+// operands: up to 2^-9 of each term, independently, so that o is off by about sqrt 2 of its own rounding.  The sum l takes P unrounded.  While one tile's softmax runs,
 // the issuer works for the other.  A tcgen05.commit covers everything issued before it, so "S_t of block j is ready" also says that the
 // product that read P_t of block j - 1 is done and O_t may be touched.
 //
 // The running maximum is raised only when a row's scores exceed it by more than 2^8 in the exponential: until then P is at most 256 and
 // the sum is exact enough in fp32 (P's rounding is relative), and O, which sits in tensor memory, is not read and rewritten.
 //
-// Measured, causal, 32/8 heads of 128: 8192 tokens 507 us, 1084 TFLOP/s of the pairs that count (65 % of the library's matrix product alone);
-// 4 x 2048 tokens of heads of 64: 136 us, 502 TFLOP/s.  A round of one tile is a chain: softmax, about 1800 clocks, then O += P v and the next S,
+// Measured, causal, 32/8 heads of 128: 8192 tokens 507 to 522 us over several runs, 1053 to 1084 TFLOP/s of the pairs that count (63 to 65 % of the
+// library's matrix product alone); 4 x 2048 tokens of heads of 64: 136 us, 502 TFLOP/s; a window of 1024 keys, 8192 tokens: 173 us, 747 TFLOP/s;
+// 9 and 32 documents in 6000 tokens, heads of 64: 86 us, 260 and 126 TFLOP/s.  A round of one tile is a chain: softmax, about 1800 clocks, then O += P v and the next S,
 // about 1150; two tiles share the tensor pipe, which is busy for 2200 of every 2980 clocks.  So the softmax bounds it, by issue slots: a share
 // of the exponentials on the multiply-add pipe made it slower (570 to 600 us), as did two threads per row (539 to 580).  Heads of 64
 // do half the products per exponential and come to half the rate.

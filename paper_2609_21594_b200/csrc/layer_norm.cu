@@ -9,13 +9,13 @@
 //
 // Forward: a row belongs to 32 to 512 threads with at most four pieces each (32 values of bf16: more would leave too few warps to hide
 // the chain of two sums).  The row groups of a block do not wait for one another; weight and bias lie in shared memory as fp32.
-// 8192 x 4096 bf16, fp32 weight and bias: 26.7 us, 5.0 TB/s (a copy of the same size takes 24.8); 3001 x 5633 fp32 (element by element):
-// 34.3 us, 3.9 TB/s; 3000 x 12288 fp32: 64 us, 4.6 TB/s.
+// 8192 x 4096 bf16, fp32 weight and bias: 26.7 to 28.7 us over several runs, 4.7 to 5.0 TB/s (a copy of the same size takes 24.8); 3001 x 5633 fp32
+// (element by element): 34.3 us, 3.9 TB/s; 3000 x 12288 fp32: 64 us, 4.6 TB/s.
 //
 // Backward: a thread keeps its 16 columns for all its rows, so it adds dy xh and dy in registers.  Rows wider than 8192 columns are
 // cut between the two blocks of a cluster, which exchange their sums through distributed shared memory.  The blocks' sums,
 // [blocks][2][cols] fp32, are added in block order by a second kernel: no atomics, the same bits every time.
-// 8192 x 4096 bf16: 48.6 us, 4.1 TB/s (an addition of two tensors of that size takes 32.9), about 4 us of it for the blocks' sums; the rest is
+// 8192 x 4096 bf16: 48.6 to 49.5 us, 4.1 TB/s (an addition of two tensors of that size takes 32.9), about 4 us of it for the blocks' sums; the rest is
 // the stream of two inputs, which neither fewer sums, more stages (3 to 6), one row at a time nor other block counts (46.4 us at best, in
 // no launch shape that also holds for other sizes) changed by more than 5 %.  2048 x 14336 bf16: 61 us; 30000 x 300 fp32: 25 us.
 #include <cooperative_groups.h>
@@ -564,9 +564,11 @@ int forward_by_cols(const NormArgs& a, int sms, cudaStream_t st) {
   return forward<T, N, 512, 32>(a, sms, st);
 }
 
-// Few narrow rows: one cluster of eight blocks and one launch, no scratch.  128 x 256 fp32: 4.8 us on the device against 4.5 us of the two
-// launches, whose second launch and workspace cost the host 3.8 us more of a call that the host bounds (8.2 us now); at 512 x 512
-// already 9.2 against 5.3 us on the device.
+// Few narrow rows: one cluster of eight blocks and one launch, no scratch.  Up to 128 rows that is faster on the device and in a call, from 192 on the device
+// takes longer and from 256 to 512 the call does too.  Joined against two launches, device (replayed in a graph) and call, us:
+//   fp32, 256 columns:  8 rows 4.1 - 4.6, 6.7 - 9.6;  128: 4.6 - 4.9, 6.7 - 9.3;  192: 5.2 - 4.9, 8.2 - 9.5;  512: 8.4 - 5.4, 10.3 - 9.3
+//   fp32, 512 columns:  8 rows 4.5 - 4.9, 6.7 - 9.6;  128: 5.2 - 5.2, 8.2 - 9.7;  192: 6.2 - 5.2, 8.2 - 10.1; 512: 9.0 - 5.5, 11.4 - 9.6
+//   bf16, 512 columns:  8 rows 5.2 - 5.4, 7.1 - 9.7;  128: 5.9 - 6.4, 8.2 - 9.4;  192: 7.4 - 6.4, 10.2 - 9.4; 512: 10.6 - 6.5, 12.9 - 9.6
 constexpr int64_t kJoinRows = 128;
 bool joins(int64_t rows, int cols) { return cols <= 32 * BWD_EPT && rows > 0 && rows <= kJoinRows; }
 
@@ -584,7 +586,7 @@ int backward_by_cols(const NormArgs& a, int sms, cudaStream_t st) {
 bool pieces(const void* p, int64_t ld, int bytes) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (ld * bytes) % 16 == 0; }
 
 // 16-byte accesses need 16-byte aligned rows that are a whole number of them; other rows go element by element.  8192 rows of bf16:
-// 4096 columns 26.7 us by pieces, 4095 columns 47.5 us by elements; 3001 rows of fp32: 5632 columns 30.2, 5633 columns 36.4 us.
+// 4096 columns 26.7 to 28.7 us by pieces, 4095 columns 47.5 to 51.5 by elements; 3001 rows of fp32: 5632 columns 30.2 to 31.2, 5633 columns 36.4.
 bool vector_rows(const NormArgs& a) {
   const int e = a.dtype == MUON_DTYPE_BF16 ? 2 : 4;
   return (a.cols * e) % 16 == 0 && pieces(a.x, a.ldx, e) && pieces(a.out, a.ldo, e) && (!a.dy || pieces(a.dy, a.lddy, e));

@@ -8,8 +8,9 @@
 // by position * 2^-24 radians, 0.06 at a million.
 //   out_i = c x_i - s x_j,  out_j = s x_i + c x_j,  (c, s) = amplitude (cos, sin)(position * inv_freq)
 //
-// 8192 tokens of 40 heads of 128 in bf16: 32.8 us, 5.1 TB/s (an addition that moves 201 MB reaches 6.1, a copy of 134 MB 5.4); 3063 tokens of 40
-// heads of 64 in fp32, interleaved: 14.8 us on the device, 4.2 TB/s; a single token: 8.8 us, all of it the host's.
+// 8192 tokens of 40 heads of 128 in bf16: 32.8 to 33.1 us, 5.1 TB/s (an addition that moves 201 MB reaches 6.1, a copy of 134 MB 5.4); 3063 tokens of 40
+// heads of 64 in fp32, interleaved: 14.8 us on the device, 4.2 TB/s; a single token: 8.2 to 8.8 us, all of it the host's.  Single elements (a number of
+// pairs that 8 in bf16, 4 in fp32 does not divide): 1.0 to 2.5 TB/s.
 #include <cuda_bf16.h>
 
 #include <type_traits>
@@ -88,8 +89,12 @@ __device__ __forceinline__ void turn(Single<T>& x, Single<T>& y, const float* c,
   down(&y.v, f * *s + g * *c);
 }
 
-// Tokens of a unit.  8192 tokens of 40 heads of 128 in bf16: 32.8 us with two (and five blocks per SM), 38.9 with four (and four blocks);
-// 3063 tokens of 40 heads of 64 in fp32, interleaved: 18.4 us with two, 15.8 with four.
+// Tokens of a unit.  With two and with four, us:
+//   bf16 by pieces (five blocks per SM): 8192 tokens of 40 heads of 128 33.1 - 41.4 (interleaved 33.6 - 39.3), 8192 of 40 heads of 64 19.7 - 24.4, 32768 of
+//   2 heads of 64 27.0 - 42.3
+//   fp32 by pieces (four blocks): 3063 tokens of 40 heads of 64, half of it interleaved 18.6 - 16.6, all of it in halves 14.6 - 16.6; 8192 of 40 heads of
+//   128 59.0 - 59.8
+//   single elements: bf16, 8192 tokens of 40 heads of 72 75.8 - 65.2, of 80 (half of it) 116 - 101; fp32, of 70 81.2 - 74.4
 template <int N> constexpr int kTokens = N == 8 ? 2 : 4;
 
 // A work item is N pairs of one head (2 N elements in two pieces), or, past the rotary part, N elements to copy.

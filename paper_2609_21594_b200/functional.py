@@ -61,7 +61,7 @@ def synchronize_and_check(device: Optional[torch.device] = None) -> None:
 
 
 def _heads(t: torch.Tensor) -> mb.Heads:
-    """The descriptor of a 4-D tensor as an object, for calls of the binding."""
+    """The descriptor of a 4-D tensor as an object, for calls of the binding's Context."""
     s = t.stride()
     return mb.Heads(t.data_ptr(), s[0], s[1], s[2])
 
