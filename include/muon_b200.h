@@ -512,6 +512,83 @@ int muon_attention_backward(muon_ctx_t* ctx, const muon_attention_desc_t* desc, 
                             const muon_heads_t* dq, const muon_heads_t* dk, const muon_heads_t* dv, void* workspace,
                             size_t workspace_bytes, void* stream);
 
+/* A matrix of rows: ld elements (at least its columns) from one row to the next. */
+typedef struct {
+  void*   data;
+  int64_t ld;
+} muon_rows_t;
+
+/* A matrix in 8 bits: e4m3 codes and, for every block of block_rows x 128 elements (ragged at the ends), a byte e for the scale 2^(e - 127); an
+ * element stands for its code times its block's scale.  muon_quantize takes the least scale (from 2^-127 on) that brings the largest finite
+ * magnitude of the block to at most 448, the largest code, so that the one thing it rounds is the code itself: to the nearest, ties to even.
+ * A NaN or an infinity is kept as NaN and has no share in the scale; a block of zeros has e = 0.  A scale's byte of 255 stands for NaN. */
+typedef struct {
+  void*    codes;                /* [rows][ld], one byte each */
+  int64_t  ld;
+  uint8_t* scales;               /* [ceil(rows / block_rows)][lds] */
+  int64_t  lds;                  /* at least ceil(cols / 128) */
+  int32_t  block_rows;           /* 1 (activations) or 128 (weights) */
+  int32_t  reserved;             /* must be 0 */
+} muon_blocks_t;
+
+/* x [rows][cols] of `dtype` into 8 bits, and back (rounded once to `dtype`).  What lies behind the columns of a row is neither read nor written. */
+int muon_quantize(muon_ctx_t* ctx, int32_t dtype, int64_t rows, int64_t cols, const muon_rows_t* x, const muon_blocks_t* out, void* stream);
+int muon_dequantize(muon_ctx_t* ctx, int32_t dtype, int64_t rows, int64_t cols, const muon_blocks_t* in, const muon_rows_t* y, void* stream);
+
+/* Gated feed-forward block on `tokens` rows of x:
+ *   g = x w_gate^T,  u = x w_up^T,  h = act(g) u,  y = h w_down^T          w_gate, w_up: [hidden][dim];  w_down: [dim][hidden]
+ * act(g) = g s(w(g)) with the logistic function s:  SILU  w = g;  GELU  w = 2 sqrt(2 / pi) (g + 0.044715 g^3)  (the tanh form).
+ * Sums are fp32; h is formed from the sums and rounded once to dtype.  What the backward pass needs of g and u is kept
+ *   KEEP_NONE  not at all (inference)
+ *   KEEP_FULL  in dtype
+ *   KEEP_8BIT  in 8 bits with block_rows = 1, and x with them: (dim + 2 hidden) bytes a token and their scales; g and u are rounded from the fp32 sums */
+#define MUON_ACTIVATION_SILU 0
+#define MUON_ACTIVATION_GELU 1
+#define MUON_KEEP_NONE 0
+#define MUON_KEEP_FULL 1
+#define MUON_KEEP_8BIT 2
+typedef struct {
+  int32_t dtype;                 /* of all tensors.  MUON_DTYPE_BF16: tensor cores when every pointer is 16-byte aligned, every ld is a multiple */
+                                 /* of 8 and so are dim and hidden; otherwise, and for MUON_DTYPE_FP32, CUDA cores                             */
+  int32_t activation, keep;
+  int32_t tokens, dim, hidden;
+} muon_feed_forward_desc_t;
+
+/* What the forward pass kept: gate and up with KEEP_FULL, the others with KEEP_8BIT.  Fields that do not apply are not looked at. */
+typedef struct {
+  muon_rows_t   gate, up;        /* [tokens][hidden] */
+  muon_blocks_t x8, gate8, up8;  /* [tokens][dim], [tokens][hidden] twice */
+} muon_feed_forward_kept_t;
+
+/* Bytes of scratch, 256-byte aligned, of the forward (backward = 0) or backward (1) call.  Host arithmetic only. */
+int muon_feed_forward_workspace_bytes(const muon_feed_forward_desc_t* desc, int32_t backward, size_t* bytes);
+
+int muon_feed_forward_forward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* desc, const muon_rows_t* x, const muon_rows_t* w_gate, const muon_rows_t* w_up,
+                              const muon_rows_t* w_down, const muon_rows_t* y, const muon_feed_forward_kept_t* kept, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* From what was kept (x itself with KEEP_FULL, where x8 holds it otherwise and x is NULL):  dh = dy w_down,  dg = dh u act'(g),  du = dh act(g),
+ *   dx = dg w_gate + du w_up,  dw_gate = dg^T x,  dw_up = du^T x,  dw_down = dy^T (act(g) u)
+ * dh stays fp32; dg, du and act(g) u are rounded once to dtype.  Results that are NULL are not formed.  With no tokens dw_* are zeros. */
+int muon_feed_forward_backward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* desc, const muon_rows_t* dy, const muon_rows_t* x, const muon_rows_t* w_gate,
+                               const muon_rows_t* w_up, const muon_rows_t* w_down, const muon_feed_forward_kept_t* kept, const muon_rows_t* dx,
+                               const muon_rows_t* dw_gate, const muon_rows_t* dw_up, const muon_rows_t* dw_down, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/* Linear layer whose products are formed in 8 bits:  y = Q(x) w8^T with w8 [out][dim] in blocks of 128 x 128 and Q(x) in blocks of 1 x 128, which the call
+ * writes to x8: what was multiplied is what the backward pass keeps.  x, y: bf16; sums are fp32. */
+typedef struct {
+  int32_t tokens, dim, out;
+  int32_t reserved;              /* must be 0 */
+} muon_linear_blocks_desc_t;
+int muon_linear_blocks_forward(muon_ctx_t* ctx, const muon_linear_blocks_desc_t* desc, const muon_rows_t* x, const muon_blocks_t* w8, const muon_rows_t* y,
+                             const muon_blocks_t* x8, void* stream);
+
+/* dx = Q(dy) w8 with Q(dy) in blocks of 1 x 128, and dw = dy^T x8 with dy as it is (bf16).  dx or dw may be NULL. */
+int muon_linear_blocks_workspace_bytes(const muon_linear_blocks_desc_t* desc, size_t* bytes);
+int muon_linear_blocks_backward(muon_ctx_t* ctx, const muon_linear_blocks_desc_t* desc, const muon_rows_t* dy, const muon_blocks_t* x8, const muon_blocks_t* w8,
+                              const muon_rows_t* dx, const muon_rows_t* dw, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Device-side status word: the tensor-core pipeline bounds every wait on a barrier; a wait
  * that gives up records a non-zero code here and the kernel exits cleanly.  Reads the word
  * after synchronising `stream`; 0 = no bounded wait ever expired on this context. */

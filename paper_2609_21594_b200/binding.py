@@ -30,6 +30,8 @@ ENGINE_TENSOR, ENGINE_CUDA_CORE, ENGINE_TENSOR_1CTA = 0, 1, 2
 ORTHO_NO_NORMALIZE = 1
 PHASE_MOMENTUM, PHASE_NS, PHASE_UPDATE, PHASE_GATHER, PHASE_SCATTER = range(5)
 ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BY_PARTS = 0, 1, 2
+ACTIVATION_SILU, ACTIVATION_GELU = 0, 1
+KEEP_NONE, KEEP_FULL, KEEP_8BIT = 0, 1, 2
 PHASE_NAMES = ("momentum", "ns", "update", "gather", "scatter")
 
 
@@ -84,6 +86,27 @@ class AttentionDesc(C.Structure):
                 ("q_offsets", C.c_void_p), ("k_offsets", C.c_void_p)]
 
 
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("ld", C.c_int64)]
+
+
+class Blocks(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("ld", C.c_int64), ("scales", C.c_void_p), ("lds", C.c_int64), ("block_rows", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class FeedForwardDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("activation", C.c_int32), ("keep", C.c_int32), ("tokens", C.c_int32), ("dim", C.c_int32), ("hidden", C.c_int32)]
+
+
+class FeedForwardKept(C.Structure):
+    _fields_ = [("gate", Rows), ("up", Rows), ("x8", Blocks), ("gate8", Blocks), ("up8", Blocks)]
+
+
+class LinearBlocksDesc(C.Structure):
+    _fields_ = [("tokens", C.c_int32), ("dim", C.c_int32), ("out", C.c_int32), ("reserved", C.c_int32)]
+
+
 _vp = C.c_void_p
 _sig = {
     "muon_default_options": (C.c_int, [C.POINTER(Options)]),
@@ -134,6 +157,14 @@ _sig = {
     "muon_attention_forward": (C.c_int, [_vp] * 8),
     "muon_attention_workspace_bytes": (C.c_int, [_vp, C.POINTER(C.c_size_t)]),
     "muon_attention_backward": (C.c_int, [_vp] * 12 + [C.c_size_t, _vp]),
+    "muon_quantize": (C.c_int, [_vp, C.c_int32, C.c_int64, C.c_int64, _vp, _vp, _vp]),
+    "muon_dequantize": (C.c_int, [_vp, C.c_int32, C.c_int64, C.c_int64, _vp, _vp, _vp]),
+    "muon_feed_forward_workspace_bytes": (C.c_int, [_vp, C.c_int32, C.POINTER(C.c_size_t)]),
+    "muon_feed_forward_forward": (C.c_int, [_vp] * 9 + [C.c_size_t, _vp]),
+    "muon_feed_forward_backward": (C.c_int, [_vp] * 13 + [C.c_size_t, _vp]),
+    "muon_linear_blocks_forward": (C.c_int, [_vp] * 7),
+    "muon_linear_blocks_workspace_bytes": (C.c_int, [_vp, C.POINTER(C.c_size_t)]),
+    "muon_linear_blocks_backward": (C.c_int, [_vp] * 8 + [C.c_size_t, _vp]),
     "muon_last_device_status": (C.c_int, [_vp, _vp, C.POINTER(C.c_int32)]),
     "muon_clear_device_status": (C.c_int, [_vp, _vp]),
     "muon_device_status_word": (C.c_int, [_vp, C.POINTER(_vp)]),
@@ -293,6 +324,10 @@ def _at(x):
     return x if type(x) is int else C.byref(x)
 
 
+def _maybe(x):
+    return None if x is None else _at(x)
+
+
 def muon_layer_norm_workspace_bytes(desc) -> int:
     out = C.c_size_t(0)
     _check(lib.muon_layer_norm_workspace_bytes(_at(desc), C.byref(out)), "muon_layer_norm_workspace_bytes")
@@ -302,6 +337,18 @@ def muon_layer_norm_workspace_bytes(desc) -> int:
 def muon_attention_workspace_bytes(desc) -> int:
     out = C.c_size_t(0)
     _check(lib.muon_attention_workspace_bytes(_at(desc), C.byref(out)), "muon_attention_workspace_bytes")
+    return out.value
+
+
+def muon_feed_forward_workspace_bytes(desc, backward: bool) -> int:
+    out = C.c_size_t(0)
+    _check(lib.muon_feed_forward_workspace_bytes(_at(desc), 1 if backward else 0, C.byref(out)), "muon_feed_forward_workspace_bytes")
+    return out.value
+
+
+def muon_linear_blocks_workspace_bytes(desc) -> int:
+    out = C.c_size_t(0)
+    _check(lib.muon_linear_blocks_workspace_bytes(_at(desc), C.byref(out)), "muon_linear_blocks_workspace_bytes")
     return out.value
 
 
@@ -532,6 +579,29 @@ class Context:
                                  workspace_bytes, _stream(stream))
         if rc:
             raise MuonError(rc, "muon_attention_backward")
+
+    # Matrices are Rows and Blocks structures, or None where a call allows NULL.
+    def muon_quantize(self, dtype, rows, cols, x, out, stream=None) -> None:
+        _check(lib.muon_quantize(self.handle, dtype, rows, cols, _maybe(x), _maybe(out), _stream(stream)), "muon_quantize")
+
+    def muon_dequantize(self, dtype, rows, cols, blocks, y, stream=None) -> None:
+        _check(lib.muon_dequantize(self.handle, dtype, rows, cols, _maybe(blocks), _maybe(y), _stream(stream)), "muon_dequantize")
+
+    def muon_feed_forward_forward(self, desc, x, w_gate, w_up, w_down, y, kept, workspace, workspace_bytes, stream=None) -> None:
+        _check(lib.muon_feed_forward_forward(self.handle, *map(_maybe, (desc, x, w_gate, w_up, w_down, y, kept)), workspace, workspace_bytes,
+                                             _stream(stream)), "muon_feed_forward_forward")
+
+    def muon_feed_forward_backward(self, desc, dy, x, w_gate, w_up, w_down, kept, dx, dw_gate, dw_up, dw_down, workspace, workspace_bytes,
+                                   stream=None) -> None:
+        _check(lib.muon_feed_forward_backward(self.handle, *map(_maybe, (desc, dy, x, w_gate, w_up, w_down, kept, dx, dw_gate, dw_up, dw_down)),
+                                              workspace, workspace_bytes, _stream(stream)), "muon_feed_forward_backward")
+
+    def muon_linear_blocks_forward(self, desc, x, w8, y, x8, stream=None) -> None:
+        _check(lib.muon_linear_blocks_forward(self.handle, *map(_maybe, (desc, x, w8, y, x8)), _stream(stream)), "muon_linear_blocks_forward")
+
+    def muon_linear_blocks_backward(self, desc, dy, x8, w8, dx, dw, workspace, workspace_bytes, stream=None) -> None:
+        _check(lib.muon_linear_blocks_backward(self.handle, *map(_maybe, (desc, dy, x8, w8, dx, dw)), workspace, workspace_bytes, _stream(stream)),
+               "muon_linear_blocks_backward")
 
     def muon_last_device_status(self, stream=None) -> int:
         v = C.c_int32(0)

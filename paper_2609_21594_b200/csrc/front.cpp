@@ -376,6 +376,273 @@ std::tuple<Tensor, Tensor, Tensor> attention_backward(const Tensor& dout, const 
   return {dq, dk, dv};
 }
 
+// ------------------------------------------------------------------ 8-bit blocks
+// Codes [..., cols] with rows 16 bytes apart or a multiple of that, so that the tensor cores can take them, and their scales.
+struct Packed {
+  Tensor codes, scales;
+};
+Packed new_packed(at::IntArrayRef sizes, const at::TensorOptions& options, int64_t block_rows) {
+  std::vector<int64_t> shape(sizes.begin(), sizes.end()), scales = shape;
+  const int64_t cols = shape.back(), ld = (cols + 15) / 16 * 16;
+  shape.back() = ld;
+  scales.back() = (cols + 127) / 128;
+  if (block_rows > 1) scales[0] = (scales[0] + block_rows - 1) / block_rows;
+  const Tensor codes = at::empty(shape, options.dtype(at::kFloat8_e4m3fn));
+  return {ld == cols ? codes : codes.narrow(-1, 0, cols), at::empty(scales, options.dtype(at::kByte))};
+}
+
+// A packed matrix as the C ABI takes it, and the tensors that keep its memory.
+struct PackedView {
+  Tensor codes, scales;
+  int64_t rows, cols;
+  muon_blocks_t b = {};
+};
+PackedView packed(const Tensor& codes, const Tensor& scales, int64_t block_rows, const char* what) {
+  PackedView v;
+  if (codes.scalar_type() != at::kFloat8_e4m3fn) bad(std::string(what) + " must have codes of float8_e4m3fn, not " + c10::toString(codes.scalar_type()));
+  if (scales.scalar_type() != at::kByte) bad(std::string(what) + " must have scales of uint8, not " + c10::toString(scales.scalar_type()));
+  v.codes = rows_of(codes, what);
+  v.rows = v.codes.size(0);
+  v.cols = v.codes.size(1);
+  std::vector<int64_t> each(codes.sizes().begin(), codes.sizes().end());
+  each.back() = (v.cols + 127) / 128;
+  const bool rows = scales.sizes().equals(each);
+  const bool squares = codes.dim() == 2 && scales.dim() == 2 && scales.size(0) == (v.rows + 127) / 128 && scales.size(1) == each.back();
+  if (block_rows == 0) block_rows = rows ? 1 : 128;     // one row alone: both are the same
+  if (!(block_rows == 1 ? rows : squares))
+    bad(std::string(what) + " has codes " + shape_text(codes) + " and scales " + shape_text(scales) + ", which do not fit blocks of " +
+        std::to_string(block_rows) + " x 128");
+  v.scales = rows_of(scales, what);
+  v.b.codes = v.codes.data_ptr();
+  v.b.ld = v.rows > 1 ? row_stride(v.codes) : (v.cols + 15) / 16 * 16;
+  v.b.scales = static_cast<uint8_t*>(v.scales.data_ptr());
+  v.b.lds = row_stride(v.scales);
+  v.b.block_rows = int32_t(block_rows);
+  return v;
+}
+
+muon_rows_t rows_view(const Tensor& r) { return {r.data_ptr(), row_stride(r)}; }
+const muon_rows_t* maybe(const MaybeTensor& t, muon_rows_t* v) {
+  if (!t) return nullptr;
+  *v = rows_view(*t);
+  return v;
+}
+MaybeTensor new_scratch(size_t bytes, const Tensor& like) {
+  return bytes ? MaybeTensor(at::empty({int64_t(bytes)}, like.options().dtype(at::kByte))) : MaybeTensor();
+}
+
+std::tuple<Tensor, Tensor> quantize(const Tensor& x, int64_t block_rows) {
+  const int index = index_of(x);
+  if (block_rows != 1 && block_rows != 128) bad("block_rows is 1 or 128");
+  if (block_rows == 128 && x.dim() != 2) bad("blocks of 128 x 128 take a matrix");
+  c10::cuda::OptionalCUDAGuard guard(x.device());
+  const int dtype = dtype_of(x, "x");
+  const Tensor r = rows_of(x, "x");
+  const Packed out = new_packed(x.sizes(), x.options(), block_rows);
+  const PackedView v = packed(out.codes, out.scales, block_rows, "the result");
+  const muon_rows_t in = rows_view(r);
+  check(muon_quantize(context(index), dtype, r.size(0), r.size(1), &in, &v.b, stream_of(index)), "muon_quantize");
+  return {out.codes, out.scales};
+}
+
+Tensor dequantize(const Tensor& codes, const Tensor& scales, at::ScalarType dtype) {
+  const int index = index_of(codes);
+  same_device(scales, index);
+  if (dtype != at::kBFloat16 && dtype != at::kFloat) bad(std::string("dtype must be bf16 or fp32, not ") + c10::toString(dtype));
+  c10::cuda::OptionalCUDAGuard guard(codes.device());
+  const PackedView v = packed(codes, scales, 0, "the input");
+  Tensor y = at::empty(codes.sizes(), codes.options().dtype(dtype));
+  const muon_rows_t out = {y.data_ptr(), v.cols};
+  check(muon_dequantize(context(index), dtype_of(y, "y"), v.rows, v.cols, &v.b, &out, stream_of(index)), "muon_dequantize");
+  return y;
+}
+
+// ------------------------------------------------------------------ gated feed-forward block
+struct FeedForwardCall {
+  int index;
+  muon_feed_forward_desc_t d = {};
+  Tensor gate, up, down;                               // the weights, with contiguous rows
+  std::vector<int64_t> hidden_shape;                   // of g and u
+  muon_rows_t w[3];
+};
+// `x`: x, or dy of the same shape.
+FeedForwardCall feed_forward_call(const Tensor& x, const char* name, const Tensor& w_gate, const Tensor& w_up, const Tensor& w_down,
+                                  const std::string& activation) {
+  FeedForwardCall c;
+  c.index = index_of(x);
+  for (const Tensor* w : {&w_gate, &w_up, &w_down}) same_device(*w, c.index);
+  if (activation != "silu" && activation != "gelu") bad("activation is 'silu' or 'gelu'");
+  if (x.dim() < 1 || w_gate.dim() != 2 || !w_up.sizes().equals(w_gate.sizes()) || w_down.dim() != 2 || w_down.size(0) != w_gate.size(1) ||
+      w_down.size(1) != w_gate.size(0) || x.size(-1) != w_gate.size(1) || w_gate.numel() == 0)
+    bad("shapes do not fit: " + std::string(name) + " " + shape_text(x) + ", w_gate " + shape_text(w_gate) + ", w_up " + shape_text(w_up) + ", w_down " +
+        shape_text(w_down));
+  for (const Tensor* w : {&w_gate, &w_up, &w_down})
+    if (w->scalar_type() != x.scalar_type()) bad(std::string(name) + " and the weights must have one dtype");
+  c.d.dtype = dtype_of(x, name);
+  c.d.activation = activation == "silu" ? MUON_ACTIVATION_SILU : MUON_ACTIVATION_GELU;
+  c.d.dim = narrow(w_gate.size(1));
+  c.d.hidden = narrow(w_gate.size(0));
+  c.d.tokens = narrow(x.numel() / c.d.dim);
+  c.hidden_shape.assign(x.sizes().begin(), x.sizes().end());
+  c.hidden_shape.back() = c.d.hidden;
+  return c;
+}
+// After the device is set: copies of weights whose rows are not contiguous.
+void lay_out(FeedForwardCall& c, const Tensor& w_gate, const Tensor& w_up, const Tensor& w_down) {
+  c.gate = rows_of(w_gate, "w_gate");
+  c.up = rows_of(w_up, "w_up");
+  c.down = rows_of(w_down, "w_down");
+  c.w[0] = rows_view(c.gate);
+  c.w[1] = rows_view(c.up);
+  c.w[2] = rows_view(c.down);
+}
+
+std::tuple<Tensor, std::vector<Tensor>> feed_forward_forward(const Tensor& x, const Tensor& w_gate, const Tensor& w_up, const Tensor& w_down,
+                                                             const std::string& activation, const std::string& checkpoint) {
+  FeedForwardCall c = feed_forward_call(x, "x", w_gate, w_up, w_down, activation);
+  if (checkpoint != "full" && checkpoint != "8bit" && checkpoint != "none") bad("checkpoint is 'full', '8bit' or 'none'");
+  c10::cuda::OptionalCUDAGuard guard(x.device());
+  lay_out(c, w_gate, w_up, w_down);
+  c.d.keep = checkpoint == "full" ? MUON_KEEP_FULL : checkpoint == "8bit" ? MUON_KEEP_8BIT : MUON_KEEP_NONE;
+  const Tensor r = rows_of(x, "x");
+  Tensor y = new_like(x);
+  std::vector<Tensor> kept;
+  std::vector<PackedView> views;
+  muon_feed_forward_kept_t k = {};
+  if (c.d.keep == MUON_KEEP_FULL) {
+    for (muon_rows_t* t : {&k.gate, &k.up}) {
+      kept.push_back(at::empty(c.hidden_shape, x.options()));
+      *t = {kept.back().data_ptr(), c.d.hidden};
+    }
+  } else if (c.d.keep == MUON_KEEP_8BIT) {
+    for (muon_blocks_t* t : {&k.x8, &k.gate8, &k.up8}) {
+      const Packed p = new_packed(t == &k.x8 ? x.sizes() : at::IntArrayRef(c.hidden_shape), x.options(), 1);
+      kept.push_back(p.codes);
+      kept.push_back(p.scales);
+      views.push_back(packed(p.codes, p.scales, 1, "the result"));
+      *t = views.back().b;
+    }
+  }
+  size_t n = 0;
+  check(muon_feed_forward_workspace_bytes(&c.d, 0, &n), "muon_feed_forward_workspace_bytes");
+  const MaybeTensor ws = new_scratch(n, x);
+  const muon_rows_t in = rows_view(r), out = {y.data_ptr(), c.d.dim};
+  check(muon_feed_forward_forward(context(c.index), &c.d, &in, &c.w[0], &c.w[1], &c.w[2], &out, &k, address(ws), n, stream_of(c.index)),
+        "muon_feed_forward_forward");
+  return {y, kept};
+}
+
+std::tuple<MaybeTensor, MaybeTensor, MaybeTensor, MaybeTensor> feed_forward_backward(const Tensor& dy, const MaybeTensor& x, const Tensor& w_gate,
+                                                                                     const Tensor& w_up, const Tensor& w_down,
+                                                                                     const std::vector<Tensor>& kept, const std::string& activation,
+                                                                                     const std::vector<bool>& need) {
+  FeedForwardCall c = feed_forward_call(dy, "dy", w_gate, w_up, w_down, activation);
+  same_device(x, c.index);
+  for (const Tensor& t : kept) same_device(t, c.index);
+  if (need.size() != 4) bad("need says of x, w_gate, w_up and w_down whether their gradients are wanted");
+  if (kept.size() != 2 && kept.size() != 6) bad("kept is what feed_forward_forward gave: two tensors (checkpoint 'full') or six ('8bit')");
+  c10::cuda::OptionalCUDAGuard guard(dy.device());
+  lay_out(c, w_gate, w_up, w_down);
+  muon_feed_forward_kept_t k = {};
+  std::vector<Tensor> hold;
+  std::vector<PackedView> views;
+  muon_rows_t in_x = {};
+  if (kept.size() == 2) {
+    c.d.keep = MUON_KEEP_FULL;
+    if (!x) bad("x is needed with checkpoint 'full'");
+    if (!x->sizes().equals(dy.sizes()) || x->scalar_type() != dy.scalar_type()) bad("x must have the shape and dtype of dy");
+    for (const Tensor& t : kept) {
+      if (!t.sizes().equals(c.hidden_shape) || t.scalar_type() != dy.scalar_type()) bad("what was kept does not fit dy and the weights");
+      hold.push_back(rows_of(t, "kept"));
+    }
+    k.gate = rows_view(hold[0]);
+    k.up = rows_view(hold[1]);
+    hold.push_back(rows_of(*x, "x"));
+    in_x = rows_view(hold[2]);
+  } else {
+    c.d.keep = MUON_KEEP_8BIT;
+    if (x) bad("x is part of what was kept in 8 bits: give None");
+    muon_blocks_t* to[3] = {&k.x8, &k.gate8, &k.up8};
+    for (int i = 0; i < 3; ++i) {
+      if (!kept[size_t(2 * i)].sizes().equals(i ? at::IntArrayRef(c.hidden_shape) : dy.sizes())) bad("what was kept does not fit dy and the weights");
+      views.push_back(packed(kept[size_t(2 * i)], kept[size_t(2 * i + 1)], 1, "kept"));
+      *to[i] = views.back().b;
+    }
+  }
+  const Tensor r = rows_of(dy, "dy");
+  MaybeTensor dx, dw[3];
+  muon_rows_t out[4];
+  if (need[0]) dx = new_like(dy);
+  for (int i = 0; i < 3; ++i)
+    if (need[size_t(i + 1)]) dw[i] = at::empty({i < 2 ? c.d.hidden : c.d.dim, i < 2 ? c.d.dim : c.d.hidden}, dy.options());
+  size_t n = 0;
+  check(muon_feed_forward_workspace_bytes(&c.d, 1, &n), "muon_feed_forward_workspace_bytes");
+  const MaybeTensor ws = new_scratch(n, dy);
+  const muon_rows_t in = rows_view(r);
+  if (dx) out[0] = {dx->data_ptr(), c.d.dim};
+  check(muon_feed_forward_backward(context(c.index), &c.d, &in, kept.size() == 2 ? &in_x : nullptr, &c.w[0], &c.w[1], &c.w[2], &k, dx ? &out[0] : nullptr,
+                                   maybe(dw[0], &out[1]), maybe(dw[1], &out[2]), maybe(dw[2], &out[3]), address(ws), n, stream_of(c.index)),
+        "muon_feed_forward_backward");
+  return {dx, dw[0], dw[1], dw[2]};
+}
+
+// ------------------------------------------------------------------ 8-bit linear layer
+std::tuple<Tensor, Tensor, Tensor> linear_8bit_forward(const Tensor& x, const Tensor& w_codes, const Tensor& w_scales) {
+  const int index = index_of(x);
+  same_device(w_codes, index);
+  same_device(w_scales, index);
+  if (x.scalar_type() != at::kBFloat16) bad(std::string("x must be bf16, not ") + c10::toString(x.scalar_type()));
+  if (w_codes.dim() != 2 || x.dim() < 1 || x.size(-1) != w_codes.size(1) || w_codes.numel() == 0)
+    bad("shapes do not fit: x " + shape_text(x) + ", weight " + shape_text(w_codes));
+  c10::cuda::OptionalCUDAGuard guard(x.device());
+  const PackedView w = packed(w_codes, w_scales, 128, "the weight");
+  const Tensor r = rows_of(x, "x");
+  muon_linear_blocks_desc_t d = {};
+  d.tokens = narrow(r.size(0));
+  d.dim = narrow(r.size(1));
+  d.out = narrow(w.rows);
+  std::vector<int64_t> shape(x.sizes().begin(), x.sizes().end());
+  shape.back() = w.rows;
+  Tensor y = at::empty(shape, x.options());
+  const Packed p = new_packed(x.sizes(), x.options(), 1);
+  const PackedView x8 = packed(p.codes, p.scales, 1, "the result");
+  const muon_rows_t in = rows_view(r), out = {y.data_ptr(), w.rows};
+  check(muon_linear_blocks_forward(context(index), &d, &in, &w.b, &out, &x8.b, stream_of(index)), "muon_linear_blocks_forward");
+  return {y, p.codes, p.scales};
+}
+
+std::tuple<MaybeTensor, MaybeTensor> linear_8bit_backward(const Tensor& dy, const Tensor& x_codes, const Tensor& x_scales, const Tensor& w_codes,
+                                                          const Tensor& w_scales, const std::vector<bool>& need) {
+  const int index = index_of(dy);
+  for (const Tensor* t : {&x_codes, &x_scales, &w_codes, &w_scales}) same_device(*t, index);
+  if (need.size() != 2) bad("need says of x and the weight whether their gradients are wanted");
+  if (dy.scalar_type() != at::kBFloat16) bad(std::string("dy must be bf16, not ") + c10::toString(dy.scalar_type()));
+  if (w_codes.dim() != 2 || dy.dim() < 1 || dy.dim() != x_codes.dim() || dy.size(-1) != w_codes.size(0) || x_codes.size(-1) != w_codes.size(1) ||
+      w_codes.numel() == 0 || !dy.sizes().slice(0, size_t(dy.dim() - 1)).equals(x_codes.sizes().slice(0, size_t(dy.dim() - 1))))
+    bad("shapes do not fit: dy " + shape_text(dy) + ", x " + shape_text(x_codes) + ", weight " + shape_text(w_codes));
+  c10::cuda::OptionalCUDAGuard guard(dy.device());
+  const PackedView w = packed(w_codes, w_scales, 128, "the weight"), x = packed(x_codes, x_scales, 1, "x");
+  const Tensor r = rows_of(dy, "dy");
+  muon_linear_blocks_desc_t d = {};
+  d.tokens = narrow(r.size(0));
+  d.dim = narrow(w.cols);
+  d.out = narrow(w.rows);
+  MaybeTensor dx, dw;
+  muon_rows_t out[2] = {};
+  if (need[0]) {
+    dx = at::empty(x_codes.sizes(), dy.options());
+    out[0] = {dx->data_ptr(), w.cols};
+  }
+  if (need[1]) dw = at::empty({w.rows, w.cols}, dy.options());
+  size_t n = 0;
+  check(muon_linear_blocks_workspace_bytes(&d, &n), "muon_linear_blocks_workspace_bytes");
+  const MaybeTensor ws = new_scratch(n, dy);
+  const muon_rows_t in = rows_view(r);
+  check(muon_linear_blocks_backward(context(index), &d, &in, &x.b, &w.b, dx ? &out[0] : nullptr, maybe(dw, &out[1]), address(ws), n, stream_of(index)),
+        "muon_linear_blocks_backward");
+  return {dx, dw};
+}
+
 }  // namespace
 
 PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
@@ -424,4 +691,40 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
   m.def("attention_backward", &attention_backward, release(), py::arg("do"), py::arg("q"), py::arg("k"), py::arg("v"), py::arg("o"), py::arg("lse"),
         py::arg("causal") = true, py::arg("window") = 0, py::arg("scale") = none, py::arg("q_lens") = none, py::arg("k_lens") = none,
         py::arg("q_offsets") = none, py::arg("k_offsets") = none, "(dq, dk, dv) from what `attention_forward` took and gave.");
+  m.def("quantize", &quantize, release(), py::arg("x"), py::arg("block_rows") = 1,
+        "(codes, scales) of bf16 or fp32 x [..., cols]: float8_e4m3fn codes of x's shape and uint8 scales e that stand for 2 ** (e - 127), one for each\n"
+        "1 x 128 elements ([..., ceil(cols / 128)]; activations) or, with block_rows=128, 128 x 128 of a matrix (weights).  The scale is the least\n"
+        "that brings the block's largest finite magnitude to at most 448; codes are the nearest, ties to even.  NaN and infinities are kept as NaN.");
+  m.def(
+      "dequantize",
+      [](const Tensor& codes, const Tensor& scales, const py::object& dtype) {
+        const at::ScalarType t = torch::python::detail::py_object_to_dtype(dtype);
+        py::gil_scoped_release no_gil;
+        return dequantize(codes, scales, t);
+      },
+      py::arg("codes"), py::arg("scales"), py::arg("dtype"), "What `quantize` gave, as bf16 or fp32 (rounded once).");
+  m.def(
+      "feed_forward_forward",
+      [](const Tensor& x, const Tensor& w_gate, const Tensor& w_up, const Tensor& w_down, const std::string& activation, const std::string& checkpoint) {
+        std::tuple<Tensor, std::vector<Tensor>> r;
+        {
+          py::gil_scoped_release no_gil;
+          r = feed_forward_forward(x, w_gate, w_up, w_down, activation, checkpoint);
+        }
+        return py::make_tuple(std::get<0>(r), py::tuple(py::cast(std::get<1>(r))));
+      },
+      py::arg("x"), py::arg("w_gate"), py::arg("w_up"), py::arg("w_down"), py::arg("activation") = "silu", py::arg("checkpoint") = "full",
+        "(y, kept): y = (act(x w_gate') * (x w_up')) w_down' for x [..., dim], w_gate, w_up [hidden, dim], w_down [dim, hidden], all bf16 or fp32.\n"
+        "activation: 'silu' or 'gelu' (tanh form).  checkpoint, what is kept for the backward pass: 'full' (gate, up) in x's dtype; '8bit' codes and\n"
+        "scales of x, gate and up as `quantize` gives them; 'none' ().  Sums are fp32; the hidden activation is rounded once to x's dtype.");
+  m.def("feed_forward_backward", &feed_forward_backward, release(), py::arg("dy"), py::arg("x"), py::arg("w_gate"), py::arg("w_up"), py::arg("w_down"),
+        py::arg("kept"), py::arg("activation") = "silu", py::arg("need") = std::vector<bool>(4, true),
+        "(dx, dw_gate, dw_up, dw_down) from what `feed_forward_forward` took and kept; x is None where '8bit' kept it.  need: which of them are formed\n"
+        "(the others are None).  The gradients are those of the block at the kept gate and up.");
+  m.def("linear_8bit_forward", &linear_8bit_forward, release(), py::arg("x"), py::arg("w_codes"), py::arg("w_scales"),
+        "(y, x_codes, x_scales): y = Q(x) w' for bf16 x [..., dim] and w [out, dim] in 8 bits (`quantize` with block_rows=128); Q(x) in blocks of 1 x 128\n"
+        "is what the backward pass takes.");
+  m.def("linear_8bit_backward", &linear_8bit_backward, release(), py::arg("dy"), py::arg("x_codes"), py::arg("x_scales"), py::arg("w_codes"),
+        py::arg("w_scales"), py::arg("need") = std::vector<bool>(2, true),
+        "(dx, dw), bf16: dx = Q(dy) w, dw = dy' Q(x) with dy itself.  need: which of the two are formed (the other is None).");
 }

@@ -1,37 +1,13 @@
 // extern "C" entry points of the layer operators: argument validation and the choice of kernels.
 #include <cmath>
-#include <initializer_list>
 
-#include "boxes.h"
-#include "layer_ops.h"
+#include "layer_checks.h"
 
 using namespace muon;
 
 namespace {
 
 constexpr double kTwoPi = 6.283185307179586476925286766559;
-
-bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-bool known_dtype(int32_t d) { return d == MUON_DTYPE_BF16 || d == MUON_DTYPE_FP32; }
-
-size_t bytes_of(int32_t d) { return d == MUON_DTYPE_BF16 ? 2 : 4; }
-
-// The context's device must be current; its SM count comes with the answer.
-int device_of(const muon_ctx* ctx, int* sms) {
-  int dev = -1;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev != ctx->device) return MUON_ERR_CUDA;
-  return cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess ? MUON_OK : MUON_ERR_CUDA;
-}
-
-int launched(muon_ctx* ctx, int n) {
-  if (n < 0) {
-    (void)cudaGetLastError();      // a refused launch is this call's error, not the next one's
-    return n;
-  }
-  ctx->launches += n;
-  return MUON_OK;
-}
 
 int check_norm(const muon_norm_desc_t* d) {
   if (!d || !known_dtype(d->dtype) || !known_dtype(d->param_dtype) || (d->center != 0 && d->center != 1) || d->reserved != 0) return MUON_ERR_INVALID_ARG;
@@ -63,23 +39,6 @@ bool good_output(const muon_heads_t* t, size_t elem, int64_t batch, int64_t toke
 Box box_of(const muon_heads_t* t, size_t elem, int64_t batch, int64_t tokens, int64_t heads, int64_t dim) {
   const int64_t e = int64_t(elem);
   return Box(t->data, batch, tokens, heads, dim * e, t->batch_stride * e, t->token_stride * e, t->head_stride * e);
-}
-Box rows_of(const void* p, int64_t rows, int64_t cols, int64_t ld, size_t elem) {
-  const int64_t e = int64_t(elem);
-  return Box(p, 1, 1, rows, cols * e, 0, 0, ld * e);
-}
-
-// Whether a result lies over an input or over another result.  The first result may be one of `in_place` exactly.
-bool results_clash(std::initializer_list<Box> results, std::initializer_list<Box> inputs, std::initializer_list<Box> in_place = {}) {
-  for (const Box* r = results.begin(); r != results.end(); ++r) {
-    for (const Box& in : inputs)
-      if (boxes_meet(*r, in)) return true;
-    for (const Box& in : in_place)
-      if (!(r == results.begin() && same_box(*r, in)) && boxes_meet(*r, in)) return true;
-    for (const Box* other = results.begin(); other != r; ++other)
-      if (boxes_meet(*r, *other)) return true;
-  }
-  return false;
 }
 
 int check_attention(const muon_attention_desc_t* d) {

@@ -1,0 +1,99 @@
+// Shared declarations of the matrix products around the gated feed-forward block and the 8-bit linear layer.  Internal to the library.
+//
+//   C[m][n] = sum over segments s and k of A_s(m, k) B_s(n, k)
+//
+// with a choice of epilogues.  One description serves two engines: tensor cores (product_tc.cu) where TMA can address every tensor,
+// CUDA cores (product_simt.cu) for fp32 and for everything else.
+#pragma once
+
+#include "layer_ops.h"
+
+namespace muon {
+
+// 8-bit blocks: e4m3 codes and a byte e for every block of 128 columns of `block_rows` (1 or 128) rows, which stands for 2^(e - 127).
+constexpr int kBlock = 128;
+constexpr int kTypeBf16 = MUON_DTYPE_BF16, kTypeFp32 = MUON_DTYPE_FP32, kTypeE4m3 = 2;
+
+// A matrix as it lies in memory: rows of `ld` elements.
+struct Operand {
+  const void* data;
+  int64_t ld;
+  int32_t type;
+  int32_t mn_major;            // 0: memory row = row of the operand, column = k;  1: memory row = k, column = row of the operand
+  const uint8_t* scales;       // e4m3: [memory rows / block_rows][columns / 128]
+  int64_t lds;
+  int32_t block_rows;
+};
+
+enum EpilogueKind : int32_t {
+  kPlain,                      // C
+  kGated,                      // B_0 and B_1 are two matrices of n rows: g = A B_0', u = A B_1', h = act(g) u; writes h, and g and u where asked
+  kGrad,                       // C = dh stays in the kernel; reads g and u; writes dg = dh u act'(g), du = dh act(g), h = act(g) u
+};
+
+struct Epilogue {
+  EpilogueKind kind;
+  int32_t type;                // of what is written: bf16 or fp32
+  int32_t activation;
+  int32_t gate_up_type;        // kGated: of g and u as written (bf16, fp32, e4m3); kGrad: as read
+  void* c;                     // kPlain: C; kGated, kGrad: h
+  int64_t ldc;
+  void* gate;                  // kGated: g or null; kGrad: dg
+  void* up;                    // kGated: u or null; kGrad: du
+  int64_t ld_gate, ld_up;
+  Operand in_gate, in_up;      // kGrad: g and u.  kGated with e4m3: where codes and scales of g and u go
+};
+
+struct Product {
+  Operand a[2], b[2];
+  int32_t segments;
+  int32_t m, n, k;             // k: of each segment
+  Epilogue e;
+};
+
+constexpr int kMaxProducts = 3;   // of a launch
+
+inline bool products_tc_take(const Product*, int) { return false; }
+inline int launch_products_tc(muon_ctx*, const Product*, int, cudaStream_t) { return MUON_ERR_UNSUPPORTED; }
+int launch_product_simt(const Product& p, int sms, cudaStream_t st);
+
+int launch_quantize(int dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx, const Operand& out, int sms, cudaStream_t st);
+int launch_dequantize(int dtype, int64_t rows, int64_t cols, const Operand& in, void* y, int64_t ldy, int sms, cudaStream_t st);
+
+#ifdef __CUDACC__
+// 2^(e - 127) for a scale's byte; 255 is a NaN.
+__device__ __forceinline__ float scale_of(uint32_t e) { return __uint_as_float(e == 0 ? 0x00400000u : e == 255 ? 0x7fffffffu : e << 23); }
+// 2^(127 - e): what a block is multiplied with before it is rounded.  e <= 247 as `scale_byte` gives it, so that this is a normal number.
+__device__ __forceinline__ float inverse_scale_of(uint32_t e) { return __uint_as_float((254u - e) << 23); }
+// The byte of the least power of two (from 2^-127 on) that brings `top`, the bits of a block's largest finite magnitude, to at most 448 =
+// 1.75 * 2^8: a mantissa above 1.75 carries into the exponent.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
+  const int e = int((top + 0x1fffffu) >> 23) - 8;
+  return uint32_t(e < 0 ? 0 : e);
+}
+// The magnitude's bits of a finite value, 0 of a NaN or an infinity: neither has a share in the scale, and both are kept as NaN.
+__device__ __forceinline__ uint32_t finite_bits(float x) {
+  const uint32_t u = __float_as_uint(x) & 0x7fffffffu;
+  return u < 0x7f800000u ? u : 0u;
+}
+__device__ __forceinline__ float infinite_to_nan(float x) { return (__float_as_uint(x) & 0x7fffffffu) < 0x7f800000u ? x : __uint_as_float(0x7fffffffu); }
+
+// act(g) = g s(w(g)) with the logistic function s:  silu: w = g;  gelu (tanh form, (1 + tanh z) / 2 = s(2z)): w = 2 sqrt(2 / pi) (g + 0.044715 g^3).
+// act'(g) = s + g s (1 - s) w'(g).  FAST: the exponential and the quotient of the special-function unit (2^-21 relative), for results that are
+// rounded to bf16.
+template <bool FAST>
+__device__ __forceinline__ void activate(int activation, float g, float* a, float* slope) {
+  float w = g, dw = 1.f;
+  if (activation == MUON_ACTIVATION_GELU) {
+    constexpr float k = 1.5957691216057308f, c = 0.044715f;
+    const float g2 = fminf(g * g, 1e12f);     // beyond, s is 0 or 1 and 0 times w' has to stay 0
+    w = k * g * fmaf(c, g2, 1.f);
+    dw = k * fmaf(3.f * c, g2, 1.f);
+  }
+  const float s = FAST ? __fdividef(1.f, 1.f + __expf(-w)) : 1.f / (1.f + expf(-w));
+  *a = g * s;
+  *slope = fmaf(g * s * (1.f - s), dw, s);
+}
+#endif
+
+}  // namespace muon

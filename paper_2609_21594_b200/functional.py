@@ -1,8 +1,9 @@
-"""torch front end of the layer operators: layer norm, rotary positions and attention, forward and backward.
+"""torch front end of the layer operators: layer norm, rotary positions, attention, the gated feed-forward block and the 8-bit linear layer, forward
+and backward.
 
 What a training program needs around the matrices that `optim.Muon` updates.  The `*_forward` / `*_backward` pairs are defined in
 `csrc/front.cpp` (argument checks and marshalling, built as `_front`) and their arithmetic runs in the CUDA library, on the current
-stream of the tensors' device.  `layer_norm`, `rotary` and `attention` are differentiable; the pairs are the same calls for programs that
+stream of the tensors' device.  `layer_norm`, `rotary`, `attention`, `feed_forward` and `linear_8bit` are differentiable; the pairs are the same calls for programs that
 keep their own tape.  Each host thread has a context of its own per device (autograd calls backward passes from another thread); all
 of a device's record an expired wait in one word, which `synchronize_and_check` reads.
 A thread's first call on a device makes its context, which allocates: calls are captured into a graph after one ordinary call.
@@ -23,6 +24,7 @@ except ImportError as e:
     raise ImportError("the torch front end of the layer operators (_front.so) is missing or does not fit this torch: build it with "
                       "`python -m paper_2609_21594_b200.build`, which needs a C++ compiler and the headers of Python and torch") from e
 from ._front import attention_backward, attention_forward, layer_norm_backward, layer_norm_forward, rotary_forward  # noqa: F401
+from ._front import dequantize, feed_forward_backward, feed_forward_forward, linear_8bit_backward, linear_8bit_forward, quantize  # noqa: F401
 from .binding import muon_rotary_frequencies as rotary_frequencies  # noqa: F401  (part of this module's interface)
 
 
@@ -130,3 +132,50 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
               q_offsets: Optional[torch.Tensor] = None, k_offsets: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Differentiable `attention_forward`: o alone."""
     return _Attention.apply(q, k, v, causal, window, scale, q_lens, k_lens, q_offsets, k_offsets)
+
+
+class _FeedForward(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, w_down, activation, checkpoint):
+        y, kept = feed_forward_forward(x, w_gate, w_up, w_down, activation, checkpoint)
+        ctx.save_for_backward(x if checkpoint == "full" else None, w_gate, w_up, w_down, *kept)
+        ctx.activation = activation
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, w_gate, w_up, w_down, *kept = ctx.saved_tensors
+        return feed_forward_backward(dy, x, w_gate, w_up, w_down, kept, ctx.activation, ctx.needs_input_grad[:4]) + (None, None)
+
+
+def feed_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, activation: str = "silu",
+                 checkpoint: str = "full") -> torch.Tensor:
+    """Differentiable `feed_forward_forward`: y alone.  checkpoint: "full" or "8bit"; where nothing asks for gradients nothing is kept."""
+    if checkpoint not in ("full", "8bit"):
+        raise ValueError("checkpoint is 'full' or '8bit'")
+    if not (torch.is_grad_enabled() and any(t.requires_grad for t in (x, w_gate, w_up, w_down))):
+        return feed_forward_forward(x, w_gate, w_up, w_down, activation, "none")[0]
+    return _FeedForward.apply(x, w_gate, w_up, w_down, activation, checkpoint)
+
+
+class _Linear8bit(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight):
+        w_codes, w_scales = quantize(weight, 128)
+        y, x_codes, x_scales = linear_8bit_forward(x, w_codes, w_scales)
+        ctx.save_for_backward(x_codes, x_scales, w_codes, w_scales)
+        ctx.dtype = weight.dtype
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        dx, dw = linear_8bit_backward(dy, *ctx.saved_tensors, ctx.needs_input_grad)
+        return dx, None if dw is None else dw.to(ctx.dtype)
+
+
+def linear_8bit(x: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
+    """Differentiable x weight' whose products are formed in 8 bits (`linear_8bit_forward`, `linear_8bit_backward`): bf16 x [..., dim], bf16 or fp32
+    weight [out, dim].  Keeps x and the weight in 8 bits for the backward pass.  The gradient of the rounding to 8 bits is taken as 1."""
+    return _Linear8bit.apply(x, weight)
