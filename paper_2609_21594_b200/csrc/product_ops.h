@@ -53,8 +53,9 @@ struct Product {
 
 constexpr int kMaxProducts = 3;   // of a launch
 
-inline bool products_tc_take(const Product*, int) { return false; }
-inline int launch_products_tc(muon_ctx*, const Product*, int, cudaStream_t) { return MUON_ERR_UNSUPPORTED; }
+// The tensor-core engine takes a list of products with operands of one type and one order in memory, if TMA can address all tensors.
+bool products_tc_take(const Product* p, int count);
+int launch_products_tc(muon_ctx* ctx, const Product* p, int count, cudaStream_t st);
 int launch_product_simt(const Product& p, int sms, cudaStream_t st);
 
 int launch_quantize(int dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx, const Operand& out, int sms, cudaStream_t st);

@@ -1,0 +1,810 @@
+// Matrix products on the tensor cores: pairs of CTAs, persistent over a list of 256 x 256 tiles.
+//
+//   C[m][n] = sum_s sum_k A_s(m, k) B_s(n, k)          operands bf16, or e4m3 with a power of two for every 128 values of k
+//
+// CTA r of a pair owns 128 rows of the tile and stages, for each k-block of 128 bytes, its rows of A and half of the columns of B; the
+// leader (r = 0) issues tcgen05.mma.cta_group::2 of 256 x N.  Operands come by TMA as they lie in memory, K-major or MN-major (summed
+// over the rows: the backward products need no transposed copy).  Accumulators alternate between two places in tensor memory, so that a
+// tile's epilogue runs under the next tile's products.  Eight epilogue warps, two per quarter of the rows; a thread holds 64 columns of one
+// row at a time and hands them to TMA through 4 KiB of its warp's own, so that epilogue warps never wait for one another.
+//
+// Gated product: the leader's half of B is 128 rows of w_gate and its peer's the same rows of w_up, so columns [0, 128) of the accumulator are g
+// and [128, 256) are u of the same elements: one thread holds both, and 128 columns of g are one block of the 8-bit form.
+// Gradient of the gate: the accumulator is dh, which never leaves the chip; g and u come in, dg, du and h go out.
+//
+// 8 bits: tcgen05.mma.kind::mxf8f6f4 multiplies each group of 32 values of k with the scales of its row of A and of B, taken from tensor memory.  A
+// block of 128 is four such groups with one scale.  A warp of its own gathers the bytes of four blocks into the order that tcgen05.cp spreads
+// over the lanes; the issuer copies them (12 columns) every fourth k-block.  Two accumulators of 256 columns would leave no room for them, so the
+// second one begins 16 columns inside the first: the next tile begins when those 16 columns have been read, which the epilogue does first.
+//
+// Synchronisation as in the Newton-Schulz kernel, all waits bounded: full / empty per stage, tfull / tempty per accumulator, an abort flag in both CTAs.
+#include <cuda_fp8.h>
+
+#include <algorithm>
+
+#include "product_ops.h"
+#include "tc_common.cuh"
+
+namespace muon {
+namespace {
+
+using namespace tc;
+
+constexpr int kRows = 128;                     // of A per CTA
+constexpr int kStages = 5;
+constexpr uint32_t kHalfBytes = kRows * 128;   // 16 KiB: 128 rows of 128 bytes
+constexpr uint32_t kStageBytes = 2 * kHalfBytes;
+constexpr int kEpiWarps = 8;
+constexpr uint32_t kPieceBytes = 32 * 128;     // what an epilogue warp hands over at once: 32 rows of 64 bf16
+constexpr int kGroupTiles = 8;                 // tiles of rows that a stretch of the tile list stays in: what they and as many columns read fits L2
+constexpr int kScaleRing = 4;                  // groups of four k-blocks whose scales are on their way
+constexpr uint32_t kScaleBytes = 3 * 512;      // of a group: 128 rows of A, 256 of B, four bytes each
+constexpr uint32_t kScaleCol = 496;            // tensor memory columns of the scales
+constexpr uint32_t kSecondAccumulator8 = 240;
+
+template <bool EIGHT>
+struct Shape {
+  static constexpr int pieces = EIGHT ? 1 : 2; // buffers per epilogue warp
+  static constexpr uint32_t epi_off = kStages * kStageBytes;
+  static constexpr uint32_t scale_off = epi_off + kEpiWarps * pieces * kPieceBytes;
+  static constexpr uint32_t bar_off = scale_off + (EIGHT ? kScaleRing * kScaleBytes : 0);
+  static constexpr uint32_t bytes = bar_off + 512 + 1024;
+  static constexpr int threads = 32 * (2 + kEpiWarps + (EIGHT ? 1 : 0));
+};
+static_assert(Shape<false>::bytes <= 232448 && Shape<true>::bytes <= 232448, "227 KiB of shared memory");
+
+struct Scales {                                // of an operand: the byte of (row, k-block) is at (row >> row_shift) * row_step + block * block_step
+  const uint8_t* p;
+  int64_t row_step, block_step;
+  int32_t row_shift, rows;
+};
+struct TcProduct {
+  CUtensorMap a[2], b[2];
+  CUtensorMap out[3];                          // C; or h, g, u; or h, dg, du
+  CUtensorMap in[2];                           // g, u
+  Scales sa, sb;
+  int32_t m, n, kblocks, segments;             // kblocks: of a segment
+  int32_t tiles_m, tiles_n, tile_begin;
+  int32_t tile_cols;                           // columns of C that a tile forms
+};
+struct TcProducts {
+  TcProduct p[kMaxProducts];
+  int32_t count, total_tiles;
+  int32_t half;                                // columns of B per CTA: 128 or 64
+  int32_t activation, gate_up_type, keep;      // keep: g and u are written
+  Operand gate, up;                            // 8-bit g and u
+  int32_t codes_wide;                          // their rows take 16-byte accesses
+  int32_t* status;
+};
+
+// ------------------------------------------------------------------ PTX
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t map_to_cta(uint32_t local_addr, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local_addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ void st_cluster_u32(uint32_t cluster_addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr), "r"(v) : "memory");
+}
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar_cluster_addr, int x, int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar_cluster_addr), "r"(x), "r"(y)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y)
+      : "memory");
+}
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, uint32_t src, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(src), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void tc_mma_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tc_mma_pair_scaled(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                                   uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+      ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+      : "memory");
+}
+// 32 rows of 16 bytes into four columns, repeated in every quarter of the lanes, in both CTAs.
+__device__ __forceinline__ void tc_copy_scales_pair(uint32_t d_tmem, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(d_tmem), "l"(desc) : "memory");
+}
+// Arrives on the barrier at this shared-memory offset in both CTAs of the pair once everything issued so far is done.
+__device__ __forceinline__ void tc_commit_pair(uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .b16 m;\n\t"
+      "mov.b16 m, 3;\n\t"
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n\t}"
+      ::"r"(bar)
+      : "memory");
+}
+
+// Descriptors are a constant high part and the address in 16-byte units.  K-major: 8 rows of 128 bytes each kilobyte.  MN-major: 8 values of k
+// each kilobyte, and the next 64 columns (bf16) 8 KiB further.  Scales: no swizzle, 8 rows of 16 bytes each 128 bytes.
+constexpr uint64_t kDescK = (uint64_t(1) << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) | (uint64_t(2) << 61);
+constexpr uint64_t kDescMN = (uint64_t(8192 >> 4) << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) | (uint64_t(2) << 61);
+constexpr uint64_t kDescScales = (uint64_t(128 >> 4) << 32) | (uint64_t(1) << 46);
+
+// Instruction descriptor of the scaled kind: e4m3 operands, scales that are powers of two; which of a cell's four bytes holds them is added per k-block.
+__device__ __forceinline__ constexpr uint32_t make_idesc_scaled(bool b_mn_major, int m, int n) {
+  return (uint32_t(b_mn_major ? 1 : 0) << 16) | (uint32_t(n >> 3) << 17) | (1u << 23) | (uint32_t(m >> 4) << 24);
+}
+__device__ __forceinline__ uint32_t scale_byte_ids(uint32_t id) { return (id << 4) | (id << 29); }
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&p);
+}
+__device__ __forceinline__ float low(uint32_t pair) { return __uint_as_float(pair << 16); }
+__device__ __forceinline__ float high(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
+
+// ------------------------------------------------------------------ tiles
+struct Tile {
+  int prob, m0, n0;                            // first row of the pair, first column of C
+};
+// Within kGroupTiles tiles of rows the rows run fastest: the pairs at work at a time share the operands of about as many tiles of rows as of columns.
+__device__ __forceinline__ Tile decode(const TcProducts& L, int t) {
+  Tile r;
+  r.prob = 0;
+  for (int i = 1; i < L.count; ++i)
+    if (t >= L.p[i].tile_begin) r.prob = i;
+  const TcProduct& p = L.p[r.prob];
+  t -= p.tile_begin;
+  const int per_group = kGroupTiles * p.tiles_n;
+  const int g = t / per_group, in = t - g * per_group;
+  const int rows = min(kGroupTiles, p.tiles_m - g * kGroupTiles);
+  const int c = in / rows;
+  r.m0 = (g * kGroupTiles + in - c * rows) * (2 * kRows);
+  r.n0 = c * p.tile_cols;
+  return r;
+}
+
+struct Ring {
+  uint32_t base, bars;
+  volatile int* abort_flag;
+  uint32_t it, s, ph;                          // k-blocks so far, place in the ring and its phase
+  __device__ __forceinline__ void advance() {
+    ++it;
+    if (++s == uint32_t(kStages)) {
+      s = 0;
+      ph ^= 1u;
+    }
+  }
+};
+
+// ------------------------------------------------------------------ epilogue
+// One epilogue warp's 32 rows.  `emit` hands 64 columns, two to a word, to TMA.
+template <int PIECES>
+struct Piece {
+  uint32_t buf;                                // this warp's shared memory
+  uint32_t next;                               // buffer to use
+  int lane;
+  __device__ __forceinline__ void emit(const CUtensorMap* map, const uint32_t (&w)[32], int col, int row) {
+    const uint32_t at = buf + next * kPieceBytes;
+    if (lane == 0) tma_wait_read<PIECES - 1>();          // what was last stored from this buffer has been read
+    __syncwarp();
+    const uint32_t line = at + uint32_t(lane) * 128u;
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(line + (uint32_t(q ^ (lane & 7)) << 4)), "r"(w[4 * q]), "r"(w[4 * q + 1]),
+                   "r"(w[4 * q + 2]), "r"(w[4 * q + 3])
+                   : "memory");
+    fence_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      tma_store(map, at, col, row);
+      tma_commit();
+    }
+    next = next + 1 == PIECES ? 0 : next + 1;
+  }
+};
+
+__device__ __forceinline__ void load64(uint32_t taddr, uint32_t (&v)[64]) {
+  __syncwarp();
+  tc_ld32(taddr, *reinterpret_cast<uint32_t(*)[32]>(&v[0]));
+  tc_ld32(taddr + 32, *reinterpret_cast<uint32_t(*)[32]>(&v[32]));
+}
+
+// The bits of the largest finite magnitude in 128 columns of the accumulator.
+__device__ __forceinline__ uint32_t top_of_block(uint32_t taddr) {
+  uint32_t top = 0;
+  __syncwarp();
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) {
+    uint32_t v[32];
+    tc_ld32(taddr + uint32_t(i * 32), v);
+    tc_wait_ld();
+#pragma unroll
+    for (int k = 0; k < 32; ++k) top = max(top, finite_bits(__uint_as_float(v[k])));
+  }
+  return top;
+}
+// 64 values as codes, the columns from `left` on left alone.
+__device__ __forceinline__ void store_codes(uint8_t* p, const uint32_t (&v)[64], float inverse, int left, bool wide) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t pair[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int at = q * 16 + i * 4 + h * 2;
+        pair[h] = __nv_cvt_float2_to_fp8x2(make_float2(infinite_to_nan(__uint_as_float(v[at])) * inverse, infinite_to_nan(__uint_as_float(v[at + 1])) * inverse),
+                                           __NV_SATFINITE, __NV_E4M3);
+      }
+      w[i] = pair[0] | pair[1] << 16;
+    }
+    if (wide && left >= (q + 1) * 16) {
+      *reinterpret_cast<uint4*>(p + q * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (q * 16 + i < left) p[q * 16 + i] = uint8_t(w[i >> 2] >> (8 * (i & 3)));
+    }
+  }
+}
+__device__ __forceinline__ void load_codes(const uint8_t* p, uint32_t (&w)[16], int left, bool wide) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    if (wide && left >= (q + 1) * 16) {
+      const uint4 x = __ldg(reinterpret_cast<const uint4*>(p) + q);
+      w[4 * q] = x.x; w[4 * q + 1] = x.y; w[4 * q + 2] = x.z; w[4 * q + 3] = x.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[4 * q + i] = 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (q * 16 + i < left) w[4 * q + (i >> 2)] |= uint32_t(__ldg(p + q * 16 + i)) << (8 * (i & 3));
+    }
+  }
+}
+__device__ __forceinline__ float2 values_of(uint32_t pair) {
+  return __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(__nv_fp8x2_storage_t(pair & 0xffffu), __NV_E4M3)));
+}
+
+template <bool A_MN, bool B_MN, bool EIGHT, int EPI>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<EIGHT>::threads, 1) product_pair_kernel(const __grid_constant__ TcProducts L) {
+  using S = Shape<EIGHT>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* gen_base = smem_raw + (base - raw);
+  const uint32_t bars = base + S::bar_off;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen_base + S::bar_off + 480);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen_base + S::bar_off + 488);
+  auto bar = [&](int i) { return bars + uint32_t(i) * 8u; };
+  auto full_bar = [&](uint32_t s) { return bar(int(s)); };
+  auto empty_bar = [&](uint32_t s) { return bar(kStages + int(s)); };
+  constexpr int kT = 2 * kStages;
+  auto tfull_bar = [&](uint32_t i) { return bar(kT + int(i)); };
+  auto tempty_bar = [&](uint32_t i) { return bar(kT + 2 + int(i)); };
+  const uint32_t drain_bar = bar(kT + 4), shared_bar = bar(kT + 5);     // shared_bar: the columns that both accumulators use have been read
+  auto input_bar = [&](int w) { return bar(kT + 6 + w); };
+  auto sfull_bar = [&](uint32_t i) { return bar(kT + 6 + kEpiWarps + int(i)); };
+  auto sempty_bar = [&](uint32_t i) { return bar(kT + 6 + kEpiWarps + kScaleRing + int(i)); };
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  const bool leader_cta = rank == 0;
+  const int pair_id = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
+  const uint32_t peer_abort = map_to_cta(base + S::bar_off + 488, rank ^ 1u);
+  auto give_up = [&](int code) {
+    *abort_flag = 1;
+    st_cluster_u32(peer_abort, 1u);
+    atomicExch(L.status, code);
+  };
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(tfull_bar(i), 1);
+      mbar_init(tempty_bar(i), 2 * kEpiWarps);
+    }
+    mbar_init(drain_bar, 1);
+    mbar_init(shared_bar, kEpiWarps);                 // the four warps of each CTA that read those columns
+    for (int i = 0; i < kEpiWarps; ++i) mbar_init(input_bar(i), 1);
+    if constexpr (EIGHT)
+      for (int i = 0; i < kScaleRing; ++i) {
+        mbar_init(sfull_bar(i), 2);                   // both CTAs' scales
+        mbar_init(sempty_bar(i), 1);
+      }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  auto accumulator = [&](uint32_t acc) { return tmem_base + acc * (EIGHT ? kSecondAccumulator8 : 256u); };
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------ TMA producer (one per CTA)
+    if (lane == 0) {
+      Ring c{base, bars, abort_flag, 0u, 0u, 0u};
+      const uint32_t full0 = map_to_cta(full_bar(0), 0);
+      const uint32_t stage_tx = 2 * (kHalfBytes + kHalfBytes / 128 * uint32_t(L.half));
+      bool ok = true;
+      for (int t = pair_id; t < L.total_tiles && ok; t += num_pairs) {
+        const Tile tl = decode(L, t);
+        const TcProduct& p = L.p[tl.prob];
+        const int arow = tl.m0 + int(rank) * kRows;
+        const int brow = EPI == kGated ? tl.n0 : tl.n0 + int(rank) * L.half;
+        for (int seg = 0; seg < p.segments && ok; ++seg) {
+          const CUtensorMap* ma = &p.a[seg];
+          const CUtensorMap* mbm = EPI == kGated ? &p.b[rank] : &p.b[seg];
+          for (int kb = 0; kb < p.kblocks; ++kb, c.advance()) {
+            if (!mbar_wait(empty_bar(c.s), c.ph ^ 1u, abort_flag)) { ok = false; break; }
+            const uint32_t sa = base + c.s * kStageBytes, sb = sa + kHalfBytes;
+            if (leader_cta) mbar_expect_tx(full_bar(c.s), stage_tx);
+            const uint32_t fb = full0 + c.s * 8u;
+            const int k0 = kb * (EIGHT ? 128 : 64);
+            if constexpr (A_MN) {
+              tma_load_pair(sa, ma, fb, arow, k0);
+              tma_load_pair(sa + kHalfBytes / 2, ma, fb, arow + 64, k0);
+            } else {
+              tma_load_pair(sa, ma, fb, k0, arow);
+            }
+            if constexpr (B_MN && !EIGHT) {
+              tma_load_pair(sb, mbm, fb, brow, k0);
+              if (L.half == 128) tma_load_pair(sb + kHalfBytes / 2, mbm, fb, brow + 64, k0);
+            } else if constexpr (B_MN) {
+              tma_load_pair(sb, mbm, fb, brow, k0);
+            } else {
+              tma_load_pair(sb, mbm, fb, k0, brow);
+            }
+          }
+        }
+      }
+      if (!ok) give_up(31);
+      if (leader_cta) {   // every armed stage (both CTAs' bytes) has landed before shared memory is released
+        const uint32_t issued = c.it;
+        for (uint32_t j = (issued > kStages ? issued - kStages : 0); j < issued; ++j)
+          if (!mbar_wait(full_bar(j % kStages), (j / kStages) & 1u, abort_flag, false, WAIT_CYCLES / 8)) atomicExch(L.status, 32);
+      }
+      if (*abort_flag)    // loads this CTA issued for a stage the leader never armed: give them time to land
+        for (int i = 0; i < 64; ++i) __nanosleep(1000);
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ MMA issuer (leader CTA only)
+    if (lane == 0) {
+      if (leader_cta) {
+        Ring c{base, bars, abort_flag, 0u, 0u, 0u};
+        uint32_t tile_it = 0, group = 0;
+        bool ok = true;
+        constexpr uint64_t a_hi = A_MN ? kDescMN : kDescK, b_hi = B_MN ? kDescMN : kDescK;
+        // a step is 32 bytes of k: along a 128-byte row, or that many rows (16 of bf16, 32 of 8 bits) of 128 bytes
+        constexpr uint32_t a_step = A_MN ? 16 * 128 / 16 : 2, b_step = B_MN ? (EIGHT ? 32 : 16) * 128 / 16 : 2;
+        const uint32_t idesc = EIGHT ? make_idesc_scaled(B_MN, 2 * kRows, 2 * L.half) : make_idesc(B_MN, 2 * kRows, 2 * L.half, A_MN);
+        for (int t = pair_id; t < L.total_tiles && ok; t += num_pairs, ++tile_it) {
+          const TcProduct& p = L.p[decode(L, t).prob];
+          const uint32_t acc = tile_it & 1u, aph = (tile_it >> 1) & 1u;
+          const int num_kb = p.kblocks * p.segments;
+          if (!mbar_wait(tempty_bar(acc), aph ^ 1u, abort_flag)) { ok = false; break; }
+          if (EIGHT && tile_it > 0 && !mbar_wait(shared_bar, (tile_it - 1) & 1u, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t d_tmem = accumulator(acc);
+          for (int kb = 0; kb < num_kb; ++kb, c.advance()) {
+            if constexpr (EIGHT) {
+              if ((kb & 3) == 0) {
+                const uint32_t place = group % kScaleRing;
+                if (!mbar_wait(sfull_bar(place), (group / kScaleRing) & 1u, abort_flag)) { ok = false; break; }
+                asm volatile("fence.acq_rel.cluster;" ::: "memory");       // the peer's half of them, too
+                tc_fence_after();
+                const uint32_t from = (base + S::scale_off + place * kScaleBytes) >> 4;
+#pragma unroll
+                for (int i = 0; i < 3; ++i) tc_copy_scales_pair(tmem_base + kScaleCol + uint32_t(4 * i), kDescScales | uint64_t(from + uint32_t(i) * 32u));
+                tc_commit_pair(sempty_bar(place));
+                ++group;
+              }
+            }
+            if (!mbar_wait(full_bar(c.s), c.ph, abort_flag)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t a0 = (base + c.s * kStageBytes) >> 4, b0 = a0 + (kHalfBytes >> 4);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint64_t da = a_hi | uint64_t(a0 + uint32_t(k) * a_step), db = b_hi | uint64_t(b0 + uint32_t(k) * b_step);
+              const uint32_t more = (kb > 0 || k > 0) ? 1u : 0u;
+              if constexpr (EIGHT) tc_mma_pair_scaled(d_tmem, da, db, idesc | scale_byte_ids(uint32_t(kb & 3)), tmem_base + kScaleCol, tmem_base + kScaleCol + 4, more);
+              else tc_mma_pair(d_tmem, da, db, idesc, more);
+            }
+            tc_commit_pair(empty_bar(c.s));
+          }
+          if (ok) tc_commit_pair(tfull_bar(acc));
+        }
+        if (!ok) give_up(33);
+        tc_commit_pair(drain_bar);       // arrives in both CTAs once everything issued above has finished
+      }
+      if (!mbar_wait(drain_bar, 0, abort_flag, false, WAIT_CYCLES / 8)) atomicExch(L.status, 35);
+    }
+  } else if (EIGHT && warp == 2 + kEpiWarps) {
+    // ------------------------------------------------------------------ scales: four k-blocks at a time
+    if constexpr (EIGHT) {
+      uint32_t group = 0;
+      bool ok = true;
+      const uint32_t sfull0 = map_to_cta(sfull_bar(0), 0);
+      for (int t = pair_id; t < L.total_tiles && ok; t += num_pairs) {
+        const Tile tl = decode(L, t);
+        const TcProduct& p = L.p[tl.prob];
+        for (int kb = 0; kb < p.kblocks; kb += 4, ++group) {
+          const uint32_t place = group % kScaleRing;
+          if (!mbar_wait(sempty_bar(place), ((group / kScaleRing) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+          // lane i gathers rows i, i + 32, i + 64, i + 96 of each 128: a word of four blocks' bytes each
+          uint32_t w[3][4];
+#pragma unroll
+          for (int part = 0; part < 3; ++part)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const Scales& s = part ? p.sb : p.sa;
+              const int row = (part ? tl.n0 + (part - 1) * 128 : tl.m0 + int(rank) * kRows) + r * 32 + lane;
+              uint32_t v = 0;
+              if (row < s.rows) {
+                const uint8_t* q = s.p + int64_t(row >> s.row_shift) * s.row_step + int64_t(kb) * s.block_step;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  if (kb + j < p.kblocks) v |= uint32_t(__ldg(q + j * s.block_step)) << (8 * j);
+              }
+              w[part][r] = v;
+            }
+          const uint32_t to = base + S::scale_off + place * kScaleBytes + uint32_t(lane) * 16u;
+#pragma unroll
+          for (int part = 0; part < 3; ++part)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + uint32_t(part) * 512u), "r"(w[part][0]), "r"(w[part][1]), "r"(w[part][2]),
+                         "r"(w[part][3])
+                         : "memory");
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(sfull0 + place * 8u);
+        }
+      }
+      if (!ok && lane == 0) give_up(36);
+    }
+  } else {
+    // ------------------------------------------------------------------ epilogue warps (per CTA: its 128 rows)
+    const int ew = warp - 2, quad = warp & 3, part = ew >> 2;
+    Piece<S::pieces> out{base + S::epi_off + uint32_t(ew) * (S::pieces * kPieceBytes), 0u, lane};
+    const int chunks = (EPI == kGated ? L.half : 2 * L.half) / 64;
+    uint32_t tile_it = 0, iph = 0;
+    bool ok = true;
+    for (int t = pair_id; t < L.total_tiles && ok; t += num_pairs, ++tile_it) {
+      const Tile tl = decode(L, t);
+      const TcProduct& p = L.p[tl.prob];
+      const uint32_t acc = tile_it & 1u, aph = (tile_it >> 1) & 1u;
+      const uint32_t taddr = accumulator(acc) + (uint32_t(quad * 32) << 16);
+      const int row0 = tl.m0 + int(rank) * kRows + quad * 32, row = row0 + lane;
+      bool ready = false;
+      auto wait_tile = [&]() {
+        if (!ready) {
+          ready = mbar_wait(tfull_bar(acc), aph, abort_flag);
+          tc_fence_after();
+        }
+        return ready;
+      };
+      // two halves of the chunks, one for each warp of a quarter; 8 bits: the half that holds the shared columns (the end of the first accumulator, the
+      // beginning of the second) has them in its first chunk
+      const int per_part = chunks >= 2 ? chunks / 2 : 1;
+      const bool backwards = EIGHT && acc == 0;
+      for (int i = 0; i < per_part && part * per_part < chunks && ok; ++i) {
+        const int chunk = part * per_part + (backwards ? per_part - 1 - i : i);
+        const int col = tl.n0 + chunk * 64;
+        if constexpr (EPI == kPlain) {
+          if (!wait_tile()) { ok = false; break; }
+          uint32_t v[64], w[32];
+          load64(taddr + uint32_t(chunk * 64), v);
+          tc_wait_ld();
+          if (EIGHT && i == 0 && part == (acc == 0 ? 1 : 0)) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(map_to_cta(shared_bar, 0));
+          }
+#pragma unroll
+          for (int k = 0; k < 32; ++k) w[k] = pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
+          if (col < p.n && row0 < p.m) out.emit(&p.out[0], w, col, row0);
+        } else if constexpr (EPI == kGated) {
+          if (!wait_tile()) { ok = false; break; }
+          uint32_t g[64], u[64], w[32];
+          const uint32_t at = taddr + uint32_t(chunk * 64), up = uint32_t(L.half);
+          uint32_t eg = 0, eu = 0;
+          const bool eight = L.keep && L.gate_up_type == kTypeE4m3;
+          if (eight) {
+            eg = scale_byte(top_of_block(taddr));
+            eu = scale_byte(top_of_block(taddr + up));
+          }
+          load64(at, g);
+          load64(at + up, u);
+          tc_wait_ld();
+#pragma unroll
+          for (int k = 0; k < 32; ++k) {
+            float a[2], s;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) activate<true>(L.activation, __uint_as_float(g[2 * k + h]), &a[h], &s);
+            w[k] = pack2(a[0] * __uint_as_float(u[2 * k]), a[1] * __uint_as_float(u[2 * k + 1]));
+          }
+          if (col < p.n && row0 < p.m) {
+            out.emit(&p.out[0], w, col, row0);
+            if (eight) {
+              if (row < p.m) {
+                auto put = [&](const Operand& o, const uint32_t (&v)[64], uint32_t e) {
+                  store_codes(static_cast<uint8_t*>(const_cast<void*>(o.data)) + row * o.ld + col, v, inverse_scale_of(e), p.n - col, L.codes_wide != 0);
+                  if (part == 0) const_cast<uint8_t*>(o.scales)[row * o.lds + (col >> 7)] = uint8_t(e);
+                };
+                put(L.gate, g, eg);
+                put(L.up, u, eu);
+              }
+            } else if (L.keep) {
+#pragma unroll
+              for (int k = 0; k < 32; ++k) w[k] = pack2(__uint_as_float(g[2 * k]), __uint_as_float(g[2 * k + 1]));
+              out.emit(&p.out[1], w, col, row0);
+#pragma unroll
+              for (int k = 0; k < 32; ++k) w[k] = pack2(__uint_as_float(u[2 * k]), __uint_as_float(u[2 * k + 1]));
+              out.emit(&p.out[2], w, col, row0);
+            }
+          }
+        } else {
+          // g and u: by TMA into this warp's two buffers, or as 8 bits into registers, while the products still run.  dg and du then take the buffers.
+          const bool inside = col < p.n && row0 < p.m, eight = L.gate_up_type == kTypeE4m3;
+          uint32_t cg[16], cu[16];
+          float sg = 0.f, su = 0.f;
+          if (inside) {
+            if (lane == 0) tma_wait_read<0>();
+            __syncwarp();
+            if (eight) {
+#pragma unroll
+              for (int k = 0; k < 16; ++k) cg[k] = cu[k] = 0;
+              if (row < p.m) {
+                load_codes(static_cast<const uint8_t*>(L.gate.data) + row * L.gate.ld + col, cg, p.n - col, L.codes_wide != 0);
+                load_codes(static_cast<const uint8_t*>(L.up.data) + row * L.up.ld + col, cu, p.n - col, L.codes_wide != 0);
+                sg = scale_of(__ldg(L.gate.scales + row * L.gate.lds + (col >> 7)));
+                su = scale_of(__ldg(L.up.scales + row * L.up.lds + (col >> 7)));
+              }
+            } else if (lane == 0) {
+              mbar_expect_tx(input_bar(ew), 2 * kPieceBytes);
+              tma_load(out.buf, &p.in[0], input_bar(ew), col, row0);
+              tma_load(out.buf + kPieceBytes, &p.in[1], input_bar(ew), col, row0);
+            }
+          }
+          if (!wait_tile()) { ok = false; break; }
+          if (!inside) continue;
+          if (!eight) {
+            if (!mbar_wait(input_bar(ew), iph, abort_flag)) { ok = false; break; }
+            iph ^= 1u;
+          }
+          uint32_t v[64], w[32];
+          load64(taddr + uint32_t(chunk * 64), v);
+          tc_wait_ld();
+          const uint32_t line = out.buf + uint32_t(lane) * 128u;
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            uint32_t dg[4], du[4];
+            const uint32_t at = line + (uint32_t(q ^ (lane & 7)) << 4);
+            if (!eight) {
+              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(dg[0]), "=r"(dg[1]), "=r"(dg[2]), "=r"(dg[3]) : "r"(at));
+              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(du[0]), "=r"(du[1]), "=r"(du[2]), "=r"(du[3]) : "r"(at + kPieceBytes));
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int pair = q * 4 + k;
+              float2 g, u;
+              if (eight) {
+                g = values_of(cg[pair >> 1] >> (16 * (pair & 1)));
+                u = values_of(cu[pair >> 1] >> (16 * (pair & 1)));
+                g.x *= sg; g.y *= sg;
+                u.x *= su; u.y *= su;
+              } else {
+                g = make_float2(low(dg[k]), high(dg[k]));
+                u = make_float2(low(du[k]), high(du[k]));
+              }
+              const float d0 = __uint_as_float(v[2 * pair]), d1 = __uint_as_float(v[2 * pair + 1]);
+              float a0, a1, s0, s1;
+              activate<true>(L.activation, g.x, &a0, &s0);
+              activate<true>(L.activation, g.y, &a1, &s1);
+              dg[k] = pack2(d0 * u.x * s0, d1 * u.y * s1);
+              du[k] = pack2(d0 * a0, d1 * a1);
+              w[pair] = pack2(a0 * u.x, a1 * u.y);
+            }
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(dg[0]), "r"(dg[1]), "r"(dg[2]), "r"(dg[3]) : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + kPieceBytes), "r"(du[0]), "r"(du[1]), "r"(du[2]), "r"(du[3]) : "memory");
+          }
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            tma_store(&p.out[1], out.buf, col, row0);
+            tma_commit();
+            tma_store(&p.out[2], out.buf + kPieceBytes, col, row0);
+            tma_commit();
+          }
+          out.next = 0;
+          out.emit(&p.out[0], w, col, row0);
+        }
+      }
+      if (ok && !wait_tile()) ok = false;           // a warp without a chunk hands the accumulator back, too
+      if (!ok) break;
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(map_to_cta(tempty_bar(acc), 0));
+    }
+    if (lane == 0) {
+      tma_wait_all();                               // every store has landed before the CTA retires
+      if (!ok) {                                    // g and u may still be landing
+        for (int i = 0; i < 64; ++i) __nanosleep(1000);
+        give_up(34);
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();            // neither CTA retires while its peer may still signal its barriers or read its tiles
+  tc_fence_after();
+  if (warp == 1) {
+    __syncwarp();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------ host
+bool addressable(const void* p, int64_t ld, int elem) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * elem % 16 == 0 && ld * elem < (int64_t(1) << 40);
+}
+int elem_of(int type) { return type == kTypeBf16 ? 2 : 1; }
+
+struct Encoder {
+  muon_ctx* ctx;
+  bool ok = true;
+  void map(CUtensorMap* to, const void* data, int type, int64_t ld, int64_t cols, int64_t rows, uint32_t box_cols, uint32_t box_rows) {
+    const cuuint64_t dims[2] = {cuuint64_t(cols), cuuint64_t(rows)};
+    const cuuint64_t strides[1] = {cuuint64_t(ld * elem_of(type))};
+    const cuuint32_t box[2] = {box_cols, box_rows}, estr[2] = {1u, 1u};
+    ok = ok && reinterpret_cast<EncodeFn>(ctx->tmap_encode)(
+                   to, type == kTypeBf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(data), dims, strides, box, estr,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    ++ctx->tmap_encodes;
+  }
+  // `rows`: of the operand in a tile of a CTA
+  void operand(CUtensorMap* to, const Operand& o, int64_t n, int64_t k, uint32_t rows) {
+    const uint32_t line = 128 / uint32_t(elem_of(o.type));
+    if (o.mn_major) map(to, o.data, o.type, o.ld, n, k, line, line);
+    else map(to, o.data, o.type, o.ld, k, n, line, rows);
+  }
+  void piece(CUtensorMap* to, const void* data, int64_t ld, int64_t m, int64_t n) { map(to, data, kTypeBf16, ld, n, m, 64, 32); }
+};
+
+template <bool A_MN, bool B_MN, bool EIGHT, int EPI>
+int launch(const TcProducts& L, int device, int pairs, cudaStream_t st) {
+  static SharedMemoryLimit limit;
+  using S = Shape<EIGHT>;
+  if (!limit.raise(device, S::bytes, product_pair_kernel<A_MN, B_MN, EIGHT, EPI>)) return MUON_ERR_CUDA;
+  product_pair_kernel<A_MN, B_MN, EIGHT, EPI><<<unsigned(2 * std::min(L.total_tiles, pairs)), S::threads, S::bytes, st>>>(L);
+  return cudaGetLastError() == cudaSuccess ? 1 : MUON_ERR_CUDA;
+}
+
+Scales scales_of(const Operand& o, int rows) {
+  const int shift = o.block_rows == 1 ? 0 : 7;
+  if (o.mn_major) return {o.scales, 1, o.lds, 7, rows};       // the block of a column; blocks of rows are those of k
+  return {o.scales, o.lds, 1, shift, rows};
+}
+
+}  // namespace
+
+bool products_tc_take(const Product* list, int count) {
+  if (count < 1 || count > kMaxProducts) return false;
+  for (int i = 0; i < count; ++i) {
+    const Product& p = list[i];
+    const Epilogue& e = p.e;
+    const int type = p.a[0].type, ns = e.kind == kGated ? 2 : p.segments;
+    if (p.m < 1 || p.n < 1 || p.k < 1 || e.type != kTypeBf16 || e.kind != list[0].e.kind || type != list[0].a[0].type) return false;
+    if (type != kTypeBf16 && type != kTypeE4m3) return false;
+    for (int s = 0; s < ns; ++s) {
+      const Operand& b = p.b[s];
+      if (b.type != type || !addressable(b.data, b.ld, elem_of(type)) || b.mn_major != list[0].b[0].mn_major) return false;
+      if (b.type == kTypeE4m3 && b.mn_major && b.block_rows != kBlock) return false;
+    }
+    for (int s = 0; s < p.segments; ++s) {
+      const Operand& a = p.a[s];
+      if (a.type != type || !addressable(a.data, a.ld, elem_of(type)) || a.mn_major != list[0].a[0].mn_major) return false;
+    }
+    const bool amn = p.a[0].mn_major, bmn = p.b[0].mn_major;
+    if (type == kTypeE4m3 ? amn || e.kind != kPlain || p.segments != 1 : (e.kind == kGated && (amn || bmn)) || (e.kind == kGrad && (amn || !bmn)) || (amn && !bmn))
+      return false;
+    if (p.n % 8 || !addressable(e.c, e.ldc, 2)) return false;
+    if (e.kind == kGated && e.gate && (!addressable(e.gate, e.ld_gate, 2) || !addressable(e.up, e.ld_up, 2))) return false;
+    if (e.kind == kGrad) {
+      if (!addressable(e.gate, e.ld_gate, 2) || !addressable(e.up, e.ld_up, 2)) return false;
+      if (e.gate_up_type == kTypeBf16 && (!addressable(e.in_gate.data, e.in_gate.ld, 2) || !addressable(e.in_up.data, e.in_up.ld, 2))) return false;
+    }
+  }
+  return true;
+}
+
+int launch_products_tc(muon_ctx* ctx, const Product* list, int count, cudaStream_t st) {
+  const int sms = tc_pair_grid_setup(ctx->device);
+  if (sms < 0) return sms;
+  if (!ctx->tmap_encode) return MUON_ERR_CUDA;
+  TcProducts L = {};
+  const Epilogue& e0 = list[0].e;
+  const bool eight = list[0].a[0].type == kTypeE4m3, amn = list[0].a[0].mn_major, bmn = list[0].b[0].mn_major;
+  const bool codes = e0.gate_up_type == kTypeE4m3 && e0.kind != kPlain;
+  L.count = count;
+  L.half = 128;
+  L.activation = e0.activation;
+  L.gate_up_type = e0.gate_up_type;
+  L.keep = e0.kind == kGated && (e0.gate || codes);
+  L.gate = e0.in_gate;
+  L.up = e0.in_up;
+  L.codes_wide = codes && addressable(L.gate.data, L.gate.ld, 1) && addressable(L.up.data, L.up.ld, 1);
+  L.status = ctx->d_status;
+  Encoder enc = {ctx};
+  int64_t tiles = 0;
+  for (int i = 0; i < count; ++i) {
+    const Product& q = list[i];
+    TcProduct& p = L.p[i];
+    p.m = q.m;
+    p.n = q.n;
+    p.kblocks = (q.k + (eight ? 127 : 63)) / (eight ? 128 : 64);
+    p.segments = q.segments;
+    p.tile_cols = q.e.kind == kGated ? L.half : 2 * L.half;
+    p.tiles_m = (q.m + 2 * kRows - 1) / (2 * kRows);
+    p.tiles_n = (q.n + p.tile_cols - 1) / p.tile_cols;
+    p.tile_begin = int32_t(tiles);
+    tiles += int64_t(p.tiles_m) * p.tiles_n;
+    if (tiles > INT32_MAX - 4096) return MUON_ERR_UNSUPPORTED;
+    for (int s = 0; s < q.segments; ++s) enc.operand(&p.a[s], q.a[s], q.m, q.k, kRows);
+    for (int s = 0; s < (q.e.kind == kGated ? 2 : q.segments); ++s) enc.operand(&p.b[s], q.b[s], q.n, q.k, uint32_t(L.half));
+    enc.piece(&p.out[0], q.e.c, q.e.ldc, q.m, q.n);
+    if (q.e.kind == kGrad || (q.e.kind == kGated && q.e.gate)) {
+      enc.piece(&p.out[1], q.e.gate, q.e.ld_gate, q.m, q.n);
+      enc.piece(&p.out[2], q.e.up, q.e.ld_up, q.m, q.n);
+    }
+    if (q.e.kind == kGrad && !codes) {
+      enc.piece(&p.in[0], q.e.in_gate.data, q.e.in_gate.ld, q.m, q.n);
+      enc.piece(&p.in[1], q.e.in_up.data, q.e.in_up.ld, q.m, q.n);
+    }
+    if (eight) {
+      p.sa = scales_of(q.a[0], q.m);
+      p.sb = scales_of(q.b[0], q.n);
+    }
+  }
+  if (!enc.ok) return MUON_ERR_CUDA;
+  L.total_tiles = int32_t(tiles);
+  const int pairs = sms / 2, dev = ctx->device;
+  if (eight) return bmn ? launch<false, true, true, kPlain>(L, dev, pairs, st) : launch<false, false, true, kPlain>(L, dev, pairs, st);
+  if (e0.kind == kGated) return launch<false, false, false, kGated>(L, dev, pairs, st);
+  if (e0.kind == kGrad) return launch<false, true, false, kGrad>(L, dev, pairs, st);
+  if (amn) return launch<true, true, false, kPlain>(L, dev, pairs, st);
+  return bmn ? launch<false, true, false, kPlain>(L, dev, pairs, st) : launch<false, false, false, kPlain>(L, dev, pairs, st);
+}
+
+}  // namespace muon
