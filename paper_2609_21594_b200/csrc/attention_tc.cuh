@@ -134,26 +134,6 @@ __device__ __forceinline__ uint64_t exp2_poly(uint64_t v) {
   return mul2(p, two(__int_as_float(0x3f800000 + (__float_as_int(n.x) << 23)), __int_as_float(0x3f800000 + (__float_as_int(n.y) << 23))));
 }
 
-// The issuing warp runs converged, its warp index taken from lane 0 and every wait followed by a vote, and one elected lane issues: then
-// descriptors and addresses are values of the whole warp and stay in uniform registers.  A step has to take less than the 64 clocks that
-// its instruction keeps the tensor cores busy; issued from a branch on the lane it took 85, with descriptors formed anew each time 107.
-__device__ __forceinline__ bool elect_one() {
-  uint32_t one;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "elect.sync _|p, 0xffffffff;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(one));
-  return one != 0;
-}
-// Runs f on the elected lane.  Without the meeting behind it the other lanes go on to the next wait and share the issue slots with it.
-template <typename F>
-__device__ __forceinline__ void elected(bool go, F f) {
-  if (go && elect_one()) f();
-  __syncwarp();
-}
-__device__ __forceinline__ int uniform_warp() { return __shfl_sync(0xffffffffu, int(threadIdx.x >> 5), 0); }
-
 // Descriptors are formed once per tile: a step adds to the address field, which no address in shared memory carries out of.
 //
 // S[128 x 128] = X Y^T over the head: both tiles K-major.  `ksteps` steps of 16 elements cover head_dim.

@@ -10,7 +10,7 @@
 namespace muon {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kSquareThreads = 512;
 
 __device__ __forceinline__ uint32_t codes2(float lo, float hi) { return __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3); }
 __device__ __forceinline__ float2 values2(uint32_t pair) {
@@ -18,66 +18,84 @@ __device__ __forceinline__ float2 values2(uint32_t pair) {
   return __half22float2(__half2(h));
 }
 
-// Eight consecutive elements of a row; those from `left` on count as zeros.
-template <typename T, bool WIDE>
-__device__ __forceinline__ void load8(const T* p, int left, float (&v)[8]) {
-  if constexpr (WIDE) {
-    if (left >= 8) {
-      if constexpr (sizeof(T) == 2) {
-        const uint4 q = __ldg(reinterpret_cast<const uint4*>(p));
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+// Up to N consecutive elements of a row, by 16 bytes; those from `left` on count as zeros.
+template <typename T, int N>
+__device__ __forceinline__ void load_run(const T* p, int left, float (&v)[N]) {
+  if (left >= N) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[2 * i] = __uint_as_float(w[i] << 16);
-          v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    for (int q = 0; q < N * int(sizeof(T)) / 16; ++q) {
+      const uint4 x = __ldg(reinterpret_cast<const uint4*>(p) + q);
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 2) {
+          v[q * 8 + 2 * i] = __uint_as_float(w[i] << 16);
+          v[q * 8 + 2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        } else {
+          v[q * 4 + i] = __uint_as_float(w[i]);
         }
-      } else {
-        const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
       }
-      return;
     }
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = i < left ? float(p[i]) : 0.f;
-}
-
-template <bool WIDE>
-__device__ __forceinline__ void store8(uint8_t* p, int left, const float (&v)[8], float inverse) {
-  uint32_t c[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) c[i] = codes2(infinite_to_nan(v[2 * i]) * inverse, infinite_to_nan(v[2 * i + 1]) * inverse);
-  if (WIDE && left >= 8) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (i < left) p[i] = uint8_t(c[i >> 1] >> (8 * (i & 1)));
+  for (int i = 0; i < N; ++i) v[i] = i < left ? float(p[i]) : 0.f;
+}
+// Their codes; `odd`: infinities among them become NaN (the conversion would make them the largest code).
+template <int N>
+__device__ __forceinline__ void store_run(uint8_t* p, int left, const float (&v)[N], float inverse, bool odd) {
+  uint32_t c[N / 4];
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) {
+    float x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = (odd ? infinite_to_nan(v[4 * i + k]) : v[4 * i + k]) * inverse;
+    c[i] = codes2(x[0], x[1]) | codes2(x[2], x[3]) << 16;
+  }
+  if (left >= N) {
+    if constexpr (N == 16) *reinterpret_cast<uint4*>(p) = make_uint4(c[0], c[1], c[2], c[3]);
+    else *reinterpret_cast<uint2*>(p) = make_uint2(c[0], c[1]);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (i < left) p[i] = uint8_t(c[i >> 2] >> (8 * (i & 3)));
+}
+// The bits of the largest finite magnitude.  The plain maximum passes over NaN; only an infinity makes it look at every value again.
+template <int N>
+__device__ __forceinline__ uint32_t finite_top(const float (&v)[N], bool* odd) {
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(v[i]));
+  uint32_t bits = __float_as_uint(top);
+  *odd = bits == 0x7f800000u;
+  if (*odd) {
+    bits = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) bits = max(bits, finite_bits(v[i]));
+  }
+  return bits;
 }
 
-// Blocks of 1 x 128: sixteen lanes hold a block, eight elements each, and find its largest magnitude by shuffles.  Blocks are counted along the rows,
-// one row after the other; a group of lanes takes UNROLL consecutive ones, so that its loads are in flight together and the division that
-// finds the row is made once.
-template <typename T, bool WIDE, int UNROLL>
+// Blocks of 1 x 128: eight lanes hold a block, sixteen elements each, and find its largest magnitude by shuffles.  Blocks are counted along the
+// rows, one row after the other; a group of lanes takes UNROLL consecutive ones, so that its loads are in flight together and the division
+// that finds the row is made once.
+template <typename T, int UNROLL>
 __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const T* x, int64_t ldx, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds,
-                                                                 int64_t rows, int32_t cols) {
-  const int64_t per_row = (cols + kBlock - 1) / kBlock, total = rows * per_row;
-  const int sub = threadIdx.x & 15;
-  const int64_t first = (int64_t(blockIdx.x) * (kThreads / 16) + (threadIdx.x >> 4)) * UNROLL;
-  int64_t row = first < total ? first / per_row : rows;
-  int32_t blk = first < total ? int32_t(first - row * per_row) : 0;
-  float v[UNROLL][8];
+                                                                 int64_t rows, int32_t cols, uint32_t per_row) {
+  const int sub = threadIdx.x & 7;
+  const int64_t first = (int64_t(blockIdx.x) * (kThreads / 8) + (threadIdx.x >> 3)) * UNROLL;
+  int64_t row = first <= UINT32_MAX ? int64_t(uint32_t(first) / per_row) : first / per_row;
+  uint32_t blk = uint32_t(first - row * per_row);
+  float v[UNROLL][16];
   int64_t at_row[UNROLL];
-  int32_t at_blk[UNROLL];
+  uint32_t at_blk[UNROLL];
 #pragma unroll
   for (int u = 0; u < UNROLL; ++u) {
     at_row[u] = row;
     at_blk[u] = blk;
-    const int col = blk * kBlock + sub * 8;
-    const int left = row < rows ? cols - col : 0;
-    load8<T, WIDE>(x + row * ldx + col, left, v[u]);
+    const int col = int(blk) * kBlock + sub * 16;
+    load_run(x + row * ldx + col, row < rows ? cols - col : 0, v[u]);
     if (++blk == per_row) {
       blk = 0;
       ++row;
@@ -85,81 +103,159 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const T* x, int
   }
 #pragma unroll
   for (int u = 0; u < UNROLL; ++u) {
-    uint32_t top = 0;
+    bool odd;
+    uint32_t top = finite_top(v[u], &odd);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, finite_bits(v[u][i]));
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+    for (int d = 1; d < 8; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
     if (at_row[u] >= rows) continue;
     const uint32_t e = scale_byte(top);
-    const int col = at_blk[u] * kBlock + sub * 8;
-    store8<WIDE>(codes + at_row[u] * ldc + col, cols - col, v[u], inverse_scale_of(e));
+    const int col = int(at_blk[u]) * kBlock + sub * 16;
+    store_run(codes + at_row[u] * ldc + col, cols - col, v[u], inverse_scale_of(e), odd);
     if (sub == 0) scales[at_row[u] * lds + at_blk[u]] = uint8_t(e);
   }
 }
 
-// Blocks of 128 x 128: a thread block each, 64 elements a thread kept in registers between the maximum and the rounding.
+// The same for rows that no wide load fits: a warp per block, a lane takes elements l, l + 32, l + 64, l + 96.
+template <typename T, int UNROLL>
+__global__ void __launch_bounds__(kThreads) quantize_rows_any_kernel(const T* x, int64_t ldx, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds,
+                                                                     int64_t rows, int32_t cols, uint32_t per_row) {
+  const int lane = threadIdx.x & 31;
+  const int64_t first = (int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * UNROLL;
+  int64_t row = first / per_row;
+  uint32_t blk = uint32_t(first - row * per_row);
+  float v[UNROLL][4];
+  int64_t at_row[UNROLL];
+  uint32_t at_blk[UNROLL];
+#pragma unroll
+  for (int u = 0; u < UNROLL; ++u) {
+    at_row[u] = row;
+    at_blk[u] = blk;
+    const T* p = x + row * ldx + int64_t(blk) * kBlock + lane;
+    const int left = row < rows ? cols - int(blk) * kBlock - lane : 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[u][j] = 32 * j < left ? float(p[32 * j]) : 0.f;
+    if (++blk == per_row) {
+      blk = 0;
+      ++row;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < UNROLL; ++u) {
+    bool odd;
+    const uint32_t top = __reduce_max_sync(0xffffffffu, finite_top(v[u], &odd));
+    if (at_row[u] >= rows) continue;
+    const uint32_t e = scale_byte(top);
+    const float inverse = inverse_scale_of(e);
+    uint8_t* p = codes + at_row[u] * ldc + int64_t(at_blk[u]) * kBlock + lane;
+    const int left = cols - int(at_blk[u]) * kBlock - lane;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (32 * j < left) p[32 * j] = uint8_t(codes2(infinite_to_nan(v[u][j]) * inverse, 0.f));
+    if (lane == 0) scales[at_row[u] * lds + at_blk[u]] = uint8_t(e);
+  }
+}
+
+// Blocks of 128 x 128: a thread block each, 32 elements a thread kept in registers between the maximum and the rounding.  WIDE: sixteen lanes to a
+// row, eight elements each; else a warp to a row, elements 32 apart.
 template <typename T, bool WIDE>
-__global__ void __launch_bounds__(kThreads) quantize_squares_kernel(const T* x, int64_t ldx, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds,
+__global__ void __launch_bounds__(kSquareThreads) quantize_squares_kernel(const T* x, int64_t ldx, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds,
                                                                     int64_t rows, int32_t cols) {
-  __shared__ uint32_t tops[kThreads / 32];
+  __shared__ uint32_t tops[kSquareThreads / 32];
+  constexpr int kPer = WIDE ? 8 : 4, kTimes = kBlock * kBlock / kSquareThreads / kPer, kStride = kBlock / kTimes;      // elements of a row, rows of a thread and between them
   const int64_t per_row = (cols + kBlock - 1) / kBlock;
   const int64_t brow = int64_t(blockIdx.x) / per_row;
   const int bcol = int(int64_t(blockIdx.x) - brow * per_row);
-  const int64_t row0 = brow * kBlock + (threadIdx.x >> 4);
-  const int col = bcol * kBlock + (threadIdx.x & 15) * 8;
-  float v[8][8];
+  const int64_t row0 = brow * kBlock + (WIDE ? threadIdx.x >> 4 : threadIdx.x >> 5);
+  const int col = bcol * kBlock + (WIDE ? int(threadIdx.x & 15) * 8 : int(threadIdx.x & 31));
+  float v[kTimes][kPer];
   uint32_t top = 0;
+  bool odd = false;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) load8<T, WIDE>(x + (row0 + 16 * i) * ldx + col, row0 + 16 * i < rows ? cols - col : 0, v[i]);
+  for (int i = 0; i < kTimes; ++i) {
+    const int64_t row = row0 + kStride * i;
+    const int left = row < rows ? cols - col : 0;
+    if constexpr (WIDE) {
+      load_run(x + row * ldx + col, left, v[i]);
+    } else {
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+      for (int j = 0; j < kPer; ++j) v[i][j] = 32 * j < left ? float(x[row * ldx + col + 32 * j]) : 0.f;
+    }
+  }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, finite_bits(v[i][j]));
+  for (int i = 0; i < kTimes; ++i) {
+    bool some;
+    top = max(top, finite_top(v[i], &some));
+    odd |= some;
+  }
   top = __reduce_max_sync(0xffffffffu, top);
   if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kThreads / 32; ++i) top = max(top, tops[i]);
+  for (int i = 0; i < kSquareThreads / 32; ++i) top = max(top, tops[i]);
   const uint32_t e = scale_byte(top);
   const float inverse = inverse_scale_of(e);
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (row0 + 16 * i < rows) store8<WIDE>(codes + (row0 + 16 * i) * ldc + col, cols - col, v[i], inverse);
+  for (int i = 0; i < kTimes; ++i) {
+    const int64_t row = row0 + kStride * i;
+    if (row >= rows) break;
+    uint8_t* p = codes + row * ldc + col;
+    if constexpr (WIDE) {
+      store_run(p, cols - col, v[i], inverse, odd);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kPer; ++j)
+        if (32 * j < cols - col) p[32 * j] = uint8_t(codes2(infinite_to_nan(v[i][j]) * inverse, 0.f));
+    }
+  }
   if (threadIdx.x == 0) scales[brow * lds + bcol] = uint8_t(e);
 }
 
-// Sixteen codes a thread: they lie in one block.
-template <typename T, bool WIDE>
+// Sixteen codes at a time, which lie in one block; a thread takes UNROLL of them, a block of threads apart.
+template <typename T, int UNROLL>
 __global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int32_t row_shift, T* y,
-                                                              int64_t ldy, int64_t rows, int32_t cols) {
-  const int64_t per_row = (cols + 15) / 16;
-  const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-  const int64_t row = i / per_row;
-  if (row >= rows) return;
-  const int col = int(i - row * per_row) * 16;
-  const int left = cols - col;
-  const uint8_t* p = codes + row * ldc + col;
-  T* out = y + row * ldy + col;
-  const float scale = scale_of(__ldg(scales + (row >> row_shift) * lds + (col >> 7)));
-  uint32_t w[4] = {0, 0, 0, 0};
-  if (WIDE && left >= 16) {
-    const uint4 q = __ldg(reinterpret_cast<const uint4*>(p));
-    w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
-  } else {
+                                                              int64_t ldy, int64_t rows, int32_t cols, uint32_t per_row) {
+  const int64_t first = int64_t(blockIdx.x) * (kThreads * UNROLL) + threadIdx.x;
+  uint4 in[UNROLL];
+  uint8_t e[UNROLL];
+  int64_t row[UNROLL];
+  int col[UNROLL];
 #pragma unroll
-    for (int k = 0; k < 16; ++k)
-      if (k < left) w[k >> 2] |= uint32_t(p[k]) << (8 * (k & 3));
-  }
-  float v[16];
+  for (int u = 0; u < UNROLL; ++u) {
+    const int64_t i = first + u * kThreads;
+    row[u] = i <= UINT32_MAX ? int64_t(uint32_t(i) / per_row) : i / per_row;
+    col[u] = int(i - row[u] * per_row) * 16;
+    if (row[u] >= rows) continue;
+    const uint8_t* p = codes + row[u] * ldc + col[u];
+    e[u] = __ldg(scales + (row[u] >> row_shift) * lds + (col[u] >> 7));
+    if (cols - col[u] >= 16) {
+      in[u] = __ldg(reinterpret_cast<const uint4*>(p));
+    } else {
+      uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const float2 f = values2(w[k >> 1] >> (16 * (k & 1)));
-    v[2 * k] = f.x * scale;
-    v[2 * k + 1] = f.y * scale;
+      for (int k = 0; k < 16; ++k)
+        if (k < cols - col[u]) w[k >> 2] |= uint32_t(p[k]) << (8 * (k & 3));
+      in[u] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
   }
-  if (WIDE && left >= 16) {
-    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+  for (int u = 0; u < UNROLL; ++u) {
+    if (row[u] >= rows) break;
+    const float scale = scale_of(e[u]);
+    const int left = cols - col[u];
+    T* out = y + row[u] * ldy + col[u];
+    const uint32_t w[4] = {in[u].x, in[u].y, in[u].z, in[u].w};
+    float v[16];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float2 f = values2(w[k >> 1] >> (16 * (k & 1)));
+      v[2 * k] = f.x * scale;
+      v[2 * k + 1] = f.y * scale;
+    }
+    if (left < 16) {
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+        if (k < left) out[k] = T(v[k]);
+    } else if constexpr (sizeof(T) == 2) {
       uint32_t o[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
@@ -172,11 +268,40 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint8_t* cod
 #pragma unroll
       for (int k = 0; k < 4; ++k) reinterpret_cast<float4*>(out)[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
     }
-    return;
+  }
+}
+
+// Rows that no wide access fits: a warp takes 128 columns, a lane elements l, l + 32, l + 64, l + 96, so that each access of the warp is one run.
+template <typename T, int UNROLL>
+__global__ void __launch_bounds__(kThreads) dequantize_any_kernel(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int32_t row_shift,
+                                                                  T* y, int64_t ldy, int64_t rows, int32_t cols, uint32_t per_row) {
+  const int lane = threadIdx.x & 31;
+  const int64_t first = (int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * UNROLL;
+  int64_t row = first / per_row;
+  uint32_t blk = uint32_t(first - row * per_row);
+  uint8_t c[UNROLL][4], e[UNROLL];
+  T* out[UNROLL];
+  int left[UNROLL];
+#pragma unroll
+  for (int u = 0; u < UNROLL; ++u) {
+    left[u] = row < rows ? cols - int(blk) * kBlock - lane : 0;
+    out[u] = y + row * ldy + int64_t(blk) * kBlock + lane;
+    const uint8_t* p = codes + row * ldc + int64_t(blk) * kBlock + lane;
+    e[u] = row < rows ? __ldg(scales + (row >> row_shift) * lds + blk) : 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c[u][j] = 32 * j < left[u] ? __ldg(p + 32 * j) : 0;
+    if (++blk == per_row) {
+      blk = 0;
+      ++row;
+    }
   }
 #pragma unroll
-  for (int k = 0; k < 16; ++k)
-    if (k < left) out[k] = T(v[k]);
+  for (int u = 0; u < UNROLL; ++u) {
+    const float scale = scale_of(e[u]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (32 * j < left[u]) out[u][32 * j] = T(values2(c[u][j]).x * scale);
+  }
 }
 
 bool wide(const void* p, int64_t ld_bytes, int align) { return reinterpret_cast<uintptr_t>(p) % align == 0 && ld_bytes % align == 0; }
@@ -186,19 +311,19 @@ template <typename T>
 int quantize(int64_t rows, int64_t cols, const T* x, int64_t ldx, const Operand& out, cudaStream_t st) {
   uint8_t* codes = const_cast<uint8_t*>(static_cast<const uint8_t*>(out.data));
   uint8_t* scales = const_cast<uint8_t*>(out.scales);
-  const bool w = wide(x, ldx * int64_t(sizeof(T)), 16) && wide(codes, out.ld, 8);
+  const bool w = wide(x, ldx * int64_t(sizeof(T)), 16) && wide(codes, out.ld, 16);
   const int64_t per_row = (cols + kBlock - 1) / kBlock;
   if (out.block_rows == 1) {
-    constexpr int kUnroll = 4;
-    const int64_t per_block = int64_t(kThreads / 16) * kUnroll, blocks = (rows * per_row + per_block - 1) / per_block;
+    constexpr int kUnroll = sizeof(T) == 2 ? 2 : 1, kAnyUnroll = 4;
+    const int64_t per_block = w ? int64_t(kThreads / 8) * kUnroll : int64_t(kThreads / 32) * kAnyUnroll, blocks = (rows * per_row + per_block - 1) / per_block;
     if (blocks > INT32_MAX) return MUON_ERR_UNSUPPORTED;
-    auto* k = w ? quantize_rows_kernel<T, true, kUnroll> : quantize_rows_kernel<T, false, kUnroll>;
-    k<<<unsigned(blocks), kThreads, 0, st>>>(x, ldx, codes, out.ld, scales, out.lds, rows, int32_t(cols));
+    auto* k = w ? quantize_rows_kernel<T, kUnroll> : quantize_rows_any_kernel<T, kAnyUnroll>;
+    k<<<unsigned(blocks), kThreads, 0, st>>>(x, ldx, codes, out.ld, scales, out.lds, rows, int32_t(cols), uint32_t(per_row));
   } else {
     const int64_t blocks = (rows + kBlock - 1) / kBlock * per_row;
     if (blocks > INT32_MAX) return MUON_ERR_UNSUPPORTED;
     auto* k = w ? quantize_squares_kernel<T, true> : quantize_squares_kernel<T, false>;
-    k<<<unsigned(blocks), kThreads, 0, st>>>(x, ldx, codes, out.ld, scales, out.lds, rows, int32_t(cols));
+    k<<<unsigned(blocks), kSquareThreads, 0, st>>>(x, ldx, codes, out.ld, scales, out.lds, rows, int32_t(cols));
   }
   return done(1);
 }
@@ -206,11 +331,13 @@ int quantize(int64_t rows, int64_t cols, const T* x, int64_t ldx, const Operand&
 template <typename T>
 int dequantize(int64_t rows, int64_t cols, const Operand& in, T* y, int64_t ldy, cudaStream_t st) {
   const uint8_t* codes = static_cast<const uint8_t*>(in.data);
-  const int64_t blocks = (rows * ((cols + 15) / 16) + kThreads - 1) / kThreads;
-  if (blocks > INT32_MAX) return MUON_ERR_UNSUPPORTED;
+  constexpr int kUnroll = 2, kAnyUnroll = 4;
   const bool w = wide(codes, in.ld, 16) && wide(y, ldy * int64_t(sizeof(T)), 16);
-  auto* k = w ? dequantize_kernel<T, true> : dequantize_kernel<T, false>;
-  k<<<unsigned(blocks), kThreads, 0, st>>>(codes, in.ld, in.scales, in.lds, in.block_rows == 1 ? 0 : 7, y, ldy, rows, int32_t(cols));
+  const int64_t per_row = w ? (cols + 15) / 16 : (cols + kBlock - 1) / kBlock;
+  const int64_t per_block = w ? kThreads * kUnroll : kThreads / 32 * kAnyUnroll, blocks = (rows * per_row + per_block - 1) / per_block;
+  if (blocks > INT32_MAX) return MUON_ERR_UNSUPPORTED;
+  auto* k = w ? dequantize_kernel<T, kUnroll> : dequantize_any_kernel<T, kAnyUnroll>;
+  k<<<unsigned(blocks), kThreads, 0, st>>>(codes, in.ld, in.scales, in.lds, in.block_rows == 1 ? 0 : 7, y, ldy, rows, int32_t(cols), uint32_t(per_row));
   return done(1);
 }
 

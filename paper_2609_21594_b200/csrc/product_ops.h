@@ -79,21 +79,27 @@ __device__ __forceinline__ uint32_t finite_bits(float x) {
 }
 __device__ __forceinline__ float infinite_to_nan(float x) { return (__float_as_uint(x) & 0x7fffffffu) < 0x7f800000u ? x : __uint_as_float(0x7fffffffu); }
 
-// act(g) = g s(w(g)) with the logistic function s:  silu: w = g;  gelu (tanh form, (1 + tanh z) / 2 = s(2z)): w = 2 sqrt(2 / pi) (g + 0.044715 g^3).
-// act'(g) = s + g s (1 - s) w'(g).  FAST: the exponential and the quotient of the special-function unit (2^-21 relative), for results that are
-// rounded to bf16.
+// act(g) = g s(w(g)) with the logistic function s and w = k g (1 + c g^2):  silu: k = 1, c = 0;  gelu (tanh form, (1 + tanh z) / 2 = s(2z)):
+// k = 2 sqrt(2 / pi), c = 0.044715.  act'(g) = s + g s (1 - s) w'(g).  Both forms cost the same instructions: a branch between them, taken for
+// every element, keeps the exponentials of neighbouring elements from overlapping.
+struct Activation {
+  float k, c;
+};
+__device__ __forceinline__ Activation activation_of(int kind) { return kind == MUON_ACTIVATION_GELU ? Activation{1.5957691216057308f, 0.044715f} : Activation{1.f, 0.f}; }
+// FAST: the exponential and the reciprocal of the special-function unit (2^-21 relative), for results that are rounded to bf16.
 template <bool FAST>
-__device__ __forceinline__ void activate(int activation, float g, float* a, float* slope) {
-  float w = g, dw = 1.f;
-  if (activation == MUON_ACTIVATION_GELU) {
-    constexpr float k = 1.5957691216057308f, c = 0.044715f;
-    const float g2 = fminf(g * g, 1e12f);     // beyond, s is 0 or 1 and 0 times w' has to stay 0
-    w = k * g * fmaf(c, g2, 1.f);
-    dw = k * fmaf(3.f * c, g2, 1.f);
+__device__ __forceinline__ void activate(const Activation& f, float g, float* a, float* slope) {
+  const float g2 = fminf(g * g, 1e12f);       // beyond, s is 0 or 1, and 0 times w' has to stay 0
+  const float w = f.k * g * fmaf(f.c, g2, 1.f), dw = f.k * fmaf(3.f * f.c, g2, 1.f);
+  float s;
+  if constexpr (FAST) {
+    const float t = 1.f + __expf(-w);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(t));
+  } else {
+    s = 1.f / (1.f + expf(-w));
   }
-  const float s = FAST ? __fdividef(1.f, 1.f + __expf(-w)) : 1.f / (1.f + expf(-w));
   *a = g * s;
-  *slope = fmaf(g * s * (1.f - s), dw, s);
+  *slope = fmaf(*a * (1.f - s), dw, s);
 }
 #endif
 

@@ -124,6 +124,7 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
     __syncthreads();
   }
   const Epilogue& e = p.e;
+  const Activation f = activation_of(e.activation);
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int64_t row = m0 + (i / H) * (TILE / 2) + ty * H + i % H;
@@ -131,9 +132,9 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
     float v[R];
 #pragma unroll
     for (int j = 0; j < H; ++j) {
-      const float2 f = both(acc[i][j]);
-      v[2 * j] = f.x;
-      v[2 * j + 1] = f.y;
+      const float2 pair = both(acc[i][j]);
+      v[2 * j] = pair.x;
+      v[2 * j + 1] = pair.y;
     }
     if (gated) {                            // v[0, H) are g and v[H, R) u of the same columns
 #pragma unroll
@@ -141,7 +142,7 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
         const int64_t col = n0 + tx * H + j;
         if (col >= p.n) continue;
         float a, slope;
-        activate<false>(e.activation, v[j], &a, &slope);
+        activate<false>(f, v[j], &a, &slope);
         put(e.c, e.type, row * e.ldc + col, a * v[H + j]);
         if (e.gate) {
           put(e.gate, e.gate_up_type, row * e.ld_gate + col, v[j]);
@@ -160,7 +161,7 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
       }
       const float g = element_of(e.in_gate, row, col), u = element_of(e.in_up, row, col);
       float a, slope;
-      activate<false>(e.activation, g, &a, &slope);
+      activate<false>(f, g, &a, &slope);
       put(e.gate, e.type, row * e.ld_gate + col, v[j] * u * slope);
       put(e.up, e.type, row * e.ld_up + col, v[j] * a);
       put(e.c, e.type, row * e.ldc + col, a * u);

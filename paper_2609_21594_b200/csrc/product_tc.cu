@@ -6,7 +6,7 @@
 // leader (r = 0) issues tcgen05.mma.cta_group::2 of 256 x N.  Operands come by TMA as they lie in memory, K-major or MN-major (summed
 // over the rows: the backward products need no transposed copy).  Accumulators alternate between two places in tensor memory, so that a
 // tile's epilogue runs under the next tile's products.  Eight epilogue warps, two per quarter of the rows; a thread holds 64 columns of one
-// row at a time and hands them to TMA through 4 KiB of its warp's own, so that epilogue warps never wait for one another.
+// row at a time and reads and writes memory itself, 32 bytes (a sector) at a time.
 //
 // Gated product: the leader's half of B is 128 rows of w_gate and its peer's the same rows of w_up, so columns [0, 128) of the accumulator are g
 // and [128, 256) are u of the same elements: one thread holds both, and 128 columns of g are one block of the 8-bit form.
@@ -31,11 +31,10 @@ namespace {
 using namespace tc;
 
 constexpr int kRows = 128;                     // of A per CTA
-constexpr int kStages = 5;
+constexpr int kStages = 6;
 constexpr uint32_t kHalfBytes = kRows * 128;   // 16 KiB: 128 rows of 128 bytes
 constexpr uint32_t kStageBytes = 2 * kHalfBytes;
 constexpr int kEpiWarps = 8;
-constexpr uint32_t kPieceBytes = 32 * 128;     // what an epilogue warp hands over at once: 32 rows of 64 bf16
 constexpr int kGroupTiles = 8;                 // tiles of rows that a stretch of the tile list stays in: what they and as many columns read fits L2
 constexpr int kScaleRing = 4;                  // groups of four k-blocks whose scales are on their way
 constexpr uint32_t kScaleBytes = 3 * 512;      // of a group: 128 rows of A, 256 of B, four bytes each
@@ -44,9 +43,7 @@ constexpr uint32_t kSecondAccumulator8 = 240;
 
 template <bool EIGHT>
 struct Shape {
-  static constexpr int pieces = EIGHT ? 1 : 2; // buffers per epilogue warp
-  static constexpr uint32_t epi_off = kStages * kStageBytes;
-  static constexpr uint32_t scale_off = epi_off + kEpiWarps * pieces * kPieceBytes;
+  static constexpr uint32_t scale_off = kStages * kStageBytes;
   static constexpr uint32_t bar_off = scale_off + (EIGHT ? kScaleRing * kScaleBytes : 0);
   static constexpr uint32_t bytes = bar_off + 512 + 1024;
   static constexpr int threads = 32 * (2 + kEpiWarps + (EIGHT ? 1 : 0));
@@ -57,11 +54,14 @@ struct Scales {                                // of an operand: the byte of (ro
   const uint8_t* p;
   int64_t row_step, block_step;
   int32_t row_shift, rows;
+  int32_t words;                               // four blocks' bytes are an aligned word
 };
 struct TcProduct {
   CUtensorMap a[2], b[2];
-  CUtensorMap out[3];                          // C; or h, g, u; or h, dg, du
-  CUtensorMap in[2];                           // g, u
+  __nv_bfloat16* out[3];                       // C; or h, g, u; or h, dg, du
+  int64_t ld[3];
+  const __nv_bfloat16* in[2];                  // g, u
+  int64_t ld_in[2];
   Scales sa, sb;
   int32_t m, n, kblocks, segments;             // kblocks: of a segment
   int32_t tiles_m, tiles_n, tile_begin;
@@ -71,9 +71,10 @@ struct TcProducts {
   TcProduct p[kMaxProducts];
   int32_t count, total_tiles;
   int32_t half;                                // columns of B per CTA: 128 or 64
-  int32_t activation, gate_up_type, keep;      // keep: g and u are written
+  int32_t activation, keep;                    // keep: g and u are written
   Operand gate, up;                            // 8-bit g and u
   int32_t codes_wide;                          // their rows take 16-byte accesses
+  int32_t sectors;                             // all bf16 rows begin on a 32-byte sector
   int32_t* status;
 };
 
@@ -95,6 +96,22 @@ __device__ __forceinline__ void cluster_sync_all() {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
+// mbar_wait on what threads of the peer CTA wrote before they arrived.
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  const long long t0 = clock64();
+  for (uint32_t spins = 1;; ++spins) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    if (ok) return true;
+    if ((spins & 255u) == 0 && (*abort_flag || clock64() - t0 > WAIT_CYCLES)) return false;
+  }
+}
 __device__ __forceinline__ void st_cluster_u32(uint32_t cluster_addr, uint32_t v) {
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr), "r"(v) : "memory");
 }
@@ -104,14 +121,15 @@ __device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* m
       ::"r"(dst), "l"(map), "r"(bar_cluster_addr), "r"(x), "r"(y)
       : "memory");
 }
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-      ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y)
-      : "memory");
+__device__ __forceinline__ void store32(void* p, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]),
+               "r"(w[6]), "r"(w[7])
+               : "memory");
 }
-__device__ __forceinline__ void tma_store(const CUtensorMap* map, uint32_t src, int x, int y) {
-  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(src), "r"(x), "r"(y) : "memory");
+__device__ __forceinline__ void load32(const void* p, uint32_t* w) {
+  asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+               : "l"(p));
 }
 __device__ __forceinline__ void tc_mma_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -163,6 +181,39 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 __device__ __forceinline__ float low(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float high(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
 
+// The bytes of k-blocks kb to kb + 3 (0 past the last) for rows `row`, + 32, + 64, + 96 of an operand.  Rows of 128 x 128 blocks share theirs, and bytes
+// that lie together come as a word; otherwise all loads are issued before the first is waited for.
+__device__ __forceinline__ void gather_scales(const Scales& s, int row, int kb, int kblocks, uint32_t (&w)[4]) {
+  const bool shared = s.row_shift != 0, word = s.words && kb + 4 <= kblocks;
+  const uint8_t* base = s.p + int64_t(kb) * s.block_step;
+  uint32_t v[4][4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const uint8_t* q = base + int64_t(min(row + 32 * r, s.rows - 1) >> s.row_shift) * s.row_step;
+    if (shared && r > 0) continue;
+    if (word) {
+      v[r][0] = __ldg(reinterpret_cast<const uint32_t*>(q));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[r][j] = __ldg(q + int64_t(min(j, kblocks - 1 - kb)) * s.block_step);
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    uint32_t x = v[r][0];
+    if (shared && r > 0) {
+      w[r] = w[0];
+      continue;
+    }
+    if (!word) {
+#pragma unroll
+      for (int j = 1; j < 4; ++j)
+        if (kb + j < kblocks) x |= v[r][j] << (8 * j);
+    }
+    w[r] = x;
+  }
+}
+
 // ------------------------------------------------------------------ tiles
 struct Tile {
   int prob, m0, n0;                            // first row of the pair, first column of C
@@ -198,31 +249,20 @@ struct Ring {
 };
 
 // ------------------------------------------------------------------ epilogue
-// One epilogue warp's 32 rows.  `emit` hands 64 columns, two to a word, to TMA.
-template <int PIECES>
-struct Piece {
-  uint32_t buf;                                // this warp's shared memory
-  uint32_t next;                               // buffer to use
-  int lane;
-  __device__ __forceinline__ void emit(const CUtensorMap* map, const uint32_t (&w)[32], int col, int row) {
-    const uint32_t at = buf + next * kPieceBytes;
-    if (lane == 0) tma_wait_read<PIECES - 1>();          // what was last stored from this buffer has been read
-    __syncwarp();
-    const uint32_t line = at + uint32_t(lane) * 128u;
+// 16 columns (two to a word) of a row of bf16, of which `left`, a multiple of 8, are inside.
+__device__ __forceinline__ void put16(__nv_bfloat16* p, const uint32_t* w, int left, bool sectors) {
+  if (left >= 16 && sectors) return store32(p, w);
+  if (left >= 8) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  if (left >= 16) *reinterpret_cast<uint4*>(p + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+}
+__device__ __forceinline__ void get16(const __nv_bfloat16* p, uint32_t* w, int left, bool sectors) {
+  if (left >= 16 && sectors) return load32(p, w);
 #pragma unroll
-    for (int q = 0; q < 8; ++q)
-      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(line + (uint32_t(q ^ (lane & 7)) << 4)), "r"(w[4 * q]), "r"(w[4 * q + 1]),
-                   "r"(w[4 * q + 2]), "r"(w[4 * q + 3])
-                   : "memory");
-    fence_async_smem();
-    __syncwarp();
-    if (lane == 0) {
-      tma_store(map, at, col, row);
-      tma_commit();
-    }
-    next = next + 1 == PIECES ? 0 : next + 1;
+  for (int h = 0; h < 2; ++h) {
+    const uint4 x = left >= 8 * (h + 1) ? __ldg(reinterpret_cast<const uint4*>(p) + h) : make_uint4(0, 0, 0, 0);
+    w[4 * h] = x.x; w[4 * h + 1] = x.y; w[4 * h + 2] = x.z; w[4 * h + 3] = x.w;
   }
-};
+}
 
 __device__ __forceinline__ void load64(uint32_t taddr, uint32_t (&v)[64]) {
   __syncwarp();
@@ -230,33 +270,49 @@ __device__ __forceinline__ void load64(uint32_t taddr, uint32_t (&v)[64]) {
   tc_ld32(taddr + 32, *reinterpret_cast<uint32_t(*)[32]>(&v[32]));
 }
 
-// The bits of the largest finite magnitude in 128 columns of the accumulator.
-__device__ __forceinline__ uint32_t top_of_block(uint32_t taddr) {
-  uint32_t top = 0;
+// The bits of the largest finite magnitude in 128 columns of the accumulator; *odd: there is an infinity.
+__device__ __forceinline__ uint32_t top_of_block(uint32_t taddr, bool* odd) {
+  float top = 0.f;
   __syncwarp();
-#pragma unroll 1
-  for (int i = 0; i < 4; ++i) {
-    uint32_t v[32];
-    tc_ld32(taddr + uint32_t(i * 32), v);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t v[64];
+    load64(taddr + uint32_t(i * 64), v);
     tc_wait_ld();
 #pragma unroll
-    for (int k = 0; k < 32; ++k) top = max(top, finite_bits(__uint_as_float(v[k])));
+    for (int k = 0; k < 64; ++k) top = fmaxf(top, fabsf(__uint_as_float(v[k])));      // a NaN loses
   }
-  return top;
-}
-// 64 values as codes, the columns from `left` on left alone.
-__device__ __forceinline__ void store_codes(uint8_t* p, const uint32_t (&v)[64], float inverse, int left, bool wide) {
+  *odd = top == __uint_as_float(0x7f800000u);
+  if (__any_sync(0xffffffffu, *odd)) {
+    uint32_t finite = 0;
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) {
+      uint32_t v[32];
+      tc_ld32(taddr + uint32_t(i * 32), v);
+      tc_wait_ld();
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
+      for (int k = 0; k < 32; ++k) finite = max(finite, finite_bits(__uint_as_float(v[k])));
+    }
+    return finite;
+  }
+  return __float_as_uint(top);
+}
+// 32 values as codes; the columns from `left` on are left alone.
+__device__ __forceinline__ void store_codes(uint8_t* p, const uint32_t* v, float inverse, bool odd, int left, bool wide) {
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       uint32_t pair[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int at = q * 16 + i * 4 + h * 2;
-        pair[h] = __nv_cvt_float2_to_fp8x2(make_float2(infinite_to_nan(__uint_as_float(v[at])) * inverse, infinite_to_nan(__uint_as_float(v[at + 1])) * inverse),
-                                           __NV_SATFINITE, __NV_E4M3);
+        float lo = __uint_as_float(v[q * 16 + i * 4 + h * 2]), hi = __uint_as_float(v[q * 16 + i * 4 + h * 2 + 1]);
+        if (odd) {
+          lo = infinite_to_nan(lo);
+          hi = infinite_to_nan(hi);
+        }
+        pair[h] = __nv_cvt_float2_to_fp8x2(make_float2(lo * inverse, hi * inverse), __NV_SATFINITE, __NV_E4M3);
       }
       w[i] = pair[0] | pair[1] << 16;
     }
@@ -288,7 +344,8 @@ __device__ __forceinline__ float2 values_of(uint32_t pair) {
   return __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(__nv_fp8x2_storage_t(pair & 0xffffu), __NV_E4M3)));
 }
 
-template <bool A_MN, bool B_MN, bool EIGHT, int EPI>
+// CODES: g and u, as they are written (kGated) or read (kGrad), are 8-bit blocks.
+template <bool A_MN, bool B_MN, bool EIGHT, int EPI, bool CODES>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<EIGHT>::threads, 1) product_pair_kernel(const __grid_constant__ TcProducts L) {
   using S = Shape<EIGHT>;
   extern __shared__ uint8_t smem_raw[];
@@ -305,11 +362,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<EIGHT>::thread
   auto tfull_bar = [&](uint32_t i) { return bar(kT + int(i)); };
   auto tempty_bar = [&](uint32_t i) { return bar(kT + 2 + int(i)); };
   const uint32_t drain_bar = bar(kT + 4), shared_bar = bar(kT + 5);     // shared_bar: the columns that both accumulators use have been read
-  auto input_bar = [&](int w) { return bar(kT + 6 + w); };
-  auto sfull_bar = [&](uint32_t i) { return bar(kT + 6 + kEpiWarps + int(i)); };
-  auto sempty_bar = [&](uint32_t i) { return bar(kT + 6 + kEpiWarps + kScaleRing + int(i)); };
+  auto sfull_bar = [&](uint32_t i) { return bar(kT + 6 + int(i)); };
+  auto sempty_bar = [&](uint32_t i) { return bar(kT + 6 + kScaleRing + int(i)); };
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform_warp(), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const bool leader_cta = rank == 0;
   const int pair_id = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
@@ -331,7 +387,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<EIGHT>::thread
     }
     mbar_init(drain_bar, 1);
     mbar_init(shared_bar, kEpiWarps);                 // the four warps of each CTA that read those columns
-    for (int i = 0; i < kEpiWarps; ++i) mbar_init(input_bar(i), 1);
     if constexpr (EIGHT)
       for (int i = 0; i < kScaleRing; ++i) {
         mbar_init(sfull_bar(i), 2);                   // both CTAs' scales
@@ -400,57 +455,66 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<EIGHT>::thread
         for (int i = 0; i < 64; ++i) __nanosleep(1000);
     }
   } else if (warp == 1) {
-    // ------------------------------------------------------------------ MMA issuer (leader CTA only)
-    if (lane == 0) {
-      if (leader_cta) {
-        Ring c{base, bars, abort_flag, 0u, 0u, 0u};
-        uint32_t tile_it = 0, group = 0;
-        bool ok = true;
-        constexpr uint64_t a_hi = A_MN ? kDescMN : kDescK, b_hi = B_MN ? kDescMN : kDescK;
-        // a step is 32 bytes of k: along a 128-byte row, or that many rows (16 of bf16, 32 of 8 bits) of 128 bytes
-        constexpr uint32_t a_step = A_MN ? 16 * 128 / 16 : 2, b_step = B_MN ? (EIGHT ? 32 : 16) * 128 / 16 : 2;
-        const uint32_t idesc = EIGHT ? make_idesc_scaled(B_MN, 2 * kRows, 2 * L.half) : make_idesc(B_MN, 2 * kRows, 2 * L.half, A_MN);
-        for (int t = pair_id; t < L.total_tiles && ok; t += num_pairs, ++tile_it) {
-          const TcProduct& p = L.p[decode(L, t).prob];
-          const uint32_t acc = tile_it & 1u, aph = (tile_it >> 1) & 1u;
-          const int num_kb = p.kblocks * p.segments;
-          if (!mbar_wait(tempty_bar(acc), aph ^ 1u, abort_flag)) { ok = false; break; }
-          if (EIGHT && tile_it > 0 && !mbar_wait(shared_bar, (tile_it - 1) & 1u, abort_flag)) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t d_tmem = accumulator(acc);
-          for (int kb = 0; kb < num_kb; ++kb, c.advance()) {
-            if constexpr (EIGHT) {
-              if ((kb & 3) == 0) {
-                const uint32_t place = group % kScaleRing;
-                if (!mbar_wait(sfull_bar(place), (group / kScaleRing) & 1u, abort_flag)) { ok = false; break; }
-                asm volatile("fence.acq_rel.cluster;" ::: "memory");       // the peer's half of them, too
-                tc_fence_after();
+    // ------------------------------------------------------------------ MMA issuer (leader CTA only), converged: see elect_one
+    if (leader_cta) {
+      Ring c{base, bars, abort_flag, 0u, 0u, 0u};
+      uint32_t tile_it = 0, group = 0;
+      bool ok = true;
+      constexpr uint64_t a_hi = A_MN ? kDescMN : kDescK, b_hi = B_MN ? kDescMN : kDescK;
+      // a step is 32 bytes of k: along a 128-byte row, or that many rows (16 of bf16, 32 of 8 bits) of 128 bytes
+      constexpr uint32_t a_step = A_MN ? 16 * 128 / 16 : 2, b_step = B_MN ? (EIGHT ? 32 : 16) * 128 / 16 : 2;
+      const uint32_t idesc = EIGHT ? make_idesc_scaled(B_MN, 2 * kRows, 2 * L.half) : make_idesc(B_MN, 2 * kRows, 2 * L.half, A_MN);
+      auto all = [](bool v) { return __all_sync(0xffffffffu, v) != 0; };
+      for (int t = pair_id; t < L.total_tiles && ok; t += num_pairs, ++tile_it) {
+        const TcProduct& p = L.p[decode(L, t).prob];
+        const uint32_t acc = tile_it & 1u, aph = (tile_it >> 1) & 1u;
+        const int num_kb = p.kblocks * p.segments;
+        ok = all(mbar_wait(tempty_bar(acc), aph ^ 1u, abort_flag));
+        if (EIGHT && ok && tile_it > 0) ok = all(mbar_wait(shared_bar, (tile_it - 1) & 1u, abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t d_tmem = accumulator(acc);
+        for (int kb = 0; kb < num_kb; ++kb, c.advance()) {
+          if constexpr (EIGHT) {
+            if ((kb & 3) == 0) {
+              const uint32_t place = group % kScaleRing;
+              ok = all(mbar_wait_cluster(sfull_bar(place), (group / kScaleRing) & 1u, abort_flag));
+              if (!ok) break;
+              tc_fence_after();
+              elected(true, [&] {
                 const uint32_t from = (base + S::scale_off + place * kScaleBytes) >> 4;
 #pragma unroll
                 for (int i = 0; i < 3; ++i) tc_copy_scales_pair(tmem_base + kScaleCol + uint32_t(4 * i), kDescScales | uint64_t(from + uint32_t(i) * 32u));
                 tc_commit_pair(sempty_bar(place));
-                ++group;
-              }
+              });
+              ++group;
             }
-            if (!mbar_wait(full_bar(c.s), c.ph, abort_flag)) { ok = false; break; }
-            tc_fence_after();
+          }
+          ok = all(mbar_wait(full_bar(c.s), c.ph, abort_flag));
+          if (!ok) break;
+          tc_fence_after();
+          elected(true, [&] {
             const uint32_t a0 = (base + c.s * kStageBytes) >> 4, b0 = a0 + (kHalfBytes >> 4);
+            const uint64_t da = a_hi | uint64_t(a0), db = b_hi | uint64_t(b0);
+            const uint32_t id = EIGHT ? idesc | scale_byte_ids(uint32_t(kb & 3)) : idesc;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const uint64_t da = a_hi | uint64_t(a0 + uint32_t(k) * a_step), db = b_hi | uint64_t(b0 + uint32_t(k) * b_step);
               const uint32_t more = (kb > 0 || k > 0) ? 1u : 0u;
-              if constexpr (EIGHT) tc_mma_pair_scaled(d_tmem, da, db, idesc | scale_byte_ids(uint32_t(kb & 3)), tmem_base + kScaleCol, tmem_base + kScaleCol + 4, more);
-              else tc_mma_pair(d_tmem, da, db, idesc, more);
+              if constexpr (EIGHT)
+                tc_mma_pair_scaled(d_tmem, da + uint64_t(k * a_step), db + uint64_t(k * b_step), id, tmem_base + kScaleCol, tmem_base + kScaleCol + 4, more);
+              else
+                tc_mma_pair(d_tmem, da + uint64_t(k * a_step), db + uint64_t(k * b_step), id, more);
             }
             tc_commit_pair(empty_bar(c.s));
-          }
-          if (ok) tc_commit_pair(tfull_bar(acc));
+          });
         }
-        if (!ok) give_up(33);
-        tc_commit_pair(drain_bar);       // arrives in both CTAs once everything issued above has finished
+        if (ok) elected(true, [&] { tc_commit_pair(tfull_bar(acc)); });
       }
-      if (!mbar_wait(drain_bar, 0, abort_flag, false, WAIT_CYCLES / 8)) atomicExch(L.status, 35);
+      if (!ok && lane == 0) give_up(33);
+      __syncwarp();
+      elected(true, [&] { tc_commit_pair(drain_bar); });       // arrives in both CTAs once everything issued above has finished
     }
+    if (lane == 0 && !mbar_wait(drain_bar, 0, abort_flag, false, WAIT_CYCLES / 8)) atomicExch(L.status, 35);
   } else if (EIGHT && warp == 2 + kEpiWarps) {
     // ------------------------------------------------------------------ scales: four k-blocks at a time
     if constexpr (EIGHT) {
@@ -465,21 +529,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<EIGHT>::thread
           if (!mbar_wait(sempty_bar(place), ((group / kScaleRing) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
           // lane i gathers rows i, i + 32, i + 64, i + 96 of each 128: a word of four blocks' bytes each
           uint32_t w[3][4];
-#pragma unroll
-          for (int part = 0; part < 3; ++part)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const Scales& s = part ? p.sb : p.sa;
-              const int row = (part ? tl.n0 + (part - 1) * 128 : tl.m0 + int(rank) * kRows) + r * 32 + lane;
-              uint32_t v = 0;
-              if (row < s.rows) {
-                const uint8_t* q = s.p + int64_t(row >> s.row_shift) * s.row_step + int64_t(kb) * s.block_step;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                  if (kb + j < p.kblocks) v |= uint32_t(__ldg(q + j * s.block_step)) << (8 * j);
-              }
-              w[part][r] = v;
-            }
+          gather_scales(p.sa, tl.m0 + int(rank) * kRows + lane, kb, p.kblocks, w[0]);
+          gather_scales(p.sb, tl.n0 + lane, kb, p.kblocks, w[1]);
+          gather_scales(p.sb, tl.n0 + 128 + lane, kb, p.kblocks, w[2]);
           const uint32_t to = base + S::scale_off + place * kScaleBytes + uint32_t(lane) * 16u;
 #pragma unroll
           for (int part = 0; part < 3; ++part)
@@ -496,9 +548,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<EIGHT>::thread
   } else {
     // ------------------------------------------------------------------ epilogue warps (per CTA: its 128 rows)
     const int ew = warp - 2, quad = warp & 3, part = ew >> 2;
-    Piece<S::pieces> out{base + S::epi_off + uint32_t(ew) * (S::pieces * kPieceBytes), 0u, lane};
+    const bool sectors = L.sectors != 0;
     const int chunks = (EPI == kGated ? L.half : 2 * L.half) / 64;
-    uint32_t tile_it = 0, iph = 0;
+    const Activation act = activation_of(L.activation);
+    uint32_t tile_it = 0;
     bool ok = true;
     for (int t = pair_id; t < L.total_tiles && ok; t += num_pairs, ++tile_it) {
       const Tile tl = decode(L, t);
@@ -533,122 +586,127 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<EIGHT>::thread
           }
 #pragma unroll
           for (int k = 0; k < 32; ++k) w[k] = pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
-          if (col < p.n && row0 < p.m) out.emit(&p.out[0], w, col, row0);
+          if (row < p.m) {
+            __nv_bfloat16* o = p.out[0] + row * p.ld[0] + col;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) put16(o + 16 * q, w + 8 * q, p.n - col - 16 * q, sectors);
+          }
         } else if constexpr (EPI == kGated) {
           if (!wait_tile()) { ok = false; break; }
-          uint32_t g[64], u[64], w[32];
+          const bool inside = col < p.n && row0 < p.m, full = !CODES && L.keep;
+          if (!inside) continue;
           const uint32_t at = taddr + uint32_t(chunk * 64), up = uint32_t(L.half);
           uint32_t eg = 0, eu = 0;
-          const bool eight = L.keep && L.gate_up_type == kTypeE4m3;
-          if (eight) {
-            eg = scale_byte(top_of_block(taddr));
-            eu = scale_byte(top_of_block(taddr + up));
-          }
-          load64(at, g);
-          load64(at + up, u);
-          tc_wait_ld();
-#pragma unroll
-          for (int k = 0; k < 32; ++k) {
-            float a[2], s;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) activate<true>(L.activation, __uint_as_float(g[2 * k + h]), &a[h], &s);
-            w[k] = pack2(a[0] * __uint_as_float(u[2 * k]), a[1] * __uint_as_float(u[2 * k + 1]));
-          }
-          if (col < p.n && row0 < p.m) {
-            out.emit(&p.out[0], w, col, row0);
-            if (eight) {
-              if (row < p.m) {
-                auto put = [&](const Operand& o, const uint32_t (&v)[64], uint32_t e) {
-                  store_codes(static_cast<uint8_t*>(const_cast<void*>(o.data)) + row * o.ld + col, v, inverse_scale_of(e), p.n - col, L.codes_wide != 0);
-                  if (part == 0) const_cast<uint8_t*>(o.scales)[row * o.lds + (col >> 7)] = uint8_t(e);
-                };
-                put(L.gate, g, eg);
-                put(L.up, u, eu);
+          bool odd_g = false, odd_u = false;
+          uint8_t *cg = nullptr, *cu = nullptr;
+          if constexpr (CODES) {
+            eg = scale_byte(top_of_block(taddr, &odd_g));
+            eu = scale_byte(top_of_block(taddr + up, &odd_u));
+            if (row < p.m) {
+              cg = static_cast<uint8_t*>(const_cast<void*>(L.gate.data)) + row * L.gate.ld + col;
+              cu = static_cast<uint8_t*>(const_cast<void*>(L.up.data)) + row * L.up.ld + col;
+              if (part == 0) {
+                const_cast<uint8_t*>(L.gate.scales)[row * L.gate.lds + (col >> 7)] = uint8_t(eg);
+                const_cast<uint8_t*>(L.up.scales)[row * L.up.lds + (col >> 7)] = uint8_t(eu);
               }
-            } else if (L.keep) {
+            }
+          }
+          const float ig = inverse_scale_of(eg), iu = inverse_scale_of(eu);
 #pragma unroll
-              for (int k = 0; k < 32; ++k) w[k] = pack2(__uint_as_float(g[2 * k]), __uint_as_float(g[2 * k + 1]));
-              out.emit(&p.out[1], w, col, row0);
+          for (int h = 0; h < 2; ++h) {
+            uint32_t g[32], u[32];
+            __syncwarp();
+            tc_ld32(at + uint32_t(h * 32), g);
+            tc_ld32(at + up + uint32_t(h * 32), u);
+            tc_wait_ld();
 #pragma unroll
-              for (int k = 0; k < 32; ++k) w[k] = pack2(__uint_as_float(u[2 * k]), __uint_as_float(u[2 * k + 1]));
-              out.emit(&p.out[2], w, col, row0);
+            for (int q = 0; q < 2; ++q) {
+              const int c = col + h * 32 + q * 16, left = row < p.m ? p.n - c : 0;
+              uint32_t w[8];
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const int at = q * 16 + 2 * k;
+                float a[2], s;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) activate<true>(act, __uint_as_float(g[at + e]), &a[e], &s);
+                w[k] = pack2(a[0] * __uint_as_float(u[at]), a[1] * __uint_as_float(u[at + 1]));
+              }
+              put16(p.out[0] + row * p.ld[0] + c, w, left, sectors);
+              if (full) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) w[k] = pack2(__uint_as_float(g[q * 16 + 2 * k]), __uint_as_float(g[q * 16 + 2 * k + 1]));
+                put16(p.out[1] + row * p.ld[1] + c, w, left, sectors);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) w[k] = pack2(__uint_as_float(u[q * 16 + 2 * k]), __uint_as_float(u[q * 16 + 2 * k + 1]));
+                put16(p.out[2] + row * p.ld[2] + c, w, left, sectors);
+              }
+            }
+            if (CODES && cg) {
+              store_codes(cg + h * 32, g, ig, odd_g, p.n - col - h * 32, L.codes_wide != 0);
+              store_codes(cu + h * 32, u, iu, odd_u, p.n - col - h * 32, L.codes_wide != 0);
             }
           }
         } else {
-          // g and u: by TMA into this warp's two buffers, or as 8 bits into registers, while the products still run.  dg and du then take the buffers.
-          const bool inside = col < p.n && row0 < p.m, eight = L.gate_up_type == kTypeE4m3;
-          uint32_t cg[16], cu[16];
+          // g and u come while the products still run
+          const bool inside = col < p.n && row0 < p.m;
+          uint32_t cg[CODES ? 16 : 32], cu[CODES ? 16 : 32];
           float sg = 0.f, su = 0.f;
           if (inside) {
-            if (lane == 0) tma_wait_read<0>();
-            __syncwarp();
-            if (eight) {
-#pragma unroll
-              for (int k = 0; k < 16; ++k) cg[k] = cu[k] = 0;
-              if (row < p.m) {
-                load_codes(static_cast<const uint8_t*>(L.gate.data) + row * L.gate.ld + col, cg, p.n - col, L.codes_wide != 0);
-                load_codes(static_cast<const uint8_t*>(L.up.data) + row * L.up.ld + col, cu, p.n - col, L.codes_wide != 0);
+            const bool mine = row < p.m;
+            if constexpr (CODES) {
+              const int left = mine ? p.n - col : 0;
+              load_codes(static_cast<const uint8_t*>(L.gate.data) + row * L.gate.ld + col, cg, left, L.codes_wide != 0);
+              load_codes(static_cast<const uint8_t*>(L.up.data) + row * L.up.ld + col, cu, left, L.codes_wide != 0);
+              if (mine) {
                 sg = scale_of(__ldg(L.gate.scales + row * L.gate.lds + (col >> 7)));
                 su = scale_of(__ldg(L.up.scales + row * L.up.lds + (col >> 7)));
               }
-            } else if (lane == 0) {
-              mbar_expect_tx(input_bar(ew), 2 * kPieceBytes);
-              tma_load(out.buf, &p.in[0], input_bar(ew), col, row0);
-              tma_load(out.buf + kPieceBytes, &p.in[1], input_bar(ew), col, row0);
+            } else {
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                const int left = mine ? p.n - col - 16 * q : 0;
+                get16(p.in[0] + row * p.ld_in[0] + col + 16 * q, cg + 8 * q, left, sectors);
+                get16(p.in[1] + row * p.ld_in[1] + col + 16 * q, cu + 8 * q, left, sectors);
+              }
             }
           }
           if (!wait_tile()) { ok = false; break; }
           if (!inside) continue;
-          if (!eight) {
-            if (!mbar_wait(input_bar(ew), iph, abort_flag)) { ok = false; break; }
-            iph ^= 1u;
-          }
-          uint32_t v[64], w[32];
-          load64(taddr + uint32_t(chunk * 64), v);
-          tc_wait_ld();
-          const uint32_t line = out.buf + uint32_t(lane) * 128u;
+          uint32_t v[32];
 #pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            uint32_t dg[4], du[4];
-            const uint32_t at = line + (uint32_t(q ^ (lane & 7)) << 4);
-            if (!eight) {
-              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(dg[0]), "=r"(dg[1]), "=r"(dg[2]), "=r"(dg[3]) : "r"(at));
-              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(du[0]), "=r"(du[1]), "=r"(du[2]), "=r"(du[3]) : "r"(at + kPieceBytes));
+          for (int q = 0; q < 4; ++q) {
+            if (q % 2 == 0) {
+              __syncwarp();
+              tc_ld32(taddr + uint32_t(chunk * 64 + q * 16), v);
+              tc_wait_ld();
             }
+            uint32_t w[8], wg[8], wu[8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const int pair = q * 4 + k;
+            for (int k = 0; k < 8; ++k) {
+              const int pair = q * 8 + k;
               float2 g, u;
-              if (eight) {
+              if constexpr (CODES) {
                 g = values_of(cg[pair >> 1] >> (16 * (pair & 1)));
                 u = values_of(cu[pair >> 1] >> (16 * (pair & 1)));
                 g.x *= sg; g.y *= sg;
                 u.x *= su; u.y *= su;
               } else {
-                g = make_float2(low(dg[k]), high(dg[k]));
-                u = make_float2(low(du[k]), high(du[k]));
+                g = make_float2(low(cg[pair]), high(cg[pair]));
+                u = make_float2(low(cu[pair]), high(cu[pair]));
               }
-              const float d0 = __uint_as_float(v[2 * pair]), d1 = __uint_as_float(v[2 * pair + 1]);
+              const float d0 = __uint_as_float(v[(2 * pair) & 31]), d1 = __uint_as_float(v[(2 * pair + 1) & 31]);
               float a0, a1, s0, s1;
-              activate<true>(L.activation, g.x, &a0, &s0);
-              activate<true>(L.activation, g.y, &a1, &s1);
-              dg[k] = pack2(d0 * u.x * s0, d1 * u.y * s1);
-              du[k] = pack2(d0 * a0, d1 * a1);
-              w[pair] = pack2(a0 * u.x, a1 * u.y);
+              activate<true>(act, g.x, &a0, &s0);
+              activate<true>(act, g.y, &a1, &s1);
+              wg[k] = pack2(d0 * u.x * s0, d1 * u.y * s1);
+              wu[k] = pack2(d0 * a0, d1 * a1);
+              w[k] = pack2(a0 * u.x, a1 * u.y);
             }
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(dg[0]), "r"(dg[1]), "r"(dg[2]), "r"(dg[3]) : "memory");
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + kPieceBytes), "r"(du[0]), "r"(du[1]), "r"(du[2]), "r"(du[3]) : "memory");
+            const int c = col + 16 * q, left = row < p.m ? p.n - c : 0;
+            put16(p.out[1] + row * p.ld[1] + c, wg, left, sectors);
+            put16(p.out[2] + row * p.ld[2] + c, wu, left, sectors);
+            put16(p.out[0] + row * p.ld[0] + c, w, left, sectors);
           }
-          fence_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            tma_store(&p.out[1], out.buf, col, row0);
-            tma_commit();
-            tma_store(&p.out[2], out.buf + kPieceBytes, col, row0);
-            tma_commit();
-          }
-          out.next = 0;
-          out.emit(&p.out[0], w, col, row0);
         }
       }
       if (ok && !wait_tile()) ok = false;           // a warp without a chunk hands the accumulator back, too
@@ -657,13 +715,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<EIGHT>::thread
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(map_to_cta(tempty_bar(acc), 0));
     }
-    if (lane == 0) {
-      tma_wait_all();                               // every store has landed before the CTA retires
-      if (!ok) {                                    // g and u may still be landing
-        for (int i = 0; i < 64; ++i) __nanosleep(1000);
-        give_up(34);
-      }
-    }
+    if (!ok && lane == 0) give_up(34);
   }
   tc_fence_before();
   __syncthreads();
@@ -699,22 +751,21 @@ struct Encoder {
     if (o.mn_major) map(to, o.data, o.type, o.ld, n, k, line, line);
     else map(to, o.data, o.type, o.ld, k, n, line, rows);
   }
-  void piece(CUtensorMap* to, const void* data, int64_t ld, int64_t m, int64_t n) { map(to, data, kTypeBf16, ld, n, m, 64, 32); }
 };
 
-template <bool A_MN, bool B_MN, bool EIGHT, int EPI>
+template <bool A_MN, bool B_MN, bool EIGHT, int EPI, bool CODES = false>
 int launch(const TcProducts& L, int device, int pairs, cudaStream_t st) {
   static SharedMemoryLimit limit;
   using S = Shape<EIGHT>;
-  if (!limit.raise(device, S::bytes, product_pair_kernel<A_MN, B_MN, EIGHT, EPI>)) return MUON_ERR_CUDA;
-  product_pair_kernel<A_MN, B_MN, EIGHT, EPI><<<unsigned(2 * std::min(L.total_tiles, pairs)), S::threads, S::bytes, st>>>(L);
+  if (!limit.raise(device, S::bytes, product_pair_kernel<A_MN, B_MN, EIGHT, EPI, CODES>)) return MUON_ERR_CUDA;
+  product_pair_kernel<A_MN, B_MN, EIGHT, EPI, CODES><<<unsigned(2 * std::min(L.total_tiles, pairs)), S::threads, S::bytes, st>>>(L);
   return cudaGetLastError() == cudaSuccess ? 1 : MUON_ERR_CUDA;
 }
 
 Scales scales_of(const Operand& o, int rows) {
   const int shift = o.block_rows == 1 ? 0 : 7;
-  if (o.mn_major) return {o.scales, 1, o.lds, 7, rows};       // the block of a column; blocks of rows are those of k
-  return {o.scales, o.lds, 1, shift, rows};
+  if (o.mn_major) return {o.scales, 1, o.lds, 7, rows, 0};    // the block of a column; blocks of rows are those of k
+  return {o.scales, o.lds, 1, shift, rows, o.lds % 4 == 0 && reinterpret_cast<uintptr_t>(o.scales) % 4 == 0};
 }
 
 }  // namespace
@@ -760,11 +811,11 @@ int launch_products_tc(muon_ctx* ctx, const Product* list, int count, cudaStream
   L.count = count;
   L.half = 128;
   L.activation = e0.activation;
-  L.gate_up_type = e0.gate_up_type;
-  L.keep = e0.kind == kGated && (e0.gate || codes);
+  L.keep = e0.kind == kGated && e0.gate;
   L.gate = e0.in_gate;
   L.up = e0.in_up;
   L.codes_wide = codes && addressable(L.gate.data, L.gate.ld, 1) && addressable(L.up.data, L.up.ld, 1);
+  L.sectors = 1;
   L.status = ctx->d_status;
   Encoder enc = {ctx};
   int64_t tiles = 0;
@@ -783,14 +834,19 @@ int launch_products_tc(muon_ctx* ctx, const Product* list, int count, cudaStream
     if (tiles > INT32_MAX - 4096) return MUON_ERR_UNSUPPORTED;
     for (int s = 0; s < q.segments; ++s) enc.operand(&p.a[s], q.a[s], q.m, q.k, kRows);
     for (int s = 0; s < (q.e.kind == kGated ? 2 : q.segments); ++s) enc.operand(&p.b[s], q.b[s], q.n, q.k, uint32_t(L.half));
-    enc.piece(&p.out[0], q.e.c, q.e.ldc, q.m, q.n);
+    auto rows = [&](__nv_bfloat16** to, int64_t* ld, const void* data, int64_t stride) {
+      *to = static_cast<__nv_bfloat16*>(const_cast<void*>(data));
+      *ld = stride;
+      L.sectors = L.sectors && reinterpret_cast<uintptr_t>(data) % 32 == 0 && stride % 16 == 0;
+    };
+    rows(&p.out[0], &p.ld[0], q.e.c, q.e.ldc);
     if (q.e.kind == kGrad || (q.e.kind == kGated && q.e.gate)) {
-      enc.piece(&p.out[1], q.e.gate, q.e.ld_gate, q.m, q.n);
-      enc.piece(&p.out[2], q.e.up, q.e.ld_up, q.m, q.n);
+      rows(&p.out[1], &p.ld[1], q.e.gate, q.e.ld_gate);
+      rows(&p.out[2], &p.ld[2], q.e.up, q.e.ld_up);
     }
     if (q.e.kind == kGrad && !codes) {
-      enc.piece(&p.in[0], q.e.in_gate.data, q.e.in_gate.ld, q.m, q.n);
-      enc.piece(&p.in[1], q.e.in_up.data, q.e.in_up.ld, q.m, q.n);
+      rows(const_cast<__nv_bfloat16**>(&p.in[0]), &p.ld_in[0], q.e.in_gate.data, q.e.in_gate.ld);
+      rows(const_cast<__nv_bfloat16**>(&p.in[1]), &p.ld_in[1], q.e.in_up.data, q.e.in_up.ld);
     }
     if (eight) {
       p.sa = scales_of(q.a[0], q.m);
@@ -801,8 +857,8 @@ int launch_products_tc(muon_ctx* ctx, const Product* list, int count, cudaStream
   L.total_tiles = int32_t(tiles);
   const int pairs = sms / 2, dev = ctx->device;
   if (eight) return bmn ? launch<false, true, true, kPlain>(L, dev, pairs, st) : launch<false, false, true, kPlain>(L, dev, pairs, st);
-  if (e0.kind == kGated) return launch<false, false, false, kGated>(L, dev, pairs, st);
-  if (e0.kind == kGrad) return launch<false, true, false, kGrad>(L, dev, pairs, st);
+  if (e0.kind == kGated) return codes ? launch<false, false, false, kGated, true>(L, dev, pairs, st) : launch<false, false, false, kGated>(L, dev, pairs, st);
+  if (e0.kind == kGrad) return codes ? launch<false, true, false, kGrad, true>(L, dev, pairs, st) : launch<false, true, false, kGrad>(L, dev, pairs, st);
   if (amn) return launch<true, true, false, kPlain>(L, dev, pairs, st);
   return bmn ? launch<false, true, false, kPlain>(L, dev, pairs, st) : launch<false, false, false, kPlain>(L, dev, pairs, st);
 }

@@ -113,6 +113,26 @@ __device__ __forceinline__ void tc_ld32(uint32_t taddr, uint32_t (&r)[32]) {
 }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
+// The issuing warp runs converged, its warp index taken from lane 0 and every wait followed by a vote, and one elected lane issues: then
+// descriptors and addresses are values of the whole warp and stay in uniform registers.  A step has to take less than the 64 clocks that
+// its instruction keeps the tensor cores busy; issued from a branch on the lane it took 85, with descriptors formed anew each time 107.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(one));
+  return one != 0;
+}
+// Runs f on the elected lane.  Without the meeting behind it the other lanes go on to the next wait and share the issue slots with it.
+template <typename F>
+__device__ __forceinline__ void elected(bool go, F f) {
+  if (go && elect_one()) f();
+  __syncwarp();
+}
+__device__ __forceinline__ int uniform_warp() { return __shfl_sync(0xffffffffu, int(threadIdx.x >> 5), 0); }
+
 // Shared-memory matrix descriptor, 128-byte swizzle (layout type 2), descriptor version 1.
 // lbo/sbo in bytes.  K-major: lbo is unused by the hardware for swizzled layouts (set to 16),
 // sbo = distance between 8-row groups.  MN-major: lbo = distance between 64-element column
