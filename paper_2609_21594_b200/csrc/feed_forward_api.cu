@@ -181,7 +181,7 @@ struct LinearScratch {
 LinearScratch linear_scratch(const muon_linear_blocks_desc_t* d, Scratch* s) {
   LinearScratch r = {};
   r.dy8.ld = up_to(d->out, 16);
-  r.dy8.lds = blocks_of(d->out);
+  r.dy8.lds = up_to(blocks_of(d->out), 16);       // the tensor cores' scales are read 16 bytes at a time
   r.dy8.block_rows = 1;
   r.dy8.codes = s->take(d->tokens * r.dy8.ld);
   r.dy8.scales = static_cast<uint8_t*>(s->take(d->tokens * r.dy8.lds));

@@ -377,7 +377,8 @@ std::tuple<Tensor, Tensor, Tensor> attention_backward(const Tensor& dout, const 
 }
 
 // ------------------------------------------------------------------ 8-bit blocks
-// Codes [..., cols] with rows 16 bytes apart or a multiple of that, so that the tensor cores can take them, and their scales.
+// Codes [..., cols] with rows 16 bytes apart or a multiple of that, so that the tensor cores can take them, and their scales, whose rows are
+// 4 bytes apart or a multiple of 16 where there are more than 8: so they are read fastest.
 struct Packed {
   Tensor codes, scales;
 };
@@ -387,8 +388,10 @@ Packed new_packed(at::IntArrayRef sizes, const at::TensorOptions& options, int64
   shape.back() = ld;
   scales.back() = (cols + 127) / 128;
   if (block_rows > 1) scales[0] = (scales[0] + block_rows - 1) / block_rows;
-  const Tensor codes = at::empty(shape, options.dtype(at::kFloat8_e4m3fn));
-  return {ld == cols ? codes : codes.narrow(-1, 0, cols), at::empty(scales, options.dtype(at::kByte))};
+  const int64_t blocks = scales.back(), lds = blocks > 8 ? (blocks + 15) / 16 * 16 : (blocks + 3) / 4 * 4;
+  scales.back() = lds;
+  const Tensor codes = at::empty(shape, options.dtype(at::kFloat8_e4m3fn)), bytes = at::empty(scales, options.dtype(at::kByte));
+  return {ld == cols ? codes : codes.narrow(-1, 0, cols), lds == blocks ? bytes : bytes.narrow(-1, 0, blocks)};
 }
 
 // A packed matrix as the C ABI takes it, and the tensors that keep its memory.

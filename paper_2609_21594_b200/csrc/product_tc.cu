@@ -13,8 +13,8 @@
 // Gradient of the gate: the accumulator is dh, which never leaves the chip; g and u come in, dg, du and h go out.
 //
 // 8 bits: tcgen05.mma.kind::mxf8f6f4 multiplies each group of 32 values of k with the scales of its row of A and of B, taken from tensor memory.  A
-// block of 128 is four such groups with one scale.  A warp of its own gathers the bytes of four blocks into the order that tcgen05.cp spreads
-// over the lanes; the issuer copies them (12 columns) every fourth k-block.  Two accumulators of 256 columns would leave no room for them, so the
+// block of 128 is four such groups with one scale.  A warp of its own gathers the bytes of sixteen blocks into the order that tcgen05.cp spreads
+// over the lanes; the issuer copies four blocks' bytes (12 columns) every fourth k-block.  Two accumulators of 256 columns would leave no room for them, so the
 // second one begins 16 columns inside the first: the next tile begins when those 16 columns have been read, which the epilogue does first.
 //
 // Synchronisation as in the Newton-Schulz kernel, all waits bounded: full / empty per stage, tfull / tempty per accumulator, an abort flag in both CTAs.
@@ -36,8 +36,10 @@ constexpr uint32_t kHalfBytes = kRows * 128;   // 16 KiB: 128 rows of 128 bytes
 constexpr uint32_t kStageBytes = 2 * kHalfBytes;
 constexpr int kEpiWarps = 8;
 constexpr int kGroupTiles = 8;                 // tiles of rows that a stretch of the tile list stays in: what they and as many columns read fits L2
-constexpr int kScaleRing = 4;                  // groups of four k-blocks whose scales are on their way
-constexpr uint32_t kScaleBytes = 3 * 512;      // of a group: 128 rows of A, 256 of B, four bytes each
+constexpr int kScaleBlocks = 16;               // k-blocks whose scales are gathered at a time: a round of gathering takes as long as the products of six
+constexpr int kScaleRing = 2;
+constexpr uint32_t kScaleWord = 3 * 512;       // scales of four k-blocks: 128 rows of A, 256 of B, four bytes each
+constexpr uint32_t kScaleBytes = kScaleBlocks / 4 * kScaleWord;
 constexpr uint32_t kScaleCol = 496;            // tensor memory columns of the scales
 constexpr uint32_t kSecondAccumulator8 = 240;
 
@@ -48,13 +50,14 @@ struct Shape {
   static constexpr uint32_t bytes = bar_off + 512 + 1024;
   static constexpr int threads = 32 * (2 + kEpiWarps + (EIGHT ? 1 : 0));
 };
+static_assert(kScaleBlocks == 16, "gather_scales");
 static_assert(Shape<false>::bytes <= 232448 && Shape<true>::bytes <= 232448, "227 KiB of shared memory");
 
 struct Scales {                                // of an operand: the byte of (row, k-block) is at (row >> row_shift) * row_step + block * block_step
   const uint8_t* p;
   int64_t row_step, block_step;
   int32_t row_shift, rows;
-  int32_t words;                               // four blocks' bytes are an aligned word
+  int32_t wide;                                // blocks whose bytes lie together and aligned in every row: 16, 4 or 1
 };
 struct TcProduct {
   CUtensorMap a[2], b[2];
@@ -181,36 +184,48 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 __device__ __forceinline__ float low(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float high(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
 
-// The bytes of k-blocks kb to kb + 3 (0 past the last) for rows `row`, + 32, + 64, + 96 of an operand.  Rows of 128 x 128 blocks share theirs, and bytes
-// that lie together come as a word; otherwise all loads are issued before the first is waited for.
-__device__ __forceinline__ void gather_scales(const Scales& s, int row, int kb, int kblocks, uint32_t (&w)[4]) {
-  const bool shared = s.row_shift != 0, word = s.words && kb + 4 <= kblocks;
+// The bytes of k-blocks kb to kb + 15 (0 past the last), as four words, for rows `row0` + lane + 0, 32, 64 and 96 of an operand.  All loads are
+// issued before the first is waited for.
+__device__ __forceinline__ void gather_scales(const Scales& s, int row0, int kb, int kblocks, int lane, uint32_t (&w)[4][4]) {
   const uint8_t* base = s.p + int64_t(kb) * s.block_step;
-  uint32_t v[4][4];
+  const int left = kblocks - kb;
+  if (s.row_shift) {                           // blocks of 128 rows: one lane takes one byte, and all the words are the same for every row
+    uint32_t v = 0;
+    if (lane < kScaleBlocks && lane < left && row0 < s.rows) v = uint32_t(__ldg(base + int64_t(row0 >> s.row_shift) * s.row_step + lane * s.block_step));
+    v <<= 8 * (lane & 3);
+    v |= __shfl_xor_sync(0xffffffffu, v, 1);
+    v |= __shfl_xor_sync(0xffffffffu, v, 2);
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const uint8_t* q = base + int64_t(min(row + 32 * r, s.rows - 1) >> s.row_shift) * s.row_step;
-    if (shared && r > 0) continue;
-    if (word) {
-      v[r][0] = __ldg(reinterpret_cast<const uint32_t*>(q));
-    } else {
+    for (int i = 0; i < 4; ++i) w[0][i] = __shfl_sync(0xffffffffu, v, 4 * i);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[r][j] = __ldg(q + int64_t(min(j, kblocks - 1 - kb)) * s.block_step);
+    for (int r = 1; r < 4; ++r)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[r][i] = w[0][i];
+    return;
+  }
+  if (s.wide >= 16 && left >= 16) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const uint4 x = __ldg(reinterpret_cast<const uint4*>(base + int64_t(min(row0 + lane + 32 * r, s.rows - 1)) * s.row_step));
+      w[r][0] = x.x; w[r][1] = x.y; w[r][2] = x.z; w[r][3] = x.w;
     }
+    return;
   }
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
-    uint32_t x = v[r][0];
-    if (shared && r > 0) {
-      w[r] = w[0];
-      continue;
-    }
-    if (!word) {
+    const uint8_t* q = base + int64_t(min(row0 + lane + 32 * r, s.rows - 1)) * s.row_step;
 #pragma unroll
-      for (int j = 1; j < 4; ++j)
-        if (kb + j < kblocks) x |= v[r][j] << (8 * j);
+    for (int i = 0; i < 4; ++i) {
+      uint32_t x = 0;
+      if (s.wide >= 4 && left >= 4 * i + 4) {
+        x = __ldg(reinterpret_cast<const uint32_t*>(q) + i);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (4 * i + j < left) x |= uint32_t(__ldg(q + 4 * i + j)) << (8 * j);
+      }
+      w[r][i] = x;
     }
-    w[r] = x;
   }
 }
 
@@ -478,16 +493,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<EIGHT>::thread
           if constexpr (EIGHT) {
             if ((kb & 3) == 0) {
               const uint32_t place = group % kScaleRing;
-              ok = all(mbar_wait_cluster(sfull_bar(place), (group / kScaleRing) & 1u, abort_flag));
-              if (!ok) break;
-              tc_fence_after();
+              if (kb % kScaleBlocks == 0) {
+                ok = all(mbar_wait_cluster(sfull_bar(place), (group / kScaleRing) & 1u, abort_flag));
+                if (!ok) break;
+                tc_fence_after();
+              }
+              const bool last = kb % kScaleBlocks == kScaleBlocks - 4 || kb + 4 >= num_kb;
               elected(true, [&] {
-                const uint32_t from = (base + S::scale_off + place * kScaleBytes) >> 4;
+                const uint32_t from = (base + S::scale_off + place * kScaleBytes + uint32_t(kb % kScaleBlocks / 4) * kScaleWord) >> 4;
 #pragma unroll
                 for (int i = 0; i < 3; ++i) tc_copy_scales_pair(tmem_base + kScaleCol + uint32_t(4 * i), kDescScales | uint64_t(from + uint32_t(i) * 32u));
-                tc_commit_pair(sempty_bar(place));
+                if (last) tc_commit_pair(sempty_bar(place));
               });
-              ++group;
+              if (last) ++group;
             }
           }
           ok = all(mbar_wait(full_bar(c.s), c.ph, abort_flag));
@@ -516,7 +534,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<EIGHT>::thread
     }
     if (lane == 0 && !mbar_wait(drain_bar, 0, abort_flag, false, WAIT_CYCLES / 8)) atomicExch(L.status, 35);
   } else if (EIGHT && warp == 2 + kEpiWarps) {
-    // ------------------------------------------------------------------ scales: four k-blocks at a time
+    // ------------------------------------------------------------------ scales
     if constexpr (EIGHT) {
       uint32_t group = 0;
       bool ok = true;
@@ -524,20 +542,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<EIGHT>::thread
       for (int t = pair_id; t < L.total_tiles && ok; t += num_pairs) {
         const Tile tl = decode(L, t);
         const TcProduct& p = L.p[tl.prob];
-        for (int kb = 0; kb < p.kblocks; kb += 4, ++group) {
+        for (int kb = 0; kb < p.kblocks; kb += kScaleBlocks, ++group) {
           const uint32_t place = group % kScaleRing;
           if (!mbar_wait(sempty_bar(place), ((group / kScaleRing) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-          // lane i gathers rows i, i + 32, i + 64, i + 96 of each 128: a word of four blocks' bytes each
-          uint32_t w[3][4];
-          gather_scales(p.sa, tl.m0 + int(rank) * kRows + lane, kb, p.kblocks, w[0]);
-          gather_scales(p.sb, tl.n0 + lane, kb, p.kblocks, w[1]);
-          gather_scales(p.sb, tl.n0 + 128 + lane, kb, p.kblocks, w[2]);
+          uint32_t w[3][4][4];
+          gather_scales(p.sa, tl.m0 + int(rank) * kRows, kb, p.kblocks, lane, w[0]);
+          gather_scales(p.sb, tl.n0, kb, p.kblocks, lane, w[1]);
+          gather_scales(p.sb, tl.n0 + 128, kb, p.kblocks, lane, w[2]);
           const uint32_t to = base + S::scale_off + place * kScaleBytes + uint32_t(lane) * 16u;
 #pragma unroll
-          for (int part = 0; part < 3; ++part)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + uint32_t(part) * 512u), "r"(w[part][0]), "r"(w[part][1]), "r"(w[part][2]),
-                         "r"(w[part][3])
-                         : "memory");
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int part = 0; part < 3; ++part)
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + uint32_t(i) * kScaleWord + uint32_t(part) * 512u), "r"(w[part][0][i]),
+                           "r"(w[part][1][i]), "r"(w[part][2][i]), "r"(w[part][3][i])
+                           : "memory");
           fence_async_smem();
           __syncwarp();
           if (lane == 0) mbar_arrive_cluster(sfull0 + place * 8u);
@@ -764,8 +783,9 @@ int launch(const TcProducts& L, int device, int pairs, cudaStream_t st) {
 
 Scales scales_of(const Operand& o, int rows) {
   const int shift = o.block_rows == 1 ? 0 : 7;
-  if (o.mn_major) return {o.scales, 1, o.lds, 7, rows, 0};    // the block of a column; blocks of rows are those of k
-  return {o.scales, o.lds, 1, shift, rows, o.lds % 4 == 0 && reinterpret_cast<uintptr_t>(o.scales) % 4 == 0};
+  if (o.mn_major) return {o.scales, 1, o.lds, 7, rows, 1};    // the block of a column; blocks of rows are those of k
+  const uintptr_t place = reinterpret_cast<uintptr_t>(o.scales) | uintptr_t(o.lds);
+  return {o.scales, o.lds, 1, shift, rows, place % 16 == 0 ? 16 : place % 4 == 0 ? 4 : 1};
 }
 
 }  // namespace
