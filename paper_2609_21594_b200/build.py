@@ -18,7 +18,7 @@ LIB = os.path.join(HERE, "libmuon_b200.so")
 FRONT = os.path.join(HERE, "_front.so")
 SOURCES = ["api.cu", "plan.cu", "layout_kernels.cu", "elementwise_kernels.cu", "ns_simt.cu", "ns_tcgen05.cu", "ns_tcgen05_pair.cu", "ns_tables.cu",
            "layer_api.cu", "layer_norm.cu", "rotary.cu", "attention_simt.cu", "attention_fwd.cu", "attention_bwd.cu",
-           "feed_forward_api.cu", "pack8.cu", "product_simt.cu", "product_tc.cu"]
+           "feed_forward_api.cu", "pack8.cu", "product_simt.cu", "product_tc.cu", "product_few.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"] + os.environ.get("MUON_NVCC_EXTRA", "").split()
 

@@ -72,12 +72,13 @@ struct Launches {
     const int r = launched(ctx, n);
     if (rc == MUON_OK) rc = r;
   }
-  void products(const Product* p, int n) {
+  // follows: the call's last launch is right before this one in the stream, and writes nothing but what it takes as A
+  void products(const Product* p, int n, bool follows = false) {
     if (rc != MUON_OK || n == 0) return;
-    if (products_tc_take(p, n)) return count(launch_products_tc(ctx, p, n, st));
+    if (products_tc_take(p, n)) return count(n == 1 && product_few_takes(*p) ? launch_product_few(ctx, *p, sms, follows, st) : launch_products_tc(ctx, p, n, st));
     for (int i = 0; i < n && rc == MUON_OK; ++i) count(launch_product_simt(p[i], sms, st));
   }
-  void product(const Product& p) { products(&p, 1); }
+  void product(const Product& p, bool follows = false) { products(&p, 1, follows); }
   void quantize(int dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx, const Operand& out) {
     if (rc == MUON_OK) count(launch_quantize(dtype, rows, cols, x, ldx, out, sms, st));
   }
@@ -293,7 +294,7 @@ int muon_feed_forward_forward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* d
       }
     }
   }
-  l.product(plain(t, dim, hidden, operand(w.h, w.ldh, d->dtype), operand(w_down, d->dtype), y->data, y->ld, d->dtype));
+  l.product(plain(t, dim, hidden, operand(w.h, w.ldh, d->dtype), operand(w_down, d->dtype), y->data, y->ld, d->dtype), true);
   return l.rc;
 }
 
@@ -348,7 +349,7 @@ int muon_feed_forward_backward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* 
     p.segments = 2;
     p.a[1] = operand(w.dup, w.ldh, dt);
     p.b[1] = operand(w_up, dt, true);
-    l.product(p);
+    l.product(p, true);
   }
   Operand ox = operand(x, dt, true);
   if (!given_x && (dw_gate || dw_up)) {
@@ -378,7 +379,7 @@ int muon_linear_blocks_forward(muon_ctx_t* ctx, const muon_linear_blocks_desc_t*
   Launches l = {ctx, 0, static_cast<cudaStream_t>(stream)};
   if ((rc = device_of(ctx, &l.sms)) != MUON_OK) return rc;
   l.quantize(kTypeBf16, t, dim, x->data, x->ld, operand(x8));
-  l.product(plain(t, out, dim, operand(x8), operand(w8), y->data, y->ld, kTypeBf16));
+  l.product(plain(t, out, dim, operand(x8), operand(w8), y->data, y->ld, kTypeBf16), true);
   return l.rc;
 }
 
@@ -415,7 +416,7 @@ int muon_linear_blocks_backward(muon_ctx_t* ctx, const muon_linear_blocks_desc_t
   if ((rc = device_of(ctx, &l.sms)) != MUON_OK) return rc;
   if (rw) {
     l.quantize(kTypeBf16, t, out, dy->data, dy->ld, operand(&w.dy8));
-    l.product(plain(t, dim, out, operand(&w.dy8), operand(w8, true), dx->data, dx->ld, kTypeBf16));
+    l.product(plain(t, dim, out, operand(&w.dy8), operand(w8, true), dx->data, dx->ld, kTypeBf16), true);
   }
   if (dw) {
     const muon_rows_t none = {nullptr, out};

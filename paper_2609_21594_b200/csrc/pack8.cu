@@ -83,6 +83,7 @@ __device__ __forceinline__ uint32_t finite_top(const float (&v)[N], bool* odd) {
 template <typename T, int UNROLL>
 __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const T* x, int64_t ldx, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds,
                                                                  int64_t rows, int32_t cols, uint32_t per_row) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // a product that follows may request its weights
   const int sub = threadIdx.x & 7;
   const int64_t first = (int64_t(blockIdx.x) * (kThreads / 8) + (threadIdx.x >> 3)) * UNROLL;
   int64_t row = first <= UINT32_MAX ? int64_t(uint32_t(first) / per_row) : first / per_row;
