@@ -76,7 +76,7 @@ struct Launches {
   void products(const Product* p, int n, bool follows = false) {
     if (rc != MUON_OK || n == 0) return;
     if (products_tc_take(p, n)) return count(n == 1 && product_few_takes(*p) ? launch_product_few(ctx, *p, sms, follows, st) : launch_products_tc(ctx, p, n, st));
-    for (int i = 0; i < n && rc == MUON_OK; ++i) count(launch_product_simt(p[i], sms, st));
+    count(launch_products_simt(p, n, sms, st));
   }
   void product(const Product& p, bool follows = false) { products(&p, 1, follows); }
   void quantize(int dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx, const Operand& out) {
@@ -285,7 +285,7 @@ int muon_feed_forward_forward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* d
       q.e.gate = w.gate;
       q.e.up = w.up;
       q.e.ld_gate = q.e.ld_up = hidden;
-      l.count(launch_product_simt(q, l.sms, l.st));
+      l.count(launch_products_simt(&q, 1, l.sms, l.st));
       for (const Operand* o : {&p.e.in_gate, &p.e.in_up}) {
         Operand part = *o;
         part.data = static_cast<const uint8_t*>(o->data) + r * o->ld;

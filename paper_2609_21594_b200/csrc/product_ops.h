@@ -61,7 +61,7 @@ int launch_products_tc(muon_ctx* ctx, const Product* p, int count, cudaStream_t 
 constexpr int kFewRows = 128;
 bool product_few_takes(const Product& p);
 int launch_product_few(muon_ctx* ctx, const Product& p, int sms, bool follows, cudaStream_t st);
-int launch_product_simt(const Product& p, int sms, cudaStream_t st);
+int launch_products_simt(const Product* p, int count, int sms, cudaStream_t st);      // operands of one type
 
 int launch_quantize(int dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx, const Operand& out, int sms, cudaStream_t st);
 int launch_dequantize(int dtype, int64_t rows, int64_t cols, const Operand& in, void* y, int64_t ldy, int sms, cudaStream_t st);
