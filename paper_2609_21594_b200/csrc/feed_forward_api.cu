@@ -73,12 +73,12 @@ struct Launches {
     if (rc == MUON_OK) rc = r;
   }
   // follows: the call's last launch is right before this one in the stream, and writes nothing but what it takes as A
-  void products(const Product* p, int n, bool follows = false) {
+  void products(const Product* p, int n, int siblings, bool follows = false) {
     if (rc != MUON_OK || n == 0) return;
-    if (products_tc_take(p, n)) return count(n == 1 && product_few_takes(*p) ? launch_product_few(ctx, *p, sms, follows, st) : launch_products_tc(ctx, p, n, st));
-    count(launch_products_simt(p, n, sms, st));
+    if (products_tc_take(p, n)) return count(n == 1 && product_few_takes(*p, sms) ? launch_product_few(ctx, *p, sms, follows, st) : launch_products_tc(ctx, p, n, st));
+    count(launch_products_simt(p, n, siblings, sms, st));
   }
-  void product(const Product& p, bool follows = false) { products(&p, 1, follows); }
+  void product(const Product& p, bool follows = false) { products(&p, 1, 1, follows); }
   void quantize(int dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx, const Operand& out) {
     if (rc == MUON_OK) count(launch_quantize(dtype, rows, cols, x, ldx, out, sms, st));
   }
@@ -285,7 +285,7 @@ int muon_feed_forward_forward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* d
       q.e.gate = w.gate;
       q.e.up = w.up;
       q.e.ld_gate = q.e.ld_up = hidden;
-      l.count(launch_products_simt(&q, 1, l.sms, l.st));
+      l.count(launch_products_simt(&q, 1, 1, l.sms, l.st));
       for (const Operand* o : {&p.e.in_gate, &p.e.in_up}) {
         Operand part = *o;
         part.data = static_cast<const uint8_t*>(o->data) + r * o->ld;
@@ -361,7 +361,7 @@ int muon_feed_forward_backward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* 
   if (dw_gate) list[n++] = plain(hidden, dim, t, operand(w.dgate, w.ldh, dt, true), ox, dw_gate->data, dw_gate->ld, dt);
   if (dw_up) list[n++] = plain(hidden, dim, t, operand(w.dup, w.ldh, dt, true), ox, dw_up->data, dw_up->ld, dt);
   if (dw_down) list[n++] = plain(dim, hidden, t, operand(dy, dt, true), operand(w.h, w.ldh, dt, true), dw_down->data, dw_down->ld, dt);
-  l.products(list, n);
+  l.products(list, n, kMaxProducts);
   return l.rc;
 }
 

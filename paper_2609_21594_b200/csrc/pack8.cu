@@ -18,10 +18,26 @@ __device__ __forceinline__ float2 values2(uint32_t pair) {
   return __half22float2(__half2(h));
 }
 
-// Up to N consecutive elements of a row, by 16 bytes; those from `left` on count as zeros.
-template <typename T, int N>
-__device__ __forceinline__ void load_run(const T* p, int left, float (&v)[N]) {
-  if (left >= N) {
+// Up to N consecutive elements of a row, by 16 bytes; those from `left` on count as zeros.  WORDS: bf16 that begins anywhere, moved out of aligned
+// words, of which none may end behind `last`.
+template <bool WORDS, typename T, int N>
+__device__ __forceinline__ void load_run(const T* p, int left, const T* last, float (&v)[N]) {
+  if constexpr (WORDS) {
+    const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p) >> 1) & 1u;
+    const uint32_t* q = reinterpret_cast<const uint32_t*>(p - off);
+    if (left >= N && reinterpret_cast<const T*>(q + N / 2 + 1) <= last) {
+      uint32_t w[N / 2 + 1];
+#pragma unroll
+      for (int i = 0; i <= N / 2; ++i) w[i] = __ldg(q + i);
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) {
+        const uint32_t x = __funnelshift_r(w[i], w[i + 1], 16 * off);
+        v[2 * i] = __uint_as_float(x << 16);
+        v[2 * i + 1] = __uint_as_float(x & 0xffff0000u);
+      }
+      return;
+    }
+  } else if (left >= N) {
 #pragma unroll
     for (int q = 0; q < N * int(sizeof(T)) / 16; ++q) {
       const uint4 x = __ldg(reinterpret_cast<const uint4*>(p) + q);
@@ -80,7 +96,7 @@ __device__ __forceinline__ uint32_t finite_top(const float (&v)[N], bool* odd) {
 // Blocks of 1 x 128: eight lanes hold a block, sixteen elements each, and find its largest magnitude by shuffles.  Blocks are counted along the
 // rows, one row after the other; a group of lanes takes UNROLL consecutive ones, so that its loads are in flight together and the division
 // that finds the row is made once.
-template <typename T, int UNROLL>
+template <typename T, int UNROLL, bool WORDS>
 __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const T* x, int64_t ldx, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds,
                                                                  int64_t rows, int32_t cols, uint32_t per_row) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // a product that follows may request its weights
@@ -96,7 +112,7 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const T* x, int
     at_row[u] = row;
     at_blk[u] = blk;
     const int col = int(blk) * kBlock + sub * 16;
-    load_run(x + row * ldx + col, row < rows ? cols - col : 0, v[u]);
+    load_run<WORDS>(x + row * ldx + col, row < rows ? cols - col : 0, x + (rows - 1) * ldx + cols, v[u]);
     if (++blk == per_row) {
       blk = 0;
       ++row;
@@ -176,7 +192,7 @@ __global__ void __launch_bounds__(kSquareThreads) quantize_squares_kernel(const 
     const int64_t row = row0 + kStride * i;
     const int left = row < rows ? cols - col : 0;
     if constexpr (WIDE) {
-      load_run(x + row * ldx + col, left, v[i]);
+      load_run<false>(x + row * ldx + col, left, x, v[i]);
     } else {
 #pragma unroll
       for (int j = 0; j < kPer; ++j) v[i][j] = 32 * j < left ? float(x[row * ldx + col + 32 * j]) : 0.f;
@@ -272,36 +288,80 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint8_t* cod
   }
 }
 
-// Rows that no wide access fits: a warp takes 128 columns, a lane elements l, l + 32, l + 64, l + 96, so that each access of the warp is one run.
+// Rows of y that begin anywhere: a thread takes the eight elements between two 16-byte borders of y (the first of a row those before the first
+// border) and moves their codes, which begin anywhere, out of two or three aligned words.  They may lie in two blocks.
 template <typename T, int UNROLL>
 __global__ void __launch_bounds__(kThreads) dequantize_any_kernel(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int32_t row_shift,
                                                                   T* y, int64_t ldy, int64_t rows, int32_t cols, uint32_t per_row) {
-  const int lane = threadIdx.x & 31;
-  const int64_t first = (int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * UNROLL;
-  int64_t row = first / per_row;
-  uint32_t blk = uint32_t(first - row * per_row);
-  uint8_t c[UNROLL][4], e[UNROLL];
-  T* out[UNROLL];
-  int left[UNROLL];
+  const int64_t first = int64_t(blockIdx.x) * (kThreads * UNROLL) + threadIdx.x;
+  const uint8_t* const last = codes + (rows - 1) * ldc + cols;
+  constexpr int kBorder = 16 / int(sizeof(T));
+  uint32_t w[UNROLL][2];
+  uint8_t e[UNROLL][2];
+  int64_t row[UNROLL];
+  int col[UNROLL], count[UNROLL];
+  bool whole[UNROLL];
 #pragma unroll
   for (int u = 0; u < UNROLL; ++u) {
-    left[u] = row < rows ? cols - int(blk) * kBlock - lane : 0;
-    out[u] = y + row * ldy + int64_t(blk) * kBlock + lane;
-    const uint8_t* p = codes + row * ldc + int64_t(blk) * kBlock + lane;
-    e[u] = row < rows ? __ldg(scales + (row >> row_shift) * lds + blk) : 0;
+    const int64_t i = first + u * kThreads;
+    row[u] = i <= UINT32_MAX ? int64_t(uint32_t(i) / per_row) : i / per_row;
+    count[u] = 0;
+    if (row[u] >= rows) continue;
+    const int g = int(i - row[u] * per_row);
+    const int before = int(reinterpret_cast<uintptr_t>(y + row[u] * ldy) / sizeof(T)) & (kBorder - 1), head = (kBorder - before) & (kBorder - 1);
+    col[u] = g == 0 ? 0 : head + (g - 1) * 8;
+    count[u] = g == 0 ? min(head, cols) : min(8, cols - col[u]);
+    whole[u] = g > 0 && count[u] == 8;
+    if (count[u] <= 0) continue;
+    const uint8_t* s = scales + (row[u] >> row_shift) * lds;
+    e[u][0] = __ldg(s + (col[u] >> 7));
+    e[u][1] = __ldg(s + ((col[u] + count[u] - 1) >> 7));
+    const uint8_t* p = codes + row[u] * ldc + col[u];
+    const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 3u;
+    const uint8_t* base = p - off;
+    if (whole[u] && base >= codes && base + 12 <= last) {
+      const uint32_t* q = reinterpret_cast<const uint32_t*>(base);
+      const uint32_t a = __ldg(q), b = __ldg(q + 1), c = __ldg(q + 2);
+      w[u][0] = __funnelshift_r(a, b, 8 * off);
+      w[u][1] = __funnelshift_r(b, c, 8 * off);
+    } else {
+      w[u][0] = w[u][1] = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) c[u][j] = 32 * j < left[u] ? __ldg(p + 32 * j) : 0;
-    if (++blk == per_row) {
-      blk = 0;
-      ++row;
+      for (int k = 0; k < 8; ++k)
+        if (k < count[u]) w[u][k >> 2] |= uint32_t(p[k]) << (8 * (k & 3));
     }
   }
 #pragma unroll
   for (int u = 0; u < UNROLL; ++u) {
-    const float scale = scale_of(e[u]);
+    if (count[u] <= 0) continue;
+    const float lo = scale_of(e[u][0]), hi = scale_of(e[u][1]);
+    const int border = ((col[u] >> 7) + 1) * kBlock - col[u];       // elements from here on lie in the second block
+    float v[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (32 * j < left[u]) out[u][32 * j] = T(values2(c[u][j]).x * scale);
+    for (int k = 0; k < 4; ++k) {
+      const float2 f = values2(w[u][k >> 1] >> (16 * (k & 1)));
+      v[2 * k] = f.x * (2 * k < border ? lo : hi);
+      v[2 * k + 1] = f.y * (2 * k + 1 < border ? lo : hi);
+    }
+    T* out = y + row[u] * ldy + col[u];
+    if (whole[u]) {
+      if constexpr (sizeof(T) == 2) {
+        uint32_t o[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+          o[k] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+        *reinterpret_cast<uint4*>(out) = make_uint4(o[0], o[1], o[2], o[3]);
+      } else {
+        reinterpret_cast<float4*>(out)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(out)[1] = make_float4(v[4], v[5], v[6], v[7]);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < count[u]) out[k] = T(v[k]);
+    }
   }
 }
 
@@ -316,9 +376,13 @@ int quantize(int64_t rows, int64_t cols, const T* x, int64_t ldx, const Operand&
   const int64_t per_row = (cols + kBlock - 1) / kBlock;
   if (out.block_rows == 1) {
     constexpr int kUnroll = sizeof(T) == 2 ? 2 : 1, kAnyUnroll = 4;
-    const int64_t per_block = w ? int64_t(kThreads / 8) * kUnroll : int64_t(kThreads / 32) * kAnyUnroll, blocks = (rows * per_row + per_block - 1) / per_block;
+    // bf16 that begins anywhere, into codes that begin at 16 bytes, as the torch front end's do
+    const bool words = sizeof(T) == 2 && !w && wide(codes, out.ld, 16);
+    const int64_t per_block = w || words ? int64_t(kThreads / 8) * kUnroll : int64_t(kThreads / 32) * kAnyUnroll, blocks = (rows * per_row + per_block - 1) / per_block;
     if (blocks > INT32_MAX) return MUON_ERR_UNSUPPORTED;
-    auto* k = w ? quantize_rows_kernel<T, kUnroll> : quantize_rows_any_kernel<T, kAnyUnroll>;
+    auto* k = w ? quantize_rows_kernel<T, kUnroll, false> : quantize_rows_any_kernel<T, kAnyUnroll>;
+    if constexpr (sizeof(T) == 2)
+      if (words) k = quantize_rows_kernel<T, kUnroll, true>;
     k<<<unsigned(blocks), kThreads, 0, st>>>(x, ldx, codes, out.ld, scales, out.lds, rows, int32_t(cols), uint32_t(per_row));
   } else {
     const int64_t blocks = (rows + kBlock - 1) / kBlock * per_row;
@@ -332,12 +396,12 @@ int quantize(int64_t rows, int64_t cols, const T* x, int64_t ldx, const Operand&
 template <typename T>
 int dequantize(int64_t rows, int64_t cols, const Operand& in, T* y, int64_t ldy, cudaStream_t st) {
   const uint8_t* codes = static_cast<const uint8_t*>(in.data);
-  constexpr int kUnroll = 2, kAnyUnroll = 4;
+  constexpr int kUnroll = 2;
   const bool w = wide(codes, in.ld, 16) && wide(y, ldy * int64_t(sizeof(T)), 16);
-  const int64_t per_row = w ? (cols + 15) / 16 : (cols + kBlock - 1) / kBlock;
-  const int64_t per_block = w ? kThreads * kUnroll : kThreads / 32 * kAnyUnroll, blocks = (rows * per_row + per_block - 1) / per_block;
+  const int64_t per_row = w ? (cols + 15) / 16 : (cols + 7) / 8 + 1;
+  const int64_t per_block = kThreads * kUnroll, blocks = (rows * per_row + per_block - 1) / per_block;
   if (blocks > INT32_MAX) return MUON_ERR_UNSUPPORTED;
-  auto* k = w ? dequantize_kernel<T, kUnroll> : dequantize_any_kernel<T, kAnyUnroll>;
+  auto* k = w ? dequantize_kernel<T, kUnroll> : dequantize_any_kernel<T, kUnroll>;
   k<<<unsigned(blocks), kThreads, 0, st>>>(codes, in.ld, in.scales, in.lds, in.block_rows == 1 ? 0 : 7, y, ldy, rows, int32_t(cols), uint32_t(per_row));
   return done(1);
 }

@@ -27,6 +27,7 @@ constexpr uint32_t kWord = 2 * 512;             // scales of four k-blocks: 128 
 constexpr uint32_t kScales = kScaleBlocks / 4 * kWord;
 constexpr int kScaleRing = 2;
 constexpr int kMaxSplit = 8;
+constexpr int kMaxTokens = 128;                 // of a block
 
 struct FewArgs {
   CUtensorMap w[2], x[2];                       // of each segment; gated: w_gate and w_up
@@ -37,7 +38,7 @@ struct FewArgs {
   Operand gate, up;                             // 8-bit g and u
   Scales sw, sx;
   int32_t m, n, kblocks, segments;
-  int32_t tokens;                               // columns of the instruction: m rounded up to 16
+  int32_t tokens;                               // columns of the instruction, a multiple of 16; blockIdx.y: which of them
   int32_t stages, split, columns;               // columns: of tensor memory
   int32_t activation, keep, codes_wide;
   uint32_t stage_bytes, scale_off, bar_off;
@@ -98,7 +99,7 @@ __global__ void __launch_bounds__(kThreads, 2) product_few_kernel(const __grid_c
 
   const int warp = uniform_warp(), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
-  const int n0 = int(blockIdx.x / unsigned(L.split)) * kRowsW;
+  const int n0 = int(blockIdx.x / unsigned(L.split)) * kRowsW, t0 = int(blockIdx.y) * L.tokens;
   const int all_kb = L.kblocks * L.segments;
   const int kb0 = int(int64_t(all_kb) * rank / L.split), kb1 = int(int64_t(all_kb) * (rank + 1) / L.split);
   auto give_up = [&](int code) {
@@ -153,7 +154,7 @@ __global__ void __launch_bounds__(kThreads, 2) product_few_kernel(const __grid_c
       };
       auto rows = [&](int kb, int s) {
         const int seg = kb >= L.kblocks ? 1 : 0, k0 = (kb - seg * L.kblocks) * (EIGHT ? 128 : 64);
-        tma_load(base + uint32_t(s) * L.stage_bytes + kTiles * kTileBytes, &L.x[seg], full_bar(s), k0, 0);
+        tma_load(base + uint32_t(s) * L.stage_bytes + kTiles * kTileBytes, &L.x[seg], full_bar(s), k0, t0);
       };
       const int first = min(L.stages, kb1 - kb0);
       for (int i = 0; i < first; ++i) weights(kb0 + i, i);
@@ -242,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, 2) product_few_kernel(const __grid_c
         if (!ok) break;
         uint32_t w[2][4][4];
         gather_scales(L.sw, n0, kb, kb1, lane, w[0]);
-        gather_scales(L.sx, 0, kb, kb1, lane, w[1]);
+        gather_scales(L.sx, t0, kb, kb1, lane, w[1]);
         const uint32_t to = base + L.scale_off + place * kScales + uint32_t(lane) * 16u;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -284,11 +285,12 @@ __global__ void __launch_bounds__(kThreads, 2) product_few_kernel(const __grid_c
   cluster_sync_all();                           // every block of the cluster has left its sums
   const Activation act = activation_of(L.activation);
   const int col = n0 + lane * 4;
-  for (int t = int(rank) * (kThreads / 32) + warp; t < L.m; t += L.split * (kThreads / 32)) {
+  for (int i = int(rank) * (kThreads / 32) + warp; i < min(L.tokens, L.m - t0); i += L.split * (kThreads / 32)) {
+    const int t = t0 + i;
     float sum[kTiles][4];
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-      const uint32_t at = base + uint32_t((i * L.tokens + t) * kRowsW + lane * 4) * 4u;
+    for (int k = 0; k < kTiles; ++k) {
+      const uint32_t at = base + uint32_t((k * L.tokens + i) * kRowsW + lane * 4) * 4u;
       float4 part[kMaxSplit];
 #pragma unroll
       for (int r = 0; r < kMaxSplit; ++r)
@@ -302,7 +304,7 @@ __global__ void __launch_bounds__(kThreads, 2) product_few_kernel(const __grid_c
           v.z += part[r].z;
           v.w += part[r].w;
         }
-      sum[i][0] = v.x; sum[i][1] = v.y; sum[i][2] = v.z; sum[i][3] = v.w;
+      sum[k][0] = v.x; sum[k][1] = v.y; sum[k][2] = v.z; sum[k][3] = v.w;
     }
     const bool inside = col < L.n;              // a multiple of 8 columns: four are all inside or all outside
     auto put = [&](int which, float a, float b, float c, float d) {
@@ -391,7 +393,7 @@ int launch(const FewArgs& L, int device, uint32_t bytes, bool follows, cudaStrea
   static SharedMemoryLimit limit;
   if (!limit.raise(device, kWholeSm, product_few_kernel<W_MN, EIGHT, EPI, CODES>)) return MUON_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(unsigned((L.n + kRowsW - 1) / kRowsW * L.split), 1, 1);
+  cfg.gridDim = dim3(unsigned((L.n + kRowsW - 1) / kRowsW * L.split), unsigned((L.m + L.tokens - 1) / L.tokens), 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.dynamicSmemBytes = bytes;
   cfg.stream = st;
@@ -406,9 +408,45 @@ int launch(const FewArgs& L, int device, uint32_t bytes, bool follows, cudaStrea
   return cudaLaunchKernelEx(&cfg, product_few_kernel<W_MN, EIGHT, EPI, CODES>, L) == cudaSuccess ? 1 : MUON_ERR_CUDA;
 }
 
+// How the work is cut, and about how many clocks that takes.
+struct FewPlan {
+  int tokens, split, stages;
+  uint32_t stage_bytes, sums, extra;
+  double clocks;
+};
+FewPlan plan_few(const Product& q, int sms) {
+  FewPlan r = {};
+  const bool eight = q.a[0].type == kTypeE4m3;
+  const int tiles = q.e.kind == kGated ? 2 : 1;
+  const int64_t wide = (int64_t(q.n) + kRowsW - 1) / kRowsW, total = int64_t((q.k + (eight ? 127 : 63)) / (eight ? 128 : 64)) * q.segments;
+  r.extra = (eight ? kScaleRing * kScales : 0) + 256 + 1024;
+  int64_t blocks = 0, on_sm = 0;
+  uint32_t room = 0;
+  // As many blocks as fit at once: first by parts of k, then, where tiles and k are few, by parts of the tokens, each of which reads the weights again
+  // (from L2) but adds up less.
+  for (int parts = (q.m + kMaxTokens - 1) / kMaxTokens;; parts *= 2) {
+    r.tokens = ((q.m + parts - 1) / parts + 15) / 16 * 16;
+    r.sums = uint32_t(tiles * r.tokens) * kRowsW * 4u;  // take the ring's place in the end
+    room = r.sums + r.extra <= kHalfSm ? kHalfSm : kWholeSm;
+    on_sm = room == kHalfSm ? 2 : 1;
+    r.split = int(std::max<int64_t>(1, std::min<int64_t>({kMaxSplit, sms * on_sm / wide, total})));
+    blocks = wide * r.split * ((q.m + r.tokens - 1) / r.tokens);
+    if (r.tokens == 16 || blocks * 2 > sms * on_sm) break;
+  }
+  const int64_t each = (total + r.split - 1) / r.split;
+  r.stage_bytes = uint32_t(tiles) * kTileBytes + uint32_t(r.tokens) * 128u;
+  r.stages = int(std::min<int64_t>({kMaxStages, (room - r.extra) / r.stage_bytes, each}));
+  // A multiprocessor takes in 64 bytes a clock; sums are written, read by a peer and added at 16 bytes a clock.
+  const double busy = double(std::min<int64_t>(on_sm, (blocks + sms - 1) / sms)) * (double(each) * r.stage_bytes / 64 + r.sums / 16.0);
+  r.clocks = double((blocks + sms * on_sm - 1) / (sms * on_sm)) * busy + 8000;
+  return r;
+}
+
 }  // namespace
 
-bool product_few_takes(const Product& p) { return p.m <= kFewRows && !p.a[0].mn_major; }
+bool product_few_takes(const Product& p, int sms) {
+  return p.m <= kFewRows && !p.a[0].mn_major && plan_few(p, sms).clocks < 0.85 * products_tc_clocks(&p, 1, sms);
+}
 
 int launch_product_few(muon_ctx* ctx, const Product& q, int sms, bool follows, cudaStream_t st) {
   if (!ctx->tmap_encode) return MUON_ERR_CUDA;
@@ -420,16 +458,12 @@ int launch_product_few(muon_ctx* ctx, const Product& q, int sms, bool follows, c
   L.n = q.n;
   L.kblocks = (q.k + (eight ? 127 : 63)) / (eight ? 128 : 64);
   L.segments = q.segments;
-  L.tokens = (q.m + 15) / 16 * 16;
-  L.stage_bytes = uint32_t(tiles) * kTileBytes + uint32_t(L.tokens) * 128u;
-  // the sums that take the ring's place in the end, and two blocks to a multiprocessor where these fit a half of it
-  const uint32_t sums = uint32_t(tiles * L.tokens) * kRowsW * 4u, extra = (eight ? kScaleRing * kScales : 0) + 256 + 1024;
-  const uint32_t room = sums + extra <= kHalfSm ? kHalfSm : kWholeSm;
-  const int64_t wide = (int64_t(q.n) + kRowsW - 1) / kRowsW, slots = int64_t(sms) * (room == kHalfSm ? 2 : 1);
-  const int total = L.kblocks * L.segments;
-  L.split = int(std::max<int64_t>(1, std::min<int64_t>({kMaxSplit, slots / wide, int64_t(total)})));
-  L.stages = std::min({kMaxStages, int((room - extra) / L.stage_bytes), (total + L.split - 1) / L.split});
-  const uint32_t ring = std::max(uint32_t(L.stages) * L.stage_bytes, sums);
+  const FewPlan plan = plan_few(q, sms);
+  L.tokens = plan.tokens;
+  L.split = plan.split;
+  L.stages = plan.stages;
+  L.stage_bytes = plan.stage_bytes;
+  const uint32_t ring = std::max(uint32_t(L.stages) * L.stage_bytes, plan.sums);
   L.scale_off = (ring + 1023u) & ~1023u;
   L.bar_off = L.scale_off + (eight ? kScaleRing * kScales : 0);
   const int columns = tiles * L.tokens + (eight ? 8 : 0);

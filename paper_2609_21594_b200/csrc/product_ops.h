@@ -56,12 +56,15 @@ constexpr int kMaxProducts = 3;   // of a launch
 // The tensor-core engine takes a list of products with operands of one type and one order in memory, if TMA can address all tensors.
 bool products_tc_take(const Product* p, int count);
 int launch_products_tc(muon_ctx* ctx, const Product* p, int count, cudaStream_t st);
-// Of these, products of at most kFewRows rows, whose time is that of reading B, have a kernel of their own.  follows: the launch before this one in the
-// stream is of the same call and does not write B, so this one may begin before that one has ended.
-constexpr int kFewRows = 128;
-bool product_few_takes(const Product& p);
+// About how many clocks they take there, from the rounds of tiles.
+double products_tc_clocks(const Product* p, int count, int sms);
+// Products of few rows, whose time is that of reading B, have a kernel of their own, which takes them where its blocks are expected to be done sooner.
+// follows: the launch before this one in the stream is of the same call and does not write B, so this one may begin before that one has ended.
+constexpr int kFewRows = 1024;
+bool product_few_takes(const Product& p, int sms);
 int launch_product_few(muon_ctx* ctx, const Product& p, int sms, bool follows, cudaStream_t st);
-int launch_products_simt(const Product* p, int count, int sms, cudaStream_t st);      // operands of one type
+// Operands of one type.  siblings: products of about this size that a call may launch together, of which `count` are wanted now.
+int launch_products_simt(const Product* p, int count, int siblings, int sms, cudaStream_t st);
 
 int launch_quantize(int dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx, const Operand& out, int sms, cudaStream_t st);
 int launch_dequantize(int dtype, int64_t rows, int64_t cols, const Operand& in, void* y, int64_t ldy, int sms, cudaStream_t st);

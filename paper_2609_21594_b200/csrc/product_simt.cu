@@ -1,6 +1,6 @@
 // Matrix products on CUDA cores: fp32, and every layout that TMA cannot address.
 //
-// A block of 256 threads forms a TILE x TILE tile of C, R x R of it per thread (R = TILE / 16), from 16 values of k at a time, staged in shared
+// A block of 256 threads forms a TILE x TILE tile of C, R x R of it per thread (R = TILE / 16), from 16 or 32 values of k at a time, staged in shared
 // memory as fp32 and loaded one step ahead.  A thread's rows and columns are two runs, one in each half of the tile, so that its operands are
 // two wide loads without bank conflicts, and so that in a gated product (columns [0, TILE/2) of the tile are those of B_0, the others
 // the same columns of B_1) it holds g and u of the same elements.  Sums are fp32, by two-wide multiply-adds.
@@ -19,7 +19,10 @@ namespace muon {
 namespace {
 
 namespace cg = cooperative_groups;
-constexpr int kThreads = 256, kStep = 16, kMaxSplit = 8;
+constexpr int kThreads = 256, kMaxSplit = 8;
+// Values of k in a step.  The small tiles are latency-bound: twice as many in flight (32 instead of 16) halve the number of waits.
+template <int TILE> constexpr int kStep = TILE == 64 ? 32 : 16;
+template <int TILE> constexpr int kPitch = TILE == 64 ? 66 : 132;      // of a staged row: neighbouring k in other banks, rows aligned for the wide loads
 
 struct SimtArgs {
   Product p[kMaxProducts];
@@ -44,10 +47,10 @@ __device__ __forceinline__ float element_of(const Operand& o, int64_t row, int64
   return value_at<kTypeE4m3>(p + at) * scale_of(__ldg(o.scales + row / o.block_rows * o.lds + (col >> 7)));
 }
 
-// What a thread loads of an operand in every step: R elements, SLOT apart along the memory's rows.  Threads run along these rows.
+// What a thread loads of an operand in every step.  Threads run along the memory's rows.
 template <int TILE, int TYPE>
 struct Loader {
-  static constexpr int R = TILE / 16;
+  static constexpr int kStepK = kStep<TILE>, kLoads = TILE * kStepK / kThreads, kRowsApart = kThreads / kStepK;
   const Operand *lo, *hi;       // hi: of the second half of the tile, which is another matrix or the same
   bool mn;
   int row_lo, row_hi, rows;     // of the operand: the first element's in each half of the tile
@@ -57,26 +60,26 @@ struct Loader {
     hi = halves ? &second_half : &first_half;
     mn = lo->mn_major != 0;
     rows = rows_;
-    k = mn ? int(threadIdx.x) / TILE : int(threadIdx.x) % kStep;
-    row_lo = first + (mn ? int(threadIdx.x) % TILE : int(threadIdx.x) / kStep);
+    k = mn ? int(threadIdx.x) / TILE : int(threadIdx.x) % kStepK;
+    row_lo = first + (mn ? int(threadIdx.x) % TILE : int(threadIdx.x) / kStepK);
     row_hi = halves ? row_lo : row_lo + TILE / 2;
   }
-  __device__ __forceinline__ void load(int k0, int kdim, float (&v)[R]) const {
+  __device__ __forceinline__ void load(int k0, int kdim, float (&v)[kLoads]) const {
     if (mn) {                   // slot i is kThreads / TILE values of k further
       const bool in = row_lo < rows;
 #pragma unroll
-      for (int i = 0; i < R; ++i) {
+      for (int i = 0; i < kLoads; ++i) {
         const int kk = k0 + k + i * (kThreads / TILE);
         v[i] = 0.f;
         if (in && kk < kdim) v[i] = one(*lo, kk, row_lo);
       }
-    } else {                    // slot i is 16 rows further
+    } else {                    // slot i is kRowsApart rows further
       const bool in = k0 + k < kdim;
 #pragma unroll
-      for (int i = 0; i < R; ++i) {
-        const int r = (i < R / 2 ? row_lo : row_hi) + (i % (R / 2)) * 16;
+      for (int i = 0; i < kLoads; ++i) {
+        const int r = (i < kLoads / 2 ? row_lo : row_hi) + (i % (kLoads / 2)) * kRowsApart;
         v[i] = 0.f;
-        if (in && r < rows) v[i] = one(i < R / 2 ? *lo : *hi, r, k0 + k);
+        if (in && r < rows) v[i] = one(i < kLoads / 2 ? *lo : *hi, r, k0 + k);
       }
     }
   }
@@ -85,12 +88,12 @@ struct Loader {
     if constexpr (TYPE == kTypeE4m3) return x * scale_of(__ldg(m.scales + (m.block_rows == 1 ? r : r >> 7) * m.lds + (c >> 7)));
     return x;
   }
-  __device__ __forceinline__ void stage(float (*s)[TILE + 4], const float (&v)[R]) const {
+  __device__ __forceinline__ void stage(float (*s)[kPitch<TILE>], const float (&v)[kLoads]) const {
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
+    for (int i = 0; i < kLoads; ++i) {
       const int idx = int(threadIdx.x) + i * kThreads;
       if (mn) s[idx / TILE][idx % TILE] = v[i];
-      else s[idx % kStep][idx / kStep] = v[i];
+      else s[idx % kStepK][idx / kStepK] = v[i];
     }
   }
 };
@@ -137,8 +140,8 @@ __device__ __forceinline__ void finish(const Product& p, const Activation& f, in
 
 template <int TILE, int TYPE>
 __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant__ SimtArgs L) {
-  constexpr int R = TILE / 16, H = R / 2;
-  __shared__ __align__(16) float stages[4][kStep][TILE + 4];      // two places for A, two for B
+  constexpr int R = TILE / 16, H = R / 2, kStepK = kStep<TILE>;
+  __shared__ __align__(16) float stages[4][kStepK][kPitch<TILE>];      // two places for A, two for B
   const int block = int(blockIdx.x) / L.split, rank = int(blockIdx.x) % L.split;
   int which = 0;
   for (int i = 1; i < L.count; ++i)
@@ -149,10 +152,10 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
   const int m0 = tile % tiles_m * TILE, n0 = tile / tiles_m * (gated ? TILE / 2 : TILE);
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   uint64_t acc[R][H] = {};
-  const int steps = (p.k + kStep - 1) / kStep, total = steps * p.segments;
+  const int steps = (p.k + kStepK - 1) / kStepK, total = steps * p.segments;
   const int begin = int(int64_t(total) * rank / L.split), end = int(int64_t(total) * (rank + 1) / L.split);
-  float va[R], vb[R];
   Loader<TILE, TYPE> la, lb;
+  float va[decltype(la)::kLoads], vb[decltype(lb)::kLoads];
   int segment = -1;
   auto load = [&](int t) {
     const int s = t >= steps ? 1 : 0;
@@ -161,8 +164,8 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
       lb.init(p.b[s], p.b[1], gated, n0, p.n);
       segment = s;
     }
-    la.load((t - s * steps) * kStep, p.k, va);
-    lb.load((t - s * steps) * kStep, p.k, vb);
+    la.load((t - s * steps) * kStepK, p.k, va);
+    lb.load((t - s * steps) * kStepK, p.k, vb);
   };
   auto keep = [&](int t) {
     la.stage(stages[t & 1], va);
@@ -176,7 +179,7 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
   for (int t = begin; t < end; ++t) {
     if (t + 1 < end) load(t + 1);
 #pragma unroll
-    for (int k = 0; k < kStep; ++k) {
+    for (int k = 0; k < kStepK; ++k) {
       float a[R];
       uint64_t b[H];
 #pragma unroll
@@ -208,27 +211,28 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
   auto row_of = [&](int i) { return (i / H) * (TILE / 2) + ty * H + i % H; };
   if constexpr (TILE == 64) {
     if (L.split > 1) {
-      constexpr int kPitch = TILE + 1;
-      static_assert(TILE * kPitch <= 4 * kStep * (TILE + 4), "the sums take the place of the operands");
+      constexpr int kRow = TILE + 1;
+      static_assert(TILE * kRow <= 4 * kStepK * kPitch<TILE>, "the sums take the place of the operands");
       float* sums = &stages[0][0][0];
 #pragma unroll
       for (int i = 0; i < R; ++i)
 #pragma unroll
         for (int j = 0; j < H; ++j) {
           const float2 pair = both(acc[i][j]);
-          float* to = sums + row_of(i) * kPitch + (2 * j / H) * (TILE / 2) + tx * H + (2 * j) % H;
+          float* to = sums + row_of(i) * kRow + (2 * j / H) * (TILE / 2) + tx * H + (2 * j) % H;
           to[0] = pair.x;
           to[1] = pair.y;
         }
       cg::cluster_group cl = cg::this_cluster();
       cl.sync();
+#pragma unroll 2
       for (int i = rank * kThreads + int(threadIdx.x); i < TILE * TILE / 2; i += L.split * kThreads) {
         const int r = i / (TILE / 2), c = i % (TILE / 2);
         float first[kMaxSplit], second[kMaxSplit];
 #pragma unroll
         for (int q = 0; q < kMaxSplit; ++q)
           if (q < L.split) {
-            const float* from = cl.map_shared_rank(sums, unsigned(q)) + r * kPitch + c;
+            const float* from = cl.map_shared_rank(sums, unsigned(q)) + r * kRow + c;
             first[q] = from[0];
             second[q] = from[TILE / 2];
           }
@@ -276,7 +280,7 @@ int launch(const SimtArgs& L, int64_t tiles, cudaStream_t st) {
 
 }  // namespace
 
-int launch_products_simt(const Product* list, int count, int sms, cudaStream_t st) {
+int launch_products_simt(const Product* list, int count, int siblings, int sms, cudaStream_t st) {
   SimtArgs L = {};
   int64_t tiles[2] = {0, 0}, most[2] = {0, 0};      // of 64 and of 128: of all products, of one of them
   int64_t begin[2][kMaxProducts] = {}, steps = INT64_MAX;
@@ -291,15 +295,15 @@ int launch_products_simt(const Product* list, int count, int sms, cudaStream_t s
       tiles[s] += n;
       most[s] = std::max(most[s], n);
     }
-    steps = std::min<int64_t>(steps, (int64_t(p.k) + kStep - 1) / kStep * p.segments);
+    steps = std::min<int64_t>(steps, (int64_t(p.k) + kStep<64> - 1) / kStep<64> * p.segments);
     ++L.count;
   }
   if (L.count == 0) return 0;
   // A tile of 128 reads each operand half as often; with fewer of them than multiprocessors most of the device would stand still.
-  const int large = most[1] >= sms ? 1 : 0;
-  // Three blocks of the small tiles fit a multiprocessor; a part of k is worth a block from four steps on.  One product decides, not how many
-  // come with it: a gradient is the same, bit for bit, whichever others are wanted.
-  L.split = large ? 1 : int(std::max<int64_t>(1, std::min<int64_t>({kMaxSplit, 3 * int64_t(sms) / most[0], steps / 4})));
+  const int large = most[1] * siblings >= sms ? 1 : 0;
+  // Three blocks of the small tiles fit a multiprocessor; a part of k is worth a block from four steps on.  `siblings` decides, not how many of them
+  // are in this launch: a gradient is the same, bit for bit, whichever others are wanted.
+  L.split = large ? 1 : int(std::max<int64_t>(1, std::min<int64_t>({kMaxSplit, 3 * int64_t(sms) / (most[0] * siblings), steps / 4})));
   if (tiles[large] * L.split > INT32_MAX) return MUON_ERR_UNSUPPORTED;
   for (int i = 0; i < L.count; ++i) L.tile_begin[i] = int32_t(begin[large][i]);
   switch (list[0].a[0].type) {

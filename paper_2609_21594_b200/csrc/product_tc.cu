@@ -614,7 +614,34 @@ int launch(const TcProducts& L, int device, int pairs, cudaStream_t st) {
   return cudaGetLastError() == cudaSuccess ? 1 : MUON_ERR_CUDA;
 }
 
+// Columns of B per CTA, and about how many clocks the launch takes: rounds of tiles times k-blocks, which take 560 clocks with 256 columns and 450 with
+// 128 (whose operands are three quarters of the bytes for half of the work), and 12000 for what does not grow.  Narrow tiles pay where wide ones
+// leave pairs without work.  8 bits: the scales of blocks of kept g and u need 128 columns of both, and MN-major operands come 128 columns at a time.
+struct PairPlan {
+  int half;
+  double clocks;
+};
+PairPlan plan_pairs(const Product* list, int count, int sms) {
+  const Product& first = list[0];
+  const bool eight = first.a[0].type == kTypeE4m3, gated = first.e.kind == kGated;
+  const bool may_narrow = !(eight && first.b[0].mn_major) && !(gated && first.e.gate_up_type == kTypeE4m3);
+  PairPlan best = {};
+  for (int half = 128; half >= (may_narrow ? 64 : 128); half /= 2) {
+    const int64_t cols = gated ? half : 2 * half, pairs = sms / 2;
+    int64_t tiles = 0, kblocks = 0;
+    for (int i = 0; i < count; ++i) {
+      tiles += (int64_t(list[i].m) + 2 * kRows - 1) / (2 * kRows) * ((list[i].n + cols - 1) / cols);
+      kblocks = std::max<int64_t>(kblocks, int64_t((list[i].k + (eight ? 127 : 63)) / (eight ? 128 : 64)) * list[i].segments);
+    }
+    const double clocks = double((tiles + pairs - 1) / pairs) * double(kblocks) * (half == 128 ? 560 : 450) + 12000;
+    if (half == 128 || clocks < best.clocks) best = {half, clocks};
+  }
+  return best;
+}
+
 }  // namespace
+
+double products_tc_clocks(const Product* list, int count, int sms) { return plan_pairs(list, count, sms).clocks; }
 
 bool products_tc_take(const Product* list, int count) {
   if (count < 1 || count > kMaxProducts) return false;
@@ -654,8 +681,9 @@ int launch_products_tc(muon_ctx* ctx, const Product* list, int count, cudaStream
   const Epilogue& e0 = list[0].e;
   const bool eight = list[0].a[0].type == kTypeE4m3, amn = list[0].a[0].mn_major, bmn = list[0].b[0].mn_major;
   const bool codes = e0.gate_up_type == kTypeE4m3 && e0.kind != kPlain;
+  const int pairs = sms / 2, dev = ctx->device;
   L.count = count;
-  L.half = 128;
+  L.half = plan_pairs(list, count, sms).half;
   L.activation = e0.activation;
   L.keep = e0.kind == kGated && e0.gate;
   L.gate = e0.in_gate;
@@ -701,7 +729,6 @@ int launch_products_tc(muon_ctx* ctx, const Product* list, int count, cudaStream
   }
   if (!enc.ok) return MUON_ERR_CUDA;
   L.total_tiles = int32_t(tiles);
-  const int pairs = sms / 2, dev = ctx->device;
   if (eight) return bmn ? launch<false, true, true, kPlain>(L, dev, pairs, st) : launch<false, false, true, kPlain>(L, dev, pairs, st);
   if (e0.kind == kGated) return codes ? launch<false, false, false, kGated, true>(L, dev, pairs, st) : launch<false, false, false, kGated>(L, dev, pairs, st);
   if (e0.kind == kGrad) return codes ? launch<false, true, false, kGrad, true>(L, dev, pairs, st) : launch<false, true, false, kGrad>(L, dev, pairs, st);
