@@ -382,16 +382,20 @@ std::tuple<Tensor, Tensor, Tensor> attention_backward(const Tensor& dout, const 
 struct Packed {
   Tensor codes, scales;
 };
+Tensor new_pitched(at::IntArrayRef sizes, int64_t ld, const at::TensorOptions& options) {
+  if (ld == sizes.back()) return at::empty(sizes, options);
+  c10::SmallVector<int64_t, 6> strides(sizes.size(), 1);
+  int64_t next = ld;
+  for (size_t i = sizes.size() - 1; i-- > 0; next *= std::max<int64_t>(sizes[i], 1)) strides[i] = next;
+  return at::empty_strided(sizes, strides, options);
+}
 Packed new_packed(at::IntArrayRef sizes, const at::TensorOptions& options, int64_t block_rows) {
-  std::vector<int64_t> shape(sizes.begin(), sizes.end()), scales = shape;
-  const int64_t cols = shape.back(), ld = (cols + 15) / 16 * 16;
-  shape.back() = ld;
-  scales.back() = (cols + 127) / 128;
+  c10::SmallVector<int64_t, 6> scales(sizes.begin(), sizes.end());
+  const int64_t cols = sizes.back(), blocks = (cols + 127) / 128;
+  scales.back() = blocks;
   if (block_rows > 1) scales[0] = (scales[0] + block_rows - 1) / block_rows;
-  const int64_t blocks = scales.back(), lds = blocks > 8 ? (blocks + 15) / 16 * 16 : (blocks + 3) / 4 * 4;
-  scales.back() = lds;
-  const Tensor codes = at::empty(shape, options.dtype(at::kFloat8_e4m3fn)), bytes = at::empty(scales, options.dtype(at::kByte));
-  return {ld == cols ? codes : codes.narrow(-1, 0, cols), lds == blocks ? bytes : bytes.narrow(-1, 0, blocks)};
+  return {new_pitched(sizes, (cols + 15) / 16 * 16, options.dtype(at::kFloat8_e4m3fn)),
+          new_pitched(scales, blocks > 8 ? (blocks + 15) / 16 * 16 : (blocks + 3) / 4 * 4, options.dtype(at::kByte))};
 }
 
 // A packed matrix as the C ABI takes it, and the tensors that keep its memory.
@@ -407,9 +411,9 @@ PackedView packed(const Tensor& codes, const Tensor& scales, int64_t block_rows,
   v.codes = rows_of(codes, what);
   v.rows = v.codes.size(0);
   v.cols = v.codes.size(1);
-  std::vector<int64_t> each(codes.sizes().begin(), codes.sizes().end());
+  c10::SmallVector<int64_t, 6> each(codes.sizes().begin(), codes.sizes().end());
   each.back() = (v.cols + 127) / 128;
-  const bool rows = scales.sizes().equals(each);
+  const bool rows = scales.sizes().equals(at::IntArrayRef(each));
   const bool squares = codes.dim() == 2 && scales.dim() == 2 && scales.size(0) == (v.rows + 127) / 128 && scales.size(1) == each.back();
   if (block_rows == 0) block_rows = rows ? 1 : 128;     // one row alone: both are the same
   if (!(block_rows == 1 ? rows : squares))

@@ -77,6 +77,20 @@ __device__ __forceinline__ void store_run(uint8_t* p, int left, const float (&v)
   for (int i = 0; i < N; ++i)
     if (i < left) p[i] = uint8_t(c[i >> 2] >> (8 * (i & 3)));
 }
+// Eight values to an address on a 16-byte border.
+__device__ __forceinline__ void store_values(__nv_bfloat16* out, const float* v) {
+  uint32_t o[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+    o[k] = *reinterpret_cast<const uint32_t*>(&b);
+  }
+  *reinterpret_cast<uint4*>(out) = make_uint4(o[0], o[1], o[2], o[3]);
+}
+__device__ __forceinline__ void store_values(float* out, const float* v) {
+  reinterpret_cast<float4*>(out)[0] = make_float4(v[0], v[1], v[2], v[3]);
+  reinterpret_cast<float4*>(out)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
 // The bits of the largest finite magnitude.  The plain maximum passes over NaN; only an infinity makes it look at every value again.
 template <int N>
 __device__ __forceinline__ uint32_t finite_top(const float (&v)[N], bool* odd) {
@@ -93,43 +107,28 @@ __device__ __forceinline__ uint32_t finite_top(const float (&v)[N], bool* odd) {
   return bits;
 }
 
-// Blocks of 1 x 128: eight lanes hold a block, sixteen elements each, and find its largest magnitude by shuffles.  Blocks are counted along the
-// rows, one row after the other; a group of lanes takes UNROLL consecutive ones, so that its loads are in flight together and the division
-// that finds the row is made once.
-template <typename T, int UNROLL, bool WORDS>
+// Blocks of 1 x 128: eight lanes hold a block, sixteen elements each, and find its largest magnitude by shuffles.  Blocks are counted along the rows,
+// one row after the other.  One block a group: with two or four, whose loads would be in flight together, the registers cost more threads
+// than that gains (8192 x 14336 of bf16: 57 us, 5.6 TB/s moved is 1 block; 65 us 2; 110 us 4).  Bound by memory.
+template <typename T, bool WORDS>
 __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const T* x, int64_t ldx, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds,
                                                                  int64_t rows, int32_t cols, uint32_t per_row) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // a product that follows may request its weights
   const int sub = threadIdx.x & 7;
-  const int64_t first = (int64_t(blockIdx.x) * (kThreads / 8) + (threadIdx.x >> 3)) * UNROLL;
-  int64_t row = first <= UINT32_MAX ? int64_t(uint32_t(first) / per_row) : first / per_row;
-  uint32_t blk = uint32_t(first - row * per_row);
-  float v[UNROLL][16];
-  int64_t at_row[UNROLL];
-  uint32_t at_blk[UNROLL];
+  const int64_t block = int64_t(blockIdx.x) * (kThreads / 8) + (threadIdx.x >> 3);
+  const int64_t row = block <= UINT32_MAX ? int64_t(uint32_t(block) / per_row) : block / per_row;
+  const uint32_t blk = uint32_t(block - row * per_row);
+  const int col = int(blk) * kBlock + sub * 16;
+  float v[16];
+  load_run<WORDS>(x + row * ldx + col, row < rows ? cols - col : 0, x + (rows - 1) * ldx + cols, v);
+  bool odd;
+  uint32_t top = finite_top(v, &odd);
 #pragma unroll
-  for (int u = 0; u < UNROLL; ++u) {
-    at_row[u] = row;
-    at_blk[u] = blk;
-    const int col = int(blk) * kBlock + sub * 16;
-    load_run<WORDS>(x + row * ldx + col, row < rows ? cols - col : 0, x + (rows - 1) * ldx + cols, v[u]);
-    if (++blk == per_row) {
-      blk = 0;
-      ++row;
-    }
-  }
-#pragma unroll
-  for (int u = 0; u < UNROLL; ++u) {
-    bool odd;
-    uint32_t top = finite_top(v[u], &odd);
-#pragma unroll
-    for (int d = 1; d < 8; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-    if (at_row[u] >= rows) continue;
-    const uint32_t e = scale_byte(top);
-    const int col = int(at_blk[u]) * kBlock + sub * 16;
-    store_run(codes + at_row[u] * ldc + col, cols - col, v[u], inverse_scale_of(e), odd);
-    if (sub == 0) scales[at_row[u] * lds + at_blk[u]] = uint8_t(e);
-  }
+  for (int d = 1; d < 8; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+  if (row >= rows) return;
+  const uint32_t e = scale_byte(top);
+  store_run(codes + row * ldc + col, cols - col, v, inverse_scale_of(e), odd);
+  if (sub == 0) scales[row * lds + blk] = uint8_t(e);
 }
 
 // The same for rows that no wide load fits: a warp per block, a lane takes elements l, l + 32, l + 64, l + 96.
@@ -227,142 +226,87 @@ __global__ void __launch_bounds__(kSquareThreads) quantize_squares_kernel(const 
   if (threadIdx.x == 0) scales[brow * lds + bcol] = uint8_t(e);
 }
 
-// Sixteen codes at a time, which lie in one block; a thread takes UNROLL of them, a block of threads apart.
-template <typename T, int UNROLL>
+// Sixteen codes a thread, which lie in one block (8192 x 14336 to bf16: 57 to 61 us, 5.8 to 6.2 TB/s; two at a time 62 us).
+template <typename T>
 __global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int32_t row_shift, T* y,
                                                               int64_t ldy, int64_t rows, int32_t cols, uint32_t per_row) {
-  const int64_t first = int64_t(blockIdx.x) * (kThreads * UNROLL) + threadIdx.x;
-  uint4 in[UNROLL];
-  uint8_t e[UNROLL];
-  int64_t row[UNROLL];
-  int col[UNROLL];
+  const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+  const int64_t row = i <= UINT32_MAX ? int64_t(uint32_t(i) / per_row) : i / per_row;
+  if (row >= rows) return;
+  const int col = int(i - row * per_row) * 16, left = cols - col;
+  const uint8_t* p = codes + row * ldc + col;
+  const float scale = scale_of(__ldg(scales + (row >> row_shift) * lds + (col >> 7)));
+  uint32_t w[4] = {0, 0, 0, 0};
+  if (left >= 16) {
+    const uint4 q = __ldg(reinterpret_cast<const uint4*>(p));
+    w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+  } else {
 #pragma unroll
-  for (int u = 0; u < UNROLL; ++u) {
-    const int64_t i = first + u * kThreads;
-    row[u] = i <= UINT32_MAX ? int64_t(uint32_t(i) / per_row) : i / per_row;
-    col[u] = int(i - row[u] * per_row) * 16;
-    if (row[u] >= rows) continue;
-    const uint8_t* p = codes + row[u] * ldc + col[u];
-    e[u] = __ldg(scales + (row[u] >> row_shift) * lds + (col[u] >> 7));
-    if (cols - col[u] >= 16) {
-      in[u] = __ldg(reinterpret_cast<const uint4*>(p));
-    } else {
-      uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-      for (int k = 0; k < 16; ++k)
-        if (k < cols - col[u]) w[k >> 2] |= uint32_t(p[k]) << (8 * (k & 3));
-      in[u] = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    for (int k = 0; k < 16; ++k)
+      if (k < left) w[k >> 2] |= uint32_t(p[k]) << (8 * (k & 3));
   }
+  float v[16];
 #pragma unroll
-  for (int u = 0; u < UNROLL; ++u) {
-    if (row[u] >= rows) break;
-    const float scale = scale_of(e[u]);
-    const int left = cols - col[u];
-    T* out = y + row[u] * ldy + col[u];
-    const uint32_t w[4] = {in[u].x, in[u].y, in[u].z, in[u].w};
-    float v[16];
+  for (int k = 0; k < 8; ++k) {
+    const float2 f = values2(w[k >> 1] >> (16 * (k & 1)));
+    v[2 * k] = f.x * scale;
+    v[2 * k + 1] = f.y * scale;
+  }
+  T* out = y + row * ldy + col;
+  if (left < 16) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float2 f = values2(w[k >> 1] >> (16 * (k & 1)));
-      v[2 * k] = f.x * scale;
-      v[2 * k + 1] = f.y * scale;
-    }
-    if (left < 16) {
-#pragma unroll
-      for (int k = 0; k < 16; ++k)
-        if (k < left) out[k] = T(v[k]);
-    } else if constexpr (sizeof(T) == 2) {
-      uint32_t o[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-        o[k] = *reinterpret_cast<const uint32_t*>(&b);
-      }
-      reinterpret_cast<uint4*>(out)[0] = make_uint4(o[0], o[1], o[2], o[3]);
-      reinterpret_cast<uint4*>(out)[1] = make_uint4(o[4], o[5], o[6], o[7]);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) reinterpret_cast<float4*>(out)[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
-    }
+    for (int k = 0; k < 16; ++k)
+      if (k < left) out[k] = T(v[k]);
+  } else {
+    store_values(out, v);
+    store_values(out + 8, v + 8);
   }
 }
 
 // Rows of y that begin anywhere: a thread takes the eight elements between two 16-byte borders of y (the first of a row those before the first
-// border) and moves their codes, which begin anywhere, out of two or three aligned words.  They may lie in two blocks.
-template <typename T, int UNROLL>
+// border) and moves their codes, which begin anywhere, out of three aligned words.  They may lie in two blocks.
+template <typename T>
 __global__ void __launch_bounds__(kThreads) dequantize_any_kernel(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int32_t row_shift,
                                                                   T* y, int64_t ldy, int64_t rows, int32_t cols, uint32_t per_row) {
-  const int64_t first = int64_t(blockIdx.x) * (kThreads * UNROLL) + threadIdx.x;
-  const uint8_t* const last = codes + (rows - 1) * ldc + cols;
   constexpr int kBorder = 16 / int(sizeof(T));
-  uint32_t w[UNROLL][2];
-  uint8_t e[UNROLL][2];
-  int64_t row[UNROLL];
-  int col[UNROLL], count[UNROLL];
-  bool whole[UNROLL];
+  const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+  const int64_t row = i <= UINT32_MAX ? int64_t(uint32_t(i) / per_row) : i / per_row;
+  if (row >= rows) return;
+  const int g = int(i - row * per_row);
+  const int head = (kBorder - (int(reinterpret_cast<uintptr_t>(y + row * ldy) / sizeof(T)) & (kBorder - 1))) & (kBorder - 1);
+  const int col = g == 0 ? 0 : head + (g - 1) * 8, count = g == 0 ? min(head, cols) : min(8, cols - col);
+  if (count <= 0) return;
+  const bool whole = g > 0 && count == 8;
+  const uint8_t* s = scales + (row >> row_shift) * lds;
+  const uint32_t first = __ldg(s + (col >> 7)), second = __ldg(s + ((col + count - 1) >> 7));
+  const uint8_t* p = codes + row * ldc + col;
+  const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 3u;
+  const uint8_t* base = p - off;
+  uint32_t w[2] = {0, 0};
+  if (whole && base >= codes && base + 12 <= codes + (rows - 1) * ldc + cols) {
+    const uint32_t* q = reinterpret_cast<const uint32_t*>(base);
+    const uint32_t a = __ldg(q), b = __ldg(q + 1), c = __ldg(q + 2);
+    w[0] = __funnelshift_r(a, b, 8 * off);
+    w[1] = __funnelshift_r(b, c, 8 * off);
+  } else {
 #pragma unroll
-  for (int u = 0; u < UNROLL; ++u) {
-    const int64_t i = first + u * kThreads;
-    row[u] = i <= UINT32_MAX ? int64_t(uint32_t(i) / per_row) : i / per_row;
-    count[u] = 0;
-    if (row[u] >= rows) continue;
-    const int g = int(i - row[u] * per_row);
-    const int before = int(reinterpret_cast<uintptr_t>(y + row[u] * ldy) / sizeof(T)) & (kBorder - 1), head = (kBorder - before) & (kBorder - 1);
-    col[u] = g == 0 ? 0 : head + (g - 1) * 8;
-    count[u] = g == 0 ? min(head, cols) : min(8, cols - col[u]);
-    whole[u] = g > 0 && count[u] == 8;
-    if (count[u] <= 0) continue;
-    const uint8_t* s = scales + (row[u] >> row_shift) * lds;
-    e[u][0] = __ldg(s + (col[u] >> 7));
-    e[u][1] = __ldg(s + ((col[u] + count[u] - 1) >> 7));
-    const uint8_t* p = codes + row[u] * ldc + col[u];
-    const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 3u;
-    const uint8_t* base = p - off;
-    if (whole[u] && base >= codes && base + 12 <= last) {
-      const uint32_t* q = reinterpret_cast<const uint32_t*>(base);
-      const uint32_t a = __ldg(q), b = __ldg(q + 1), c = __ldg(q + 2);
-      w[u][0] = __funnelshift_r(a, b, 8 * off);
-      w[u][1] = __funnelshift_r(b, c, 8 * off);
-    } else {
-      w[u][0] = w[u][1] = 0;
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (k < count[u]) w[u][k >> 2] |= uint32_t(p[k]) << (8 * (k & 3));
-    }
+    for (int k = 0; k < 8; ++k)
+      if (k < count) w[k >> 2] |= uint32_t(p[k]) << (8 * (k & 3));
   }
+  const float lo = scale_of(first), hi = scale_of(second);
+  const int border = ((col >> 7) + 1) * kBlock - col;       // elements from here on lie in the second block
+  float v[8];
 #pragma unroll
-  for (int u = 0; u < UNROLL; ++u) {
-    if (count[u] <= 0) continue;
-    const float lo = scale_of(e[u][0]), hi = scale_of(e[u][1]);
-    const int border = ((col[u] >> 7) + 1) * kBlock - col[u];       // elements from here on lie in the second block
-    float v[8];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float2 f = values2(w[u][k >> 1] >> (16 * (k & 1)));
-      v[2 * k] = f.x * (2 * k < border ? lo : hi);
-      v[2 * k + 1] = f.y * (2 * k + 1 < border ? lo : hi);
-    }
-    T* out = y + row[u] * ldy + col[u];
-    if (whole[u]) {
-      if constexpr (sizeof(T) == 2) {
-        uint32_t o[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-          o[k] = *reinterpret_cast<const uint32_t*>(&b);
-        }
-        *reinterpret_cast<uint4*>(out) = make_uint4(o[0], o[1], o[2], o[3]);
-      } else {
-        reinterpret_cast<float4*>(out)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(out)[1] = make_float4(v[4], v[5], v[6], v[7]);
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (k < count[u]) out[k] = T(v[k]);
-    }
+  for (int k = 0; k < 4; ++k) {
+    const float2 f = values2(w[k >> 1] >> (16 * (k & 1)));
+    v[2 * k] = f.x * (2 * k < border ? lo : hi);
+    v[2 * k + 1] = f.y * (2 * k + 1 < border ? lo : hi);
   }
+  T* out = y + row * ldy + col;
+  if (whole) return store_values(out, v);
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (k < count) out[k] = T(v[k]);
 }
 
 bool wide(const void* p, int64_t ld_bytes, int align) { return reinterpret_cast<uintptr_t>(p) % align == 0 && ld_bytes % align == 0; }
@@ -375,14 +319,14 @@ int quantize(int64_t rows, int64_t cols, const T* x, int64_t ldx, const Operand&
   const bool w = wide(x, ldx * int64_t(sizeof(T)), 16) && wide(codes, out.ld, 16);
   const int64_t per_row = (cols + kBlock - 1) / kBlock;
   if (out.block_rows == 1) {
-    constexpr int kUnroll = sizeof(T) == 2 ? 2 : 1, kAnyUnroll = 4;
+    constexpr int kAnyUnroll = 4;
     // bf16 that begins anywhere, into codes that begin at 16 bytes, as the torch front end's do
     const bool words = sizeof(T) == 2 && !w && wide(codes, out.ld, 16);
-    const int64_t per_block = w || words ? int64_t(kThreads / 8) * kUnroll : int64_t(kThreads / 32) * kAnyUnroll, blocks = (rows * per_row + per_block - 1) / per_block;
+    const int64_t per_block = w || words ? kThreads / 8 : kThreads / 32 * kAnyUnroll, blocks = (rows * per_row + per_block - 1) / per_block;
     if (blocks > INT32_MAX) return MUON_ERR_UNSUPPORTED;
-    auto* k = w ? quantize_rows_kernel<T, kUnroll, false> : quantize_rows_any_kernel<T, kAnyUnroll>;
+    auto* k = w ? quantize_rows_kernel<T, false> : quantize_rows_any_kernel<T, kAnyUnroll>;
     if constexpr (sizeof(T) == 2)
-      if (words) k = quantize_rows_kernel<T, kUnroll, true>;
+      if (words) k = quantize_rows_kernel<T, true>;
     k<<<unsigned(blocks), kThreads, 0, st>>>(x, ldx, codes, out.ld, scales, out.lds, rows, int32_t(cols), uint32_t(per_row));
   } else {
     const int64_t blocks = (rows + kBlock - 1) / kBlock * per_row;
@@ -396,12 +340,11 @@ int quantize(int64_t rows, int64_t cols, const T* x, int64_t ldx, const Operand&
 template <typename T>
 int dequantize(int64_t rows, int64_t cols, const Operand& in, T* y, int64_t ldy, cudaStream_t st) {
   const uint8_t* codes = static_cast<const uint8_t*>(in.data);
-  constexpr int kUnroll = 2;
   const bool w = wide(codes, in.ld, 16) && wide(y, ldy * int64_t(sizeof(T)), 16);
   const int64_t per_row = w ? (cols + 15) / 16 : (cols + 7) / 8 + 1;
-  const int64_t per_block = kThreads * kUnroll, blocks = (rows * per_row + per_block - 1) / per_block;
+  const int64_t blocks = (rows * per_row + kThreads - 1) / kThreads;
   if (blocks > INT32_MAX) return MUON_ERR_UNSUPPORTED;
-  auto* k = w ? dequantize_kernel<T, kUnroll> : dequantize_any_kernel<T, kUnroll>;
+  auto* k = w ? dequantize_kernel<T> : dequantize_any_kernel<T>;
   k<<<unsigned(blocks), kThreads, 0, st>>>(codes, in.ld, in.scales, in.lds, in.block_rows == 1 ? 0 : 7, y, ldy, rows, int32_t(cols), uint32_t(per_row));
   return done(1);
 }
