@@ -1,9 +1,9 @@
 // Matrix products on CUDA cores: fp32, and every layout that TMA cannot address.
 //
-// A block of 256 threads forms a TILE x TILE tile of C, R x R of it per thread (R = TILE / 16), from 16 or 32 values of k at a time, staged in shared
-// memory as fp32 and loaded one step ahead.  A thread's rows and columns are two runs, one in each half of the tile, so that its operands are
-// two wide loads without bank conflicts, and so that in a gated product (columns [0, TILE/2) of the tile are those of B_0, the others
-// the same columns of B_1) it holds g and u of the same elements.  Sums are fp32, by two-wide multiply-adds.
+// A block forms a TILE x TILE tile of C, 8 x 8 (TILE = 128, 256 threads) or 8 x 4 (64, 128 threads) of it per thread, from 8 or 32 values of k at a
+// time, staged in shared memory as fp32 and loaded one step ahead.  A thread's rows and columns are two runs, one in each half of the tile, so
+// that its operands are wide loads without bank conflicts, and so that in a gated product (columns [0, TILE/2) of the tile are those of B_0,
+// the others the same columns of B_1) it holds g and u of the same elements.  Sums are fp32, by multiply-adds of two rows at a time.
 //
 // Where 128 x 128 tiles would leave multiprocessors idle, the tiles are 64 x 64 and the blocks of a cluster each take a part of k; the parts are added
 // in the order of the ranks, so the sum is the same in every run.
@@ -19,10 +19,15 @@ namespace muon {
 namespace {
 
 namespace cg = cooperative_groups;
-constexpr int kThreads = 256, kMaxSplit = 8;
-// Values of k in a step.  The small tiles are latency-bound: twice as many in flight (32 instead of 16) halve the number of waits.
-template <int TILE> constexpr int kStep = TILE == 64 ? 32 : 16;
-template <int TILE> constexpr int kPitch = TILE == 64 ? 66 : 132;      // of a staged row: neighbouring k in other banks, rows aligned for the wide loads
+constexpr int kMaxSplit = 8;
+template <int TILE>
+struct Tile {
+  static constexpr int columns = TILE / 16, threads = TILE * TILE / (8 * columns);     // of C per thread: 8 rows of `columns`
+  static constexpr int step = TILE == 64 ? 32 : 8;       // values of k; the small tiles wait more for memory, so that more is in flight there
+  static constexpr int blocks = TILE == 64 ? 4 : 2;      // on a multiprocessor: what one waits for, the others cover
+  static constexpr int pitch = TILE + 4;                 // of a staged row: eight neighbouring k of four rows lie in 32 banks
+  static constexpr int loads = TILE * step / threads;    // elements of an operand that a thread loads in a step
+};
 
 struct SimtArgs {
   Product p[kMaxProducts];
@@ -47,53 +52,61 @@ __device__ __forceinline__ float element_of(const Operand& o, int64_t row, int64
   return value_at<kTypeE4m3>(p + at) * scale_of(__ldg(o.scales + row / o.block_rows * o.lds + (col >> 7)));
 }
 
-// What a thread loads of an operand in every step.  Threads run along the memory's rows.
+// What a thread loads of an operand in every step: along the memory's rows, eight values of k (a sector of fp32) or all rows of the tile.
 template <int TILE, int TYPE>
 struct Loader {
-  static constexpr int kStepK = kStep<TILE>, kLoads = TILE * kStepK / kThreads, kRowsApart = kThreads / kStepK;
-  const Operand *lo, *hi;       // hi: of the second half of the tile, which is another matrix or the same
+  using T = Tile<TILE>;
+  static constexpr int kGroups = T::step / 8, kRowsApart = T::threads / 8, kApart = T::threads / TILE;
+  // of the two halves of the tile, which are of one matrix or of two; in registers, for the launch's arguments are far away
+  const char *lo, *hi;
+  int64_t ld_lo, ld_hi;
+  const Operand* blocks;        // 8 bits: the scales (one matrix)
   bool mn;
   int row_lo, row_hi, rows;     // of the operand: the first element's in each half of the tile
   int k;                        // of the first element, from the step's beginning on
   __device__ __forceinline__ void init(const Operand& first_half, const Operand& second_half, bool halves, int first, int rows_) {
-    lo = &first_half;
-    hi = halves ? &second_half : &first_half;
-    mn = lo->mn_major != 0;
+    const Operand& second = halves ? second_half : first_half;
+    lo = static_cast<const char*>(first_half.data);
+    hi = static_cast<const char*>(second.data);
+    ld_lo = first_half.ld;
+    ld_hi = second.ld;
+    blocks = &first_half;
+    mn = first_half.mn_major != 0;
     rows = rows_;
-    k = mn ? int(threadIdx.x) / TILE : int(threadIdx.x) % kStepK;
-    row_lo = first + (mn ? int(threadIdx.x) % TILE : int(threadIdx.x) / kStepK);
+    k = mn ? int(threadIdx.x) / TILE : int(threadIdx.x) % 8;
+    row_lo = first + (mn ? int(threadIdx.x) % TILE : int(threadIdx.x) / 8);
     row_hi = halves ? row_lo : row_lo + TILE / 2;
   }
-  __device__ __forceinline__ void load(int k0, int kdim, float (&v)[kLoads]) const {
-    if (mn) {                   // slot i is kThreads / TILE values of k further
+  __device__ __forceinline__ void load(int k0, int kdim, float (&v)[T::loads]) const {
+    if (mn) {
       const bool in = row_lo < rows;
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int kk = k0 + k + i * (kThreads / TILE);
+      for (int i = 0; i < T::loads; ++i) {
+        const int kk = k0 + k + i * kApart;
         v[i] = 0.f;
-        if (in && kk < kdim) v[i] = one(*lo, kk, row_lo);
+        if (in && kk < kdim) v[i] = one(lo, ld_lo, kk, row_lo);
       }
-    } else {                    // slot i is kRowsApart rows further
-      const bool in = k0 + k < kdim;
+    } else {
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int r = (i < kLoads / 2 ? row_lo : row_hi) + (i % (kLoads / 2)) * kRowsApart;
+      for (int i = 0; i < T::loads; ++i) {
+        const int group = i / kGroups, kk = k0 + k + 8 * (i % kGroups);
+        const bool first = group * kRowsApart < TILE / 2;
+        const int r = first ? row_lo + group * kRowsApart : row_hi + group * kRowsApart - TILE / 2;
         v[i] = 0.f;
-        if (in && r < rows) v[i] = one(i < kLoads / 2 ? *lo : *hi, r, k0 + k);
+        if (r < rows && kk < kdim) v[i] = one(first ? lo : hi, first ? ld_lo : ld_hi, r, kk);
       }
     }
   }
-  static __device__ __forceinline__ float one(const Operand& m, int64_t r, int c) {
-    const float x = value_at<TYPE>(static_cast<const char*>(m.data) + (r * m.ld + c) * kSizeOf<TYPE>);
-    if constexpr (TYPE == kTypeE4m3) return x * scale_of(__ldg(m.scales + (m.block_rows == 1 ? r : r >> 7) * m.lds + (c >> 7)));
+  __device__ __forceinline__ float one(const char* base, int64_t ld, int64_t r, int c) const {
+    const float x = value_at<TYPE>(base + (r * ld + c) * kSizeOf<TYPE>);
+    if constexpr (TYPE == kTypeE4m3) return x * scale_of(__ldg(blocks->scales + (blocks->block_rows == 1 ? r : r >> 7) * blocks->lds + (c >> 7)));
     return x;
   }
-  __device__ __forceinline__ void stage(float (*s)[kPitch<TILE>], const float (&v)[kLoads]) const {
+  __device__ __forceinline__ void stage(float (*s)[T::pitch], const float (&v)[T::loads]) const {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int idx = int(threadIdx.x) + i * kThreads;
-      if (mn) s[idx / TILE][idx % TILE] = v[i];
-      else s[idx % kStepK][idx / kStepK] = v[i];
+    for (int i = 0; i < T::loads; ++i) {
+      if (mn) s[int(threadIdx.x) / TILE + i * kApart][int(threadIdx.x) % TILE] = v[i];
+      else s[int(threadIdx.x) % 8 + 8 * (i % kGroups)][int(threadIdx.x) / 8 + i / kGroups * kRowsApart] = v[i];
     }
   }
 };
@@ -139,9 +152,10 @@ __device__ __forceinline__ void finish(const Product& p, const Activation& f, in
 }
 
 template <int TILE, int TYPE>
-__global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant__ SimtArgs L) {
-  constexpr int R = TILE / 16, H = R / 2, kStepK = kStep<TILE>;
-  __shared__ __align__(16) float stages[4][kStepK][kPitch<TILE>];      // two places for A, two for B
+__global__ void __launch_bounds__(Tile<TILE>::threads, Tile<TILE>::blocks) product_kernel(const __grid_constant__ SimtArgs L) {
+  using T = Tile<TILE>;
+  constexpr int N = T::columns, H = N / 2;                        // columns of a thread, and those in each half of the tile
+  __shared__ __align__(16) float stages[4][T::step][T::pitch];    // two places for A, two for B
   const int block = int(blockIdx.x) / L.split, rank = int(blockIdx.x) % L.split;
   int which = 0;
   for (int i = 1; i < L.count; ++i)
@@ -151,11 +165,11 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
   const int tiles_m = (p.m + TILE - 1) / TILE, tile = block - L.tile_begin[which];
   const int m0 = tile % tiles_m * TILE, n0 = tile / tiles_m * (gated ? TILE / 2 : TILE);
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  uint64_t acc[R][H] = {};
-  const int steps = (p.k + kStepK - 1) / kStepK, total = steps * p.segments;
+  uint64_t acc[4][N] = {};                                        // two rows each: 0, 1 and 2, 3 of the run in either half
+  const int steps = (p.k + T::step - 1) / T::step, total = steps * p.segments;
   const int begin = int(int64_t(total) * rank / L.split), end = int(int64_t(total) * (rank + 1) / L.split);
   Loader<TILE, TYPE> la, lb;
-  float va[decltype(la)::kLoads], vb[decltype(lb)::kLoads];
+  float va[T::loads], vb[T::loads];
   int segment = -1;
   auto load = [&](int t) {
     const int s = t >= steps ? 1 : 0;
@@ -164,8 +178,8 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
       lb.init(p.b[s], p.b[1], gated, n0, p.n);
       segment = s;
     }
-    la.load((t - s * steps) * kStepK, p.k, va);
-    lb.load((t - s * steps) * kStepK, p.k, vb);
+    la.load((t - s * steps) * T::step, p.k, va);
+    lb.load((t - s * steps) * T::step, p.k, vb);
   };
   auto keep = [&](int t) {
     la.stage(stages[t & 1], va);
@@ -178,55 +192,60 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
   __syncthreads();
   for (int t = begin; t < end; ++t) {
     if (t + 1 < end) load(t + 1);
-#pragma unroll
-    for (int k = 0; k < kStepK; ++k) {
-      float a[R];
-      uint64_t b[H];
+    // the operands of a value of k are read while the one before is multiplied
+    uint64_t a[2][4];
+    float b[2][N];
+    auto fetch = [&](int k, int to) {
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        const float* pa = &stages[t & 1][k][half * (TILE / 2) + ty * H];
+        const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(&stages[t & 1][k][half * (TILE / 2) + ty * 4]);
+        a[to][half * 2] = x.x;
+        a[to][half * 2 + 1] = x.y;
         const float* pb = &stages[2 + (t & 1)][k][half * (TILE / 2) + tx * H];
         if constexpr (H == 4) {
-          const float4 x = *reinterpret_cast<const float4*>(pa);
-          a[half * 4] = x.x; a[half * 4 + 1] = x.y; a[half * 4 + 2] = x.z; a[half * 4 + 3] = x.w;
-          const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(pb);
-          b[half * 2] = y.x;
-          b[half * 2 + 1] = y.y;
+          const float4 y = *reinterpret_cast<const float4*>(pb);
+          b[to][half * 4] = y.x; b[to][half * 4 + 1] = y.y; b[to][half * 4 + 2] = y.z; b[to][half * 4 + 3] = y.w;
         } else {
-          const float2 x = *reinterpret_cast<const float2*>(pa);
-          a[half * 2] = x.x;
-          a[half * 2 + 1] = x.y;
-          b[half] = *reinterpret_cast<const uint64_t*>(pb);
+          const float2 y = *reinterpret_cast<const float2*>(pb);
+          b[to][half * 2] = y.x;
+          b[to][half * 2 + 1] = y.y;
         }
       }
+    };
+    fetch(0, 0);
+#pragma unroll 8
+    for (int k = 0; k < T::step; ++k) {
+      if (k + 1 < T::step) fetch(k + 1, (k + 1) & 1);
 #pragma unroll
-      for (int i = 0; i < R; ++i)
+      for (int j = 0; j < N; ++j) {
+        const uint64_t bb = twice(b[k & 1][j]);
 #pragma unroll
-        for (int j = 0; j < H; ++j) acc[i][j] = fma2(twice(a[i]), b[j], acc[i][j]);
+        for (int i = 0; i < 4; ++i) acc[i][j] = fma2(a[k & 1][i], bb, acc[i][j]);
+      }
     }
     if (t + 1 < end) keep(t + 1);       // the other place, which every thread left before the last meeting
     __syncthreads();
   }
   const Activation f = activation_of(p.e.activation);
-  auto row_of = [&](int i) { return (i / H) * (TILE / 2) + ty * H + i % H; };
+  auto row_of = [&](int i) { return (i / 2) * (TILE / 2) + ty * 4 + (i % 2) * 2; };      // the first of a pair's rows
   if constexpr (TILE == 64) {
     if (L.split > 1) {
       constexpr int kRow = TILE + 1;
-      static_assert(TILE * kRow <= 4 * kStepK * kPitch<TILE>, "the sums take the place of the operands");
+      static_assert(TILE * kRow <= 4 * T::step * T::pitch, "the sums take the place of the operands");
       float* sums = &stages[0][0][0];
 #pragma unroll
-      for (int i = 0; i < R; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < H; ++j) {
+        for (int j = 0; j < N; ++j) {
           const float2 pair = both(acc[i][j]);
-          float* to = sums + row_of(i) * kRow + (2 * j / H) * (TILE / 2) + tx * H + (2 * j) % H;
+          float* to = sums + row_of(i) * kRow + (j / H) * (TILE / 2) + tx * H + j % H;
           to[0] = pair.x;
-          to[1] = pair.y;
+          to[kRow] = pair.y;
         }
       cg::cluster_group cl = cg::this_cluster();
       cl.sync();
 #pragma unroll 2
-      for (int i = rank * kThreads + int(threadIdx.x); i < TILE * TILE / 2; i += L.split * kThreads) {
+      for (int i = rank * T::threads + int(threadIdx.x); i < TILE * TILE / 2; i += L.split * T::threads) {
         const int r = i / (TILE / 2), c = i % (TILE / 2);
         float first[kMaxSplit], second[kMaxSplit];
 #pragma unroll
@@ -250,24 +269,20 @@ __global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant
     }
   }
 #pragma unroll
-  for (int i = 0; i < R; ++i) {
-    float v[R];
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < H; ++j) {
-      const float2 pair = both(acc[i][j]);
-      v[2 * j] = pair.x;
-      v[2 * j + 1] = pair.y;
+      const float2 first = both(acc[i][j]), second = both(acc[i][H + j]);
+      finish<TILE>(p, f, m0 + row_of(i), n0, tx * H + j, first.x, second.x);
+      finish<TILE>(p, f, m0 + row_of(i) + 1, n0, tx * H + j, first.y, second.y);
     }
-#pragma unroll
-    for (int j = 0; j < H; ++j) finish<TILE>(p, f, m0 + row_of(i), n0, tx * H + j, v[j], v[H + j]);
-  }
 }
 
 template <int TILE, int TYPE>
 int launch(const SimtArgs& L, int64_t tiles, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(tiles * L.split), 1, 1);
-  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.blockDim = dim3(Tile<TILE>::threads, 1, 1);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -295,7 +310,7 @@ int launch_products_simt(const Product* list, int count, int siblings, int sms, 
       tiles[s] += n;
       most[s] = std::max(most[s], n);
     }
-    steps = std::min<int64_t>(steps, (int64_t(p.k) + kStep<64> - 1) / kStep<64> * p.segments);
+    steps = std::min<int64_t>(steps, (int64_t(p.k) + Tile<64>::step - 1) / Tile<64>::step * p.segments);
     ++L.count;
   }
   if (L.count == 0) return 0;
