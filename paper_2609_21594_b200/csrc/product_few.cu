@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(kThreads, 2) product_few_kernel(const __grid_c
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  // The next part of the call may begin.  Only now: its blocks take tensor memory, too, and wait for this launch's end before they give it back.
+  // the next part of the call may begin
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t scale_col = tmem_base + uint32_t(kTiles * L.tokens);
 
@@ -494,7 +494,7 @@ int launch_product_few(muon_ctx* ctx, const Product& q, int sms, bool follows, c
     L.sx = scales_of(q.a[0], q.m);
   }
   const int dev = ctx->device;
-  const uint32_t bytes = L.bar_off + 256 + 1024;
+  const uint32_t bytes = std::max(L.bar_off + 256 + 1024, shared_for_columns(uint32_t(L.columns)));
   if (eight) return wmn ? launch<true, true, kPlain>(L, dev, bytes, follows, st) : launch<false, true, kPlain>(L, dev, bytes, follows, st);
   if (e.kind == kGated) return codes ? launch<false, false, kGated, true>(L, dev, bytes, follows, st) : launch<false, false, kGated>(L, dev, bytes, follows, st);
   if (e.kind == kGrad) return codes ? launch<true, false, kGrad, true>(L, dev, bytes, follows, st) : launch<true, false, kGrad>(L, dev, bytes, follows, st);

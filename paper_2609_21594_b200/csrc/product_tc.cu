@@ -26,7 +26,6 @@ namespace {
 using namespace prod;
 
 constexpr int kRows = 128;                     // of A per CTA
-constexpr int kStages = 6;
 constexpr uint32_t kHalfBytes = kRows * 128;   // 16 KiB: 128 rows of 128 bytes
 constexpr uint32_t kStageBytes = 2 * kHalfBytes;
 constexpr int kEpiWarps = 8;
@@ -39,12 +38,13 @@ constexpr uint32_t kSecondAccumulator8 = 240;
 
 template <bool EIGHT>
 struct Shape {
-  static constexpr uint32_t scale_off = kStages * kStageBytes;
+  static constexpr int stages = EIGHT ? 6 : 7;
+  static constexpr uint32_t scale_off = stages * kStageBytes;
   static constexpr uint32_t bar_off = scale_off + (EIGHT ? kScaleRing * kScaleBytes : 0);
-  static constexpr uint32_t bytes = bar_off + 512 + 1024;
+  static constexpr uint32_t bytes = shared_for_columns(512);      // all there is: see there
+  static_assert(bar_off + 512 + 1024 <= bytes, "227 KiB of shared memory");
   static constexpr int threads = 32 * (2 + kEpiWarps + (EIGHT ? 1 : 0));
 };
-static_assert(Shape<false>::bytes <= 232448 && Shape<true>::bytes <= 232448, "227 KiB of shared memory");
 
 struct TcProduct {
   CUtensorMap a[2], b[2];
@@ -127,13 +127,12 @@ __device__ __forceinline__ Tile decode(const TcProducts& L, int t) {
   return r;
 }
 
+template <int STAGES>
 struct Ring {
-  uint32_t base, bars;
-  volatile int* abort_flag;
   uint32_t it, s, ph;                          // k-blocks so far, place in the ring and its phase
   __device__ __forceinline__ void advance() {
     ++it;
-    if (++s == uint32_t(kStages)) {
+    if (++s == uint32_t(STAGES)) {
       s = 0;
       ph ^= 1u;
     }
@@ -230,8 +229,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<EIGHT>::thread
   volatile int* abort_flag = reinterpret_cast<volatile int*>(gen_base + S::bar_off + 488);
   auto bar = [&](int i) { return bars + uint32_t(i) * 8u; };
   auto full_bar = [&](uint32_t s) { return bar(int(s)); };
+  constexpr int kStages = S::stages, kT = 2 * kStages;
   auto empty_bar = [&](uint32_t s) { return bar(kStages + int(s)); };
-  constexpr int kT = 2 * kStages;
   auto tfull_bar = [&](uint32_t i) { return bar(kT + int(i)); };
   auto tempty_bar = [&](uint32_t i) { return bar(kT + 2 + int(i)); };
   const uint32_t drain_bar = bar(kT + 4), shared_bar = bar(kT + 5);     // shared_bar: the columns that both accumulators use have been read
@@ -283,7 +282,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<EIGHT>::thread
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer (one per CTA)
     if (lane == 0) {
-      Ring c{base, bars, abort_flag, 0u, 0u, 0u};
+      Ring<kStages> c{0u, 0u, 0u};
       const uint32_t full0 = map_to_cta(full_bar(0), 0);
       const uint32_t stage_tx = 2 * (kHalfBytes + kHalfBytes / 128 * uint32_t(L.half));
       bool ok = true;
@@ -330,7 +329,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<EIGHT>::thread
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer (leader CTA only), converged: see elect_one
     if (leader_cta) {
-      Ring c{base, bars, abort_flag, 0u, 0u, 0u};
+      Ring<kStages> c{0u, 0u, 0u};
       uint32_t tile_it = 0, group = 0;
       bool ok = true;
       constexpr uint64_t a_hi = A_MN ? kDescMN : kDescK, b_hi = B_MN ? kDescMN : kDescK;

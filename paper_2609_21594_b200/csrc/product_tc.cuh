@@ -21,6 +21,14 @@ struct Scales {                                // of an operand in 8 bits: the b
 };
 constexpr int kScaleBlocks = 16;               // k-blocks whose scales are gathered at a time: a round of gathering takes as long as the products of six
 
+// Tensor memory is handed out to blocks as they ask for it, and a block that waits for some while its cluster waits for it could wait for good: its peers may
+// hold what a block of another cluster, which holds what this one wants, is waiting for.  So every kernel of clusters that takes tensor memory also
+// takes the same share of shared memory, of which a block is given all before it starts: then there is always enough of the former.
+constexpr uint32_t kSmShared = 228 * 1024, kBlockReserved = 1024, kSmColumns = 512, kMostShared = 227 * 1024;
+__host__ __device__ constexpr uint32_t shared_for_columns(uint32_t columns) {
+  return columns * (kSmShared / kSmColumns) > kMostShared ? kMostShared : columns * (kSmShared / kSmColumns) - kBlockReserved;
+}
+
 // ------------------------------------------------------------------ PTX
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;

@@ -217,3 +217,25 @@ def test_refusals():
                  lambda: F.feed_forward_backward(dy[:2], None, wg, wu, wd, kept8)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("tokens,dim,hidden", [(40, 256, 384), (300, 256, 384), (40, 100, 130)])
+def test_what_is_kept_in_8_bits_of_values_that_are_not_finite(tokens, dim, hidden):
+    """Every engine: a NaN or an infinity in gate or up is kept as NaN and has no share in its block's scale."""
+    from paper_2609_21594_b200 import functional as F
+
+    x, wg, wu, wd, _ = make(tokens, dim, hidden, torch.bfloat16)
+    _, clean = F.feed_forward_forward(x, wg, wu, wd, "silu", "8bit")
+    wg[5] = float("inf")                                     # column 5 of gate: infinities of both signs, or NaN
+    wu[7] = float("nan")
+    _, kept = F.feed_forward_forward(x, wg, wu, wd, "silu", "8bit")
+    for i, bad in ((2, 5), (4, 7)):
+        rest = torch.ones(hidden, dtype=torch.bool, device="cuda")
+        rest[bad] = False
+        assert torch.isnan(kept[i].float()[:, bad]).all() and torch.isfinite(kept[i].float()[:, rest]).all()
+        # the scale is that of the other columns: theirs are the codes of the clean product wherever column `bad` was not the largest
+        e = ref.scale_bytes(ref.unpack(clean[i].float(), clean[i + 1], 1).masked_fill(~rest, 0.0), 1)
+        same = e == clean[i + 1].long()
+        spread = ref.spread(same, kept[i].shape, 1) & rest
+        assert torch.equal(kept[i + 1][same], clean[i + 1][same]) and torch.equal(kept[i].float()[spread], clean[i].float()[spread])
+        assert same.float().mean() > 0.9
