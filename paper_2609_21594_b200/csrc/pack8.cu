@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_any_kernel(const T* x,
 // Blocks of 128 x 128: a thread block each, 32 elements a thread kept in registers between the maximum and the rounding.  WIDE: sixteen lanes to a
 // row, eight elements each; else a warp to a row, elements 32 apart.
 template <typename T, bool WIDE>
-__global__ void __launch_bounds__(kSquareThreads) quantize_squares_kernel(const T* x, int64_t ldx, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds,
+__global__ void __launch_bounds__(kSquareThreads, 3) quantize_squares_kernel(const T* x, int64_t ldx, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds,
                                                                     int64_t rows, int32_t cols) {
   __shared__ uint32_t tops[kSquareThreads / 32];
   constexpr int kPer = WIDE ? 8 : 4, kTimes = kBlock * kBlock / kSquareThreads / kPer, kStride = kBlock / kTimes;      // elements of a row, rows of a thread and between them

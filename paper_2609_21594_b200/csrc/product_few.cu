@@ -445,7 +445,8 @@ FewPlan plan_few(const Product& q, int sms) {
 }  // namespace
 
 bool product_few_takes(const Product& p, int sms) {
-  return p.m <= kFewRows && !p.a[0].mn_major && plan_few(p, sms).clocks < 0.85 * products_tc_clocks(&p, 1, sms);
+  // what grows has to be clearly less, what does not is about 4000 clocks less in any case
+  return p.m <= kFewRows && !p.a[0].mn_major && plan_few(p, sms).clocks < 0.85 * products_tc_clocks(&p, 1, sms) + 1800;
 }
 
 int launch_product_few(muon_ctx* ctx, const Product& q, int sms, bool follows, cudaStream_t st) {
