@@ -548,8 +548,9 @@ int muon_dequantize(muon_ctx_t* ctx, int32_t dtype, int64_t rows, int64_t cols, 
 #define MUON_KEEP_FULL 1
 #define MUON_KEEP_8BIT 2
 typedef struct {
-  int32_t dtype;                 /* of all tensors.  MUON_DTYPE_BF16: tensor cores when every pointer is 16-byte aligned, every ld is a multiple */
-                                 /* of 8 and so are dim and hidden; otherwise, and for MUON_DTYPE_FP32, CUDA cores                             */
+  int32_t dtype;                 /* of all tensors.  MUON_DTYPE_BF16: tensor cores when every pointer is 16-byte aligned and every ld a multiple */
+                                 /* of 8; where dim or hidden is not and the products are large, by way of copies in the scratch; otherwise,   */
+                                 /* and for MUON_DTYPE_FP32, CUDA cores                                                                        */
   int32_t activation, keep;
   int32_t tokens, dim, hidden;
 } muon_feed_forward_desc_t;
@@ -581,11 +582,14 @@ typedef struct {
   int32_t tokens, dim, out;
   int32_t reserved;              /* must be 0 */
 } muon_linear_blocks_desc_t;
-int muon_linear_blocks_forward(muon_ctx_t* ctx, const muon_linear_blocks_desc_t* desc, const muon_rows_t* x, const muon_blocks_t* w8, const muon_rows_t* y,
-                             const muon_blocks_t* x8, void* stream);
+/* Bytes of scratch, 256-byte aligned, of the forward (backward = 0) or backward (1) call.  Host arithmetic only. */
+int muon_linear_blocks_workspace_bytes(const muon_linear_blocks_desc_t* desc, int32_t backward, size_t* bytes);
 
-/* dx = Q(dy) w8 with Q(dy) in blocks of 1 x 128, and dw = dy^T x8 with dy as it is (bf16).  dx or dw may be NULL. */
-int muon_linear_blocks_workspace_bytes(const muon_linear_blocks_desc_t* desc, size_t* bytes);
+int muon_linear_blocks_forward(muon_ctx_t* ctx, const muon_linear_blocks_desc_t* desc, const muon_rows_t* x, const muon_blocks_t* w8, const muon_rows_t* y,
+                               const muon_blocks_t* x8, void* workspace, size_t workspace_bytes, void* stream);
+
+/* dx = Q(dy) w8 with Q(dy) in blocks of 1 x 128, and dw = dy^T x8 with dy as it is (bf16).  dx or dw may be NULL.  Rows whose distance is a multiple of
+ * 16 bytes and begin on 16 bytes go to the tensor cores; of dim or out that 16 or 8 does not divide, large products by way of copies in the scratch. */
 int muon_linear_blocks_backward(muon_ctx_t* ctx, const muon_linear_blocks_desc_t* desc, const muon_rows_t* dy, const muon_blocks_t* x8, const muon_blocks_t* w8,
                               const muon_rows_t* dx, const muon_rows_t* dw, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -162,8 +162,8 @@ _sig = {
     "muon_feed_forward_workspace_bytes": (C.c_int, [_vp, C.c_int32, C.POINTER(C.c_size_t)]),
     "muon_feed_forward_forward": (C.c_int, [_vp] * 9 + [C.c_size_t, _vp]),
     "muon_feed_forward_backward": (C.c_int, [_vp] * 13 + [C.c_size_t, _vp]),
-    "muon_linear_blocks_forward": (C.c_int, [_vp] * 7),
-    "muon_linear_blocks_workspace_bytes": (C.c_int, [_vp, C.POINTER(C.c_size_t)]),
+    "muon_linear_blocks_forward": (C.c_int, [_vp] * 7 + [C.c_size_t, _vp]),
+    "muon_linear_blocks_workspace_bytes": (C.c_int, [_vp, C.c_int32, C.POINTER(C.c_size_t)]),
     "muon_linear_blocks_backward": (C.c_int, [_vp] * 8 + [C.c_size_t, _vp]),
     "muon_last_device_status": (C.c_int, [_vp, _vp, C.POINTER(C.c_int32)]),
     "muon_clear_device_status": (C.c_int, [_vp, _vp]),
@@ -346,9 +346,9 @@ def muon_feed_forward_workspace_bytes(desc, backward: bool) -> int:
     return out.value
 
 
-def muon_linear_blocks_workspace_bytes(desc) -> int:
+def muon_linear_blocks_workspace_bytes(desc, backward: bool) -> int:
     out = C.c_size_t(0)
-    _check(lib.muon_linear_blocks_workspace_bytes(_at(desc), C.byref(out)), "muon_linear_blocks_workspace_bytes")
+    _check(lib.muon_linear_blocks_workspace_bytes(_at(desc), 1 if backward else 0, C.byref(out)), "muon_linear_blocks_workspace_bytes")
     return out.value
 
 
@@ -596,8 +596,9 @@ class Context:
         _check(lib.muon_feed_forward_backward(self.handle, *map(_maybe, (desc, dy, x, w_gate, w_up, w_down, kept, dx, dw_gate, dw_up, dw_down)),
                                               workspace, workspace_bytes, _stream(stream)), "muon_feed_forward_backward")
 
-    def muon_linear_blocks_forward(self, desc, x, w8, y, x8, stream=None) -> None:
-        _check(lib.muon_linear_blocks_forward(self.handle, *map(_maybe, (desc, x, w8, y, x8)), _stream(stream)), "muon_linear_blocks_forward")
+    def muon_linear_blocks_forward(self, desc, x, w8, y, x8, workspace, workspace_bytes, stream=None) -> None:
+        _check(lib.muon_linear_blocks_forward(self.handle, *map(_maybe, (desc, x, w8, y, x8)), workspace, workspace_bytes, _stream(stream)),
+               "muon_linear_blocks_forward")
 
     def muon_linear_blocks_backward(self, desc, dy, x8, w8, dx, dw, workspace, workspace_bytes, stream=None) -> None:
         _check(lib.muon_linear_blocks_backward(self.handle, *map(_maybe, (desc, dy, x8, w8, dx, dw)), workspace, workspace_bytes, _stream(stream)),

@@ -9,6 +9,9 @@ namespace {
 
 constexpr int64_t kMaxTokens = (int64_t(1) << 31) - 1 - 512;      // tile coordinates past the last row stay in 32 bits
 constexpr int64_t kUnalignedRows = 512;                           // rows at a time whose fp32 g and u wait for their 8 bits (CUDA cores only)
+// Multiply-adds of a product from which on it is worth copying what TMA cannot address (rows of an odd number of elements) into rows that it can:
+// two launches of a few us against CUDA cores at a hundredth of the tensor cores' rate (2^25 take about 10 us there).
+constexpr int64_t kWorthCopies = int64_t(1) << 25;
 
 int64_t up_to(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 int64_t blocks_of(int64_t n) { return (n + kBlock - 1) / kBlock; }
@@ -72,13 +75,23 @@ struct Launches {
     const int r = launched(ctx, n);
     if (rc == MUON_OK) rc = r;
   }
-  // follows: the call's last launch is right before this one in the stream, and writes nothing but what it takes as A
+  // follows: the call's last launch is right before this one in the stream, and writes nothing but what it takes as A.  Each product's engine is its own
+  // affair: a gradient has the same bits whichever others are wanted.
   void products(const Product* p, int n, int siblings, bool follows = false) {
-    if (rc != MUON_OK || n == 0) return;
-    if (products_tc_take(p, n)) return count(n == 1 && product_few_takes(*p, sms) ? launch_product_few(ctx, *p, sms, follows, st) : launch_products_tc(ctx, p, n, st));
-    count(launch_products_simt(p, n, siblings, sms, st));
+    Product part[2][kMaxProducts];
+    int count[2] = {0, 0};
+    for (int i = 0; i < n; ++i) {
+      const int tc = products_tc_take(p + i, 1) ? 1 : 0;
+      part[tc][count[tc]++] = p[i];
+    }
+    if (rc == MUON_OK && count[1] == 1 && product_few_takes(part[1][0], sms)) this->count(launch_product_few(ctx, part[1][0], sms, follows, st));
+    else if (rc == MUON_OK && count[1] > 0) this->count(launch_products_tc(ctx, part[1], count[1], st));
+    if (rc == MUON_OK && count[0] > 0) this->count(launch_products_simt(part[0], count[0], siblings, sms, st));
   }
   void product(const Product& p, bool follows = false) { products(&p, 1, 1, follows); }
+  void copies(const CopyTask* list, int n) {
+    if (rc == MUON_OK && n > 0) count(launch_copies(list, n, sms, st));
+  }
   void quantize(int dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx, const Operand& out) {
     if (rc == MUON_OK) count(launch_quantize(dtype, rows, cols, x, ldx, out, sms, st));
   }
@@ -101,6 +114,32 @@ int check_scratch(const void* workspace, size_t have, size_t need) {
   if (need == 0) return MUON_OK;
   if (!workspace || have < need) return MUON_ERR_WORKSPACE_TOO_SMALL;
   return aligned_to(workspace, 256) ? MUON_OK : MUON_ERR_INVALID_ARG;
+}
+
+// Operands and results that TMA cannot address and that have room in the scratch are copied there and back.
+struct Copies {
+  CopyTask in[kMaxCopies], out[kMaxCopies];
+  int ins = 0, outs = 0;
+  static int64_t pitch(int64_t cols, int type) { return up_to(cols, 16 / size_of_type(type)); }
+  Operand take(Operand o, int64_t rows, int64_t cols, void* room) {
+    if (!room || addressable(o.data, o.ld, o.type)) return o;
+    const int e = size_of_type(o.type);
+    const int64_t ld = pitch(cols, o.type);
+    in[ins++] = {o.data, room, o.ld * e, ld * e, rows, cols * e, e};
+    o.data = room;
+    o.ld = ld;
+    return o;
+  }
+  muon_rows_t give(const muon_rows_t* to, int64_t rows, int64_t cols, void* room, int type) {
+    if (!room || addressable(to->data, to->ld, type)) return *to;
+    const int e = size_of_type(type);
+    const int64_t ld = pitch(cols, type);
+    out[outs++] = {room, to->data, ld * e, to->ld * e, rows, cols * e, e};
+    return {room, ld};
+  }
+};
+void* room(Scratch* s, bool odd, int64_t rows, int64_t cols, int type) {
+  return odd ? s->take(rows * Copies::pitch(cols, type) * size_of_type(type)) : nullptr;
 }
 
 // ------------------------------------------------------------------ feed-forward block
@@ -138,9 +177,19 @@ struct KeptBoxes {
   }
 };
 
+// Whether rows of dim and of hidden elements get room for copies.
+struct Odd {
+  bool dim, hidden;
+  explicit Odd(const muon_feed_forward_desc_t* d) {
+    const bool worth = d->dtype == kTypeBf16 && int64_t(d->tokens) * d->dim >= (kWorthCopies + d->hidden - 1) / d->hidden;
+    dim = worth && d->dim % 8 != 0;
+    hidden = worth && d->hidden % 8 != 0;
+  }
+};
 struct ForwardScratch {
   int64_t ldh;
   void *h, *gate, *up;           // gate, up: fp32, for kUnalignedRows rows
+  void *x, *w_gate, *w_up, *w_down, *y, *kept_gate, *kept_up;      // copies
 };
 ForwardScratch forward_scratch(const muon_feed_forward_desc_t* d, Scratch* s) {
   ForwardScratch r = {};
@@ -151,11 +200,21 @@ ForwardScratch forward_scratch(const muon_feed_forward_desc_t* d, Scratch* s) {
     r.gate = s->take(rows * d->hidden * 4);
     r.up = s->take(rows * d->hidden * 4);
   }
+  const Odd odd(d);
+  const int64_t t = d->tokens;
+  r.x = room(s, odd.dim, t, d->dim, d->dtype);
+  r.w_gate = room(s, odd.dim, d->hidden, d->dim, d->dtype);
+  r.w_up = room(s, odd.dim, d->hidden, d->dim, d->dtype);
+  r.y = room(s, odd.dim, t, d->dim, d->dtype);
+  r.w_down = room(s, odd.hidden, d->dim, d->hidden, d->dtype);
+  r.kept_gate = room(s, odd.hidden && d->keep == MUON_KEEP_FULL, t, d->hidden, d->dtype);
+  r.kept_up = room(s, odd.hidden && d->keep == MUON_KEEP_FULL, t, d->hidden, d->dtype);
   return r;
 }
 struct BackwardScratch {
   int64_t ldh, ldx;
   void *dgate, *dup, *h, *x;
+  void *dy, *given_x, *w_gate, *w_up, *w_down, *gate, *up, *dx, *dw_gate, *dw_up, *dw_down;      // copies
 };
 BackwardScratch backward_scratch(const muon_feed_forward_desc_t* d, Scratch* s) {
   BackwardScratch r = {};
@@ -166,6 +225,20 @@ BackwardScratch backward_scratch(const muon_feed_forward_desc_t* d, Scratch* s) 
   r.dup = s->take(d->tokens * r.ldh * e);
   r.h = s->take(d->tokens * r.ldh * e);
   if (d->keep == MUON_KEEP_8BIT) r.x = s->take(d->tokens * r.ldx * e);
+  const Odd odd(d);
+  const bool full = d->keep == MUON_KEEP_FULL;
+  const int64_t t = d->tokens;
+  r.dy = room(s, odd.dim, t, d->dim, d->dtype);
+  r.given_x = room(s, odd.dim && full, t, d->dim, d->dtype);
+  r.w_gate = room(s, odd.dim, d->hidden, d->dim, d->dtype);
+  r.w_up = room(s, odd.dim, d->hidden, d->dim, d->dtype);
+  r.dx = room(s, odd.dim, t, d->dim, d->dtype);
+  r.dw_gate = room(s, odd.dim, d->hidden, d->dim, d->dtype);
+  r.dw_up = room(s, odd.dim, d->hidden, d->dim, d->dtype);
+  r.w_down = room(s, odd.hidden, d->dim, d->hidden, d->dtype);
+  r.dw_down = room(s, odd.hidden, d->dim, d->hidden, d->dtype);
+  r.gate = room(s, odd.hidden && full, t, d->hidden, d->dtype);
+  r.up = room(s, odd.hidden && full, t, d->hidden, d->dtype);
   return r;
 }
 
@@ -178,9 +251,19 @@ struct LinearScratch {
   muon_blocks_t dy8;
   void* x;
   int64_t ldx;
+  void *w8, *y, *dy, *dx, *dw;   // copies
 };
-LinearScratch linear_scratch(const muon_linear_blocks_desc_t* d, Scratch* s) {
+LinearScratch linear_scratch(const muon_linear_blocks_desc_t* d, bool backward, Scratch* s) {
   LinearScratch r = {};
+  const bool worth = int64_t(d->tokens) * d->dim >= (kWorthCopies + d->out - 1) / d->out;
+  r.w8 = room(s, worth && d->dim % 16 != 0, d->out, d->dim, kTypeE4m3);
+  if (!backward) {
+    r.y = room(s, worth && d->out % 8 != 0, d->tokens, d->out, kTypeBf16);
+    return r;
+  }
+  r.dy = room(s, worth && d->out % 8 != 0, d->tokens, d->out, kTypeBf16);
+  r.dx = room(s, worth && d->dim % 8 != 0, d->tokens, d->dim, kTypeBf16);
+  r.dw = room(s, worth && d->dim % 8 != 0, d->out, d->dim, kTypeBf16);
   r.dy8.ld = up_to(d->out, 16);
   r.dy8.lds = up_to(blocks_of(d->out), 16);       // the tensor cores' scales are read 16 bytes at a time
   r.dy8.block_rows = 1;
@@ -256,22 +339,29 @@ int muon_feed_forward_forward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* d
   Launches l = {ctx, 0, static_cast<cudaStream_t>(stream)};
   if ((rc = device_of(ctx, &l.sms)) != MUON_OK) return rc;
 
-  Product p = plain(t, hidden, dim, operand(x, d->dtype), operand(w_gate, d->dtype), w.h, w.ldh, d->dtype);
-  p.b[1] = operand(w_up, d->dtype);
+  const int dt = d->dtype;
+  Copies c;
+  const Operand ox = c.take(operand(x, dt), t, dim, w.x);
+  Product p = plain(t, hidden, dim, ox, c.take(operand(w_gate, dt), hidden, dim, w.w_gate), w.h, w.ldh, dt);
+  p.b[1] = c.take(operand(w_up, dt), hidden, dim, w.w_up);
+  const Operand down = c.take(operand(w_down, dt), dim, hidden, w.w_down);
+  const muon_rows_t oy = c.give(y, t, dim, w.y, dt);
   p.e.kind = kGated;
   p.e.activation = d->activation;
-  p.e.gate_up_type = d->dtype;
+  p.e.gate_up_type = dt;
   if (d->keep == MUON_KEEP_FULL) {
-    p.e.gate = kept->gate.data;
-    p.e.ld_gate = kept->gate.ld;
-    p.e.up = kept->up.data;
-    p.e.ld_up = kept->up.ld;
+    const muon_rows_t gate = c.give(&kept->gate, t, hidden, w.kept_gate, dt), up = c.give(&kept->up, t, hidden, w.kept_up, dt);
+    p.e.gate = gate.data;
+    p.e.ld_gate = gate.ld;
+    p.e.up = up.data;
+    p.e.ld_up = up.ld;
   } else if (d->keep == MUON_KEEP_8BIT) {
     p.e.gate_up_type = kTypeE4m3;
     p.e.in_gate = operand(&kept->gate8);
     p.e.in_up = operand(&kept->up8);
-    l.quantize(d->dtype, t, dim, x->data, x->ld, operand(&kept->x8));
+    l.quantize(dt, t, dim, x->data, x->ld, operand(&kept->x8));
   }
+  l.copies(c.in, c.ins);
   if (d->keep != MUON_KEEP_8BIT || products_tc_take(&p, 1)) {
     l.product(p);
   } else {                       // on CUDA cores a tile does not hold a block's columns: g and u wait in fp32, some rows at a time
@@ -279,7 +369,7 @@ int muon_feed_forward_forward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* d
       const int64_t n = t - r < kUnalignedRows ? t - r : kUnalignedRows;
       Product q = p;
       q.m = int32_t(n);
-      q.a[0].data = static_cast<const char*>(x->data) + r * x->ld * int64_t(e);
+      q.a[0].data = static_cast<const char*>(ox.data) + r * ox.ld * int64_t(e);
       q.e.c = static_cast<char*>(w.h) + r * w.ldh * int64_t(e);
       q.e.gate_up_type = kTypeFp32;
       q.e.gate = w.gate;
@@ -294,7 +384,8 @@ int muon_feed_forward_forward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* d
       }
     }
   }
-  l.product(plain(t, dim, hidden, operand(w.h, w.ldh, d->dtype), operand(w_down, d->dtype), y->data, y->ld, d->dtype), true);
+  l.product(plain(t, dim, hidden, operand(w.h, w.ldh, dt), down, oy.data, oy.ld, dt), true);
+  l.copies(c.out, c.outs);
   return l.rc;
 }
 
@@ -332,63 +423,94 @@ int muon_feed_forward_backward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* 
   const muon_rows_t none = {nullptr, dim};
   if (!dy) dy = &none;           // no tokens: the products below have no k
   if (!x) x = &none;
+  const bool weights = dw_gate || dw_up || dw_down, by_x = dw_gate || dw_up;
+  Copies c;
+  auto turned = [](Operand o) {
+    o.mn_major = 1;
+    return o;
+  };
+  const Operand ody = c.take(operand(dy, dt), t, dim, w.dy), down = c.take(operand(w_down, dt, true), dim, hidden, w.w_down);
+  Operand gate = operand(&kept->gate8), up = operand(&kept->up8), ox = operand(w.x, w.ldx, dt);
+  if (given_x) {
+    gate = c.take(operand(&kept->gate, dt), t, hidden, w.gate);
+    up = c.take(operand(&kept->up, dt), t, hidden, w.up);
+    ox = by_x ? c.take(operand(x, dt), t, dim, w.given_x) : operand(x, dt);
+  }
+  muon_rows_t odx = none, odg = none, odu = none, odd = none;
+  Operand by_gate = {}, by_up = {};
+  if (dx) {
+    by_gate = c.take(operand(w_gate, dt, true), hidden, dim, w.w_gate);
+    by_up = c.take(operand(w_up, dt, true), hidden, dim, w.w_up);
+    odx = c.give(dx, t, dim, w.dx, dt);
+  }
+  if (dw_gate) odg = c.give(dw_gate, hidden, dim, w.dw_gate, dt);
+  if (dw_up) odu = c.give(dw_up, hidden, dim, w.dw_up, dt);
+  if (dw_down) odd = c.give(dw_down, dim, hidden, w.dw_down, dt);
   if (t > 0) {
-    Product p = plain(t, hidden, dim, operand(dy, dt), operand(w_down, dt, true), w.h, w.ldh, dt);
+    l.copies(c.in, c.ins);
+    Product p = plain(t, hidden, dim, ody, down, w.h, w.ldh, dt);
     p.e.kind = kGrad;
     p.e.activation = d->activation;
     p.e.gate = w.dgate;
     p.e.up = w.dup;
     p.e.ld_gate = p.e.ld_up = w.ldh;
-    p.e.in_gate = given_x ? operand(&kept->gate, dt) : operand(&kept->gate8);
-    p.e.in_up = given_x ? operand(&kept->up, dt) : operand(&kept->up8);
-    p.e.gate_up_type = p.e.in_gate.type;
+    p.e.in_gate = gate;
+    p.e.in_up = up;
+    p.e.gate_up_type = gate.type;
     l.product(p);
   }
   if (dx && t > 0) {
-    Product p = plain(t, dim, hidden, operand(w.dgate, w.ldh, dt), operand(w_gate, dt, true), dx->data, dx->ld, dt);
+    Product p = plain(t, dim, hidden, operand(w.dgate, w.ldh, dt), by_gate, odx.data, odx.ld, dt);
     p.segments = 2;
     p.a[1] = operand(w.dup, w.ldh, dt);
-    p.b[1] = operand(w_up, dt, true);
+    p.b[1] = by_up;
     l.product(p, true);
   }
-  Operand ox = operand(x, dt, true);
-  if (!given_x && (dw_gate || dw_up)) {
-    if (t > 0) l.dequantize(dt, t, dim, operand(&kept->x8), w.x, w.ldx);
-    ox = operand(w.x, w.ldx, dt, true);
+  if (weights) {
+    if (!given_x && by_x && t > 0) l.dequantize(dt, t, dim, operand(&kept->x8), w.x, w.ldx);
+    Product list[kMaxProducts];
+    int n = 0;
+    if (dw_gate) list[n++] = plain(hidden, dim, t, operand(w.dgate, w.ldh, dt, true), turned(ox), odg.data, odg.ld, dt);
+    if (dw_up) list[n++] = plain(hidden, dim, t, operand(w.dup, w.ldh, dt, true), turned(ox), odu.data, odu.ld, dt);
+    if (dw_down) list[n++] = plain(dim, hidden, t, turned(ody), operand(w.h, w.ldh, dt, true), odd.data, odd.ld, dt);
+    l.products(list, n, kMaxProducts);
   }
-  Product list[kMaxProducts];
-  int n = 0;
-  if (dw_gate) list[n++] = plain(hidden, dim, t, operand(w.dgate, w.ldh, dt, true), ox, dw_gate->data, dw_gate->ld, dt);
-  if (dw_up) list[n++] = plain(hidden, dim, t, operand(w.dup, w.ldh, dt, true), ox, dw_up->data, dw_up->ld, dt);
-  if (dw_down) list[n++] = plain(dim, hidden, t, operand(dy, dt, true), operand(w.h, w.ldh, dt, true), dw_down->data, dw_down->ld, dt);
-  l.products(list, n, kMaxProducts);
+  l.copies(c.out, c.outs);
   return l.rc;
 }
 
 int muon_linear_blocks_forward(muon_ctx_t* ctx, const muon_linear_blocks_desc_t* d, const muon_rows_t* x, const muon_blocks_t* w8, const muon_rows_t* y,
-                             const muon_blocks_t* x8, void* stream) {
+                             const muon_blocks_t* x8, void* workspace, size_t workspace_bytes, void* stream) {
   if (!ctx) return MUON_ERR_INVALID_ARG;
   int rc = check_linear(d);
   if (rc != MUON_OK) return rc;
   if (d->tokens == 0) return MUON_OK;
   const int64_t t = d->tokens, dim = d->dim, out = d->out;
   if (!good_rows(x, t, dim, 2) || !good_rows(y, t, out, 2) || !good_blocks(w8, out, dim, kBlock) || !good_blocks(x8, t, dim, 1)) return MUON_ERR_INVALID_ARG;
-  if (results_clash({rows_box(y, t, out, 2), codes_box(*x8, t, dim), scales_box(*x8, t, dim)},
+  Scratch s = {static_cast<char*>(workspace)};
+  const LinearScratch w = linear_scratch(d, false, &s);
+  if ((rc = check_scratch(workspace, workspace_bytes, s.used)) != MUON_OK) return rc;
+  if (results_clash({rows_box(y, t, out, 2), codes_box(*x8, t, dim), scales_box(*x8, t, dim), run_of(workspace, int64_t(s.used))},
                     {rows_box(x, t, dim, 2), codes_box(*w8, out, dim), scales_box(*w8, out, dim)}))
     return MUON_ERR_INVALID_ARG;
   Launches l = {ctx, 0, static_cast<cudaStream_t>(stream)};
   if ((rc = device_of(ctx, &l.sms)) != MUON_OK) return rc;
+  Copies c;
+  const Operand ow = c.take(operand(w8), out, dim, w.w8);
+  const muon_rows_t oy = c.give(y, t, out, w.y, kTypeBf16);
+  l.copies(c.in, c.ins);
   l.quantize(kTypeBf16, t, dim, x->data, x->ld, operand(x8));
-  l.product(plain(t, out, dim, operand(x8), operand(w8), y->data, y->ld, kTypeBf16), true);
+  l.product(plain(t, out, dim, operand(x8), ow, oy.data, oy.ld, kTypeBf16), true);
+  l.copies(c.out, c.outs);
   return l.rc;
 }
 
-int muon_linear_blocks_workspace_bytes(const muon_linear_blocks_desc_t* desc, size_t* bytes) {
-  if (!bytes) return MUON_ERR_INVALID_ARG;
+int muon_linear_blocks_workspace_bytes(const muon_linear_blocks_desc_t* desc, int32_t backward, size_t* bytes) {
+  if (!bytes || (backward != 0 && backward != 1)) return MUON_ERR_INVALID_ARG;
   const int rc = check_linear(desc);
   if (rc != MUON_OK) return rc;
   Scratch s = {nullptr};
-  linear_scratch(desc, &s);
+  linear_scratch(desc, backward == 1, &s);
   *bytes = s.used;
   return MUON_OK;
 }
@@ -404,7 +526,7 @@ int muon_linear_blocks_backward(muon_ctx_t* ctx, const muon_linear_blocks_desc_t
       (dx && !good_rows(dx, t, dim, 2)) || (dw && !good_rows(dw, out, dim, 2)))
     return MUON_ERR_INVALID_ARG;
   Scratch s = {static_cast<char*>(workspace)};
-  const LinearScratch w = linear_scratch(d, &s);
+  const LinearScratch w = linear_scratch(d, true, &s);
   if ((rc = check_scratch(workspace, workspace_bytes, s.used)) != MUON_OK) return rc;
   const Box nothing = run_of(nullptr, 0);
   const bool rx = dw && t > 0, rw = dx && t > 0;
@@ -414,15 +536,27 @@ int muon_linear_blocks_backward(muon_ctx_t* ctx, const muon_linear_blocks_desc_t
     return MUON_ERR_INVALID_ARG;
   Launches l = {ctx, 0, static_cast<cudaStream_t>(stream)};
   if ((rc = device_of(ctx, &l.sms)) != MUON_OK) return rc;
+  const muon_rows_t none = {nullptr, out};
+  if (t == 0) dy = &none;
+  Copies c;
+  const Operand ody = dw ? c.take(operand(dy, kTypeBf16, true), t, out, w.dy) : operand(dy, kTypeBf16, true);
+  Operand ow = {};
+  muon_rows_t odx = none, odw = none;
+  if (rw) {
+    ow = c.take(operand(w8, true), out, dim, w.w8);
+    odx = c.give(dx, t, dim, w.dx, kTypeBf16);
+  }
+  if (dw) odw = c.give(dw, out, dim, w.dw, kTypeBf16);
+  if (t > 0) l.copies(c.in, c.ins);
   if (rw) {
     l.quantize(kTypeBf16, t, out, dy->data, dy->ld, operand(&w.dy8));
-    l.product(plain(t, dim, out, operand(&w.dy8), operand(w8, true), dx->data, dx->ld, kTypeBf16), true);
+    l.product(plain(t, dim, out, operand(&w.dy8), ow, odx.data, odx.ld, kTypeBf16), true);
   }
   if (dw) {
-    const muon_rows_t none = {nullptr, out};
     if (rx) l.dequantize(kTypeBf16, t, dim, operand(x8), w.x, w.ldx);
-    l.product(plain(out, dim, t, operand(rx ? dy : &none, kTypeBf16, true), operand(w.x, w.ldx, kTypeBf16, true), dw->data, dw->ld, kTypeBf16));
+    l.product(plain(out, dim, t, ody, operand(w.x, w.ldx, kTypeBf16, true), odw.data, odw.ld, kTypeBf16));
   }
+  l.copies(c.out, c.outs);
   return l.rc;
 }
 

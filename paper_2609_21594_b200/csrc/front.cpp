@@ -428,7 +428,8 @@ PackedView packed(const Tensor& codes, const Tensor& scales, int64_t block_rows,
   return v;
 }
 
-muon_rows_t rows_view(const Tensor& r) { return {r.data_ptr(), row_stride(r)}; }
+// One row alone has no distance to a next one, and gets one that the tensor cores take.
+muon_rows_t rows_view(const Tensor& r) { return {r.data_ptr(), r.size(0) > 1 ? row_stride(r) : (r.size(1) + 7) / 8 * 8}; }
 const muon_rows_t* maybe(const MaybeTensor& t, muon_rows_t* v) {
   if (!t) return nullptr;
   *v = rows_view(*t);
@@ -518,8 +519,9 @@ std::tuple<Tensor, std::vector<Tensor>> feed_forward_forward(const Tensor& x, co
   muon_feed_forward_kept_t k = {};
   if (c.d.keep == MUON_KEEP_FULL) {
     for (muon_rows_t* t : {&k.gate, &k.up}) {
-      kept.push_back(at::empty(c.hidden_shape, x.options()));
-      *t = {kept.back().data_ptr(), c.d.hidden};
+      const int64_t ld = (int64_t(c.d.hidden) + 7) / 8 * 8;
+      kept.push_back(new_pitched(c.hidden_shape, ld, x.options()));
+      *t = {kept.back().data_ptr(), ld};
     }
   } else if (c.d.keep == MUON_KEEP_8BIT) {
     for (muon_blocks_t* t : {&k.x8, &k.gate8, &k.up8}) {
@@ -614,7 +616,10 @@ std::tuple<Tensor, Tensor, Tensor> linear_8bit_forward(const Tensor& x, const Te
   const Packed p = new_packed(x.sizes(), x.options(), 1);
   const PackedView x8 = packed(p.codes, p.scales, 1, "the result");
   const muon_rows_t in = rows_view(r), out = {y.data_ptr(), w.rows};
-  check(muon_linear_blocks_forward(context(index), &d, &in, &w.b, &out, &x8.b, stream_of(index)), "muon_linear_blocks_forward");
+  size_t n = 0;
+  check(muon_linear_blocks_workspace_bytes(&d, 0, &n), "muon_linear_blocks_workspace_bytes");
+  const MaybeTensor ws = new_scratch(n, x);
+  check(muon_linear_blocks_forward(context(index), &d, &in, &w.b, &out, &x8.b, address(ws), n, stream_of(index)), "muon_linear_blocks_forward");
   return {y, p.codes, p.scales};
 }
 
@@ -642,7 +647,7 @@ std::tuple<MaybeTensor, MaybeTensor> linear_8bit_backward(const Tensor& dy, cons
   }
   if (need[1]) dw = at::empty({w.rows, w.cols}, dy.options());
   size_t n = 0;
-  check(muon_linear_blocks_workspace_bytes(&d, &n), "muon_linear_blocks_workspace_bytes");
+  check(muon_linear_blocks_workspace_bytes(&d, 1, &n), "muon_linear_blocks_workspace_bytes");
   const MaybeTensor ws = new_scratch(n, dy);
   const muon_rows_t in = rows_view(r);
   check(muon_linear_blocks_backward(context(index), &d, &in, &x.b, &w.b, dx ? &out[0] : nullptr, maybe(dw, &out[1]), address(ws), n, stream_of(index)),

@@ -309,6 +309,52 @@ __global__ void __launch_bounds__(kThreads) dequantize_any_kernel(const uint8_t*
     if (k < count) out[k] = T(v[k]);
 }
 
+struct CopyList {
+  CopyTask task[kMaxCopies];
+  int64_t begin[kMaxCopies];                 // first of a task's warps
+  int32_t count;
+};
+// A warp moves a run of kRun bytes of a row: whole words of the destination, each out of the two words of the source that hold it, and what is left at the
+// ends by elements.
+constexpr int kRun = 1024;
+template <typename E>
+__device__ __forceinline__ void copy_run(const char* from, char* to, int bytes, const char* first, const char* last, int lane) {
+  const int head = min(int((4 - (reinterpret_cast<uintptr_t>(to) & 3)) & 3), bytes), words = (bytes - head) / 4, tail = head + words * 4;
+  const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(from + head)) & 3u;
+  for (int i = lane; i < words; i += 32) {
+    const char* p = from + head + 4 * i;
+    uint32_t w = 0;
+    if (off == 0) {
+      w = *reinterpret_cast<const uint32_t*>(p);
+    } else if (p - off >= first && p - off + 8 <= last) {
+      w = __funnelshift_r(*reinterpret_cast<const uint32_t*>(p - off), *reinterpret_cast<const uint32_t*>(p - off + 4), 8 * off);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4 / int(sizeof(E)); ++k) w |= uint32_t(reinterpret_cast<const E*>(p)[k]) << (8 * sizeof(E) * k);
+    }
+    *reinterpret_cast<uint32_t*>(to + head + 4 * i) = w;
+  }
+  const int at = lane * int(sizeof(E));
+  if (at < head) *reinterpret_cast<E*>(to + at) = *reinterpret_cast<const E*>(from + at);
+  if (tail + at < bytes) *reinterpret_cast<E*>(to + tail + at) = *reinterpret_cast<const E*>(from + tail + at);
+}
+__global__ void __launch_bounds__(kThreads) copy_rows_kernel(const __grid_constant__ CopyList L) {
+  const int64_t warp = int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
+  int which = 0;
+  for (int i = 1; i < L.count; ++i)
+    if (warp >= L.begin[i]) which = i;
+  const CopyTask& t = L.task[which];
+  const int64_t per_row = (t.bytes + kRun - 1) / kRun, i = warp - L.begin[which], row = i / per_row, at = (i - row * per_row) * kRun;
+  if (row >= t.rows) return;
+  const char* first = static_cast<const char*>(t.from);
+  const char* from = first + row * t.ld_from + at;
+  char* to = static_cast<char*>(t.to) + row * t.ld_to + at;
+  const char* last = first + (t.rows - 1) * t.ld_from + t.bytes;
+  const int bytes = int(min(int64_t(kRun), t.bytes - at));
+  if (t.unit == 1) copy_run<uint8_t>(from, to, bytes, first, last, threadIdx.x & 31);
+  else copy_run<uint16_t>(from, to, bytes, first, last, threadIdx.x & 31);
+}
+
 bool wide(const void* p, int64_t ld_bytes, int align) { return reinterpret_cast<uintptr_t>(p) % align == 0 && ld_bytes % align == 0; }
 int done(int n) { return cudaGetLastError() == cudaSuccess ? n : MUON_ERR_CUDA; }
 
@@ -350,6 +396,22 @@ int dequantize(int64_t rows, int64_t cols, const Operand& in, T* y, int64_t ldy,
 }
 
 }  // namespace
+
+int launch_copies(const CopyTask* list, int count, int, cudaStream_t st) {
+  CopyList L = {};
+  int64_t warps = 0;
+  for (int i = 0; i < count; ++i) {
+    L.task[i] = list[i];
+    L.begin[i] = warps;
+    warps += list[i].rows * ((list[i].bytes + kRun - 1) / kRun);
+  }
+  L.count = count;
+  const int64_t blocks = (warps + kThreads / 32 - 1) / (kThreads / 32);
+  if (blocks == 0) return 0;
+  if (blocks > INT32_MAX) return MUON_ERR_UNSUPPORTED;
+  copy_rows_kernel<<<unsigned(blocks), kThreads, 0, st>>>(L);
+  return done(1);
+}
 
 int launch_quantize(int dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx, const Operand& out, int, cudaStream_t st) {
   if (rows == 0) return 0;

@@ -306,9 +306,18 @@ __global__ void __launch_bounds__(kThreads, 2) product_few_kernel(const __grid_c
         }
       sum[k][0] = v.x; sum[k][1] = v.y; sum[k][2] = v.z; sum[k][3] = v.w;
     }
-    const bool inside = col < L.n;              // a multiple of 8 columns: four are all inside or all outside
+    const int left = L.n - col;
+    const bool inside = left > 0, whole = left >= 4;
     auto put = [&](int which, float a, float b, float c, float d) {
-      if (inside) *reinterpret_cast<uint2*>(L.out[which] + t * L.ld[which] + col) = make_uint2(pack2(a, b), pack2(c, d));
+      const uint32_t w[2] = {pack2(a, b), pack2(c, d)};
+      __nv_bfloat16* to = L.out[which] + t * L.ld[which] + col;
+      if (whole) {
+        *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+          if (i < left) reinterpret_cast<uint16_t*>(to)[i] = uint16_t(w[i >> 1] >> (16 * (i & 1)));
+      }
     };
     if constexpr (EPI == kPlain) {
       put(0, sum[0][0], sum[0][1], sum[0][2], sum[0][3]);
@@ -334,11 +343,12 @@ __global__ void __launch_bounds__(kThreads, 2) product_few_kernel(const __grid_c
           for (int i = 0; i < 2; ++i)
             c[i] = __nv_cvt_float2_to_fp8x2(make_float2(infinite_to_nan(v[2 * i]) * inverse, infinite_to_nan(v[2 * i + 1]) * inverse), __NV_SATFINITE, __NV_E4M3);
           uint8_t* p = static_cast<uint8_t*>(const_cast<void*>(o.data)) + t * o.ld + col;
-          if (inside && L.codes_wide) {
+          if (whole && L.codes_wide) {
             *reinterpret_cast<uint32_t*>(p) = c[0] | c[1] << 16;
-          } else if (inside) {
+          } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = uint8_t(c[i >> 1] >> (8 * (i & 1)));
+            for (int i = 0; i < 4; ++i)
+              if (i < left) p[i] = uint8_t(c[i >> 1] >> (8 * (i & 1)));
           }
           if (lane == 0) const_cast<uint8_t*>(o.scales)[t * o.lds + (col >> 7)] = uint8_t(e);
         };
@@ -356,11 +366,12 @@ __global__ void __launch_bounds__(kThreads, 2) product_few_kernel(const __grid_c
             const uint8_t* p = static_cast<const uint8_t*>(o.data) + t * o.ld + col;
             const float scale = scale_of(__ldg(o.scales + t * o.lds + (col >> 7)));
             uint32_t c = 0;
-            if (L.codes_wide) {
+            if (whole && L.codes_wide) {
               c = __ldg(reinterpret_cast<const uint32_t*>(p));
             } else {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) c |= uint32_t(__ldg(p + i)) << (8 * i);
+              for (int i = 0; i < 4; ++i)
+                if (i < left) c |= uint32_t(__ldg(p + i)) << (8 * i);
             }
             const float2 lo = values_of(c), hi = values_of(c >> 16);
             v[0] = lo.x * scale; v[1] = lo.y * scale; v[2] = hi.x * scale; v[3] = hi.y * scale;
@@ -369,7 +380,15 @@ __global__ void __launch_bounds__(kThreads, 2) product_few_kernel(const __grid_c
           take(L.up, u);
         } else {
           auto take = [&](int which, float (&v)[4]) {
-            const uint2 x = __ldg(reinterpret_cast<const uint2*>(L.in[which] + t * L.ld_in[which] + col));
+            const __nv_bfloat16* from = L.in[which] + t * L.ld_in[which] + col;
+            uint2 x = make_uint2(0, 0);
+            if (whole) {
+              x = __ldg(reinterpret_cast<const uint2*>(from));
+            } else {
+              const uint16_t* q = reinterpret_cast<const uint16_t*>(from);
+              x.x = uint32_t(__ldg(q)) | (left > 1 ? uint32_t(__ldg(q + 1)) << 16 : 0u);
+              x.y = left > 2 ? uint32_t(__ldg(q + 2)) : 0u;
+            }
             v[0] = low(x.x); v[1] = high(x.x); v[2] = low(x.y); v[3] = high(x.y);
           };
           take(0, g);
@@ -473,7 +492,7 @@ int launch_product_few(muon_ctx* ctx, const Product& q, int sms, bool follows, c
   L.keep = e.kind == kGated && e.gate;
   L.gate = e.in_gate;
   L.up = e.in_up;
-  L.codes_wide = codes && addressable(L.gate.data, L.gate.ld, 1) && addressable(L.up.data, L.up.ld, 1);
+  L.codes_wide = codes && addressable(L.gate.data, L.gate.ld, kTypeE4m3) && addressable(L.up.data, L.up.ld, kTypeE4m3);
   L.status = ctx->d_status;
   Encoder enc = {ctx};
   for (int s = 0; s < (tiles == 2 ? 2 : q.segments); ++s) enc.operand(&L.w[s], q.b[s], q.n, q.k, kRowsW);

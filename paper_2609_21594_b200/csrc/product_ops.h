@@ -53,6 +53,24 @@ struct Product {
 
 constexpr int kMaxProducts = 3;   // of a launch
 
+// What TMA asks of rows of `ld` elements: the first, and the distance between two, on 16 bytes.
+inline int size_of_type(int type) { return type == kTypeFp32 ? 4 : type == kTypeBf16 ? 2 : 1; }
+inline bool addressable(const void* p, int64_t ld, int type) {
+  const int64_t bytes = ld * size_of_type(type);
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && bytes % 16 == 0 && bytes < (int64_t(1) << 40);
+}
+
+// Rows of bytes to another place, for tensors that TMA cannot address: into rows that it can, or out of them.  `unit`: bytes of an element, which
+// source and destination are aligned to.
+struct CopyTask {
+  const void* from;
+  void* to;
+  int64_t ld_from, ld_to, rows, bytes;     // in bytes
+  int32_t unit;
+};
+constexpr int kMaxCopies = 8;
+int launch_copies(const CopyTask* list, int count, int sms, cudaStream_t st);
+
 // The tensor-core engine takes a list of products with operands of one type and one order in memory, if TMA can address all tensors.
 bool products_tc_take(const Product* p, int count);
 int launch_products_tc(muon_ctx* ctx, const Product* p, int count, cudaStream_t st);

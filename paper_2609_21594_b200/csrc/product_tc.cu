@@ -652,21 +652,21 @@ bool products_tc_take(const Product* list, int count) {
     if (type != kTypeBf16 && type != kTypeE4m3) return false;
     for (int s = 0; s < ns; ++s) {
       const Operand& b = p.b[s];
-      if (b.type != type || !addressable(b.data, b.ld, elem_of(type)) || b.mn_major != list[0].b[0].mn_major) return false;
+      if (b.type != type || !addressable(b.data, b.ld, type) || b.mn_major != list[0].b[0].mn_major) return false;
       if (b.type == kTypeE4m3 && b.mn_major && b.block_rows != kBlock) return false;
     }
     for (int s = 0; s < p.segments; ++s) {
       const Operand& a = p.a[s];
-      if (a.type != type || !addressable(a.data, a.ld, elem_of(type)) || a.mn_major != list[0].a[0].mn_major) return false;
+      if (a.type != type || !addressable(a.data, a.ld, type) || a.mn_major != list[0].a[0].mn_major) return false;
     }
     const bool amn = p.a[0].mn_major, bmn = p.b[0].mn_major;
     if (type == kTypeE4m3 ? amn || e.kind != kPlain || p.segments != 1 : (e.kind == kGated && (amn || bmn)) || (e.kind == kGrad && (amn || !bmn)) || (amn && !bmn))
       return false;
-    if (p.n % 8 || !addressable(e.c, e.ldc, 2)) return false;
-    if (e.kind == kGated && e.gate && (!addressable(e.gate, e.ld_gate, 2) || !addressable(e.up, e.ld_up, 2))) return false;
+    if (!addressable(e.c, e.ldc, kTypeBf16)) return false;
+    if (e.kind == kGated && e.gate && (!addressable(e.gate, e.ld_gate, kTypeBf16) || !addressable(e.up, e.ld_up, kTypeBf16))) return false;
     if (e.kind == kGrad) {
-      if (!addressable(e.gate, e.ld_gate, 2) || !addressable(e.up, e.ld_up, 2)) return false;
-      if (e.gate_up_type == kTypeBf16 && (!addressable(e.in_gate.data, e.in_gate.ld, 2) || !addressable(e.in_up.data, e.in_up.ld, 2))) return false;
+      if (!addressable(e.gate, e.ld_gate, kTypeBf16) || !addressable(e.up, e.ld_up, kTypeBf16)) return false;
+      if (e.gate_up_type == kTypeBf16 && (!addressable(e.in_gate.data, e.in_gate.ld, kTypeBf16) || !addressable(e.in_up.data, e.in_up.ld, kTypeBf16))) return false;
     }
   }
   return true;
@@ -687,7 +687,7 @@ int launch_products_tc(muon_ctx* ctx, const Product* list, int count, cudaStream
   L.keep = e0.kind == kGated && e0.gate;
   L.gate = e0.in_gate;
   L.up = e0.in_up;
-  L.codes_wide = codes && addressable(L.gate.data, L.gate.ld, 1) && addressable(L.up.data, L.up.ld, 1);
+  L.codes_wide = codes && addressable(L.gate.data, L.gate.ld, kTypeE4m3) && addressable(L.up.data, L.up.ld, kTypeE4m3);
   L.sectors = 1;
   L.status = ctx->d_status;
   Encoder enc = {ctx};

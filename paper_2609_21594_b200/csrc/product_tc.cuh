@@ -140,19 +140,29 @@ __device__ __forceinline__ void gather_scales(const Scales& s, int row0, int kb,
   }
 }
 
-// 16 columns (two to a word) of a row of bf16, of which `left`, a multiple of 8, are inside.
+// 16 columns (two to a word) of a row of bf16 that begins on 16 bytes, of which `left` are inside.
 __device__ __forceinline__ void put16(__nv_bfloat16* p, const uint32_t* w, int left, bool sectors) {
   if (left >= 16 && sectors) return store32(p, w);
   if (left >= 8) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-  if (left >= 16) *reinterpret_cast<uint4*>(p + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+  if (left >= 16) {
+    *reinterpret_cast<uint4*>(p + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (i < left && (left < 8) == (i < 8)) reinterpret_cast<uint16_t*>(p)[i] = uint16_t(w[i >> 1] >> (16 * (i & 1)));
 }
 __device__ __forceinline__ void get16(const __nv_bfloat16* p, uint32_t* w, int left, bool sectors) {
   if (left >= 16 && sectors) return load32(p, w);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const uint4 x = left >= 8 * (h + 1) ? __ldg(reinterpret_cast<const uint4*>(p) + h) : make_uint4(0, 0, 0, 0);
+    uint4 x = make_uint4(0, 0, 0, 0);
+    if (left >= 8 * (h + 1)) x = __ldg(reinterpret_cast<const uint4*>(p) + h);
     w[4 * h] = x.x; w[4 * h + 1] = x.y; w[4 * h + 2] = x.z; w[4 * h + 3] = x.w;
   }
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (i < left && left < 16 && (left < 8) == (i < 8)) w[i >> 1] |= uint32_t(__ldg(reinterpret_cast<const uint16_t*>(p) + i)) << (16 * (i & 1));
 }
 
 __device__ __forceinline__ float2 values_of(uint32_t pair) {
@@ -160,17 +170,12 @@ __device__ __forceinline__ float2 values_of(uint32_t pair) {
 }
 
 // ------------------------------------------------------------------ host
-inline bool addressable(const void* p, int64_t ld, int elem) {
-  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * elem % 16 == 0 && ld * elem < (int64_t(1) << 40);
-}
-inline int elem_of(int type) { return type == kTypeBf16 ? 2 : 1; }
-
 struct Encoder {
   muon_ctx* ctx;
   bool ok = true;
   void map(CUtensorMap* to, const void* data, int type, int64_t ld, int64_t cols, int64_t rows, uint32_t box_cols, uint32_t box_rows) {
     const cuuint64_t dims[2] = {cuuint64_t(cols), cuuint64_t(rows)};
-    const cuuint64_t strides[1] = {cuuint64_t(ld * elem_of(type))};
+    const cuuint64_t strides[1] = {cuuint64_t(ld * size_of_type(type))};
     const cuuint32_t box[2] = {box_cols, box_rows}, estr[2] = {1u, 1u};
     ok = ok && reinterpret_cast<EncodeFn>(ctx->tmap_encode)(
                    to, type == kTypeBf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(data), dims, strides, box, estr,
@@ -179,7 +184,7 @@ struct Encoder {
   }
   // `rows`: of the operand in a tile of a CTA
   void operand(CUtensorMap* to, const Operand& o, int64_t n, int64_t k, uint32_t rows) {
-    const uint32_t line = 128 / uint32_t(elem_of(o.type));
+    const uint32_t line = 128 / uint32_t(size_of_type(o.type));
     if (o.mn_major) map(to, o.data, o.type, o.ld, n, k, line, line);
     else map(to, o.data, o.type, o.ld, k, n, line, rows);
   }

@@ -32,7 +32,7 @@ def test_scratch_and_refusals():
     assert mb.muon_feed_forward_workspace_bytes(desc(keep=mb.KEEP_8BIT), True) == 3 * up(100 * 136 * 2) + up(100 * 64 * 2)      # and x
     assert mb.muon_feed_forward_workspace_bytes(desc(keep=mb.KEEP_8BIT), False) == up(100 * 136 * 2) + 2 * up(100 * 130 * 4)
     assert mb.muon_feed_forward_workspace_bytes(desc(tokens=0), True) == 0
-    long = [mb.muon_feed_forward_workspace_bytes(desc(keep=mb.KEEP_8BIT, tokens=t), False) - up(t * 136 * 2) for t in (512, 5000)]
+    long = [mb.muon_feed_forward_workspace_bytes(desc(keep=mb.KEEP_8BIT, tokens=t, hidden=136), False) - up(t * 136 * 2) for t in (512, 5000)]
     assert long[0] == long[1]                                                                             # the fp32 rows are those of 512 tokens at most
     assert mb.muon_feed_forward_workspace_bytes(desc(dtype=mb.DTYPE_FP32), False) == up(100 * 136 * 4)
     for kw, code in ((dict(dtype=2), -1), (dict(activation=2), -1), (dict(keep=3), -1), (dict(tokens=-1), -1), (dict(dim=0), -1), (dict(hidden=0), -1),
@@ -41,10 +41,23 @@ def test_scratch_and_refusals():
             mb.muon_feed_forward_workspace_bytes(desc(**kw), True)
         assert e.value.code == code, kw
     lin = mb.LinearBlocksDesc(100, 64, 130, 0)
-    assert mb.muon_linear_blocks_workspace_bytes(lin) == up(100 * 144) + up(100 * 16) + up(100 * 64 * 2)
+    assert mb.muon_linear_blocks_workspace_bytes(lin, False) == 0
+    assert mb.muon_linear_blocks_workspace_bytes(lin, True) == up(100 * 144) + up(100 * 16) + up(100 * 64 * 2)
+    # rows that TMA cannot address have room for copies where the products are large: 4096 * 64 * 130 and 4096 * 65 * 130 are more than 2^25
+    t, big = 4096, mb.LinearBlocksDesc(4096, 64, 130, 0)
+    assert mb.muon_linear_blocks_workspace_bytes(big, False) == up(t * 136 * 2)                                          # y
+    big.dim = 65
+    assert mb.muon_linear_blocks_workspace_bytes(big, False) == up(t * 136 * 2) + up(130 * 80)                           # and w8
+    assert mb.muon_linear_blocks_workspace_bytes(big, True) == (up(130 * 80) + up(t * 136 * 2) + up(t * 72 * 2) + up(130 * 72 * 2)       # w8, dy, dx, dw
+                                                                + up(t * 144) + up(t * 16) + up(t * 72 * 2))             # dy in 8 bits, x
+    odd = desc(tokens=t)                                                                                                 # hidden = 130: w_down, gate, up
+    assert mb.muon_feed_forward_workspace_bytes(odd, False) == up(t * 136 * 2) + up(64 * 136 * 2) + 2 * up(t * 136 * 2)
+    assert mb.muon_feed_forward_workspace_bytes(odd, True) == 3 * up(t * 136 * 2) + 2 * up(64 * 136 * 2) + 2 * up(t * 136 * 2)
+    odd.dtype = mb.DTYPE_FP32
+    assert mb.muon_feed_forward_workspace_bytes(odd, False) == up(t * 136 * 4)
     for fields, code in (((-1, 64, 130, 0), -1), ((1, 0, 130, 0), -1), ((1, 64, 0, 0), -1), ((1, 64, 130, 1), -1), ((2**31 - 1, 64, 130, 0), -3)):
         with pytest.raises(mb.MuonError) as e:
-            mb.muon_linear_blocks_workspace_bytes(mb.LinearBlocksDesc(*fields))
+            mb.muon_linear_blocks_workspace_bytes(mb.LinearBlocksDesc(*fields), True)
         assert e.value.code == code, fields
 
 

@@ -219,6 +219,37 @@ def test_refusals():
             call()
 
 
+# products large enough that odd rows are copied for the tensor cores: dim, hidden, both; one token (rows that need no copy but the weights')
+ODD = [(700, 250, 264), (260, 256, 1021), (1100, 301, 643), (1, 5001, 6999), (70, 1000, 1413)]
+
+
+@pytest.mark.parametrize("keep", ["full", "8bit"])
+@pytest.mark.parametrize("tokens,dim,hidden", ODD)
+def test_odd_rows_on_the_tensor_cores(tokens, dim, hidden, keep):
+    from paper_2609_21594_b200 import functional as F
+
+    assert tokens * dim * hidden >= 2 ** 25
+    x, *w, dy = make(tokens, dim, hidden, torch.bfloat16)
+    want = ref.feed_forward(x, *w, "gelu")
+    y, kept = F.feed_forward_forward(x, *w, "gelu", keep)
+    assert y.is_contiguous() and ref.worst(y, want["y"]) <= 1
+    if keep == "full":
+        at = (x, *kept)
+        for got, name in zip(kept, ("gate", "up")):
+            assert ref.worst(got, (want[name][0], ref.rounded(*want[name], torch.bfloat16))) <= 1
+    else:
+        at = tuple(ref.unpack(kept[i].float(), kept[i + 1], 1) for i in (0, 2, 4))
+    wants = ref.feed_forward_backward(dy, *at, *w, "gelu")
+    for contiguous in (False, True):                         # kept as the call gave it, and as a program that copied it has it
+        given = tuple(t.contiguous() for t in kept) if contiguous else kept
+        got = F.feed_forward_backward(dy, x if keep == "full" else None, *w, given, "gelu")
+        for g, r in zip(got, wants):
+            assert g.is_contiguous() and ref.worst(g, r) <= 1
+    for k in range(4):
+        need = [i == k for i in range(4)]
+        assert torch.equal(F.feed_forward_backward(dy, x if keep == "full" else None, *w, kept, "gelu", need)[k], got[k])
+
+
 @pytest.mark.parametrize("tokens,dim,hidden", [(40, 256, 384), (300, 256, 384), (40, 100, 130)])
 def test_what_is_kept_in_8_bits_of_values_that_are_not_finite(tokens, dim, hidden):
     """Every engine: a NaN or an infinity in gate or up is kept as NaN and has no share in its block's scale."""

@@ -41,6 +41,31 @@ def test_forward_and_backward(tokens, dim, out):
     assert alone[0] is None and torch.equal(alone[1], dw)
 
 
+@pytest.mark.parametrize("tokens,dim,out", [(700, 250, 264), (260, 512, 1021), (1100, 301, 643), (1, 5001, 6999), (70, 1000, 1413), (300, 424, 1000)])
+def test_odd_rows_on_the_tensor_cores(tokens, dim, out):
+    """Products large enough that rows that TMA cannot address are copied for them; codes as `quantize` gives them, and packed together."""
+    from paper_2609_21594_b200 import functional as F
+
+    assert tokens * dim * out >= 2 ** 25
+    x, w, dy = make(tokens, dim, out)
+    w8 = F.quantize(w, 128)
+    want = None
+    for codes in (w8, tuple(t.contiguous() for t in w8)):
+        y, *x8 = F.linear_8bit_forward(x, *codes)
+        xv, wv = ref.unpack(x8[0].float(), x8[1], 1), ref.unpack(w8[0].float(), w8[1], 128)
+        v, off = ref.product(xv, wv)
+        assert y.is_contiguous() and ref.worst(y, (v, ref.rounded(v, off, torch.bfloat16))) <= 1
+        for given in (x8, [t.contiguous() for t in x8]):
+            dx, dw = F.linear_8bit_backward(dy, *given, *codes)
+            v, off = ref.product(ref.unpack(*ref.pack(dy, 1), 1), wv.T)
+            assert ref.worst(dx, (v, ref.rounded(v, off, torch.bfloat16))) <= 1
+            v, off = ref.product(dy.double().T, xv.T)
+            assert ref.worst(dw, (v, ref.rounded(v, off, torch.bfloat16))) <= 1
+            if want is None:
+                want = (y, dx, dw)
+            assert all(torch.equal(a, b) for a, b in zip((y, dx, dw), want))
+
+
 def test_views_and_shapes():
     """Codes inside wider rows, and at addresses that no wide load takes; x of more than two dimensions."""
     from paper_2609_21594_b200 import functional as F
