@@ -9,6 +9,11 @@
 // Two blocks run on a multiprocessor, so one loads while the other adds up.  Where the call before this one in the stream is a part of the same call,
 // the launch may begin before that one has ended: weights, which it does not write, are requested at once, tokens after griddepcontrol.wait.
 //
+// What bounds it.  One token: the bytes of the weights (4096 x 14336, both products 58 us, 6.1 TB/s; the kernel of CTA pairs takes 137).  More tokens: 64
+// bytes a clock that a multiprocessor takes in, and the sums on their way through shared memory (128 tokens 78 us against 109); from a few
+// hundred on the pairs win, by the estimate of plan_few (2048 x 5632, two products: 256 tokens 33 us against 41, 512 tokens 51 with the pairs' first product
+// and 85 without).
+//
 // All waits are bounded, as in the Newton-Schulz kernel; a block that gives up still meets its cluster.
 #include "product_tc.cuh"
 

@@ -7,6 +7,9 @@
 //
 // Where 128 x 128 tiles would leave multiprocessors idle, the tiles are 64 x 64 and the blocks of a cluster each take a part of k; the parts are added
 // in the order of the ranks, so the sum is the same in every run.
+//
+// What bounds it: 1024 x 1024 x 2816, both products 650 us, 27 TFLOP/s of 74, the multiply-add pipe 59 % busy while blocks run, and 352 blocks of the
+// gated product where 296 fit at once.  389 x 250 x 1021, backward, 77 us on the device: starts, meetings and ends of short sums.
 #include <cooperative_groups.h>
 #include <cuda_fp8.h>
 

@@ -17,6 +17,14 @@
 // over the lanes; the issuer copies four blocks' bytes (12 columns) every fourth k-block.  Two accumulators of 256 columns would leave no room for them, so the
 // second one begins 16 columns inside the first: the next tile begins when those 16 columns have been read, which the epilogue does first.
 //
+// What bounds it.  A k-block keeps the tensor cores busy for 512 clocks and brings 32 KiB to each multiprocessor, about what the second-level cache hands
+// out in that time, and the matrix instructions read as much from shared memory as it has: so the epilogue stays away from shared memory (staged there
+// and stored by TMA, the gated product with g and u kept ran at 88 % of the tensor pipe, the gradient at 68 %; now 98 and 84 to 86 %).  4096 tokens of
+// 4096 x 14336 (under ncu, clocks 1.4 to 1.5 GHz under the power limit): gated 616 us, 1561 TFLOP/s; down 328, 1466; gradient 363, 1326;
+// dx 659, 1461; the weights' gradients 949, 1521.  8 bits 180 us, 2667 TFLOP/s, 81 % of the pipe: between tiles the 16 shared columns and 3 copies
+// of scales per four k-blocks.  The gradient's epilogue moves 320 KiB a tile and ends after the next tile's products do when k
+// is short (3001 x 2048 x 5632: 79 us, 55 % of the pipe); sixteen epilogue warps instead of eight did not change that (80 us).
+//
 // Synchronisation as in the Newton-Schulz kernel, all waits bounded: full / empty per stage, tfull / tempty per accumulator, an abort flag in both CTAs.
 #include "product_tc.cuh"
 
