@@ -421,7 +421,9 @@ int muon_feed_forward_backward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* 
 
   const int dt = d->dtype;
   const muon_rows_t none = {nullptr, dim};
-  if (!dy) dy = &none;           // no tokens: the products below have no k
+  const muon_feed_forward_kept_t nothing = {};
+  if (t == 0) kept = &nothing;   // no tokens: the products below have no k, and what has rows of tokens may be NULL
+  if (!dy) dy = &none;
   if (!x) x = &none;
   const bool weights = dw_gate || dw_up || dw_down, by_x = dw_gate || dw_up;
   Copies c;

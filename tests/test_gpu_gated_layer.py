@@ -280,6 +280,15 @@ def test_c_calls_refuse_what_lies_over_something_else():
     d.keep = mb.KEEP_NONE
     with pytest.raises(mb.MuonError):
         backward()
+    # no tokens: what has rows of them may be NULL, and the weights' gradients are zeros
+    for keep in (mb.KEEP_FULL, mb.KEEP_8BIT):
+        d.keep, d.tokens = keep, 0
+        for t in (dg, du, dd):
+            t.fill_(7.0)
+        forward(x=None, y=None, kept=None, workspace=None, workspace_bytes=0)
+        backward(dy=None, x=None, dx=None, kept=None, workspace=None, workspace_bytes=0)
+        assert not any(t.any() for t in (dg, du, dd))
+    d.tokens = 16
     # a wider row of the result keeps what lies behind its columns
     d.keep = mb.KEEP_FULL
     wide = torch.full((16, 80), 7.0, device="cuda").bfloat16()
