@@ -10,8 +10,8 @@ namespace {
 constexpr int64_t kMaxTokens = (int64_t(1) << 31) - 1 - 512;      // tile coordinates past the last row stay in 32 bits
 constexpr int64_t kUnalignedRows = 512;                           // rows at a time whose fp32 g and u wait for their 8 bits (CUDA cores only)
 // Multiply-adds of a product from which on it is worth copying what TMA cannot address (rows of an odd number of elements) into rows that it can:
-// two launches of a few us against CUDA cores at a hundredth of the tensor cores' rate (2^25 take about 10 us there).
-constexpr int64_t kWorthCopies = int64_t(1) << 25;
+// two launches more against CUDA cores.  20 x 301 x 700 (2^22), 8-bit linear layer: 27 us there, 21 by copies, backward 51 and 33; 8 x 4096 x 1003 85 and 18.
+constexpr int64_t kWorthCopies = int64_t(1) << 21;
 
 int64_t up_to(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 int64_t blocks_of(int64_t n) { return (n + kBlock - 1) / kBlock; }

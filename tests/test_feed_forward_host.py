@@ -43,7 +43,7 @@ def test_scratch_and_refusals():
     lin = mb.LinearBlocksDesc(100, 64, 130, 0)
     assert mb.muon_linear_blocks_workspace_bytes(lin, False) == 0
     assert mb.muon_linear_blocks_workspace_bytes(lin, True) == up(100 * 144) + up(100 * 16) + up(100 * 64 * 2)
-    # rows that TMA cannot address have room for copies where the products are large: 4096 * 64 * 130 and 4096 * 65 * 130 are more than 2^25
+    # rows that TMA cannot address have room for copies where the products are large: 4096 * 64 * 130 and 4096 * 65 * 130 are more than 2^21, 100 * 64 * 130 is not
     t, big = 4096, mb.LinearBlocksDesc(4096, 64, 130, 0)
     assert mb.muon_linear_blocks_workspace_bytes(big, False) == up(t * 136 * 2)                                          # y
     big.dim = 65

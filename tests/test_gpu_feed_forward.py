@@ -228,7 +228,7 @@ ODD = [(700, 250, 264), (260, 256, 1021), (1100, 301, 643), (1, 5001, 6999), (70
 def test_odd_rows_on_the_tensor_cores(tokens, dim, hidden, keep):
     from paper_2609_21594_b200 import functional as F
 
-    assert tokens * dim * hidden >= 2 ** 25
+    assert tokens * dim * hidden >= 2 ** 21
     x, *w, dy = make(tokens, dim, hidden, torch.bfloat16)
     want = ref.feed_forward(x, *w, "gelu")
     y, kept = F.feed_forward_forward(x, *w, "gelu", keep)
