@@ -570,7 +570,8 @@ int muon_feed_forward_forward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* d
 
 /* From what was kept (x itself with KEEP_FULL, where x8 holds it otherwise and x is NULL):  dh = dy w_down,  dg = dh u act'(g),  du = dh act(g),
  *   dx = dg w_gate + du w_up,  dw_gate = dg^T x,  dw_up = du^T x,  dw_down = dy^T (act(g) u)
- * dh stays fp32; dg, du and act(g) u are rounded once to dtype.  Results that are NULL are not formed.  With no tokens dw_* are zeros. */
+ * dh stays fp32; dg, du and act(g) u are rounded once to dtype.  Results that are NULL are not formed.  With no tokens dw_* are zeros, and what has
+ * rows of tokens may be NULL.  Of this call and those beside it: no result may lie over an input, another result or the scratch. */
 int muon_feed_forward_backward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* desc, const muon_rows_t* dy, const muon_rows_t* x, const muon_rows_t* w_gate,
                                const muon_rows_t* w_up, const muon_rows_t* w_down, const muon_feed_forward_kept_t* kept, const muon_rows_t* dx,
                                const muon_rows_t* dw_gate, const muon_rows_t* dw_up, const muon_rows_t* dw_down, void* workspace,
