@@ -75,20 +75,19 @@ struct Launches {
     const int r = launched(ctx, n);
     if (rc == MUON_OK) rc = r;
   }
-  // follows: the call's last launch is right before this one in the stream, and writes nothing but what it takes as A.  Each product's engine is its own
-  // affair: a gradient has the same bits whichever others are wanted.
-  void products(const Product* p, int n, int siblings, bool follows = false) {
+  // Each product's engine is its own affair: a gradient has the same bits whichever others are wanted.
+  void products(const Product* p, int n, int siblings, Before before = kBeforeAny) {
     Product part[2][kMaxProducts];
     int count[2] = {0, 0};
     for (int i = 0; i < n; ++i) {
       const int tc = products_tc_take(p + i, 1) ? 1 : 0;
       part[tc][count[tc]++] = p[i];
     }
-    if (rc == MUON_OK && count[1] == 1 && product_few_takes(part[1][0], sms)) this->count(launch_product_few(ctx, part[1][0], sms, follows, st));
-    else if (rc == MUON_OK && count[1] > 0) this->count(launch_products_tc(ctx, part[1], count[1], st));
+    if (rc == MUON_OK && count[1] == 1 && product_few_takes(part[1][0], sms)) this->count(launch_product_few(ctx, part[1][0], sms, before, st));
+    else if (rc == MUON_OK && count[1] > 0) this->count(launch_products_tc(ctx, part[1], count[1], before, st));
     if (rc == MUON_OK && count[0] > 0) this->count(launch_products_simt(part[0], count[0], siblings, sms, st));
   }
-  void product(const Product& p, bool follows = false) { products(&p, 1, 1, follows); }
+  void product(const Product& p, Before before = kBeforeAny) { products(&p, 1, 1, before); }
   void copies(const CopyTask* list, int n) {
     if (rc == MUON_OK && n > 0) count(launch_copies(list, n, sms, st));
   }
@@ -384,7 +383,7 @@ int muon_feed_forward_forward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* d
       }
     }
   }
-  l.product(plain(t, dim, hidden, operand(w.h, w.ldh, dt), down, oy.data, oy.ld, dt), true);
+  l.product(plain(t, dim, hidden, operand(w.h, w.ldh, dt), down, oy.data, oy.ld, dt), kBeforeLeavesB);
   l.copies(c.out, c.outs);
   return l.rc;
 }
@@ -466,7 +465,7 @@ int muon_feed_forward_backward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* 
     p.segments = 2;
     p.a[1] = operand(w.dup, w.ldh, dt);
     p.b[1] = by_up;
-    l.product(p, true);
+    l.product(p, kBeforeLeavesB);
   }
   if (weights) {
     if (!given_x && by_x && t > 0) l.dequantize(dt, t, dim, operand(&kept->x8), w.x, w.ldx);
@@ -475,7 +474,7 @@ int muon_feed_forward_backward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* 
     if (dw_gate) list[n++] = plain(hidden, dim, t, operand(w.dgate, w.ldh, dt, true), turned(ox), odg.data, odg.ld, dt);
     if (dw_up) list[n++] = plain(hidden, dim, t, operand(w.dup, w.ldh, dt, true), turned(ox), odu.data, odu.ld, dt);
     if (dw_down) list[n++] = plain(dim, hidden, t, turned(ody), operand(w.h, w.ldh, dt, true), odd.data, odd.ld, dt);
-    l.products(list, n, kMaxProducts);
+    l.products(list, n, kMaxProducts, t > 0 ? kBeforeSameCall : kBeforeAny);
   }
   l.copies(c.out, c.outs);
   return l.rc;
@@ -502,7 +501,7 @@ int muon_linear_blocks_forward(muon_ctx_t* ctx, const muon_linear_blocks_desc_t*
   const muon_rows_t oy = c.give(y, t, out, w.y, kTypeBf16);
   l.copies(c.in, c.ins);
   l.quantize(kTypeBf16, t, dim, x->data, x->ld, operand(x8));
-  l.product(plain(t, out, dim, operand(x8), ow, oy.data, oy.ld, kTypeBf16), true);
+  l.product(plain(t, out, dim, operand(x8), ow, oy.data, oy.ld, kTypeBf16), kBeforeLeavesB);
   l.copies(c.out, c.outs);
   return l.rc;
 }
@@ -552,11 +551,11 @@ int muon_linear_blocks_backward(muon_ctx_t* ctx, const muon_linear_blocks_desc_t
   if (t > 0) l.copies(c.in, c.ins);
   if (rw) {
     l.quantize(kTypeBf16, t, out, dy->data, dy->ld, operand(&w.dy8));
-    l.product(plain(t, dim, out, operand(&w.dy8), ow, odx.data, odx.ld, kTypeBf16), true);
+    l.product(plain(t, dim, out, operand(&w.dy8), ow, odx.data, odx.ld, kTypeBf16), kBeforeLeavesB);
   }
   if (dw) {
     if (rx) l.dequantize(kTypeBf16, t, dim, operand(x8), w.x, w.ldx);
-    l.product(plain(out, dim, t, ody, operand(w.x, w.ldx, kTypeBf16, true), odw.data, odw.ld, kTypeBf16));
+    l.product(plain(out, dim, t, ody, operand(w.x, w.ldx, kTypeBf16, true), odw.data, odw.ld, kTypeBf16), rx ? kBeforeSameCall : kBeforeAny);
   }
   l.copies(c.out, c.outs);
   return l.rc;

@@ -473,8 +473,9 @@ bool product_few_takes(const Product& p, int sms) {
   return p.m <= kFewRows && !p.a[0].mn_major && plan_few(p, sms).clocks < 0.85 * products_tc_clocks(&p, 1, sms) + 1800;
 }
 
-int launch_product_few(muon_ctx* ctx, const Product& q, int sms, bool follows, cudaStream_t st) {
+int launch_product_few(muon_ctx* ctx, const Product& q, int sms, Before before, cudaStream_t st) {
   if (!ctx->tmap_encode) return MUON_ERR_CUDA;
+  const bool follows = before == kBeforeLeavesB;
   FewArgs L = {};
   const Epilogue& e = q.e;
   const bool eight = q.a[0].type == kTypeE4m3, wmn = q.b[0].mn_major, codes = e.kind != kPlain && e.gate_up_type == kTypeE4m3;

@@ -73,14 +73,17 @@ int launch_copies(const CopyTask* list, int count, int sms, cudaStream_t st);
 
 // The tensor-core engine takes a list of products with operands of one type and one order in memory, if TMA can address all tensors.
 bool products_tc_take(const Product* p, int count);
-int launch_products_tc(muon_ctx* ctx, const Product* p, int count, cudaStream_t st);
+// What the launch right before this one in the stream is: anything; one of the same call, so this one may be brought up while that one ends; or one of
+// the same call that does not write B, which may be read before that one has ended.
+enum Before { kBeforeAny, kBeforeSameCall, kBeforeLeavesB };
+int launch_products_tc(muon_ctx* ctx, const Product* p, int count, Before before, cudaStream_t st);
 // About how many clocks they take there, from the rounds of tiles.
 double products_tc_clocks(const Product* p, int count, int sms);
 // Products of few rows, whose time is that of reading B, have a kernel of their own, which takes them where its blocks are expected to be done sooner.
-// follows: the launch before this one in the stream is of the same call and does not write B, so this one may begin before that one has ended.
 constexpr int kFewRows = 1024;
 bool product_few_takes(const Product& p, int sms);
-int launch_product_few(muon_ctx* ctx, const Product& p, int sms, bool follows, cudaStream_t st);
+// It begins early after kBeforeLeavesB alone: it asks for B at once.
+int launch_product_few(muon_ctx* ctx, const Product& p, int sms, Before before, cudaStream_t st);
 // Operands of one type.  siblings: products of about this size that a call may launch together, of which `count` are wanted now.
 int launch_products_simt(const Product* p, int count, int siblings, int sms, cudaStream_t st);
 
