@@ -403,7 +403,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<EIGHT>::thread
       __syncwarp();
       elected(true, [&] { tc_commit_pair(drain_bar); });       // arrives in both CTAs once everything issued above has finished
     }
-    if (lane == 0 && !mbar_wait(drain_bar, 0, abort_flag, false, WAIT_CYCLES / 8)) atomicExch(L.status, 35);
   } else if (EIGHT && warp == 2 + kEpiWarps) {
     // ------------------------------------------------------------------ scales
     if constexpr (EIGHT) {
@@ -609,6 +608,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<EIGHT>::thread
   }
   tc_fence_before();
   __syncthreads();
+  // The CTA's last tile is done or given up, so what the leader issued is about to have finished, too.  Waited for from the launch's beginning on, as warp 1
+  // of the leader's peer could, this would be a wait for the whole launch, which may take longer than any limit meant for a part of it.
+  if (warp == 1) {
+    if (lane == 0 && !mbar_wait(drain_bar, 0, abort_flag, false, WAIT_CYCLES / 8)) atomicExch(L.status, 35);
+    __syncwarp();
+  }
   cluster_sync_all();            // neither CTA retires while its peer may still signal its barriers or read its tiles
   tc_fence_after();
   if (warp == 1) {
