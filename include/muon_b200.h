@@ -550,7 +550,7 @@ int muon_dequantize(muon_ctx_t* ctx, int32_t dtype, int64_t rows, int64_t cols, 
 typedef struct {
   int32_t dtype;                 /* of all tensors.  MUON_DTYPE_BF16: tensor cores when every pointer is 16-byte aligned and every ld a multiple */
                                  /* of 8; where dim or hidden is not and the products are large, by way of copies in the scratch; otherwise,   */
-                                 /* and for MUON_DTYPE_FP32, CUDA cores                                                                        */
+                                 /* for sums over more than 2^20 of dim or hidden, and for MUON_DTYPE_FP32, CUDA cores                         */
   int32_t activation, keep;
   int32_t tokens, dim, hidden;
 } muon_feed_forward_desc_t;
@@ -570,7 +570,8 @@ int muon_feed_forward_forward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* d
 
 /* From what was kept (x itself with KEEP_FULL, where x8 holds it otherwise and x is NULL):  dh = dy w_down,  dg = dh u act'(g),  du = dh act(g),
  *   dx = dg w_gate + du w_up,  dw_gate = dg^T x,  dw_up = du^T x,  dw_down = dy^T (act(g) u)
- * dh stays fp32; dg, du and act(g) u are rounded once to dtype.  Results that are NULL are not formed.  With no tokens dw_* are zeros, and what has
+ * dh stays fp32; dg, du and act(g) u are rounded once to dtype.  Sums over more than 2^18 tokens are formed in parts of as many, which are added in fp32:
+ * the tensor cores cut a sum's last bits instead of rounding them.  Results that are NULL are not formed.  With no tokens dw_* are zeros, and what has
  * rows of tokens may be NULL.  Of this call and those beside it: no result may lie over an input, another result or the scratch. */
 int muon_feed_forward_backward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* desc, const muon_rows_t* dy, const muon_rows_t* x, const muon_rows_t* w_gate,
                                const muon_rows_t* w_up, const muon_rows_t* w_down, const muon_feed_forward_kept_t* kept, const muon_rows_t* dx,
@@ -590,7 +591,8 @@ int muon_linear_blocks_forward(muon_ctx_t* ctx, const muon_linear_blocks_desc_t*
                                const muon_blocks_t* x8, void* workspace, size_t workspace_bytes, void* stream);
 
 /* dx = Q(dy) w8 with Q(dy) in blocks of 1 x 128, and dw = dy^T x8 with dy as it is (bf16).  dx or dw may be NULL.  Rows whose distance is a multiple of
- * 16 bytes and begin on 16 bytes go to the tensor cores; of dim or out that 16 or 8 does not divide, large products by way of copies in the scratch. */
+ * 16 bytes and begin on 16 bytes go to the tensor cores; of dim or out that 16 or 8 does not divide, large products by way of copies in the scratch.
+ * Long sums are formed as above. */
 int muon_linear_blocks_backward(muon_ctx_t* ctx, const muon_linear_blocks_desc_t* desc, const muon_rows_t* dy, const muon_blocks_t* x8, const muon_blocks_t* w8,
                               const muon_rows_t* dx, const muon_rows_t* dw, void* workspace, size_t workspace_bytes, void* stream);
 

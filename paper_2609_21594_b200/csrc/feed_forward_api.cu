@@ -1,5 +1,7 @@
 // extern "C" entry points of the gated feed-forward block, of activations in 8 bits and of the 8-bit linear layer: argument validation, layout
 // of the scratch, and the list of products that each call is.
+#include <algorithm>
+
 #include "layer_checks.h"
 #include "product_ops.h"
 
@@ -84,8 +86,23 @@ struct Launches {
       part[tc][count[tc]++] = p[i];
     }
     if (rc == MUON_OK && count[1] == 1 && product_few_takes(part[1][0], sms)) this->count(launch_product_few(ctx, part[1][0], sms, before, st));
-    else if (rc == MUON_OK && count[1] > 0) this->count(launch_products_tc(ctx, part[1], count[1], before, st));
+    else if (count[1] > 0) products_tc(part[1], count[1], before);
     if (rc == MUON_OK && count[0] > 0) this->count(launch_products_simt(part[0], count[0], siblings, sms, st));
+  }
+  // Sums over more tokens than kLongestSum one part after the other, a launch each.
+  void products_tc(Product* p, int n, Before before) {
+    const int64_t k = p[0].k, step = p[0].e.sums ? kLongestSum : k;
+    for (int64_t k0 = 0; k0 < k && rc == MUON_OK; k0 += step) {
+      for (int i = 0; i < n; ++i) {
+        p[i].k = int32_t(std::min(step, k - k0));
+        p[i].e.add = k0 > 0;
+        p[i].e.hold = k0 + step < k;
+      }
+      this->count(launch_products_tc(ctx, p, n, k0 > 0 ? kBeforeSameCall : before, st));
+      if (k0 + step < k)
+        for (int i = 0; i < n; ++i)
+          for (Operand* o : {&p[i].a[0], &p[i].b[0]}) o->data = static_cast<const char*>(o->data) + step * o->ld * size_of_type(o->type);
+    }
   }
   void product(const Product& p, Before before = kBeforeAny) { products(&p, 1, 1, before); }
   void copies(const CopyTask* list, int n) {
@@ -113,6 +130,22 @@ int check_scratch(const void* workspace, size_t have, size_t need) {
   if (need == 0) return MUON_OK;
   if (!workspace || have < need) return MUON_ERR_WORKSPACE_TOO_SMALL;
   return aligned_to(workspace, 256) ? MUON_OK : MUON_ERR_INVALID_ARG;
+}
+
+// Where the parts of the sum over `tokens` meet that a gradient of rows x cols is.
+struct Sums {
+  float* data;
+  int64_t ld;
+};
+Sums sums_of(Scratch* s, int64_t tokens, int64_t rows, int64_t cols, int type) {
+  if (tokens <= kLongestSum || type != kTypeBf16) return {nullptr, 0};
+  const int64_t ld = up_to(cols, 64);
+  return {static_cast<float*>(s->take(rows * ld * 4)), ld};
+}
+Product with(Product p, const Sums& s) {
+  p.e.sums = s.data;
+  p.e.ld_sums = s.ld;
+  return p;
 }
 
 // Operands and results that TMA cannot address and that have room in the scratch are copied there and back.
@@ -214,6 +247,7 @@ struct BackwardScratch {
   int64_t ldh, ldx;
   void *dgate, *dup, *h, *x;
   void *dy, *given_x, *w_gate, *w_up, *w_down, *gate, *up, *dx, *dw_gate, *dw_up, *dw_down;      // copies
+  Sums sum_gate, sum_up, sum_down;
 };
 BackwardScratch backward_scratch(const muon_feed_forward_desc_t* d, Scratch* s) {
   BackwardScratch r = {};
@@ -238,6 +272,9 @@ BackwardScratch backward_scratch(const muon_feed_forward_desc_t* d, Scratch* s) 
   r.dw_down = room(s, odd.hidden, d->dim, d->hidden, d->dtype);
   r.gate = room(s, odd.hidden && full, t, d->hidden, d->dtype);
   r.up = room(s, odd.hidden && full, t, d->hidden, d->dtype);
+  r.sum_gate = sums_of(s, t, d->hidden, d->dim, d->dtype);
+  r.sum_up = sums_of(s, t, d->hidden, d->dim, d->dtype);
+  r.sum_down = sums_of(s, t, d->dim, d->hidden, d->dtype);
   return r;
 }
 
@@ -251,6 +288,7 @@ struct LinearScratch {
   void* x;
   int64_t ldx;
   void *w8, *y, *dy, *dx, *dw;   // copies
+  Sums sum;                      // of dw
 };
 LinearScratch linear_scratch(const muon_linear_blocks_desc_t* d, bool backward, Scratch* s) {
   LinearScratch r = {};
@@ -270,6 +308,7 @@ LinearScratch linear_scratch(const muon_linear_blocks_desc_t* d, bool backward, 
   r.dy8.scales = static_cast<uint8_t*>(s->take(d->tokens * r.dy8.lds));
   r.ldx = up_to(d->dim, 8);
   r.x = s->take(d->tokens * r.ldx * 2);
+  r.sum = sums_of(s, d->tokens, d->out, d->dim, kTypeBf16);
   return r;
 }
 
@@ -471,9 +510,9 @@ int muon_feed_forward_backward(muon_ctx_t* ctx, const muon_feed_forward_desc_t* 
     if (!given_x && by_x && t > 0) l.dequantize(dt, t, dim, operand(&kept->x8), w.x, w.ldx);
     Product list[kMaxProducts];
     int n = 0;
-    if (dw_gate) list[n++] = plain(hidden, dim, t, operand(w.dgate, w.ldh, dt, true), turned(ox), odg.data, odg.ld, dt);
-    if (dw_up) list[n++] = plain(hidden, dim, t, operand(w.dup, w.ldh, dt, true), turned(ox), odu.data, odu.ld, dt);
-    if (dw_down) list[n++] = plain(dim, hidden, t, turned(ody), operand(w.h, w.ldh, dt, true), odd.data, odd.ld, dt);
+    if (dw_gate) list[n++] = with(plain(hidden, dim, t, operand(w.dgate, w.ldh, dt, true), turned(ox), odg.data, odg.ld, dt), w.sum_gate);
+    if (dw_up) list[n++] = with(plain(hidden, dim, t, operand(w.dup, w.ldh, dt, true), turned(ox), odu.data, odu.ld, dt), w.sum_up);
+    if (dw_down) list[n++] = with(plain(dim, hidden, t, turned(ody), operand(w.h, w.ldh, dt, true), odd.data, odd.ld, dt), w.sum_down);
     l.products(list, n, kMaxProducts, t > 0 ? kBeforeSameCall : kBeforeAny);
   }
   l.copies(c.out, c.outs);
@@ -555,7 +594,8 @@ int muon_linear_blocks_backward(muon_ctx_t* ctx, const muon_linear_blocks_desc_t
   }
   if (dw) {
     if (rx) l.dequantize(kTypeBf16, t, dim, operand(x8), w.x, w.ldx);
-    l.product(plain(out, dim, t, ody, operand(w.x, w.ldx, kTypeBf16, true), odw.data, odw.ld, kTypeBf16), rx ? kBeforeSameCall : kBeforeAny);
+    l.product(with(plain(out, dim, t, ody, operand(w.x, w.ldx, kTypeBf16, true), odw.data, odw.ld, kTypeBf16), w.sum),
+              rx ? kBeforeSameCall : kBeforeAny);
   }
   l.copies(c.out, c.outs);
   return l.rc;

@@ -42,6 +42,9 @@ struct Epilogue {
   void* up;                    // kGated: u or null; kGrad: du
   int64_t ld_gate, ld_up;
   Operand in_gate, in_up;      // kGrad: g and u.  kGated with e4m3: where codes and scales of g and u go
+  float* sums;                 // kPlain with a sum longer than kLongestSum: fp32 [m][ld_sums], where its parts meet; else null
+  int64_t ld_sums;             // a multiple of 64
+  int32_t add, hold;           // of a part: earlier ones are in `sums`; later ones follow, so that it stays there and C is not written
 };
 
 struct Product {
@@ -52,6 +55,12 @@ struct Product {
 };
 
 constexpr int kMaxProducts = 3;   // of a launch
+
+// The tensor cores cut a sum to fp32 where others round it, so a sum of many terms ends up too small: against 64 bits, of random terms, by 0.0012 of the
+// result (norm) after 2^20 of them, 0.0049 after 2^22, 0.074 after 2^26, where the rounding to bf16 is 0.0016.  Sums over tokens, which may be that many,
+// are therefore formed in parts of kLongestSum (0.0003), which are added in fp32, rounded.  Sums over dim, hidden and out have no such parts and go to
+// the CUDA cores from kMostSum on.  No tile takes longer than 2^15 k-blocks of 560 to 800 clocks, a hundredth of what its waits are given.
+constexpr int32_t kLongestSum = 1 << 18, kMostSum = 1 << 20;
 
 // What TMA asks of rows of `ld` elements: the first, and the distance between two, on 16 bytes.
 inline int size_of_type(int type) { return type == kTypeFp32 ? 4 : type == kTypeBf16 ? 2 : 1; }

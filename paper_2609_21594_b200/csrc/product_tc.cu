@@ -60,6 +60,8 @@ struct TcProduct {
   int64_t ld[3];
   const __nv_bfloat16* in[2];                  // g, u
   int64_t ld_in[2];
+  float* sums;                                 // where the parts of a long sum meet, or null
+  int64_t ld_sums;
   Scales sa, sb;
   int32_t m, n, kblocks, segments;             // kblocks: of a segment
   int32_t tiles_m, tiles_n, tile_begin;
@@ -70,6 +72,7 @@ struct TcProducts {
   int32_t count, total_tiles;
   int32_t half;                                // columns of B per CTA: 128 or 64
   int32_t activation, keep;                    // keep: g and u are written
+  int32_t add, hold;                           // of a part of a long sum, see Epilogue
   Operand gate, up;                            // 8-bit g and u
   int32_t codes_wide;                          // their rows take 16-byte accesses
   int32_t sectors;                             // all bf16 rows begin on a 32-byte sector
@@ -473,6 +476,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Shape<EIGHT>::thread
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(map_to_cta(shared_bar, 0));
           }
+          if constexpr (A_MN) {
+            if (p.sums && row < p.m && col < p.n) {
+              float4* s = reinterpret_cast<float4*>(p.sums + row * p.ld_sums + col);
+              if (L.add) {
+#pragma unroll
+                for (int q = 0; q < 16; ++q) {
+                  const float4 x = s[q];
+                  v[4 * q] = __float_as_uint(__uint_as_float(v[4 * q]) + x.x);
+                  v[4 * q + 1] = __float_as_uint(__uint_as_float(v[4 * q + 1]) + x.y);
+                  v[4 * q + 2] = __float_as_uint(__uint_as_float(v[4 * q + 2]) + x.z);
+                  v[4 * q + 3] = __float_as_uint(__uint_as_float(v[4 * q + 3]) + x.w);
+                }
+              }
+              if (L.hold) {
+#pragma unroll
+                for (int q = 0; q < 16; ++q)
+                  s[q] = make_float4(__uint_as_float(v[4 * q]), __uint_as_float(v[4 * q + 1]), __uint_as_float(v[4 * q + 2]), __uint_as_float(v[4 * q + 3]));
+              }
+            }
+            if (L.hold) continue;
+          }
 #pragma unroll
           for (int k = 0; k < 32; ++k) w[k] = pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
           if (row < p.m) {
@@ -676,6 +700,7 @@ bool products_tc_take(const Product* list, int count) {
     const Product& p = list[i];
     const Epilogue& e = p.e;
     const int type = p.a[0].type, ns = e.kind == kGated ? 2 : p.segments;
+    if (!e.sums && int64_t(p.k) * p.segments > kMostSum) return false;
     if (p.m < 1 || p.n < 1 || p.k < 1 || e.type != kTypeBf16 || e.kind != list[0].e.kind || type != list[0].a[0].type) return false;
     if (type != kTypeBf16 && type != kTypeE4m3) return false;
     for (int s = 0; s < ns; ++s) {
@@ -714,6 +739,8 @@ int launch_products_tc(muon_ctx* ctx, const Product* list, int count, Before bef
   L.half = plan_pairs(list, count, sms).half;
   L.activation = e0.activation;
   L.keep = e0.kind == kGated && e0.gate;
+  L.add = e0.add;
+  L.hold = e0.hold;
   L.gate = e0.in_gate;
   L.up = e0.in_up;
   L.codes_wide = codes && addressable(L.gate.data, L.gate.ld, kTypeE4m3) && addressable(L.up.data, L.up.ld, kTypeE4m3);
@@ -750,6 +777,8 @@ int launch_products_tc(muon_ctx* ctx, const Product* list, int count, Before bef
       rows(const_cast<__nv_bfloat16**>(&p.in[0]), &p.ld_in[0], q.e.in_gate.data, q.e.in_gate.ld);
       rows(const_cast<__nv_bfloat16**>(&p.in[1]), &p.ld_in[1], q.e.in_up.data, q.e.in_up.ld);
     }
+    p.sums = q.e.sums;
+    p.ld_sums = q.e.ld_sums;
     if (eight) {
       p.sa = scales_of(q.a[0], q.m);
       p.sb = scales_of(q.b[0], q.n);

@@ -31,3 +31,69 @@ def test_a_launch_of_half_a_second_reports_no_expired_wait():
     assert float((y[rows].double() - value).norm() / value.norm()) < 2 * ref.half(torch.bfloat16)
     del x, w, y
     torch.cuda.empty_cache()
+
+
+def squares(a):
+    return float((a * a).sum())
+
+
+def check_long_sum(got, parts):
+    """`parts`: pairs of 64-bit factors, a few tokens at a time.  Off by the result's rounding and little else: sums that are cut instead of rounded may add a
+    fifth of it to the norm's square (2^18 terms of random sign: a twentieth), where those of 2^21 terms in one piece add twice of it."""
+    value = sum(a().T @ b() for a, b in parts)
+    alone = squares(value.to(got.dtype).double() - value)
+    assert squares(got.double() - value) <= 1.2 * alone
+
+
+@pytest.mark.parametrize("keep", ["full", "8bit"])
+@pytest.mark.parametrize("tokens,dim,hidden", [((1 << 21) + 77, 64, 136), ((1 << 21) + 1, 50, 72), (1 << 20, 72, 264)])
+def test_sums_over_many_tokens(tokens, dim, hidden, keep):
+    from paper_2609_21594_b200 import functional as F
+
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x, dy = (torch.empty((tokens, dim), device="cuda").normal_(0, 1, generator=g).bfloat16() for _ in range(2))
+    w = [torch.empty(s, device="cuda").normal_(0, s[1] ** -0.5, generator=g).bfloat16() for s in ((hidden, dim), (hidden, dim), (dim, hidden))]
+    _, kept = F.feed_forward_forward(x, *w, "silu", keep)
+    _, *got = F.feed_forward_backward(dy, x if keep == "full" else None, *w, kept)
+
+    def piece(i):                                            # (dg, du, h, x, dy) of some tokens, rounded as documented
+        at = slice(i, i + (1 << 18))
+        xi, gi, ui = (x[at].double(), kept[0][at].double(), kept[1][at].double()) if keep == "full" else (
+            ref.unpack(kept[k][at].float(), kept[k + 1][at], 1) for k in (0, 2, 4))
+        a, slope = ref.act_and_slope(gi, "silu")
+        dh = dy[at].double() @ w[2].double()
+        return [t.bfloat16().double() for t in (dh * ui * slope, dh * a, a * ui)] + [xi.bfloat16().double(), dy[at].double()]
+
+    starts = range(0, tokens, 1 << 18)
+    for k, (a, b) in enumerate(((0, 3), (1, 3), (4, 2))):
+        check_long_sum(got[k], [(lambda i=i: piece(i)[a], lambda i=i: piece(i)[b]) for i in starts])
+        need = [False] + [i == k for i in range(3)]
+        assert torch.equal(F.feed_forward_backward(dy, x if keep == "full" else None, *w, kept, "silu", need)[k + 1], got[k])
+    F.synchronize_and_check()
+
+
+def test_sums_over_many_tokens_of_the_8_bit_layer():
+    from paper_2609_21594_b200 import functional as F
+
+    tokens, dim, out = (1 << 21) + 77, 64, 136
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x, dy = (torch.empty((tokens, n), device="cuda").normal_(0, 1, generator=g).bfloat16() for n in (dim, out))
+    w8 = F.quantize(torch.empty((out, dim), device="cuda").normal_(0, 1, generator=g), 128)
+    _, *x8 = F.linear_8bit_forward(x, *w8)
+    _, dw = F.linear_8bit_backward(dy, *x8, *w8)
+    starts = range(0, tokens, 1 << 18)
+    cut = lambda i: slice(i, i + (1 << 18))  # noqa: E731
+    check_long_sum(dw, [(lambda i=i: dy[cut(i)].double(), lambda i=i: ref.unpack(x8[0][cut(i)].float(), x8[1][cut(i)], 1)) for i in starts])
+
+
+def test_a_row_too_long_for_the_tensor_cores():
+    """dim = 2^21: sums that the tensor cores would cut by as much as the result's rounding, on CUDA cores."""
+    from paper_2609_21594_b200 import functional as F
+
+    n = 1 << 21
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x, wg, wu = (torch.empty((r, n), device="cuda").normal_(0, s, generator=g).bfloat16() for r, s in ((40, 1), (64, n ** -0.5), (64, n ** -0.5)))
+    wd = torch.zeros((n, 64), dtype=torch.bfloat16, device="cuda")
+    _, (gate, up) = F.feed_forward_forward(x, wg, wu, wd)
+    for got, w in ((gate, wg), (up, wu)):
+        check_long_sum(got, [(lambda i=i: x[:, i:i + (1 << 18)].double().T, lambda i=i, w=w: w[:, i:i + (1 << 18)].double().T) for i in range(0, n, 1 << 18)])
