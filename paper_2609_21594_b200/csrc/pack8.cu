@@ -6,6 +6,7 @@
 #include <cuda_fp8.h>
 
 #include "product_ops.h"
+#include "words.h"
 
 namespace muon {
 namespace {
@@ -18,20 +19,23 @@ __device__ __forceinline__ float2 values2(uint32_t pair) {
   return __half22float2(__half2(h));
 }
 
-// Up to N consecutive elements of a row, by 16 bytes; those from `left` on count as zeros.  WORDS: bf16 that begins anywhere, moved out of aligned
-// words, of which none may end behind `last`.
+// Reads what no launch writes while this one runs.
+struct ReadOnly {
+  template <typename T> __device__ __forceinline__ T operator()(const T* p) const { return __ldg(p); }
+};
+
+// Up to N consecutive elements of a row, by 16 bytes; those from `left` on count as zeros.  WORDS: bf16 that begins anywhere in the row that begins at `first`,
+// moved out of aligned words.
 template <bool WORDS, typename T, int N>
-__device__ __forceinline__ void load_run(const T* p, int left, const T* last, float (&v)[N]) {
+__device__ __forceinline__ void load_run(const T* p, int left, const T* first, float (&v)[N]) {
   if constexpr (WORDS) {
-    const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p) >> 1) & 1u;
-    const uint32_t* q = reinterpret_cast<const uint32_t*>(p - off);
-    if (left >= N && reinterpret_cast<const T*>(q + N / 2 + 1) <= last) {
+    if (left >= N) {
       uint32_t w[N / 2 + 1];
-#pragma unroll
-      for (int i = 0; i <= N / 2; ++i) w[i] = __ldg(q + i);
+      const uint32_t off = words_of_run<uint16_t, N>(reinterpret_cast<const char*>(p), reinterpret_cast<const char*>(first), reinterpret_cast<const char*>(p + left),
+                                                     w, ReadOnly());
 #pragma unroll
       for (int i = 0; i < N / 2; ++i) {
-        const uint32_t x = __funnelshift_r(w[i], w[i + 1], 16 * off);
+        const uint32_t x = __funnelshift_r(w[i], w[i + 1], 8 * off);
         v[2 * i] = __uint_as_float(x << 16);
         v[2 * i + 1] = __uint_as_float(x & 0xffff0000u);
       }
@@ -120,7 +124,7 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const T* x, int
   const uint32_t blk = uint32_t(block - row * per_row);
   const int col = int(blk) * kBlock + sub * 16;
   float v[16];
-  load_run<WORDS>(x + row * ldx + col, row < rows ? cols - col : 0, x + (rows - 1) * ldx + cols, v);
+  load_run<WORDS>(x + row * ldx + col, row < rows ? cols - col : 0, x + row * ldx, v);
   bool odd;
   uint32_t top = finite_top(v, &odd);
 #pragma unroll
@@ -191,7 +195,7 @@ __global__ void __launch_bounds__(kSquareThreads, 3) quantize_squares_kernel(con
     const int64_t row = row0 + kStride * i;
     const int left = row < rows ? cols - col : 0;
     if constexpr (WIDE) {
-      load_run<false>(x + row * ldx + col, left, x, v[i]);
+      load_run<false>(x + row * ldx + col, left, x + row * ldx, v[i]);
     } else {
 #pragma unroll
       for (int j = 0; j < kPer; ++j) v[i][j] = 32 * j < left ? float(x[row * ldx + col + 32 * j]) : 0.f;
@@ -279,15 +283,14 @@ __global__ void __launch_bounds__(kThreads) dequantize_any_kernel(const uint8_t*
   const bool whole = g > 0 && count == 8;
   const uint8_t* s = scales + (row >> row_shift) * lds;
   const uint32_t first = __ldg(s + (col >> 7)), second = __ldg(s + ((col + count - 1) >> 7));
+  const char* begin = reinterpret_cast<const char*>(codes + row * ldc);
   const uint8_t* p = codes + row * ldc + col;
-  const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 3u;
-  const uint8_t* base = p - off;
   uint32_t w[2] = {0, 0};
-  if (whole && base >= codes && base + 12 <= codes + (rows - 1) * ldc + cols) {
-    const uint32_t* q = reinterpret_cast<const uint32_t*>(base);
-    const uint32_t a = __ldg(q), b = __ldg(q + 1), c = __ldg(q + 2);
-    w[0] = __funnelshift_r(a, b, 8 * off);
-    w[1] = __funnelshift_r(b, c, 8 * off);
+  if (whole) {
+    uint32_t x[3];
+    const uint32_t off = words_of_run<uint8_t, 8>(reinterpret_cast<const char*>(p), begin, begin + cols, x, ReadOnly());
+    w[0] = __funnelshift_r(x[0], x[1], 8 * off);
+    w[1] = __funnelshift_r(x[1], x[2], 8 * off);
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
@@ -315,24 +318,15 @@ struct CopyList {
   int32_t count;
 };
 // A warp moves a run of kRun bytes of a row: whole words of the destination, each out of the two words of the source that hold it, and what is left at the
-// ends by elements.
+// ends by elements.  [first, last): the row that the run is of.
 constexpr int kRun = 1024;
 template <typename E>
 __device__ __forceinline__ void copy_run(const char* from, char* to, int bytes, const char* first, const char* last, int lane) {
   const int head = min(int((4 - (reinterpret_cast<uintptr_t>(to) & 3)) & 3), bytes), words = (bytes - head) / 4, tail = head + words * 4;
-  const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(from + head)) & 3u;
   for (int i = lane; i < words; i += 32) {
-    const char* p = from + head + 4 * i;
-    uint32_t w = 0;
-    if (off == 0) {
-      w = *reinterpret_cast<const uint32_t*>(p);
-    } else if (p - off >= first && p - off + 8 <= last) {
-      w = __funnelshift_r(*reinterpret_cast<const uint32_t*>(p - off), *reinterpret_cast<const uint32_t*>(p - off + 4), 8 * off);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 4 / int(sizeof(E)); ++k) w |= uint32_t(reinterpret_cast<const E*>(p)[k]) << (8 * sizeof(E) * k);
-    }
-    *reinterpret_cast<uint32_t*>(to + head + 4 * i) = w;
+    uint32_t w[2];
+    const uint32_t off = words_of_run<E, 4 / int(sizeof(E))>(from + head + 4 * i, first, last, w, ReadOnly());
+    *reinterpret_cast<uint32_t*>(to + head + 4 * i) = __funnelshift_r(w[0], w[1], 8 * off);
   }
   const int at = lane * int(sizeof(E));
   if (at < head) *reinterpret_cast<E*>(to + at) = *reinterpret_cast<const E*>(from + at);
@@ -346,10 +340,10 @@ __global__ void __launch_bounds__(kThreads) copy_rows_kernel(const __grid_consta
   const CopyTask& t = L.task[which];
   const int64_t per_row = (t.bytes + kRun - 1) / kRun, i = warp - L.begin[which], row = i / per_row, at = (i - row * per_row) * kRun;
   if (row >= t.rows) return;
-  const char* first = static_cast<const char*>(t.from);
-  const char* from = first + row * t.ld_from + at;
+  const char* first = static_cast<const char*>(t.from) + row * t.ld_from;
+  const char* from = first + at;
   char* to = static_cast<char*>(t.to) + row * t.ld_to + at;
-  const char* last = first + (t.rows - 1) * t.ld_from + t.bytes;
+  const char* last = first + t.bytes;
   const int bytes = int(min(int64_t(kRun), t.bytes - at));
   if (t.unit == 1) copy_run<uint8_t>(from, to, bytes, first, last, threadIdx.x & 31);
   else copy_run<uint16_t>(from, to, bytes, first, last, threadIdx.x & 31);
