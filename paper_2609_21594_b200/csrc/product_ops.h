@@ -124,7 +124,10 @@ struct Activation {
   float k, c;
 };
 __device__ __forceinline__ Activation activation_of(int kind) { return kind == MUON_ACTIVATION_GELU ? Activation{1.5957691216057308f, 0.044715f} : Activation{1.f, 0.f}; }
-// FAST: the exponential and the reciprocal of the special-function unit (2^-21 relative), for results that are rounded to bf16.
+// FAST: the exponential and the reciprocal of the special-function unit, for results that are rounded to bf16.  The exponential's error grows with its
+// argument (2 + 1.2 |w| units of 2^-23), and so does that of w's own roundings in it: s is off by at most (6 + 4 |w|) 2^-23 of its value, 2^-14 at w = -87, in
+// both forms; the slope by as much of each of its two parts.  Below -87, where s is less than the least normal number, it may count as 0: act(g) is then
+// off by less than 89 * 2^-126.
 template <bool FAST>
 __device__ __forceinline__ void activate(const Activation& f, float g, float* a, float* slope) {
   const float g2 = fminf(g * g, 1e12f);       // beyond, s is 0 or 1, and 0 times w' has to stay 0
