@@ -538,7 +538,8 @@ int muon_dequantize(muon_ctx_t* ctx, int32_t dtype, int64_t rows, int64_t cols, 
 /* Gated feed-forward block on `tokens` rows of x:
  *   g = x w_gate^T,  u = x w_up^T,  h = act(g) u,  y = h w_down^T          w_gate, w_up: [hidden][dim];  w_down: [dim][hidden]
  * act(g) = g s(w(g)) with the logistic function s:  SILU  w = g;  GELU  w = 2 sqrt(2 / pi) (g + 0.044715 g^3)  (the tanh form).
- * Sums are fp32; h is formed from the sums and rounded once to dtype.  What the backward pass needs of g and u is kept
+ * Sums are fp32; h is formed from the sums and rounded once to dtype.  The tensor cores take bf16 alone: fp32 is half as fast as a library's products
+ * where there is much to multiply.  What the backward pass needs of g and u is kept
  *   KEEP_NONE  not at all (inference)
  *   KEEP_FULL  in dtype
  *   KEEP_8BIT  in 8 bits with block_rows = 1, and x with them: (dim + 2 hidden) bytes a token and their scales; g and u are rounded from the fp32 sums */
