@@ -97,3 +97,39 @@ def test_a_row_too_long_for_the_tensor_cores():
     _, (gate, up) = F.feed_forward_forward(x, wg, wu, wd)
     for got, w in ((gate, wg), (up, wu)):
         check_long_sum(got, [(lambda i=i: x[:, i:i + (1 << 18)].double().T, lambda i=i, w=w: w[:, i:i + (1 << 18)].double().T) for i in range(0, n, 1 << 18)])
+
+
+def test_long_sums_in_a_graph_on_another_stream_and_off_the_alignment():
+    from paper_2609_21594_b200 import functional as F
+
+    tokens, dim, hidden = (1 << 19) + 130, 40, 56
+    g = torch.Generator(device="cuda").manual_seed(1)
+    r = lambda *s: torch.empty(s, device="cuda").normal_(0, 1, generator=g).bfloat16()  # noqa: E731
+    inputs = [[r(tokens, dim), r(tokens, dim), r(tokens, hidden), r(tokens, hidden)] for _ in range(2)]          # dy, x, gate, up
+    w = [r(hidden, dim), r(hidden, dim), r(dim, hidden)]
+    call = lambda dy, x, gate, up: F.feed_forward_backward(dy, x, *w, [gate, up])  # noqa: E731
+    wants = [call(*i) for i in inputs]
+    given = [t.clone() for t in inputs[0]]
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        call(*given)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        out = call(*given)
+    for k in (1, 0, 1):
+        for to, t in zip(given, inputs[k]):
+            to.copy_(t)
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(out, wants[k]))
+    # rows that begin one element off: CUDA cores, whose sums have no parts
+    wide = [torch.cat([t[:, :1], t, t[:, :1].expand(-1, 8 - 1)], 1)[:, 1:1 + t.shape[1]] for t in inputs[0]]
+    starts = range(0, tokens, 1 << 18)
+    for a, b in zip(call(*wide)[1:], wants[0][1:]):
+        assert float((a.double() - b.double()).norm() / b.double().norm()) < ref.half(torch.bfloat16)      # both are rounded once, most of them alike
+    dy = inputs[0][0]
+    cut = lambda t, i: t[i:i + (1 << 18)].double()  # noqa: E731
+    products = [(lambda i=i: cut(dy, i), lambda i=i: (ref.act(cut(inputs[0][2], i), "silu") * cut(inputs[0][3], i)).bfloat16().double()) for i in starts]
+    check_long_sum(wants[0][3], products)
+    check_long_sum(call(*wide)[3], products)
+    F.synchronize_and_check()
